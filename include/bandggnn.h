@@ -22,7 +22,8 @@
  *   - Shapes: S (block size) in {32, 64, 128, 256, 512}; H (state size) a multiple of 32 in
  *     [32, 256]; P (edge types) in [1, 64].
  *   - dtype BG_BF16: states E, weights W, W_ih, W_hh are bf16 and accumulation is fp32.
- *     dtype BG_F32: all fp32.  Biases, messages Y and every gradient are fp32 for both dtypes.
+ *     dtype BG_F32: all fp32.  Biases, messages Y and every gradient are fp32 for both dtypes
+ *     (bg_xent_bwd can also write bf16 gradients).
  */
 #ifndef BANDGGNN_H_
 #define BANDGGNN_H_
@@ -310,6 +311,70 @@ int bg_readout_loss(const bg_plan* plan, bg_dtype dtype, int32_t H, const void* 
 int bg_adam_step(int64_t n, float* master, void* working, bg_dtype working_dtype, float* m,
                  float* v, const float* grad, float lr, float beta1, float beta2, float eps,
                  int32_t step, void* stream);
+
+/* ---- token operators (device) --------------------------------------------------------------
+ * The two ends of a model over token-labelled nodes: token ids become initial states, and final
+ * states are scored against a vocabulary; both can share one [V, H] table.  None needs a plan: rows
+ * are rows, in band order or in any other.  n up to 2^30 rows, V in [1, 2^24].  An id or target of V
+ * or more counts as negative (no row) and is reported by bg_check_device as BG_EDEVICE (site 130:
+ * an id; 131: a target).  n = 0 is valid everywhere.
+ *
+ * Dropout keeps no mask.  The elements of the (flat) array are numbered from 0; element i is dropped
+ * where its 16 random bits are below round(p 2^16), and kept elements are multiplied by
+ * 2^16 / (2^16 - round(p 2^16)).  The bits are those of Philox4x32 with 7 rounds (Salmon et al.,
+ * SC 2011): key = seed (low word first), counter = (i / 8, call) (64 bits each, low word first),
+ * element i has bits 16 (i % 2) .. 16 (i % 2) + 15 of output word (i % 8) / 2.  The same (seed, call)
+ * give the same mask, so the backward call passes its forward call's; a training step uses a `call`
+ * of its own for every dropout.  p in [0, 1]: 0 keeps everything as it is, 1 drops everything.  What
+ * stands in a dropped place is not used, infinities and NaN included.
+ *
+ * bg_dropout_fwd: y[i] = residual[i] + drop(x[i]) (residual may be NULL); x, residual, y: n elements
+ * of dtype, the sum is fp32 and is rounded once.  y may be x or residual.
+ * bg_dropout_bwd: dx[i] = drop(dy[i]) (fp32), added to dx with BG_ACCUM; dx may be dy without it.
+ * (The gradient of `residual` is dy itself.) */
+int bg_dropout_fwd(bg_dtype dtype, int64_t n, float p, int64_t seed, int64_t call, const void* x,
+                   const void* residual, void* y, void* stream);
+int bg_dropout_bwd(int64_t n, float p, int64_t seed, int64_t call, const float* dy, float* dx,
+                   uint32_t flags, void* stream);
+
+/* Embedding lookup: out[i] = drop(scale * table[ids[i]]), a zero row where ids[i] < 0 (padding
+ * rows).  ids [n] int32, table [V, H] dtype, out [n, H] dtype; the dropout numbers the elements of
+ * out. */
+int bg_embed_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const int32_t* ids,
+                 const void* table, float scale, float p, int64_t seed, int64_t call, void* out,
+                 void* stream);
+/* Scratch of bg_embed_bwd (0 for arguments out of range). */
+size_t bg_embed_workspace_bytes(int64_t n, int32_t H, int32_t V);
+/* Its gradient: dtable[v] = scale * sum over ids[i] = v of drop(dout[i]).  dout [n, H] fp32, dtable
+ * [V, H] fp32: every row is written (0 for tokens that do not occur), or, with BG_ACCUM, the rows of
+ * the tokens that occur are added to.  The rows are summed in the order of a stable sort by
+ * token: the same input gives the same bits. */
+int bg_embed_bwd(int64_t n, int32_t H, int32_t V, const int32_t* ids, const float* dout, float scale,
+                 float p, int64_t seed, int64_t call, float* dtable, uint32_t flags, void* ws,
+                 size_t ws_bytes, void* stream);
+
+/* Softmax cross entropy of states against the vocabulary, without ever storing the [n, V] logits
+ * z = X W^T:
+ *   lse[i] = log sum_v exp(z[i][v]),   loss[i] = lse[i] - z[i][target[i]].
+ * X [n, H] and W [V, H] dtype, target [n] int32, loss and lse [n] fp32.  A row with target[i] < 0 is
+ * left out: loss and lse are 0, its X is not used (it may hold anything). */
+#define BG_OP_XENT_FWD 5
+#define BG_OP_XENT_BWD 6
+/* Scratch of bg_xent_fwd / bg_xent_bwd (op); 0 for arguments out of range. */
+size_t bg_xent_workspace_bytes(bg_dtype dtype, int64_t n, int32_t H, int32_t V, int32_t op);
+int bg_xent_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
+                const int32_t* target, float* loss, float* lse, void* ws, size_t ws_bytes,
+                void* stream);
+/* Gradient of sum_i dloss[i] loss[i]; lse is bg_xent_fwd's of the same X, W and target:
+ *   dX[i] = dloss[i] (softmax(z[i]) - onehot(target[i])) W,
+ *   dW    = sum_i dloss[i] (softmax(z[i]) - onehot(target[i]))^T X[i].
+ * dloss [n] fp32 (not used in rows left out, whose dX is 0).  dX [n, H] and dW [V, H] in
+ * grad_dtype, either of them may be NULL (not computed).  grad_dtype BG_F32: probabilities enter the
+ * products with 22 bits, down to an absolute 2^-38 (times the largest |dloss|, for dW); BG_ACCUM adds to dX and dW instead of overwriting them.  grad_dtype BG_BF16
+ * (dtype BG_BF16 only, no BG_ACCUM): they enter rounded to bf16, as the results are. */
+int bg_xent_bwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
+                const int32_t* target, const float* lse, const float* dloss, bg_dtype grad_dtype,
+                void* dX, void* dW, uint32_t flags, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- diagnostics --------------------------------------------------------------------------- */
 const char* bg_last_error(void);

@@ -24,6 +24,7 @@ BG_FLOPS_BAND, BG_FLOPS_XFORM, BG_FLOPS_GRU, BG_FLOPS_NNZ = 0, 1, 2, 3
 (BG_EXPORT_PERM, BG_EXPORT_OFFSETS, BG_EXPORT_MASKS, BG_EXPORT_MASKS_T, BG_EXPORT_BW,
  BG_EXPORT_GATHER, BG_EXPORT_SUPER_EDGES, BG_EXPORT_SUPER_COUNT) = range(8)
 BG_OP_PROPAGATE_FWD, BG_OP_PROPAGATE_BWD, BG_OP_GGNN_FWD, BG_OP_GGNN_BWD, BG_OP_READOUT = range(5)
+BG_OP_XENT_FWD, BG_OP_XENT_BWD = 5, 6
 BG_KID_BAND_FWD, BG_KID_BAND_BWD, BG_KID_GRU_FWD, BG_KID_GRU_BWD, BG_KID_DW = range(5)
 STATUS = {0: "BG_OK", -1: "BG_EINVAL", -2: "BG_ECAPACITY", -3: "BG_ENOMEM", -4: "BG_ECUDA",
           -5: "BG_ETIMEOUT", -6: "BG_EDEVICE", -7: "BG_ESTATE"}
@@ -112,6 +113,16 @@ def load(path: str = LIB_PATH):
         "bg_band_uses_tensor_cores": (c.c_int, [vp, c.c_int, i32]),
         "bg_reach_filter": (c.c_int, [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]),
         "bg_plan_partition": (c.c_int, [vp, i32, i32, vp, vp]),
+        "bg_dropout_fwd": (c.c_int, [c.c_int, i64, f32, i64, i64, vp, vp, vp, vp]),
+        "bg_dropout_bwd": (c.c_int, [i64, f32, i64, i64, vp, vp, c.c_uint32, vp]),
+        "bg_embed_fwd": (c.c_int, [c.c_int, i64, i32, i32, vp, vp, f32, f32, i64, i64, vp, vp]),
+        "bg_embed_workspace_bytes": (sz, [i64, i32, i32]),
+        "bg_embed_bwd": (c.c_int, [i64, i32, i32, vp, vp, f32, f32, i64, i64, vp, c.c_uint32, vp, sz,
+                                   vp]),
+        "bg_xent_workspace_bytes": (sz, [c.c_int, i64, i32, i32, i32]),
+        "bg_xent_fwd": (c.c_int, [c.c_int, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "bg_xent_bwd": (c.c_int, [c.c_int, i64, i32, i32, vp, vp, vp, vp, vp, c.c_int, vp, vp,
+                                  c.c_uint32, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -364,6 +375,103 @@ def adam_step(master, working, m, v, grad, lr, beta1, beta2, eps, step, stream=N
                                _dev_ptr(working, "working"), wdt, _dev_ptr(m, "m"),
                                _dev_ptr(v, "v"), _dev_ptr(grad, "grad"), lr, beta1, beta2, eps,
                                step, _stream(stream)))
+
+
+# --------------------------------------------------------------------------------- token operators
+
+
+def _shaped(t, name, dtype, *shape):
+    """Device pointer of a contiguous CUDA tensor of this element type and shape (None passes)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
+    return _dev_ptr(t, name)
+
+
+def _elements(t, name, dtype, n):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements of {dtype}, not {t.numel()} of {t.dtype}")
+    return _dev_ptr(t, name)
+
+
+def _torch_dtype(code):
+    import torch
+    return torch.bfloat16 if code == BG_BF16 else torch.float32
+
+
+def dropout_fwd(dtype, x, y, p, seed, call, residual=None, stream=None):
+    """y = residual + drop(x) elementwise (tensors of `dtype` with equal element counts)."""
+    dt = dtype_code(dtype)
+    td, n = _torch_dtype(dt), x.numel()
+    _check(load().bg_dropout_fwd(dt, n, p, seed, call, _elements(x, "x", td, n),
+                                 _elements(residual, "residual", td, n),
+                                 _elements(y, "y", td, n), _stream(stream)))
+
+
+def dropout_bwd(dy, dx, p, seed, call, flags=0, stream=None):
+    """dx (+)= drop(dy) with the mask of the forward call of the same (p, seed, call); fp32."""
+    td, n = _torch_dtype(BG_F32), dy.numel()
+    _check(load().bg_dropout_bwd(n, p, seed, call, _elements(dy, "dy", td, n),
+                                 _elements(dx, "dx", td, n), flags, _stream(stream)))
+
+
+def embed_fwd(dtype, ids, table, out, scale=1.0, p=0.0, seed=0, call=0, stream=None):
+    """out[i] = drop(scale * table[ids[i]]), zero rows where ids[i] < 0; ids [n] int32."""
+    import torch
+    dt = dtype_code(dtype)
+    td, n, (V, H) = _torch_dtype(dt), ids.numel(), table.shape
+    _check(load().bg_embed_fwd(dt, n, H, V, _shaped(ids, "ids", torch.int32, n),
+                               _shaped(table, "table", td, V, H), scale, p, seed, call,
+                               _shaped(out, "out", td, n, H), _stream(stream)))
+
+
+def embed_workspace_bytes(n, H, V) -> int:
+    return int(load().bg_embed_workspace_bytes(n, H, V))
+
+
+def embed_bwd(ids, dout, dtable, ws, scale=1.0, p=0.0, seed=0, call=0, flags=0, stream=None):
+    """dtable[v] (+)= scale * sum over ids[i] = v of drop(dout[i]); fp32."""
+    import torch
+    n, (V, H) = ids.numel(), dtable.shape
+    _check(load().bg_embed_bwd(n, H, V, _shaped(ids, "ids", torch.int32, n),
+                               _shaped(dout, "dout", torch.float32, n, H), scale, p, seed, call,
+                               _shaped(dtable, "dtable", torch.float32, V, H), flags,
+                               _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
+                               _stream(stream)))
+
+
+def xent_workspace_bytes(dtype, n, H, V, op) -> int:
+    return int(load().bg_xent_workspace_bytes(dtype_code(dtype), n, H, V, op))
+
+
+def xent_fwd(dtype, X, W, target, loss, lse, ws, stream=None):
+    """loss[i] = lse[i] - X[i] . W[target[i]], lse[i] = log sum_v exp(X[i] . W[v]); 0 for rows with
+    target[i] < 0."""
+    import torch
+    dt = dtype_code(dtype)
+    td, n, (V, H) = _torch_dtype(dt), target.numel(), W.shape
+    _check(load().bg_xent_fwd(dt, n, H, V, _shaped(X, "X", td, n, H), _shaped(W, "W", td, V, H),
+                              _shaped(target, "target", torch.int32, n),
+                              _shaped(loss, "loss", torch.float32, n),
+                              _shaped(lse, "lse", torch.float32, n), _dev_ptr(ws, "ws"),
+                              ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def xent_bwd(dtype, X, W, target, lse, dloss, grad_dtype, dX, dW, ws, flags=0, stream=None):
+    """Gradients of sum_i dloss[i] loss[i] in grad_dtype; dX or dW may be None."""
+    import torch
+    dt, gt = dtype_code(dtype), dtype_code(grad_dtype)
+    td, gd, n, (V, H) = _torch_dtype(dt), _torch_dtype(gt), target.numel(), W.shape
+    _check(load().bg_xent_bwd(dt, n, H, V, _shaped(X, "X", td, n, H), _shaped(W, "W", td, V, H),
+                              _shaped(target, "target", torch.int32, n),
+                              _shaped(lse, "lse", torch.float32, n),
+                              _shaped(dloss, "dloss", torch.float32, n), gt,
+                              _shaped(dX, "dX", gd, n, H), _shaped(dW, "dW", gd, V, H), flags,
+                              _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
+                              _stream(stream)))
 
 
 def check_device(stream=None):

@@ -153,6 +153,8 @@ int status_word_ptr(int** out) {
 }
 }  // namespace
 
+int bg_status_word(int** out) { return status_word_ptr(out); }
+
 int* bg_status_word_if_created(int dev) {
   if (dev < 0 || dev >= 64) return nullptr;
   std::lock_guard<std::mutex> g(g_status_mu);

@@ -72,6 +72,8 @@ void bg_clear_error();
 // The device status word of device `dev` that bounded waits write and bg_check_device reads, or
 // NULL when it has not been created yet (api.cu; bg_plan_upload creates it).  Never allocates.
 int* bg_status_word_if_created(int dev);
+// The same for the current device, created on first use (one small allocation).
+int bg_status_word(int** out);
 // Device-side set-up of the allocation-free entry point for the current device (noalloc.cu):
 // resolves its static scratch array's address and loads the forward kernels of this plan's block
 // size.  Called by bg_plan_upload, which allocates anyway.

@@ -1,0 +1,525 @@
+"""GPU parity of the token operators (dropout, embedding, vocabulary cross entropy) against plain
+64-bit implementations, at the sizes, masks and values where they can go wrong.
+
+Every bound below is derived from the arithmetic the operators promise; u = 2^-24 is half the gap of
+fp32, and a result rounded to bf16 adds 2^-8 of itself.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import token_ref as ref
+from gpu_common import ensure_built
+from paper_1906_11786_gb300 import _binding as L
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = 2.0 ** -8  # rounding to bf16 (8 significant bits), relative
+TD = {"f32": torch.float32, "bf16": torch.bfloat16}
+SEED, CALL = 0x1906_1178_6000_0001, 0x7FFF_0000_1234
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    ensure_built()
+
+
+def dev(x, dtype):
+    return torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(TD[dtype]).cuda()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def within(got, want, tol, what=""):
+    """|got - want| <= tol element by element (tol an array or a number)."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert got.shape == want.shape
+    over = np.abs(got - want) - tol
+    assert np.all(np.isfinite(got)), f"{what}: not finite"
+    assert over.size == 0 or over.max() <= 0, \
+        f"{what}: {np.abs(got - want).flat[over.argmax()]:.3e} off at {over.argmax()}"
+
+
+# ------------------------------------------------------------------------------ dropout
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 255, 2048, 4097, 100003])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 1.0])
+def test_dropout(dtype, n, p):
+    rng = np.random.default_rng(n)
+    x, r = dev(rng.standard_normal(n), dtype), dev(rng.standard_normal(n), dtype)
+    for res in (None, r):
+        y = torch.full_like(x, float("nan"))
+        L.dropout_fwd(dtype, x, y, p, SEED, CALL, residual=res)
+        d = ref.drop(host(x), p, SEED, CALL)
+        want = d + (host(r) if res is not None else 0.0)
+        # the scale, its product and the sum: one rounding each
+        tol = 2 * U * np.abs(d) + U * np.abs(want) * 1.01
+        within(host(y), want, tol + (HALF * 1.01 * np.abs(want) if dtype == "bf16" else 0))
+    if dtype == "f32":
+        dx = x.clone()
+        L.dropout_bwd(r, dx, p, SEED, CALL, flags=L.BG_ACCUM)
+        d = ref.drop(host(r), p, SEED, CALL)
+        within(host(dx), host(x) + d, 2 * U * np.abs(d) + U * 1.01 * np.abs(host(x) + d))
+
+
+def test_dropout_keeps_the_stated_share():
+    """Kept elements are binomial: within 6 standard deviations of (1 - p) n for every p, and masks of
+    different calls agree as often as independent ones do."""
+    n = 1 << 20
+    x, y = torch.ones(n, device="cuda"), torch.empty(n, device="cuda")
+    for p in (0.1, 0.25, 0.5, 0.9):
+        L.dropout_fwd("f32", x, y, p, SEED, CALL)
+        share = 1 - round(p * 65536) / 65536
+        assert abs(int((y != 0).sum()) - share * n) < 6 * np.sqrt(n * share * (1 - share))
+    L.dropout_fwd("f32", x, y, 0.5, SEED, CALL)
+    z = torch.empty_like(y)
+    for seed, call in ((SEED + 1, CALL), (SEED, CALL + 1)):
+        L.dropout_fwd("f32", x, z, 0.5, seed, call)
+        assert abs(int(((y != 0) == (z != 0)).sum()) - n / 2) < 6 * np.sqrt(n / 4)
+
+
+def test_dropout_in_place_and_with_values_that_are_not_finite():
+    n, p = 1003, 0.5
+    k = ref.keep(0, n, p, SEED, CALL)
+    x = torch.where(torch.from_numpy(k).cuda(), torch.ones(n, device="cuda"),
+                    torch.full((n,), float("nan"), device="cuda"))
+    r = torch.arange(n, device="cuda", dtype=torch.float32)
+    y = r.clone()
+    L.dropout_fwd("f32", x, y, p, SEED, CALL, residual=y)  # y is the residual
+    assert torch.equal(y, r + 2.0 * torch.from_numpy(k).cuda())
+    L.dropout_fwd("f32", x, x, p, SEED, CALL)  # y is x
+    assert torch.equal(x, 2.0 * torch.from_numpy(k).cuda().float())
+    bad = torch.tensor([float("inf"), float("nan")] * 500, device="cuda")
+    out = torch.empty_like(bad)
+    L.dropout_fwd("f32", bad, out, 1.0, SEED, CALL)
+    assert torch.count_nonzero(out) == 0
+
+
+def test_dropout_past_32_bits_of_elements():
+    n = (1 << 32) + 11
+    x = torch.ones(n, device="cuda", dtype=torch.bfloat16)
+    L.dropout_fwd("bf16", x, x, 0.25, SEED, CALL)
+    for first in (0, (1 << 31) - 5, (1 << 32) - 5, n - 16):
+        got = (x[first:first + 16] != 0).cpu().numpy()
+        assert np.array_equal(got, ref.keep(first, len(got), 0.25, SEED, CALL))
+
+
+# ------------------------------------------------------------------------------ embedding
+
+
+def make_ids(rng, n, V, kind):
+    if kind == "uniform":
+        return rng.integers(0, V, n).astype(np.int32)
+    if kind == "one":  # every row the same token
+        return np.full(n, V // 2, np.int32)
+    if kind == "none":
+        return np.full(n, -1, np.int32)
+    w = 1.0 / np.arange(2, V + 2)  # frequent and rare tokens, every fifth row padding
+    ids = rng.choice(V, n, p=w / w.sum()).astype(np.int32)
+    ids[rng.random(n) < 0.2] = -1
+    return ids
+
+
+EMBED = [(1, 32, 1, "uniform"), (2, 64, 2, "uniform"), (31, 96, 3, "zipf"), (33, 256, 40, "one"),
+         (512, 64, 1000, "zipf"), (2047, 160, 511, "zipf"), (2049, 128, 512, "uniform"),
+         (5000, 224, 513, "zipf"), (4100, 64, 70000, "uniform"), (9000, 32, 300000, "zipf"),
+         (70001, 32, 17, "zipf"), (20000, 256, 30, "one"), (100, 64, 50, "none")]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,H,V,kind", EMBED)
+def test_embed_fwd(dtype, n, H, V, kind):
+    rng = np.random.default_rng(n + H)
+    ids = make_ids(rng, n, V, kind)
+    table, scale = dev(rng.standard_normal((V, H)), dtype), 1.7
+    for p in (0.0, 0.3):
+        out = torch.full((n, H), float("nan"), device="cuda", dtype=TD[dtype])
+        L.embed_fwd(dtype, torch.from_numpy(ids).cuda(), table, out, scale=scale, p=p, seed=SEED,
+                    call=CALL)
+        want = ref.embed_fwd(ids, host(table), float(np.float32(scale)), p, SEED, CALL)
+        # scale * kept scale (rounded), two products
+        tol = 3.01 * U * np.abs(want) + (1.01 * HALF * np.abs(want) if dtype == "bf16" else 0)
+        within(host(out), want, tol)
+
+
+@pytest.mark.parametrize("n,H,V,kind", EMBED)
+def test_embed_bwd(n, H, V, kind):
+    rng = np.random.default_rng(n + H)
+    ids = make_ids(rng, n, V, kind)
+    dout, scale = rng.standard_normal((n, H)).astype(np.float32), 0.6
+    dout[ids < 0] = np.nan  # padding rows are not read
+    d_ids, d_out = torch.from_numpy(ids).cuda(), torch.from_numpy(dout).cuda()
+    ws = torch.empty(L.embed_workspace_bytes(n, H, V), device="cuda", dtype=torch.uint8)
+    for p in (0.0, 0.3):
+        want, mag, count = ref.embed_bwd(ids, np.nan_to_num(dout), V, float(np.float32(scale)), p,
+                                         SEED, CALL)
+        # a sum of `count` terms in fp32, its scale and the product
+        tol = (count[:, None] + 3) * U * mag
+        got = torch.full((V, H), float("nan"), device="cuda")
+        ws.fill_(0xA5)
+        L.embed_bwd(d_ids, d_out, got, ws, scale=scale, p=p, seed=SEED, call=CALL)
+        within(host(got), want, tol)
+        again = torch.full((V, H), float("nan"), device="cuda")
+        ws.fill_(0x5A)
+        L.embed_bwd(d_ids, d_out, again, ws, scale=scale, p=p, seed=SEED, call=CALL)
+        assert torch.equal(got, again), "the sum's order is fixed"
+        base = torch.from_numpy(rng.standard_normal((V, H)).astype(np.float32)).cuda()
+        acc = base.clone()
+        L.embed_bwd(d_ids, d_out, acc, ws, scale=scale, p=p, seed=SEED, call=CALL, flags=L.BG_ACCUM)
+        assert torch.equal(acc, base + got), "BG_ACCUM adds the finished sum"
+
+
+def test_embed_gradient_is_the_adjoint():
+    """<embed(D), G> = <D, embed_bwd(G)>: the lookup is linear in its table, so differences of it are
+    the lookup itself.  Both sides are sums of n H products of fp32 values with a few roundings each."""
+    n, H, V, p = 3001, 64, 257, 0.25
+    rng = np.random.default_rng(5)
+    ids = torch.from_numpy(make_ids(rng, n, V, "zipf")).cuda()
+    D = torch.from_numpy(rng.standard_normal((V, H)).astype(np.float32)).cuda()
+    G = torch.from_numpy(rng.standard_normal((n, H)).astype(np.float32)).cuda()
+    out, dD = torch.empty(n, H, device="cuda"), torch.empty(V, H, device="cuda")
+    ws = torch.empty(L.embed_workspace_bytes(n, H, V), device="cuda", dtype=torch.uint8)
+    L.embed_fwd("f32", ids, D, out, scale=1.5, p=p, seed=SEED, call=CALL)
+    L.embed_bwd(ids, G, dD, ws, scale=1.5, p=p, seed=SEED, call=CALL)
+    a, b = float((out.double() * G).sum()), float((D.double() * dD).sum())
+    mag = float((out.double() * G).abs().sum())
+    assert abs(a - b) <= (n + 8) * U * mag
+
+
+def test_embed_reports_ids_past_the_table():
+    L.check_device()
+    ids = torch.tensor([3, 9, 10, 2 ** 31 - 1, -7, 0], device="cuda", dtype=torch.int32)
+    table = torch.arange(640, device="cuda", dtype=torch.float32).reshape(10, 64) + 1
+    out = torch.full((6, 64), float("nan"), device="cuda")
+    L.embed_fwd("f32", ids, table, out)
+    with pytest.raises(L.BandGGNNError, match="site 130"):
+        L.check_device()
+    L.check_device()
+    assert torch.equal(out[[0, 1, 5]], table[[3, 9, 0]]) and torch.count_nonzero(out[2:5]) == 0
+    d = torch.full((10, 64), float("nan"), device="cuda")
+    ws = torch.empty(L.embed_workspace_bytes(6, 64, 10), device="cuda", dtype=torch.uint8)
+    L.embed_bwd(ids, torch.ones(6, 64, device="cuda"), d, ws)
+    with pytest.raises(L.BandGGNNError, match="site 130"):
+        L.check_device()
+    want = torch.zeros(10, 64, device="cuda")
+    want[[3, 9, 0]] = 1
+    assert torch.equal(d, want)
+
+
+def test_embed_of_no_rows():
+    d = torch.full((7, 64), float("nan"), device="cuda")
+    none = torch.empty(0, device="cuda", dtype=torch.int32)
+    ws = torch.empty(L.embed_workspace_bytes(0, 64, 7), device="cuda", dtype=torch.uint8)
+    L.embed_bwd(none, torch.empty(0, 64, device="cuda"), d, ws, flags=L.BG_ACCUM)
+    assert torch.isnan(d).all()
+    L.embed_bwd(none, torch.empty(0, 64, device="cuda"), d, ws)
+    assert torch.count_nonzero(d) == 0
+
+
+def test_embed_past_32_bits_of_elements():
+    """n H just over 2^31: the last rows' offsets need 64 bits, forward and backward."""
+    n, H, V = (1 << 23) + 5, 256, 3
+    ids = torch.full((n,), -1, device="cuda", dtype=torch.int32)
+    ids[-4:] = torch.tensor([0, 2, 1, 2], device="cuda", dtype=torch.int32)
+    table = torch.arange(V * H, device="cuda", dtype=torch.float32).reshape(V, H)
+    out = torch.empty(n, H, device="cuda")
+    L.embed_fwd("f32", ids, table, out)
+    assert torch.equal(out[-4:], table[[0, 2, 1, 2]]) and torch.count_nonzero(out[:-4]) == 0
+    d = torch.empty(V, H, device="cuda")
+    ws = torch.empty(L.embed_workspace_bytes(n, H, V), device="cuda", dtype=torch.uint8)
+    L.embed_bwd(ids, out, d, ws)
+    assert torch.equal(d, table * torch.tensor([1.0, 1.0, 2.0], device="cuda")[:, None])
+
+
+# ------------------------------------------------------------------------------ cross entropy
+
+
+def xent_inputs(n, H, V, dtype, share=1.0, zscale=2.0, seed=0):
+    rng = np.random.default_rng(seed + n + H + V)
+    W = rng.standard_normal((V, H)) * zscale / np.sqrt(H)
+    target = rng.integers(0, V, n).astype(np.int32)
+    X = rng.standard_normal((n, H)) + rng.random((n, 1)) * 2 * W[target]
+    target[rng.random(n) >= share] = -1
+    g = (0.5 + rng.random(n)).astype(np.float32) / max(n, 1)
+    return dev(X, dtype), dev(W, dtype), target, g
+
+
+def run_xent(dtype, X, W, target, g, grad, flags=0, into=None):
+    n, (V, H) = target.size, W.shape
+    t, gd = torch.from_numpy(target).cuda(), torch.from_numpy(g).cuda()
+    loss, lse = (torch.full((n,), float("nan"), device="cuda") for _ in range(2))
+    need = max(L.xent_workspace_bytes(dtype, n, H, V, op) for op in (L.BG_OP_XENT_FWD,
+                                                                   L.BG_OP_XENT_BWD))
+    ws = torch.full((need,), 0xA5, device="cuda", dtype=torch.uint8)
+    L.xent_fwd(dtype, X, W, t, loss, lse, ws)
+    dX, dW = into or (torch.full((m, H), float("nan"), device="cuda", dtype=TD[grad])
+                      for m in (n, V))
+    ws.fill_(0x5A)
+    L.xent_bwd(dtype, X, W, t, lse, gd, grad, dX, dW, ws, flags=flags)
+    return loss, lse, dX, dW
+
+
+def xent_bounds(r, n, H, V, grad):
+    """Element bounds.  A logit: H products to 21 bits or better, added in fp32 (at most H u of their
+    magnitude, the tensor core's truncating adds included as 2 u each).  exp and log: 2^-20 of
+    themselves, of arguments that carry the logits' error.  A gradient element: each term is off by
+    the error of its probability and of its representation in the product (2^-19, and in bf16 twice
+    2^-8: the probability's rounding and the result's), and the sums add V u or n u of the terms'
+    magnitude.  A probability keeps its bits down to an absolute 2^-38 (for dW: of the largest weight),
+    below which it may be lost, as everything below 2^-126 is."""
+    dz = (2 * H * U + 2.0 ** -21) * r["zabs"]
+    loss = 2 * dz + 2.0 ** -20 * (1 + np.abs(r["lse"]))
+    term = 2 * dz + 2.0 ** -19 + (2.0 ** -7 if grad == "bf16" else 0)
+    bX = (term + 2 * V * U) * r["absX"] + 2.0 ** -38 * r["allX"] + 2.0 ** -126
+    bW = (term + 2 * n * U) * r["absW"] + 2.0 ** -38 * r["allW"] + 2.0 ** -126
+    return loss, bX, bW
+
+
+def rel2(got, want):
+    """2-norm of the difference over that of the result."""
+    return float(np.linalg.norm(host(got) - want) / max(np.linalg.norm(want), 1e-300))
+
+
+def check_xent(dtype, grad, X, W, target, g, share_used=None):
+    n, (V, H) = target.size, W.shape
+    got = run_xent(dtype, X, W, target, g, grad)
+    r = ref.xent(host(X), host(W), target, g)
+    loss, bX, bW = xent_bounds(r, n, H, V, grad)
+    used = (target >= 0) & (target < V)
+    within(host(got[1]), r["lse"], loss * used, "lse")
+    within(host(got[0]), r["loss"], loss * used, "loss")
+    within(host(got[2]), r["dX"], bX, "dX")
+    within(host(got[3]), r["dW"], bW, "dW")
+    # over all elements roundings average out: 2^-16 of the norm in fp32, where it is not small by
+    # cancellation, and 2^-8 in bf16
+    if V > 1 and used.any():
+        lim = 2.0 ** -8 if grad == "bf16" else 2.0 ** -16
+        assert rel2(got[2], r["dX"]) < lim and rel2(got[3], r["dW"]) < lim
+    return got
+
+
+TYPES = [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")]
+XENT = [(1, 32, 1, 1.0), (1, 64, 2, 1.0), (2, 128, 1000, 1.0), (1, 256, 4099, 1.0),
+        (63, 96, 65, 1.0), (127, 64, 127, 0.5), (128, 160, 128, 1.0), (129, 192, 257, 0.7),
+        (300, 224, 513, 0.15), (513, 256, 1023, 1.0), (1000, 32, 3001, 1.0), (2500, 64, 400, 0.15),
+        (4097, 128, 130, 1.0), (700, 256, 2049, 0.02)]
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+@pytest.mark.parametrize("n,H,V,share", XENT)
+def test_xent(dtype, grad, n, H, V, share):
+    check_xent(dtype, grad, *xent_inputs(n, H, V, dtype, share))
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_xent_of_larger_shapes(dtype, grad):
+    """Several tiles a block in both directions, every row of each side checked."""
+    check_xent(dtype, grad, *xent_inputs(9001, 64, 6007, dtype, 0.9))
+    check_xent(dtype, grad, *xent_inputs(3001, 256, 9001, dtype, 0.9))
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_xent_of_confident_and_of_wrong_rows(dtype, grad):
+    """Logits in the hundreds: softmax is all but one-hot, right or wrong, and nothing overflows."""
+    X, W, target, g = xent_inputs(260, 64, 301, dtype, 1.0, zscale=40.0)
+    check = host(X) @ host(W).T
+    assert np.abs(check).max() > 300
+    got = run_xent(dtype, X, W, target, g, grad)
+    r = ref.xent(host(X), host(W), target, g)
+    loss, bX, bW = xent_bounds(r, 260, 64, 301, grad)
+    for t, w, b in zip(got, (r["loss"], r["lse"], r["dX"], r["dW"]), (loss, loss, bX, bW)):
+        within(host(t), w, b)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_xent_rows_left_out_may_hold_anything(dtype, grad):
+    X, W, target, g = xent_inputs(333, 96, 210, dtype, 0.4)
+    out = torch.from_numpy(target < 0).cuda()
+    a = run_xent(dtype, X, W, target, g, grad)
+    X[out] = float("nan")
+    X[torch.nonzero(out)[::3, 0]] = float("inf")
+    g = np.where(target < 0, np.float32("nan"), g)
+    b = run_xent(dtype, X, W, target, g, grad)
+    for u, v in zip(a, b):
+        assert torch.equal(u, v)
+    for u in a[:3]:
+        assert torch.count_nonzero(u[out]) == 0
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_xent_with_no_row_left(dtype, grad):
+    X, W, target, g = xent_inputs(200, 64, 150, dtype)
+    target[:] = -1
+    for t in run_xent(dtype, X, W, target, g, grad):
+        assert torch.count_nonzero(t) == 0
+    # and with no rows at all
+    none = np.zeros(0, np.int32)
+    for t in run_xent(dtype, X[:0], W, none, np.zeros(0, np.float32), grad):
+        assert torch.count_nonzero(t) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_xent_accumulates_and_skips_what_is_not_asked(dtype):
+    X, W, target, g = xent_inputs(190, 128, 140, dtype, 0.8)
+    _, lse, dX, dW = run_xent(dtype, X, W, target, g, "f32")
+    bX, bW = torch.randn_like(dX), torch.randn_like(dW)
+    aX, aW = bX.clone(), bW.clone()
+    run_xent(dtype, X, W, target, g, "f32", flags=L.BG_ACCUM, into=(aX, aW))
+    # one more rounding of the sum, in either order
+    assert (aX - (bX + dX)).abs().max() <= 4 * U * (bX.abs() + dX.abs()).max()
+    assert (aW - (bW + dW)).abs().max() <= 4 * U * (bW.abs() + dW.abs()).max()
+    t, gd = torch.from_numpy(target).cuda(), torch.from_numpy(g).cuda()
+    ws = torch.empty(L.xent_workspace_bytes(dtype, 190, 128, 140, L.BG_OP_XENT_BWD), device="cuda",
+                     dtype=torch.uint8)
+    oX, oW = torch.empty_like(dX), torch.empty_like(dW)
+    L.xent_bwd(dtype, X, W, t, lse, gd, "f32", oX, None, ws)
+    L.xent_bwd(dtype, X, W, t, lse, gd, "f32", None, oW, ws)
+    assert torch.equal(oX, dX) and torch.equal(oW, dW)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_xent_gives_the_same_bits_again(dtype, grad):
+    args = xent_inputs(3000, 64, 2000, dtype, 0.9)
+    a, b = (run_xent(dtype, *args, grad) for _ in range(2))
+    for u, v in zip(a, b):
+        assert torch.equal(u, v)
+
+
+def test_xent_reports_targets_past_the_vocabulary():
+    X, W, target, g = xent_inputs(150, 64, 90, "bf16")
+    target[[3, 140]] = [90, 2 ** 31 - 1]
+    L.check_device()
+    got = run_xent("bf16", X, W, target, g, "f32")
+    with pytest.raises(L.BandGGNNError, match="site 131"):
+        L.check_device()
+    target[[3, 140]] = -1
+    for u, v in zip(got, run_xent("bf16", X, W, target, g, "f32")):
+        assert torch.equal(u, v)
+    L.check_device()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** 50])
+def test_xent_of_small_and_large_values(scale):
+    """X small and W large by the same power of two, or the other way round: the logits are the same
+    bits, dX and dW scale by it."""
+    X, W, target, g = xent_inputs(140, 64, 300, "f32")
+    a = run_xent("f32", X, W, target, g, "f32")
+    b = run_xent("f32", X * scale, W / scale, target, g, "f32")
+    r = ref.xent(host(X), host(W), target, g)
+    loss, bX, bW = xent_bounds(r, 140, 64, 300, "f32")
+    within(host(b[0]), r["loss"], loss)
+    within(host(b[2]) * scale, r["dX"], bX)
+    within(host(b[3]) / scale, r["dW"], bW)
+    for u, v in zip(a[:2], b[:2]):
+        assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_xent_gradient_against_differences(dtype):
+    """Directional differences of the forward itself, over states and table.  With step e along a
+    direction whose logits move by at most m, the central difference is off by e^2 m^3 / 6 of the
+    weights' sum, and by the loss's rounding over e."""
+    n, H, V = 96, 64, 200
+    X, W, target, g = xent_inputs(n, H, V, dtype)
+    rng = np.random.default_rng(3)
+    r = ref.xent(host(X), host(W), target, g)
+    _, _, dX, dW = run_xent(dtype, X, W, target, g, "f32")
+    # differences are taken in fp32 on the values the gradient was taken at
+    Xf, Wf = X.float(), W.float()
+    for which, d in (("X", dX), ("W", dW)):
+        D = rng.standard_normal(tuple(d.shape))
+        Dd = dev(D, "f32")
+        move = host(Dd) @ host(Wf).T if which == "X" else host(Xf) @ host(Dd).T
+        m = 2 * np.abs(move).max()
+        e = 0.02 / m
+        f = []
+        for s in (e, -e):
+            args = (Xf + s * Dd, Wf) if which == "X" else (Xf, Wf + s * Dd)
+            f.append(float((host(run_xent("f32", *args, target, g, "f32")[0]) * g).sum()))
+        got = float((host(d) * host(Dd)).sum())
+        want = (f[0] - f[1]) / (2 * e)
+        loss, bX, bW = xent_bounds(r, n, H, V, "f32")
+        # X + e D itself is rounded to fp32: a logit moves by u of its magnitude
+        tol = g.sum() * ((e * m) ** 2 * m / 6 + (loss.max() + 2 * U * r["zabs"]) / e)
+        assert abs(got - want) <= tol, (which, got, want, tol)
+
+
+def test_xent_past_32_bits_of_elements():
+    """n H just over 2^31 with few labelled rows, the last ones among them."""
+    n, H, V = (1 << 23) + 70, 256, 5
+    X = torch.zeros(n, H, device="cuda", dtype=torch.bfloat16)
+    target = np.full(n, -1, np.int32)
+    at = np.array([0, 5, 1 << 20, (1 << 23) - 1, n - 2, n - 1])
+    target[at] = [0, 4, 2, 3, 1, 0]
+    small, W, _, _ = xent_inputs(6, H, V, "bf16")
+    X[torch.from_numpy(at).cuda()] = small
+    g = np.ones(n, np.float32)
+    loss, lse, dX, dW = run_xent("bf16", X, W, target, g, "bf16")
+    r = ref.xent(host(small), host(W), target[at], g[at])
+    b, bX, bW = xent_bounds(r, 6, H, V, "bf16")
+    pick = torch.from_numpy(at).cuda()
+    within(host(loss[pick]), r["loss"], b)
+    within(host(dX[pick]), r["dX"], bX)
+    within(host(dW), r["dW"], bW)
+    assert int(torch.count_nonzero(loss)) == int(np.count_nonzero(host(loss[pick])))
+    dX[pick] = 0
+    assert torch.count_nonzero(dX) == 0
+
+
+# ------------------------------------------------------------------------------ streams
+
+
+def test_token_operators_run_on_the_stream_they_are_given():
+    """Inputs made on a side stream, operators given that stream, results read after it alone; and the
+    same calls captured in a CUDA graph and replayed on new values."""
+    n, H, V = 700, 64, 333
+    X, W, target, g = xent_inputs(n, H, V, "bf16", 0.8)
+    want = run_xent("bf16", X, W, target, g, "f32")
+    st = torch.cuda.Stream()
+    t, gd = torch.from_numpy(target).cuda(), torch.from_numpy(g).cuda()
+    ws = torch.empty(max(L.xent_workspace_bytes("bf16", n, H, V, op)
+                         for op in (L.BG_OP_XENT_FWD, L.BG_OP_XENT_BWD)), device="cuda",
+                     dtype=torch.uint8)
+    ews = torch.empty(L.embed_workspace_bytes(n, H, V), device="cuda", dtype=torch.uint8)
+    x2 = torch.zeros_like(X)
+    outs = [torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"),
+            torch.zeros(n, H, device="cuda"), torch.zeros(V, H, device="cuda")]
+    dE = torch.zeros(V, H, device="cuda")
+
+    def calls(stream):
+        L.dropout_fwd("bf16", x2, x2, 0.0, SEED, CALL, stream=stream)
+        L.xent_fwd("bf16", x2, W, t, outs[0], outs[1], ws, stream=stream)
+        L.xent_bwd("bf16", x2, W, t, outs[1], gd, "f32", outs[2], outs[3], ws, stream=stream)
+        L.embed_bwd(t, outs[2], dE, ews, stream=stream)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        x2.copy_(X)
+    calls(st)
+    st.synchronize()
+    for u, v in zip(outs, want):
+        assert torch.equal(u, v)
+    first = dE.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        calls(None)
+    for o in outs + [dE]:
+        o.zero_()
+    x2.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.count_nonzero(outs[2]) and not torch.equal(outs[2], want[2])
+    x2.copy_(X)
+    graph.replay()
+    torch.cuda.synchronize()
+    for u, v in zip(outs, want):
+        assert torch.equal(u, v)
+    assert torch.equal(dE, first)

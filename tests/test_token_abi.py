@@ -1,0 +1,122 @@
+"""Token operators without a GPU: the generator's published test vectors, refusals, sizes."""
+from __future__ import annotations
+
+import pytest
+import token_ref as ref
+
+from paper_1906_11786_gb300 import _binding as L
+from paper_1906_11786_gb300 import build as B
+
+LOW = ref.LOW
+P16 = 1 << 20  # an aligned address that is never read
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    B.build()
+    return L.load()
+
+
+def test_reference_generator_matches_the_published_vectors():
+    """The known answers that Random123 (Salmon et al.) gives for 7 rounds."""
+    want = {(0, 0): "5f6fb709 0d893f64 4f121f81 4f730a48",
+            (LOW, LOW): "5207ddc2 45165e59 4d8ee751 8c52f662"}
+    for (c, k), words in want.items():
+        got = ref.philox_scalar([c] * 4, [k] * 2)
+        assert " ".join(f"{w:08x}" for w in got) == words
+
+
+def test_reference_mask_numbers_elements_as_stated():
+    seed, call, p = 0x0123456789ABCDEF, 0x7EDCBA9876543210, 0.375
+    got = ref.keep(3, 50, p, seed, call)
+    for j in range(50):
+        i = 3 + j
+        w = ref.philox_scalar([i // 8 & LOW, i // 8 >> 32, call & LOW, call >> 32],
+                              [seed & LOW, seed >> 32])
+        bits = (w[(i % 8) // 2] >> (16 * (i % 2))) & 0xFFFF
+        assert got[j] == (bits >= 24576)
+
+
+def _refused(rc, word, code=-1):
+    assert rc == code, rc
+    assert word in L.load().bg_last_error().decode()
+
+
+@pytest.mark.parametrize("p", [-0.1, 1.5, float("nan")])
+def test_probability_out_of_range_is_refused(lib, p):
+    a = P16
+    _refused(lib.bg_dropout_fwd(L.BG_F32, 8, p, 0, 0, a, None, a, None), "p must")
+    _refused(lib.bg_dropout_bwd(8, p, 0, 0, a, a, 0, None), "p must")
+    _refused(lib.bg_embed_fwd(L.BG_F32, 8, 64, 9, a, a, 1.0, p, 0, 0, a, None), "p must")
+    _refused(lib.bg_embed_bwd(8, 64, 9, a, a, 1.0, p, 0, 0, a, 0, a, 1 << 30, None), "p must")
+
+
+@pytest.mark.parametrize("n,H,V,word", [(-1, 64, 9, "n must"), ((1 << 30) + 1, 64, 9, "n must"),
+                                        (8, 48, 9, "H must"), (8, 0, 9, "H must"),
+                                        (8, 288, 9, "H must"), (8, 64, 0, "V must"),
+                                        (8, 64, (1 << 24) + 1, "V must")])
+def test_shapes_out_of_range_are_refused(lib, n, H, V, word):
+    a = P16
+    _refused(lib.bg_embed_fwd(L.BG_F32, n, H, V, a, a, 1.0, 0.0, 0, 0, a, None), word)
+    _refused(lib.bg_embed_bwd(n, H, V, a, a, 1.0, 0.0, 0, 0, a, 0, a, 1 << 40, None), word)
+    _refused(lib.bg_xent_fwd(L.BG_F32, n, H, V, a, a, a, a, a, a, 1 << 40, None), word)
+    _refused(lib.bg_xent_bwd(L.BG_F32, n, H, V, a, a, a, a, a, L.BG_F32, a, a, 0, a, 1 << 40, None),
+             word)
+    assert lib.bg_embed_workspace_bytes(n, H, V) == 0
+    assert lib.bg_xent_workspace_bytes(L.BG_BF16, n, H, V, L.BG_OP_XENT_FWD) == 0
+
+
+def test_pointers_types_and_flags_are_checked(lib):
+    a, odd = P16, P16 + 8
+    _refused(lib.bg_dropout_fwd(7, 8, 0.1, 0, 0, a, None, a, None), "dtype")
+    _refused(lib.bg_dropout_fwd(L.BG_F32, -1, 0.1, 0, 0, a, None, a, None), "n < 0")
+    _refused(lib.bg_dropout_fwd(L.BG_F32, 8, 0.1, 0, 0, None, None, a, None), "x is NULL")
+    _refused(lib.bg_dropout_fwd(L.BG_F32, 8, 0.1, 0, 0, a, odd, a, None), "residual not 16-byte")
+    _refused(lib.bg_dropout_bwd(8, 0.1, 0, 0, a, a, L.BG_ACCUM, None), "BG_ACCUM")
+    _refused(lib.bg_dropout_bwd(8, 0.1, 0, 0, a, a, 4, None), "flags")
+    _refused(lib.bg_embed_fwd(5, 8, 64, 9, a, a, 1.0, 0.0, 0, 0, a, None), "dtype")
+    _refused(lib.bg_embed_fwd(L.BG_F32, 8, 64, 9, a, odd, 1.0, 0.0, 0, 0, a, None), "table not")
+    _refused(lib.bg_embed_bwd(8, 64, 9, a, a, 1.0, 0.0, 0, 0, a, 2, a, 1 << 30, None), "flags")
+    _refused(lib.bg_embed_bwd(8, 64, 9, a, a, 1.0, 0.0, 0, 0, a, 0, a, 16, None), "workspace",
+             code=-2)
+    need = lib.bg_xent_workspace_bytes(L.BG_F32, 8, 64, 9, L.BG_OP_XENT_FWD)
+    _refused(lib.bg_xent_fwd(L.BG_F32, 8, 64, 9, a, a, a, a, a, a, need - 1, None), "workspace",
+             code=-2)
+    _refused(lib.bg_xent_fwd(L.BG_F32, 8, 64, 9, a, None, a, a, a, a, 1 << 30, None), "W is NULL")
+    big = 1 << 40
+    bwd = lib.bg_xent_bwd
+    _refused(bwd(L.BG_F32, 8, 64, 9, a, a, a, a, a, L.BG_BF16, a, a, 0, a, big, None), "fp32")
+    _refused(bwd(L.BG_BF16, 8, 64, 9, a, a, a, a, a, L.BG_BF16, a, a, 1, a, big, None), "BG_ACCUM")
+    _refused(bwd(L.BG_BF16, 8, 64, 9, a, a, a, a, a, L.BG_F32, None, None, 0, a, big, None), "dX and")
+    _refused(bwd(L.BG_BF16, 8, 64, 9, a, a, a, a, a, 3, a, a, 0, a, big, None), "dtype")
+    assert lib.bg_xent_workspace_bytes(L.BG_F32, 8, 64, 9, L.BG_OP_READOUT) == 0
+
+
+def test_nothing_to_do_is_done_without_a_device(lib):
+    assert lib.bg_dropout_fwd(L.BG_BF16, 0, 0.5, 1, 2, None, None, None, None) == 0
+    assert lib.bg_dropout_bwd(0, 0.5, 1, 2, None, None, 0, None) == 0
+    assert lib.bg_embed_fwd(L.BG_BF16, 0, 64, 9, None, None, 1.0, 0.0, 0, 0, None, None) == 0
+    assert lib.bg_xent_fwd(L.BG_BF16, 0, 64, 9, None, P16, None, None, None, None, 0, None) == 0
+
+
+def test_binding_checks_types_and_shapes():
+    import torch
+    x = torch.zeros(8)
+    with pytest.raises(ValueError, match="x must have"):
+        L.dropout_fwd("bf16", x, x, 0.1, 0, 0)
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        L.dropout_fwd("f32", x, x, 0.1, 0, 0)
+    with pytest.raises(ValueError, match="ids must be"):
+        L.embed_fwd("f32", torch.zeros(3), torch.zeros(5, 64), torch.zeros(3, 64))
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        L.embed_bwd(torch.zeros(0, dtype=torch.int32), torch.zeros(4, 64), torch.zeros(5, 64), x)
+
+
+def test_workspaces_grow_with_the_work(lib):
+    assert 0 < lib.bg_embed_workspace_bytes(0, 64, 9)
+    assert lib.bg_embed_workspace_bytes(1000, 64, 9) < lib.bg_embed_workspace_bytes(100000, 64, 9)
+    # nothing in them grows with n x V
+    n, H, V = 1 << 20, 256, 1 << 20
+    for dt in (L.BG_F32, L.BG_BF16):
+        for op in (L.BG_OP_XENT_FWD, L.BG_OP_XENT_BWD):
+            assert 0 < lib.bg_xent_workspace_bytes(dt, n, H, V, op) < 64 * H * (n + V)
