@@ -315,7 +315,7 @@ int bg_adam_step(int64_t n, float* master, void* working, bg_dtype working_dtype
 /* ---- token operators (device) --------------------------------------------------------------
  * The two ends of a model over token-labelled nodes: token ids become initial states, and final
  * states are scored against a vocabulary; both can share one [V, H] table.  None needs a plan: rows
- * are rows, in band order or in any other.  n up to 2^30 rows, V in [1, 2^24].  An id or target of V
+ * are rows, in band order or in any other.  n up to 2^29 rows, V in [1, 2^24].  An id or target of V
  * or more counts as negative (no row) and is reported by bg_check_device as BG_EDEVICE (site 130:
  * an id; 131: a target).  n = 0 is valid everywhere.
  *

@@ -34,11 +34,11 @@ int check_dtype(bg_dtype dt) {
   return dt == BG_F32 || dt == BG_BF16 ? BG_OK : bg_fail(BG_EINVAL, "unknown dtype");
 }
 
-constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxRows = (int64_t)1 << 29;
 constexpr int32_t kMaxVocab = 1 << 24;
 
 int check_shape(int64_t n, int32_t H, int32_t V) {
-  if (n < 0 || n > kMaxRows) return bg_fail(BG_EINVAL, "n must be in [0, 2^30]");
+  if (n < 0 || n > kMaxRows) return bg_fail(BG_EINVAL, "n must be in [0, 2^29]");
   if (H < 32 || H > 256 || H % 32) return bg_fail(BG_EINVAL, "H must be a multiple of 32 in [32, 256]");
   if (V < 1 || V > kMaxVocab) return bg_fail(BG_EINVAL, "V must be in [1, 2^24]");
   return BG_OK;

@@ -2,224 +2,1389 @@
 // gradient; the [n, V] logits are never in memory:
 //   z = X W^T,  lse_i = log sum_v exp(z_iv),  loss_i = lse_i - z_{i,t_i}
 //   P = softmax(z) - onehot(t),  dX = diag(g) P W,  dW = P^T diag(g) X     (g: the loss's gradient)
-// A block keeps 64 rows of one side (X for the loss and dX, W for dW), walks the other side 64 rows
-// at a time and recomputes the 64 x 64 logits between them; the gradients take exp(z - lse) from the
-// forward's lse.  Everything is fp32 in shared memory and registers.
+//
+// Three kinds of kernels:
+//   k_xent_count, k_xent_rows   the labelled rows of X, gathered side by side (rows left out cost
+//                               nothing after this and may hold anything), and the operands' 16-bit forms
+//   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, running maximum and sum
+//   k_xent_bwd (+ join)         128 x 128 tiles of z recomputed, P written back over z in tensor
+//                               memory as the A operand of the second product; once with the rows of X
+//                               staying (dX) and once with the rows of W (dW)
+// A staying tile of 128 rows against one passing tile is a unit; the units of a launch, staying tile
+// by staying tile, are cut into as many equal runs as there are SMs, so one row or a hundred thousand
+// fill the card alike.  A staying tile whose units fall to several CTAs leaves partial results, which
+// the join adds in the order of the CTAs.  The number of labelled rows is known on the device only:
+// every kernel derives its runs from it.
+//
+// Number formats ("forms") of the operands:
+//   bf16           X and W as they are; P rounded to bf16 (bf16 gradients, whose own rounding is as large)
+//   fp16, 1 term   bf16 X and W with fp32 gradients: scaled by a power of two, they are exact in
+//                  fp16 (down to 2^-29 of the largest), and P, as the sum of two fp16 terms, keeps 22 bits;
+//                  fp16 and bf16 operands cannot be mixed in one product
+//   fp16, 2 terms  fp32 X and W, each the sum of two fp16 terms (22 bits); products of the two low
+//                  terms (2^-22) are left out
+// The tensor core truncates when it adds to its fp32 accumulator (measured: 0.2-0.45 x 2^-24 of the
+// accumulator lost per 16-element step), so a gradient in fp32 leaves tensor memory every kDrainSteps
+// steps and is added up in registers.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include <algorithm>
 #include <cmath>
 
+#include "gemm_tc.h"
 #include "kernels.h"
+#include "tc_util.cuh"
 #include "token.h"
 
 namespace bg {
 
+using namespace tc;
+
 namespace {
 
-enum Mode { kLoss = 0, kDX = 1, kDW = 2 };
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kDrainSteps = 64;
 
-struct XentKernel {
-  int64_t n;
+enum Form { kBf16 = 0, kF16x1 = 1, kF16x2 = 2 };
+
+// ------------------------------------------------------------------------------ workspace
+inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
+
+constexpr int kMaxRowBlocks = 2048;
+constexpr int kTableBlocks = 304;  // of the table's amax and conversion
+
+// Rows of one block of k_xent_count / k_xent_rows: at most kMaxRowBlocks blocks, since each adds up the
+// counts of those before it.
+inline int64_t rows_per_block(int64_t n) {
+  return 256 * std::max<int64_t>(1, (n + 256LL * kMaxRowBlocks - 1) / (256LL * kMaxRowBlocks));
+}
+
+struct Ws {
+  int64_t rb, nb, cap, vcap;  // rows a block, blocks, X rows and W rows rounded up to whole tiles
+  size_t head, counts, amax, row, tgt, lse, g, hit, x, w, full, part, total;
+};
+
+Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
+  Ws w{};
+  w.rb = rows_per_block(n);
+  w.nb = std::max<int64_t>(1, (n + w.rb - 1) / w.rb);
+  w.cap = (n + 127) / 128 * 128;
+  w.vcap = ((int64_t)V + 127) / 128 * 128;
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o += al(bytes);
+    return at;
+  };
+  const int terms = form == kF16x2 ? 2 : 1;
+  w.head = take(16);
+  w.counts = take((size_t)w.nb * 4);
+  w.amax = take((size_t)(2 * w.nb + kTableBlocks) * 4);
+  w.row = take((size_t)w.cap * 4);
+  w.tgt = take((size_t)w.cap * 4);
+  w.lse = take((size_t)w.cap * 4);
+  w.g = take((size_t)w.cap * 4);
+  w.hit = take((size_t)w.cap * 4);
+  w.x = take((size_t)terms * w.cap * H * 2);
+  w.w = take(form == kBf16 ? 0 : (size_t)terms * w.vcap * H * 2);
+  w.full = take(backward ? 0 : (size_t)w.cap * 16);
+  w.part = take(backward ? (size_t)ctas * 2 * 128 * H * 4 : (size_t)ctas * 2 * 256 * 8);
+  w.total = o;
+  return w;
+}
+
+// ------------------------------------------------------------------------------ rows
+struct RowArgs {
+  int form, x_bf16, backward, grad_bf16, clear_dx;
+  int64_t n, rb, nb, cap, vcap;
   int H, V;
   const void* X;
   const void* W;
   const int32_t* target;
-  float* loss;
-  float* lse;         // written by the loss, read by the gradients
+  const float* lse_in;
   const float* dloss;
-  void* grad;
-  int grad_bf16, accumulate;
+  int* head;  // number of labelled rows; exponents of the scales of X, W and dloss (fp16 forms)
+  int* counts;
+  uint32_t* amax;  // [nb] of X, [nb] of dloss, [kTableBlocks] of W: bits of the largest finite |x|
+  int32_t* row;
+  int32_t* tgt;
+  float* lse;
+  float* g;
+  uint16_t* x;
+  uint16_t* w;
+  float* loss;
+  float* lse_out;
+  void* dX;
   int* status;
 };
 
-__device__ __forceinline__ float ld(const float* p) { return *p; }
-__device__ __forceinline__ float ld(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-
-__device__ __forceinline__ int row_target(const XentKernel& k, int64_t i) {
-  if (i >= k.n) return -1;
-  const int t = k.target[i];
-  if (t >= k.V) {
-    if (atomicCAS(k.status, 0, 2) == 0) atomicExch(k.status + 1, kSiteXentTarget);
-    return -1;
+__device__ __forceinline__ void load8f(const void* p, int bf16, int64_t at, float* v) {
+  if (bf16) {
+    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + at);
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = __uint_as_float(u[j] << 16);
+      v[2 * j + 1] = __uint_as_float(u[j] & 0xFFFF0000u);
+    }
+  } else {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+    const float4 a = q[0], b = q[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   }
-  return t;
 }
 
-template <typename T, int MODE>
-__global__ void __launch_bounds__(256) k_xent(XentKernel k) {
-  extern __shared__ float sm[];
-  const int H = k.H, ld_ = H + 1;
-  float* A = sm;              // [64][H + 1]: the rows that stay
-  float* B = A + 64 * ld_;    // [64][H + 1]: the rows that pass
-  float* P = B + 64 * ld_;    // [64][65]
-  float* top = P + 64 * 65;   // per staying row: running maximum and sum (kLoss)
-  float* sum = top + 64;
-  float* hit = sum + 64;      // the target's logit
-  float* slse = hit + 64;     // of the X rows at hand
-  float* sg = slse + 64;
-  int* tgt = reinterpret_cast<int*>(sg + 64);
-  const int tid = threadIdx.x;
-  const T* X = static_cast<const T*>(k.X);
-  const T* W = static_cast<const T*>(k.W);
-  const int64_t a0 = (int64_t)blockIdx.x * 64;
-  const int64_t na = MODE == kDW ? k.V : k.n, nb = MODE == kDW ? k.n : k.V;
-  auto load_x = [&](float* dst, int64_t i0) {
-    if (tid < 64) {
-      const int t = row_target(k, i0 + tid);
-      tgt[tid] = t;
-      slse[tid] = MODE != kLoss && t >= 0 ? k.lse[i0 + tid] : 0.f;
-      sg[tid] = MODE != kLoss && t >= 0 ? k.dloss[i0 + tid] : 0.f;
-    }
-    __syncthreads();
-    for (int e = tid; e < 64 * H; e += 256) {
-      const int r = e / H, h = e % H;
-      dst[r * ld_ + h] = tgt[r] >= 0 ? ld(X + (i0 + r) * H + h) : 0.f;
-    }
-  };
-  auto load_w = [&](float* dst, int64_t v0) {
-    for (int e = tid; e < 64 * H; e += 256) {
-      const int r = e / H, h = e % H;
-      dst[r * ld_ + h] = v0 + r < k.V ? ld(W + (v0 + r) * H + h) : 0.f;
-    }
-  };
-  if (MODE == kDW) load_w(A, a0); else load_x(A, a0);
-  if (tid < 64) {
-    top[tid] = -INFINITY;
-    sum[tid] = 0.f;
-    hit[tid] = 0.f;
+__device__ __forceinline__ uint32_t amax8(const float* v, uint32_t m) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t b = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+    if (b < 0x7F800000u) m = max(m, b);
   }
-  float acc[64];
-#pragma unroll
-  for (int r = 0; r < 64; ++r) acc[r] = 0.f;
-  const int tr = tid / 16 * 4, tc = tid % 16 * 4;
-  for (int64_t b0 = 0; b0 < nb; b0 += 64) {
-    __syncthreads();
-    if (MODE == kDW) load_x(B, b0); else load_w(B, b0);
-    __syncthreads();
-    float z[4][4] = {};
-    for (int h = 0; h < H; ++h) {
-      float a[4], b[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        a[j] = A[(tr + j) * ld_ + h];
-        b[j] = B[(tc + j) * ld_ + h];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[i][j] = fmaf(a[i], b[j], z[i][j]);
+  return m;
+}
+
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* sm) {
+  v = __reduce_max_sync(0xffffffffu, v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+  __syncthreads();
+  uint32_t r = 0;
+  for (int i = 0; i < 8; ++i) r = max(r, sm[i]);
+  return r;
+}
+
+// Exponent k such that values of magnitude up to the one with these bits, times 2^k, are below 2^15.
+__device__ __forceinline__ int shift_of(uint32_t bits) { return 14 - max((int)(bits >> 23) - 127, -100); }
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+
+// Labelled rows of each block of rb rows and, for the fp16 forms, the largest finite magnitudes of
+// the labelled rows of X, of their dloss, and of W.
+__global__ void __launch_bounds__(256) k_xent_count(RowArgs a) {
+  __shared__ uint32_t sm[8];
+  grid_dep_launch();
+  grid_dep_wait();
+  const int lanes = a.H / 8;
+  if ((int64_t)blockIdx.x >= a.nb) {
+    const int b = blockIdx.x - (int)a.nb;
+    uint32_t mx = 0;
+    const int64_t chunks = (int64_t)a.V * lanes;
+    for (int64_t i = (int64_t)b * 256 + threadIdx.x; i < chunks; i += (int64_t)kTableBlocks * 256) {
+      float v[8];
+      load8f(a.W, a.x_bf16, i * 8, v);
+      mx = amax8(v, mx);
     }
+    mx = block_max(mx, sm);
+    if (threadIdx.x == 0) a.amax[2 * a.nb + b] = mx;
+    return;
+  }
+  const int64_t r0 = blockIdx.x * a.rb, r1 = min(a.n, r0 + a.rb);
+  int c = 0;
+  uint32_t mg = 0;
+  for (int64_t i = r0 + threadIdx.x; i < r1; i += 256) {
+    const int t = a.target[i];
+    if (t >= 0 && t < a.V) {
+      ++c;
+      if (a.form != kBf16 && a.backward) {
+        const uint32_t b = __float_as_uint(a.dloss[i]) & 0x7FFFFFFFu;
+        if (b < 0x7F800000u) mg = max(mg, b);
+      }
+    }
+  }
+  c = __reduce_add_sync(0xffffffffu, c);
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = c;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int s = 0;
+    for (int i = 0; i < 8; ++i) s += sm[i];
+    a.counts[blockIdx.x] = s;
+  }
+  if (a.form == kBf16) return;
+  uint32_t mx = 0;
+  const int rows = 256 / lanes, r = threadIdx.x / lanes, q = threadIdx.x % lanes;
+  if (r < rows)
+    for (int64_t i = r0 + r; i < r1; i += rows) {
+      const int t = a.target[i];
+      if (t < 0 || t >= a.V) continue;
+      float v[8];
+      load8f(a.X, a.x_bf16, i * a.H + q * 8, v);
+      mx = amax8(v, mx);
+    }
+  mx = block_max(mx, sm);
+  mg = block_max(mg, sm);
+  if (threadIdx.x == 0) {
+    a.amax[blockIdx.x] = mx;
+    a.amax[a.nb + blockIdx.x] = mg;
+  }
+}
+
+// 8 elements to the form's terms: plane t of `dst` starts at t * plane.
+__device__ __forceinline__ void put8(uint16_t* dst, int64_t plane, int64_t at, int form, float scale,
+                                     const float* v) {
+  uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int ar = tr + i, br = tc + j;
-        float v = z[i][j];
-        if (MODE != kLoss) {
-          const int x = MODE == kDX ? ar : br;
-          const int64_t voc = MODE == kDX ? b0 + br : a0 + ar;
-          v = tgt[x] >= 0 && voc < k.V
-                  ? sg[x] * (expf(v - slse[x]) - (voc == tgt[x] ? 1.f : 0.f))
-                  : 0.f;
+  for (int j = 0; j < 4; ++j) {
+    const float x = v[2 * j] * scale, y = v[2 * j + 1] * scale;
+    const __half2 h = __floats2half2_rn(x, y);
+    hi[j] = *reinterpret_cast<const uint32_t*>(&h);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+    lo[j] = *reinterpret_cast<const uint32_t*>(&l);
+  }
+  *reinterpret_cast<uint4*>(dst + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  if (form == kF16x2)
+    *reinterpret_cast<uint4*>(dst + plane + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
+// The labelled rows, side by side in their order: X in the form's terms, the row each came from, its
+// target and, for the gradient, its lse and g; the outputs of the rows left out.  The last block adds
+// empty rows up to a whole tile (zeros, lse = +inf: every probability 0) and the number of rows.  The
+// blocks from nb on convert W.
+__global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
+  __shared__ int wsum[8];
+  __shared__ uint32_t sm[8];
+  __shared__ int64_t from[256];  // row of each slot of the group at hand
+  grid_dep_launch();
+  grid_dep_wait();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int lanes = a.H / 8, rows = 256 / lanes, rr = tid / lanes, q = tid % lanes;
+  uint32_t mx = 0, mg = 0, mw = 0;
+  if (a.form != kBf16) {
+    for (int64_t i = tid; i < a.nb; i += 256) {
+      mx = max(mx, a.amax[i]);
+      mg = max(mg, a.amax[a.nb + i]);
+    }
+    for (int i = tid; i < kTableBlocks; i += 256) mw = max(mw, a.amax[2 * a.nb + i]);
+    mx = block_max(mx, sm);
+    mg = block_max(mg, sm);
+    mw = block_max(mw, sm);
+  }
+  if ((int64_t)blockIdx.x >= a.nb) {
+    const int b = blockIdx.x - (int)a.nb;
+    const float scale = pow2(shift_of(mw));
+    const int64_t chunks = (int64_t)a.V * lanes, all = a.vcap * lanes;
+    for (int64_t i = (int64_t)b * 256 + tid; i < all; i += (int64_t)kTableBlocks * 256) {
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (i < chunks) load8f(a.W, a.x_bf16, i * 8, v);
+      put8(a.w, a.vcap * a.H, i * 8, a.form, scale, v);
+    }
+    return;
+  }
+  const float scale = a.form == kBf16 ? 1.f : pow2(shift_of(mx));
+  int64_t base = 0;
+  {
+    int c = 0;
+    for (int64_t i = tid; i < (int64_t)blockIdx.x; i += 256) c += a.counts[i];
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (lane == 0) wsum[warp] = c;
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) base += wsum[i];
+  }
+  const int64_t r0 = blockIdx.x * a.rb, r1 = min(a.n, r0 + a.rb);
+  for (int64_t g0 = r0; g0 < r1; g0 += 256) {
+    const int64_t i = g0 + tid;
+    int t = i < r1 ? a.target[i] : -1;
+    if (t >= a.V) {
+      if (atomicCAS(a.status, 0, 2) == 0) atomicExch(a.status + 1, kSiteXentTarget);
+      t = -1;
+    }
+    const unsigned ballot = __ballot_sync(0xffffffffu, t >= 0);
+    __syncthreads();
+    if (lane == 0) wsum[warp] = __popc(ballot);
+    __syncthreads();
+    int before = 0, count = 0;
+    for (int w = 0; w < 8; ++w) {
+      before += w < warp ? wsum[w] : 0;
+      count += wsum[w];
+    }
+    if (t >= 0) {
+      const int k = before + __popc(ballot & ((1u << lane) - 1));
+      const int64_t slot = base + k;
+      from[k] = i;
+      a.row[slot] = (int32_t)i;
+      a.tgt[slot] = t;
+      if (a.backward) {
+        a.lse[slot] = a.form == kBf16 ? a.lse_in[i] * kLog2e : a.lse_in[i];
+        a.g[slot] = a.dloss[i];
+      }
+    } else if (i < r1 && !a.backward) {
+      a.loss[i] = 0.f;
+      a.lse_out[i] = 0.f;
+    }
+    __syncthreads();
+    if (rr < rows) {
+      for (int k = rr; k < count; k += rows) {
+        const int64_t src = from[k] * a.H + q * 8, dst = (base + k) * a.H + q * 8;
+        if (a.form == kBf16) {
+          *reinterpret_cast<uint4*>(a.x + dst) =
+              *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.X) + src);
+        } else {
+          float v[8];
+          load8f(a.X, a.x_bf16, src, v);
+          put8(a.x, a.cap * a.H, dst, a.form, scale, v);
         }
-        P[ar * 65 + br] = v;
       }
-    __syncthreads();
-    if (MODE == kLoss) {
-      if (tid < 64 && tgt[tid] >= 0) {
-        const int m = (int)min((int64_t)64, nb - b0);
-        float mx = top[tid];
-        for (int c = 0; c < m; ++c) mx = fmaxf(mx, P[tid * 65 + c]);
-        float s = mx == -INFINITY ? 0.f : sum[tid] * expf(top[tid] - mx);
-        if (mx != -INFINITY)
-          for (int c = 0; c < m; ++c) s += expf(P[tid * 65 + c] - mx);
-        top[tid] = mx;
-        sum[tid] = s;
-        if (tgt[tid] >= b0 && tgt[tid] < b0 + m) hit[tid] = P[tid * 65 + tgt[tid] - b0];
+      if (a.clear_dx)
+        for (int k = rr; k < 256 && g0 + k < r1; k += rows) {
+          const int tk = a.target[g0 + k];
+          if (tk >= 0 && tk < a.V) continue;
+          const int64_t at = (g0 + k) * a.H + q * 8;
+          const uint4 zero = make_uint4(0, 0, 0, 0);
+          if (a.grad_bf16) {
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.dX) + at) = zero;
+          } else {
+            uint4* p = reinterpret_cast<uint4*>(static_cast<float*>(a.dX) + at);
+            p[0] = zero;
+            p[1] = zero;
+          }
+        }
+    }
+    base += count;
+  }
+  if ((int64_t)blockIdx.x == a.nb - 1) {
+    const int64_t end = (base + 127) / 128 * 128;
+    if (tid == 0) {
+      a.head[0] = (int)base;
+      if (a.form != kBf16) {
+        a.head[1] = shift_of(mx);
+        a.head[2] = shift_of(mw);
+        a.head[3] = shift_of(mg);
       }
-    } else if (tid < H) {
-      for (int c = 0; c < 64; ++c) {
-        const float b = B[c * ld_ + tid];
+    }
+    for (int64_t s = base + tid; s < end; s += 256) {
+      a.row[s] = -1;
+      a.tgt[s] = -1;
+      if (a.backward) {
+        a.lse[s] = INFINITY;
+        a.g[s] = 0.f;
+      }
+    }
+    if (rr < rows)
+      for (int64_t s = base + rr; s < end; s += rows) {
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(a.x + s * a.H + q * 8) = zero;
+        if (a.form == kF16x2) *reinterpret_cast<uint4*>(a.x + (a.cap + s) * a.H + q * 8) = zero;
+      }
+  }
+}
+
+// ------------------------------------------------------------------------------ units
+// Unit u = t * ct + j is staying tile t against passing tile j; CTA c takes [begin(c), begin(c + 1)).
+// With fewer units than CTAs the last CTAs take none, so that those between a tile's first and last
+// all have a part of it.
+struct Units {
+  int64_t ct, U;
+  int G;  // CTAs that take units
+  __device__ Units(int64_t rt, int64_t ct_, int ctas)
+      : ct(ct_), U(rt * ct_), G((int)min((int64_t)ctas, rt * ct_)) {}
+  __device__ int64_t begin(int c) const { return c >= G ? U : U * c / G; }
+  // the CTA that unit u falls to (u < U)
+  __device__ int owner(int64_t u) const {
+    int c = (int)(u * G / U);
+    while (begin(c + 1) <= u) ++c;
+    while (begin(c) > u) --c;
+    return c;
+  }
+  // which of its two partial results CTA c keeps of tile t, one it shares with others
+  __device__ int slot(int c, int64_t t) const { return t == begin(c) / ct ? 0 : 1; }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
+      "%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+// Shared-memory descriptor of an MN-major operand with the 128-byte swizzle: rows of 64 elements along
+// N, one row a K index, 8-row groups 1024 bytes apart (stride byte offset), the next 64 elements of
+// N at `lbo` bytes (leading byte offset).
+__device__ __forceinline__ uint64_t desc_sw128_mnmajor(uint32_t start, uint32_t lbo) {
+  uint64_t d = 0;
+  d |= (uint64_t)((start >> 4) & 0x3FFFu);
+  d |= (uint64_t)((lbo >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// kind::f16 instruction descriptor, M = 128; b_mn: B is MN-major.
+__device__ __forceinline__ uint32_t idesc16(int bf16, int N, int b_mn) {
+  return (bf16 ? idesc_bf16_f32(128, N) : idesc_f16_f32(128, N)) | (uint32_t)b_mn << 16;
+}
+
+constexpr int kFwdThreads = 320;  // 8 epilogue warps, a TMA warp, an MMA warp
+// The backward adds two idle warps, so that registers can move between whole warpgroups: 384 x 168 at
+// launch = 256 x 224 (epilogue, which holds up to 128 gradient sums a thread) + 128 x 56.
+constexpr int kBwdThreads = 384;
+
+// ------------------------------------------------------------------------------ forward
+struct FwdArgs {
+  int H, V;
+  int64_t cap, vcap;
+  const int* head;
+  const int32_t* tgt;
+  float* hit;    // [cap] logit of the target
+  float2* full;  // [2][cap] maximum and sum of each half, of the tiles one CTA has all units of
+  float2* part;  // [G][2][2][128] of the others
+  int* status;
+};
+
+// z tiles of 128 rows x 256 columns.  X's tile stays in shared memory, W passes through a ring in
+// pieces of 256 rows x 64 elements, two accumulators of 256 columns fill tensor memory.
+template <int HC, int T>
+struct FCfg {
+  static constexpr int A_BYTES = T * HC * 16384;
+  static constexpr int PIECE = 32768;
+  static constexpr int ROOM = (232448 - 2048 - A_BYTES) / PIECE;
+  static constexpr int ST = ROOM < 6 ? ROOM : 6;
+  static constexpr int NP = T == 1 ? HC : 3 * HC;  // 64-element pieces of the product
+  static constexpr int SMEM = A_BYTES + ST * PIECE + 2048;
+  static_assert(ST >= 2 && SMEM <= 232448, "shared memory");
+};
+
+struct FwdBars {
+  uint64_t a_full, a_empty, full[6], empty[6], s_full[2], s_empty[2], drain;
+  uint32_t tmem;
+  int abort;
+};
+
+// Running maximum (in units of c z) and sum of 32 columns more.
+__device__ __forceinline__ void online32(const uint32_t* v, float c, float& m, float& l) {
+  float top = __uint_as_float(v[0]);
 #pragma unroll
-        for (int r = 0; r < 64; ++r) acc[r] = fmaf(P[r * 65 + c], b, acc[r]);
+  for (int j = 1; j < 32; ++j) top = fmaxf(top, __uint_as_float(v[j]));
+  const float mn = fmaxf(m, top * c);
+  float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    s0 += ex2(fmaf(__uint_as_float(v[j]), c, -mn));
+    s1 += ex2(fmaf(__uint_as_float(v[j + 1]), c, -mn));
+    s2 += ex2(fmaf(__uint_as_float(v[j + 2]), c, -mn));
+    s3 += ex2(fmaf(__uint_as_float(v[j + 3]), c, -mn));
+  }
+  l = fmaf(l, ex2(m - mn), (s0 + s1) + (s2 + s3));
+  m = mn;
+}
+
+template <int HC, int T>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+    k_xent_fwd(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
+               FwdArgs a) {
+  using C = FCfg<HC, T>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  uint8_t* ring = smem + C::A_BYTES;
+  FwdBars* bars = reinterpret_cast<FwdBars*>(ring + C::ST * C::PIECE);
+  volatile int* abort = &bars->abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(&bars->a_full, 1);
+    mbar_init(&bars->a_empty, 1);
+    for (int s = 0; s < C::ST; ++s) {
+      mbar_init(&bars->full[s], 1);
+      mbar_init(&bars->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&bars->s_full[b], 1);
+      mbar_init(&bars->s_empty[b], 8);
+    }
+    mbar_init(&bars->drain, 1);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc(&bars->tmem, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  grid_dep_launch();
+  grid_dep_wait();
+  const uint32_t tmem = bars->tmem;
+  const int64_t rows = a.head[0];
+  const Units un((rows + 127) / 128, (a.V + 255) / 256, gridDim.x);
+  const int64_t u0 = un.begin(blockIdx.x), u1 = un.begin(blockIdx.x + 1);
+
+  if (warp == 8) {
+    if (lane == 0) {
+      tma_prefetch_desc(&tmX);
+      tma_prefetch_desc(&tmW);
+      uint32_t it = 0, seg = 0;
+      bool ok = true;
+      for (int64_t u = u0; u < u1 && ok; ++u) {
+        const int64_t t = u / un.ct, j = u % un.ct;
+        if (u == u0 || j == 0) {
+          ok = seg == 0 || mbar_wait(&bars->a_empty, (seg - 1) & 1, a.status, 701, abort, 32);
+          if (!ok) break;
+          mbar_expect_tx(&bars->a_full, C::A_BYTES);
+          for (int p = 0; p < T * HC; ++p)
+            tma_load_2d(smem + p * 16384, &tmX, &bars->a_full, p % HC * 64,
+                        (int)((p / HC) * a.cap + t * 128));
+          ++seg;
+        }
+        for (int p = 0; p < C::NP && ok; ++p, ++it) {
+          const int s = it % C::ST;
+          ok = mbar_wait(&bars->empty[s], ((it / C::ST) & 1) ^ 1, a.status, 702, abort, 32);
+          if (!ok) break;
+          mbar_expect_tx(&bars->full[s], C::PIECE);
+          tma_load_2d(ring + s * C::PIECE, &tmW, &bars->full[s], p % HC * 64,
+                      (int)((T == 2 && p < HC ? a.vcap : 0) + j * 256));
+        }
+      }
+      if (*abort) {  // copies in flight land before the block leaves
+        for (uint32_t k = 0; seg && k < (1u << 22) && !mbar_try(&bars->a_full, (seg - 1) & 1); ++k) {
+        }
+        for (uint32_t q = it > C::ST ? it - C::ST : 0; q < it; ++q)
+          for (uint32_t k = 0; k < (1u << 22) && !mbar_try(&bars->full[q % C::ST], (q / C::ST) & 1); ++k) {
+          }
+      }
+    }
+  } else if (warp == 9) {
+    const bool leader = elect_one_sync();
+    const uint32_t idesc = idesc16(T == 1, 256, 0);
+    const uint32_t A = smem_u32(smem), R = smem_u32(ring);
+    uint32_t it = 0, seg = 0, n = 0;
+    bool ok = true;
+    for (int64_t u = u0; u < u1 && ok; ++u, ++n) {
+      const int64_t j = u % un.ct;
+      if (u == u0 || j == 0) {
+        ok = mbar_wait(&bars->a_full, seg & 1, a.status, 703, abort);
+        ++seg;
+      }
+      const int b = n & 1;
+      ok = ok && mbar_wait(&bars->s_empty[b], ((n >> 1) & 1) ^ 1, a.status, 704, abort);
+      for (int p = 0; p < C::NP && ok; ++p, ++it) {
+        const int s = it % C::ST;
+        ok = mbar_wait(&bars->full[s], (it / C::ST) & 1, a.status, 705, abort);
+        if (!ok) break;
+        tc_fence_after();
+        // two terms: high x low, low x high, then high x high, so that the accumulator is small
+        // (and loses little) in the first two thirds
+        const int ab = T == 2 && p >= HC && p < 2 * HC ? p : p % HC;
+        const int steps = min(4, (a.H - p % HC * 64) / 16);
+        for (int kk = 0; kk < steps; ++kk)
+          if (leader)
+            mma_ss(tmem + b * 256, desc_sw128_kmajor(A + ab * 16384 + kk * 32),
+                   desc_sw128_kmajor(R + s * C::PIECE + kk * 32), idesc, p > 0 || kk > 0);
+        if (leader) tc_commit(&bars->empty[s]);
+        __syncwarp();
+      }
+      if (ok && leader) {
+        tc_commit(&bars->s_full[b]);
+        if (u + 1 == u1 || j + 1 == un.ct) tc_commit(&bars->a_empty);
+      }
+      __syncwarp();
+    }
+    if (leader) tc_commit(&bars->drain);
+    __syncwarp();
+    for (uint32_t k = 0; k < (1u << 24) && !mbar_try(&bars->drain, 0); ++k) {
+    }
+  } else {
+    // warps 0-3: columns 0-127 of a tile, warps 4-7: columns 128-255; a thread is a row
+    const int q = warp & 3, h = warp >> 2, r = q * 32 + lane;
+    float c = kLog2e;
+    if (T == 2) c *= pow2(max(-126, min(127, -(a.head[1] + a.head[2]))));
+    const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + h * 128;
+    float m = -3.0e38f, l = 0.f;
+    int tgt = -1;
+    uint32_t n = 0;
+    for (int64_t u = u0; u < u1; ++u, ++n) {
+      const int64_t t = u / un.ct, j = u % un.ct;
+      if (u == u0 || j == 0) {
+        m = -3.0e38f;
+        l = 0.f;
+        tgt = a.tgt[t * 128 + r];
+      }
+      const int b = n & 1;
+      if (!mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 32)) break;
+      tc_fence_after();
+      const int64_t v0 = j * 256 + h * 128;
+      uint32_t x[2][32];
+      tmem_ld32(base + b * 256, x[0]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        tmem_wait_ld();
+        if (k < 3) tmem_ld32(base + b * 256 + (k + 1) * 32, x[(k + 1) & 1]);
+        uint32_t* v = x[k & 1];
+        const int64_t w0 = v0 + k * 32;
+        if (w0 + 32 > a.V) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (w0 + i >= a.V) v[i] = 0xFF800000u;
+        }
+        const int at = (int)(tgt - w0);
+        const bool here = tgt >= 0 && at >= 0 && at < 32;
+        if (__any_sync(0xffffffffu, here)) {
+          float z = 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i == at) z = __uint_as_float(v[i]);
+          if (here) a.hit[t * 128 + r] = z * (c / kLog2e);
+        }
+        online32(v, c, m, l);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->s_empty[b]);
+      if (u + 1 == u1 || j + 1 == un.ct) {
+        const int64_t f = t * un.ct;
+        const bool whole = u0 <= f && f + un.ct <= u1;
+        // the sum's reference is m itself, so that the join undoes exactly what was done here
+        if (whole)
+          a.full[h * a.cap + t * 128 + r] = make_float2(m, l);
+        else
+          a.part[(((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, t)) * 2 + h) * 128 + r] =
+              make_float2(m, l);
       }
     }
   }
-  if (MODE == kLoss) {
-    if (tid < 64 && a0 + tid < k.n) {
-      const float l = tgt[tid] >= 0 ? top[tid] + logf(sum[tid]) : 0.f;
-      k.lse[a0 + tid] = l;
-      k.loss[a0 + tid] = tgt[tid] >= 0 ? l - hit[tid] : 0.f;
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// One warp a labelled row: its maxima and sums together, lse and loss.
+__global__ void __launch_bounds__(256)
+    k_xent_join(int V, int64_t cap, int G, const int* __restrict__ head,
+                const int32_t* __restrict__ row, const float* __restrict__ hit,
+                const float2* __restrict__ full, const float2* __restrict__ part,
+                float* __restrict__ loss, float* __restrict__ lse) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t rows = head[0];
+  const Units un((rows + 127) / 128, (V + 255) / 256, G);
+  for (int64_t s = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); s < rows; s += (int64_t)gridDim.x * 8) {
+    const int64_t t = s / 128;
+    const int r = (int)(s % 128);
+    const int c0 = un.owner(t * un.ct), c1 = un.owner(t * un.ct + un.ct - 1);
+    float m = -3.0e38f, l = 0.f;
+    const int n = c0 == c1 ? 2 : 2 * (c1 - c0 + 1);
+    for (int i = lane; i < n; i += 32) {
+      const int c = c0 + i / 2;
+      const float2 p = c0 == c1 ? full[i * cap + s]
+                                : part[(((int64_t)c * 2 + un.slot(c, t)) * 2 + (i & 1)) * 128 + r];
+      const float mn = fmaxf(m, p.x);
+      l = l * ex2(m - mn) + p.y * ex2(p.x - mn);
+      m = mn;
     }
-  } else if (tid < H) {
+    float top = m;
 #pragma unroll
-    for (int r = 0; r < 64; ++r) {
-      if (a0 + r >= na) continue;
-      const int64_t at = (a0 + r) * H + tid;
-      if (k.grad_bf16) {
-        static_cast<__nv_bfloat16*>(k.grad)[at] = __float2bfloat16(acc[r]);
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    l *= ex2(m - top);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (lane == 0) {
+      // top is c z of the largest logit with c = kLog2e as rounded: divide by that very number
+      const float v = (float)(((double)top + log2((double)l)) / (double)kLog2e);
+      lse[row[s]] = v;
+      loss[row[s]] = v - hit[s];
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------ backward
+struct BwdArgs {
+  int dw;  // the rows of W stay (dW); else the rows of X (dX)
+  int H, V, accumulate;
+  int64_t scap, pcap;  // rows of a plane of the staying and of the passing operand
+  const int* head;
+  const int32_t* row;
+  const int32_t* tgt;
+  const float* lse;
+  const float* g;
+  void* out;
+  float* part;  // [G][2][128][H]
+  int* status;
+};
+
+// One unit: z = S B^T (S the staying tile, B the passing one), P from z, G += P B.  B serves both
+// products: as its rows lie (K-major) in the first, transposed (MN-major) in the second.
+template <int HC, int FORM>
+struct BCfg {
+  static constexpr int T = FORM == kF16x2 ? 2 : 1;   // terms of S and B
+  static constexpr int PT = FORM == kBf16 ? 1 : 2;   // terms of P
+  static constexpr bool KEEP = FORM != kBf16;        // G is added up in registers
+  static constexpr int NB = T == 2 && HC > 2 ? 64 : 128;  // passing rows of a unit
+  static constexpr int S_BYTES = T * HC * 16384;
+  static constexpr int BOX = NB * 128;  // 64 elements of each passing row
+  static constexpr int B_BYTES = T * HC * BOX;
+  static constexpr int STATS = 3 * NB * 4;  // lse, g and target of passing X rows
+  static constexpr int ROOM = (232448 - 2048 - S_BYTES) / (B_BYTES + 2048);
+  static constexpr int ST = ROOM < 4 ? ROOM : 4;
+  static constexpr int SMEM = S_BYTES + ST * (B_BYTES + 2048) + 2048;
+  static constexpr int GCOLS = HC * 64;
+  static constexpr int STEPS = NB / 16 * (T == 2 ? 3 : PT);  // accumulating steps of a unit
+  static constexpr int DRAIN = KEEP ? kDrainSteps / STEPS : 1 << 30;  // units before G leaves TMEM
+  static_assert(ST >= 1 && SMEM <= 232448, "shared memory");
+  static_assert(GCOLS + 2 * NB <= 512, "tensor memory");
+  static_assert(DRAIN >= 1, "drain interval");
+};
+
+struct BwdBars {
+  uint64_t s_full, s_empty, full[4], empty[4], z_full[2], p_full[2], g_full, g_empty, drain;
+  uint32_t tmem;
+  int abort;
+};
+
+// P of 32 columns from their logits, in place.
+// Row statistics (dX): mine = {lse, target - first column}.  Column statistics (dW): arrays.
+template <int FORM, bool DW>
+__device__ __forceinline__ void probs32(uint32_t* v, float descale, float up, float lse, int hit,
+                                        const float* col_lse, const float* col_g,
+                                        const int* col_tgt, int64_t first_row, int r) {
+  const int lane = threadIdx.x & 31;
+  if (!DW) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float z = __uint_as_float(v[i]);
+      const float e = FORM == kBf16 ? ex2(fmaf(z, kLog2e, -lse))
+                                    : ex2(fmaf(fmaf(z, descale, -lse), kLog2e, up));
+      v[i] = __float_as_uint(e);
+    }
+    const bool here = hit >= 0 && hit < 32;
+    if (__any_sync(0xffffffffu, here)) {
+      const float one = FORM == kBf16 ? 1.f : 32768.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i == hit) v[i] = __float_as_uint(__uint_as_float(v[i]) - one);
+    }
+  } else {
+    const float upg = FORM == kBf16 ? 1.f : ex2(up);
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      const float4 ls = *reinterpret_cast<const float4*>(col_lse + i);
+      const float4 gg = *reinterpret_cast<const float4*>(col_g + i);
+      const float lc[4] = {ls.x, ls.y, ls.z, ls.w}, gc[4] = {gg.x, gg.y, gg.z, gg.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float z = __uint_as_float(v[i + k]);
+        const float e = FORM == kBf16 ? ex2(fmaf(z, kLog2e, -lc[k]))
+                                      : ex2(fmaf(fmaf(z, descale, -lc[k]), kLog2e, up));
+        v[i + k] = __float_as_uint(e * gc[k]);
+      }
+    }
+    const int64_t at = (int64_t)col_tgt[lane] - first_row;
+    unsigned hits = __ballot_sync(0xffffffffu, at >= 0 && at < 128);
+    if (hits) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (hits >> i & 1) {
+          if (col_tgt[i] - first_row == r)
+            v[i] = __float_as_uint(__uint_as_float(v[i]) - col_g[i] * upg);
+        }
+    }
+  }
+}
+
+template <int HC, int FORM, bool DW>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+    k_xent_bwd(const __grid_constant__ CUtensorMap tmS, const __grid_constant__ CUtensorMap tmB,
+               BwdArgs a, int out_bf16) {
+  using C = BCfg<HC, FORM>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  uint8_t* ring = smem + C::S_BYTES;
+  uint8_t* stats = ring + C::ST * C::B_BYTES;  // 2048 bytes a stage
+  BwdBars* bars = reinterpret_cast<BwdBars*>(stats + C::ST * 2048);
+  volatile int* abort = &bars->abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(&bars->s_full, 1);
+    mbar_init(&bars->s_empty, 1);
+    for (int s = 0; s < C::ST; ++s) {
+      mbar_init(&bars->full[s], 1);
+      mbar_init(&bars->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&bars->z_full[b], 1);
+      mbar_init(&bars->p_full[b], 8);
+    }
+    mbar_init(&bars->g_full, 1);
+    mbar_init(&bars->g_empty, 8);
+    mbar_init(&bars->drain, 1);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc(&bars->tmem, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  grid_dep_launch();
+  grid_dep_wait();
+  const uint32_t tmem = bars->tmem, zbuf = tmem + C::GCOLS;
+  const int64_t rows = a.head[0];
+  const Units un(DW ? (a.V + 127) / 128 : (rows + 127) / 128,
+                 DW ? (rows + C::NB - 1) / C::NB : (a.V + C::NB - 1) / C::NB, gridDim.x);
+  const int64_t u0 = un.begin(blockIdx.x), u1 = un.begin(blockIdx.x + 1);
+
+  if (warp >= 10) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  } else if (warp == 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (lane == 0) {
+      tma_prefetch_desc(&tmS);
+      tma_prefetch_desc(&tmB);
+      uint32_t it = 0, seg = 0;
+      bool ok = true;
+      for (int64_t u = u0; u < u1 && ok; ++u, ++it) {
+        const int64_t t = u / un.ct, j = u % un.ct;
+        if (u == u0 || j == 0) {
+          ok = seg == 0 || mbar_wait_inline(&bars->s_empty, (seg - 1) & 1, a.status, 711, abort, 32);
+          if (!ok) break;
+          mbar_expect_tx(&bars->s_full, C::S_BYTES);
+          for (int p = 0; p < C::T * HC; ++p)
+            tma_load_2d(smem + p * 16384, &tmS, &bars->s_full, p % HC * 64,
+                        (int)((p / HC) * a.scap + t * 128));
+          ++seg;
+        }
+        const int s = it % C::ST;
+        ok = mbar_wait_inline(&bars->empty[s], ((it / C::ST) & 1) ^ 1, a.status, 712, abort, 32);
+        if (!ok) break;
+        mbar_expect_tx(&bars->full[s], C::B_BYTES + (DW ? C::STATS : 0));
+        for (int p = 0; p < C::T * HC; ++p)
+          tma_load_2d(ring + s * C::B_BYTES + p * C::BOX, &tmB, &bars->full[s], p % HC * 64,
+                      (int)((p / HC) * a.pcap + j * C::NB));
+        if (DW) {
+          bulk_load(stats + s * 2048, a.lse + j * C::NB, C::NB * 4, &bars->full[s]);
+          bulk_load(stats + s * 2048 + C::NB * 4, a.g + j * C::NB, C::NB * 4, &bars->full[s]);
+          bulk_load(stats + s * 2048 + C::NB * 8, a.tgt + j * C::NB, C::NB * 4, &bars->full[s]);
+        }
+      }
+      if (*abort) {  // copies in flight land before the block leaves
+        for (uint32_t k = 0; seg && k < (1u << 22) && !mbar_try(&bars->s_full, (seg - 1) & 1); ++k) {
+        }
+        for (uint32_t q = it > C::ST ? it - C::ST : 0; q < it; ++q)
+          for (uint32_t k = 0; k < (1u << 22) && !mbar_try(&bars->full[q % C::ST], (q / C::ST) & 1); ++k) {
+          }
+      }
+    }
+  } else if (warp == 9) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const bool leader = elect_one_sync();
+    const uint32_t iz = idesc16(FORM == kBf16, C::NB, 0), ig = idesc16(FORM == kBf16, a.H, 1);
+    const uint32_t S = smem_u32(smem), R = smem_u32(ring);
+    const int ks = a.H / 16;
+    // z = S B^T of the unit in ring stage s; two terms: low x high and high x low first
+    auto z_product = [&](int s, int b) {
+      const uint32_t B = R + s * C::B_BYTES, d = zbuf + b * C::NB;
+      constexpr int n = C::T == 2 ? 3 : 1;
+      for (int pr = 0; pr < n; ++pr) {
+        const uint32_t as = S + (n == 3 && pr == 0 ? HC * 16384 : 0);
+        const uint32_t bs = B + (n == 3 && pr == 1 ? HC * C::BOX : 0);
+        for (int k = 0; k < ks; ++k)
+          if (leader)
+            mma_ss(d, desc_sw128_kmajor(as + (k >> 2) * 16384 + (k & 3) * 32),
+                   desc_sw128_kmajor(bs + (k >> 2) * C::BOX + (k & 3) * 32), iz, pr > 0 || k > 0);
+      }
+    };
+    // G (+)= P B, small products first
+    auto g_product = [&](int s, int b, bool add) {
+      const uint32_t B = R + s * C::B_BYTES, p = zbuf + b * C::NB;
+      constexpr int n = C::T == 2 ? 3 : C::PT;
+      for (int pr = 0; pr < n; ++pr) {
+        const uint32_t pa = p + (C::PT == 2 && pr == 0 ? 16 : 0);
+        const uint32_t bs = B + (n == 3 && pr == 1 ? HC * C::BOX : 0);
+#pragma unroll
+        for (int k = 0; k < C::NB / 16; ++k)
+          if (leader)
+            mma_ts(tmem, pa + (k >> 1) * 32 + (k & 1) * 8, desc_sw128_mnmajor(bs + k * 2048, C::BOX),
+                   ig, add || pr > 0 || k > 0);
+      }
+    };
+    uint32_t it = 0, seg = 0, groups = 0;
+    bool ok = true;
+    int in_group = 0;     // units of the running group whose G has been issued
+    bool last = false;    // the previous unit ended its staying tile
+    // the second product of unit `k` (its number in this CTA's run)
+    auto second = [&](uint32_t k, bool ends) {
+      ok = ok && mbar_wait_inline(&bars->p_full[k & 1], (k >> 1) & 1, a.status, 713, abort);
+      if (ok && in_group == 0 && groups > 0)
+        ok = mbar_wait_inline(&bars->g_empty, (groups - 1) & 1, a.status, 714, abort);
+      if (!ok) return;
+      tc_fence_after();
+      g_product(k % C::ST, k & 1, in_group > 0);
+      if (leader) tc_commit(&bars->empty[k % C::ST]);
+      if (++in_group == C::DRAIN || ends) {
+        if (leader) tc_commit(&bars->g_full);
+        ++groups;
+        in_group = 0;
+      }
+      __syncwarp();
+    };
+    for (int64_t u = u0; u < u1 && ok; ++u, ++it) {
+      const int64_t j = u % un.ct;
+      if (C::ST == 1 && it > 0) second(it - 1, last);
+      if (u == u0 || j == 0) {
+        ok = ok && mbar_wait_inline(&bars->s_full, seg & 1, a.status, 715, abort);
+        ++seg;
+      }
+      const int s = it % C::ST;
+      ok = ok && mbar_wait_inline(&bars->full[s], (it / C::ST) & 1, a.status, 716, abort);
+      if (!ok) break;
+      tc_fence_after();
+      z_product(s, it & 1);
+      const bool ends = u + 1 == u1 || j + 1 == un.ct;
+      if (leader) {
+        tc_commit(&bars->z_full[it & 1]);
+        if (ends) tc_commit(&bars->s_empty);
+      }
+      __syncwarp();
+      if (C::ST > 1 && it > 0) second(it - 1, last);
+      last = ends;
+    }
+    if (it > 0) second(it - 1, last);
+    if (leader) tc_commit(&bars->drain);
+    __syncwarp();
+    for (uint32_t k = 0; k < (1u << 24) && !mbar_try(&bars->drain, 0); ++k) {
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // warps 0-3: the first half of a unit's columns and of G's, warps 4-7: the second; a thread is a row
+    const int q = warp & 3, h = warp >> 2, r = q * 32 + lane;
+    constexpr int HALF = C::NB / 2, GH = HC * 32;
+    const uint32_t quarter = (uint32_t)(q * 32) << 16;
+    const int sx = FORM == kBf16 ? 0 : a.head[1], sw = FORM == kBf16 ? 0 : a.head[2];
+    const float descale = FORM == kBf16 ? 1.f : pow2(max(-126, min(127, -(sx + sw))));
+    // P is scaled by 2^up: probabilities to 2^15 for dX, times g to 2^15 for dW
+    const int up = FORM == kBf16 ? 0 : DW ? a.head[3] : 15;
+    float acc[C::KEEP ? GH : 1];
+    uint32_t it = 0, groups = 0;
+    int in_group = 0;
+    bool fresh = true, pending = false, ok = true;
+    float lse = 0.f;
+    int tgt = -1;
+    // adds the finished group of G to the registers
+    auto collect = [&]() {
+      if (!mbar_wait_inline(&bars->g_full, groups & 1, a.status, 717, abort, 32)) return false;
+      ++groups;
+      tc_fence_after();
+      if (C::KEEP) {
+#pragma unroll
+        for (int c = 0; c < GH; c += 32) {
+          uint32_t v[32];
+          tmem_ld32(tmem + quarter + h * GH + c, v);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            acc[C::KEEP ? c + i : 0] = fresh ? __uint_as_float(v[i])
+                                             : acc[C::KEEP ? c + i : 0] + __uint_as_float(v[i]);
+        }
+        fresh = false;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->g_empty);
+      }
+      return true;
+    };
+    for (int64_t u = u0; u < u1 && ok; ++u, ++it) {
+      const int64_t t = u / un.ct, j = u % un.ct;
+      if (!DW && (u == u0 || j == 0)) {
+        lse = a.lse[t * 128 + r];
+        tgt = a.tgt[t * 128 + r];
+      }
+      const int b = it & 1;
+      ok = mbar_wait_inline(&bars->z_full[b], (it >> 1) & 1, a.status, 718, abort, 32);
+      if (!ok) break;
+      tc_fence_after();
+      const uint8_t* st = stats + it % C::ST * 2048;
+#pragma unroll
+      for (int k = 0; k < HALF / 32; ++k) {
+        const int c0 = h * HALF + k * 32;
+        const uint32_t at = zbuf + quarter + b * C::NB + c0;
+        uint32_t v[32];
+        tmem_ld32(at, v);
+        tmem_wait_ld();
+        const float* cl = reinterpret_cast<const float*>(st) + c0;
+        const float* cg = reinterpret_cast<const float*>(st) + C::NB + c0;
+        const int* ctg = reinterpret_cast<const int*>(st) + 2 * C::NB + c0;
+        const int64_t w0 = j * C::NB + c0;
+        probs32<FORM, DW>(v, descale, (float)up, lse, tgt < 0 ? -1 : (int)max((int64_t)-1, min((int64_t)32, tgt - w0)),
+                          cl, cg, ctg, t * 128, r);
+        if (!DW && w0 + 32 > a.V) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (w0 + i >= a.V) v[i] = 0;
+        }
+        uint32_t o[32];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = __uint_as_float(v[2 * i]), y = __uint_as_float(v[2 * i + 1]);
+          if (FORM == kBf16) {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
+            o[i] = *reinterpret_cast<const uint32_t*>(&p);
+          } else {
+            const __half2 p = __floats2half2_rn(x, y);
+            o[i] = *reinterpret_cast<const uint32_t*>(&p);
+            const float2 f = __half22float2(p);
+            const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+            o[16 + i] = *reinterpret_cast<const uint32_t*>(&l);
+          }
+        }
+        if (FORM == kBf16)
+          tmem_st16(at, o);
+        else
+          tmem_st32(at, o);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->p_full[b]);
+      if (pending) {
+        ok = collect();
+        pending = false;
+        if (!ok) break;
+      }
+      const bool ends = u + 1 == u1 || j + 1 == un.ct;
+      if (++in_group == C::DRAIN || ends) {
+        in_group = 0;
+        pending = !ends;
+      }
+      if (!ends) continue;
+      ok = collect();
+      if (!ok) break;
+      fresh = true;
+      // the tile's result: finished where this CTA had all its units, else for the join
+      const int64_t f = t * un.ct;
+      const bool whole = u0 <= f && f + un.ct <= u1;
+      int64_t orow = t * 128 + r;
+      float s1 = 1.f, s2 = 1.f, s3 = 1.f;
+      if (DW) {
+        if (orow >= a.V) orow = -1;
+        if (FORM != kBf16) s1 = pow2(-up), s2 = pow2(-sx);
       } else {
-        float* g = static_cast<float*>(k.grad) + at;
-        *g = k.accumulate ? *g + acc[r] : acc[r];
+        s3 = a.g[orow];
+        orow = a.row[orow];
+        if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-sw);
+      }
+      float* pt = a.part + (((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, t)) * 128 + r) * a.H;
+#pragma unroll
+      for (int c = 0; c < GH; c += 32) {
+        const int col = h * GH + c;
+        uint32_t v[32];
+        if (C::KEEP) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(acc[C::KEEP ? c + i : 0]);
+        } else if (col < a.H) {
+          tmem_ld32(tmem + quarter + col, v);
+          tmem_wait_ld();
+        }
+        if (col >= a.H) continue;
+        float* x = reinterpret_cast<float*>(v);
+        if (!whole) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            *reinterpret_cast<float4*>(pt + col + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          continue;
+        }
+        if (orow < 0) continue;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = x[i] * s1 * s2 * s3;
+        if (out_bf16) {
+          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.out) + orow * a.H + col;
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            __nv_bfloat162 w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = __floats2bfloat162_rn(x[i + 2 * k], x[i + 2 * k + 1]);
+            *reinterpret_cast<uint4*>(o + i) = *reinterpret_cast<const uint4*>(w);
+          }
+        } else {
+          float* o = static_cast<float*>(a.out) + orow * a.H + col;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            float4 w = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            if (a.accumulate) {
+              const float4 p = *reinterpret_cast<const float4*>(o + i);
+              w = make_float4(w.x + p.x, w.y + p.y, w.z + p.z, w.w + p.w);
+            }
+            *reinterpret_cast<float4*>(o + i) = w;
+          }
+        }
+      }
+      if (!C::KEEP) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->g_empty);
       }
     }
   }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
 }
 
-template <typename T, int MODE>
-cudaError_t launch(const XentKernel& k, cudaStream_t st) {
-  const size_t smem = (2 * 64 * (size_t)(k.H + 1) + 64 * 65 + 6 * 64) * sizeof(float);
-  cudaError_t e = cudaFuncSetAttribute(k_xent<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)smem);
+// Tiles that several CTAs have parts of: the sum of the parts in the order of the CTAs.  A block
+// takes 32 rows x 32 columns; a dW without labelled rows is written as zeros here.
+__global__ void __launch_bounds__(256)
+    k_xent_bwd_join(BwdArgs a, int form, int nb, int G, int out_bf16) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int64_t rows = a.head[0], t = blockIdx.x;
+  const int64_t rt = a.dw ? (a.V + 127) / 128 : (rows + 127) / 128;
+  const Units un(rt, a.dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, G);
+  if (t >= rt) return;
+  const int hb = a.H / 32;
+  const int col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x & 7) * 4;
+  const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x >> 3);
+  int64_t orow = t * 128 + r;
+  float s1 = 1.f, s2 = 1.f, s3 = 1.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (un.ct > 0) {
+    const int c0 = un.owner(t * un.ct), c1 = un.owner(t * un.ct + un.ct - 1);
+    if (c0 == c1) return;
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+      const float4 p = *reinterpret_cast<const float4*>(
+          a.part + (((int64_t)c * 2 + un.slot(c, t)) * 128 + r) * a.H + col);
+      x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
+    }
+  }
+  if (a.dw) {
+    if (orow >= a.V) return;
+    if (form != kBf16) s1 = pow2(-a.head[3]), s2 = pow2(-a.head[1]);
+  } else {
+    s3 = a.g[orow];
+    orow = a.row[orow];
+    if (orow < 0) return;
+    if (form != kBf16) s1 = pow2(-15), s2 = pow2(-a.head[2]);
+  }
+  x = make_float4(x.x * s1 * s2 * s3, x.y * s1 * s2 * s3, x.z * s1 * s2 * s3, x.w * s1 * s2 * s3);
+  if (out_bf16) {
+    __nv_bfloat162 w[2] = {__floats2bfloat162_rn(x.x, x.y), __floats2bfloat162_rn(x.z, x.w)};
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + orow * a.H + col) =
+        *reinterpret_cast<const uint2*>(w);
+  } else {
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.out) + orow * a.H + col);
+    if (a.accumulate) {
+      const float4 p = *o;
+      x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
+    }
+    *o = x;
+  }
+}
+
+// ------------------------------------------------------------------------------ host
+struct Call {
+  int form, H, V, sms;
+  int64_t n;
+  Ws w;
+  char* base;
+  cudaStream_t st;
+  CUtensorMap x128, w128;  // boxes of 128 rows
+  template <typename P>
+  P* at(size_t off) const { return reinterpret_cast<P*>(base + off); }
+};
+
+// Count, gather and convert: fills everything the tile kernels read.
+cudaError_t prepare(const XentArgs& a, Call& c, RowArgs r) {
+  r.form = c.form;
+  r.x_bf16 = a.bf16;
+  r.n = a.n;
+  r.rb = c.w.rb;
+  r.nb = c.w.nb;
+  r.cap = c.w.cap;
+  r.vcap = c.w.vcap;
+  r.H = a.H;
+  r.V = a.V;
+  r.X = a.X;
+  r.W = a.W;
+  r.target = a.target;
+  r.head = c.at<int>(c.w.head);
+  r.counts = c.at<int>(c.w.counts);
+  r.amax = c.at<uint32_t>(c.w.amax);
+  r.row = c.at<int32_t>(c.w.row);
+  r.tgt = c.at<int32_t>(c.w.tgt);
+  r.lse = c.at<float>(c.w.lse);
+  r.g = c.at<float>(c.w.g);
+  r.x = c.at<uint16_t>(c.w.x);
+  r.w = c.at<uint16_t>(c.w.w);
+  r.status = a.status;
+  const int table = c.form == kBf16 ? 0 : kTableBlocks;
+  cudaError_t e;
+  if (c.w.nb > 1 || c.form != kBf16) {
+    e = launch_pdl(k_xent_count, dim3((unsigned)c.w.nb + table), dim3(256), 0, c.st, r);
+    if (e != cudaSuccess) return e;
+    note_launch();
+  }
+  e = launch_pdl(k_xent_rows, dim3((unsigned)c.w.nb + table), dim3(256), 0, c.st, r);
   if (e != cudaSuccess) return e;
-  const int64_t rows = MODE == kDW ? k.V : k.n;
-  k_xent<T, MODE><<<(unsigned)((rows + 63) / 64), 256, smem, st>>>(k);
   note_launch();
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
-XentKernel base(const XentArgs& a) {
-  XentKernel k{};
-  k.n = a.n;
-  k.H = a.H;
-  k.V = a.V;
-  k.X = a.X;
-  k.W = a.W;
-  k.target = a.target;
-  k.status = a.status;
-  return k;
+// Tensor maps over the gathered rows of X and over W (as it is, or its converted planes).
+bool map_x(const Call& c, CUtensorMap* m, int box) {
+  const int64_t rows = (c.form == kF16x2 ? 2 : 1) * c.w.cap;
+  return make_map_ld(m, c.base + c.w.x, rows, c.H, c.H, box);
+}
+bool map_w(const Call& c, const void* W, CUtensorMap* m, int box) {
+  if (c.form == kBf16) return make_map_ld(m, W, c.V, c.H, c.H, box);
+  return make_map_ld(m, c.base + c.w.w, (c.form == kF16x2 ? 2 : 1) * c.w.vcap, c.H, c.H, box);
+}
+
+template <int HC, int T>
+cudaError_t run_fwd(const Call& c, const void* W, const FwdArgs& f) {
+  using C = FCfg<HC, T>;
+  CUtensorMap mx, mw;
+  if (!map_x(c, &mx, 128) || !map_w(c, W, &mw, 256)) return cudaErrorInvalidValue;
+  cudaError_t e = cudaFuncSetAttribute(k_xent_fwd<HC, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       C::SMEM);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(k_xent_fwd<HC, T>, dim3(c.sms), dim3(kFwdThreads), C::SMEM, c.st, mx, mw, f);
+}
+
+template <int HC, int FORM, bool DW>
+cudaError_t run_bwd(const Call& c, const void* W, const BwdArgs& b, int out_bf16) {
+  using C = BCfg<HC, FORM>;
+  CUtensorMap ms, mb;
+  if (!(DW ? map_w(c, W, &ms, 128) && map_x(c, &mb, C::NB)
+           : map_x(c, &ms, 128) && map_w(c, W, &mb, C::NB)))
+    return cudaErrorInvalidValue;
+  cudaError_t e = cudaFuncSetAttribute(k_xent_bwd<HC, FORM, DW>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(k_xent_bwd<HC, FORM, DW>, dim3(c.sms), dim3(kBwdThreads), C::SMEM, c.st, ms, mb, b,
+                 out_bf16);
+  if (e != cudaSuccess) return e;
+  note_launch();
+  const int64_t tiles = DW ? c.w.vcap / 128 : c.w.cap / 128;
+  e = launch_pdl(k_xent_bwd_join, dim3((unsigned)tiles, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM,
+                 C::NB, c.sms, out_bf16);
+  if (e != cudaSuccess) return e;
+  note_launch();
+  return cudaSuccess;
+}
+
+template <int FORM, bool DW>
+cudaError_t run_bwd_h(const Call& c, const void* W, const BwdArgs& b, int out_bf16) {
+  switch ((c.H + 63) / 64) {
+    case 1: return run_bwd<1, FORM, DW>(c, W, b, out_bf16);
+    case 2: return run_bwd<2, FORM, DW>(c, W, b, out_bf16);
+    case 3: return run_bwd<3, FORM, DW>(c, W, b, out_bf16);
+    default: return run_bwd<4, FORM, DW>(c, W, b, out_bf16);
+  }
+}
+
+Call make_call(const XentArgs& a, int form, int backward, cudaStream_t st) {
+  Call c;
+  c.form = form;
+  c.H = a.H;
+  c.V = a.V;
+  c.n = a.n;
+  c.sms = gemm_tn_num_sms();
+  c.w = layout(form, a.n, a.H, a.V, backward, c.sms);
+  c.base = static_cast<char*>(a.ws);
+  c.st = st;
+  return c;
 }
 
 }  // namespace
 
-size_t xent_ws_bytes(int, int64_t, int, int, int) { return 256; }
+size_t xent_ws_bytes(int bf16, int64_t n, int H, int V, int backward) {
+  constexpr int kSms = 152;
+  if (!bf16) return layout(kF16x2, n, H, V, backward, kSms).total;
+  return layout(backward ? kF16x1 : kBf16, n, H, V, backward, kSms).total;
+}
 
 cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st) {
   if (a.n == 0) return cudaSuccess;
-  XentKernel k = base(a);
-  k.loss = loss;
-  k.lse = lse;
-  return a.bf16 ? launch<__nv_bfloat16, kLoss>(k, st) : launch<float, kLoss>(k, st);
+  Call c = make_call(a, a.bf16 ? kBf16 : kF16x2, 0, st);
+  RowArgs r{};
+  r.loss = loss;
+  r.lse_out = lse;
+  cudaError_t e = prepare(a, c, r);
+  if (e != cudaSuccess) return e;
+  const FwdArgs f{a.H, a.V, c.w.cap, c.w.vcap, c.at<int>(c.w.head), c.at<int32_t>(c.w.tgt),
+                  c.at<float>(c.w.hit), c.at<float2>(c.w.full), c.at<float2>(c.w.part), a.status};
+  switch ((a.H + 63) / 64 * 2 + (a.bf16 ? 0 : 1)) {
+    case 2: e = run_fwd<1, 1>(c, a.W, f); break;
+    case 3: e = run_fwd<1, 2>(c, a.W, f); break;
+    case 4: e = run_fwd<2, 1>(c, a.W, f); break;
+    case 5: e = run_fwd<2, 2>(c, a.W, f); break;
+    case 6: e = run_fwd<3, 1>(c, a.W, f); break;
+    case 7: e = run_fwd<3, 2>(c, a.W, f); break;
+    case 8: e = run_fwd<4, 1>(c, a.W, f); break;
+    default: e = run_fwd<4, 2>(c, a.W, f); break;
+  }
+  if (e != cudaSuccess) return e;
+  note_launch();
+  const int grid = (int)std::min<int64_t>((a.n + 7) / 8, 152 * 8);
+  e = launch_pdl(k_xent_join, dim3(grid), dim3(256), 0, st, a.V, c.w.cap, c.sms, f.head,
+                 c.at<int32_t>(c.w.row), f.hit, f.full, f.part, loss, lse);
+  if (e != cudaSuccess) return e;
+  note_launch();
+  return cudaSuccess;
 }
 
 cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, int grad_bf16,
                      void* dX, void* dW, int accumulate, cudaStream_t st) {
-  XentKernel k = base(a);
-  k.lse = const_cast<float*>(lse);
-  k.dloss = dloss;
-  k.grad_bf16 = grad_bf16;
-  k.accumulate = accumulate;
-  cudaError_t e = cudaSuccess;
-  if (dX && a.n > 0) {
-    k.grad = dX;
-    e = a.bf16 ? launch<__nv_bfloat16, kDX>(k, st) : launch<float, kDX>(k, st);
+  if (a.n == 0) {
+    if (!dW || accumulate) return cudaSuccess;
+    return cudaMemsetAsync(dW, 0, (size_t)a.V * a.H * (grad_bf16 ? 2 : 4), st);
   }
-  if (e == cudaSuccess && dW) {
-    k.grad = dW;
-    e = a.bf16 ? launch<__nv_bfloat16, kDW>(k, st) : launch<float, kDW>(k, st);
+  const int form = grad_bf16 ? kBf16 : a.bf16 ? kF16x1 : kF16x2;
+  Call c = make_call(a, form, 1, st);
+  RowArgs r{};
+  r.backward = 1;
+  r.grad_bf16 = grad_bf16;
+  r.clear_dx = dX && !accumulate;
+  r.lse_in = lse;
+  r.dloss = dloss;
+  r.dX = dX;
+  cudaError_t e = prepare(a, c, r);
+  if (e != cudaSuccess) return e;
+  BwdArgs b{};
+  b.H = a.H;
+  b.V = a.V;
+  b.accumulate = accumulate;
+  b.head = c.at<int>(c.w.head);
+  b.row = c.at<int32_t>(c.w.row);
+  b.tgt = c.at<int32_t>(c.w.tgt);
+  b.lse = c.at<float>(c.w.lse);
+  b.g = c.at<float>(c.w.g);
+  b.part = c.at<float>(c.w.part);
+  b.status = a.status;
+  for (int dw = 0; dw < 2; ++dw) {
+    b.dw = dw;
+    b.out = dw ? dW : dX;
+    b.scap = dw ? c.w.vcap : c.w.cap;
+    b.pcap = dw ? c.w.cap : c.w.vcap;
+    if (!b.out) continue;
+    if (form == kBf16)
+      e = dw ? run_bwd_h<kBf16, true>(c, a.W, b, 1) : run_bwd_h<kBf16, false>(c, a.W, b, 1);
+    else if (form == kF16x1)
+      e = dw ? run_bwd_h<kF16x1, true>(c, a.W, b, 0) : run_bwd_h<kF16x1, false>(c, a.W, b, 0);
+    else
+      e = dw ? run_bwd_h<kF16x2, true>(c, a.W, b, 0) : run_bwd_h<kF16x2, false>(c, a.W, b, 0);
+    if (e != cudaSuccess) return e;
   }
-  return e;
+  return cudaSuccess;
 }
 
 }  // namespace bg

@@ -120,3 +120,32 @@ def test_workspaces_grow_with_the_work(lib):
     for dt in (L.BG_F32, L.BG_BF16):
         for op in (L.BG_OP_XENT_FWD, L.BG_OP_XENT_BWD):
             assert 0 < lib.bg_xent_workspace_bytes(dt, n, H, V, op) < 64 * H * (n + V)
+
+
+def test_every_barrier_of_the_cross_entropy_kernels_is_initialised():
+    """Each kernel of xent.cu initialises exactly the mbarriers that its struct declares and that it
+    waits on or signals."""
+    import os
+    import re
+    src = open(os.path.join(os.path.dirname(L.LIB_PATH), "csrc", "xent.cu")).read()
+    kernels = re.findall(r"\n    k_xent_(fwd|bwd)\(const __grid_constant__.*?\n}\n", src, flags=re.S)
+    assert kernels == ["fwd", "bwd"]
+    for m in re.finditer(r"struct (Fwd|Bwd)Bars \{\s*uint64_t ([^;]*);", src):
+        fields = {f.split("[")[0].strip() for f in m.group(2).split(",")}
+        body = re.search(r"\n    k_xent_" + m.group(1).lower() + r"\(const __grid.*?\n}\n", src,
+                         flags=re.S).group(0)
+        init = set(re.findall(r"mbar_init\(&bars->(\w+)", body))
+        used = set(re.findall(r"&bars->(\w+)", body)) - {"tmem", "abort"}
+        assert init == fields == used, (fields, init, used)
+
+
+def test_register_shares_add_up_to_the_launch():
+    """setmaxnreg moves registers that the launch owns: the warpgroups' shares sum to 384 x 168."""
+    import os
+    import re
+    src = open(os.path.join(os.path.dirname(L.LIB_PATH), "csrc", "xent.cu")).read()
+    dec = set(re.findall(r"setmaxnreg\.dec\.sync\.aligned\.u32 (\d+)", src))
+    inc = set(re.findall(r"setmaxnreg\.inc\.sync\.aligned\.u32 (\d+)", src))
+    assert len(dec) == len(inc) == 1
+    assert "kBwdThreads = 384" in src
+    assert 128 * int(dec.pop()) + 256 * int(inc.pop()) <= 384 * 168
