@@ -386,6 +386,30 @@ struct Units {
     while (begin(c) > u) --c;
     return c;
   }
+  // staying and passing tile of the next unit of a run
+  struct Walk {
+    int t, j;
+    bool starts, ends;  // the unit is the first (last) of its staying tile in this run
+    int64_t left;
+    int ct;
+    __device__ Walk(const Units& u, int c) : ct((int)u.ct) {
+      const int64_t u0 = u.begin(c);
+      left = u.begin(c + 1) - u0;
+      t = left > 0 ? (int)(u0 / u.ct) : 0;
+      j = left > 0 ? (int)(u0 - (int64_t)t * u.ct) : 0;
+      starts = true;
+      ends = left == 1 || j + 1 == ct;
+    }
+    __device__ bool more() const { return left > 0; }
+    __device__ void next() {
+      --left;
+      starts = ends;
+      if (++j == ct) j = 0, ++t;
+      ends = left == 1 || j + 1 == ct;
+    }
+  };
+  // whether CTA c has all units of tile t
+  __device__ bool whole(int c, int64_t t) const { return begin(c) <= t * ct && t * ct + ct <= begin(c + 1); }
   // which of its two partial results CTA c keeps of tile t, one it shares with others
   __device__ int slot(int c, int64_t t) const { return t == begin(c) / ct ? 0 : 1; }
 };
@@ -516,7 +540,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   const uint32_t tmem = bars->tmem;
   const int64_t rows = a.head[0];
   const Units un((rows + 127) / 128, (a.V + 255) / 256, gridDim.x);
-  const int64_t u0 = un.begin(blockIdx.x), u1 = un.begin(blockIdx.x + 1);
+  Units::Walk w(un, blockIdx.x);
 
   if (warp == 8) {
     if (lane == 0) {
@@ -524,15 +548,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
       tma_prefetch_desc(&tmW);
       uint32_t it = 0, seg = 0;
       bool ok = true;
-      for (int64_t u = u0; u < u1 && ok; ++u) {
-        const int64_t t = u / un.ct, j = u % un.ct;
-        if (u == u0 || j == 0) {
+      for (; w.more() && ok; w.next()) {
+        if (w.starts) {
           ok = seg == 0 || mbar_wait(&bars->a_empty, (seg - 1) & 1, a.status, 701, abort, 32);
           if (!ok) break;
           mbar_expect_tx(&bars->a_full, C::A_BYTES);
           for (int p = 0; p < T * HC; ++p)
             tma_load_2d(smem + p * 16384, &tmX, &bars->a_full, p % HC * 64,
-                        (int)((p / HC) * a.cap + t * 128));
+                        (int)((p / HC) * a.cap) + w.t * 128);
           ++seg;
         }
         for (int p = 0; p < C::NP && ok; ++p, ++it) {
@@ -541,7 +564,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
           if (!ok) break;
           mbar_expect_tx(&bars->full[s], C::PIECE);
           tma_load_2d(ring + s * C::PIECE, &tmW, &bars->full[s], p % HC * 64,
-                      (int)((T == 2 && p < HC ? a.vcap : 0) + j * 256));
+                      (int)(T == 2 && p < HC ? a.vcap : 0) + w.j * 256);
         }
       }
       if (*abort) {  // copies in flight land before the block leaves
@@ -555,12 +578,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   } else if (warp == 9) {
     const bool leader = elect_one_sync();
     const uint32_t idesc = idesc16(T == 1, 256, 0);
-    const uint32_t A = smem_u32(smem), R = smem_u32(ring);
+    const uint64_t A = desc_sw128_kmajor(smem_u32(smem)), R = desc_sw128_kmajor(smem_u32(ring));
     uint32_t it = 0, seg = 0, n = 0;
     bool ok = true;
-    for (int64_t u = u0; u < u1 && ok; ++u, ++n) {
-      const int64_t j = u % un.ct;
-      if (u == u0 || j == 0) {
+    for (; w.more() && ok; w.next(), ++n) {
+      if (w.starts) {
         ok = mbar_wait(&bars->a_full, seg & 1, a.status, 703, abort);
         ++seg;
       }
@@ -574,17 +596,19 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         // two terms: high x low, low x high, then high x high, so that the accumulator is small
         // (and loses little) in the first two thirds
         const int ab = T == 2 && p >= HC && p < 2 * HC ? p : p % HC;
-        const int steps = min(4, (a.H - p % HC * 64) / 16);
-        for (int kk = 0; kk < steps; ++kk)
-          if (leader)
-            mma_ss(tmem + b * 256, desc_sw128_kmajor(A + ab * 16384 + kk * 32),
-                   desc_sw128_kmajor(R + s * C::PIECE + kk * 32), idesc, p > 0 || kk > 0);
+        // past H the pieces hold zeros; a step is 32 bytes, 2 in a descriptor's units
+        const uint64_t ad = A + ab * (16384 >> 4), bd = R + s * (C::PIECE >> 4);
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_ss(tmem + b * 256, ad + kk * 2, bd + kk * 2, idesc, p > 0 || kk > 0);
+        }
         if (leader) tc_commit(&bars->empty[s]);
         __syncwarp();
       }
       if (ok && leader) {
         tc_commit(&bars->s_full[b]);
-        if (u + 1 == u1 || j + 1 == un.ct) tc_commit(&bars->a_empty);
+        if (w.ends) tc_commit(&bars->a_empty);
       }
       __syncwarp();
     }
@@ -601,9 +625,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     float m = -3.0e38f, l = 0.f;
     int tgt = -1;
     uint32_t n = 0;
-    for (int64_t u = u0; u < u1; ++u, ++n) {
-      const int64_t t = u / un.ct, j = u % un.ct;
-      if (u == u0 || j == 0) {
+    for (; w.more(); w.next(), ++n) {
+      const int64_t t = w.t, j = w.j;
+      if (w.starts) {
         m = -3.0e38f;
         l = 0.f;
         tgt = a.tgt[t * 128 + r];
@@ -639,11 +663,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->s_empty[b]);
-      if (u + 1 == u1 || j + 1 == un.ct) {
-        const int64_t f = t * un.ct;
-        const bool whole = u0 <= f && f + un.ct <= u1;
+      if (w.ends) {
         // the sum's reference is m itself, so that the join undoes exactly what was done here
-        if (whole)
+        if (un.whole(blockIdx.x, t))
           a.full[h * a.cap + t * 128 + r] = make_float2(m, l);
         else
           a.part[(((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, t)) * 2 + h) * 128 + r] =
@@ -660,43 +682,47 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   }
 }
 
-// One warp a labelled row: its maxima and sums together, lse and loss.
+// A labelled row's maxima and sums together, lse and loss.  `lanes` threads share a row: 32 where a row
+// may have parts in every CTA, 1 where it has few.
 __global__ void __launch_bounds__(256)
-    k_xent_join(int V, int64_t cap, int G, const int* __restrict__ head,
+    k_xent_join(int V, int64_t cap, int G, int lanes, const int* __restrict__ head,
                 const int32_t* __restrict__ row, const float* __restrict__ hit,
                 const float2* __restrict__ full, const float2* __restrict__ part,
                 float* __restrict__ loss, float* __restrict__ lse) {
   grid_dep_launch();
   grid_dep_wait();
-  const int lane = threadIdx.x & 31;
   const int64_t rows = head[0];
   const Units un((rows + 127) / 128, (V + 255) / 256, G);
-  for (int64_t s = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); s < rows; s += (int64_t)gridDim.x * 8) {
-    const int64_t t = s / 128;
-    const int r = (int)(s % 128);
+  // a block's 256 / lanes rows lie in at most two tiles, a warp's in one
+  const int64_t s = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+  const int sub = threadIdx.x % lanes, r = (int)(s % 128);
+  const int64_t t = s / 128;
+  float m = -3.0e38f, l = 0.f;
+  if (s < rows) {
     const int c0 = un.owner(t * un.ct), c1 = un.owner(t * un.ct + un.ct - 1);
-    float m = -3.0e38f, l = 0.f;
     const int n = c0 == c1 ? 2 : 2 * (c1 - c0 + 1);
-    for (int i = lane; i < n; i += 32) {
+    for (int i = sub; i < n; i += lanes) {
       const int c = c0 + i / 2;
       const float2 p = c0 == c1 ? full[i * cap + s]
-                                : part[(((int64_t)c * 2 + un.slot(c, t)) * 2 + (i & 1)) * 128 + r];
+                                : part[(((int64_t)c * 2 + (c == c0 ? un.slot(c, t) : 0)) * 2 + (i & 1)) * 128 + r];
       const float mn = fmaxf(m, p.x);
       l = l * ex2(m - mn) + p.y * ex2(p.x - mn);
       m = mn;
     }
-    float top = m;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    l *= ex2(m - top);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (lane == 0) {
-      // top is c z of the largest logit with c = kLog2e as rounded: divide by that very number
-      const float v = (float)(((double)top + log2((double)l)) / (double)kLog2e);
-      lse[row[s]] = v;
-      loss[row[s]] = v - hit[s];
-    }
+  }
+  float top = m;
+  for (int o = lanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  l *= ex2(m - top);
+  for (int o = lanes / 2; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  if (sub == 0 && s < rows) {
+    // (top + log2 l) / c with c = kLog2e as it was rounded: c' = 1 / c in two parts, so that the only
+    // error that counts is the result's own rounding
+    constexpr float inv = (float)(1.0 / (double)kLog2e), rest = (float)(1.0 / (double)kLog2e - (double)inv);
+    const float lg = log2f(l), hi = top * inv;
+    const float lo = fmaf(top, inv, -hi) + fmaf(top, rest, lg * inv);
+    const float v = hi + lo;
+    lse[row[s]] = v;
+    loss[row[s]] = (hi - hit[s]) + lo;
   }
 }
 
@@ -782,14 +808,19 @@ __device__ __forceinline__ void probs32(uint32_t* v, float descale, float up, fl
       }
     }
     const int64_t at = (int64_t)col_tgt[lane] - first_row;
-    unsigned hits = __ballot_sync(0xffffffffu, at >= 0 && at < 128);
-    if (hits) {
+    if (__any_sync(0xffffffffu, at >= 0 && at < 128)) {
+      // frequent tokens have hits in every unit: all 32 columns at once, without branches
+      const int mine = (int)first_row + r;
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (hits >> i & 1) {
-          if (col_tgt[i] - first_row == r)
-            v[i] = __float_as_uint(__uint_as_float(v[i]) - col_g[i] * upg);
-        }
+      for (int i = 0; i < 32; i += 4) {
+        const int4 tt = *reinterpret_cast<const int4*>(col_tgt + i);
+        const float4 gg = *reinterpret_cast<const float4*>(col_g + i);
+        const int tc[4] = {tt.x, tt.y, tt.z, tt.w};
+        const float gc[4] = {gg.x, gg.y, gg.z, gg.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (tc[k] == mine) v[i + k] = __float_as_uint(fmaf(gc[k], -upg, __uint_as_float(v[i + k])));
+      }
     }
   }
 }
@@ -837,7 +868,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   const int64_t rows = a.head[0];
   const Units un(DW ? (a.V + 127) / 128 : (rows + 127) / 128,
                  DW ? (rows + C::NB - 1) / C::NB : (a.V + C::NB - 1) / C::NB, gridDim.x);
-  const int64_t u0 = un.begin(blockIdx.x), u1 = un.begin(blockIdx.x + 1);
+  Units::Walk w(un, blockIdx.x);
 
   if (warp >= 10) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -848,15 +879,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       tma_prefetch_desc(&tmB);
       uint32_t it = 0, seg = 0;
       bool ok = true;
-      for (int64_t u = u0; u < u1 && ok; ++u, ++it) {
-        const int64_t t = u / un.ct, j = u % un.ct;
-        if (u == u0 || j == 0) {
+      for (; w.more() && ok; w.next(), ++it) {
+        if (w.starts) {
           ok = seg == 0 || mbar_wait_inline(&bars->s_empty, (seg - 1) & 1, a.status, 711, abort, 32);
           if (!ok) break;
           mbar_expect_tx(&bars->s_full, C::S_BYTES);
           for (int p = 0; p < C::T * HC; ++p)
             tma_load_2d(smem + p * 16384, &tmS, &bars->s_full, p % HC * 64,
-                        (int)((p / HC) * a.scap + t * 128));
+                        (int)((p / HC) * a.scap) + w.t * 128);
           ++seg;
         }
         const int s = it % C::ST;
@@ -865,11 +895,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         mbar_expect_tx(&bars->full[s], C::B_BYTES + (DW ? C::STATS : 0));
         for (int p = 0; p < C::T * HC; ++p)
           tma_load_2d(ring + s * C::B_BYTES + p * C::BOX, &tmB, &bars->full[s], p % HC * 64,
-                      (int)((p / HC) * a.pcap + j * C::NB));
+                      (int)((p / HC) * a.pcap) + w.j * C::NB);
         if (DW) {
-          bulk_load(stats + s * 2048, a.lse + j * C::NB, C::NB * 4, &bars->full[s]);
-          bulk_load(stats + s * 2048 + C::NB * 4, a.g + j * C::NB, C::NB * 4, &bars->full[s]);
-          bulk_load(stats + s * 2048 + C::NB * 8, a.tgt + j * C::NB, C::NB * 4, &bars->full[s]);
+          bulk_load(stats + s * 2048, a.lse + (int64_t)w.j * C::NB, C::NB * 4, &bars->full[s]);
+          bulk_load(stats + s * 2048 + C::NB * 4, a.g + (int64_t)w.j * C::NB, C::NB * 4, &bars->full[s]);
+          bulk_load(stats + s * 2048 + C::NB * 8, a.tgt + (int64_t)w.j * C::NB, C::NB * 4, &bars->full[s]);
         }
       }
       if (*abort) {  // copies in flight land before the block leaves
@@ -884,33 +914,42 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     const bool leader = elect_one_sync();
     const uint32_t iz = idesc16(FORM == kBf16, C::NB, 0), ig = idesc16(FORM == kBf16, a.H, 1);
-    const uint32_t S = smem_u32(smem), R = smem_u32(ring);
-    const int ks = a.H / 16;
-    // z = S B^T of the unit in ring stage s; two terms: low x high and high x low first
+    // a descriptor's address field is in 16 bytes
+    const uint64_t S = desc_sw128_kmajor(smem_u32(smem)), RK = desc_sw128_kmajor(smem_u32(ring)),
+                   RN = desc_sw128_mnmajor(smem_u32(ring), C::BOX);
+    // z = S B^T of the unit in ring stage s (past H both hold zeros); two terms: low x high and
+    // high x low first
     auto z_product = [&](int s, int b) {
-      const uint32_t B = R + s * C::B_BYTES, d = zbuf + b * C::NB;
+      const uint64_t B = RK + s * (C::B_BYTES >> 4);
+      const uint32_t d = zbuf + b * C::NB;
       constexpr int n = C::T == 2 ? 3 : 1;
+#pragma unroll
       for (int pr = 0; pr < n; ++pr) {
-        const uint32_t as = S + (n == 3 && pr == 0 ? HC * 16384 : 0);
-        const uint32_t bs = B + (n == 3 && pr == 1 ? HC * C::BOX : 0);
-        for (int k = 0; k < ks; ++k)
-          if (leader)
-            mma_ss(d, desc_sw128_kmajor(as + (k >> 2) * 16384 + (k & 3) * 32),
-                   desc_sw128_kmajor(bs + (k >> 2) * C::BOX + (k & 3) * 32), iz, pr > 0 || k > 0);
+        const uint64_t as = S + (n == 3 && pr == 0 ? HC * (16384 >> 4) : 0);
+        const uint64_t bs = B + (n == 3 && pr == 1 ? HC * (C::BOX >> 4) : 0);
+        if (leader) {
+#pragma unroll
+          for (int k = 0; k < HC * 4; ++k)
+            mma_ss(d, as + (k >> 2) * (16384 >> 4) + (k & 3) * 2,
+                   bs + (k >> 2) * (C::BOX >> 4) + (k & 3) * 2, iz, pr > 0 || k > 0);
+        }
       }
     };
     // G (+)= P B, small products first
     auto g_product = [&](int s, int b, bool add) {
-      const uint32_t B = R + s * C::B_BYTES, p = zbuf + b * C::NB;
+      const uint64_t B = RN + s * (C::B_BYTES >> 4);
+      const uint32_t p = zbuf + b * C::NB;
       constexpr int n = C::T == 2 ? 3 : C::PT;
+#pragma unroll
       for (int pr = 0; pr < n; ++pr) {
         const uint32_t pa = p + (C::PT == 2 && pr == 0 ? 16 : 0);
-        const uint32_t bs = B + (n == 3 && pr == 1 ? HC * C::BOX : 0);
+        const uint64_t bs = B + (n == 3 && pr == 1 ? HC * (C::BOX >> 4) : 0);
+        if (leader) {
 #pragma unroll
-        for (int k = 0; k < C::NB / 16; ++k)
-          if (leader)
-            mma_ts(tmem, pa + (k >> 1) * 32 + (k & 1) * 8, desc_sw128_mnmajor(bs + k * 2048, C::BOX),
-                   ig, add || pr > 0 || k > 0);
+          for (int k = 0; k < C::NB / 16; ++k)
+            mma_ts(tmem, pa + (k >> 1) * 32 + (k & 1) * 8, bs + k * (2048 >> 4), ig,
+                   add || pr > 0 || k > 0);
+        }
       }
     };
     uint32_t it = 0, seg = 0, groups = 0;
@@ -933,10 +972,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       }
       __syncwarp();
     };
-    for (int64_t u = u0; u < u1 && ok; ++u, ++it) {
-      const int64_t j = u % un.ct;
+    for (; w.more() && ok; w.next(), ++it) {
       if (C::ST == 1 && it > 0) second(it - 1, last);
-      if (u == u0 || j == 0) {
+      if (w.starts) {
         ok = ok && mbar_wait_inline(&bars->s_full, seg & 1, a.status, 715, abort);
         ++seg;
       }
@@ -945,14 +983,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       if (!ok) break;
       tc_fence_after();
       z_product(s, it & 1);
-      const bool ends = u + 1 == u1 || j + 1 == un.ct;
       if (leader) {
         tc_commit(&bars->z_full[it & 1]);
-        if (ends) tc_commit(&bars->s_empty);
+        if (w.ends) tc_commit(&bars->s_empty);
       }
       __syncwarp();
       if (C::ST > 1 && it > 0) second(it - 1, last);
-      last = ends;
+      last = w.ends;
     }
     if (it > 0) second(it - 1, last);
     if (leader) tc_commit(&bars->drain);
@@ -998,9 +1035,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       }
       return true;
     };
-    for (int64_t u = u0; u < u1 && ok; ++u, ++it) {
-      const int64_t t = u / un.ct, j = u % un.ct;
-      if (!DW && (u == u0 || j == 0)) {
+    for (; w.more() && ok; w.next(), ++it) {
+      const int64_t t = w.t, j = w.j;
+      if (!DW && w.starts) {
         lse = a.lse[t * 128 + r];
         tgt = a.tgt[t * 128 + r];
       }
@@ -1056,18 +1093,16 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         pending = false;
         if (!ok) break;
       }
-      const bool ends = u + 1 == u1 || j + 1 == un.ct;
-      if (++in_group == C::DRAIN || ends) {
+      if (++in_group == C::DRAIN || w.ends) {
         in_group = 0;
-        pending = !ends;
+        pending = !w.ends;
       }
-      if (!ends) continue;
+      if (!w.ends) continue;
       ok = collect();
       if (!ok) break;
       fresh = true;
       // the tile's result: finished where this CTA had all its units, else for the join
-      const int64_t f = t * un.ct;
-      const bool whole = u0 <= f && f + un.ct <= u1;
+      const bool whole = un.whole(blockIdx.x, t);
       int64_t orow = t * 128 + r;
       float s1 = 1.f, s2 = 1.f, s3 = 1.f;
       if (DW) {
@@ -1139,31 +1174,48 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   }
 }
 
-// Tiles that several CTAs have parts of: the sum of the parts in the order of the CTAs.  A block
-// takes 32 rows x 32 columns; a dW without labelled rows is written as zeros here.
+// Tiles that several CTAs have parts of: the sum of the parts in the order of the CTAs.  Block row c
+// takes the tile that CTA c is the first to begin inside of, 32 rows x 32 columns a block; without
+// labelled rows the tiles of dW are written as zeros here.
 __global__ void __launch_bounds__(256)
-    k_xent_bwd_join(BwdArgs a, int form, int nb, int G, int out_bf16) {
+    k_xent_bwd_join(BwdArgs a, int form, int nb, int out_bf16) {
   grid_dep_launch();
   grid_dep_wait();
-  const int64_t rows = a.head[0], t = blockIdx.x;
+  const int64_t rows = a.head[0];
   const int64_t rt = a.dw ? (a.V + 127) / 128 : (rows + 127) / 128;
-  const Units un(rt, a.dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, G);
-  if (t >= rt) return;
+  const Units un(rt, a.dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, gridDim.x);
   const int hb = a.H / 32;
   const int col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x & 7) * 4;
   const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x >> 3);
+  if (un.ct == 0) {
+    if (!a.dw || a.accumulate) return;
+    for (int64_t v = (int64_t)blockIdx.x * 128 + r; v < a.V; v += (int64_t)gridDim.x * 128) {
+      if (out_bf16)
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + v * a.H + col) = make_uint2(0, 0);
+      else
+        *reinterpret_cast<float4*>(static_cast<float*>(a.out) + v * a.H + col) =
+            make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    return;
+  }
+  const int c = blockIdx.x;
+  const int64_t begin = un.begin(c);
+  if (c >= un.G || c == 0 || begin % un.ct == 0) return;
+  const int64_t t = begin / un.ct, first = t * un.ct, end = first + un.ct;
+  if (un.begin(c - 1) > first) return;  // an earlier CTA begins inside the tile too
   int64_t orow = t * 128 + r;
   float s1 = 1.f, s2 = 1.f, s3 = 1.f;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (un.ct > 0) {
-    const int c0 = un.owner(t * un.ct), c1 = un.owner(t * un.ct + un.ct - 1);
-    if (c0 == c1) return;
-#pragma unroll 4
-    for (int c = c0; c <= c1; ++c) {
-      const float4 p = *reinterpret_cast<const float4*>(
-          a.part + (((int64_t)c * 2 + un.slot(c, t)) * 128 + r) * a.H + col);
-      x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
-    }
+  // CTA c - 1 has the first part (in its second place unless the tile is its first), the others begin
+  // with this tile
+  const float* part = a.part + (int64_t)r * a.H + col;
+  const int64_t stride = 128LL * a.H;
+  float4 x = *reinterpret_cast<const float4*>(part + ((int64_t)(c - 1) * 2 + un.slot(c - 1, t)) * stride);
+  int last = c;
+  while (last + 1 < un.G && un.begin(last + 1) < end) ++last;
+#pragma unroll 8
+  for (int k = c; k <= last; ++k) {
+    const float4 p = *reinterpret_cast<const float4*>(part + (int64_t)k * 2 * stride);
+    x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
   }
   if (a.dw) {
     if (orow >= a.V) return;
@@ -1273,9 +1325,8 @@ cudaError_t run_bwd(const Call& c, const void* W, const BwdArgs& b, int out_bf16
                  out_bf16);
   if (e != cudaSuccess) return e;
   note_launch();
-  const int64_t tiles = DW ? c.w.vcap / 128 : c.w.cap / 128;
-  e = launch_pdl(k_xent_bwd_join, dim3((unsigned)tiles, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM,
-                 C::NB, c.sms, out_bf16);
+  e = launch_pdl(k_xent_bwd_join, dim3(c.sms, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM, C::NB,
+                 out_bf16);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
@@ -1334,8 +1385,10 @@ cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st
   }
   if (e != cudaSuccess) return e;
   note_launch();
-  const int grid = (int)std::min<int64_t>((a.n + 7) / 8, 152 * 8);
-  e = launch_pdl(k_xent_join, dim3(grid), dim3(256), 0, st, a.V, c.w.cap, c.sms, f.head,
+  // row tiles x CTAs a tile <= SMs + row tiles: with 8 tiles or more a row has at most 20 parts or so
+  const int lanes = c.w.cap / 128 < 8 ? 32 : 1;
+  const int64_t grid = (a.n * lanes + 255) / 256;
+  e = launch_pdl(k_xent_join, dim3((unsigned)grid), dim3(256), 0, st, a.V, c.w.cap, c.sms, lanes, f.head,
                  c.at<int32_t>(c.w.row), f.hit, f.full, f.part, loss, lse);
   if (e != cudaSuccess) return e;
   note_launch();
