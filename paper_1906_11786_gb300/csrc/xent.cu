@@ -7,7 +7,7 @@
 //   k_xent_count, k_xent_rows   the labelled rows of X, gathered side by side (rows left out cost
 //                               nothing after this and may hold anything), and the operands' 16-bit forms
 //   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, running maximum and sum
-//   k_xent_bwd (+ join)         128 x 128 tiles of z recomputed, P written back over z in tensor
+//   k_xent_bwd (+ join)         128 x 128 (64) tiles of z recomputed, P written back over z in tensor
 //                               memory as the A operand of the second product; once with the rows of X
 //                               staying (dX) and once with the rows of W (dW)
 // A staying tile of 128 rows against one passing tile is a unit; the units of a launch, staying tile
@@ -62,7 +62,7 @@ inline int64_t rows_per_block(int64_t n) {
 
 struct Ws {
   int64_t rb, nb, cap, vcap;  // rows a block, blocks, X rows and W rows rounded up to whole tiles
-  size_t head, counts, amax, row, tgt, lse, g, hit, x, w, full, part, total;
+  size_t head, counts, amax, row, tgt, nlse, g, hit, x, w, full, part, total;
 };
 
 Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
@@ -83,13 +83,13 @@ Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
   w.amax = take((size_t)(2 * w.nb + kTableBlocks) * 4);
   w.row = take((size_t)w.cap * 4);
   w.tgt = take((size_t)w.cap * 4);
-  w.lse = take((size_t)w.cap * 4);
+  w.nlse = take((size_t)w.cap * 4);
   w.g = take((size_t)w.cap * 4);
   w.hit = take((size_t)w.cap * 4);
   w.x = take((size_t)terms * w.cap * H * 2);
   w.w = take(form == kBf16 ? 0 : (size_t)terms * w.vcap * H * 2);
-  w.full = take(backward ? 0 : (size_t)w.cap * 16);
-  w.part = take(backward ? (size_t)ctas * 2 * 128 * H * 4 : (size_t)ctas * 2 * 256 * 8);
+  w.full = take(backward ? 0 : (size_t)w.cap * 32);
+  w.part = take(backward ? (size_t)ctas * 2 * 128 * H * 4 : (size_t)ctas * 2 * 512 * 8);
   w.total = o;
   return w;
 }
@@ -109,7 +109,7 @@ struct RowArgs {
   uint32_t* amax;  // [nb] of X, [nb] of dloss, [kTableBlocks] of W: bits of the largest finite |x|
   int32_t* row;
   int32_t* tgt;
-  float* lse;
+  float* nlse;  // -lse (bf16 form: times log2 e)
   float* g;
   uint16_t* x;
   uint16_t* w;
@@ -239,7 +239,7 @@ __device__ __forceinline__ void put8(uint16_t* dst, int64_t plane, int64_t at, i
 
 // The labelled rows, side by side in their order: X in the form's terms, the row each came from, its
 // target and, for the gradient, its lse and g; the outputs of the rows left out.  The last block adds
-// empty rows up to a whole tile (zeros, lse = +inf: every probability 0) and the number of rows.  The
+// empty rows up to a whole tile (zeros, -lse = -inf: every probability 0) and the number of rows.  The
 // blocks from nb on convert W.
 __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
   __shared__ int wsum[8];
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
       a.row[slot] = (int32_t)i;
       a.tgt[slot] = t;
       if (a.backward) {
-        a.lse[slot] = a.form == kBf16 ? a.lse_in[i] * kLog2e : a.lse_in[i];
+        a.nlse[slot] = a.form == kBf16 ? -a.lse_in[i] * kLog2e : -a.lse_in[i];
         a.g[slot] = a.dloss[i];
       }
     } else if (i < r1 && !a.backward) {
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
       a.row[s] = -1;
       a.tgt[s] = -1;
       if (a.backward) {
-        a.lse[s] = INFINITY;
+        a.nlse[s] = -INFINITY;
         a.g[s] = 0.f;
       }
     }
@@ -420,13 +420,66 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+// two fp32 at a time
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pack2u(uint32_t a, uint32_t b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
-      "%14,%15,%16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+// Fragments of 16 lanes: a thread has, of every 8 columns, columns 2 (l % 4) and + 1 in rows l / 4 and
+// + 8 (.16x256b); stores of packed pairs: of every 4 columns, column l % 4 in those rows (.16x128b).
+__device__ __forceinline__ void tmem_ld_frag32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_frag16(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+                 "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st_frag8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 
 // Shared-memory descriptor of an MN-major operand with the 128-byte swizzle: rows of 64 elements along
@@ -447,10 +500,12 @@ __device__ __forceinline__ uint32_t idesc16(int bf16, int N, int b_mn) {
   return (bf16 ? idesc_bf16_f32(128, N) : idesc_f16_f32(128, N)) | (uint32_t)b_mn << 16;
 }
 
-constexpr int kFwdThreads = 320;  // 8 epilogue warps, a TMA warp, an MMA warp
-// The backward adds two idle warps, so that registers can move between whole warpgroups: 384 x 168 at
-// launch = 256 x 224 (epilogue, which holds up to 128 gradient sums a thread) + 128 x 56.
-constexpr int kBwdThreads = 384;
+constexpr int kFwdThreads = 576;  // 16 epilogue warps, a TMA warp, an MMA warp
+// The backward has 16 epilogue warps, a TMA warp, an MMA warp for each product and an idle warp, so that
+// registers can move between whole warpgroups: of 640 x 96 at launch, 512 x 104 go to the epilogue (up to
+// 64 gradient sums a thread) and 128 x 64 stay.
+constexpr int kBwdThreads = 640;
+constexpr int kMaxStages = 6;
 
 // ------------------------------------------------------------------------------ forward
 struct FwdArgs {
@@ -459,8 +514,8 @@ struct FwdArgs {
   const int* head;
   const int32_t* tgt;
   float* hit;    // [cap] logit of the target
-  float2* full;  // [2][cap] maximum and sum of each half, of the tiles one CTA has all units of
-  float2* part;  // [G][2][2][128] of the others
+  float2* full;  // [4][cap] reference and sum of each quarter, of the tiles one CTA has all units of
+  float2* part;  // [G][2][4][128] of the others
   int* status;
 };
 
@@ -483,22 +538,42 @@ struct FwdBars {
   int abort;
 };
 
-// Running maximum (in units of c z) and sum of 32 columns more.
-__device__ __forceinline__ void online32(const uint32_t* v, float c, float& m, float& l) {
-  float top = __uint_as_float(v[0]);
+// Sum of exp2(c z - m) over 32 columns.
+__device__ __forceinline__ float sum32(const uint32_t* v, float c, float m) {
+  const uint64_t c2 = pack2(c, c), m2 = pack2(-m, -m);
+  uint64_t s[2] = {0, 0};
 #pragma unroll
-  for (int j = 1; j < 32; ++j) top = fmaxf(top, __uint_as_float(v[j]));
-  const float mn = fmaxf(m, top * c);
-  float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+  for (int j = 0; j < 32; j += 4)
 #pragma unroll
-  for (int j = 0; j < 32; j += 4) {
-    s0 += ex2(fmaf(__uint_as_float(v[j]), c, -mn));
-    s1 += ex2(fmaf(__uint_as_float(v[j + 1]), c, -mn));
-    s2 += ex2(fmaf(__uint_as_float(v[j + 2]), c, -mn));
-    s3 += ex2(fmaf(__uint_as_float(v[j + 3]), c, -mn));
+    for (int k = 0; k < 2; ++k) {
+      float a, b;
+      unpack2(fma2(pack2u(v[j + 2 * k], v[j + 2 * k + 1]), c2, m2), a, b);
+      s[k] = add2(s[k], pack2(ex2(a), ex2(b)));
+    }
+  float a, b;
+  unpack2(add2(s[0], s[1]), a, b);
+  return a + b;
+}
+
+// 32 columns more to a row's sum l = sum exp2(c z - m).  m need not be the running maximum, only near
+// it: it is the maximum of the row's first columns, and moves up when a sum passes 2^40 (so nothing
+// overflows, and what an early m made too large keeps all its bits).  This takes the maximum out of
+// the common path.
+__device__ __forceinline__ void online32(const uint32_t* v, float c, bool first, float& m, float& l) {
+  float s = 0.f;
+  if (!first) s = sum32(v, c, m);
+  if (first || !(s <= 0x1p40f)) {
+    float top[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
+#pragma unroll
+    for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(v[j]));
+    const float mn = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c);
+    l *= ex2(m - mn);
+    m = mn;
+    s = sum32(v, c, m);
   }
-  l = fmaf(l, ex2(m - mn), (s0 + s1) + (s2 + s3));
-  m = mn;
+  l += s;
 }
 
 template <int HC, int T>
@@ -522,13 +597,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->s_full[b], 1);
-      mbar_init(&bars->s_empty[b], 8);
+      mbar_init(&bars->s_empty[b], 16);
     }
     mbar_init(&bars->drain, 1);
     bars->abort = 0;
     fence_mbar_init();
   }
-  if (warp == 9) {
+  if (warp == 17) {
     tmem_alloc(&bars->tmem, 512);
     tmem_relinquish();
   }
@@ -542,7 +617,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   const Units un((rows + 127) / 128, (a.V + 255) / 256, gridDim.x);
   Units::Walk w(un, blockIdx.x);
 
-  if (warp == 8) {
+  if (warp == 16) {
     if (lane == 0) {
       tma_prefetch_desc(&tmX);
       tma_prefetch_desc(&tmW);
@@ -575,7 +650,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
           }
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == 17) {
     const bool leader = elect_one_sync();
     const uint32_t idesc = idesc16(T == 1, 256, 0);
     const uint64_t A = desc_sw128_kmajor(smem_u32(smem)), R = desc_sw128_kmajor(smem_u32(ring));
@@ -617,65 +692,66 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     for (uint32_t k = 0; k < (1u << 24) && !mbar_try(&bars->drain, 0); ++k) {
     }
   } else {
-    // warps 0-3: columns 0-127 of a tile, warps 4-7: columns 128-255; a thread is a row
-    const int q = warp & 3, h = warp >> 2, r = q * 32 + lane;
+    // a thread is a row; each warpgroup has 64 columns of a tile
+    const int q = warp & 3, wg = warp >> 2, r = q * 32 + lane;
     float c = kLog2e;
     if (T == 2) c *= pow2(max(-126, min(127, -(a.head[1] + a.head[2]))));
-    const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + h * 128;
+    const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + wg * 64;
     float m = -3.0e38f, l = 0.f;
     int tgt = -1;
     uint32_t n = 0;
     for (; w.more(); w.next(), ++n) {
-      const int64_t t = w.t, j = w.j;
       if (w.starts) {
         m = -3.0e38f;
         l = 0.f;
-        tgt = a.tgt[t * 128 + r];
+        tgt = a.tgt[w.t * 128 + r];
       }
       const int b = n & 1;
-      if (!mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 32)) break;
+      if (!mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 20)) break;
       tc_fence_after();
-      const int64_t v0 = j * 256 + h * 128;
       uint32_t x[2][32];
       tmem_ld32(base + b * 256, x[0]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 2; ++k) {
         tmem_wait_ld();
-        if (k < 3) tmem_ld32(base + b * 256 + (k + 1) * 32, x[(k + 1) & 1]);
-        uint32_t* v = x[k & 1];
-        const int64_t w0 = v0 + k * 32;
+        if (k == 0) {
+          tmem_ld32(base + b * 256 + 32, x[1]);
+        } else {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->s_empty[b]);
+        }
+        uint32_t* v = x[k];
+        const int w0 = w.j * 256 + wg * 64 + k * 32;
         if (w0 + 32 > a.V) {
 #pragma unroll
           for (int i = 0; i < 32; ++i)
             if (w0 + i >= a.V) v[i] = 0xFF800000u;
         }
-        const int at = (int)(tgt - w0);
+        const int at = tgt - w0;
         const bool here = tgt >= 0 && at >= 0 && at < 32;
         if (__any_sync(0xffffffffu, here)) {
           float z = 0.f;
 #pragma unroll
           for (int i = 0; i < 32; ++i)
             if (i == at) z = __uint_as_float(v[i]);
-          if (here) a.hit[t * 128 + r] = z * (c / kLog2e);
+          if (here) a.hit[w.t * 128 + r] = z * (c / kLog2e);
         }
-        online32(v, c, m, l);
+        online32(v, c, w.starts && k == 0, m, l);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->s_empty[b]);
       if (w.ends) {
         // the sum's reference is m itself, so that the join undoes exactly what was done here
-        if (un.whole(blockIdx.x, t))
-          a.full[h * a.cap + t * 128 + r] = make_float2(m, l);
+        if (un.whole(blockIdx.x, w.t))
+          a.full[wg * a.cap + w.t * 128 + r] = make_float2(m, l);
         else
-          a.part[(((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, t)) * 2 + h) * 128 + r] =
+          a.part[(((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, w.t)) * 4 + wg) * 128 + r] =
               make_float2(m, l);
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 17) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 512);
@@ -700,11 +776,12 @@ __global__ void __launch_bounds__(256)
   float m = -3.0e38f, l = 0.f;
   if (s < rows) {
     const int c0 = un.owner(t * un.ct), c1 = un.owner(t * un.ct + un.ct - 1);
-    const int n = c0 == c1 ? 2 : 2 * (c1 - c0 + 1);
+    const int n = c0 == c1 ? 4 : 4 * (c1 - c0 + 1);
     for (int i = sub; i < n; i += lanes) {
-      const int c = c0 + i / 2;
+      const int c = c0 + i / 4;
       const float2 p = c0 == c1 ? full[i * cap + s]
-                                : part[(((int64_t)c * 2 + (c == c0 ? un.slot(c, t) : 0)) * 2 + (i & 1)) * 128 + r];
+                                : part[(((int64_t)c * 2 +
+                                         (c == c0 ? un.slot(c, t) : 0)) * 4 + (i & 3)) * 128 + r];
       const float mn = fmaxf(m, p.x);
       l = l * ex2(m - mn) + p.y * ex2(p.x - mn);
       m = mn;
@@ -734,7 +811,7 @@ struct BwdArgs {
   const int* head;
   const int32_t* row;
   const int32_t* tgt;
-  const float* lse;
+  const float* nlse;
   const float* g;
   void* out;
   float* part;  // [G][2][128][H]
@@ -743,85 +820,137 @@ struct BwdArgs {
 
 // One unit: z = S B^T (S the staying tile, B the passing one), P from z, G += P B.  B serves both
 // products: as its rows lie (K-major) in the first, transposed (MN-major) in the second.
+//
+// A passing tile has 128 rows, and 64 at H > 128, where 128 would leave room for two ring stages and
+// the loads would be waited for (measured at H = 256: 3700 cycles per 128 rows instead of the 2048
+// that the products take).  Tensor memory holds G and as many units' z as fit beside it.
 template <int HC, int FORM>
 struct BCfg {
   static constexpr int T = FORM == kF16x2 ? 2 : 1;   // terms of S and B
   static constexpr int PT = FORM == kBf16 ? 1 : 2;   // terms of P
   static constexpr bool KEEP = FORM != kBf16;        // G is added up in registers
-  static constexpr int NB = T == 2 && HC > 2 ? 64 : 128;  // passing rows of a unit
+  static constexpr int NB = HC > 2 ? 64 : 128;       // passing rows of a unit
+  // Units of 64 rows: two teams of warps take them in turn, 32 columns a thread; where a thread also
+  // holds 64 sums, all warps take every unit, 16 columns a thread.
+  static constexpr int TEAMS = NB == 64 && !KEEP ? 2 : 1;
+  static constexpr int WARPS = 16 / TEAMS;           // of a team
+  static constexpr int CW = NB * TEAMS / 4;          // columns of a thread
   static constexpr int S_BYTES = T * HC * 16384;
   static constexpr int BOX = NB * 128;  // 64 elements of each passing row
   static constexpr int B_BYTES = T * HC * BOX;
-  static constexpr int STATS = 3 * NB * 4;  // lse, g and target of passing X rows
+  static constexpr int STATS = 3 * NB * 4;  // -lse, g and target of passing X rows
   static constexpr int ROOM = (232448 - 2048 - S_BYTES) / (B_BYTES + 2048);
-  static constexpr int ST = ROOM < 4 ? ROOM : 4;
+  static constexpr int ST = ROOM < kMaxStages ? ROOM : kMaxStages;
   static constexpr int SMEM = S_BYTES + ST * (B_BYTES + 2048) + 2048;
   static constexpr int GCOLS = HC * 64;
+  static constexpr int ZROOM = (512 - GCOLS) / NB;
+  static constexpr int ZB = ZROOM < 4 ? ZROOM : 4;   // units' z in tensor memory
   static constexpr int STEPS = NB / 16 * (T == 2 ? 3 : PT);  // accumulating steps of a unit
   static constexpr int DRAIN = KEEP ? kDrainSteps / STEPS : 1 << 30;  // units before G leaves TMEM
   static_assert(ST >= 1 && SMEM <= 232448, "shared memory");
-  static_assert(GCOLS + 2 * NB <= 512, "tensor memory");
+  static_assert(ZB >= 2 && ZB % TEAMS == 0, "tensor memory");
   static_assert(DRAIN >= 1, "drain interval");
 };
 
 struct BwdBars {
-  uint64_t s_full, s_empty, full[4], empty[4], z_full[2], p_full[2], g_full, g_empty, drain;
+  uint64_t s_full, s_empty, full[kMaxStages], empty[kMaxStages], z_full[4], z_empty[4], p_full[4], g_full, g_empty, drain_z, drain_g;
   uint32_t tmem;
   int abort;
 };
 
-// P of 32 columns from their logits, in place.
-// Row statistics (dX): mine = {lse, target - first column}.  Column statistics (dW): arrays.
-template <int FORM, bool DW>
-__device__ __forceinline__ void probs32(uint32_t* v, float descale, float up, float lse, int hit,
-                                        const float* col_lse, const float* col_g,
-                                        const int* col_tgt, int64_t first_row, int r) {
-  const int lane = threadIdx.x & 31;
-  if (!DW) {
+// A place in a ring of N and the parity of its turn.
+template <int N>
+struct Turn {
+  int i = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++i == N) i = 0, parity ^= 1;
+  }
+};
+
+// P of N columns of a row (a thread's) from their logits, for dX: nlse = -lse of the row, hit = its
+// target's place among the columns.
+template <int FORM, int N>
+__device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, float nlse, int hit) {
+  const uint64_t l2e = pack2(kLog2e, kLog2e), ds = pack2(descale, descale), up2 = pack2(up, up);
+  const uint64_t nl = pack2(nlse, nlse);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float z = __uint_as_float(v[i]);
-      const float e = FORM == kBf16 ? ex2(fmaf(z, kLog2e, -lse))
-                                    : ex2(fmaf(fmaf(z, descale, -lse), kLog2e, up));
-      v[i] = __float_as_uint(e);
+  for (int i = 0; i < N; i += 2) {
+    uint64_t x = pack2u(v[i], v[i + 1]);
+    x = FORM == kBf16 ? fma2(x, l2e, nl) : fma2(fma2(x, ds, nl), l2e, up2);
+    float a, b;
+    unpack2(x, a, b);
+    v[i] = __float_as_uint(ex2(a));
+    v[i + 1] = __float_as_uint(ex2(b));
+  }
+  const bool here = hit >= 0 && hit < N;
+  if (__any_sync(0xffffffffu, here)) {
+    const float one = FORM == kBf16 ? 1.f : 32768.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i == hit) v[i] = __float_as_uint(__uint_as_float(v[i]) - one);
+  }
+}
+
+// The same for dW, whose statistics (-lse, g, target of the passing X rows) go by column.  Were a
+// thread a row here too, it would read every column's: at 32 columns a warp 16 shared-memory loads of
+// 512 bytes, more than the SM can deliver in the time of the products (measured: 1.8 x the time of the
+// dX kernel at H = 64).  So tensor memory is read in fragments in which a thread has two neighbouring
+// columns of every 8, in rows l / 4, + 8, + 16, + 24 of its warp's 32 (l = lane): a quarter of the
+// loads.  v[16 h + 4 g + 2 a + b]: row 16 h + 8 a + l / 4, column 8 g + 2 (l % 4) + b.
+template <int FORM, int N>
+__device__ __forceinline__ void probs_col(uint32_t* v, float descale, float up, const float* col_nlse,
+                                          const float* col_g, const int* col_tgt, int first,
+                                          int mine) {
+  const uint64_t l2e = pack2(kLog2e, kLog2e), ds = pack2(descale, descale), up2 = pack2(up, up);
+  const int lane = threadIdx.x & 31, c = 2 * (lane & 3);
+  const int at = col_tgt[lane & (N - 1)] - first;
+  const bool hits = __any_sync(0xffffffffu, at >= 0 && at < 128);
+#pragma unroll
+  for (int g = 0; g < N / 8; ++g) {
+    const uint64_t nl = *reinterpret_cast<const uint64_t*>(col_nlse + 8 * g + c);
+    const float2 gg = *reinterpret_cast<const float2*>(col_g + 8 * g + c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t* p = v + (k >> 1) * (N / 2) + 4 * g + 2 * (k & 1);
+      uint64_t x = pack2u(p[0], p[1]);
+      x = FORM == kBf16 ? fma2(x, l2e, nl) : fma2(fma2(x, ds, nl), l2e, up2);
+      float a, b;
+      unpack2(x, a, b);
+      p[0] = __float_as_uint(ex2(a) * gg.x);
+      p[1] = __float_as_uint(ex2(b) * gg.y);
     }
-    const bool here = hit >= 0 && hit < 32;
-    if (__any_sync(0xffffffffu, here)) {
-      const float one = FORM == kBf16 ? 1.f : 32768.f;
+  }
+  if (hits) {
+    const float upg = FORM == kBf16 ? -1.f : -ex2(up);
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i == hit) v[i] = __float_as_uint(__uint_as_float(v[i]) - one);
-    }
-  } else {
-    const float upg = FORM == kBf16 ? 1.f : ex2(up);
-#pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-      const float4 ls = *reinterpret_cast<const float4*>(col_lse + i);
-      const float4 gg = *reinterpret_cast<const float4*>(col_g + i);
-      const float lc[4] = {ls.x, ls.y, ls.z, ls.w}, gc[4] = {gg.x, gg.y, gg.z, gg.w};
+    for (int g = 0; g < N / 8; ++g) {
+      const int2 tt = *reinterpret_cast<const int2*>(col_tgt + 8 * g + c);
+      const float2 gg = *reinterpret_cast<const float2*>(col_g + 8 * g + c);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float z = __uint_as_float(v[i + k]);
-        const float e = FORM == kBf16 ? ex2(fmaf(z, kLog2e, -lc[k]))
-                                      : ex2(fmaf(fmaf(z, descale, -lc[k]), kLog2e, up));
-        v[i + k] = __float_as_uint(e * gc[k]);
+        uint32_t* p = v + (k >> 1) * (N / 2) + 4 * g + 2 * (k & 1);
+        const int row = mine + 16 * (k >> 1) + 8 * (k & 1);
+        if (tt.x == row) p[0] = __float_as_uint(fmaf(gg.x, upg, __uint_as_float(p[0])));
+        if (tt.y == row) p[1] = __float_as_uint(fmaf(gg.y, upg, __uint_as_float(p[1])));
       }
     }
-    const int64_t at = (int64_t)col_tgt[lane] - first_row;
-    if (__any_sync(0xffffffffu, at >= 0 && at < 128)) {
-      // frequent tokens have hits in every unit: all 32 columns at once, without branches
-      const int mine = (int)first_row + r;
-#pragma unroll
-      for (int i = 0; i < 32; i += 4) {
-        const int4 tt = *reinterpret_cast<const int4*>(col_tgt + i);
-        const float4 gg = *reinterpret_cast<const float4*>(col_g + i);
-        const int tc[4] = {tt.x, tt.y, tt.z, tt.w};
-        const float gc[4] = {gg.x, gg.y, gg.z, gg.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (tc[k] == mine) v[i + k] = __float_as_uint(fmaf(gc[k], -upg, __uint_as_float(v[i + k])));
-      }
-    }
+  }
+}
+
+// Two neighbouring values of P as the form's terms.
+template <int FORM>
+__device__ __forceinline__ void terms(uint32_t a, uint32_t b, uint32_t& hi, uint32_t& lo) {
+  const float x = __uint_as_float(a), y = __uint_as_float(b);
+  if (FORM == kBf16) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
+    hi = *reinterpret_cast<const uint32_t*>(&p);
+  } else {
+    const __half2 p = __floats2half2_rn(x, y);
+    hi = *reinterpret_cast<const uint32_t*>(&p);
+    const float2 f = __half22float2(p);
+    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
   }
 }
 
@@ -845,17 +974,19 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       mbar_init(&bars->full[s], 1);
       mbar_init(&bars->empty[s], 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < C::ZB; ++b) {
       mbar_init(&bars->z_full[b], 1);
-      mbar_init(&bars->p_full[b], 8);
+      mbar_init(&bars->z_empty[b], 1);
+      mbar_init(&bars->p_full[b], C::WARPS);
     }
     mbar_init(&bars->g_full, 1);
-    mbar_init(&bars->g_empty, 8);
-    mbar_init(&bars->drain, 1);
+    mbar_init(&bars->g_empty, 16);
+    mbar_init(&bars->drain_z, 1);
+    mbar_init(&bars->drain_g, 1);
     bars->abort = 0;
     fence_mbar_init();
   }
-  if (warp == 9) {
+  if (warp == 17) {
     tmem_alloc(&bars->tmem, 512);
     tmem_relinquish();
   }
@@ -868,18 +999,17 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   const int64_t rows = a.head[0];
   const Units un(DW ? (a.V + 127) / 128 : (rows + 127) / 128,
                  DW ? (rows + C::NB - 1) / C::NB : (a.V + C::NB - 1) / C::NB, gridDim.x);
-  Units::Walk w(un, blockIdx.x);
 
-  if (warp >= 10) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-  } else if (warp == 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  if (warp == 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (lane == 0) {
+      Units::Walk w(un, blockIdx.x);
       tma_prefetch_desc(&tmS);
       tma_prefetch_desc(&tmB);
       uint32_t it = 0, seg = 0;
+      Turn<C::ST> s;
       bool ok = true;
-      for (; w.more() && ok; w.next(), ++it) {
+      for (; w.more() && ok; w.next(), s.next(), ++it) {
         if (w.starts) {
           ok = seg == 0 || mbar_wait_inline(&bars->s_empty, (seg - 1) & 1, a.status, 711, abort, 32);
           if (!ok) break;
@@ -889,17 +1019,18 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                         (int)((p / HC) * a.scap) + w.t * 128);
           ++seg;
         }
-        const int s = it % C::ST;
-        ok = mbar_wait_inline(&bars->empty[s], ((it / C::ST) & 1) ^ 1, a.status, 712, abort, 32);
+        ok = mbar_wait_inline(&bars->empty[s.i], s.parity ^ 1, a.status, 712, abort, 32);
         if (!ok) break;
-        mbar_expect_tx(&bars->full[s], C::B_BYTES + (DW ? C::STATS : 0));
+        mbar_expect_tx(&bars->full[s.i], C::B_BYTES + (DW ? C::STATS : 0));
         for (int p = 0; p < C::T * HC; ++p)
-          tma_load_2d(ring + s * C::B_BYTES + p * C::BOX, &tmB, &bars->full[s], p % HC * 64,
+          tma_load_2d(ring + s.i * C::B_BYTES + p * C::BOX, &tmB, &bars->full[s.i], p % HC * 64,
                       (int)((p / HC) * a.pcap) + w.j * C::NB);
         if (DW) {
-          bulk_load(stats + s * 2048, a.lse + (int64_t)w.j * C::NB, C::NB * 4, &bars->full[s]);
-          bulk_load(stats + s * 2048 + C::NB * 4, a.g + (int64_t)w.j * C::NB, C::NB * 4, &bars->full[s]);
-          bulk_load(stats + s * 2048 + C::NB * 8, a.tgt + (int64_t)w.j * C::NB, C::NB * 4, &bars->full[s]);
+          uint8_t* d = stats + s.i * 2048;
+          const int64_t at = (int64_t)w.j * C::NB;
+          bulk_load(d, a.nlse + at, C::NB * 4, &bars->full[s.i]);
+          bulk_load(d + C::NB * 4, a.g + at, C::NB * 4, &bars->full[s.i]);
+          bulk_load(d + C::NB * 8, a.tgt + at, C::NB * 4, &bars->full[s.i]);
         }
       }
       if (*abort) {  // copies in flight land before the block leaves
@@ -910,121 +1041,134 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
           }
       }
     }
-  } else if (warp == 9) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  } else if (warp == 17) {
+    // z = S B^T, as many units ahead as tensor memory and the ring hold
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    Units::Walk w(un, blockIdx.x);
     const bool leader = elect_one_sync();
-    const uint32_t iz = idesc16(FORM == kBf16, C::NB, 0), ig = idesc16(FORM == kBf16, a.H, 1);
+    const uint32_t iz = idesc16(FORM == kBf16, C::NB, 0);
     // a descriptor's address field is in 16 bytes
-    const uint64_t S = desc_sw128_kmajor(smem_u32(smem)), RK = desc_sw128_kmajor(smem_u32(ring)),
-                   RN = desc_sw128_mnmajor(smem_u32(ring), C::BOX);
-    // z = S B^T of the unit in ring stage s (past H both hold zeros); two terms: low x high and
-    // high x low first
-    auto z_product = [&](int s, int b) {
-      const uint64_t B = RK + s * (C::B_BYTES >> 4);
-      const uint32_t d = zbuf + b * C::NB;
+    const uint64_t S = desc_sw128_kmajor(smem_u32(smem)), R = desc_sw128_kmajor(smem_u32(ring));
+    uint32_t seg = 0;
+    Turn<C::ST> s;
+    Turn<C::ZB> b;
+    bool ok = true;
+    for (; w.more() && ok; w.next(), s.next(), b.next()) {
+      if (w.starts) {
+        ok = mbar_wait_inline(&bars->s_full, seg & 1, a.status, 715, abort);
+        ++seg;
+      }
+      ok = ok && mbar_wait_inline(&bars->z_empty[b.i], b.parity ^ 1, a.status, 719, abort);
+      ok = ok && mbar_wait_inline(&bars->full[s.i], s.parity, a.status, 716, abort);
+      if (!ok) break;
+      tc_fence_after();
+      const uint64_t B = R + s.i * (C::B_BYTES >> 4);
+      const uint32_t d = zbuf + b.i * C::NB;
+      // past H both operands hold zeros; two terms: low x high and high x low first, while the
+      // accumulator is small
       constexpr int n = C::T == 2 ? 3 : 1;
+      if (leader) {
 #pragma unroll
-      for (int pr = 0; pr < n; ++pr) {
-        const uint64_t as = S + (n == 3 && pr == 0 ? HC * (16384 >> 4) : 0);
-        const uint64_t bs = B + (n == 3 && pr == 1 ? HC * (C::BOX >> 4) : 0);
-        if (leader) {
+        for (int pr = 0; pr < n; ++pr) {
+          const uint64_t as = S + (n == 3 && pr == 0 ? HC * (16384 >> 4) : 0);
+          const uint64_t bs = B + (n == 3 && pr == 1 ? HC * (C::BOX >> 4) : 0);
 #pragma unroll
           for (int k = 0; k < HC * 4; ++k)
             mma_ss(d, as + (k >> 2) * (16384 >> 4) + (k & 3) * 2,
                    bs + (k >> 2) * (C::BOX >> 4) + (k & 3) * 2, iz, pr > 0 || k > 0);
         }
+        tc_commit(&bars->z_full[b.i]);
+        if (w.ends) tc_commit(&bars->s_empty);
       }
-    };
+      __syncwarp();
+    }
+    if (leader) tc_commit(&bars->drain_z);
+    __syncwarp();
+    for (uint32_t k = 0; k < (1u << 24) && !mbar_try(&bars->drain_z, 0); ++k) {
+    }
+  } else if (warp == 18) {
     // G (+)= P B, small products first
-    auto g_product = [&](int s, int b, bool add) {
-      const uint64_t B = RN + s * (C::B_BYTES >> 4);
-      const uint32_t p = zbuf + b * C::NB;
-      constexpr int n = C::T == 2 ? 3 : C::PT;
-#pragma unroll
-      for (int pr = 0; pr < n; ++pr) {
-        const uint32_t pa = p + (C::PT == 2 && pr == 0 ? 16 : 0);
-        const uint64_t bs = B + (n == 3 && pr == 1 ? HC * (C::BOX >> 4) : 0);
-        if (leader) {
-#pragma unroll
-          for (int k = 0; k < C::NB / 16; ++k)
-            mma_ts(tmem, pa + (k >> 1) * 32 + (k & 1) * 8, bs + k * (2048 >> 4), ig,
-                   add || pr > 0 || k > 0);
-        }
-      }
-    };
-    uint32_t it = 0, seg = 0, groups = 0;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    Units::Walk w(un, blockIdx.x);
+    const bool leader = elect_one_sync();
+    const uint32_t ig = idesc16(FORM == kBf16, a.H, 1);
+    const uint64_t R = desc_sw128_mnmajor(smem_u32(ring), C::BOX);
+    uint32_t groups = 0;
+    int in_group = 0;
+    Turn<C::ST> s;
+    Turn<C::ZB> b;
     bool ok = true;
-    int in_group = 0;     // units of the running group whose G has been issued
-    bool last = false;    // the previous unit ended its staying tile
-    // the second product of unit `k` (its number in this CTA's run)
-    auto second = [&](uint32_t k, bool ends) {
-      ok = ok && mbar_wait_inline(&bars->p_full[k & 1], (k >> 1) & 1, a.status, 713, abort);
+    for (; w.more() && ok; w.next(), s.next(), b.next()) {
+      ok = mbar_wait_inline(&bars->p_full[b.i], b.parity, a.status, 713, abort);
       if (ok && in_group == 0 && groups > 0)
         ok = mbar_wait_inline(&bars->g_empty, (groups - 1) & 1, a.status, 714, abort);
-      if (!ok) return;
+      if (!ok) break;
       tc_fence_after();
-      g_product(k % C::ST, k & 1, in_group > 0);
-      if (leader) tc_commit(&bars->empty[k % C::ST]);
-      if (++in_group == C::DRAIN || ends) {
-        if (leader) tc_commit(&bars->g_full);
+      const uint64_t B = R + s.i * (C::B_BYTES >> 4);
+      const uint32_t p = zbuf + b.i * C::NB;
+      constexpr int n = C::T == 2 ? 3 : C::PT;
+      const bool close = ++in_group == C::DRAIN || w.ends;
+      if (leader) {
+#pragma unroll
+        for (int pr = 0; pr < n; ++pr) {
+          // 16 columns of z hold 16 of P: 8 columns of the high terms, 8 of the low ones
+          const uint32_t pa = p + (C::PT == 2 && pr == 0 ? 8 : 0);
+          const uint64_t bs = B + (n == 3 && pr == 1 ? HC * (C::BOX >> 4) : 0);
+#pragma unroll
+          for (int k = 0; k < C::NB / 16; ++k)
+            mma_ts(tmem, pa + k * 16, bs + k * (2048 >> 4), ig,
+                   in_group > 1 || pr > 0 || k > 0);
+        }
+        tc_commit(&bars->empty[s.i]);
+        tc_commit(&bars->z_empty[b.i]);
+        if (close) tc_commit(&bars->g_full);
+      }
+      if (close) {
         ++groups;
         in_group = 0;
       }
       __syncwarp();
-    };
-    for (; w.more() && ok; w.next(), ++it) {
-      if (C::ST == 1 && it > 0) second(it - 1, last);
-      if (w.starts) {
-        ok = ok && mbar_wait_inline(&bars->s_full, seg & 1, a.status, 715, abort);
-        ++seg;
-      }
-      const int s = it % C::ST;
-      ok = ok && mbar_wait_inline(&bars->full[s], (it / C::ST) & 1, a.status, 716, abort);
-      if (!ok) break;
-      tc_fence_after();
-      z_product(s, it & 1);
-      if (leader) {
-        tc_commit(&bars->z_full[it & 1]);
-        if (w.ends) tc_commit(&bars->s_empty);
-      }
-      __syncwarp();
-      if (C::ST > 1 && it > 0) second(it - 1, last);
-      last = w.ends;
     }
-    if (it > 0) second(it - 1, last);
-    if (leader) tc_commit(&bars->drain);
+    if (leader) tc_commit(&bars->drain_g);
     __syncwarp();
-    for (uint32_t k = 0; k < (1u << 24) && !mbar_try(&bars->drain, 0); ++k) {
+    for (uint32_t k = 0; k < (1u << 24) && !mbar_try(&bars->drain_g, 0); ++k) {
     }
+  } else if (warp > 18) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    // warps 0-3: the first half of a unit's columns and of G's, warps 4-7: the second; a thread is a row
-    const int q = warp & 3, h = warp >> 2, r = q * 32 + lane;
-    constexpr int HALF = C::NB / 2, GH = HC * 32;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    Units::Walk w(un, blockIdx.x);
+    // a thread is a row; its warpgroup has 32 columns of each unit of its team, and GQ columns of G
+    const int q = warp & 3, wg = warp >> 2, r = q * 32 + lane;
+    constexpr int GQ = HC * 16;
+    const int team = C::TEAMS == 2 ? wg >> 1 : 0;
+    const int c0 = (C::TEAMS == 2 ? wg & 1 : wg) * C::CW;
     const uint32_t quarter = (uint32_t)(q * 32) << 16;
     const int sx = FORM == kBf16 ? 0 : a.head[1], sw = FORM == kBf16 ? 0 : a.head[2];
     const float descale = FORM == kBf16 ? 1.f : pow2(max(-126, min(127, -(sx + sw))));
     // P is scaled by 2^up: probabilities to 2^15 for dX, times g to 2^15 for dW
     const int up = FORM == kBf16 ? 0 : DW ? a.head[3] : 15;
-    float acc[C::KEEP ? GH : 1];
-    uint32_t it = 0, groups = 0;
-    int in_group = 0;
+    float acc[C::KEEP ? GQ : 1];
+    uint32_t groups = 0;
+    int in_group = 0, turn = 0;
+    Turn<C::ST> s;
+    Turn<C::ZB> b;
     bool fresh = true, pending = false, ok = true;
-    float lse = 0.f;
+    float nlse = 0.f;
     int tgt = -1;
-    // adds the finished group of G to the registers
+    // takes the finished group of G: adds it to the registers
     auto collect = [&]() {
       if (!mbar_wait_inline(&bars->g_full, groups & 1, a.status, 717, abort, 32)) return false;
       ++groups;
       tc_fence_after();
       if (C::KEEP) {
 #pragma unroll
-        for (int c = 0; c < GH; c += 32) {
-          uint32_t v[32];
-          tmem_ld32(tmem + quarter + h * GH + c, v);
+        for (int c = 0; c < GQ; c += 16) {
+          uint32_t v[16];
+          tmem_ld16(tmem + quarter + wg * GQ + c, v);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
+          for (int i = 0; i < 16; ++i)
             acc[C::KEEP ? c + i : 0] = fresh ? __uint_as_float(v[i])
                                              : acc[C::KEEP ? c + i : 0] + __uint_as_float(v[i]);
         }
@@ -1035,59 +1179,72 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       }
       return true;
     };
-    for (; w.more() && ok; w.next(), ++it) {
-      const int64_t t = w.t, j = w.j;
+    for (; w.more() && ok; w.next(), s.next(), b.next()) {
       if (!DW && w.starts) {
-        lse = a.lse[t * 128 + r];
-        tgt = a.tgt[t * 128 + r];
+        nlse = a.nlse[w.t * 128 + r];
+        tgt = a.tgt[w.t * 128 + r];
       }
-      const int b = it & 1;
-      ok = mbar_wait_inline(&bars->z_full[b], (it >> 1) & 1, a.status, 718, abort, 32);
-      if (!ok) break;
-      tc_fence_after();
-      const uint8_t* st = stats + it % C::ST * 2048;
-#pragma unroll
-      for (int k = 0; k < HALF / 32; ++k) {
-        const int c0 = h * HALF + k * 32;
-        const uint32_t at = zbuf + quarter + b * C::NB + c0;
-        uint32_t v[32];
-        tmem_ld32(at, v);
-        tmem_wait_ld();
-        const float* cl = reinterpret_cast<const float*>(st) + c0;
-        const float* cg = reinterpret_cast<const float*>(st) + C::NB + c0;
-        const int* ctg = reinterpret_cast<const int*>(st) + 2 * C::NB + c0;
-        const int64_t w0 = j * C::NB + c0;
-        probs32<FORM, DW>(v, descale, (float)up, lse, tgt < 0 ? -1 : (int)max((int64_t)-1, min((int64_t)32, tgt - w0)),
-                          cl, cg, ctg, t * 128, r);
-        if (!DW && w0 + 32 > a.V) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (w0 + i >= a.V) v[i] = 0;
-        }
-        uint32_t o[32];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = __uint_as_float(v[2 * i]), y = __uint_as_float(v[2 * i + 1]);
-          if (FORM == kBf16) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
-            o[i] = *reinterpret_cast<const uint32_t*>(&p);
+      if (C::TEAMS == 1 || turn == team) {
+        ok = mbar_wait_inline(&bars->z_full[b.i], b.parity, a.status, 718, abort, 20);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t at = zbuf + quarter + b.i * C::NB + c0;
+        uint32_t v[C::CW];
+        const int w0 = w.j * C::NB + c0;
+        if (DW) {
+          // (CW / 2 registers for each half of the warp's rows)
+          if (C::CW == 32) {
+            tmem_ld_frag32(at, v);
+            tmem_ld_frag32(at + (16u << 16), v + 16);
           } else {
-            const __half2 p = __floats2half2_rn(x, y);
-            o[i] = *reinterpret_cast<const uint32_t*>(&p);
-            const float2 f = __half22float2(p);
-            const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
-            o[16 + i] = *reinterpret_cast<const uint32_t*>(&l);
+            tmem_ld_frag16(at, v);
+            tmem_ld_frag16(at + (16u << 16), v + 8);
+          }
+          tmem_wait_ld();
+          const float* st = reinterpret_cast<const float*>(stats + s.i * 2048) + c0;
+          probs_col<FORM, C::CW>(v, descale, (float)up, st, st + C::NB,
+                                 reinterpret_cast<const int*>(st + 2 * C::NB), w.t * 128,
+                                 w.t * 128 + q * 32 + lane / 4);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < C::CW; c += 16) {
+              uint32_t hi[4], lo[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t* p = v + h * (C::CW / 2) + c / 2 + 2 * i;
+                terms<FORM>(p[0], p[1], hi[i], lo[i]);
+              }
+              tmem_st_frag8(at + (h * 16u << 16) + c, hi);
+              if (FORM != kBf16) tmem_st_frag8(at + (h * 16u << 16) + c + 8, lo);
+            }
+        } else {
+          if (C::CW == 32)
+            tmem_ld32(at, v);
+          else
+            tmem_ld16(at, v);
+          tmem_wait_ld();
+          probs_row<FORM, C::CW>(v, descale, (float)up, nlse, tgt < 0 ? -1 : tgt - w0);
+          if (w0 + C::CW > a.V) {
+#pragma unroll
+            for (int i = 0; i < C::CW; ++i)
+              if (w0 + i >= a.V) v[i] = 0;
+          }
+#pragma unroll
+          for (int c = 0; c < C::CW; c += 16) {
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) terms<FORM>(v[c + 2 * i], v[c + 2 * i + 1], hi[i], lo[i]);
+            tmem_st8(at + c, hi);
+            if (FORM != kBf16) tmem_st8(at + c + 8, lo);
           }
         }
-        if (FORM == kBf16)
-          tmem_st16(at, o);
-        else
-          tmem_st32(at, o);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->p_full[b.i]);
       }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->p_full[b]);
+      turn ^= 1;
       if (pending) {
         ok = collect();
         pending = false;
@@ -1102,8 +1259,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       if (!ok) break;
       fresh = true;
       // the tile's result: finished where this CTA had all its units, else for the join
-      const bool whole = un.whole(blockIdx.x, t);
-      int64_t orow = t * 128 + r;
+      const bool whole = un.whole(blockIdx.x, w.t);
+      int64_t orow = (int64_t)w.t * 128 + r;
       float s1 = 1.f, s2 = 1.f, s3 = 1.f;
       if (DW) {
         if (orow >= a.V) orow = -1;
@@ -1113,48 +1270,48 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         orow = a.row[orow];
         if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-sw);
       }
-      float* pt = a.part + (((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, t)) * 128 + r) * a.H;
+      float* pt = a.part + (((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, w.t)) * 128 + r) * a.H;
 #pragma unroll
-      for (int c = 0; c < GH; c += 32) {
-        const int col = h * GH + c;
-        uint32_t v[32];
+      for (int c = 0; c < GQ; c += 16) {
+        const int col = wg * GQ + c;
+        uint32_t v[16];
         if (C::KEEP) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(acc[C::KEEP ? c + i : 0]);
+          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(acc[C::KEEP ? c + i : 0]);
         } else if (col < a.H) {
-          tmem_ld32(tmem + quarter + col, v);
+          tmem_ld16(tmem + quarter + col, v);
           tmem_wait_ld();
         }
         if (col >= a.H) continue;
         float* x = reinterpret_cast<float*>(v);
         if (!whole) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
+          for (int i = 0; i < 16; i += 4)
             *reinterpret_cast<float4*>(pt + col + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
           continue;
         }
         if (orow < 0) continue;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] = x[i] * s1 * s2 * s3;
+        for (int i = 0; i < 16; ++i) x[i] = x[i] * s1 * s2 * s3;
         if (out_bf16) {
           __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.out) + orow * a.H + col;
 #pragma unroll
-          for (int i = 0; i < 32; i += 8) {
-            __nv_bfloat162 w[4];
+          for (int i = 0; i < 16; i += 8) {
+            __nv_bfloat162 h[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = __floats2bfloat162_rn(x[i + 2 * k], x[i + 2 * k + 1]);
-            *reinterpret_cast<uint4*>(o + i) = *reinterpret_cast<const uint4*>(w);
+            for (int k = 0; k < 4; ++k) h[k] = __floats2bfloat162_rn(x[i + 2 * k], x[i + 2 * k + 1]);
+            *reinterpret_cast<uint4*>(o + i) = *reinterpret_cast<const uint4*>(h);
           }
         } else {
           float* o = static_cast<float*>(a.out) + orow * a.H + col;
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            float4 w = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          for (int i = 0; i < 16; i += 4) {
+            float4 h = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
             if (a.accumulate) {
               const float4 p = *reinterpret_cast<const float4*>(o + i);
-              w = make_float4(w.x + p.x, w.y + p.y, w.z + p.z, w.w + p.w);
+              h = make_float4(h.x + p.x, h.y + p.y, h.z + p.z, h.w + p.w);
             }
-            *reinterpret_cast<float4*>(o + i) = w;
+            *reinterpret_cast<float4*>(o + i) = h;
           }
         }
       }
@@ -1167,7 +1324,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 17) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 512);
@@ -1272,7 +1429,7 @@ cudaError_t prepare(const XentArgs& a, Call& c, RowArgs r) {
   r.amax = c.at<uint32_t>(c.w.amax);
   r.row = c.at<int32_t>(c.w.row);
   r.tgt = c.at<int32_t>(c.w.tgt);
-  r.lse = c.at<float>(c.w.lse);
+  r.nlse = c.at<float>(c.w.nlse);
   r.g = c.at<float>(c.w.g);
   r.x = c.at<uint16_t>(c.w.x);
   r.w = c.at<uint16_t>(c.w.w);
@@ -1419,7 +1576,7 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
   b.head = c.at<int>(c.w.head);
   b.row = c.at<int32_t>(c.w.row);
   b.tgt = c.at<int32_t>(c.w.tgt);
-  b.lse = c.at<float>(c.w.lse);
+  b.nlse = c.at<float>(c.w.nlse);
   b.g = c.at<float>(c.w.g);
   b.part = c.at<float>(c.w.part);
   b.status = a.status;
