@@ -384,7 +384,7 @@ def _shaped(t, name, dtype, *shape):
     """Device pointer of a contiguous CUDA tensor of this element type and shape (None passes)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
     return _dev_ptr(t, name)
 
@@ -392,9 +392,18 @@ def _shaped(t, name, dtype, *shape):
 def _elements(t, name, dtype, n):
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n:
+    if t.dtype is not dtype or t.numel() != n:
         raise ValueError(f"{name} must have {n} elements of {dtype}, not {t.numel()} of {t.dtype}")
     return _dev_ptr(t, name)
+
+
+def _stream_of(stream, t):
+    """The stream given, else torch's current one on t's device (by its handle: making a Stream object
+    of it takes as long as a kernel launch)."""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return _stream(stream)
 
 
 def _torch_dtype(code):
@@ -408,14 +417,14 @@ def dropout_fwd(dtype, x, y, p, seed, call, residual=None, stream=None):
     td, n = _torch_dtype(dt), x.numel()
     _check(load().bg_dropout_fwd(dt, n, p, seed, call, _elements(x, "x", td, n),
                                  _elements(residual, "residual", td, n),
-                                 _elements(y, "y", td, n), _stream(stream)))
+                                 _elements(y, "y", td, n), _stream_of(stream, x)))
 
 
 def dropout_bwd(dy, dx, p, seed, call, flags=0, stream=None):
     """dx (+)= drop(dy) with the mask of the forward call of the same (p, seed, call); fp32."""
     td, n = _torch_dtype(BG_F32), dy.numel()
     _check(load().bg_dropout_bwd(n, p, seed, call, _elements(dy, "dy", td, n),
-                                 _elements(dx, "dx", td, n), flags, _stream(stream)))
+                                 _elements(dx, "dx", td, n), flags, _stream_of(stream, dy)))
 
 
 def embed_fwd(dtype, ids, table, out, scale=1.0, p=0.0, seed=0, call=0, stream=None):
@@ -425,7 +434,7 @@ def embed_fwd(dtype, ids, table, out, scale=1.0, p=0.0, seed=0, call=0, stream=N
     td, n, (V, H) = _torch_dtype(dt), ids.numel(), table.shape
     _check(load().bg_embed_fwd(dt, n, H, V, _shaped(ids, "ids", torch.int32, n),
                                _shaped(table, "table", td, V, H), scale, p, seed, call,
-                               _shaped(out, "out", td, n, H), _stream(stream)))
+                               _shaped(out, "out", td, n, H), _stream_of(stream, out)))
 
 
 def embed_workspace_bytes(n, H, V) -> int:
@@ -440,7 +449,7 @@ def embed_bwd(ids, dout, dtable, ws, scale=1.0, p=0.0, seed=0, call=0, flags=0, 
                                _shaped(dout, "dout", torch.float32, n, H), scale, p, seed, call,
                                _shaped(dtable, "dtable", torch.float32, V, H), flags,
                                _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
-                               _stream(stream)))
+                               _stream_of(stream, dtable)))
 
 
 def xent_workspace_bytes(dtype, n, H, V, op) -> int:
@@ -457,7 +466,7 @@ def xent_fwd(dtype, X, W, target, loss, lse, ws, stream=None):
                               _shaped(target, "target", torch.int32, n),
                               _shaped(loss, "loss", torch.float32, n),
                               _shaped(lse, "lse", torch.float32, n), _dev_ptr(ws, "ws"),
-                              ws.numel() * ws.element_size(), _stream(stream)))
+                              ws.numel() * ws.element_size(), _stream_of(stream, W)))
 
 
 def xent_bwd(dtype, X, W, target, lse, dloss, grad_dtype, dX, dW, ws, flags=0, stream=None):
@@ -471,7 +480,7 @@ def xent_bwd(dtype, X, W, target, lse, dloss, grad_dtype, dX, dW, ws, flags=0, s
                               _shaped(dloss, "dloss", torch.float32, n), gt,
                               _shaped(dX, "dX", gd, n, H), _shaped(dW, "dW", gd, V, H), flags,
                               _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
-                              _stream(stream)))
+                              _stream_of(stream, W)))
 
 
 def check_device(stream=None):

@@ -30,6 +30,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "gemm_tc.h"
@@ -52,7 +53,8 @@ enum Form { kBf16 = 0, kF16x1 = 1, kF16x2 = 2 };
 inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 
 constexpr int kMaxRowBlocks = 2048;
-constexpr int kTableBlocks = 304;  // of the table's amax and conversion
+constexpr int kTableBlocks = 304;  // at most, of the table's amax and conversion
+constexpr int64_t kDirectRows = 32768;
 
 // Rows of one block of k_xent_count / k_xent_rows: at most kMaxRowBlocks blocks, since each adds up the
 // counts of those before it.
@@ -97,6 +99,8 @@ Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
 // ------------------------------------------------------------------------------ rows
 struct RowArgs {
   int form, x_bf16, backward, grad_bf16, clear_dx;
+  int direct;  // k_xent_rows counts by itself: k_xent_count did not run
+  int tb;      // blocks that work on the table
   int64_t n, rb, nb, cap, vcap;
   int H, V;
   const void* X;
@@ -106,7 +110,7 @@ struct RowArgs {
   const float* dloss;
   int* head;  // number of labelled rows; exponents of the scales of X, W and dloss (fp16 forms)
   int* counts;
-  uint32_t* amax;  // [nb] of X, [nb] of dloss, [kTableBlocks] of W: bits of the largest finite |x|
+  uint32_t* amax;  // [nb] of X, [nb] of dloss, [tb] of W: bits of the largest finite |x|
   int32_t* row;
   int32_t* tgt;
   float* nlse;  // -lse (bf16 form: times log2 e)
@@ -170,7 +174,7 @@ __global__ void __launch_bounds__(256) k_xent_count(RowArgs a) {
     const int b = blockIdx.x - (int)a.nb;
     uint32_t mx = 0;
     const int64_t chunks = (int64_t)a.V * lanes;
-    for (int64_t i = (int64_t)b * 256 + threadIdx.x; i < chunks; i += (int64_t)kTableBlocks * 256) {
+    for (int64_t i = (int64_t)b * 256 + threadIdx.x; i < chunks; i += (int64_t)a.tb * 256) {
       float v[8];
       load8f(a.W, a.x_bf16, i * 8, v);
       mx = amax8(v, mx);
@@ -255,7 +259,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
       mx = max(mx, a.amax[i]);
       mg = max(mg, a.amax[a.nb + i]);
     }
-    for (int i = tid; i < kTableBlocks; i += 256) mw = max(mw, a.amax[2 * a.nb + i]);
+    for (int i = tid; i < a.tb; i += 256) mw = max(mw, a.amax[2 * a.nb + i]);
     mx = block_max(mx, sm);
     mg = block_max(mg, sm);
     mw = block_max(mw, sm);
@@ -264,7 +268,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
     const int b = blockIdx.x - (int)a.nb;
     const float scale = pow2(shift_of(mw));
     const int64_t chunks = (int64_t)a.V * lanes, all = a.vcap * lanes;
-    for (int64_t i = (int64_t)b * 256 + tid; i < all; i += (int64_t)kTableBlocks * 256) {
+    for (int64_t i = (int64_t)b * 256 + tid; i < all; i += (int64_t)a.tb * 256) {
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (i < chunks) load8f(a.W, a.x_bf16, i * 8, v);
       put8(a.w, a.vcap * a.H, i * 8, a.form, scale, v);
@@ -275,7 +279,17 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
   int64_t base = 0;
   {
     int c = 0;
-    for (int64_t i = tid; i < (int64_t)blockIdx.x; i += 256) c += a.counts[i];
+    if (a.direct) {
+      const int4* t4 = reinterpret_cast<const int4*>(a.target);
+#pragma unroll 4
+      for (int i = tid; i < (int)(blockIdx.x * a.rb / 4); i += 256) {
+        const int4 t = t4[i];
+        c += (t.x >= 0 && t.x < a.V) + (t.y >= 0 && t.y < a.V) + (t.z >= 0 && t.z < a.V) +
+             (t.w >= 0 && t.w < a.V);
+      }
+    } else {
+      for (int64_t i = tid; i < (int64_t)blockIdx.x; i += 256) c += a.counts[i];
+    }
     c = __reduce_add_sync(0xffffffffu, c);
     if (lane == 0) wsum[warp] = c;
     __syncthreads();
@@ -555,25 +569,14 @@ __device__ __forceinline__ float sum32(const uint32_t* v, float c, float m) {
   return a + b;
 }
 
-// 32 columns more to a row's sum l = sum exp2(c z - m).  m need not be the running maximum, only near
-// it: it is the maximum of the row's first columns, and moves up when a sum passes 2^40 (so nothing
-// overflows, and what an early m made too large keeps all its bits).  This takes the maximum out of
-// the common path.
-__device__ __forceinline__ void online32(const uint32_t* v, float c, bool first, float& m, float& l) {
-  float s = 0.f;
-  if (!first) s = sum32(v, c, m);
-  if (first || !(s <= 0x1p40f)) {
-    float top[4];
+// Largest of 64 columns.
+__device__ __forceinline__ float max64(const uint32_t* v) {
+  float top[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
+  for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
 #pragma unroll
-    for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(v[j]));
-    const float mn = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c);
-    l *= ex2(m - mn);
-    m = mn;
-    s = sum32(v, c, m);
-  }
-  l += s;
+  for (int j = 4; j < 64; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(v[j]));
+  return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
 
 template <int HC, int T>
@@ -701,44 +704,44 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     int tgt = -1;
     uint32_t n = 0;
     for (; w.more(); w.next(), ++n) {
-      if (w.starts) {
-        m = -3.0e38f;
-        l = 0.f;
-        tgt = a.tgt[w.t * 128 + r];
-      }
+      if (w.starts) tgt = a.tgt[w.t * 128 + r];
       const int b = n & 1;
       if (!mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 20)) break;
       tc_fence_after();
-      uint32_t x[2][32];
-      tmem_ld32(base + b * 256, x[0]);
+      uint32_t v[64];
+      tmem_ld32(base + b * 256, v);
+      tmem_ld32(base + b * 256 + 32, v + 32);
+      tmem_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->s_empty[b]);
+      const int w0 = w.j * 256 + wg * 64, at = tgt - w0;
+      const bool here = tgt >= 0 && at >= 0 && at < 64;
+      if (__any_sync(0xffffffffu, here || w.starts || w0 + 64 > a.V)) {
+        float z = 0.f;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        tmem_wait_ld();
-        if (k == 0) {
-          tmem_ld32(base + b * 256 + 32, x[1]);
-        } else {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bars->s_empty[b]);
+        for (int i = 0; i < 64; ++i) {
+          if (i == at) z = __uint_as_float(v[i]);
+          if (w0 + i >= a.V) v[i] = 0xFF800000u;
         }
-        uint32_t* v = x[k];
-        const int w0 = w.j * 256 + wg * 64 + k * 32;
-        if (w0 + 32 > a.V) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (w0 + i >= a.V) v[i] = 0xFF800000u;
+        if (here) a.hit[w.t * 128 + r] = z * (c / kLog2e);
+        if (w.starts) {
+          m = fmaxf(-3.0e38f, max64(v) * c);
+          l = 0.f;
         }
-        const int at = tgt - w0;
-        const bool here = tgt >= 0 && at >= 0 && at < 32;
-        if (__any_sync(0xffffffffu, here)) {
-          float z = 0.f;
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (i == at) z = __uint_as_float(v[i]);
-          if (here) a.hit[w.t * 128 + r] = z * (c / kLog2e);
-        }
-        online32(v, c, w.starts && k == 0, m, l);
       }
+      // l = sum exp2(c z - m).  m need not be the running maximum, only near it: it is the maximum of
+      // the row's first columns here, and moves up when a sum passes 2^40 (so nothing overflows,
+      // and what an early m made too large keeps all its bits).  This takes the maximum out of the
+      // common path.
+      float sum = sum32(v, c, m) + sum32(v + 32, c, m);
+      if (!(sum <= 0x1p40f)) {
+        const float mn = fmaxf(m, max64(v) * c);
+        l *= ex2(m - mn);
+        m = mn;
+        sum = sum32(v, c, m) + sum32(v + 32, c, m);
+      }
+      l += sum;
       if (w.ends) {
         // the sum's reference is m itself, so that the join undoes exactly what was done here
         if (un.whole(blockIdx.x, w.t))
@@ -805,15 +808,16 @@ __global__ void __launch_bounds__(256)
 
 // ------------------------------------------------------------------------------ backward
 struct BwdArgs {
-  int dw;  // the rows of W stay (dW); else the rows of X (dX)
-  int H, V, accumulate;
-  int64_t scap, pcap;  // rows of a plane of the staying and of the passing operand
+  int H, V, accumulate, out_bf16;
+  int split;  // CTAs that compute dX; the others compute dW
+  int64_t cap, vcap;
   const int* head;
   const int32_t* row;
   const int32_t* tgt;
   const float* nlse;
   const float* g;
-  void* out;
+  void* dX;
+  void* dW;
   float* part;  // [G][2][128][H]
   int* status;
 };
@@ -869,9 +873,10 @@ struct Turn {
 };
 
 // P of N columns of a row (a thread's) from their logits, for dX: nlse = -lse of the row, hit = its
-// target's place among the columns.
+// target's place among the columns, of which the first `valid` exist.
 template <int FORM, int N>
-__device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, float nlse, int hit) {
+__device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, float nlse, int hit,
+                                          int valid) {
   const uint64_t l2e = pack2(kLog2e, kLog2e), ds = pack2(descale, descale), up2 = pack2(up, up);
   const uint64_t nl = pack2(nlse, nlse);
 #pragma unroll
@@ -883,12 +888,13 @@ __device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, 
     v[i] = __float_as_uint(ex2(a));
     v[i + 1] = __float_as_uint(ex2(b));
   }
-  const bool here = hit >= 0 && hit < N;
-  if (__any_sync(0xffffffffu, here)) {
+  if (__any_sync(0xffffffffu, (hit >= 0 && hit < N) || valid < N)) {
     const float one = FORM == kBf16 ? 1.f : 32768.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
       if (i == hit) v[i] = __float_as_uint(__uint_as_float(v[i]) - one);
+      if (i >= valid) v[i] = 0;
+    }
   }
 }
 
@@ -954,10 +960,201 @@ __device__ __forceinline__ void terms(uint32_t a, uint32_t b, uint32_t& hi, uint
   }
 }
 
+// The epilogue warps of k_xent_bwd: P from z, and G to its destination.
 template <int HC, int FORM, bool DW>
+__device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, int cta, uint32_t tmem,
+                                             const uint8_t* stats, BwdBars* bars) {
+  using C = BCfg<HC, FORM>;
+  volatile int* abort = &bars->abort;
+  const uint32_t zbuf = tmem + C::GCOLS;
+  Units::Walk w(un, cta);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // a thread is a row; its warpgroup has 32 columns of each unit of its team, and GQ columns of G
+  const int q = warp & 3, wg = warp >> 2, r = q * 32 + lane;
+  constexpr int GQ = HC * 16;
+  const int team = C::TEAMS == 2 ? wg >> 1 : 0;
+  const int c0 = (C::TEAMS == 2 ? wg & 1 : wg) * C::CW;
+  const uint32_t quarter = (uint32_t)(q * 32) << 16;
+  const int sx = FORM == kBf16 ? 0 : a.head[1], sw = FORM == kBf16 ? 0 : a.head[2];
+  const float descale = FORM == kBf16 ? 1.f : pow2(max(-126, min(127, -(sx + sw))));
+  // P is scaled by 2^up: probabilities to 2^15 for dX, times g to 2^15 for dW
+  const int up = FORM == kBf16 ? 0 : DW ? a.head[3] : 15;
+  float acc[C::KEEP ? GQ : 1];
+  uint32_t groups = 0;
+  int in_group = 0, turn = 0;
+  Turn<C::ST> s;
+  Turn<C::ZB> b;
+  bool fresh = true, pending = false, ok = true;
+  float nlse = 0.f;
+  int tgt = -1;
+  // takes the finished group of G: adds it to the registers
+  auto collect = [&]() {
+    if (!mbar_wait_inline(&bars->g_full, groups & 1, a.status, 717, abort, 32)) return false;
+    ++groups;
+    tc_fence_after();
+    if (C::KEEP) {
+#pragma unroll
+      for (int c = 0; c < GQ; c += 16) {
+        uint32_t v[16];
+        tmem_ld16(tmem + quarter + wg * GQ + c, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          acc[C::KEEP ? c + i : 0] = fresh ? __uint_as_float(v[i])
+                                           : acc[C::KEEP ? c + i : 0] + __uint_as_float(v[i]);
+      }
+      fresh = false;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->g_empty);
+    }
+    return true;
+  };
+  for (; w.more() && ok; w.next(), s.next(), b.next()) {
+    if (!DW && w.starts) {
+      nlse = a.nlse[w.t * 128 + r];
+      tgt = a.tgt[w.t * 128 + r];
+    }
+    if (C::TEAMS == 1 || turn == team) {
+      ok = mbar_wait_inline(&bars->z_full[b.i], b.parity, a.status, 718, abort, 20);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t at = zbuf + quarter + b.i * C::NB + c0;
+      uint32_t v[C::CW];
+      const int w0 = w.j * C::NB + c0;
+      if (DW) {
+        // (CW / 2 registers for each half of the warp's rows)
+        if (C::CW == 32) {
+          tmem_ld_frag32(at, v);
+          tmem_ld_frag32(at + (16u << 16), v + 16);
+        } else {
+          tmem_ld_frag16(at, v);
+          tmem_ld_frag16(at + (16u << 16), v + 8);
+        }
+        tmem_wait_ld();
+        const float* st = reinterpret_cast<const float*>(stats + s.i * 2048) + c0;
+        probs_col<FORM, C::CW>(v, descale, (float)up, st, st + C::NB,
+                               reinterpret_cast<const int*>(st + 2 * C::NB), w.t * 128,
+                               w.t * 128 + q * 32 + lane / 4);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < C::CW; c += 16) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t* p = v + h * (C::CW / 2) + c / 2 + 2 * i;
+              terms<FORM>(p[0], p[1], hi[i], lo[i]);
+            }
+            tmem_st_frag8(at + (h * 16u << 16) + c, hi);
+            if (FORM != kBf16) tmem_st_frag8(at + (h * 16u << 16) + c + 8, lo);
+          }
+      } else {
+        if (C::CW == 32)
+          tmem_ld32(at, v);
+        else
+          tmem_ld16(at, v);
+        tmem_wait_ld();
+        probs_row<FORM, C::CW>(v, descale, (float)up, nlse, tgt < 0 ? -1 : tgt - w0, a.V - w0);
+#pragma unroll
+        for (int c = 0; c < C::CW; c += 16) {
+          uint32_t hi[8], lo[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) terms<FORM>(v[c + 2 * i], v[c + 2 * i + 1], hi[i], lo[i]);
+          tmem_st8(at + c, hi);
+          if (FORM != kBf16) tmem_st8(at + c + 8, lo);
+        }
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->p_full[b.i]);
+    }
+    turn ^= 1;
+    if (pending) {
+      ok = collect();
+      pending = false;
+      if (!ok) break;
+    }
+    if (++in_group == C::DRAIN || w.ends) {
+      in_group = 0;
+      pending = !w.ends;
+    }
+    if (!w.ends) continue;
+    ok = collect();
+    if (!ok) break;
+    fresh = true;
+    // the tile's result: finished where this CTA had all its units, else for the join
+    const bool whole = un.whole(cta, w.t);
+    int64_t orow = (int64_t)w.t * 128 + r;
+    float s1 = 1.f, s2 = 1.f, s3 = 1.f;
+    if (DW) {
+      if (orow >= a.V) orow = -1;
+      if (FORM != kBf16) s1 = pow2(-up), s2 = pow2(-sx);
+    } else {
+      s3 = a.g[orow];
+      orow = a.row[orow];
+      if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-sw);
+    }
+    float* pt = a.part + (((int64_t)blockIdx.x * 2 + un.slot(cta, w.t)) * 128 + r) * a.H;
+#pragma unroll
+    for (int c = 0; c < GQ; c += 16) {
+      const int col = wg * GQ + c;
+      uint32_t v[16];
+      if (C::KEEP) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(acc[C::KEEP ? c + i : 0]);
+      } else if (col < a.H) {
+        tmem_ld16(tmem + quarter + col, v);
+        tmem_wait_ld();
+      }
+      if (col >= a.H) continue;
+      float* x = reinterpret_cast<float*>(v);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<float4*>(pt + col + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        continue;
+      }
+      if (orow < 0) continue;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = x[i] * s1 * s2 * s3;
+      if (a.out_bf16) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(DW ? a.dW : a.dX) + orow * a.H + col;
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+          __nv_bfloat162 h[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[k] = __floats2bfloat162_rn(x[i + 2 * k], x[i + 2 * k + 1]);
+          *reinterpret_cast<uint4*>(o + i) = *reinterpret_cast<const uint4*>(h);
+        }
+      } else {
+        float* o = static_cast<float*>(DW ? a.dW : a.dX) + orow * a.H + col;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          float4 h = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          if (a.accumulate) {
+            const float4 p = *reinterpret_cast<const float4*>(o + i);
+            h = make_float4(h.x + p.x, h.y + p.y, h.z + p.z, h.w + p.w);
+          }
+          *reinterpret_cast<float4*>(o + i) = h;
+        }
+      }
+    }
+    if (!C::KEEP) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->g_empty);
+    }
+  }
+}
+
+// The first a.split CTAs compute dX (X stays), the others dW (W stays): the two have as many units.
+template <int HC, int FORM>
 __global__ void __launch_bounds__(kBwdThreads, 1)
-    k_xent_bwd(const __grid_constant__ CUtensorMap tmS, const __grid_constant__ CUtensorMap tmB,
-               BwdArgs a, int out_bf16) {
+    k_xent_bwd(const __grid_constant__ CUtensorMap tmXs, const __grid_constant__ CUtensorMap tmXp,
+               const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmWp,
+               const __grid_constant__ BwdArgs a) {
   using C = BCfg<HC, FORM>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -997,15 +1194,21 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   grid_dep_wait();
   const uint32_t tmem = bars->tmem, zbuf = tmem + C::GCOLS;
   const int64_t rows = a.head[0];
-  const Units un(DW ? (a.V + 127) / 128 : (rows + 127) / 128,
-                 DW ? (rows + C::NB - 1) / C::NB : (a.V + C::NB - 1) / C::NB, gridDim.x);
+  const bool dw = (int)blockIdx.x >= a.split;
+  const int cta = blockIdx.x - (dw ? a.split : 0);
+  const Units un(dw ? (a.V + 127) / 128 : (rows + 127) / 128,
+                 dw ? (rows + C::NB - 1) / C::NB : (a.V + C::NB - 1) / C::NB,
+                 dw ? gridDim.x - a.split : a.split);
 
   if (warp == 16) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (lane == 0) {
-      Units::Walk w(un, blockIdx.x);
-      tma_prefetch_desc(&tmS);
-      tma_prefetch_desc(&tmB);
+      Units::Walk w(un, cta);
+      const CUtensorMap* tmS = dw ? &tmWs : &tmXs;
+      const CUtensorMap* tmB = dw ? &tmXp : &tmWp;
+      const int splane = (int)(dw ? a.vcap : a.cap), pplane = (int)(dw ? a.cap : a.vcap);
+      tma_prefetch_desc(tmS);
+      tma_prefetch_desc(tmB);
       uint32_t it = 0, seg = 0;
       Turn<C::ST> s;
       bool ok = true;
@@ -1015,17 +1218,17 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
           if (!ok) break;
           mbar_expect_tx(&bars->s_full, C::S_BYTES);
           for (int p = 0; p < C::T * HC; ++p)
-            tma_load_2d(smem + p * 16384, &tmS, &bars->s_full, p % HC * 64,
-                        (int)((p / HC) * a.scap) + w.t * 128);
+            tma_load_2d(smem + p * 16384, tmS, &bars->s_full, p % HC * 64,
+                        p / HC * splane + w.t * 128);
           ++seg;
         }
         ok = mbar_wait_inline(&bars->empty[s.i], s.parity ^ 1, a.status, 712, abort, 32);
         if (!ok) break;
-        mbar_expect_tx(&bars->full[s.i], C::B_BYTES + (DW ? C::STATS : 0));
+        mbar_expect_tx(&bars->full[s.i], C::B_BYTES + (dw ? C::STATS : 0));
         for (int p = 0; p < C::T * HC; ++p)
-          tma_load_2d(ring + s.i * C::B_BYTES + p * C::BOX, &tmB, &bars->full[s.i], p % HC * 64,
-                      (int)((p / HC) * a.pcap) + w.j * C::NB);
-        if (DW) {
+          tma_load_2d(ring + s.i * C::B_BYTES + p * C::BOX, tmB, &bars->full[s.i], p % HC * 64,
+                      p / HC * pplane + w.j * C::NB);
+        if (dw) {
           uint8_t* d = stats + s.i * 2048;
           const int64_t at = (int64_t)w.j * C::NB;
           bulk_load(d, a.nlse + at, C::NB * 4, &bars->full[s.i]);
@@ -1044,7 +1247,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   } else if (warp == 17) {
     // z = S B^T, as many units ahead as tensor memory and the ring hold
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    Units::Walk w(un, blockIdx.x);
+    Units::Walk w(un, cta);
     const bool leader = elect_one_sync();
     const uint32_t iz = idesc16(FORM == kBf16, C::NB, 0);
     // a descriptor's address field is in 16 bytes
@@ -1089,7 +1292,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   } else if (warp == 18) {
     // G (+)= P B, small products first
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    Units::Walk w(un, blockIdx.x);
+    Units::Walk w(un, cta);
     const bool leader = elect_one_sync();
     const uint32_t ig = idesc16(FORM == kBf16, a.H, 1);
     const uint64_t R = desc_sw128_mnmajor(smem_u32(ring), C::BOX);
@@ -1137,190 +1340,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    Units::Walk w(un, blockIdx.x);
-    // a thread is a row; its warpgroup has 32 columns of each unit of its team, and GQ columns of G
-    const int q = warp & 3, wg = warp >> 2, r = q * 32 + lane;
-    constexpr int GQ = HC * 16;
-    const int team = C::TEAMS == 2 ? wg >> 1 : 0;
-    const int c0 = (C::TEAMS == 2 ? wg & 1 : wg) * C::CW;
-    const uint32_t quarter = (uint32_t)(q * 32) << 16;
-    const int sx = FORM == kBf16 ? 0 : a.head[1], sw = FORM == kBf16 ? 0 : a.head[2];
-    const float descale = FORM == kBf16 ? 1.f : pow2(max(-126, min(127, -(sx + sw))));
-    // P is scaled by 2^up: probabilities to 2^15 for dX, times g to 2^15 for dW
-    const int up = FORM == kBf16 ? 0 : DW ? a.head[3] : 15;
-    float acc[C::KEEP ? GQ : 1];
-    uint32_t groups = 0;
-    int in_group = 0, turn = 0;
-    Turn<C::ST> s;
-    Turn<C::ZB> b;
-    bool fresh = true, pending = false, ok = true;
-    float nlse = 0.f;
-    int tgt = -1;
-    // takes the finished group of G: adds it to the registers
-    auto collect = [&]() {
-      if (!mbar_wait_inline(&bars->g_full, groups & 1, a.status, 717, abort, 32)) return false;
-      ++groups;
-      tc_fence_after();
-      if (C::KEEP) {
-#pragma unroll
-        for (int c = 0; c < GQ; c += 16) {
-          uint32_t v[16];
-          tmem_ld16(tmem + quarter + wg * GQ + c, v);
-          tmem_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            acc[C::KEEP ? c + i : 0] = fresh ? __uint_as_float(v[i])
-                                             : acc[C::KEEP ? c + i : 0] + __uint_as_float(v[i]);
-        }
-        fresh = false;
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->g_empty);
-      }
-      return true;
-    };
-    for (; w.more() && ok; w.next(), s.next(), b.next()) {
-      if (!DW && w.starts) {
-        nlse = a.nlse[w.t * 128 + r];
-        tgt = a.tgt[w.t * 128 + r];
-      }
-      if (C::TEAMS == 1 || turn == team) {
-        ok = mbar_wait_inline(&bars->z_full[b.i], b.parity, a.status, 718, abort, 20);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t at = zbuf + quarter + b.i * C::NB + c0;
-        uint32_t v[C::CW];
-        const int w0 = w.j * C::NB + c0;
-        if (DW) {
-          // (CW / 2 registers for each half of the warp's rows)
-          if (C::CW == 32) {
-            tmem_ld_frag32(at, v);
-            tmem_ld_frag32(at + (16u << 16), v + 16);
-          } else {
-            tmem_ld_frag16(at, v);
-            tmem_ld_frag16(at + (16u << 16), v + 8);
-          }
-          tmem_wait_ld();
-          const float* st = reinterpret_cast<const float*>(stats + s.i * 2048) + c0;
-          probs_col<FORM, C::CW>(v, descale, (float)up, st, st + C::NB,
-                                 reinterpret_cast<const int*>(st + 2 * C::NB), w.t * 128,
-                                 w.t * 128 + q * 32 + lane / 4);
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int c = 0; c < C::CW; c += 16) {
-              uint32_t hi[4], lo[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t* p = v + h * (C::CW / 2) + c / 2 + 2 * i;
-                terms<FORM>(p[0], p[1], hi[i], lo[i]);
-              }
-              tmem_st_frag8(at + (h * 16u << 16) + c, hi);
-              if (FORM != kBf16) tmem_st_frag8(at + (h * 16u << 16) + c + 8, lo);
-            }
-        } else {
-          if (C::CW == 32)
-            tmem_ld32(at, v);
-          else
-            tmem_ld16(at, v);
-          tmem_wait_ld();
-          probs_row<FORM, C::CW>(v, descale, (float)up, nlse, tgt < 0 ? -1 : tgt - w0);
-          if (w0 + C::CW > a.V) {
-#pragma unroll
-            for (int i = 0; i < C::CW; ++i)
-              if (w0 + i >= a.V) v[i] = 0;
-          }
-#pragma unroll
-          for (int c = 0; c < C::CW; c += 16) {
-            uint32_t hi[8], lo[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) terms<FORM>(v[c + 2 * i], v[c + 2 * i + 1], hi[i], lo[i]);
-            tmem_st8(at + c, hi);
-            if (FORM != kBf16) tmem_st8(at + c + 8, lo);
-          }
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->p_full[b.i]);
-      }
-      turn ^= 1;
-      if (pending) {
-        ok = collect();
-        pending = false;
-        if (!ok) break;
-      }
-      if (++in_group == C::DRAIN || w.ends) {
-        in_group = 0;
-        pending = !w.ends;
-      }
-      if (!w.ends) continue;
-      ok = collect();
-      if (!ok) break;
-      fresh = true;
-      // the tile's result: finished where this CTA had all its units, else for the join
-      const bool whole = un.whole(blockIdx.x, w.t);
-      int64_t orow = (int64_t)w.t * 128 + r;
-      float s1 = 1.f, s2 = 1.f, s3 = 1.f;
-      if (DW) {
-        if (orow >= a.V) orow = -1;
-        if (FORM != kBf16) s1 = pow2(-up), s2 = pow2(-sx);
-      } else {
-        s3 = a.g[orow];
-        orow = a.row[orow];
-        if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-sw);
-      }
-      float* pt = a.part + (((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, w.t)) * 128 + r) * a.H;
-#pragma unroll
-      for (int c = 0; c < GQ; c += 16) {
-        const int col = wg * GQ + c;
-        uint32_t v[16];
-        if (C::KEEP) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(acc[C::KEEP ? c + i : 0]);
-        } else if (col < a.H) {
-          tmem_ld16(tmem + quarter + col, v);
-          tmem_wait_ld();
-        }
-        if (col >= a.H) continue;
-        float* x = reinterpret_cast<float*>(v);
-        if (!whole) {
-#pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<float4*>(pt + col + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-          continue;
-        }
-        if (orow < 0) continue;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = x[i] * s1 * s2 * s3;
-        if (out_bf16) {
-          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.out) + orow * a.H + col;
-#pragma unroll
-          for (int i = 0; i < 16; i += 8) {
-            __nv_bfloat162 h[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) h[k] = __floats2bfloat162_rn(x[i + 2 * k], x[i + 2 * k + 1]);
-            *reinterpret_cast<uint4*>(o + i) = *reinterpret_cast<const uint4*>(h);
-          }
-        } else {
-          float* o = static_cast<float*>(a.out) + orow * a.H + col;
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            float4 h = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-            if (a.accumulate) {
-              const float4 p = *reinterpret_cast<const float4*>(o + i);
-              h = make_float4(h.x + p.x, h.y + p.y, h.z + p.z, h.w + p.w);
-            }
-            *reinterpret_cast<float4*>(o + i) = h;
-          }
-        }
-      }
-      if (!C::KEEP) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->g_empty);
-      }
-    }
+    if (dw)
+      bwd_epilogue<HC, FORM, true>(a, un, cta, tmem, stats, bars);
+    else
+      bwd_epilogue<HC, FORM, false>(a, un, cta, tmem, stats, bars);
   }
   tc_fence_before();
   __syncthreads();
@@ -1335,27 +1358,29 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 // takes the tile that CTA c is the first to begin inside of, 32 rows x 32 columns a block; without
 // labelled rows the tiles of dW are written as zeros here.
 __global__ void __launch_bounds__(256)
-    k_xent_bwd_join(BwdArgs a, int form, int nb, int out_bf16) {
+    k_xent_bwd_join(BwdArgs a, int form, int nb) {
   grid_dep_launch();
   grid_dep_wait();
   const int64_t rows = a.head[0];
-  const int64_t rt = a.dw ? (a.V + 127) / 128 : (rows + 127) / 128;
-  const Units un(rt, a.dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, gridDim.x);
+  const bool dw = (int)blockIdx.x >= a.split;
+  const int c = blockIdx.x - (dw ? a.split : 0), ctas = dw ? gridDim.x - a.split : a.split;
+  const Units un(dw ? (a.V + 127) / 128 : (rows + 127) / 128,
+                 dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, ctas);
+  void* out = dw ? a.dW : a.dX;
   const int hb = a.H / 32;
   const int col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x & 7) * 4;
   const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x >> 3);
   if (un.ct == 0) {
-    if (!a.dw || a.accumulate) return;
-    for (int64_t v = (int64_t)blockIdx.x * 128 + r; v < a.V; v += (int64_t)gridDim.x * 128) {
-      if (out_bf16)
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + v * a.H + col) = make_uint2(0, 0);
+    if (!dw || a.accumulate) return;
+    for (int64_t v = (int64_t)c * 128 + r; v < a.V; v += (int64_t)ctas * 128) {
+      if (a.out_bf16)
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + v * a.H + col) = make_uint2(0, 0);
       else
-        *reinterpret_cast<float4*>(static_cast<float*>(a.out) + v * a.H + col) =
+        *reinterpret_cast<float4*>(static_cast<float*>(out) + v * a.H + col) =
             make_float4(0.f, 0.f, 0.f, 0.f);
     }
     return;
   }
-  const int c = blockIdx.x;
   const int64_t begin = un.begin(c);
   if (c >= un.G || c == 0 || begin % un.ct == 0) return;
   const int64_t t = begin / un.ct, first = t * un.ct, end = first + un.ct;
@@ -1364,7 +1389,7 @@ __global__ void __launch_bounds__(256)
   float s1 = 1.f, s2 = 1.f, s3 = 1.f;
   // CTA c - 1 has the first part (in its second place unless the tile is its first), the others begin
   // with this tile
-  const float* part = a.part + (int64_t)r * a.H + col;
+  const float* part = a.part + ((int64_t)(blockIdx.x - c) * 2 * 128 + r) * a.H + col;
   const int64_t stride = 128LL * a.H;
   float4 x = *reinterpret_cast<const float4*>(part + ((int64_t)(c - 1) * 2 + un.slot(c - 1, t)) * stride);
   int last = c;
@@ -1374,7 +1399,7 @@ __global__ void __launch_bounds__(256)
     const float4 p = *reinterpret_cast<const float4*>(part + (int64_t)k * 2 * stride);
     x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
   }
-  if (a.dw) {
+  if (dw) {
     if (orow >= a.V) return;
     if (form != kBf16) s1 = pow2(-a.head[3]), s2 = pow2(-a.head[1]);
   } else {
@@ -1384,12 +1409,12 @@ __global__ void __launch_bounds__(256)
     if (form != kBf16) s1 = pow2(-15), s2 = pow2(-a.head[2]);
   }
   x = make_float4(x.x * s1 * s2 * s3, x.y * s1 * s2 * s3, x.z * s1 * s2 * s3, x.w * s1 * s2 * s3);
-  if (out_bf16) {
+  if (a.out_bf16) {
     __nv_bfloat162 w[2] = {__floats2bfloat162_rn(x.x, x.y), __floats2bfloat162_rn(x.z, x.w)};
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + orow * a.H + col) =
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + orow * a.H + col) =
         *reinterpret_cast<const uint2*>(w);
   } else {
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.out) + orow * a.H + col);
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + orow * a.H + col);
     if (a.accumulate) {
       const float4 p = *o;
       x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
@@ -1405,7 +1430,6 @@ struct Call {
   Ws w;
   char* base;
   cudaStream_t st;
-  CUtensorMap x128, w128;  // boxes of 128 rows
   template <typename P>
   P* at(size_t off) const { return reinterpret_cast<P*>(base + off); }
 };
@@ -1434,14 +1458,19 @@ cudaError_t prepare(const XentArgs& a, Call& c, RowArgs r) {
   r.x = c.at<uint16_t>(c.w.x);
   r.w = c.at<uint16_t>(c.w.w);
   r.status = a.status;
-  const int table = c.form == kBf16 ? 0 : kTableBlocks;
+  // Up to kDirectRows rows, each block of k_xent_rows counts the rows before its own (at most 128 KB of
+  // targets, from L2) in less time than a launch takes; the fp16 forms need the magnitudes first anyway.
+  r.direct = c.form == kBf16 && a.n <= kDirectRows;
+  // of the table, at least four passes of 256 threads a block
+  r.tb = c.form == kBf16 ? 0
+                         : (int)std::min<int64_t>(kTableBlocks, ((int64_t)a.V * (a.H / 8) + 1023) / 1024);
   cudaError_t e;
-  if (c.w.nb > 1 || c.form != kBf16) {
-    e = launch_pdl(k_xent_count, dim3((unsigned)c.w.nb + table), dim3(256), 0, c.st, r);
+  if (!r.direct) {
+    e = launch_pdl(k_xent_count, dim3((unsigned)c.w.nb + r.tb), dim3(256), 0, c.st, r);
     if (e != cudaSuccess) return e;
     note_launch();
   }
-  e = launch_pdl(k_xent_rows, dim3((unsigned)c.w.nb + table), dim3(256), 0, c.st, r);
+  e = launch_pdl(k_xent_rows, dim3((unsigned)c.w.nb + r.tb), dim3(256), 0, c.st, r);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
@@ -1457,45 +1486,57 @@ bool map_w(const Call& c, const void* W, CUtensorMap* m, int box) {
   return make_map_ld(m, c.base + c.w.w, (c.form == kF16x2 ? 2 : 1) * c.w.vcap, c.H, c.H, box);
 }
 
+// Lets a kernel use `bytes` of dynamic shared memory, once a device.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 template <int HC, int T>
 cudaError_t run_fwd(const Call& c, const void* W, const FwdArgs& f) {
   using C = FCfg<HC, T>;
   CUtensorMap mx, mw;
   if (!map_x(c, &mx, 128) || !map_w(c, W, &mw, 256)) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(k_xent_fwd<HC, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       C::SMEM);
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = allow_smem(k_xent_fwd<HC, T>, C::SMEM, done);
   if (e != cudaSuccess) return e;
   return launch_pdl(k_xent_fwd<HC, T>, dim3(c.sms), dim3(kFwdThreads), C::SMEM, c.st, mx, mw, f);
 }
 
-template <int HC, int FORM, bool DW>
-cudaError_t run_bwd(const Call& c, const void* W, const BwdArgs& b, int out_bf16) {
+template <int HC, int FORM>
+cudaError_t run_bwd(const Call& c, const void* W, const BwdArgs& b) {
   using C = BCfg<HC, FORM>;
-  CUtensorMap ms, mb;
-  if (!(DW ? map_w(c, W, &ms, 128) && map_x(c, &mb, C::NB)
-           : map_x(c, &ms, 128) && map_w(c, W, &mb, C::NB)))
+  CUtensorMap xs, xp, ws, wp;
+  if (!map_x(c, &xs, 128) || !map_x(c, &xp, C::NB) || !map_w(c, W, &ws, 128) ||
+      !map_w(c, W, &wp, C::NB))
     return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(k_xent_bwd<HC, FORM, DW>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = allow_smem(k_xent_bwd<HC, FORM>, C::SMEM, done);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(k_xent_bwd<HC, FORM, DW>, dim3(c.sms), dim3(kBwdThreads), C::SMEM, c.st, ms, mb, b,
-                 out_bf16);
+  e = launch_pdl(k_xent_bwd<HC, FORM>, dim3(c.sms), dim3(kBwdThreads), C::SMEM, c.st, xs, xp, ws, wp,
+                 b);
   if (e != cudaSuccess) return e;
   note_launch();
-  e = launch_pdl(k_xent_bwd_join, dim3(c.sms, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM, C::NB,
-                 out_bf16);
+  e = launch_pdl(k_xent_bwd_join, dim3(c.sms, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM, C::NB);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
 }
 
-template <int FORM, bool DW>
-cudaError_t run_bwd_h(const Call& c, const void* W, const BwdArgs& b, int out_bf16) {
+template <int FORM>
+cudaError_t run_bwd_h(const Call& c, const void* W, const BwdArgs& b) {
   switch ((c.H + 63) / 64) {
-    case 1: return run_bwd<1, FORM, DW>(c, W, b, out_bf16);
-    case 2: return run_bwd<2, FORM, DW>(c, W, b, out_bf16);
-    case 3: return run_bwd<3, FORM, DW>(c, W, b, out_bf16);
-    default: return run_bwd<4, FORM, DW>(c, W, b, out_bf16);
+    case 1: return run_bwd<1, FORM>(c, W, b);
+    case 2: return run_bwd<2, FORM>(c, W, b);
+    case 3: return run_bwd<3, FORM>(c, W, b);
+    default: return run_bwd<4, FORM>(c, W, b);
   }
 }
 
@@ -1580,21 +1621,15 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
   b.g = c.at<float>(c.w.g);
   b.part = c.at<float>(c.w.part);
   b.status = a.status;
-  for (int dw = 0; dw < 2; ++dw) {
-    b.dw = dw;
-    b.out = dw ? dW : dX;
-    b.scap = dw ? c.w.vcap : c.w.cap;
-    b.pcap = dw ? c.w.cap : c.w.vcap;
-    if (!b.out) continue;
-    if (form == kBf16)
-      e = dw ? run_bwd_h<kBf16, true>(c, a.W, b, 1) : run_bwd_h<kBf16, false>(c, a.W, b, 1);
-    else if (form == kF16x1)
-      e = dw ? run_bwd_h<kF16x1, true>(c, a.W, b, 0) : run_bwd_h<kF16x1, false>(c, a.W, b, 0);
-    else
-      e = dw ? run_bwd_h<kF16x2, true>(c, a.W, b, 0) : run_bwd_h<kF16x2, false>(c, a.W, b, 0);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
+  b.out_bf16 = grad_bf16;
+  b.split = !dW ? c.sms : !dX ? 0 : c.sms / 2;
+  b.cap = c.w.cap;
+  b.vcap = c.w.vcap;
+  b.dX = dX;
+  b.dW = dW;
+  if (form == kBf16) return run_bwd_h<kBf16>(c, a.W, b);
+  if (form == kF16x1) return run_bwd_h<kF16x1>(c, a.W, b);
+  return run_bwd_h<kF16x2>(c, a.W, b);
 }
 
 }  // namespace bg
