@@ -7,7 +7,7 @@
 //   k_xent_count, k_xent_rows   the labelled rows of X, gathered side by side (rows left out cost
 //                               nothing after this and may hold anything), and the operands' 16-bit forms
 //   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, running maximum and sum
-//   k_xent_bwd (+ join)         128 x 128 (64) tiles of z recomputed, P written back over z in tensor
+//   k_xent_bwd (+ join)         128 x 128 tiles of z recomputed, P written back over z in tensor
 //                               memory as the A operand of the second product; once with the rows of X
 //                               staying (dX) and once with the rows of W (dW)
 // A staying tile of 128 rows against one passing tile is a unit; the units of a launch, staying tile
@@ -825,20 +825,19 @@ struct BwdArgs {
 // One unit: z = S B^T (S the staying tile, B the passing one), P from z, G += P B.  B serves both
 // products: as its rows lie (K-major) in the first, transposed (MN-major) in the second.
 //
-// A passing tile has 128 rows, and 64 at H > 128, where 128 would leave room for two ring stages and
-// the loads would be waited for (measured at H = 256: 3700 cycles per 128 rows instead of the 2048
-// that the products take).  Tensor memory holds G and as many units' z as fit beside it.
+// A passing tile has 128 rows, and 64 with two terms at H > 128, where 128 would not fit.  Tensor memory
+// holds G and as many units' z as fit beside it.  The two products are issued by a warp each: with one
+// warp, G of a unit that is ready would wait behind the next unit's z, and that for its load (measured
+// at H = 256 with two ring stages: 3660 cycles a unit instead of the 2048 that the products take).
 template <int HC, int FORM>
 struct BCfg {
   static constexpr int T = FORM == kF16x2 ? 2 : 1;   // terms of S and B
   static constexpr int PT = FORM == kBf16 ? 1 : 2;   // terms of P
   static constexpr bool KEEP = FORM != kBf16;        // G is added up in registers
-  static constexpr int NB = HC > 2 ? 64 : 128;       // passing rows of a unit
-  // Units of 64 rows: two teams of warps take them in turn, 32 columns a thread; where a thread also
-  // holds 64 sums, all warps take every unit, 16 columns a thread.
-  static constexpr int TEAMS = NB == 64 && !KEEP ? 2 : 1;
-  static constexpr int WARPS = 16 / TEAMS;           // of a team
-  static constexpr int CW = NB * TEAMS / 4;          // columns of a thread
+  static constexpr int NB = HC > 2 && T == 2 ? 64 : 128;  // passing rows of a unit
+  static constexpr int CW = NB / 4;                  // columns of z of a thread
+  // of which it works on so many at a time: fewer where it also holds up to 64 sums
+  static constexpr int PW = KEEP && HC > 2 ? 16 : CW;
   static constexpr int S_BYTES = T * HC * 16384;
   static constexpr int BOX = NB * 128;  // 64 elements of each passing row
   static constexpr int B_BYTES = T * HC * BOX;
@@ -852,7 +851,7 @@ struct BCfg {
   static constexpr int STEPS = NB / 16 * (T == 2 ? 3 : PT);  // accumulating steps of a unit
   static constexpr int DRAIN = KEEP ? kDrainSteps / STEPS : 1 << 30;  // units before G leaves TMEM
   static_assert(ST >= 1 && SMEM <= 232448, "shared memory");
-  static_assert(ZB >= 2 && ZB % TEAMS == 0, "tensor memory");
+  static_assert(ZB >= 2, "tensor memory");
   static_assert(DRAIN >= 1, "drain interval");
 };
 
@@ -969,11 +968,10 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
   const uint32_t zbuf = tmem + C::GCOLS;
   Units::Walk w(un, cta);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // a thread is a row; its warpgroup has 32 columns of each unit of its team, and GQ columns of G
+  // a thread is a row; its warpgroup has CW columns of each unit and GQ columns of G
   const int q = warp & 3, wg = warp >> 2, r = q * 32 + lane;
   constexpr int GQ = HC * 16;
-  const int team = C::TEAMS == 2 ? wg >> 1 : 0;
-  const int c0 = (C::TEAMS == 2 ? wg & 1 : wg) * C::CW;
+  const int c0 = wg * C::CW;
   const uint32_t quarter = (uint32_t)(q * 32) << 16;
   const int sx = FORM == kBf16 ? 0 : a.head[1], sw = FORM == kBf16 ? 0 : a.head[2];
   const float descale = FORM == kBf16 ? 1.f : pow2(max(-126, min(127, -(sx + sw))));
@@ -981,7 +979,7 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
   const int up = FORM == kBf16 ? 0 : DW ? a.head[3] : 15;
   float acc[C::KEEP ? GQ : 1];
   uint32_t groups = 0;
-  int in_group = 0, turn = 0;
+  int in_group = 0;
   Turn<C::ST> s;
   Turn<C::ZB> b;
   bool fresh = true, pending = false, ok = true;
@@ -1015,16 +1013,17 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       nlse = a.nlse[w.t * 128 + r];
       tgt = a.tgt[w.t * 128 + r];
     }
-    if (C::TEAMS == 1 || turn == team) {
-      ok = mbar_wait_inline(&bars->z_full[b.i], b.parity, a.status, 718, abort, 20);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t at = zbuf + quarter + b.i * C::NB + c0;
-      uint32_t v[C::CW];
-      const int w0 = w.j * C::NB + c0;
+    ok = mbar_wait_inline(&bars->z_full[b.i], b.parity, a.status, 718, abort, 20);
+    if (!ok) break;
+    tc_fence_after();
+#pragma unroll
+    for (int pc = 0; pc < C::CW; pc += C::PW) {
+      const uint32_t at = zbuf + quarter + b.i * C::NB + c0 + pc;
+      uint32_t v[C::PW];
+      const int w0 = w.j * C::NB + c0 + pc;
       if (DW) {
-        // (CW / 2 registers for each half of the warp's rows)
-        if (C::CW == 32) {
+        // (PW / 2 registers for each half of the warp's rows)
+        if (C::PW == 32) {
           tmem_ld_frag32(at, v);
           tmem_ld_frag32(at + (16u << 16), v + 16);
         } else {
@@ -1032,32 +1031,32 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
           tmem_ld_frag16(at + (16u << 16), v + 8);
         }
         tmem_wait_ld();
-        const float* st = reinterpret_cast<const float*>(stats + s.i * 2048) + c0;
-        probs_col<FORM, C::CW>(v, descale, (float)up, st, st + C::NB,
+        const float* st = reinterpret_cast<const float*>(stats + s.i * 2048) + c0 + pc;
+        probs_col<FORM, C::PW>(v, descale, (float)up, st, st + C::NB,
                                reinterpret_cast<const int*>(st + 2 * C::NB), w.t * 128,
                                w.t * 128 + q * 32 + lane / 4);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int c = 0; c < C::CW; c += 16) {
+          for (int c = 0; c < C::PW; c += 16) {
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t* p = v + h * (C::CW / 2) + c / 2 + 2 * i;
+              const uint32_t* p = v + h * (C::PW / 2) + c / 2 + 2 * i;
               terms<FORM>(p[0], p[1], hi[i], lo[i]);
             }
             tmem_st_frag8(at + (h * 16u << 16) + c, hi);
             if (FORM != kBf16) tmem_st_frag8(at + (h * 16u << 16) + c + 8, lo);
           }
       } else {
-        if (C::CW == 32)
+        if (C::PW == 32)
           tmem_ld32(at, v);
         else
           tmem_ld16(at, v);
         tmem_wait_ld();
-        probs_row<FORM, C::CW>(v, descale, (float)up, nlse, tgt < 0 ? -1 : tgt - w0, a.V - w0);
+        probs_row<FORM, C::PW>(v, descale, (float)up, nlse, tgt < 0 ? -1 : tgt - w0, a.V - w0);
 #pragma unroll
-        for (int c = 0; c < C::CW; c += 16) {
+        for (int c = 0; c < C::PW; c += 16) {
           uint32_t hi[8], lo[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) terms<FORM>(v[c + 2 * i], v[c + 2 * i + 1], hi[i], lo[i]);
@@ -1065,12 +1064,11 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
           if (FORM != kBf16) tmem_st8(at + c + 8, lo);
         }
       }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->p_full[b.i]);
     }
-    turn ^= 1;
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&bars->p_full[b.i]);
     if (pending) {
       ok = collect();
       pending = false;
@@ -1174,7 +1172,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     for (int b = 0; b < C::ZB; ++b) {
       mbar_init(&bars->z_full[b], 1);
       mbar_init(&bars->z_empty[b], 1);
-      mbar_init(&bars->p_full[b], C::WARPS);
+      mbar_init(&bars->p_full[b], 16);
     }
     mbar_init(&bars->g_full, 1);
     mbar_init(&bars->g_empty, 16);
