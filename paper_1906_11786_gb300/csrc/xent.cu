@@ -389,24 +389,24 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
 
 // ------------------------------------------------------------------------------ units
 // Unit u = t * ct + j is staying tile t against passing tile j; CTA c takes [begin(c), begin(c + 1)).
+// Where a tile has few units (kWholeUnits), the runs are of whole tiles: nothing is left to join, and
+// the launch that would do it is saved.
 // With fewer units than CTAs the last CTAs take none, so that those between a tile's first and last
 // all have a part of it.
+constexpr int kWholeUnits = 4;
 struct Units {
   int64_t ct, U;
   int G;  // CTAs that take units
   int step, nt;
-  __device__ Units(int64_t rt, int64_t ct_, int ctas, int step_ = 1)
-      : ct(ct_), U(rt * ct_), G((int)min((int64_t)ctas, rt * ct_)), step(step_), nt((int)rt) {}
+  bool tiles;  // runs are of whole staying tiles
+  __device__ Units(int64_t rt, int64_t ct_, int ctas, bool tiles_, int step_ = 1)
+      : ct(ct_), U(rt * ct_), G((int)min((int64_t)ctas, tiles_ ? rt : rt * ct_)), step(step_),
+        nt((int)rt), tiles(tiles_) {}
   // The rows that staying tile t stands for: tile t * step mod nt (step prime to nt).  Tiles of
   // frequent tokens, whose units take up to half as long again, then do not all fall to one CTA.
   __device__ int tile(int t) const { return step == 1 ? t : (int)((uint32_t)t * (uint64_t)(uint32_t)step % (uint32_t)nt); }
-  __device__ int64_t begin(int c) const { return c >= G ? U : U * c / G; }
-  // the CTA that unit u falls to (u < U)
-  __device__ int owner(int64_t u) const {
-    int c = (int)(u * G / U);
-    while (begin(c + 1) <= u) ++c;
-    while (begin(c) > u) --c;
-    return c;
+  __device__ int64_t begin(int c) const {
+    return c >= G ? U : tiles ? (int64_t)nt * c / G * ct : U * c / G;
   }
   // staying and passing tile of the next unit of a run
   struct Walk {
@@ -430,6 +430,8 @@ struct Units {
       ends = left == 1 || j + 1 == ct;
     }
   };
+  // the last CTA with units before `end` (runs that share tiles)
+  __device__ int last_before(int64_t end) const { return (int)((end * G + U - 1) / U) - 1; }
   // whether CTA c has all units of tile t
   __device__ bool whole(int c, int64_t t) const { return begin(c) <= t * ct && t * ct + ct <= begin(c + 1); }
   // which of its two partial results CTA c keeps of tile t, one it shares with others
@@ -532,14 +534,50 @@ constexpr int kMaxStages = 6;
 // ------------------------------------------------------------------------------ forward
 struct FwdArgs {
   int H, V;
-  int64_t cap, vcap;
+  int direct;  // X is the caller's, all n rows of it
+  int tiles;   // runs of whole tiles
+  int64_t n, cap, vcap;
   const int* head;
+  const int32_t* target;  // direct: the caller's
+  const int32_t* row;
   const float* stat;
   float* hit;    // [cap] logit of the target
-  float2* full;  // [4][cap] reference and sum of each quarter, of the tiles one CTA has all units of
-  float2* part;  // [G][2][4][128] of the others
+  float2* full;  // [4][cap] reference and sum of each quarter of the columns
+  float2* part;  // [G][2][4][128] the same of tiles shared by CTAs
+  float* loss;
+  float* lse;
   int* status;
 };
+
+__device__ __forceinline__ int64_t fwd_rows(const FwdArgs& a) { return a.direct ? a.n : a.head[0]; }
+
+// Target of slot s, -1 where there is none.
+__device__ __forceinline__ int fwd_target(const FwdArgs& a, int64_t s) {
+  if (!a.direct) return __float_as_int(a.stat[stat_at(s) + kTgt]);
+  int t = s < a.n ? a.target[s] : -1;
+  if (t >= a.V) {
+    if (atomicCAS(a.status, 0, 2) == 0) atomicExch(a.status + 1, kSiteXentTarget);
+    t = -1;
+  }
+  return t;
+}
+
+// lse and loss of slot s from the reference `top` (in units of kLog2e z) and the sum l to it.
+__device__ __forceinline__ void fwd_finish(const FwdArgs& a, int64_t s, int tgt, float top, float l) {
+  const int64_t i = a.direct ? s : a.row[s];
+  if (i < 0 || i >= a.n) return;
+  float v = 0.f, loss = 0.f;
+  if (tgt >= 0) {
+    // (top + log2 l) / c with c = kLog2e as it was rounded, 1 / c in two parts, so that the only error
+    // that counts is the result's own rounding
+    constexpr float inv = (float)(1.0 / (double)kLog2e), rest = (float)(1.0 / (double)kLog2e - (double)inv);
+    const float hi = top * inv, lo = fmaf(top, inv, -hi) + fmaf(top, rest, log2f(l) * inv);
+    v = hi + lo;
+    loss = (hi - a.hit[s]) + lo;
+  }
+  a.lse[i] = v;
+  a.loss[i] = loss;
+}
 
 // z tiles of 128 rows x 256 columns.  X's tile stays in shared memory, W passes through a ring in
 // pieces of 256 rows x 64 elements, two accumulators of 256 columns fill tensor memory.
@@ -555,7 +593,7 @@ struct FCfg {
 };
 
 struct FwdBars {
-  uint64_t a_full, a_empty, full[6], empty[6], s_full[2], s_empty[2], drain;
+  uint64_t a_full, a_empty, full[6], empty[6], s_full[2], s_empty[2], q_full, drain;
   uint32_t tmem;
   int abort;
 };
@@ -590,7 +628,7 @@ __device__ __forceinline__ float max64(const uint32_t* v) {
 template <int HC, int T>
 __global__ void __launch_bounds__(kFwdThreads, 1)
     k_xent_fwd(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
-               FwdArgs a) {
+               const __grid_constant__ FwdArgs a) {
   using C = FCfg<HC, T>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -610,6 +648,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
       mbar_init(&bars->s_full[b], 1);
       mbar_init(&bars->s_empty[b], 16);
     }
+    mbar_init(&bars->q_full, 16);
     mbar_init(&bars->drain, 1);
     bars->abort = 0;
     fence_mbar_init();
@@ -624,8 +663,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   grid_dep_launch();
   grid_dep_wait();
   const uint32_t tmem = bars->tmem;
-  const int64_t rows = a.head[0];
-  const Units un((rows + 127) / 128, (a.V + 255) / 256, gridDim.x);
+  const Units un((fwd_rows(a) + 127) / 128, (a.V + 255) / 256, gridDim.x, a.tiles);
   Units::Walk w(un, blockIdx.x);
 
   if (warp == 16) {
@@ -710,9 +748,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + wg * 64;
     float m = -3.0e38f, l = 0.f;
     int tgt = -1;
-    uint32_t n = 0;
+    uint32_t n = 0, finished = 0;
     for (; w.more(); w.next(), ++n) {
-      if (w.starts) tgt = __float_as_int(a.stat[stat_at(w.t * 128 + r) + kTgt]);
+      if (w.starts) tgt = fwd_target(a, (int64_t)w.t * 128 + r);
       const int b = n & 1;
       if (!mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 20)) break;
       tc_fence_after();
@@ -734,15 +772,16 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         }
         if (here) a.hit[w.t * 128 + r] = z * (c / kLog2e);
         if (w.starts) {
-          m = fmaxf(-3.0e38f, max64(v) * c);
+          m = -3.0e38f;
           l = 0.f;
         }
       }
       // l = sum exp2(c z - m).  m need not be the running maximum, only near it: it is the maximum of
-      // the row's first columns here, and moves up when a sum passes 2^40 (so nothing overflows,
+      // the row's first columns, and moves up when a sum passes 2^40 (so nothing overflows,
       // and what an early m made too large keeps all its bits).  This takes the maximum out of the
       // common path.
-      float sum = sum32(v, c, m) + sum32(v + 32, c, m);
+      float sum = INFINITY;
+      if (!w.starts) sum = sum32(v, c, m) + sum32(v + 32, c, m);
       if (!(sum <= 0x1p40f)) {
         const float mn = fmaxf(m, max64(v) * c);
         l *= ex2(m - mn);
@@ -751,12 +790,26 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
       }
       l += sum;
       if (w.ends) {
-        // the sum's reference is m itself, so that the join undoes exactly what was done here
-        if (un.whole(blockIdx.x, w.t))
-          a.full[wg * a.cap + w.t * 128 + r] = make_float2(m, l);
-        else
+        // the sum's reference is m itself, so that fwd_finish undoes exactly what was done here
+        const int64_t slot = (int64_t)w.t * 128 + r;
+        if (un.whole(blockIdx.x, w.t)) {
+          a.full[wg * a.cap + slot] = make_float2(m, l);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->q_full);
+          if (wg == 0) {
+            if (!mbar_wait(&bars->q_full, finished & 1, a.status, 707, abort, 32)) break;
+            float2 p[4];
+            for (int k = 0; k < 4; ++k) p[k] = a.full[k * a.cap + slot];
+            const float top = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x));
+            float sum = 0.f;
+            for (int k = 0; k < 4; ++k) sum += p[k].y * ex2(p[k].x - top);
+            fwd_finish(a, slot, tgt, top, sum);
+          }
+          ++finished;
+        } else {
           a.part[(((int64_t)blockIdx.x * 2 + un.slot(blockIdx.x, w.t)) * 4 + wg) * 128 + r] =
               make_float2(m, l);
+        }
       }
     }
   }
@@ -769,48 +822,47 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   }
 }
 
-// A labelled row's maxima and sums together, lse and loss.  `lanes` threads share a row: 32 where a row
-// may have parts in every CTA, 1 where it has few.
-__global__ void __launch_bounds__(256)
-    k_xent_join(int V, int64_t cap, int G, int lanes, const int* __restrict__ head,
-                const int32_t* __restrict__ row, const float* __restrict__ hit,
-                const float2* __restrict__ full, const float2* __restrict__ part,
-                float* __restrict__ loss, float* __restrict__ lse) {
+// Rows of the tiles that several CTAs have parts of.  Block c takes the tile that CTA c is the first to
+// begin inside of, a quarter of its rows a block; 2 threads share a row, 32 where it has parts of many
+// CTAs.
+__global__ void __launch_bounds__(256) k_xent_join(const __grid_constant__ FwdArgs a) {
   grid_dep_launch();
   grid_dep_wait();
-  const int64_t rows = head[0];
-  const Units un((rows + 127) / 128, (V + 255) / 256, G);
-  // a block's 256 / lanes rows lie in at most two tiles, a warp's in one
-  const int64_t s = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
-  const int sub = threadIdx.x % lanes, r = (int)(s % 128);
-  const int64_t t = s / 128;
-  float m = -3.0e38f, l = 0.f;
-  if (s < rows) {
-    const int c0 = un.owner(t * un.ct), c1 = un.owner(t * un.ct + un.ct - 1);
-    const int n = c0 == c1 ? 4 : 4 * (c1 - c0 + 1);
-    for (int i = sub; i < n; i += lanes) {
-      const int c = c0 + i / 4;
-      const float2 p = c0 == c1 ? full[i * cap + s]
-                                : part[(((int64_t)c * 2 +
-                                         (c == c0 ? un.slot(c, t) : 0)) * 4 + (i & 3)) * 128 + r];
+  const int64_t rows = fwd_rows(a);
+  const Units un((rows + 127) / 128, (a.V + 255) / 256, gridDim.x, a.tiles);
+  const int c = blockIdx.x;
+  if (c >= un.G || c == 0) return;
+  const int64_t begin = un.begin(c);
+  if (begin % un.ct == 0) return;
+  const int64_t t = begin / un.ct, first = t * un.ct, end = first + un.ct;
+  if (un.begin(c - 1) > first) return;  // an earlier CTA begins inside the tile too
+  const int last = un.last_before(end);
+  // CTA c - 1 has the first part (in its second place unless the tile is its first), the others begin
+  // with this tile
+  const float2* head = a.part + ((int64_t)(c - 1) * 2 + un.slot(c - 1, t)) * 512;
+  const float2* tail = a.part + (int64_t)c * 1024;
+  const int n = 4 * (last - c + 2), lanes = n > 16 ? 32 : 2;
+  for (int q = threadIdx.x / lanes; q < 32; q += 256 / lanes) {
+    const int r = blockIdx.y * 32 + q;
+    const int64_t s = t * 128 + r;
+    if (s >= rows) break;  // (a whole group of lanes)
+    float m = -3.0e38f, l = 0.f;
+    for (int i = threadIdx.x % lanes; i < n; i += lanes) {
+      const float2 p = i < 4 ? head[i * 128 + r] : tail[(int64_t)(i / 4 - 1) * 1024 + (i & 3) * 128 + r];
       const float mn = fmaxf(m, p.x);
       l = l * ex2(m - mn) + p.y * ex2(p.x - mn);
       m = mn;
     }
-  }
-  float top = m;
-  for (int o = lanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  l *= ex2(m - top);
-  for (int o = lanes / 2; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  if (sub == 0 && s < rows) {
-    // (top + log2 l) / c with c = kLog2e as it was rounded: c' = 1 / c in two parts, so that the only
-    // error that counts is the result's own rounding
-    constexpr float inv = (float)(1.0 / (double)kLog2e), rest = (float)(1.0 / (double)kLog2e - (double)inv);
-    const float lg = log2f(l), hi = top * inv;
-    const float lo = fmaf(top, inv, -hi) + fmaf(top, rest, lg * inv);
-    const float v = hi + lo;
-    lse[row[s]] = v;
-    loss[row[s]] = (hi - hit[s]) + lo;
+    const unsigned group = lanes == 32 ? 0xffffffffu : 3u << (threadIdx.x & 30);
+    float top = m;
+    for (int o = lanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(group, top, o));
+    l *= ex2(m - top);
+    for (int o = lanes / 2; o; o >>= 1) l += __shfl_xor_sync(group, l, o);
+    if (threadIdx.x % lanes == 0) {
+      const int64_t i = a.direct ? s : 0;
+      const int tgt = a.direct ? (a.target[i] < a.V ? a.target[i] : -1) : 0;
+      fwd_finish(a, s, tgt, top, l);
+    }
   }
 }
 
@@ -818,6 +870,7 @@ __global__ void __launch_bounds__(256)
 struct BwdArgs {
   int H, V, accumulate, out_bf16;
   int split;  // CTAs that compute dX; the others compute dW
+  int tiles;  // runs of whole tiles
   int step;   // of the order of dW's tiles
   int64_t cap, vcap;
   const int* head;
@@ -1204,7 +1257,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   const int cta = blockIdx.x - (dw ? a.split : 0);
   const Units un(dw ? (a.V + 127) / 128 : (rows + 127) / 128,
                  dw ? (rows + C::NB - 1) / C::NB : (a.V + C::NB - 1) / C::NB,
-                 dw ? gridDim.x - a.split : a.split, dw ? a.step : 1);
+                 dw ? gridDim.x - a.split : a.split, a.tiles, dw ? a.step : 1);
 
   if (warp == 16) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -1344,6 +1397,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    if (dw && un.ct == 0 && !a.accumulate) {  // no labelled rows
+      const int64_t n16 = (int64_t)a.V * a.H / (a.out_bf16 ? 8 : 4), ctas = gridDim.x - a.split;
+      for (int64_t i = (int64_t)cta * 512 + threadIdx.x; i < n16; i += ctas * 512)
+        static_cast<uint4*>(a.dW)[i] = make_uint4(0, 0, 0, 0);
+    }
     if (dw)
       bwd_epilogue<HC, FORM, true>(a, un, cta, tmem, stats, bars);
     else
@@ -1359,8 +1417,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 }
 
 // Tiles that several CTAs have parts of: the sum of the parts in the order of the CTAs.  Block row c
-// takes the tile that CTA c is the first to begin inside of, 32 rows x 32 columns a block; without
-// labelled rows the tiles of dW are written as zeros here.
+// takes the tile that CTA c is the first to begin inside of, 32 rows x 32 columns a block.
 __global__ void __launch_bounds__(256)
     k_xent_bwd_join(BwdArgs a, int form, int nb) {
   grid_dep_launch();
@@ -1369,24 +1426,14 @@ __global__ void __launch_bounds__(256)
   const bool dw = (int)blockIdx.x >= a.split;
   const int c = blockIdx.x - (dw ? a.split : 0), ctas = dw ? gridDim.x - a.split : a.split;
   const Units un(dw ? (a.V + 127) / 128 : (rows + 127) / 128,
-                 dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, ctas, dw ? a.step : 1);
+                 dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, ctas, a.tiles, dw ? a.step : 1);
   void* out = dw ? a.dW : a.dX;
   const int hb = a.H / 32;
   const int col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x & 7) * 4;
   const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x >> 3);
-  if (un.ct == 0) {
-    if (!dw || a.accumulate) return;
-    for (int64_t v = (int64_t)c * 128 + r; v < a.V; v += (int64_t)ctas * 128) {
-      if (a.out_bf16)
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + v * a.H + col) = make_uint2(0, 0);
-      else
-        *reinterpret_cast<float4*>(static_cast<float*>(out) + v * a.H + col) =
-            make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    return;
-  }
+  if (c >= un.G || c == 0) return;
   const int64_t begin = un.begin(c);
-  if (c >= un.G || c == 0 || begin % un.ct == 0) return;
+  if (begin % un.ct == 0) return;
   const int64_t t = begin / un.ct, first = t * un.ct, end = first + un.ct;
   if (un.begin(c - 1) > first) return;  // an earlier CTA begins inside the tile too
   int64_t orow = (int64_t)un.tile((int)t) * 128 + r;
@@ -1396,8 +1443,7 @@ __global__ void __launch_bounds__(256)
   const float* part = a.part + ((int64_t)(blockIdx.x - c) * 2 * 128 + r) * a.H + col;
   const int64_t stride = 128LL * a.H;
   float4 x = *reinterpret_cast<const float4*>(part + ((int64_t)(c - 1) * 2 + un.slot(c - 1, t)) * stride);
-  int last = c;
-  while (last + 1 < un.G && un.begin(last + 1) < end) ++last;
+  const int last = un.last_before(end);
 #pragma unroll 8
   for (int k = c; k <= last; ++k) {
     const float4 p = *reinterpret_cast<const float4*>(part + (int64_t)k * 2 * stride);
@@ -1502,10 +1548,12 @@ cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
 }
 
 template <int HC, int T>
-cudaError_t run_fwd(const Call& c, const void* W, const FwdArgs& f) {
+cudaError_t run_fwd(const Call& c, const XentArgs& x, const FwdArgs& f) {
   using C = FCfg<HC, T>;
   CUtensorMap mx, mw;
-  if (!map_x(c, &mx, 128) || !map_w(c, W, &mw, 256)) return cudaErrorInvalidValue;
+  if (!(f.direct ? make_map_ld(&mx, x.X, c.n, c.H, c.H, 128) : map_x(c, &mx, 128)) ||
+      !map_w(c, x.W, &mw, 256))
+    return cudaErrorInvalidValue;
   static std::atomic<uint64_t> done{0};
   cudaError_t e = allow_smem(k_xent_fwd<HC, T>, C::SMEM, done);
   if (e != cudaSuccess) return e;
@@ -1526,6 +1574,7 @@ cudaError_t run_bwd(const Call& c, const void* W, const BwdArgs& b) {
                  b);
   if (e != cudaSuccess) return e;
   note_launch();
+  if (b.tiles) return cudaSuccess;
   e = launch_pdl(k_xent_bwd_join, dim3(c.sms, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM, C::NB);
   if (e != cudaSuccess) return e;
   note_launch();
@@ -1566,30 +1615,49 @@ size_t xent_ws_bytes(int bf16, int64_t n, int H, int V, int backward) {
 cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st) {
   if (a.n == 0) return cudaSuccess;
   Call c = make_call(a, a.bf16 ? kBf16 : kF16x2, 0, st);
-  RowArgs r{};
-  r.loss = loss;
-  r.lse_out = lse;
-  cudaError_t e = prepare(a, c, r);
-  if (e != cudaSuccess) return e;
-  const FwdArgs f{a.H, a.V, c.w.cap, c.w.vcap, c.at<int>(c.w.head), c.at<float>(c.w.stat),
-                  c.at<float>(c.w.hit), c.at<float2>(c.w.full), c.at<float2>(c.w.part), a.status};
+  FwdArgs f{};
+  f.H = a.H;
+  f.V = a.V;
+  f.n = a.n;
+  f.cap = c.w.cap;
+  f.vcap = c.w.vcap;
+  f.head = c.at<int>(c.w.head);
+  f.target = a.target;
+  f.row = c.at<int32_t>(c.w.row);
+  f.stat = c.at<float>(c.w.stat);
+  f.hit = c.at<float>(c.w.hit);
+  f.full = c.at<float2>(c.w.full);
+  f.part = c.at<float2>(c.w.part);
+  f.loss = loss;
+  f.lse = lse;
+  f.status = a.status;
+  // A row's logits depend on no other row, so bf16 rows need no gathering to be right; up to two units
+  // a CTA it would only take longer (one row against 32000 x 128: 17 us with it, 13 without).
+  const int64_t ct = ((int64_t)a.V + 255) / 256, units = c.w.cap / 128 * ct;
+  f.direct = a.bf16 && units <= 2 * c.sms;
+  f.tiles = ct <= kWholeUnits;
+  cudaError_t e;
+  if (!f.direct) {
+    RowArgs r{};
+    r.loss = loss;
+    r.lse_out = lse;
+    e = prepare(a, c, r);
+    if (e != cudaSuccess) return e;
+  }
   switch ((a.H + 63) / 64 * 2 + (a.bf16 ? 0 : 1)) {
-    case 2: e = run_fwd<1, 1>(c, a.W, f); break;
-    case 3: e = run_fwd<1, 2>(c, a.W, f); break;
-    case 4: e = run_fwd<2, 1>(c, a.W, f); break;
-    case 5: e = run_fwd<2, 2>(c, a.W, f); break;
-    case 6: e = run_fwd<3, 1>(c, a.W, f); break;
-    case 7: e = run_fwd<3, 2>(c, a.W, f); break;
-    case 8: e = run_fwd<4, 1>(c, a.W, f); break;
-    default: e = run_fwd<4, 2>(c, a.W, f); break;
+    case 2: e = run_fwd<1, 1>(c, a, f); break;
+    case 3: e = run_fwd<1, 2>(c, a, f); break;
+    case 4: e = run_fwd<2, 1>(c, a, f); break;
+    case 5: e = run_fwd<2, 2>(c, a, f); break;
+    case 6: e = run_fwd<3, 1>(c, a, f); break;
+    case 7: e = run_fwd<3, 2>(c, a, f); break;
+    case 8: e = run_fwd<4, 1>(c, a, f); break;
+    default: e = run_fwd<4, 2>(c, a, f); break;
   }
   if (e != cudaSuccess) return e;
   note_launch();
-  // row tiles x CTAs a tile <= SMs + row tiles: with 8 tiles or more a row has at most 20 parts or so
-  const int lanes = c.w.cap / 128 < 8 ? 32 : 1;
-  const int64_t grid = (a.n * lanes + 255) / 256;
-  e = launch_pdl(k_xent_join, dim3((unsigned)grid), dim3(256), 0, st, a.V, c.w.cap, c.sms, lanes, f.head,
-                 c.at<int32_t>(c.w.row), f.hit, f.full, f.part, loss, lse);
+  if (f.tiles) return cudaSuccess;
+  e = launch_pdl(k_xent_join, dim3(c.sms, 4), dim3(256), 0, st, f);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
@@ -1624,6 +1692,7 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
   b.out_bf16 = grad_bf16;
   // a unit of dW takes 2-20% longer (column statistics, frequent tokens): 72 of 152 CTAs for dX
   b.split = !dW ? c.sms : !dX ? 0 : c.sms * 9 / 19;
+  b.tiles = (!dX || a.V <= kWholeUnits * 128) && (!dW || a.n <= kWholeUnits * 128);
   const int tiles = (int)(c.w.vcap / 128);
   b.step = std::max(1, (int)(tiles * 0.618));
   while (std::gcd(b.step, tiles) != 1) ++b.step;
