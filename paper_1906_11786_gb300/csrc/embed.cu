@@ -44,6 +44,17 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* v) {
   for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
   *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
 }
+// Past the caches' reach: the line is not kept in L2.
+__device__ __forceinline__ void store8_stream(float* p, const float* v) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+  __stcs(reinterpret_cast<float4*>(p + 4), make_float4(v[4], v[5], v[6], v[7]));
+}
+__device__ __forceinline__ void store8_stream(__nv_bfloat16* p, const float* v) {
+  __nv_bfloat162 h[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+  __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(h));
+}
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
@@ -54,33 +65,45 @@ __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float
 // and y may be the same array: a thread reads its elements before it writes them.
 template <typename T>
 __global__ void __launch_bounds__(256)
-    k_dropout(int64_t n, Drop d, const T* x, const T* res, T* y) {
-  const int64_t full = n / 8, blocks = (n + 7) / 8;
-  for (int64_t b = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; b < blocks;
-       b += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t i = b * 8;
-    float v[8], r[8];
-    if (b < full) {
-      load8(x + i, v);
-      if (res) load8(res + i, r);
-      if (d.thr) drop8(d, (uint64_t)b, v);
+    k_dropout(int64_t n, Drop d, const T* x, const T* res, T* y, int stream) {
+  const int64_t full = n / 8, step = (int64_t)gridDim.x * blockDim.x;
+  int64_t b = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
+  // 32 bytes of each array in flight a thread: at 64, or with more or fewer than 8 blocks an SM, both
+  // types took up to 15% longer
+  constexpr int kDropUnroll = 4 / (int)sizeof(T);
+  for (; b + (kDropUnroll - 1) * step < full; b += kDropUnroll * step) {
+    float v[kDropUnroll][8], r[kDropUnroll][8];
+#pragma unroll
+    for (int u = 0; u < kDropUnroll; ++u) {
+      load8(x + (b + u * step) * 8, v[u]);
+      if (res) load8(res + (b + u * step) * 8, r[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kDropUnroll; ++u) {
+      if (d.thr) drop8(d, (uint64_t)(b + u * step), d.scale, v[u]);
       if (res) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += r[j];
+        for (int j = 0; j < 8; ++j) v[u][j] += r[u][j];
       }
-      store8(y + i, v);
-    } else {
-      const int m = (int)(n - i);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] = j < m ? load1(x + i + j) : 0.f;
-        r[j] = j < m && res ? load1(res + i + j) : 0.f;
-      }
-      if (d.thr) drop8(d, (uint64_t)b, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < m) store1(y + i + j, res ? v[j] + r[j] : v[j]);
+      if (stream)
+        store8_stream(y + (b + u * step) * 8, v[u]);
+      else
+        store8(y + (b + u * step) * 8, v[u]);
     }
+  }
+  for (; b * 8 < n; b += step) {
+    const int64_t i = b * 8;
+    const int m = (int)min((int64_t)8, n - i);
+    float v[8], r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[j] = j < m ? load1(x + i + j) : 0.f;
+      r[j] = j < m && res ? load1(res + i + j) : 0.f;
+    }
+    if (d.thr) drop8(d, (uint64_t)b, d.scale, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < m) store1(y + i + j, res ? v[j] + r[j] : v[j]);
   }
 }
 
@@ -90,14 +113,20 @@ cudaError_t run_dropout(int64_t n, const Drop& d, const void* x, const void* res
   if (n == 0) return cudaSuccess;
   const int64_t blocks = (n + 7) / 8;
   const int grid = (int)std::min<int64_t>((blocks + 255) / 256, 152 * 8);
+  // a result that cannot stay in L2 (129 MB) beside the operands is not kept there: 37.0 -> 34.8 us at
+  // 3 x 67 MB; a smaller one is its reader's
+  const int stream = n * (int64_t)sizeof(T) * (res ? 3 : 2) > ((int64_t)128 << 20);
   k_dropout<T><<<grid, 256, 0, st>>>(n, d, static_cast<const T*>(x), static_cast<const T*>(res),
-                                     static_cast<T*>(y));
+                                     static_cast<T*>(y), stream);
   note_launch();
   return cudaGetLastError();
 }
 
 // ------------------------------------------------------------------------------ embedding lookup
-// A row is H / 8 threads; a block takes 256 / (H / 8) rows at a time.
+// A row is H / 8 threads; a thread takes the same place of kEmbedUnroll rows, whose ids, and then whose
+// table rows, are in flight together.
+constexpr int kEmbedUnroll = 2;
+
 template <typename T>
 __global__ void __launch_bounds__(256)
     k_embed_fwd(int64_t n, int H, int V, const int32_t* __restrict__ ids,
@@ -105,28 +134,41 @@ __global__ void __launch_bounds__(256)
   const int lanes = H / 8, rows = 256 / lanes;
   const int r = threadIdx.x / lanes, c = threadIdx.x % lanes;
   if (r >= rows) return;
-  for (int64_t i = (int64_t)blockIdx.x * rows + r; i < n; i += (int64_t)gridDim.x * rows) {
-    const int id = ids[i];
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (id >= V) {
-      if (c == 0 && atomicCAS(status, 0, 2) == 0) atomicExch(status + 1, kSiteEmbedId);
-    } else if (id >= 0) {
-      load8(table + (int64_t)id * H + c * 8, v);
+  const int64_t i0 = (int64_t)blockIdx.x * rows * kEmbedUnroll + r;
+  int id[kEmbedUnroll];
+  float v[kEmbedUnroll][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= scale;
-      if (d.thr) drop8(d, (uint64_t)i * lanes + c, v);
+  for (int u = 0; u < kEmbedUnroll; ++u) id[u] = i0 + u * rows < n ? ids[i0 + u * rows] : -1;
+#pragma unroll
+  for (int u = 0; u < kEmbedUnroll; ++u) {
+    if (id[u] >= 0 && id[u] < V) {
+      load8(table + (int64_t)id[u] * H + c * 8, v[u]);
+    } else {
+      if (id[u] >= V && c == 0 && atomicCAS(status, 0, 2) == 0) atomicExch(status + 1, kSiteEmbedId);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[u][j] = 0.f;
     }
-    store8(out + i * H + c * 8, v);
+  }
+#pragma unroll
+  for (int u = 0; u < kEmbedUnroll; ++u) {
+    const int64_t i = i0 + u * rows;
+    if (i >= n) break;
+    if (d.thr) {
+      drop8(d, (uint64_t)i * lanes + c, scale * d.scale, v[u]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[u][j] *= scale;
+    }
+    store8(out + i * H + c * 8, v[u]);
   }
 }
 
 // ------------------------------------------------------------------------------ embedding gradient
 // The rows of dout are summed by token in three steps that give the same bits every time: a stable
-// radix sort of (id, position), sums over pieces of kPiece sorted positions, and a join of the
+// radix sort of (id, position), sums over pieces of sorted positions, and a join of the
 // tokens that span pieces, in the order of the pieces.  An id that names no row sorts as V, after
 // all others, and is not summed.
 constexpr int kTile = 2048;  // keys a sorting block ranks at a time: 8 warps x 8 x 32
-constexpr int kPiece = 32;
 
 struct SortPlan {
   int passes, bits;  // digits of `bits` bits
@@ -140,17 +182,28 @@ SortPlan sort_plan(int64_t n, int V) {
   int bits = 1;
   while (((int64_t)1 << bits) <= V) ++bits;  // keys 0 .. V
   s.passes = (bits + 8) / 9;
-  s.bits = (bits + s.passes - 1) / s.passes;
+  s.bits = std::max(2, (bits + s.passes - 1) / s.passes);
   s.D = 1 << s.bits;
   s.T = kTile * std::max<int64_t>(1, (n + (int64_t)kTile * 152 - 1) / ((int64_t)kTile * 152));
   s.nb = (int)std::max<int64_t>(1, (n + s.T - 1) / s.T);
   return s;
 }
 
+// Sorted positions of a piece: at most kMaxPiece, and such that the pieces fill the SMs (two blocks of 256
+// threads each, H / 8 threads a piece) a whole number of times.
+constexpr int kMaxPiece = 64;
+constexpr int kMaxRun = 64 * kMaxPiece;  // sorted positions of a block of k_embed_sum (H = 32)
+int piece_size(int64_t n, int H) {
+  const int64_t slots = 152 * 2 * (256 / (H / 8));
+  const int64_t waves = (n + slots * kMaxPiece - 1) / (slots * kMaxPiece);
+  const int64_t piece = (n + slots * waves - 1) / (slots * waves);
+  return (int)std::min<int64_t>(kMaxPiece, (piece + 3) / 4 * 4);
+}
+
 inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct BwdWs {
-  size_t key[2], pos[2], hist, seen, head, tail, total;
+  size_t key[2], pos[2], hist, head, tail, total;
 };
 BwdWs bwd_ws(int64_t n, int H, int V) {
   const SortPlan s = sort_plan(n, V);
@@ -161,13 +214,13 @@ BwdWs bwd_ws(int64_t n, int H, int V) {
     o += al(bytes);
     return at;
   };
-  const size_t pieces = (size_t)((n + kPiece - 1) / kPiece);
+  const int piece = piece_size(n, H);
+  const size_t pieces = (size_t)((n + piece - 1) / piece);
   for (int i = 0; i < 2; ++i) {
     w.key[i] = take((size_t)n * 4);
     w.pos[i] = take((size_t)n * 4);
   }
   w.hist = take((size_t)s.passes * s.nb * s.D * 4);
-  w.seen = take((size_t)V);
   w.head = take(pieces * H * 4);
   w.tail = take(pieces * H * 4);
   w.total = std::max<size_t>(o, 256);
@@ -176,11 +229,10 @@ BwdWs bwd_ws(int64_t n, int H, int V) {
 
 __device__ __forceinline__ int sort_key(int id, int V) { return id < 0 || id >= V ? V : id; }
 
-// Digit counts of each block's keys for the first pass; clears the counts of the later passes and
-// the marks of the tokens that occur.
+// Digit counts of each block's keys for the first pass; clears the counts of the later passes.
 __global__ void __launch_bounds__(256)
     k_sort_count(int64_t n, int V, SortPlan s, const int32_t* __restrict__ ids,
-                 int* __restrict__ hist, uint8_t* __restrict__ seen, int* status) {
+                 int* __restrict__ hist, int* status) {
   __shared__ int cnt[512];
   grid_dep_launch();
   for (int i = threadIdx.x; i < s.D; i += 256) cnt[i] = 0;
@@ -188,7 +240,6 @@ __global__ void __launch_bounds__(256)
   const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   const int64_t per = (int64_t)s.nb * s.D;
   for (int64_t i = per + first; i < per * s.passes; i += step) hist[i] = 0;
-  for (int64_t i = first; i < V; i += step) seen[i] = 0;
   __syncthreads();
   const int64_t end = min(n, (blockIdx.x + 1) * s.T);
   for (int64_t i = blockIdx.x * s.T + threadIdx.x; i < end; i += 256) {
@@ -200,13 +251,46 @@ __global__ void __launch_bounds__(256)
   for (int i = threadIdx.x; i < s.D; i += 256) hist[(int64_t)blockIdx.x * s.D + i] = cnt[i];
 }
 
+// Stable ranks of the 256 keys of a warp (its rows of 32, in order) among its keys of equal digit; cnt
+// [512], zero before, gets the digits' counts.  A negative key takes no part.
+__device__ __forceinline__ void warp_ranks(const int* key, int shift, int D, int* cnt, int* rank) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int dig = key[k] < 0 ? -1 : (key[k] >> shift) & (D - 1);
+    const unsigned peers = __match_any_sync(0xffffffffu, dig);
+    const int lower = __popc(peers & ((1u << lane) - 1));
+    const int old = dig < 0 ? 0 : cnt[dig];
+    __syncwarp();
+    if (dig >= 0 && lower == 0) cnt[dig] = old + __popc(peers);
+    __syncwarp();
+    rank[k] = old + lower;
+  }
+}
+
+// Exclusive prefix sum over the block (256 threads) of v, sums [8] in shared memory.
+__device__ __forceinline__ int block_prefix(int v, int* sums) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int run = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += up;
+  }
+  if (lane == 31) sums[warp] = run;
+  __syncthreads();
+  int base = run - v;
+  for (int w = 0; w < warp; ++w) base += sums[w];
+  return base;
+}
+
 // One stable counting pass.  A key's place is: the keys of smaller digits, the same digit's keys of
 // earlier blocks, of earlier tiles, of earlier warps, of earlier rows of its warp, and of lower lanes.
 __global__ void __launch_bounds__(256)
     k_sort_pass(int64_t n, int V, SortPlan s, int pass, const int32_t* __restrict__ ids,
                 const int32_t* __restrict__ key_in, const int32_t* __restrict__ pos_in,
                 int32_t* __restrict__ key_out, int32_t* __restrict__ pos_out,
-                int* __restrict__ hist, uint8_t* __restrict__ seen) {
+                int* __restrict__ hist) {
   __shared__ int off[512];     // next place of each digit
   __shared__ int cnt[8][512];  // per warp: counts, then first places
   __shared__ int sums[8];
@@ -215,51 +299,37 @@ __global__ void __launch_bounds__(256)
   grid_dep_wait();
   const int shift = pass * s.bits, D = s.D;
   const int* mine = hist + (int64_t)pass * s.nb * D;
-  // two neighbouring digits a thread: D <= 512
+  // two neighbouring digits a thread: 4 <= D <= 512
   int before[2] = {0, 0}, total[2] = {0, 0};
-  for (int j = 0; j < 2; ++j) {
-    const int d = 2 * tid + j;
-    if (d < D)
-      for (int b = 0; b < s.nb; ++b) {
-        const int h = mine[(int64_t)b * D + d];
-        total[j] += h;
-        if (b < (int)blockIdx.x) before[j] += h;
+  if (2 * tid < D) {
+#pragma unroll 16
+    for (int b = 0; b < s.nb; ++b) {
+      const int2 h = *reinterpret_cast<const int2*>(mine + (int64_t)b * D + 2 * tid);
+      total[0] += h.x;
+      total[1] += h.y;
+      if (b < (int)blockIdx.x) {
+        before[0] += h.x;
+        before[1] += h.y;
       }
+    }
   }
-  int run = total[0] + total[1];
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int up = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += up;
+  const int base = block_prefix(total[0] + total[1], sums);
+  if (2 * tid < D) {
+    off[2 * tid] = base + before[0];
+    off[2 * tid + 1] = base + total[0] + before[1];
   }
-  if (lane == 31) sums[warp] = run;
-  __syncthreads();
-  int base = run - total[0] - total[1];
-  for (int w = 0; w < warp; ++w) base += sums[w];
-  if (2 * tid < D) off[2 * tid] = base + before[0];
-  if (2 * tid + 1 < D) off[2 * tid + 1] = base + total[0] + before[1];
   const int64_t begin = blockIdx.x * s.T, end = min(n, begin + s.T);
   int* next = pass + 1 < s.passes ? hist + (int64_t)(pass + 1) * s.nb * D : nullptr;
   for (int64_t t0 = begin; t0 < end; t0 += kTile) {
     for (int i = tid; i < 8 * 512; i += 256) (&cnt[0][0])[i] = 0;
     __syncthreads();
-    int key[8], rank[8];
+    int key[8], rank[8], place[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int64_t i = t0 + warp * 256 + k * 32 + lane;
       key[k] = i < end ? (pass == 0 ? sort_key(ids[i], V) : key_in[i]) : -1;
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int dig = key[k] < 0 ? -1 : (key[k] >> shift) & (D - 1);
-      const unsigned peers = __match_any_sync(0xffffffffu, dig);
-      const int lower = __popc(peers & ((1u << lane) - 1));
-      const int old = dig < 0 ? 0 : cnt[warp][dig];
-      __syncwarp();
-      if (dig >= 0 && lower == 0) cnt[warp][dig] = old + __popc(peers);
-      __syncwarp();
-      rank[k] = old + lower;
-    }
+    warp_ranks(key, shift, D, cnt[warp], rank);
     __syncthreads();
     for (int dg = tid; dg < D; dg += 256) {
       int at = off[dg];
@@ -278,147 +348,290 @@ __global__ void __launch_bounds__(256)
       const int at = cnt[warp][(key[k] >> shift) & (D - 1)] + rank[k];
       key_out[at] = key[k];
       pos_out[at] = pass == 0 ? (int32_t)i : pos_in[i];
-      if (next) atomicAdd(&next[(int64_t)(at / s.T) * D + ((key[k] >> (shift + s.bits)) & (D - 1))], 1);
-      if (pass == 0 && key[k] < V) seen[key[k]] = 1;
+      place[k] = at;
+    }
+    if (next) {
+      // counts for the next pass, one atomic for the keys of a warp row that go to the same one
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int to = key[k] < 0 ? -1
+                                  : (int)((uint32_t)place[k] / (uint32_t)s.T) * D +
+                                        ((key[k] >> (shift + s.bits)) & (D - 1));
+        const unsigned peers = __match_any_sync(0xffffffffu, to);
+        if (to >= 0 && (peers & ((1u << lane) - 1)) == 0) atomicAdd(&next[to], __popc(peers));
+      }
     }
     __syncthreads();
   }
 }
 
-// Sums of the rows of each piece of kPiece sorted positions, one group of H / 8 threads a piece.
-// A token that lies within the piece is finished here; the part of one that began in an earlier
-// piece goes to head[piece], of one that begins here and goes on to tail[piece].  The blocks from
-// `sum_blocks` on write the zero rows of the tokens that do not occur.
+// All of it for at most kTile ids, in one block.
 __global__ void __launch_bounds__(256)
-    k_embed_sum(int64_t n, int H, int V, const int32_t* __restrict__ key,
+    k_sort_small(int n, int V, SortPlan s, const int32_t* __restrict__ ids,
+                 int32_t* __restrict__ key_out, int32_t* __restrict__ pos_out,
+                 int* status) {
+  __shared__ int cnt[8][512];
+  __shared__ int sums[8];
+  __shared__ int keys[kTile], poss[kTile];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  grid_dep_launch();
+  grid_dep_wait();
+  int key[8], pos[8], rank[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int i = warp * 256 + k * 32 + lane;
+    pos[k] = i;
+    key[k] = -1;
+    if (i < n) {
+      const int id = ids[i];
+      if (id >= V && atomicCAS(status, 0, 2) == 0) atomicExch(status + 1, kSiteEmbedId);
+      key[k] = sort_key(id, V);
+    }
+  }
+  for (int p = 0; p < s.passes; ++p) {
+    const int shift = p * s.bits;
+    for (int i = tid; i < 8 * 512; i += 256) (&cnt[0][0])[i] = 0;
+    __syncthreads();
+    warp_ranks(key, shift, s.D, cnt[warp], rank);
+    __syncthreads();
+    int total[2] = {0, 0};
+    if (2 * tid < s.D)
+      for (int w = 0; w < 8; ++w) {
+        total[0] += cnt[w][2 * tid];
+        total[1] += cnt[w][2 * tid + 1];
+      }
+    int at = block_prefix(total[0] + total[1], sums);
+    if (2 * tid < s.D)
+      for (int j = 0; j < 2; ++j)
+        for (int w = 0; w < 8; ++w) {
+          const int c = cnt[w][2 * tid + j];
+          cnt[w][2 * tid + j] = at;
+          at += c;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (key[k] >= 0) {
+        const int to = cnt[warp][(key[k] >> shift) & (s.D - 1)] + rank[k];
+        keys[to] = key[k];
+        poss[to] = pos[k];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = warp * 256 + k * 32 + lane;
+      if (i < n) {
+        key[k] = keys[i];
+        pos[k] = poss[i];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int i = warp * 256 + k * 32 + lane;
+    if (i >= n) continue;
+    key_out[i] = key[k];
+    pos_out[i] = pos[k];
+  }
+}
+
+// One piece: m keys k0 (k0[-1] and k0[m] are its neighbours') and their rows of dout, columns 8 c ..
+__device__ __forceinline__ void sum_piece(int H, int V, int m, int c, int64_t q, const int* k0,
+                                          const int* rows, const float* __restrict__ dout, float scale,
+                                          const Drop& d, float* __restrict__ dtable, int accumulate,
+                                          float* __restrict__ head, float* __restrict__ tail) {
+  int cur = k0[0];
+  bool begun = k0[-1] == cur;  // the first token began in an earlier piece
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  auto finish = [&](bool goes_on) {
+    if (cur >= V) return;
+    const float f = d.thr ? scale * d.scale : scale;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] *= f;
+    if (begun || goes_on) {
+      store8((begun ? head : tail) + q * H + c * 8, acc);
+    } else {
+      float* row = dtable + (int64_t)cur * H + c * 8;
+      if (accumulate) {
+        float old[8];
+        load8(row, old);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += old[j];
+      }
+      store8(row, acc);
+    }
+  };
+  // four rows being added, four on their way
+  float v[2][4][8];
+  auto fetch = [&](int i0, float (*to)[8]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u < m && k0[i0 + u] < V) load8(dout + (int64_t)rows[i0 + u] * H + c * 8, to[u]);
+  };
+  auto add = [&](int i0, float (*from)[8]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i0 + u >= m) break;
+      const int k = k0[i0 + u];
+      if (k != cur) {
+        finish(false);
+        begun = false;
+        cur = k;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+      }
+      if (k < V) {
+        if (d.thr) drop8(d, (uint64_t)rows[i0 + u] * (H / 8) + c, 1.f, from[u]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += from[u][j];
+      }
+    }
+  };
+  fetch(0, v[0]);
+  for (int i0 = 0; i0 < m; i0 += 8) {
+    fetch(i0 + 4, v[1]);
+    add(i0, v[0]);
+    fetch(i0 + 8, v[0]);
+    add(i0 + 4, v[1]);
+  }
+  finish(k0[m] == cur);
+}
+
+// Sums of the rows of each piece of sorted positions, one group of H / 8 threads a piece.  A token that
+// lies within the piece is finished here; the part of one that began in an earlier piece goes to
+// head[piece], of one that begins here and goes on to tail[piece].  Every block also writes the zero
+// rows of its share of the table, the tokens that do not occur.
+__global__ void __launch_bounds__(256)
+    k_embed_sum(int64_t n, int H, int V, int piece, const int32_t* __restrict__ key,
                 const int32_t* __restrict__ pos, const float* __restrict__ dout, float scale,
                 Drop d, float* __restrict__ dtable, int accumulate, float* __restrict__ head,
-                float* __restrict__ tail, const uint8_t* __restrict__ seen, int sum_blocks) {
+                float* __restrict__ tail) {
+  // the block's pieces lie side by side: their keys and rows come in one go, so that the loads of dout
+  // wait for nothing but each other's registers
+  __shared__ int keys[kMaxRun + 2], rows[kMaxRun];
+  __shared__ uint8_t occurs[256];
   const int lanes = H / 8, groups = 256 / lanes;
   const int g = threadIdx.x / lanes, c = threadIdx.x % lanes;
   grid_dep_launch();
   grid_dep_wait();
-  if (g >= groups) return;
-  if ((int)blockIdx.x >= sum_blocks) {
-    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int64_t v = (int64_t)(blockIdx.x - sum_blocks) * groups + g; v < V;
-         v += (int64_t)(gridDim.x - sum_blocks) * groups)
-      if (!seen[v]) store8(dtable + v * H + c * 8, zero);
-    return;
-  }
-  const int64_t pieces = (n + kPiece - 1) / kPiece;
-  for (int64_t q = (int64_t)blockIdx.x * groups + g; q < pieces; q += (int64_t)sum_blocks * groups) {
-    const int64_t e0 = q * kPiece;
-    const int m = (int)min((int64_t)kPiece, n - e0);
-    int cur = key[e0];
-    bool begun = e0 > 0 && key[e0 - 1] == cur;  // the first token began in an earlier piece
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    auto finish = [&](bool goes_on) {
-      if (cur >= V) return;
-      const float f = d.thr ? scale * d.scale : scale;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] *= f;
-      if (begun || goes_on) {
-        store8((begun ? head : tail) + q * H + c * 8, acc);
-      } else {
-        float* row = dtable + (int64_t)cur * H + c * 8;
-        if (accumulate) {
-          float old[8];
-          load8(row, old);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] += old[j];
-        }
-        store8(row, acc);
-      }
-    };
-    for (int i0 = 0; i0 < m; i0 += 4) {
-      float v[4][8];
-      int k[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        k[u] = i0 + u < m ? key[e0 + i0 + u] : V;
-        if (k[u] < V) {
-          const int64_t i = pos[e0 + i0 + u];
-          load8(dout + i * H + c * 8, v[u]);
-          if (d.thr) {
-            const uint4 w = philox_block(d, (uint64_t)i * lanes + c);
-            const uint32_t b[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (((b[j / 2] >> (16 * (j & 1))) & 0xFFFFu) < d.thr) v[u][j] = 0.f;
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (i0 + u >= m) break;
-        if (k[u] != cur) {
-          finish(false);
-          begun = false;
-          cur = k[u];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-        }
-        if (cur < V) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] += v[u][j];
-        }
-      }
+  const int64_t first = (int64_t)blockIdx.x * groups * piece;
+  const int run = (int)max((int64_t)0, min((int64_t)groups * piece, n - first));
+  if (run > 0)
+    for (int i = threadIdx.x; i < run + 2; i += 256) {
+      const int64_t e = first + i - 1;
+      keys[i] = e >= 0 && e < n ? key[e] : -1;  // one more on either side
+      if (i < run) rows[i] = pos[first + i];
     }
-    finish(e0 + m < n && key[e0 + m] == cur);
+  __syncthreads();
+  if (g < groups && g * piece < run)
+    sum_piece(H, V, min(piece, run - g * piece), c, first / piece + g, keys + 1 + g * piece,
+              rows + g * piece, dout, scale, d, dtable, accumulate, head, tail);
+  if (accumulate) return;
+  const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int v_end = (int)((int64_t)V * (blockIdx.x + 1) / gridDim.x);
+  for (int v0 = (int)((int64_t)V * blockIdx.x / gridDim.x); v0 < v_end; v0 += 256) {
+    const int mine = v0 + threadIdx.x;
+    if (mine < v_end) {  // looked up among the sorted keys: the first of `mine` or more
+      int lo = 0, hi = (int)n;
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (key[mid] < mine) lo = mid + 1; else hi = mid;
+      }
+      occurs[threadIdx.x] = lo < n && key[lo] == mine;
+    }
+    __syncthreads();
+    if (g < groups)
+      for (int k = g; k < 256 && v0 + k < v_end; k += groups)
+        if (!occurs[k]) store8(dtable + (int64_t)(v0 + k) * H + c * 8, zero);
+    __syncthreads();
   }
 }
 
-// One block a piece in which a token begins that goes on: its sum is tail[piece] + head[piece + 1] +
-// ... in that order of quarters; each group of threads takes one run of the pieces.
+__device__ __forceinline__ void join_write(float* acc, float* row, int accumulate) {
+  if (accumulate) {
+    float old[8];
+    load8(row, old);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] += old[j];
+  }
+  store8(row, acc);
+}
+
+// Tokens that begin in piece q and go on: tail[q] + head[q + 1] + ... , in an order that depends on their
+// count alone.  A group of threads takes a piece; tokens of more than kJoinFew pieces more are left to
+// the whole block, whose groups take a run of the pieces each.
+constexpr int kJoinFew = 16;
 __global__ void __launch_bounds__(256)
-    k_embed_join(int64_t n, int H, int V, const int32_t* __restrict__ key,
+    k_embed_join(int64_t n, int H, int V, int piece, const int32_t* __restrict__ key,
                  float* __restrict__ dtable, int accumulate, const float* __restrict__ head,
                  const float* __restrict__ tail) {
   __shared__ float part[256 * 8];
+  __shared__ uint8_t many[64];
   grid_dep_wait();
-  const int64_t q = blockIdx.x, e0 = q * kPiece, e1 = e0 + kPiece;
-  if (e1 >= n) return;
-  const int cur = key[e1 - 1];
-  if (cur >= V || key[e1] != cur) return;
-  if (key[e0] == cur && e0 > 0 && key[e0 - 1] == cur) return;  // began earlier
-  // the last position of the token: the first of a larger key, less one
-  int64_t lo = e1, hi = n;
-  while (lo + 1 < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (key[mid] == cur) lo = mid; else hi = mid;
-  }
-  const int64_t last = lo / kPiece, count = last - q + 1;  // pieces q .. last
   const int lanes = H / 8, groups = 256 / lanes;
   const int g = threadIdx.x / lanes, c = threadIdx.x % lanes;
-  const int64_t per = (count + groups - 1) / groups;
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (g < groups) {
-    const int64_t end = min(count, (g + 1) * per);
-    for (int64_t i = g * per; i < end; ++i) {
-      float v[8];
-      load8((i == 0 ? tail : head) + (q + i) * H + c * 8, v);
+  const int64_t q0 = (int64_t)blockIdx.x * groups, q = q0 + g, e0 = q * piece, e1 = e0 + piece;
+  if (threadIdx.x < 64) many[threadIdx.x] = 0;
+  __syncthreads();
+  if (g < groups && e1 < n) {
+    const int cur = key[e1 - 1];
+    const bool begins = !(key[e0] == cur && e0 > 0 && key[e0 - 1] == cur);
+    if (cur < V && key[e1] == cur && begins) {
+      int next[kJoinFew];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += v[j];
+      for (int i = 0; i < kJoinFew; ++i) next[i] = e1 + (int64_t)i * piece < n ? key[e1 + (int64_t)i * piece] : -1;
+      int count = 0;
+#pragma unroll
+      for (int i = 0; i < kJoinFew; ++i) count += count == i && next[i] == cur;
+      if (count == kJoinFew) {
+        many[g] = 1;
+      } else {
+        float acc[8];
+        load8(tail + q * H + c * 8, acc);
+        for (int i = 1; i <= count; ++i) {
+          float v[8];
+          load8(head + (q + i) * H + c * 8, v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[j] += v[j];
+        }
+        join_write(acc, dtable + (int64_t)cur * H + c * 8, accumulate);
+      }
     }
-    store8(part + threadIdx.x * 8, acc);
   }
   __syncthreads();
-  if (g == 0) {
-    for (int o = 1; o < groups; ++o) {
-      float v[8];
-      load8(part + (o * lanes + c) * 8, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += v[j];
+  for (int b = 0; b < groups; ++b) {
+    if (!many[b]) continue;
+    const int64_t qb = q0 + b;
+    const int cur = key[(qb + 1) * piece];
+    int64_t count = 1;  // pieces qb .. qb + count - 1
+    for (int more = 256; more == 256; count += more) {
+      const int64_t e = (qb + count + threadIdx.x) * piece;
+      more = __syncthreads_count(e < n && key[e] == cur);
     }
-    float* row = dtable + (int64_t)cur * H + c * 8;
-    if (accumulate) {
-      float old[8];
-      load8(row, old);
+    const int64_t per = (count + groups - 1) / groups;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (g < groups) {
+      const int64_t end = min(count, (g + 1) * per);
+#pragma unroll 4
+      for (int64_t i = g * per; i < end; ++i) {
+        float v[8];
+        load8((i == 0 ? tail : head) + (qb + i) * H + c * 8, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += old[j];
+        for (int j = 0; j < 8; ++j) acc[j] += v[j];
+      }
+      store8(part + threadIdx.x * 8, acc);
     }
-    store8(row, acc);
+    __syncthreads();
+    if (g == 0) {
+      for (int o = 1; o < groups; ++o) {
+        float v[8];
+        load8(part + (o * lanes + c) * 8, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += v[j];
+      }
+      join_write(acc, dtable + (int64_t)cur * H + c * 8, accumulate);
+    }
+    __syncthreads();
   }
 }
 
@@ -438,8 +651,8 @@ cudaError_t dropout_bwd(int64_t n, const Drop& d, const float* dy, float* dx, in
 cudaError_t embed_fwd(int bf16, int64_t n, int H, int V, const int32_t* ids, const void* table,
                       float scale, const Drop& d, void* out, int* status, cudaStream_t st) {
   if (n == 0) return cudaSuccess;
-  const int rows = 256 / (H / 8);
-  const int grid = (int)std::min<int64_t>((n + rows - 1) / rows, 152 * 8);
+  const int rows = 256 / (H / 8) * kEmbedUnroll;
+  const unsigned grid = (unsigned)((n + rows - 1) / rows);
   if (bf16)
     k_embed_fwd<__nv_bfloat16><<<grid, 256, 0, st>>>(n, H, V, ids,
                                                      static_cast<const __nv_bfloat16*>(table), scale,
@@ -466,31 +679,37 @@ cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* 
   int32_t* pos[2] = {reinterpret_cast<int32_t*>(base + w.pos[0]),
                      reinterpret_cast<int32_t*>(base + w.pos[1])};
   int* hist = reinterpret_cast<int*>(base + w.hist);
-  uint8_t* seen = reinterpret_cast<uint8_t*>(base + w.seen);
   float* head = reinterpret_cast<float*>(base + w.head);
   float* tail = reinterpret_cast<float*>(base + w.tail);
-  cudaError_t e = launch_pdl(k_sort_count, dim3(s.nb), dim3(256), 0, st, n, V, s, ids, hist, seen,
-                             status);
+  cudaError_t e;
+  const bool small = n <= kTile;
+  if (small)
+    e = launch_pdl(k_sort_small, dim3(1), dim3(256), 0, st, (int)n, V, s, ids, key[(s.passes - 1) & 1],
+                   pos[(s.passes - 1) & 1], status);
+  else
+    e = launch_pdl(k_sort_count, dim3(s.nb), dim3(256), 0, st, n, V, s, ids, hist, status);
   if (e != cudaSuccess) return e;
   note_launch();
-  for (int p = 0; p < s.passes; ++p) {
+  for (int p = 0; p < s.passes && !small; ++p) {
     e = launch_pdl(k_sort_pass, dim3(s.nb), dim3(256), 0, st, n, V, s, p, ids, key[(p + 1) & 1],
-                   pos[(p + 1) & 1], key[p & 1], pos[p & 1], hist, seen);
+                   pos[(p + 1) & 1], key[p & 1], pos[p & 1], hist);
     if (e != cudaSuccess) return e;
     note_launch();
   }
   const int32_t* k = key[(s.passes - 1) & 1];
   const int32_t* at = pos[(s.passes - 1) & 1];
-  const int groups = 256 / (H / 8);
-  const int64_t pieces = (n + kPiece - 1) / kPiece;
-  const int sum_blocks = (int)std::min<int64_t>((pieces + groups - 1) / groups, 152 * 16);
-  const int zero_blocks =
-      accumulate ? 0 : (int)std::min<int64_t>(((int64_t)V + 16 * groups - 1) / (16 * groups), 152 * 4);
-  e = launch_pdl(k_embed_sum, dim3(sum_blocks + zero_blocks), dim3(256), 0, st, n, H, V, k, at, dout,
-                 scale, d, dtable, accumulate, head, tail, seen, sum_blocks);
+  const int groups = 256 / (H / 8), piece = piece_size(n, H);
+  const int64_t pieces = (n + piece - 1) / piece;
+  const int64_t sum_blocks = (pieces + groups - 1) / groups;
+  // with few rows, blocks for the table's zeros
+  const int64_t blocks =
+      accumulate ? sum_blocks : std::max<int64_t>(sum_blocks, std::min<int64_t>((V + 127) / 128, 152 * 2));
+  e = launch_pdl(k_embed_sum, dim3((unsigned)blocks), dim3(256), 0, st, n, H, V, piece, k, at, dout,
+                 scale, d, dtable, accumulate, head, tail);
   if (e != cudaSuccess) return e;
   note_launch();
-  e = launch_pdl(k_embed_join, dim3((unsigned)pieces), dim3(256), 0, st, n, H, V, k, dtable,
+  if (pieces == 1) return cudaSuccess;
+  e = launch_pdl(k_embed_join, dim3((unsigned)sum_blocks), dim3(256), 0, st, n, H, V, piece, k, dtable,
                  accumulate, head, tail);
   if (e != cudaSuccess) return e;
   note_launch();

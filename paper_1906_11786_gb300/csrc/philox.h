@@ -20,6 +20,7 @@ struct Drop {
   uint32_t k0, k1;  // key: the seed
   uint32_t c2, c3;  // upper half of the counter: the call
   uint32_t thr;     // round(p 2^16), 0 = everything kept, 65536 = nothing
+  uint32_t lim;     // thr 2^16 - 1: 16 bits in the upper half of a word are kept iff the word is larger
   float scale;      // 65536 / (65536 - thr), 0 when nothing is kept
 };
 
@@ -30,6 +31,7 @@ inline Drop make_drop(float p, int64_t seed, int64_t call) {
   d.c2 = (uint32_t)call;
   d.c3 = (uint32_t)((uint64_t)call >> 32);
   d.thr = (uint32_t)((double)p * 65536.0 + 0.5);
+  d.lim = (d.thr << 16) - 1u;
   d.scale = d.thr < 65536u ? (float)(65536.0 / (65536.0 - d.thr)) : 0.f;
   return d;
 }
@@ -53,13 +55,13 @@ __device__ __forceinline__ uint4 philox_block(const Drop& d, uint64_t b) {
 
 // v[j] <- v[j] * scale where element 8 b + j is kept, 0 where it is dropped (also where v[j] is not
 // finite).
-__device__ __forceinline__ void drop8(const Drop& d, uint64_t b, float* v) {
+__device__ __forceinline__ void drop8(const Drop& d, uint64_t b, float scale, float* v) {
   const uint4 w = philox_block(d, b);
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    v[2 * j] = (u[j] & 0xFFFFu) >= d.thr ? v[2 * j] * d.scale : 0.f;
-    v[2 * j + 1] = (u[j] >> 16) >= d.thr ? v[2 * j + 1] * d.scale : 0.f;
+    v[2 * j] = (u[j] << 16) > d.lim ? v[2 * j] * scale : 0.f;
+    v[2 * j + 1] = u[j] > d.lim ? v[2 * j + 1] * scale : 0.f;
   }
 }
 
