@@ -189,15 +189,28 @@ SortPlan sort_plan(int64_t n, int V) {
   return s;
 }
 
-// Sorted positions of a piece: at most kMaxPiece, and such that the pieces fill the SMs (two blocks of 256
-// threads each, H / 8 threads a piece) a whole number of times.
-constexpr int kMaxPiece = 64;
-constexpr int kMaxRun = 64 * kMaxPiece;  // sorted positions of a block of k_embed_sum (H = 32)
-int piece_size(int64_t n, int H) {
-  const int64_t slots = 152 * 2 * (256 / (H / 8));
-  const int64_t waves = (n + slots * kMaxPiece - 1) / (slots * kMaxPiece);
+// The blocks of k_embed_sum: a group of lanes (H / 8, rounded up to a power of two) sums a piece of sorted
+// positions; a warp has a ring of kRing rows on their way for its groups.
+constexpr int kMaxPiece = 64, kRing = 8;
+struct SumPlan {
+  int lanes, groups, piece;
+  int64_t pieces, blocks;
+  int smem;
+};
+SumPlan sum_plan(int64_t n, int H) {
+  SumPlan p;
+  p.lanes = H / 8 <= 4 ? 4 : H / 8 <= 8 ? 8 : H / 8 <= 16 ? 16 : 32;
+  p.groups = 256 / p.lanes;
+  // pieces of at most kMaxPiece that fill the SMs (two or three blocks each) a whole number of times
+  const int most = p.groups * kMaxPiece * 8 + kRing * 8192 + 1024;
+  const int64_t slots = 152LL * std::min(3, 232448 / most) * p.groups;
+  const int64_t waves = std::max<int64_t>(1, (n + slots * kMaxPiece - 1) / (slots * kMaxPiece));
   const int64_t piece = (n + slots * waves - 1) / (slots * waves);
-  return (int)std::min<int64_t>(kMaxPiece, (piece + 3) / 4 * 4);
+  p.piece = (int)std::min<int64_t>(kMaxPiece, std::max<int64_t>(4, (piece + 1) / 2 * 2));
+  p.pieces = (n + p.piece - 1) / p.piece;
+  p.blocks = (p.pieces + p.groups - 1) / p.groups;
+  p.smem = kRing * 8192 + (2 * p.groups * p.piece + 4) * 4;
+  return p;
 }
 
 inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -214,8 +227,7 @@ BwdWs bwd_ws(int64_t n, int H, int V) {
     o += al(bytes);
     return at;
   };
-  const int piece = piece_size(n, H);
-  const size_t pieces = (size_t)((n + piece - 1) / piece);
+  const size_t pieces = (size_t)sum_plan(n, H).pieces;
   for (int i = 0; i < 2; ++i) {
     w.key[i] = take((size_t)n * 4);
     w.pos[i] = take((size_t)n * 4);
@@ -435,103 +447,114 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// One piece: m keys k0 (k0[-1] and k0[m] are its neighbours') and their rows of dout, columns 8 c ..
-__device__ __forceinline__ void sum_piece(int H, int V, int m, int c, int64_t q, const int* k0,
-                                          const int* rows, const float* __restrict__ dout, float scale,
-                                          const Drop& d, float* __restrict__ dtable, int accumulate,
-                                          float* __restrict__ head, float* __restrict__ tail) {
-  int cur = k0[0];
-  bool begun = k0[-1] == cur;  // the first token began in an earlier piece
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto finish = [&](bool goes_on) {
-    if (cur >= V) return;
-    const float f = d.thr ? scale * d.scale : scale;
+// A row's finished sum to the table (adding in L2 instead, without reading the row, took twice as long).
+__device__ __forceinline__ void add_row(float* acc, float* row, int accumulate) {
+  if (accumulate) {
+    float old[8];
+    load8(row, old);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] *= f;
-    if (begun || goes_on) {
-      store8((begun ? head : tail) + q * H + c * 8, acc);
-    } else {
-      float* row = dtable + (int64_t)cur * H + c * 8;
-      if (accumulate) {
-        float old[8];
-        load8(row, old);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += old[j];
-      }
-      store8(row, acc);
-    }
-  };
-  // four rows being added, four on their way
-  float v[2][4][8];
-  auto fetch = [&](int i0, float (*to)[8]) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i0 + u < m && k0[i0 + u] < V) load8(dout + (int64_t)rows[i0 + u] * H + c * 8, to[u]);
-  };
-  auto add = [&](int i0, float (*from)[8]) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (i0 + u >= m) break;
-      const int k = k0[i0 + u];
-      if (k != cur) {
-        finish(false);
-        begun = false;
-        cur = k;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-      }
-      if (k < V) {
-        if (d.thr) drop8(d, (uint64_t)rows[i0 + u] * (H / 8) + c, 1.f, from[u]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += from[u][j];
-      }
-    }
-  };
-  fetch(0, v[0]);
-  for (int i0 = 0; i0 < m; i0 += 8) {
-    fetch(i0 + 4, v[1]);
-    add(i0, v[0]);
-    fetch(i0 + 8, v[0]);
-    add(i0 + 4, v[1]);
+    for (int j = 0; j < 8; ++j) acc[j] += old[j];
   }
-  finish(k0[m] == cur);
+  store8(row, acc);
 }
 
-// Sums of the rows of each piece of sorted positions, one group of H / 8 threads a piece.  A token that
-// lies within the piece is finished here; the part of one that began in an earlier piece goes to
-// head[piece], of one that begins here and goes on to tail[piece].  Every block also writes the zero
-// rows of its share of the table, the tokens that do not occur.
+__device__ __forceinline__ void copy16_async(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(dst)), "l"(src) : "memory");
+}
+
+// Sums of the rows of each piece of sorted positions, a group of threads a piece.  A token that lies
+// within the piece is finished here; the part of one that began in an earlier piece goes to head[piece],
+// of one that begins here and goes on to tail[piece].  Every block also writes the zero rows of its share
+// of the table, the tokens that do not occur.
+//
+// The rows of dout come through rings in shared memory, kRing - 1 rows a group ahead.  Held in registers
+// instead, the same number ahead, uniform tokens took 69 us for 131071 x 256 over 49999 (63 now); deeper or
+// shallower rings with fewer or more blocks an SM take up to 5% longer.
 __global__ void __launch_bounds__(256)
-    k_embed_sum(int64_t n, int H, int V, int piece, const int32_t* __restrict__ key,
+    k_embed_sum(int64_t n, int H, int V, SumPlan sp, const int32_t* __restrict__ key,
                 const int32_t* __restrict__ pos, const float* __restrict__ dout, float scale,
                 Drop d, float* __restrict__ dtable, int accumulate, float* __restrict__ head,
                 float* __restrict__ tail) {
-  // the block's pieces lie side by side: their keys and rows come in one go, so that the loads of dout
-  // wait for nothing but each other's registers
-  __shared__ int keys[kMaxRun + 2], rows[kMaxRun];
+  extern __shared__ __align__(16) uint8_t sum_smem[];
   __shared__ uint8_t occurs[256];
-  const int lanes = H / 8, groups = 256 / lanes;
-  const int g = threadIdx.x / lanes, c = threadIdx.x % lanes;
+  int* keys = reinterpret_cast<int*>(sum_smem + kRing * 8192);  // [groups * piece + 2]
+  int* rows = keys + sp.groups * sp.piece + 2;                  // [groups * piece]
+  const int g = threadIdx.x / sp.lanes, c = threadIdx.x % sp.lanes, lanes = H / 8;
   grid_dep_launch();
   grid_dep_wait();
-  const int64_t first = (int64_t)blockIdx.x * groups * piece;
-  const int run = (int)max((int64_t)0, min((int64_t)groups * piece, n - first));
+  // the block's pieces lie side by side: their keys and rows come in one go, one more key on either side
+  const int64_t first = (int64_t)blockIdx.x * sp.groups * sp.piece;
+  const int run = (int)max((int64_t)0, min((int64_t)sp.groups * sp.piece, n - first));
   if (run > 0)
     for (int i = threadIdx.x; i < run + 2; i += 256) {
       const int64_t e = first + i - 1;
-      keys[i] = e >= 0 && e < n ? key[e] : -1;  // one more on either side
+      keys[i] = e >= 0 && e < n ? key[e] : -1;
       if (i < run) rows[i] = pos[first + i];
     }
   __syncthreads();
-  if (g < groups && g * piece < run)
-    sum_piece(H, V, min(piece, run - g * piece), c, first / piece + g, keys + 1 + g * piece,
-              rows + g * piece, dout, scale, d, dtable, accumulate, head, tail);
+  const int e0 = g * sp.piece, m = max(0, min(sp.piece, run - e0));
+  const int warp_m = __reduce_max_sync(0xffffffffu, m);
+  if (warp_m > 0) {
+    const int* k0 = keys + 1 + e0;
+    const int64_t q = first / sp.piece + g;
+    // the warp's ring: rows of 1 KB, 32 bytes a thread
+    uint8_t* ring = sum_smem + (threadIdx.x >> 5) * (kRing * 1024) + (threadIdx.x & 31 & ~(sp.lanes - 1)) * 32;
+    auto fetch = [&](int i) {
+      if (i < m && c < lanes && k0[i] < V) {
+        const float* src = dout + (int64_t)rows[e0 + i] * H;
+        uint8_t* dst = ring + i % kRing * 1024;
+        copy16_async(dst + c * 16, src + c * 4);
+        copy16_async(dst + (c + lanes) * 16, src + (c + lanes) * 4);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int cur = m > 0 ? k0[0] : V;
+    bool begun = m > 0 && k0[-1] == cur;  // the first token began in an earlier piece
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto finish = [&](bool goes_on) {
+      if (cur >= V || c >= lanes) return;
+      const float f = d.thr ? scale * d.scale : scale;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] *= f;
+      if (begun || goes_on) {
+        store8((begun ? head : tail) + q * H + c * 8, acc);
+      } else {
+        add_row(acc, dtable + (int64_t)cur * H + c * 8, accumulate);
+      }
+    };
+    for (int i = 0; i < kRing - 1; ++i) fetch(i);
+    for (int i = 0; i < warp_m; ++i) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
+      __syncwarp();
+      if (i < m) {
+        const int k = k0[i];
+        if (k != cur) {
+          finish(false);
+          begun = false;
+          cur = k;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        }
+        if (k < V && c < lanes) {
+          float v[8];
+          load8(reinterpret_cast<const float*>(ring + i % kRing * 1024) + c * 8, v);
+          if (d.thr) drop8(d, (uint64_t)rows[e0 + i] * lanes + c, 1.f, v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[j] += v[j];
+        }
+      }
+      // the place that the row before this one had: every lane has read it before the barrier above
+      fetch(i + kRing - 1);
+    }
+    if (m > 0) finish(k0[m] == cur);
+  }
   if (accumulate) return;
   const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const int v_end = (int)((int64_t)V * (blockIdx.x + 1) / gridDim.x);
-  for (int v0 = (int)((int64_t)V * blockIdx.x / gridDim.x); v0 < v_end; v0 += 256) {
-    const int mine = v0 + threadIdx.x;
-    if (mine < v_end) {  // looked up among the sorted keys: the first of `mine` or more
+  // (tokens blockIdx.x, + gridDim.x, ...: a share of the frequent and of the rare ones)
+  const int share = (int)(((int64_t)V - blockIdx.x + gridDim.x - 1) / gridDim.x);
+  for (int s0 = 0; s0 < share; s0 += 256) {
+    if (s0 + threadIdx.x < share) {  // looked up among the sorted keys: the first of `mine` or more
+      const int mine = blockIdx.x + (s0 + threadIdx.x) * gridDim.x;
       int lo = 0, hi = (int)n;
       while (lo < hi) {
         const int mid = (lo + hi) / 2;
@@ -540,21 +563,12 @@ __global__ void __launch_bounds__(256)
       occurs[threadIdx.x] = lo < n && key[lo] == mine;
     }
     __syncthreads();
-    if (g < groups)
-      for (int k = g; k < 256 && v0 + k < v_end; k += groups)
-        if (!occurs[k]) store8(dtable + (int64_t)(v0 + k) * H + c * 8, zero);
+    if (c < lanes)
+      for (int k = g; k < 256 && s0 + k < share; k += sp.groups)
+        if (!occurs[k])
+          store8(dtable + (blockIdx.x + (int64_t)(s0 + k) * gridDim.x) * H + c * 8, zero);
     __syncthreads();
   }
-}
-
-__device__ __forceinline__ void join_write(float* acc, float* row, int accumulate) {
-  if (accumulate) {
-    float old[8];
-    load8(row, old);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += old[j];
-  }
-  store8(row, acc);
 }
 
 // Tokens that begin in piece q and go on: tail[q] + head[q + 1] + ... , in an order that depends on their
@@ -594,7 +608,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
           for (int j = 0; j < 8; ++j) acc[j] += v[j];
         }
-        join_write(acc, dtable + (int64_t)cur * H + c * 8, accumulate);
+        add_row(acc, dtable + (int64_t)cur * H + c * 8, accumulate);
       }
     }
   }
@@ -629,7 +643,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += v[j];
       }
-      join_write(acc, dtable + (int64_t)cur * H + c * 8, accumulate);
+      add_row(acc, dtable + (int64_t)cur * H + c * 8, accumulate);
     }
     __syncthreads();
   }
@@ -698,19 +712,21 @@ cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* 
   }
   const int32_t* k = key[(s.passes - 1) & 1];
   const int32_t* at = pos[(s.passes - 1) & 1];
-  const int groups = 256 / (H / 8), piece = piece_size(n, H);
-  const int64_t pieces = (n + piece - 1) / piece;
-  const int64_t sum_blocks = (pieces + groups - 1) / groups;
+  const SumPlan sp = sum_plan(n, H);
   // with few rows, blocks for the table's zeros
   const int64_t blocks =
-      accumulate ? sum_blocks : std::max<int64_t>(sum_blocks, std::min<int64_t>((V + 127) / 128, 152 * 2));
-  e = launch_pdl(k_embed_sum, dim3((unsigned)blocks), dim3(256), 0, st, n, H, V, piece, k, at, dout,
+      accumulate ? sp.blocks : std::max<int64_t>(sp.blocks, std::min<int64_t>((V + 127) / 128, 152 * 2));
+  static std::atomic<uint64_t> done{0};
+  e = allow_smem(k_embed_sum, kRing * 8192 + (2 * 64 * kMaxPiece + 4) * 4, done);  // the most it takes
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(k_embed_sum, dim3((unsigned)blocks), dim3(256), sp.smem, st, n, H, V, sp, k, at, dout,
                  scale, d, dtable, accumulate, head, tail);
   if (e != cudaSuccess) return e;
   note_launch();
-  if (pieces == 1) return cudaSuccess;
-  e = launch_pdl(k_embed_join, dim3((unsigned)sum_blocks), dim3(256), 0, st, n, H, V, piece, k, dtable,
-                 accumulate, head, tail);
+  if (sp.pieces == 1) return cudaSuccess;
+  const int groups = 256 / (H / 8);
+  e = launch_pdl(k_embed_join, dim3((unsigned)((sp.pieces + groups - 1) / groups)), dim3(256), 0, st, n,
+                 H, V, sp.piece, k, dtable, accumulate, head, tail);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;

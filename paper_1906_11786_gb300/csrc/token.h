@@ -4,6 +4,7 @@
 
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -43,6 +44,19 @@ cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st
 // Gradients in the type grad_bf16 says; dX or dW may be NULL.
 cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, int grad_bf16,
                      void* dX, void* dW, int accumulate, cudaStream_t st);
+
+// Lets a kernel use `bytes` of dynamic shared memory, once a device.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 // Sites of BG_EDEVICE records (status word): an id or a target of V or more.
 constexpr int kSiteEmbedId = 130;

@@ -30,7 +30,6 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <numeric>
 
@@ -1532,19 +1531,6 @@ bool map_x(const Call& c, CUtensorMap* m, int box) {
 bool map_w(const Call& c, const void* W, CUtensorMap* m, int box) {
   if (c.form == kBf16) return make_map_ld(m, W, c.V, c.H, c.H, box);
   return make_map_ld(m, c.base + c.w.w, (c.form == kF16x2 ? 2 : 1) * c.w.vcap, c.H, c.H, box);
-}
-
-// Lets a kernel use `bytes` of dynamic shared memory, once a device.
-template <typename K>
-cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
-  return e;
 }
 
 template <int HC, int T>
