@@ -370,7 +370,7 @@ int bg_xent_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, 
  *   dW    = sum_i dloss[i] (softmax(z[i]) - onehot(target[i]))^T X[i].
  * dloss [n] fp32 (not used in rows left out, whose dX is 0).  dX [n, H] and dW [V, H] in
  * grad_dtype, either of them may be NULL (not computed).  grad_dtype BG_F32: probabilities enter the
- * products with 22 bits, down to an absolute 2^-38 (times the largest |dloss|, for dW); BG_ACCUM adds to dX and dW instead of overwriting them.  grad_dtype BG_BF16
+ * products with 21 bits, down to an absolute 2^-38 (times the largest |dloss|, for dW); BG_ACCUM adds to dX and dW instead of overwriting them.  grad_dtype BG_BF16
  * (dtype BG_BF16 only, no BG_ACCUM): they enter rounded to bf16, as the results are. */
 int bg_xent_bwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
                 const int32_t* target, const float* lse, const float* dloss, bg_dtype grad_dtype,

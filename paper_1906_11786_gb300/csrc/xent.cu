@@ -19,7 +19,7 @@
 // Number formats ("forms") of the operands:
 //   bf16           X and W as they are; P rounded to bf16 (bf16 gradients, whose own rounding is as large)
 //   fp16, 1 term   bf16 X and W with fp32 gradients: scaled by a power of two, they are exact in
-//                  fp16 (down to 2^-29 of the largest), and P, as the sum of two fp16 terms, keeps 22 bits;
+//                  fp16 (down to 2^-29 of the largest), and P, as the sum of two fp16 terms, keeps 21 bits;
 //                  fp16 and bf16 operands cannot be mixed in one product
 //   fp16, 2 terms  fp32 X and W, each the sum of two fp16 terms (22 bits); products of the two low
 //                  terms (2^-22) are left out
@@ -53,13 +53,13 @@ enum Form { kBf16 = 0, kF16x1 = 1, kF16x2 = 2 };
 inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 
 constexpr int kMaxRowBlocks = 2048;
-constexpr int kTableBlocks = 304;  // at most, of the table's amax and conversion
+constexpr int kTableBlocks = 608;  // at most, of the table's amax and conversion
 constexpr int64_t kDirectRows = 32768;
 
-// Rows of one block of k_xent_count / k_xent_rows: at most kMaxRowBlocks blocks, since each adds up the
-// counts of those before it.
+// Rows of one block of k_xent_count / k_xent_rows: few, so that many blocks share the copying, while
+// there are at most kMaxRowBlocks blocks (each adds up the counts of those before it).
 inline int64_t rows_per_block(int64_t n) {
-  return 256 * std::max<int64_t>(1, (n + 256LL * kMaxRowBlocks - 1) / (256LL * kMaxRowBlocks));
+  return n <= 64LL * 1024 ? 64 : 256 * ((n + 256LL * kMaxRowBlocks - 1) / (256LL * kMaxRowBlocks));
 }
 
 struct Ws {
@@ -150,14 +150,19 @@ __device__ __forceinline__ uint32_t amax8(const float* v, uint32_t m) {
   return m;
 }
 
-__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* sm) {
-  v = __reduce_max_sync(0xffffffffu, v);
+// The maxima over the block of three values at once (sm [24]).
+__device__ __forceinline__ void block_max3(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t* sm) {
+  a = __reduce_max_sync(0xffffffffu, a);
+  b = __reduce_max_sync(0xffffffffu, b);
+  c = __reduce_max_sync(0xffffffffu, c);
+  const int warp = threadIdx.x >> 5;
+  if ((threadIdx.x & 31) == 0) sm[warp] = a, sm[8 + warp] = b, sm[16 + warp] = c;
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-  __syncthreads();
-  uint32_t r = 0;
-  for (int i = 0; i < 8; ++i) r = max(r, sm[i]);
-  return r;
+  for (int i = 0; i < 8; ++i) {
+    a = max(a, sm[i]);
+    b = max(b, sm[8 + i]);
+    c = max(c, sm[16 + i]);
+  }
 }
 
 // Exponent k such that values of magnitude up to the one with these bits, times 2^k, are below 2^15.
@@ -167,26 +172,27 @@ __device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)
 // Labelled rows of each block of rb rows and, for the fp16 forms, the largest finite magnitudes of
 // the labelled rows of X, of their dloss, and of W.
 __global__ void __launch_bounds__(256) k_xent_count(RowArgs a) {
-  __shared__ uint32_t sm[8];
+  __shared__ uint32_t sm[24];
+  __shared__ int sums[8];
   grid_dep_launch();
   grid_dep_wait();
   const int lanes = a.H / 8;
+  uint32_t mx = 0, mg = 0, mw = 0;
   if ((int64_t)blockIdx.x >= a.nb) {
     const int b = blockIdx.x - (int)a.nb;
-    uint32_t mx = 0;
     const int64_t chunks = (int64_t)a.V * lanes;
+#pragma unroll 4
     for (int64_t i = (int64_t)b * 256 + threadIdx.x; i < chunks; i += (int64_t)a.tb * 256) {
       float v[8];
       load8f(a.W, a.x_bf16, i * 8, v);
-      mx = amax8(v, mx);
+      mw = amax8(v, mw);
     }
-    mx = block_max(mx, sm);
-    if (threadIdx.x == 0) a.amax[2 * a.nb + b] = mx;
+    block_max3(mx, mg, mw, sm);
+    if (threadIdx.x == 0) a.amax[2 * a.nb + b] = mw;
     return;
   }
   const int64_t r0 = blockIdx.x * a.rb, r1 = min(a.n, r0 + a.rb);
   int c = 0;
-  uint32_t mg = 0;
   for (int64_t i = r0 + threadIdx.x; i < r1; i += 256) {
     const int t = a.target[i];
     if (t >= 0 && t < a.V) {
@@ -198,27 +204,24 @@ __global__ void __launch_bounds__(256) k_xent_count(RowArgs a) {
     }
   }
   c = __reduce_add_sync(0xffffffffu, c);
-  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = c;
-  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = c;
+  if (a.form != kBf16) {
+    const int rows = 256 / lanes, r = threadIdx.x / lanes, q = threadIdx.x % lanes;
+    if (r < rows)
+#pragma unroll 4
+      for (int64_t i = r0 + r; i < r1; i += rows) {
+        const int t = a.target[i];
+        if (t < 0 || t >= a.V) continue;
+        float v[8];
+        load8f(a.X, a.x_bf16, i * a.H + q * 8, v);
+        mx = amax8(v, mx);
+      }
+  }
+  block_max3(mx, mg, mw, sm);  // (and the barrier that the sums need)
   if (threadIdx.x == 0) {
     int s = 0;
-    for (int i = 0; i < 8; ++i) s += sm[i];
+    for (int i = 0; i < 8; ++i) s += sums[i];
     a.counts[blockIdx.x] = s;
-  }
-  if (a.form == kBf16) return;
-  uint32_t mx = 0;
-  const int rows = 256 / lanes, r = threadIdx.x / lanes, q = threadIdx.x % lanes;
-  if (r < rows)
-    for (int64_t i = r0 + r; i < r1; i += rows) {
-      const int t = a.target[i];
-      if (t < 0 || t >= a.V) continue;
-      float v[8];
-      load8f(a.X, a.x_bf16, i * a.H + q * 8, v);
-      mx = amax8(v, mx);
-    }
-  mx = block_max(mx, sm);
-  mg = block_max(mg, sm);
-  if (threadIdx.x == 0) {
     a.amax[blockIdx.x] = mx;
     a.amax[a.nb + blockIdx.x] = mg;
   }
@@ -248,27 +251,45 @@ __device__ __forceinline__ void put8(uint16_t* dst, int64_t plane, int64_t at, i
 // blocks from nb on convert W.
 __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
   __shared__ int wsum[8];
-  __shared__ uint32_t sm[8];
+  __shared__ uint32_t sm[24];
   __shared__ int64_t from[256];  // row of each slot of the group at hand
   grid_dep_launch();
   grid_dep_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int lanes = a.H / 8, rows = 256 / lanes, rr = tid / lanes, q = tid % lanes;
+  const bool table = (int64_t)blockIdx.x >= a.nb;
   uint32_t mx = 0, mg = 0, mw = 0;
+  int before = 0;  // labelled rows of the blocks before this one
+  if (!table) {
+    if (a.direct) {
+      const int4* t4 = reinterpret_cast<const int4*>(a.target);
+#pragma unroll 8
+      for (int i = tid; i < (int)(blockIdx.x * a.rb / 4); i += 256) {
+        const int4 t = t4[i];
+        before += (t.x >= 0 && t.x < a.V) + (t.y >= 0 && t.y < a.V) + (t.z >= 0 && t.z < a.V) +
+                  (t.w >= 0 && t.w < a.V);
+      }
+    } else {
+#pragma unroll 4
+      for (int64_t i = tid; i < (int64_t)blockIdx.x; i += 256) before += a.counts[i];
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    if (lane == 0) wsum[warp] = before;
+  }
   if (a.form != kBf16) {
+#pragma unroll 4
     for (int64_t i = tid; i < a.nb; i += 256) {
       mx = max(mx, a.amax[i]);
       mg = max(mg, a.amax[a.nb + i]);
     }
     for (int i = tid; i < a.tb; i += 256) mw = max(mw, a.amax[2 * a.nb + i]);
-    mx = block_max(mx, sm);
-    mg = block_max(mg, sm);
-    mw = block_max(mw, sm);
   }
-  if ((int64_t)blockIdx.x >= a.nb) {
+  block_max3(mx, mg, mw, sm);
+  if (table) {
     const int b = blockIdx.x - (int)a.nb;
     const float scale = pow2(shift_of(mw));
     const int64_t chunks = (int64_t)a.V * lanes, all = a.vcap * lanes;
+#pragma unroll 4
     for (int64_t i = (int64_t)b * 256 + tid; i < all; i += (int64_t)a.tb * 256) {
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (i < chunks) load8f(a.W, a.x_bf16, i * 8, v);
@@ -278,24 +299,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
   }
   const float scale = a.form == kBf16 ? 1.f : pow2(shift_of(mx));
   int64_t base = 0;
-  {
-    int c = 0;
-    if (a.direct) {
-      const int4* t4 = reinterpret_cast<const int4*>(a.target);
-#pragma unroll 4
-      for (int i = tid; i < (int)(blockIdx.x * a.rb / 4); i += 256) {
-        const int4 t = t4[i];
-        c += (t.x >= 0 && t.x < a.V) + (t.y >= 0 && t.y < a.V) + (t.z >= 0 && t.z < a.V) +
-             (t.w >= 0 && t.w < a.V);
-      }
-    } else {
-      for (int64_t i = tid; i < (int64_t)blockIdx.x; i += 256) c += a.counts[i];
-    }
-    c = __reduce_add_sync(0xffffffffu, c);
-    if (lane == 0) wsum[warp] = c;
-    __syncthreads();
-    for (int i = 0; i < 8; ++i) base += wsum[i];
-  }
+  for (int i = 0; i < 8; ++i) base += wsum[i];
   const int64_t r0 = blockIdx.x * a.rb, r1 = min(a.n, r0 + a.rb);
   for (int64_t g0 = r0; g0 < r1; g0 += 256) {
     const int64_t i = g0 + tid;
@@ -404,9 +408,15 @@ struct Units {
   // The rows that staying tile t stands for: tile t * step mod nt (step prime to nt).  Tiles of
   // frequent tokens, whose units take up to half as long again, then do not all fall to one CTA.
   __device__ int tile(int t) const { return step == 1 ? t : (int)((uint32_t)t * (uint64_t)(uint32_t)step % (uint32_t)nt); }
-  __device__ int64_t begin(int c) const {
-    return c >= G ? U : tiles ? (int64_t)nt * c / G * ct : U * c / G;
+  // (divided in 32 bits where that holds the operands, several times faster)
+  static __device__ int64_t div(int64_t x, int64_t y) {
+    return ((uint64_t)x | (uint64_t)y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
   }
+  __device__ int64_t begin(int c) const {
+    return c >= G ? U : tiles ? div((int64_t)nt * c, G) * ct : div(U * c, G);
+  }
+  // the staying tile of unit u
+  __device__ int64_t tile_of(int64_t u) const { return div(u, ct); }
   // staying and passing tile of the next unit of a run
   struct Walk {
     int t, j;
@@ -416,7 +426,7 @@ struct Units {
     __device__ Walk(const Units& u, int c) : ct((int)u.ct) {
       const int64_t u0 = u.begin(c);
       left = u.begin(c + 1) - u0;
-      t = left > 0 ? (int)(u0 / u.ct) : 0;
+      t = left > 0 ? (int)u.tile_of(u0) : 0;
       j = left > 0 ? (int)(u0 - (int64_t)t * u.ct) : 0;
       starts = true;
       ends = left == 1 || j + 1 == ct;
@@ -430,11 +440,11 @@ struct Units {
     }
   };
   // the last CTA with units before `end` (runs that share tiles)
-  __device__ int last_before(int64_t end) const { return (int)((end * G + U - 1) / U) - 1; }
+  __device__ int last_before(int64_t end) const { return (int)div(end * G + U - 1, U) - 1; }
   // whether CTA c has all units of tile t
   __device__ bool whole(int c, int64_t t) const { return begin(c) <= t * ct && t * ct + ct <= begin(c + 1); }
   // which of its two partial results CTA c keeps of tile t, one it shares with others
-  __device__ int slot(int c, int64_t t) const { return t == begin(c) / ct ? 0 : 1; }
+  __device__ int slot(int c, int64_t t) const { return t == tile_of(begin(c)) ? 0 : 1; }
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -460,6 +470,11 @@ __device__ __forceinline__ void unpack2(uint64_t x, float& a, float& b) {
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
@@ -822,8 +837,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
 }
 
 // Rows of the tiles that several CTAs have parts of.  Block c takes the tile that CTA c is the first to
-// begin inside of, a quarter of its rows a block; 2 threads share a row, 32 where it has parts of many
-// CTAs.
+// begin inside of, 8 of its rows a block; a row is 2 threads', or a warp's where it has parts of many CTAs.
 __global__ void __launch_bounds__(256) k_xent_join(const __grid_constant__ FwdArgs a) {
   grid_dep_launch();
   grid_dep_wait();
@@ -831,20 +845,19 @@ __global__ void __launch_bounds__(256) k_xent_join(const __grid_constant__ FwdAr
   const Units un((rows + 127) / 128, (a.V + 255) / 256, gridDim.x, a.tiles);
   const int c = blockIdx.x;
   if (c >= un.G || c == 0) return;
-  const int64_t begin = un.begin(c);
-  if (begin % un.ct == 0) return;
-  const int64_t t = begin / un.ct, first = t * un.ct, end = first + un.ct;
-  if (un.begin(c - 1) > first) return;  // an earlier CTA begins inside the tile too
+  const int64_t begin = un.begin(c), t = un.tile_of(begin), first = t * un.ct, end = first + un.ct;
+  if (begin == first || un.begin(c - 1) > first) return;  // none, or an earlier CTA begins inside it too
   const int last = un.last_before(end);
   // CTA c - 1 has the first part (in its second place unless the tile is its first), the others begin
   // with this tile
   const float2* head = a.part + ((int64_t)(c - 1) * 2 + un.slot(c - 1, t)) * 512;
   const float2* tail = a.part + (int64_t)c * 1024;
   const int n = 4 * (last - c + 2), lanes = n > 16 ? 32 : 2;
-  for (int q = threadIdx.x / lanes; q < 32; q += 256 / lanes) {
-    const int r = blockIdx.y * 32 + q;
+  const int q = threadIdx.x / lanes;
+  if (q < 8) {
+    const int r = blockIdx.y * 8 + q;
     const int64_t s = t * 128 + r;
-    if (s >= rows) break;  // (a whole group of lanes)
+    if (s >= rows) return;  // (a whole group of lanes)
     float m = -3.0e38f, l = 0.f;
     for (int i = threadIdx.x % lanes; i < n; i += lanes) {
       const float2 p = i < 4 ? head[i * 128 + r] : tail[(int64_t)(i / 4 - 1) * 1024 + (i & 3) * 128 + r];
@@ -972,7 +985,7 @@ __device__ __forceinline__ void probs_col(uint32_t* v, float descale, float up, 
 #pragma unroll
   for (int g = 0; g < N / 8; ++g) {
     const uint64_t nl = *reinterpret_cast<const uint64_t*>(stat + kNlse + 8 * g + c);
-    const float2 gg = *reinterpret_cast<const float2*>(stat + kG + 8 * g + c);
+    const uint64_t g2 = *reinterpret_cast<const uint64_t*>(stat + kG + 8 * g + c);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint32_t* p = v + (k >> 1) * (N / 2) + 4 * g + 2 * (k & 1);
@@ -980,8 +993,9 @@ __device__ __forceinline__ void probs_col(uint32_t* v, float descale, float up, 
       x = FORM == kBf16 ? fma2(x, l2e, nl) : fma2(fma2(x, ds, nl), l2e, up2);
       float a, b;
       unpack2(x, a, b);
-      p[0] = __float_as_uint(ex2(a) * gg.x);
-      p[1] = __float_as_uint(ex2(b) * gg.y);
+      unpack2(mul2(pack2(ex2(a), ex2(b)), g2), a, b);
+      p[0] = __float_as_uint(a);
+      p[1] = __float_as_uint(b);
     }
   }
   if (hits) {
@@ -1010,10 +1024,12 @@ __device__ __forceinline__ void terms(uint32_t a, uint32_t b, uint32_t& hi, uint
     const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
     hi = *reinterpret_cast<const uint32_t*>(&p);
   } else {
-    const __half2 p = __floats2half2_rn(x, y);
+    // the high term by cutting the mantissa to fp16's 11 bits, so that the rest is exact and nothing has to
+    // be converted back
+    const uint32_t hx = a & 0xFFFFE000u, hy = b & 0xFFFFE000u;
+    const __half2 p = __floats2half2_rn(__uint_as_float(hx), __uint_as_float(hy));
     hi = *reinterpret_cast<const uint32_t*>(&p);
-    const float2 f = __half22float2(p);
-    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+    const __half2 l = __floats2half2_rn(x - __uint_as_float(hx), y - __uint_as_float(hy));
     lo = *reinterpret_cast<const uint32_t*>(&l);
   }
 }
@@ -1416,9 +1432,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 }
 
 // Tiles that several CTAs have parts of: the sum of the parts in the order of the CTAs.  Block row c
-// takes the tile that CTA c is the first to begin inside of, 32 rows x 32 columns a block.
+// takes the tile that CTA c is the first to begin inside of, 32 rows x 32 columns a block (with a
+// whole tile's rows a block, tiles of many parts took twice as long).
 __global__ void __launch_bounds__(256)
-    k_xent_bwd_join(BwdArgs a, int form, int nb) {
+    k_xent_bwd_join(const __grid_constant__ BwdArgs a, int form, int nb) {
   grid_dep_launch();
   grid_dep_wait();
   const int64_t rows = a.head[0];
@@ -1427,35 +1444,38 @@ __global__ void __launch_bounds__(256)
   const Units un(dw ? (a.V + 127) / 128 : (rows + 127) / 128,
                  dw ? (rows + nb - 1) / nb : (a.V + nb - 1) / nb, ctas, a.tiles, dw ? a.step : 1);
   void* out = dw ? a.dW : a.dX;
-  const int hb = a.H / 32;
-  const int col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x & 7) * 4;
-  const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x >> 3);
   if (c >= un.G || c == 0) return;
-  const int64_t begin = un.begin(c);
-  if (begin % un.ct == 0) return;
-  const int64_t t = begin / un.ct, first = t * un.ct, end = first + un.ct;
-  if (un.begin(c - 1) > first) return;  // an earlier CTA begins inside the tile too
-  int64_t orow = (int64_t)un.tile((int)t) * 128 + r;
-  float s1 = 1.f, s2 = 1.f, s3 = 1.f;
+  const int64_t begin = un.begin(c), t = un.tile_of(begin), first = t * un.ct, end = first + un.ct;
+  if (begin == first) return;
+  const int64_t prev = un.begin(c - 1);
+  if (prev > first) return;  // an earlier CTA begins inside the tile too
+  const int hb = a.H / 32, col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x & 7) * 4;
+  const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x >> 3);
   // CTA c - 1 has the first part (in its second place unless the tile is its first), the others begin
   // with this tile
-  const float* part = a.part + ((int64_t)(blockIdx.x - c) * 2 * 128 + r) * a.H + col;
   const int64_t stride = 128LL * a.H;
-  float4 x = *reinterpret_cast<const float4*>(part + ((int64_t)(c - 1) * 2 + un.slot(c - 1, t)) * stride);
+  const float* part = a.part + (int64_t)(blockIdx.x - c) * 2 * stride + (int64_t)r * a.H + col;
+  const float* head = part + ((int64_t)(c - 1) * 2 + (un.tile_of(prev) == t ? 0 : 1)) * stride;
+  float4 x = *reinterpret_cast<const float4*>(head);
   const int last = un.last_before(end);
 #pragma unroll 8
   for (int k = c; k <= last; ++k) {
     const float4 p = *reinterpret_cast<const float4*>(part + (int64_t)k * 2 * stride);
     x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
   }
+  float s1 = 1.f, s2 = 1.f;
+  if (form != kBf16) {
+    s1 = pow2(dw ? -a.head[3] : -15);
+    s2 = pow2(dw ? -a.head[1] : -a.head[2]);
+  }
+  int64_t orow = (int64_t)un.tile((int)t) * 128 + r;
+  float s3 = 1.f;
   if (dw) {
     if (orow >= a.V) return;
-    if (form != kBf16) s1 = pow2(-a.head[3]), s2 = pow2(-a.head[1]);
   } else {
     s3 = a.stat[stat_at(orow) + kG];
     orow = a.row[orow];
     if (orow < 0) return;
-    if (form != kBf16) s1 = pow2(-15), s2 = pow2(-a.head[2]);
   }
   x = make_float4(x.x * s1 * s2 * s3, x.y * s1 * s2 * s3, x.z * s1 * s2 * s3, x.w * s1 * s2 * s3);
   if (a.out_bf16) {
@@ -1508,9 +1528,9 @@ cudaError_t prepare(const XentArgs& a, Call& c, RowArgs r) {
   // Up to kDirectRows rows, each block of k_xent_rows counts the rows before its own (at most 128 KB of
   // targets, from L2) in less time than a launch takes; the fp16 forms need the magnitudes first anyway.
   r.direct = c.form == kBf16 && a.n <= kDirectRows;
-  // of the table, at least four passes of 256 threads a block
+  // of the table, 256 times 8 elements a block and pass
   r.tb = c.form == kBf16 ? 0
-                         : (int)std::min<int64_t>(kTableBlocks, ((int64_t)a.V * (a.H / 8) + 1023) / 1024);
+                         : (int)std::min<int64_t>(kTableBlocks, ((int64_t)a.V * (a.H / 8) + 255) / 256);
   cudaError_t e;
   if (!r.direct) {
     e = launch_pdl(k_xent_count, dim3((unsigned)c.w.nb + r.tb), dim3(256), 0, c.st, r);
@@ -1550,9 +1570,10 @@ template <int HC, int FORM>
 cudaError_t run_bwd(const Call& c, const void* W, const BwdArgs& b) {
   using C = BCfg<HC, FORM>;
   CUtensorMap xs, xp, ws, wp;
-  if (!map_x(c, &xs, 128) || !map_x(c, &xp, C::NB) || !map_w(c, W, &ws, 128) ||
-      !map_w(c, W, &wp, C::NB))
-    return cudaErrorInvalidValue;
+  if (!map_x(c, &xs, 128) || !map_w(c, W, &ws, 128)) return cudaErrorInvalidValue;
+  xp = xs;
+  wp = ws;
+  if (C::NB != 128 && (!map_x(c, &xp, C::NB) || !map_w(c, W, &wp, C::NB))) return cudaErrorInvalidValue;
   static std::atomic<uint64_t> done{0};
   cudaError_t e = allow_smem(k_xent_bwd<HC, FORM>, C::SMEM, done);
   if (e != cudaSuccess) return e;
@@ -1643,7 +1664,7 @@ cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st
   if (e != cudaSuccess) return e;
   note_launch();
   if (f.tiles) return cudaSuccess;
-  e = launch_pdl(k_xent_join, dim3(c.sms, 4), dim3(256), 0, st, f);
+  e = launch_pdl(k_xent_join, dim3(c.sms, 16), dim3(256), 0, st, f);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
