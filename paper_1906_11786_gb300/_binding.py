@@ -386,15 +386,20 @@ def _shaped(t, name, dtype, *shape):
         return None
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
-    return _dev_ptr(t, name)
+    if t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _dev_ptr(t, name)  # raises
 
 
 def _elements(t, name, dtype, n):
+    """The same for n elements of any shape."""
     if t is None:
         return None
     if t.dtype is not dtype or t.numel() != n:
         raise ValueError(f"{name} must have {n} elements of {dtype}, not {t.numel()} of {t.dtype}")
-    return _dev_ptr(t, name)
+    if t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _dev_ptr(t, name)  # raises
 
 
 def _stream_of(stream, t):
@@ -406,15 +411,25 @@ def _stream_of(stream, t):
     return _stream(stream)
 
 
-def _torch_dtype(code):
-    import torch
-    return torch.bfloat16 if code == BG_BF16 else torch.float32
+_types = {}  # what dtype_code takes -> (code, torch dtype)
+
+
+def _type(dtype):
+    got = _types.get(dtype)
+    if got is None:
+        import torch
+        if dtype == "ids":
+            got = None, torch.int32
+        else:
+            code = dtype_code(dtype)
+            got = code, torch.bfloat16 if code == BG_BF16 else torch.float32
+        _types[dtype] = got
+    return got
 
 
 def dropout_fwd(dtype, x, y, p, seed, call, residual=None, stream=None):
     """y = residual + drop(x) elementwise (tensors of `dtype` with equal element counts)."""
-    dt = dtype_code(dtype)
-    td, n = _torch_dtype(dt), x.numel()
+    (dt, td), n = _type(dtype), x.numel()
     _check(load().bg_dropout_fwd(dt, n, p, seed, call, _elements(x, "x", td, n),
                                  _elements(residual, "residual", td, n),
                                  _elements(y, "y", td, n), _stream_of(stream, x)))
@@ -422,17 +437,15 @@ def dropout_fwd(dtype, x, y, p, seed, call, residual=None, stream=None):
 
 def dropout_bwd(dy, dx, p, seed, call, flags=0, stream=None):
     """dx (+)= drop(dy) with the mask of the forward call of the same (p, seed, call); fp32."""
-    td, n = _torch_dtype(BG_F32), dy.numel()
+    (_, td), n = _type(BG_F32), dy.numel()
     _check(load().bg_dropout_bwd(n, p, seed, call, _elements(dy, "dy", td, n),
                                  _elements(dx, "dx", td, n), flags, _stream_of(stream, dy)))
 
 
 def embed_fwd(dtype, ids, table, out, scale=1.0, p=0.0, seed=0, call=0, stream=None):
     """out[i] = drop(scale * table[ids[i]]), zero rows where ids[i] < 0; ids [n] int32."""
-    import torch
-    dt = dtype_code(dtype)
-    td, n, (V, H) = _torch_dtype(dt), ids.numel(), table.shape
-    _check(load().bg_embed_fwd(dt, n, H, V, _shaped(ids, "ids", torch.int32, n),
+    (dt, td), (_, ti), n, (V, H) = _type(dtype), _type("ids"), ids.numel(), table.shape
+    _check(load().bg_embed_fwd(dt, n, H, V, _shaped(ids, "ids", ti, n),
                                _shaped(table, "table", td, V, H), scale, p, seed, call,
                                _shaped(out, "out", td, n, H), _stream_of(stream, out)))
 
@@ -443,11 +456,10 @@ def embed_workspace_bytes(n, H, V) -> int:
 
 def embed_bwd(ids, dout, dtable, ws, scale=1.0, p=0.0, seed=0, call=0, flags=0, stream=None):
     """dtable[v] (+)= scale * sum over ids[i] = v of drop(dout[i]); fp32."""
-    import torch
-    n, (V, H) = ids.numel(), dtable.shape
-    _check(load().bg_embed_bwd(n, H, V, _shaped(ids, "ids", torch.int32, n),
-                               _shaped(dout, "dout", torch.float32, n, H), scale, p, seed, call,
-                               _shaped(dtable, "dtable", torch.float32, V, H), flags,
+    (_, td), (_, ti), n, (V, H) = _type(BG_F32), _type("ids"), ids.numel(), dtable.shape
+    _check(load().bg_embed_bwd(n, H, V, _shaped(ids, "ids", ti, n),
+                               _shaped(dout, "dout", td, n, H), scale, p, seed, call,
+                               _shaped(dtable, "dtable", td, V, H), flags,
                                _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
                                _stream_of(stream, dtable)))
 
@@ -459,25 +471,24 @@ def xent_workspace_bytes(dtype, n, H, V, op) -> int:
 def xent_fwd(dtype, X, W, target, loss, lse, ws, stream=None):
     """loss[i] = lse[i] - X[i] . W[target[i]], lse[i] = log sum_v exp(X[i] . W[v]); 0 for rows with
     target[i] < 0."""
-    import torch
-    dt = dtype_code(dtype)
-    td, n, (V, H) = _torch_dtype(dt), target.numel(), W.shape
+    (dt, td), (_, tf), (_, ti) = _type(dtype), _type(BG_F32), _type("ids")
+    n, (V, H) = target.numel(), W.shape
     _check(load().bg_xent_fwd(dt, n, H, V, _shaped(X, "X", td, n, H), _shaped(W, "W", td, V, H),
-                              _shaped(target, "target", torch.int32, n),
-                              _shaped(loss, "loss", torch.float32, n),
-                              _shaped(lse, "lse", torch.float32, n), _dev_ptr(ws, "ws"),
+                              _shaped(target, "target", ti, n),
+                              _shaped(loss, "loss", tf, n),
+                              _shaped(lse, "lse", tf, n), _dev_ptr(ws, "ws"),
                               ws.numel() * ws.element_size(), _stream_of(stream, W)))
 
 
 def xent_bwd(dtype, X, W, target, lse, dloss, grad_dtype, dX, dW, ws, flags=0, stream=None):
     """Gradients of sum_i dloss[i] loss[i] in grad_dtype; dX or dW may be None."""
-    import torch
-    dt, gt = dtype_code(dtype), dtype_code(grad_dtype)
-    td, gd, n, (V, H) = _torch_dtype(dt), _torch_dtype(gt), target.numel(), W.shape
+    (dt, td), (gt, gd), (_, tf), (_, ti) = (_type(dtype), _type(grad_dtype), _type(BG_F32),
+                                            _type("ids"))
+    n, (V, H) = target.numel(), W.shape
     _check(load().bg_xent_bwd(dt, n, H, V, _shaped(X, "X", td, n, H), _shaped(W, "W", td, V, H),
-                              _shaped(target, "target", torch.int32, n),
-                              _shaped(lse, "lse", torch.float32, n),
-                              _shaped(dloss, "dloss", torch.float32, n), gt,
+                              _shaped(target, "target", ti, n),
+                              _shaped(lse, "lse", tf, n),
+                              _shaped(dloss, "dloss", tf, n), gt,
                               _shaped(dX, "dX", gd, n, H), _shaped(dW, "dW", gd, V, H), flags,
                               _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
                               _stream_of(stream, W)))
