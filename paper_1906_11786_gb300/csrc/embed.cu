@@ -206,7 +206,7 @@ SumPlan sum_plan(int64_t n, int H) {
   const int64_t slots = 152LL * std::min(3, 232448 / most) * p.groups;
   const int64_t waves = std::max<int64_t>(1, (n + slots * kMaxPiece - 1) / (slots * kMaxPiece));
   const int64_t piece = (n + slots * waves - 1) / (slots * waves);
-  p.piece = (int)std::min<int64_t>(kMaxPiece, std::max<int64_t>(4, (piece + 1) / 2 * 2));
+  p.piece = (int)std::min<int64_t>(kMaxPiece, std::max<int64_t>(8, (piece + 1) / 2 * 2));
   p.pieces = (n + p.piece - 1) / p.piece;
   p.blocks = (p.pieces + p.groups - 1) / p.groups;
   p.smem = kRing * 8192 + (2 * p.groups * p.piece + 4) * 4;
@@ -263,12 +263,14 @@ __global__ void __launch_bounds__(256)
   for (int i = threadIdx.x; i < s.D; i += 256) hist[(int64_t)blockIdx.x * s.D + i] = cnt[i];
 }
 
-// Stable ranks of the 256 keys of a warp (its rows of 32, in order) among its keys of equal digit; cnt
+// Stable ranks of the keys of a warp (its rows of 32, in order) among its keys of equal digit; cnt
 // [512], zero before, gets the digits' counts.  A negative key takes no part.
-__device__ __forceinline__ void warp_ranks(const int* key, int shift, int D, int* cnt, int* rank) {
+__device__ __forceinline__ void warp_ranks(const int* key, int shift, int D, int* cnt, int* rank,
+                                           int rows = 8) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
+    if (k >= rows) break;
     const int dig = key[k] < 0 ? -1 : (key[k] >> shift) & (D - 1);
     const unsigned peers = __match_any_sync(0xffffffffu, dig);
     const int lower = __popc(peers & ((1u << lane) - 1));
@@ -280,7 +282,7 @@ __device__ __forceinline__ void warp_ranks(const int* key, int shift, int D, int
   }
 }
 
-// Exclusive prefix sum over the block (256 threads) of v, sums [8] in shared memory.
+// Exclusive prefix sum over the block of v, sums [warps] in shared memory.
 __device__ __forceinline__ int block_prefix(int v, int* sums) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int run = v;
@@ -374,6 +376,102 @@ __global__ void __launch_bounds__(256)
       }
     }
     __syncthreads();
+  }
+}
+
+// All of it for at most kCluster * kClusterTile ids, in one cluster of blocks: each has a tile of the keys
+// in shared memory and writes a key to where it goes, in its own or another block's.
+constexpr int kCluster = 8, kClusterThreads = 512, kClusterTile = 4096;  // 16 warps x at most 8 x 32
+struct ClusterSort {
+  int cnt[16][512];  // per warp: counts, then first places
+  int total[512];    // of the block
+  int sums[16];
+  int key[2][kClusterTile], pos[2][kClusterTile];
+};
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address in block `rank` of the cluster of what is at p here.
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, int rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(p)), "r"(rank));
+  return a;
+}
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kClusterThreads)
+    k_sort_cluster(int n, int V, SortPlan s, const int32_t* __restrict__ ids,
+                   int32_t* __restrict__ key_out, int32_t* __restrict__ pos_out, int* status) {
+  extern __shared__ __align__(16) uint8_t sort_smem[];
+  ClusterSort& b = *reinterpret_cast<ClusterSort*>(sort_smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = blockIdx.x;
+  // rows of 32 keys a warp: the blocks' tiles are as even as that allows
+  const int per = (n + kCluster * kClusterThreads - 1) / (kCluster * kClusterThreads);
+  const int tile = per * kClusterThreads;
+  grid_dep_launch();
+  grid_dep_wait();
+  for (int p = 0; p < s.passes; ++p) {
+    const int shift = p * s.bits;
+    for (int i = tid; i < 16 * s.D; i += kClusterThreads) b.cnt[i / s.D][i % s.D] = 0;
+    __syncthreads();
+    int key[8], pos[8], order[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int at = (warp * per + k) * 32 + lane, i = rank * tile + at;
+      key[k] = -1;
+      pos[k] = i;
+      if (k >= per || i >= n) continue;
+      if (p == 0) {
+        const int id = ids[i];
+        if (id >= V && atomicCAS(status, 0, 2) == 0) atomicExch(status + 1, kSiteEmbedId);
+        key[k] = sort_key(id, V);
+      } else {
+        key[k] = b.key[p & 1][at];
+        pos[k] = b.pos[p & 1][at];
+      }
+    }
+    warp_ranks(key, shift, s.D, b.cnt[warp], order, per);
+    __syncthreads();
+    if (tid < s.D) {
+      int t = 0;
+      for (int w = 0; w < 16; ++w) t += b.cnt[w][tid];
+      b.total[tid] = t;
+    }
+    cluster_sync();
+    int before = 0, total = 0;
+    if (tid < s.D) {
+#pragma unroll
+      for (int r = 0; r < kCluster; ++r) {
+        int t;
+        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(t) : "r"(cluster_addr(&b.total[tid], r)));
+        total += t;
+        before += r < rank ? t : 0;
+      }
+    }
+    int at = block_prefix(total, b.sums) + before;
+    if (tid < s.D)
+      for (int w = 0; w < 16; ++w) {
+        const int c = b.cnt[w][tid];
+        b.cnt[w][tid] = at;
+        at += c;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (key[k] < 0) continue;
+      const int to = b.cnt[warp][(key[k] >> shift) & (s.D - 1)] + order[k];
+      if (p + 1 == s.passes) {
+        key_out[to] = key[k];
+        pos_out[to] = pos[k];
+      } else {
+        const int r = to / tile, slot = to - r * tile, buf = (p + 1) & 1;
+        asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_addr(&b.key[buf][slot], r)), "r"(key[k])
+                     : "memory");
+        asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_addr(&b.pos[buf][slot], r)), "r"(pos[k])
+                     : "memory");
+      }
+    }
+    cluster_sync();  // (also: no block leaves while another may still read its totals)
   }
 }
 
@@ -696,8 +794,15 @@ cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* 
   float* head = reinterpret_cast<float*>(base + w.head);
   float* tail = reinterpret_cast<float*>(base + w.tail);
   cudaError_t e;
-  const bool small = n <= kTile;
-  if (small)
+  // 20001 ids of 10000 tokens: 17 us in one cluster, 26 as a count and two passes of many blocks (cold)
+  const bool small = n <= kCluster * kClusterTile;
+  if (n > kTile && small) {
+    static std::atomic<uint64_t> done{0};
+    e = allow_smem(k_sort_cluster, (int)sizeof(ClusterSort), done);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(k_sort_cluster, dim3(kCluster), dim3(kClusterThreads), sizeof(ClusterSort), st, (int)n, V,
+                   s, ids, key[(s.passes - 1) & 1], pos[(s.passes - 1) & 1], status);
+  } else if (small)
     e = launch_pdl(k_sort_small, dim3(1), dim3(256), 0, st, (int)n, V, s, ids, key[(s.passes - 1) & 1],
                    pos[(s.passes - 1) & 1], status);
   else
