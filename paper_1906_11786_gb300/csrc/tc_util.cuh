@@ -55,9 +55,9 @@ __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Bounded polling.
-__device__ __forceinline__ bool mbar_poll(uint64_t* bar, uint32_t parity, int* status, int site,
-                                          volatile int* abort, uint32_t backoff_ns) {
+// Slow path of mbar_wait: bounded polling after a first failed check.
+static __device__ __noinline__ bool mbar_wait_poll(uint64_t* bar, uint32_t parity, int* status, int site,
+                                            volatile int* abort, uint32_t backoff_ns) {
   for (uint32_t i = 0; i < kSpinLimit; ++i) {
     if (mbar_try(bar, parity)) return true;
     if ((i & 1023u) == 1023u && *abort) return false;
@@ -66,12 +66,6 @@ __device__ __forceinline__ bool mbar_poll(uint64_t* bar, uint32_t parity, int* s
   if (atomicCAS(status, 0, 1) == 0) atomicExch(status + 1, site);
   *abort = 1;
   return false;
-}
-
-// Slow path of mbar_wait: polling after a first failed check.
-static __device__ __noinline__ bool mbar_wait_poll(uint64_t* bar, uint32_t parity, int* status, int site,
-                                            volatile int* abort, uint32_t backoff_ns) {
-  return mbar_poll(bar, parity, status, site, abort, backoff_ns);
 }
 
 // Waits for phase `parity` of `bar` to complete; false (and a recorded timeout) if the poll
@@ -83,13 +77,6 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, int* s
                                           volatile int* abort, uint32_t backoff_ns = 0) {
   if (mbar_try(bar, parity)) return true;
   return mbar_wait_poll(bar, parity, status, site, abort, backoff_ns);
-}
-
-// The same without a call, for kernels that move registers between warpgroups (setmaxnreg): with a
-// function call in it such a kernel cannot be allocated.
-__device__ __forceinline__ bool mbar_wait_inline(uint64_t* bar, uint32_t parity, int* status, int site,
-                                                 volatile int* abort, uint32_t backoff_ns = 0) {
-  return mbar_poll(bar, parity, status, site, abort, backoff_ns);
 }
 
 // Programmatic dependent launch.  A kernel launched with programmatic stream serialization may

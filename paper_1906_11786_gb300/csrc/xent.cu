@@ -5,11 +5,17 @@
 //
 // Three kinds of kernels:
 //   k_xent_count, k_xent_rows   the labelled rows of X, gathered side by side (rows left out cost
-//                               nothing after this and may hold anything), and the operands' 16-bit forms
-//   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, running maximum and sum
+//                               nothing after this and may hold anything), and the operands' 16-bit forms;
+//                               a few microseconds, bytes and latency
+//   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, sum of exponentials.  65537 rows x
+//                               49999: 0.88 ms at H = 256, bound by the product (tensor pipe 90% active,
+//                               0.87 ms at the measured peak); 0.63 ms at H = 64, bound by the epilogue
+//                               (exponentials: 57% of the special-function rate, issue slots 53%)
 //   k_xent_bwd (+ join)         128 x 128 tiles of z recomputed, P written back over z in tensor
-//                               memory as the A operand of the second product; once with the rows of X
-//                               staying (dX) and once with the rows of W (dW)
+//                               memory as the A operand of the second product; some CTAs with the rows
+//                               of X staying (dX), the others with the rows of W (dW).  The same shape:
+//                               3.7 ms at H = 256 for four products (3.5 at the measured peak; tensor
+//                               pipe 81%), 1.7 ms at H = 64 (epilogue: issue slots 66%)
 // A staying tile of 128 rows against one passing tile is a unit; the units of a launch, staying tile
 // by staying tile, are cut into as many equal runs as there are SMs, so one row or a hundred thousand
 // fill the card alike.  A staying tile whose units fall to several CTAs leaves partial results, which
@@ -451,6 +457,20 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// mbar_wait without a call, bounded as that is: a kernel that moves registers between warpgroups
+// (setmaxnreg) cannot be allocated with a function call in it.
+__device__ __forceinline__ bool mbar_wait_inline(uint64_t* bar, uint32_t parity, int* status, int site,
+                                                 volatile int* abort, uint32_t backoff_ns = 0) {
+  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    if (mbar_try(bar, parity)) return true;
+    if ((i & 1023u) == 1023u && *abort) return false;
+    if (backoff_ns) __nanosleep(backoff_ns);
+  }
+  if (atomicCAS(status, 0, 1) == 0) atomicExch(status + 1, site);
+  *abort = 1;
+  return false;
 }
 
 // two fp32 at a time
