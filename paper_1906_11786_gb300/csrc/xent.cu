@@ -9,7 +9,7 @@
 //                               a few microseconds, bytes and latency
 //   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, sum of exponentials.  65537 rows x
 //                               49999: 0.88 ms at H = 256, bound by the product (tensor pipe 90% active,
-//                               0.87 ms at the measured peak); 0.63 ms at H = 64, bound by the epilogue
+//                               0.87 ms at the measured peak); 0.62 ms at H = 64, bound by the epilogue
 //                               (exponentials: 57% of the special-function rate, issue slots 53%)
 //   k_xent_bwd (+ join)         128 x 128 tiles of z recomputed, P written back over z in tensor
 //                               memory as the A operand of the second product; some CTAs with the rows
@@ -473,6 +473,19 @@ __device__ __forceinline__ bool mbar_wait_inline(uint64_t* bar, uint32_t parity,
   return false;
 }
 
+// The same for whole warps, with a branch that is known to be the same for all lanes.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, int* status, int site,
+                                               volatile int* abort, uint32_t backoff_ns = 0) {
+  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+    if ((i & 1023u) == 1023u && __any_sync(0xffffffffu, *abort)) return false;
+    if (backoff_ns) __nanosleep(backoff_ns);
+  }
+  if (atomicCAS(status, 0, 1) == 0) atomicExch(status + 1, site);
+  *abort = 1;
+  return false;
+}
+
 // two fp32 at a time
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
   uint64_t r;
@@ -503,6 +516,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return r;
 }
 
+__device__ __forceinline__ uint32_t tmem_ld1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr));
+  return r;
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
@@ -649,13 +667,13 @@ __device__ __forceinline__ float sum32(const uint32_t* v, float c, float m) {
   return a + b;
 }
 
-// Largest of 64 columns.
-__device__ __forceinline__ float max64(const uint32_t* v) {
+// Largest of 32 columns.
+__device__ __forceinline__ float max32(const uint32_t* v) {
   float top[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
 #pragma unroll
-  for (int j = 4; j < 64; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(v[j]));
+  for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(v[j]));
   return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
 
@@ -786,43 +804,53 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     for (; w.more(); w.next(), ++n) {
       if (w.starts) tgt = fwd_target(a, (int64_t)w.t * 128 + r);
       const int b = n & 1;
-      if (!mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 20)) break;
+      const bool ok = mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 20);
       tc_fence_after();
-      uint32_t v[64];
-      tmem_ld32(base + b * 256, v);
-      tmem_ld32(base + b * 256 + 32, v + 32);
-      tmem_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->s_empty[b]);
       const int w0 = w.j * 256 + wg * 64, at = tgt - w0;
-      const bool here = tgt >= 0 && at >= 0 && at < 64;
-      if (__any_sync(0xffffffffu, here || w.starts || w0 + 64 > a.V)) {
-        float z = 0.f;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          if (i == at) z = __uint_as_float(v[i]);
-          if (w0 + i >= a.V) v[i] = 0xFF800000u;
-        }
-        if (here) a.hit[w.t * 128 + r] = z * (c / kLog2e);
-        if (w.starts) {
-          m = -3.0e38f;
-          l = 0.f;
-        }
+      const bool here = tgt >= 0 && at >= 0 && at < 64, check = w.starts || w0 + 64 > a.V;
+      // the targets' logits, a column at a time (a warp leaves as a whole)
+      unsigned hits = __ballot_sync(0xffffffffu, here || !ok);
+      if (hits && __any_sync(0xffffffffu, !ok)) break;
+      while (hits) {
+        const int col = __shfl_sync(0xffffffffu, at, __ffs(hits) - 1);
+        const float z = __uint_as_float(tmem_ld1(base + b * 256 + col));
+        tmem_wait_ld();
+        if (here && at == col) a.hit[w.t * 128 + r] = z * (c / kLog2e);
+        hits &= ~__ballot_sync(0xffffffffu, here && at == col);
       }
       // l = sum exp2(c z - m).  m need not be the running maximum, only near it: it is the maximum of
       // the row's first columns, and moves up when a sum passes 2^40 (so nothing overflows,
       // and what an early m made too large keeps all its bits).  This takes the maximum out of the
-      // common path.
-      float sum = INFINITY;
-      if (!w.starts) sum = sum32(v, c, m) + sum32(v + 32, c, m);
-      if (!(sum <= 0x1p40f)) {
-        const float mn = fmaxf(m, max64(v) * c);
-        l *= ex2(m - mn);
-        m = mn;
-        sum = sum32(v, c, m) + sum32(v + 32, c, m);
+      // common path.  That path has one branch, the same for the whole warp, with all that is rare behind
+      // it, and 32 columns at hand: with 64, and the targets found by comparing every column, 65537
+      // rows x 49999 took 0.64 instead of 0.62 ms at H = 64, 0.68 instead of 0.61 at H = 128.
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t v[32];
+        tmem_ld32(base + b * 256 + 32 * half, v);
+        tmem_wait_ld();
+        if (half) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->s_empty[b]);
+        }
+        float sum = sum32(v, c, m);  // (of no use, and not used, where a tile starts)
+        if (__any_sync(0xffffffffu, check || !(sum <= 0x1p40f))) {
+          const bool start = w.starts && !half;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (w0 + 32 * half + i >= a.V) v[i] = 0xFF800000u;
+          if (start) {
+            m = -3.0e38f;
+            l = 0.f;
+          }
+          const float top = start || !(sum <= 0x1p40f) ? fmaxf(m, max32(v) * c) : m;
+          l *= ex2(m - top);
+          m = top;
+          sum = sum32(v, c, m);
+        }
+        l += sum;
       }
-      l += sum;
       if (w.ends) {
         // the sum's reference is m itself, so that fwd_finish undoes exactly what was done here
         const int64_t slot = (int64_t)w.t * 128 + r;
@@ -831,7 +859,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars->q_full);
           if (wg == 0) {
-            if (!mbar_wait(&bars->q_full, finished & 1, a.status, 707, abort, 32)) break;
+            if (!__all_sync(0xffffffffu, mbar_wait(&bars->q_full, finished & 1, a.status, 707, abort, 32))) break;
             float2 p[4];
             for (int k = 0; k < 4; ++k) p[k] = a.full[k * a.cap + slot];
             const float top = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x));
@@ -930,6 +958,15 @@ struct BCfg {
   static constexpr int CW = NB / 4;                  // columns of z of a thread
   // of which it works on so many at a time: fewer where it also holds up to 64 sums
   static constexpr int PW = KEEP && HC > 2 ? 16 : CW;
+  // The epilogue keeps what targets cost in a path of its own (APART), and waits with a branch that is
+  // known to be the same for the whole warp (UNIFORM).  us of dX and dW, without either -> with both: 65537 x
+  // 49999 with fp32 gradients, H = 64 2700 -> 2605, H = 128 3320 -> 3270; fp32 inputs, 20000 x 32000 at
+  // H = 128 1204 -> 1140; bf16 gradients, H = 256 3950 -> 3910.  With bf16 gradients the path apart takes
+  // back at H = 64 what the branch gains (1690 -> 1550 with the branch alone, 1686 with both).  At H = 128,
+  // where the two products take the tensor cores as long as each other and the epilogue is not what is
+  // waited for, either costs (1970 -> 2120).
+  static constexpr bool APART = KEEP || HC > 2;
+  static constexpr bool UNIFORM = KEEP || HC != 2;
   static constexpr int S_BYTES = T * HC * 16384;
   static constexpr int BOX = NB * 128;  // 64 elements of each passing row
   static constexpr int B_BYTES = T * HC * BOX;
@@ -963,9 +1000,21 @@ struct Turn {
   }
 };
 
+// Targets among a warp's values, and columns past the vocabulary, take extra work.  Whether there are any is
+// asked within the one path (kEither), or first, for a path without (kUsual) and one with that work
+// (kRare): see BCfg::APART.
+enum { kEither, kUsual, kRare };
+
+// Whether a passing row of X has its target among the 32 staying rows of W from `first`: the whole warp's
+// answer from a row a lane.
+__device__ __forceinline__ bool hit_row(const float* stat, int i, int first) {
+  const int at = __float_as_int(stat[kTgt + i]) - first;
+  return __any_sync(0xffffffffu, at >= 0 && at < 32);
+}
+
 // P of N columns of a row (a thread's) from their logits, for dX: nlse = -lse of the row, hit = its
 // target's place among the columns, of which the first `valid` exist.
-template <int FORM, int N>
+template <int FORM, int N, int PATH>
 __device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, float nlse, int hit,
                                           int valid) {
   const uint64_t l2e = pack2(kLog2e, kLog2e), ds = pack2(descale, descale), up2 = pack2(up, up);
@@ -979,7 +1028,7 @@ __device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, 
     v[i] = __float_as_uint(ex2(a));
     v[i + 1] = __float_as_uint(ex2(b));
   }
-  if (__any_sync(0xffffffffu, (hit >= 0 && hit < N) || valid < N)) {
+  if (PATH == kRare || (PATH == kEither && __any_sync(0xffffffffu, (hit >= 0 && hit < N) || valid < N))) {
     const float one = FORM == kBf16 ? 1.f : 32768.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -995,13 +1044,12 @@ __device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, 
 // dX kernel at H = 64).  So tensor memory is read in fragments in which a thread has two neighbouring
 // columns of every 8, in rows l / 4, + 8, + 16, + 24 of its warp's 32 (l = lane): a quarter of the
 // loads.  v[16 h + 4 g + 2 a + b]: row 16 h + 8 a + l / 4, column 8 g + 2 (l % 4) + b.
-template <int FORM, int N>
+template <int FORM, int N, int PATH>
 __device__ __forceinline__ void probs_col(uint32_t* v, float descale, float up, const float* stat,
-                                          int first, int mine) {
+                                          int mine) {
   const uint64_t l2e = pack2(kLog2e, kLog2e), ds = pack2(descale, descale), up2 = pack2(up, up);
   const int lane = threadIdx.x & 31, c = 2 * (lane & 3);
-  const int at = __float_as_int(stat[kTgt + (lane & (N - 1))]) - first;
-  const bool hits = __any_sync(0xffffffffu, at >= 0 && at < 128);
+  const bool hits = PATH == kEither && hit_row(stat, lane & (N - 1), mine - lane / 4);
 #pragma unroll
   for (int g = 0; g < N / 8; ++g) {
     const uint64_t nl = *reinterpret_cast<const uint64_t*>(stat + kNlse + 8 * g + c);
@@ -1018,7 +1066,7 @@ __device__ __forceinline__ void probs_col(uint32_t* v, float descale, float up, 
       p[1] = __float_as_uint(b);
     }
   }
-  if (hits) {
+  if (PATH == kRare || (PATH == kEither && hits)) {
     // all columns, without branches (skipping groups of 8 without a hit took longer)
     const float upg = FORM == kBf16 ? -1.f : -ex2(up);
 #pragma unroll
@@ -1054,6 +1102,58 @@ __device__ __forceinline__ void terms(uint32_t a, uint32_t b, uint32_t& hi, uint
   }
 }
 
+// A warp's part of a unit: P over z in tensor memory (columns from `at`).
+template <int HC, int FORM, bool DW, int PATH>
+__device__ __forceinline__ void z_to_p(uint32_t at, float descale, float up, const float* stat, int mine,
+                                       float nlse, int hit, int valid) {
+  using C = BCfg<HC, FORM>;
+  constexpr int N = PATH == kRare ? 16 : C::PW;  // (short: its time matters little)
+#pragma unroll(PATH == kRare ? 1 : 16)
+  for (int pc = 0; pc < C::CW; pc += N) {
+    uint32_t v[N];
+    if (DW) {
+      // (N / 2 registers for each half of the warp's rows)
+      if (N == 32) {
+        tmem_ld_frag32(at + pc, v);
+        tmem_ld_frag32(at + pc + (16u << 16), v + 16);
+      } else {
+        tmem_ld_frag16(at + pc, v);
+        tmem_ld_frag16(at + pc + (16u << 16), v + 8);
+      }
+      tmem_wait_ld();
+      probs_col<FORM, N, PATH>(v, descale, up, stat + pc, mine);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < N; c += 16) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t* p = v + h * (N / 2) + c / 2 + 2 * i;
+            terms<FORM>(p[0], p[1], hi[i], lo[i]);
+          }
+          tmem_st_frag8(at + pc + (h * 16u << 16) + c, hi);
+          if (FORM != kBf16) tmem_st_frag8(at + pc + (h * 16u << 16) + c + 8, lo);
+        }
+    } else {
+      if (N == 32)
+        tmem_ld32(at + pc, v);
+      else
+        tmem_ld16(at + pc, v);
+      tmem_wait_ld();
+      probs_row<FORM, N, PATH>(v, descale, up, nlse, hit - pc, valid - pc);
+#pragma unroll
+      for (int c = 0; c < N; c += 16) {
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) terms<FORM>(v[c + 2 * i], v[c + 2 * i + 1], hi[i], lo[i]);
+        tmem_st8(at + pc + c, hi);
+        if (FORM != kBf16) tmem_st8(at + pc + c + 8, lo);
+      }
+    }
+  }
+}
+
 // The epilogue warps of k_xent_bwd: P from z, and G to its destination.
 template <int HC, int FORM, bool DW>
 __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, int cta, uint32_t tmem,
@@ -1080,9 +1180,13 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
   bool fresh = true, pending = false, ok = true;
   float nlse = 0.f;
   int tgt = -1, first = 0;
+  auto wait = [&](uint64_t* bar, uint32_t parity, int site, uint32_t backoff_ns) {
+    return C::UNIFORM ? mbar_wait_warp(bar, parity, a.status, site, abort, backoff_ns)
+                      : __all_sync(0xffffffffu, mbar_wait_inline(bar, parity, a.status, site, abort, backoff_ns)) != 0;
+  };
   // takes the finished group of G: adds it to the registers
   auto collect = [&]() {
-    if (!mbar_wait_inline(&bars->g_full, groups & 1, a.status, 717, abort, 32)) return false;
+    if (!wait(&bars->g_full, groups & 1, 717, 32)) return false;
     ++groups;
     tc_fence_after();
     if (C::KEEP) {
@@ -1110,57 +1214,20 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       nlse = st[kNlse];
       tgt = __float_as_int(st[kTgt]);
     }
-    ok = mbar_wait_inline(&bars->z_full[b.i], b.parity, a.status, 718, abort, 20);
+    ok = wait(&bars->z_full[b.i], b.parity, 718, 20);
     if (!ok) break;
     tc_fence_after();
-#pragma unroll
-    for (int pc = 0; pc < C::CW; pc += C::PW) {
-      const uint32_t at = zbuf + quarter + b.i * C::NB + c0 + pc;
-      uint32_t v[C::PW];
-      const int w0 = w.j * C::NB + c0 + pc;
-      if (DW) {
-        // (PW / 2 registers for each half of the warp's rows)
-        if (C::PW == 32) {
-          tmem_ld_frag32(at, v);
-          tmem_ld_frag32(at + (16u << 16), v + 16);
-        } else {
-          tmem_ld_frag16(at, v);
-          tmem_ld_frag16(at + (16u << 16), v + 8);
-        }
-        tmem_wait_ld();
-        probs_col<FORM, C::PW>(v, descale, (float)up,
-                               reinterpret_cast<const float*>(stats + s.i * 2048) + stat_at(c0 + pc),
-                               first, first + q * 32 + lane / 4);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int c = 0; c < C::PW; c += 16) {
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t* p = v + h * (C::PW / 2) + c / 2 + 2 * i;
-              terms<FORM>(p[0], p[1], hi[i], lo[i]);
-            }
-            tmem_st_frag8(at + (h * 16u << 16) + c, hi);
-            if (FORM != kBf16) tmem_st_frag8(at + (h * 16u << 16) + c + 8, lo);
-          }
-      } else {
-        if (C::PW == 32)
-          tmem_ld32(at, v);
-        else
-          tmem_ld16(at, v);
-        tmem_wait_ld();
-        probs_row<FORM, C::PW>(v, descale, (float)up, nlse, tgt < 0 ? -1 : tgt - w0, a.V - w0);
-#pragma unroll
-        for (int c = 0; c < C::PW; c += 16) {
-          uint32_t hi[8], lo[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) terms<FORM>(v[c + 2 * i], v[c + 2 * i + 1], hi[i], lo[i]);
-          tmem_st8(at + c, hi);
-          if (FORM != kBf16) tmem_st8(at + c + 8, lo);
-        }
-      }
-    }
+    const uint32_t at = zbuf + quarter + b.i * C::NB + c0;
+    const float* st = reinterpret_cast<const float*>(stats + s.i * 2048) + stat_at(c0);
+    const int w0 = w.j * C::NB + c0, hit = tgt < 0 ? -1 : tgt - w0, mine = first + q * 32 + lane / 4;
+    bool rare = true;
+    if (C::APART)
+      rare = DW ? hit_row(st, lane & (C::CW - 1), first + q * 32)
+                : __any_sync(0xffffffffu, (hit >= 0 && hit < C::CW) || w0 + C::CW > a.V);
+    if (rare)
+      z_to_p<HC, FORM, DW, C::APART ? kRare : kEither>(at, descale, (float)up, st, mine, nlse, hit, a.V - w0);
+    else
+      z_to_p<HC, FORM, DW, kUsual>(at, descale, (float)up, st, mine, nlse, hit, a.V - w0);
     tmem_wait_st();
     tc_fence_before();
     __syncwarp();
@@ -1355,14 +1422,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       }
       ok = ok && mbar_wait_inline(&bars->z_empty[b.i], b.parity ^ 1, a.status, 719, abort);
       ok = ok && mbar_wait_inline(&bars->full[s.i], s.parity, a.status, 716, abort);
-      if (!ok) break;
       tc_fence_after();
       const uint64_t B = R + s.i * (C::B_BYTES >> 4);
       const uint32_t d = zbuf + b.i * C::NB;
       // past H both operands hold zeros; two terms: low x high and high x low first, while the
       // accumulator is small
       constexpr int n = C::T == 2 ? 3 : 1;
-      if (leader) {
+      if (leader && ok) {
 #pragma unroll
         for (int pr = 0; pr < n; ++pr) {
           const uint64_t as = S + (n == 3 && pr == 0 ? HC * (16384 >> 4) : 0);
@@ -1375,7 +1441,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         tc_commit(&bars->z_full[b.i]);
         if (w.ends) tc_commit(&bars->s_empty);
       }
-      __syncwarp();
+      ok = __all_sync(0xffffffffu, ok);  // (as a whole)
     }
     if (leader) tc_commit(&bars->drain_z);
     __syncwarp();
@@ -1397,13 +1463,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       ok = mbar_wait_inline(&bars->p_full[b.i], b.parity, a.status, 713, abort);
       if (ok && in_group == 0 && groups > 0)
         ok = mbar_wait_inline(&bars->g_empty, (groups - 1) & 1, a.status, 714, abort);
-      if (!ok) break;
       tc_fence_after();
       const uint64_t B = R + s.i * (C::B_BYTES >> 4);
       const uint32_t p = zbuf + b.i * C::NB;
       constexpr int n = C::T == 2 ? 3 : C::PT;
       const bool close = ++in_group == C::DRAIN || w.ends;
-      if (leader) {
+      if (leader && ok) {
 #pragma unroll
         for (int pr = 0; pr < n; ++pr) {
           // 16 columns of z hold 16 of P: 8 columns of the high terms, 8 of the low ones
@@ -1422,7 +1487,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         ++groups;
         in_group = 0;
       }
-      __syncwarp();
+      ok = __all_sync(0xffffffffu, ok);  // (as a whole)
     }
     if (leader) tc_commit(&bars->drain_g);
     __syncwarp();
