@@ -8,14 +8,14 @@
 //                               nothing after this and may hold anything), and the operands' 16-bit forms;
 //                               a few microseconds, bytes and latency
 //   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, sum of exponentials.  65537 rows x
-//                               49999: 0.88 ms at H = 256, bound by the product (tensor pipe 90% active,
+//                               49999: 0.87 ms at H = 256, bound by the product (tensor pipe 92% active,
 //                               0.87 ms at the measured peak); 0.62 ms at H = 64, bound by the epilogue
-//                               (exponentials: 57% of the special-function rate, issue slots 53%)
+//                               (exponentials: 59% of the special-function rate, issue slots 52%)
 //   k_xent_bwd (+ join)         128 x 128 tiles of z recomputed, P written back over z in tensor
 //                               memory as the A operand of the second product; some CTAs with the rows
 //                               of X staying (dX), the others with the rows of W (dW).  The same shape:
 //                               3.7 ms at H = 256 for four products (3.5 at the measured peak; tensor
-//                               pipe 81%), 1.7 ms at H = 64 (epilogue: issue slots 66%)
+//                               pipe 80%), 1.55 ms at H = 64 (epilogue: issue slots 68%)
 // A staying tile of 128 rows against one passing tile is a unit; the units of a launch, staying tile
 // by staying tile, are cut into as many equal runs as there are SMs, so one row or a hundred thousand
 // fill the card alike.  A staying tile whose units fall to several CTAs leaves partial results, which
