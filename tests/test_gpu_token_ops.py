@@ -338,6 +338,46 @@ def test_xent_of_confident_and_of_wrong_rows(dtype, grad):
         within(host(t), w, b)
 
 
+def check_bounds(dtype, grad, X, W, target, g):
+    n, (V, H) = target.size, W.shape
+    got = run_xent(dtype, X, W, target, g, grad)
+    r = ref.xent(host(X), host(W), target, g)
+    loss, bX, bW = xent_bounds(r, n, H, V, grad)
+    for t, w, b in zip(got, (r["loss"], r["lse"], r["dX"], r["dW"]), (loss, loss, bX, bW)):
+        within(host(t), w, b)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+@pytest.mark.parametrize("H", [64, 128, 192, 256])
+def test_xent_targets_at_every_place_of_a_tile(dtype, grad, H):
+    """Each token the target of a row or two, then one token (at the edges of what a warp, a tile and the
+    vocabulary hold) the target of all rows, and of a few in each 32."""
+    n, V = 645, 517
+    X, W, target, g = xent_inputs(n, H, V, dtype)
+    check_bounds(dtype, grad, X, W, (np.arange(n) % V).astype(np.int32), g)
+    for token in (0, 31, 32, 63, 64, 127, 128, 255, 256, 511, V - 1):
+        target[:] = token
+        check_bounds(dtype, grad, X, W, target, g)
+    target = np.where(np.arange(n) % 13 == 0, 300, np.arange(n) % 7).astype(np.int32)
+    check_bounds(dtype, grad, X, W, target, g)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_xent_of_logits_that_rise_or_fall_along_the_vocabulary(dtype, grad, sign):
+    """Logits run over hundreds from the first token to the last: a running sum's reference has to move,
+    or what comes later vanishes against it."""
+    n, H, V = 140, 64, 1500
+    rng = np.random.default_rng(11)
+    W = rng.standard_normal((V, H)) * 0.05
+    W[:, 0] = sign * np.linspace(-150.0, 150.0, V)
+    X = rng.standard_normal((n, H)) * 0.1
+    X[:, 0] = np.linspace(0.1, 2.0, n)
+    target = rng.integers(0, V, n).astype(np.int32)
+    g = (0.5 + rng.random(n)).astype(np.float32) / n
+    check_bounds(dtype, grad, dev(X, dtype), dev(W, dtype), target, g)
+
+
 @pytest.mark.parametrize("dtype,grad", TYPES)
 def test_xent_rows_left_out_may_hold_anything(dtype, grad):
     X, W, target, g = xent_inputs(333, 96, 210, dtype, 0.4)
