@@ -40,6 +40,10 @@ struct XentArgs {
   int* status;
 };
 size_t xent_ws_bytes(int bf16, int64_t n, int H, int V, int backward);
+// CTAs of a tile kernel on a device of so many SMs, and the workspace that a call takes there: never more
+// than xent_ws_bytes.
+int xent_ctas(int sms);
+size_t xent_ws_used(int bf16, int64_t n, int H, int V, int backward, int grad_bf16, int sms);
 cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st);
 // Gradients in the type grad_bf16 says; dX or dW may be NULL.
 cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, int grad_bf16,

@@ -58,6 +58,9 @@ enum Form { kBf16 = 0, kF16x1 = 1, kF16x2 = 2 };
 // ------------------------------------------------------------------------------ workspace
 inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// CTAs of a tile kernel at most: one on each SM of a GB300.  The workspace has partial results for so many,
+// whatever device a call runs on.
+constexpr int kMaxCtas = 152;
 constexpr int kMaxRowBlocks = 2048;
 constexpr int kTableBlocks = 608;  // at most, of the table's amax and conversion
 constexpr int64_t kDirectRows = 32768;
@@ -1579,7 +1582,7 @@ __global__ void __launch_bounds__(256)
 
 // ------------------------------------------------------------------------------ host
 struct Call {
-  int form, H, V, sms;
+  int form, H, V, ctas;
   int64_t n;
   Ws w;
   char* base;
@@ -1648,7 +1651,7 @@ cudaError_t run_fwd(const Call& c, const XentArgs& x, const FwdArgs& f) {
   static std::atomic<uint64_t> done{0};
   cudaError_t e = allow_smem(k_xent_fwd<HC, T>, C::SMEM, done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(k_xent_fwd<HC, T>, dim3(c.sms), dim3(kFwdThreads), C::SMEM, c.st, mx, mw, f);
+  return launch_pdl(k_xent_fwd<HC, T>, dim3(c.ctas), dim3(kFwdThreads), C::SMEM, c.st, mx, mw, f);
 }
 
 template <int HC, int FORM>
@@ -1662,12 +1665,12 @@ cudaError_t run_bwd(const Call& c, const void* W, const BwdArgs& b) {
   static std::atomic<uint64_t> done{0};
   cudaError_t e = allow_smem(k_xent_bwd<HC, FORM>, C::SMEM, done);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(k_xent_bwd<HC, FORM>, dim3(c.sms), dim3(kBwdThreads), C::SMEM, c.st, xs, xp, ws, wp,
+  e = launch_pdl(k_xent_bwd<HC, FORM>, dim3(c.ctas), dim3(kBwdThreads), C::SMEM, c.st, xs, xp, ws, wp,
                  b);
   if (e != cudaSuccess) return e;
   note_launch();
   if (b.tiles) return cudaSuccess;
-  e = launch_pdl(k_xent_bwd_join, dim3(c.sms, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM, C::NB);
+  e = launch_pdl(k_xent_bwd_join, dim3(c.ctas, c.H / 32 * 4), dim3(256), 0, c.st, b, FORM, C::NB);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
@@ -1683,30 +1686,58 @@ cudaError_t run_bwd_h(const Call& c, const void* W, const BwdArgs& b) {
   }
 }
 
-Call make_call(const XentArgs& a, int form, int backward, cudaStream_t st) {
-  Call c;
+int form_of(int bf16, int backward, int grad_bf16) {
+  return !bf16 ? kF16x2 : backward && !grad_bf16 ? kF16x1 : kBf16;
+}
+
+// SMs of the current device (asked once a device; the calls may come from several threads).
+cudaError_t device_sms(int* sms) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  *sms = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (*sms > 0) return cudaSuccess;
+  e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess && dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
+  return e;
+}
+
+cudaError_t make_call(const XentArgs& a, int form, int backward, cudaStream_t st, Call* call) {
+  Call& c = *call;
+  int sms = 0;
+  const cudaError_t e = device_sms(&sms);
+  if (e != cudaSuccess) return e;
   c.form = form;
   c.H = a.H;
   c.V = a.V;
   c.n = a.n;
-  c.sms = gemm_tn_num_sms();
-  c.w = layout(form, a.n, a.H, a.V, backward, c.sms);
+  c.ctas = xent_ctas(sms);
+  c.w = layout(form, a.n, a.H, a.V, backward, c.ctas);
   c.base = static_cast<char*>(a.ws);
   c.st = st;
-  return c;
+  return cudaSuccess;
 }
 
 }  // namespace
 
+// At least 2: a backward call that computes dX and dW has CTAs for each (none waits for another, so that
+// they need not run at the same time).
+int xent_ctas(int sms) { return std::max(2, std::min(sms, kMaxCtas)); }
+
 size_t xent_ws_bytes(int bf16, int64_t n, int H, int V, int backward) {
-  constexpr int kSms = 152;
-  if (!bf16) return layout(kF16x2, n, H, V, backward, kSms).total;
-  return layout(backward ? kF16x1 : kBf16, n, H, V, backward, kSms).total;
+  return layout(form_of(bf16, backward, 0), n, H, V, backward, kMaxCtas).total;
+}
+
+size_t xent_ws_used(int bf16, int64_t n, int H, int V, int backward, int grad_bf16, int sms) {
+  return layout(form_of(bf16, backward, grad_bf16), n, H, V, backward, xent_ctas(sms)).total;
 }
 
 cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st) {
   if (a.n == 0) return cudaSuccess;
-  Call c = make_call(a, a.bf16 ? kBf16 : kF16x2, 0, st);
+  Call c;
+  cudaError_t e = make_call(a, form_of(a.bf16, 0, 0), 0, st, &c);
+  if (e != cudaSuccess) return e;
   FwdArgs f{};
   f.H = a.H;
   f.V = a.V;
@@ -1726,9 +1757,8 @@ cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st
   // A row's logits depend on no other row, so bf16 rows need no gathering to be right; up to two units
   // a CTA it would only take longer (one row against 32000 x 128: 17 us with it, 13 without).
   const int64_t ct = ((int64_t)a.V + 255) / 256, units = c.w.cap / 128 * ct;
-  f.direct = a.bf16 && units <= 2 * c.sms;
+  f.direct = a.bf16 && units <= 2 * c.ctas;
   f.tiles = ct <= kWholeUnits;
-  cudaError_t e;
   if (!f.direct) {
     RowArgs r{};
     r.loss = loss;
@@ -1749,7 +1779,7 @@ cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st
   if (e != cudaSuccess) return e;
   note_launch();
   if (f.tiles) return cudaSuccess;
-  e = launch_pdl(k_xent_join, dim3(c.sms, 16), dim3(256), 0, st, f);
+  e = launch_pdl(k_xent_join, dim3(c.ctas, 16), dim3(256), 0, st, f);
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
@@ -1761,8 +1791,10 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
     if (!dW || accumulate) return cudaSuccess;
     return cudaMemsetAsync(dW, 0, (size_t)a.V * a.H * (grad_bf16 ? 2 : 4), st);
   }
-  const int form = grad_bf16 ? kBf16 : a.bf16 ? kF16x1 : kF16x2;
-  Call c = make_call(a, form, 1, st);
+  const int form = form_of(a.bf16, 1, grad_bf16);
+  Call c;
+  cudaError_t e = make_call(a, form, 1, st, &c);
+  if (e != cudaSuccess) return e;
   RowArgs r{};
   r.backward = 1;
   r.grad_bf16 = grad_bf16;
@@ -1770,7 +1802,7 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
   r.lse_in = lse;
   r.dloss = dloss;
   r.dX = dX;
-  cudaError_t e = prepare(a, c, r);
+  e = prepare(a, c, r);
   if (e != cudaSuccess) return e;
   BwdArgs b{};
   b.H = a.H;
@@ -1783,7 +1815,7 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
   b.status = a.status;
   b.out_bf16 = grad_bf16;
   // a unit of dW takes 2-20% longer (column statistics, frequent tokens): 72 of 152 CTAs for dX
-  b.split = !dW ? c.sms : !dX ? 0 : c.sms * 9 / 19;
+  b.split = !dW ? c.ctas : !dX ? 0 : std::max(1, c.ctas * 9 / 19);
   b.tiles = (!dX || a.V <= kWholeUnits * 128) && (!dW || a.n <= kWholeUnits * 128);
   const int tiles = (int)(c.w.vcap / 128);
   b.step = std::max(1, (int)(tiles * 0.618));

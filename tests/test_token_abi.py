@@ -150,3 +150,22 @@ def test_register_shares_add_up_to_the_launch():
     assert len(dec) == len(inc) == 1
     assert "kBwdThreads = 640" in src
     assert 128 * int(dec.pop()) + 512 * int(inc.pop()) <= 640 * 96
+
+
+def test_the_workspace_holds_what_a_call_takes_on_any_device(lib):
+    """The cross entropy's kernels keep partial results for each of their CTAs, as many as the device has
+    SMs: never more of them than the reported size has room for, and CTAs for both gradients even on a
+    single SM."""
+    import ctypes
+    ctas, used = lib["_ZN2bg9xent_ctasEi"], lib["_ZN2bg12xent_ws_usedEiliiiii"]
+    used.restype = ctypes.c_size_t
+    used.argtypes = [ctypes.c_int, ctypes.c_int64] + [ctypes.c_int] * 5
+    assert ctas(152) == 152
+    for sms in (1, 2, 3, 18, 148, 152, 153, 160, 304, 1000):
+        assert 2 <= ctas(sms) <= max(2, sms)
+        for dt in (L.BG_F32, L.BG_BF16):
+            for n, H, V in ((1, 32, 1), (700, 256, 5000), (100001, 96, 777)):
+                for op, backward in ((L.BG_OP_XENT_FWD, 0), (L.BG_OP_XENT_BWD, 1)):
+                    for grad_bf16 in (0, 1) if dt == L.BG_BF16 else (0,):
+                        assert used(dt, n, H, V, backward, grad_bf16, sms) <= \
+                            lib.bg_xent_workspace_bytes(dt, n, H, V, op)
