@@ -29,9 +29,13 @@
 //                  fp16 and bf16 operands cannot be mixed in one product
 //   fp16, 2 terms  fp32 X and W, each the sum of two fp16 terms (22 bits); products of the two low
 //                  terms (2^-22) are left out
-// The tensor core truncates when it adds to its fp32 accumulator (measured: 0.2-0.45 x 2^-24 of the
-// accumulator lost per 16-element step), so a gradient in fp32 leaves tensor memory every kDrainSteps
-// steps and is added up in registers.
+// The tensor core truncates when it adds to its fp32 accumulator.  Measured: a step of 16 products loses
+// 0.2-0.45 x 2^-24 of the accumulator where signs are mixed, 3.4 x 2^-24 where all are of one sign, always
+// towards zero, so that a sum of N steps of one sign ends up 1.7 N x 2^-24 low.  A gradient in fp32 leaves
+// tensor memory every kDrainSteps steps and is added up in registers (low by 2^-18 at most: 2.8e-6
+// measured); one in bf16 leaves it every kLongSteps steps and is added up in the CTA's partial result
+// (2^-12, an eighth of bf16's half gap; 65537 rows x 49999: 2% longer at H = 256 than without, no difference
+// at H <= 192; 1024 steps took 5%).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -51,7 +55,7 @@ using namespace tc;
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kDrainSteps = 64;
+constexpr int kDrainSteps = 64, kLongSteps = 2048;
 
 enum Form { kBf16 = 0, kF16x1 = 1, kF16x2 = 2 };
 
@@ -941,9 +945,13 @@ struct BwdArgs {
   const float* stat;
   void* dX;
   void* dW;
-  float* part;  // [G][2][128][H]
+  float* part;  // [G][2][128 x H], see part_at
   int* status;
 };
+
+// Place of columns c .. c + 3 (c a multiple of 4) of row r in a partial result: a warp, a lane a row,
+// reads and writes 512 bytes in a row.
+__device__ __forceinline__ int part_at(int r, int c) { return c * 128 + r * 4; }
 
 // One unit: z = S B^T (S the staying tile, B the passing one), P from z, G += P B.  B serves both
 // products: as its rows lie (K-major) in the first, transposed (MN-major) in the second.
@@ -981,7 +989,7 @@ struct BCfg {
   static constexpr int ZROOM = (512 - GCOLS) / NB;
   static constexpr int ZB = ZROOM < 4 ? ZROOM : 4;   // units' z in tensor memory
   static constexpr int STEPS = NB / 16 * (T == 2 ? 3 : PT);  // accumulating steps of a unit
-  static constexpr int DRAIN = KEEP ? kDrainSteps / STEPS : 1 << 30;  // units before G leaves TMEM
+  static constexpr int DRAIN = (KEEP ? kDrainSteps : kLongSteps) / STEPS;  // units before G leaves TMEM
   static_assert(ST >= 1 && SMEM <= 232448, "shared memory");
   static_assert(ZB >= 2, "tensor memory");
   static_assert(DRAIN >= 1, "drain interval");
@@ -1157,6 +1165,18 @@ __device__ __forceinline__ void z_to_p(uint32_t at, float descale, float up, con
   }
 }
 
+// v += the 16 columns of a row of a partial result that begin at p.
+__device__ __forceinline__ void add16(const float* p, uint32_t* v) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(p + part_at(0, i));
+    v[i] = __float_as_uint(__uint_as_float(v[i]) + x.x);
+    v[i + 1] = __float_as_uint(__uint_as_float(v[i + 1]) + x.y);
+    v[i + 2] = __float_as_uint(__uint_as_float(v[i + 2]) + x.z);
+    v[i + 3] = __float_as_uint(__uint_as_float(v[i + 3]) + x.w);
+  }
+}
+
 // The epilogue warps of k_xent_bwd: P from z, and G to its destination.
 template <int HC, int FORM, bool DW>
 __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, int cta, uint32_t tmem,
@@ -1180,7 +1200,7 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
   int in_group = 0;
   Turn<C::ST> s;
   Turn<C::ZB> b;
-  bool fresh = true, pending = false, ok = true;
+  bool fresh = true, pending = false, spilled = false, ok = true;
   float nlse = 0.f;
   int tgt = -1, first = 0;
   auto wait = [&](uint64_t* bar, uint32_t parity, int site, uint32_t backoff_ns) {
@@ -1240,16 +1260,18 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       pending = false;
       if (!ok) break;
     }
-    if (++in_group == C::DRAIN || w.ends) {
+    const bool close = ++in_group == C::DRAIN || w.ends;
+    if (close) {
       in_group = 0;
-      pending = !w.ends;
+      pending = C::KEEP && !w.ends;
     }
-    if (!w.ends) continue;
+    if (!(C::KEEP ? w.ends : close)) continue;
     ok = collect();
     if (!ok) break;
     fresh = true;
-    // the tile's result: finished where this CTA had all its units, else for the join
-    const bool whole = un.whole(cta, w.t);
+    // the tile's result: finished where this CTA had all its units, else for the join; of a long sum, what
+    // there is of it so far goes to the same place as what is left to the join, and is added there
+    const bool whole = w.ends && un.whole(cta, w.t);
     int64_t orow = (DW ? first : w.t * 128) + r;
     float s1 = 1.f, s2 = 1.f, s3 = 1.f;
     if (DW) {
@@ -1260,8 +1282,8 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       orow = a.row[orow];
       if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-sw);
     }
-    float* pt = a.part + (((int64_t)blockIdx.x * 2 + un.slot(cta, w.t)) * 128 + r) * a.H;
-#pragma unroll
+    float* pt = a.part + ((int64_t)blockIdx.x * 2 + un.slot(cta, w.t)) * 128 * a.H;
+#pragma unroll(C::KEEP ? 4 : 1)
     for (int c = 0; c < GQ; c += 16) {
       const int col = wg * GQ + c;
       uint32_t v[16];
@@ -1271,13 +1293,14 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       } else if (col < a.H) {
         tmem_ld16(tmem + quarter + col, v);
         tmem_wait_ld();
+        if (spilled) add16(pt + part_at(r, col), v);
       }
       if (col >= a.H) continue;
       float* x = reinterpret_cast<float*>(v);
       if (!whole) {
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<float4*>(pt + col + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          *reinterpret_cast<float4*>(pt + part_at(r, col + i)) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
         continue;
       }
       if (orow < 0) continue;
@@ -1306,6 +1329,7 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       }
     }
     if (!C::KEEP) {
+      spilled = !w.ends;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->g_empty);
@@ -1537,12 +1561,12 @@ __global__ void __launch_bounds__(256)
   if (begin == first) return;
   const int64_t prev = un.begin(c - 1);
   if (prev > first) return;  // an earlier CTA begins inside the tile too
-  const int hb = a.H / 32, col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x & 7) * 4;
-  const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x >> 3);
+  const int hb = a.H / 32, col = (int)(blockIdx.y % hb) * 32 + (threadIdx.x >> 5) * 4;
+  const int r = (int)(blockIdx.y / hb) * 32 + (threadIdx.x & 31);
   // CTA c - 1 has the first part (in its second place unless the tile is its first), the others begin
   // with this tile
   const int64_t stride = 128LL * a.H;
-  const float* part = a.part + (int64_t)(blockIdx.x - c) * 2 * stride + (int64_t)r * a.H + col;
+  const float* part = a.part + (int64_t)(blockIdx.x - c) * 2 * stride + part_at(r, col);
   const float* head = part + ((int64_t)(c - 1) * 2 + (un.tile_of(prev) == t ? 0 : 1)) * stride;
   float4 x = *reinterpret_cast<const float4*>(head);
   const int last = un.last_before(end);

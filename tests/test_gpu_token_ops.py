@@ -513,6 +513,48 @@ def test_xent_past_32_bits_of_elements():
     assert torch.count_nonzero(dX) == 0
 
 
+@pytest.mark.parametrize("which", ["dX", "dW"])
+def test_xent_bf16_gradients_of_long_sums(which):
+    """Millions of terms of one sign to an element.  The tensor core drops what does not fit its fp32
+    accumulator, all in one direction: left there, sums like these are 4% low.  They have to leave it long
+    before that.
+
+    All logits are 0, so that every probability is 1 / V, and V is such that 1 / V is within 2^-16 of a
+    bf16 number p: an element is p times a column's sum.  Rounding the result to bf16 is off by up to 2^-8
+    either way; over 256 columns of random size the mean of that is below 6 x 2^-8 / sqrt(3 x 256).  2^-13
+    on top is left for what is lost before a sum leaves the accumulator."""
+    H = 256
+    rows, V = (19456, 8421505) if which == "dX" else (1 << 23, 16448)
+    many = V if which == "dX" else rows  # the side that is summed over
+    p = float(torch.tensor(1.0 / V).to(torch.bfloat16).double())
+    assert abs(p * V - 1) < 2.0 ** -15
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    size = 1 + torch.rand(H, generator=gen, device="cuda")
+    side = torch.empty(many, H, device="cuda", dtype=torch.bfloat16)
+    total = torch.zeros(H, device="cuda", dtype=torch.float64)
+    for piece in side.split(1 << 20):
+        piece.copy_((1 + torch.rand(piece.shape, generator=gen, device="cuda")) * size)
+    side[0] = 0  # (the target's row of W)
+    for piece in side.split(1 << 20):
+        total += piece.double().sum(0)
+    none = torch.zeros(rows if which == "dX" else V, H, device="cuda", dtype=torch.bfloat16)
+    X, W = (none, side) if which == "dX" else (side, none)
+    target = torch.zeros(rows, device="cuda", dtype=torch.int32)
+    lse = torch.full((rows,), float(np.log(V)), device="cuda")
+    g = torch.ones(rows, device="cuda")
+    out = torch.full_like(none, float("nan"))
+    ws = torch.empty(L.xent_workspace_bytes("bf16", rows, H, V, L.BG_OP_XENT_BWD), device="cuda",
+                     dtype=torch.uint8)
+    dX, dW = (out, None) if which == "dX" else (None, out)
+    L.xent_bwd("bf16", X, W, target, lse, g, "bf16", dX, dW, ws)
+    L.check_device()
+    want = host(total) * p
+    for at in (1, len(out) // 2, len(out) - 1):
+        off = host(out[at]) / want - 1
+        assert np.abs(off).max() < 2.0 ** -8 + 2.0 ** -12
+        assert abs(off.mean()) < 6 * 2.0 ** -8 / np.sqrt(3 * H) + 2.0 ** -13, off.mean()
+
+
 # ------------------------------------------------------------------------------ streams
 
 
