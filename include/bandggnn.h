@@ -357,7 +357,11 @@ int bg_embed_bwd(int64_t n, int32_t H, int32_t V, const int32_t* ids, const floa
  * z = X W^T:
  *   lse[i] = log sum_v exp(z[i][v]),   loss[i] = lse[i] - z[i][target[i]].
  * X [n, H] and W [V, H] dtype, target [n] int32, loss and lse [n] fp32.  A row with target[i] < 0 is
- * left out: loss and lse are 0, its X is not used (it may hold anything). */
+ * left out: loss and lse are 0, its X is not used (it may hold anything).
+ * Precision of the operands: bf16 X and W enter as they are.  fp32 ones (and bf16 ones where
+ * gradients are fp32) enter with 22 bits, down to 2^-17 of the largest magnitude in the row for X, in all
+ * of W for W; smaller elements are off by up to 2^-39 of that magnitude.  So a row of X costs no other
+ * row its precision, but a row of W beyond 2^17 times the others does. */
 #define BG_OP_XENT_FWD 5
 #define BG_OP_XENT_BWD 6
 /* Scratch of bg_xent_fwd / bg_xent_bwd (op); 0 for arguments out of range. */
@@ -370,8 +374,10 @@ int bg_xent_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, 
  *   dW    = sum_i dloss[i] (softmax(z[i]) - onehot(target[i]))^T X[i].
  * dloss [n] fp32 (not used in rows left out, whose dX is 0).  dX [n, H] and dW [V, H] in
  * grad_dtype, either of them may be NULL (not computed).  grad_dtype BG_F32: probabilities enter the
- * products with 21 bits, down to an absolute 2^-38 (times the largest |dloss|, for dW); BG_ACCUM adds to dX and dW instead of overwriting them.  grad_dtype BG_BF16
- * (dtype BG_BF16 only, no BG_ACCUM): they enter rounded to bf16, as the results are. */
+ * products with 21 bits, down to an absolute 2^-38 (for dW: times dloss[i], down to 2^-38 of the largest
+ * |dloss[i]| max |X[i]|), and sums of terms of one sign may come out low by 2^-18 of themselves; BG_ACCUM
+ * adds to dX and dW instead of overwriting them.  grad_dtype BG_BF16 (dtype BG_BF16 only, no BG_ACCUM):
+ * they enter rounded to bf16, as the results are. */
 int bg_xent_bwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
                 const int32_t* target, const float* lse, const float* dloss, bg_dtype grad_dtype,
                 void* dX, void* dW, uint32_t flags, void* ws, size_t ws_bytes, void* stream);

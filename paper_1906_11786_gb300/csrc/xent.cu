@@ -27,8 +27,11 @@
 //   fp16, 1 term   bf16 X and W with fp32 gradients: scaled by a power of two, they are exact in
 //                  fp16 (down to 2^-29 of the largest), and P, as the sum of two fp16 terms, keeps 21 bits;
 //                  fp16 and bf16 operands cannot be mixed in one product
-//   fp16, 2 terms  fp32 X and W, each the sum of two fp16 terms (22 bits); products of the two low
-//                  terms (2^-22) are left out
+//   fp16, 2 terms  fp32 X and W, each the sum of two fp16 terms (22 bits, down to 2^-17 of the largest,
+//                  below that an absolute 2^-40 of it); products of the two low terms (2^-22) are left out
+// The largest is that of a row of X, and that of all of W.  X's exponents go with the rows' statistics (as
+// W's could not: a row of X is a thread's in the forward, a row of W a column, whose factor would have to
+// be read for each of its logits); one exponent for all of X lost other rows' bits to one large row.
 // The tensor core truncates when it adds to its fp32 accumulator.  Measured: a step of 16 products loses
 // 0.2-0.45 x 2^-24 of the accumulator where signs are mixed, 3.4 x 2^-24 where all are of one sign, always
 // towards zero, so that a sum of N steps of one sign ends up 1.7 N x 2^-24 low.  A gradient in fp32 leaves
@@ -77,7 +80,7 @@ inline int64_t rows_per_block(int64_t n) {
 
 struct Ws {
   int64_t rb, nb, cap, vcap;  // rows a block, blocks, X rows and W rows rounded up to whole tiles
-  size_t head, counts, amax, row, stat, hit, x, w, full, part, total;
+  size_t head, counts, amax, xexp, row, stat, hit, x, w, full, part, total;
 };
 
 Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
@@ -95,9 +98,10 @@ Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
   const int terms = form == kF16x2 ? 2 : 1;
   w.head = take(16);
   w.counts = take((size_t)w.nb * 4);
-  w.amax = take((size_t)(2 * w.nb + kTableBlocks) * 4);
+  w.amax = take((size_t)(w.nb + kTableBlocks) * 4);
+  w.xexp = take(form == kBf16 ? 0 : (size_t)n);
   w.row = take((size_t)w.cap * 4);
-  w.stat = take((size_t)w.cap * 12);
+  w.stat = take((size_t)w.cap * 16);
   w.hit = take((size_t)w.cap * 4);
   w.x = take((size_t)terms * w.cap * H * 2);
   w.w = take(form == kBf16 ? 0 : (size_t)terms * w.vcap * H * 2);
@@ -107,10 +111,11 @@ Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
   return w;
 }
 
-// Statistics of the gathered rows ("slots"), in blocks of 64: -lse (bf16 form: times log2 e), dloss, and
-// the target, so that one copy brings a tile's.
-enum { kNlse = 0, kG = 64, kTgt = 128 };
-__host__ __device__ __forceinline__ int64_t stat_at(int64_t slot) { return slot / 64 * 192 + slot % 64; }
+// Statistics of the gathered rows ("slots"), in blocks of 64, so that one copy brings a tile's: -lse (bf16
+// form: times log2 e), dloss (fp16 forms: times 2^e, e the exponent of the row's largest element, which X's
+// terms lack), the target, and what the row's logits are multiplied by to undo the operands' scales.
+enum { kNlse = 0, kG = 64, kTgt = 128, kDs = 192 };
+__host__ __device__ __forceinline__ int64_t stat_at(int64_t slot) { return slot / 64 * 256 + slot % 64; }
 
 // ------------------------------------------------------------------------------ rows
 struct RowArgs {
@@ -124,9 +129,10 @@ struct RowArgs {
   const int32_t* target;
   const float* lse_in;
   const float* dloss;
-  int* head;  // number of labelled rows; exponents of the scales of X, W and dloss (fp16 forms)
+  int* head;  // number of labelled rows; exponents of the scales of W and of the weights (fp16 forms)
   int* counts;
-  uint32_t* amax;  // [nb] of X, [nb] of dloss, [tb] of W: bits of the largest finite |x|
+  uint32_t* amax;  // [nb] of dloss 2^e, [tb] of W: bits of the largest finite magnitude
+  int8_t* xexp;    // [n] exponent e of each labelled row's largest finite element
   int32_t* row;
   float* stat;
   uint16_t* x;
@@ -163,80 +169,93 @@ __device__ __forceinline__ uint32_t amax8(const float* v, uint32_t m) {
   return m;
 }
 
-// The maxima over the block of three values at once (sm [24]).
-__device__ __forceinline__ void block_max3(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t* sm) {
+// The maxima over the block of two values at once (sm [16]).
+__device__ __forceinline__ void block_max2(uint32_t& a, uint32_t& b, uint32_t* sm) {
   a = __reduce_max_sync(0xffffffffu, a);
   b = __reduce_max_sync(0xffffffffu, b);
-  c = __reduce_max_sync(0xffffffffu, c);
   const int warp = threadIdx.x >> 5;
-  if ((threadIdx.x & 31) == 0) sm[warp] = a, sm[8 + warp] = b, sm[16 + warp] = c;
+  if ((threadIdx.x & 31) == 0) sm[warp] = a, sm[8 + warp] = b;
   __syncthreads();
   for (int i = 0; i < 8; ++i) {
     a = max(a, sm[i]);
     b = max(b, sm[8 + i]);
-    c = max(c, sm[16 + i]);
   }
 }
 
+// Exponent of the number with these bits, -100 at least.
+__device__ __forceinline__ int exp_of(uint32_t bits) { return max((int)(bits >> 23) - 127, -100); }
 // Exponent k such that values of magnitude up to the one with these bits, times 2^k, are below 2^15.
-__device__ __forceinline__ int shift_of(uint32_t bits) { return 14 - max((int)(bits >> 23) - 127, -100); }
+__device__ __forceinline__ int shift_of(uint32_t bits) { return 14 - exp_of(bits); }
 __device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-// Labelled rows of each block of rb rows and, for the fp16 forms, the largest finite magnitudes of
-// the labelled rows of X, of their dloss, and of W.
+// Labelled rows of each block of rb rows and, for the fp16 forms, the exponent of each one's largest finite
+// element, the largest magnitude of their weights (dloss 2^e) and of W.  X has a scale a row: one large row
+// does not cost the others their bits.
 __global__ void __launch_bounds__(256) k_xent_count(RowArgs a) {
-  __shared__ uint32_t sm[24];
+  __shared__ uint32_t sm[16];
+  __shared__ uint32_t top[256];
   __shared__ int sums[8];
   grid_dep_launch();
   grid_dep_wait();
-  const int lanes = a.H / 8;
-  uint32_t mx = 0, mg = 0, mw = 0;
+  const int lanes = a.H / 8, tid = threadIdx.x;
+  uint32_t mg = 0, mw = 0;
   if ((int64_t)blockIdx.x >= a.nb) {
     const int b = blockIdx.x - (int)a.nb;
     const int64_t chunks = (int64_t)a.V * lanes;
 #pragma unroll 4
-    for (int64_t i = (int64_t)b * 256 + threadIdx.x; i < chunks; i += (int64_t)a.tb * 256) {
+    for (int64_t i = (int64_t)b * 256 + tid; i < chunks; i += (int64_t)a.tb * 256) {
       float v[8];
       load8f(a.W, a.x_bf16, i * 8, v);
       mw = amax8(v, mw);
     }
-    block_max3(mx, mg, mw, sm);
-    if (threadIdx.x == 0) a.amax[2 * a.nb + b] = mw;
+    block_max2(mg, mw, sm);
+    if (tid == 0) a.amax[a.nb + b] = mw;
     return;
   }
   const int64_t r0 = blockIdx.x * a.rb, r1 = min(a.n, r0 + a.rb);
+  // a row is `lanes` threads; those of them that are in this warp
+  const int rows = 256 / lanes, r = tid / lanes, q = tid % lanes;
+  const int w0 = max(r * lanes, tid & ~31), w1 = min((r + 1) * lanes, (tid | 31) + 1);
+  const unsigned mates = (0xffffffffu >> (32 - (w1 - w0))) << (w0 & 31);
   int c = 0;
-  for (int64_t i = r0 + threadIdx.x; i < r1; i += 256) {
-    const int t = a.target[i];
-    if (t >= 0 && t < a.V) {
-      ++c;
-      if (a.form != kBf16 && a.backward) {
-        const uint32_t b = __float_as_uint(a.dloss[i]) & 0x7FFFFFFFu;
-        if (b < 0x7F800000u) mg = max(mg, b);
-      }
+  for (int64_t g0 = r0; g0 < r1; g0 += 256) {
+    if (a.form != kBf16) {
+      __syncthreads();
+      top[tid] = 0;
+      __syncthreads();
+      if (r < rows)
+#pragma unroll 4
+        for (int k = r; k < 256 && g0 + k < r1; k += rows) {
+          const int t = a.target[g0 + k];
+          if (t < 0 || t >= a.V) continue;
+          float v[8];
+          load8f(a.X, a.x_bf16, (g0 + k) * a.H + q * 8, v);
+          const uint32_t m = __reduce_max_sync(mates, amax8(v, 0));
+          if (tid == w0) atomicMax(&top[k], m);
+        }
+      __syncthreads();
+    }
+    const int64_t i = g0 + tid;
+    const int t = i < r1 ? a.target[i] : -1;
+    if (t < 0 || t >= a.V) continue;
+    ++c;
+    if (a.form == kBf16) continue;
+    const int e = exp_of(top[tid]);
+    a.xexp[i] = (int8_t)e;
+    if (a.backward) {
+      const uint32_t b = __float_as_uint(a.dloss[i] * pow2(e)) & 0x7FFFFFFFu;
+      if (b < 0x7F800000u) mg = max(mg, b);
     }
   }
+  __syncwarp();
   c = __reduce_add_sync(0xffffffffu, c);
-  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = c;
-  if (a.form != kBf16) {
-    const int rows = 256 / lanes, r = threadIdx.x / lanes, q = threadIdx.x % lanes;
-    if (r < rows)
-#pragma unroll 4
-      for (int64_t i = r0 + r; i < r1; i += rows) {
-        const int t = a.target[i];
-        if (t < 0 || t >= a.V) continue;
-        float v[8];
-        load8f(a.X, a.x_bf16, i * a.H + q * 8, v);
-        mx = amax8(v, mx);
-      }
-  }
-  block_max3(mx, mg, mw, sm);  // (and the barrier that the sums need)
-  if (threadIdx.x == 0) {
+  if ((tid & 31) == 0) sums[tid >> 5] = c;
+  block_max2(mg, mw, sm);  // (and the barrier that the sums need)
+  if (tid == 0) {
     int s = 0;
     for (int i = 0; i < 8; ++i) s += sums[i];
     a.counts[blockIdx.x] = s;
-    a.amax[blockIdx.x] = mx;
-    a.amax[a.nb + blockIdx.x] = mg;
+    a.amax[blockIdx.x] = mg;
   }
 }
 
@@ -264,14 +283,15 @@ __device__ __forceinline__ void put8(uint16_t* dst, int64_t plane, int64_t at, i
 // blocks from nb on convert W.
 __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
   __shared__ int wsum[8];
-  __shared__ uint32_t sm[24];
+  __shared__ uint32_t sm[16];
   __shared__ int64_t from[256];  // row of each slot of the group at hand
+  __shared__ float up[256];      // and the scale of its elements
   grid_dep_launch();
   grid_dep_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int lanes = a.H / 8, rows = 256 / lanes, rr = tid / lanes, q = tid % lanes;
   const bool table = (int64_t)blockIdx.x >= a.nb;
-  uint32_t mx = 0, mg = 0, mw = 0;
+  uint32_t mg = 0, mw = 0;
   int before = 0;  // labelled rows of the blocks before this one
   if (!table) {
     if (a.direct) {
@@ -291,13 +311,10 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
   }
   if (a.form != kBf16) {
 #pragma unroll 4
-    for (int64_t i = tid; i < a.nb; i += 256) {
-      mx = max(mx, a.amax[i]);
-      mg = max(mg, a.amax[a.nb + i]);
-    }
-    for (int i = tid; i < a.tb; i += 256) mw = max(mw, a.amax[2 * a.nb + i]);
+    for (int64_t i = tid; i < a.nb; i += 256) mg = max(mg, a.amax[i]);
+    for (int i = tid; i < a.tb; i += 256) mw = max(mw, a.amax[a.nb + i]);
   }
-  block_max3(mx, mg, mw, sm);
+  block_max2(mg, mw, sm);
   if (table) {
     const int b = blockIdx.x - (int)a.nb;
     const float scale = pow2(shift_of(mw));
@@ -310,7 +327,6 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
     }
     return;
   }
-  const float scale = a.form == kBf16 ? 1.f : pow2(shift_of(mx));
   int64_t base = 0;
   for (int i = 0; i < 8; ++i) base += wsum[i];
   const int64_t r0 = blockIdx.x * a.rb, r1 = min(a.n, r0 + a.rb);
@@ -337,9 +353,15 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
       a.row[slot] = (int32_t)i;
       float* st = a.stat + stat_at(slot);
       st[kTgt] = __int_as_float(t);
+      int e = 0;
+      if (a.form != kBf16) {
+        e = a.xexp[i];
+        up[k] = pow2(14 - e);
+        st[kDs] = pow2(max(-126, min(127, e - 14 - shift_of(mw))));
+      }
       if (a.backward) {
         st[kNlse] = a.form == kBf16 ? -a.lse_in[i] * kLog2e : -a.lse_in[i];
-        st[kG] = a.dloss[i];
+        st[kG] = a.dloss[i] * pow2(e);
       }
     } else if (i < r1 && !a.backward) {
       a.loss[i] = 0.f;
@@ -355,7 +377,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
         } else {
           float v[8];
           load8f(a.X, a.x_bf16, src, v);
-          put8(a.x, a.cap * a.H, dst, a.form, scale, v);
+          put8(a.x, a.cap * a.H, dst, a.form, up[k], v);
         }
       }
       if (a.clear_dx)
@@ -380,15 +402,15 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
     if (tid == 0) {
       a.head[0] = (int)base;
       if (a.form != kBf16) {
-        a.head[1] = shift_of(mx);
-        a.head[2] = shift_of(mw);
-        a.head[3] = shift_of(mg);
+        a.head[1] = shift_of(mw);
+        a.head[2] = shift_of(mg);
       }
     }
     for (int64_t s = base + tid; s < end; s += 256) {
       a.row[s] = -1;
       float* st = a.stat + stat_at(s);
       st[kTgt] = __int_as_float(-1);
+      st[kDs] = 1.f;
       if (a.backward) {
         st[kNlse] = -INFINITY;
         st[kG] = 0.f;
@@ -802,14 +824,19 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   } else {
     // a thread is a row; each warpgroup has 64 columns of a tile
     const int q = warp & 3, wg = warp >> 2, r = q * 32 + lane;
-    float c = kLog2e;
-    if (T == 2) c *= pow2(max(-126, min(127, -(a.head[1] + a.head[2]))));
+    float ds = 1.f, c = kLog2e;  // z ds is the logit, z c the same in base 2
     const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + wg * 64;
     float m = -3.0e38f, l = 0.f;
     int tgt = -1;
     uint32_t n = 0, finished = 0;
     for (; w.more(); w.next(), ++n) {
-      if (w.starts) tgt = fwd_target(a, (int64_t)w.t * 128 + r);
+      if (w.starts) {
+        tgt = fwd_target(a, (int64_t)w.t * 128 + r);
+        if (T == 2) {
+          ds = a.stat[stat_at((int64_t)w.t * 128 + r) + kDs];
+          c = kLog2e * ds;
+        }
+      }
       const int b = n & 1;
       const bool ok = mbar_wait(&bars->s_full[b], (n >> 1) & 1, a.status, 706, abort, 20);
       tc_fence_after();
@@ -822,7 +849,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         const int col = __shfl_sync(0xffffffffu, at, __ffs(hits) - 1);
         const float z = __uint_as_float(tmem_ld1(base + b * 256 + col));
         tmem_wait_ld();
-        if (here && at == col) a.hit[w.t * 128 + r] = z * (c / kLog2e);
+        if (here && at == col) a.hit[w.t * 128 + r] = T == 2 ? z * ds : z;
         hits &= ~__ballot_sync(0xffffffffu, here && at == col);
       }
       // l = sum exp2(c z - m).  m need not be the running maximum, only near it: it is the maximum of
@@ -943,6 +970,7 @@ struct BwdArgs {
   const int* head;
   const int32_t* row;
   const float* stat;
+  const float* dloss;
   void* dX;
   void* dW;
   float* part;  // [G][2][128 x H], see part_at
@@ -981,7 +1009,7 @@ struct BCfg {
   static constexpr int S_BYTES = T * HC * 16384;
   static constexpr int BOX = NB * 128;  // 64 elements of each passing row
   static constexpr int B_BYTES = T * HC * BOX;
-  static constexpr int STATS = 3 * NB * 4;  // of passing X rows
+  static constexpr int STATS = 4 * NB * 4;  // of passing X rows
   static constexpr int ROOM = (232448 - 2048 - S_BYTES) / (B_BYTES + 2048);
   static constexpr int ST = ROOM < kMaxStages ? ROOM : kMaxStages;
   static constexpr int SMEM = S_BYTES + ST * (B_BYTES + 2048) + 2048;
@@ -1023,8 +1051,8 @@ __device__ __forceinline__ bool hit_row(const float* stat, int i, int first) {
   return __any_sync(0xffffffffu, at >= 0 && at < 32);
 }
 
-// P of N columns of a row (a thread's) from their logits, for dX: nlse = -lse of the row, hit = its
-// target's place among the columns, of which the first `valid` exist.
+// P of N columns of a row (a thread's) from their logits, for dX: descale and nlse = -lse of the row, hit =
+// its target's place among the columns, of which the first `valid` exist.
 template <int FORM, int N, int PATH>
 __device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, float nlse, int hit,
                                           int valid) {
@@ -1049,22 +1077,22 @@ __device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, 
   }
 }
 
-// The same for dW, whose statistics (-lse, g, target of the passing X rows) go by column.  Were a
+// The same for dW, whose statistics (scale, -lse, g, target of the passing X rows) go by column.  Were a
 // thread a row here too, it would read every column's: at 32 columns a warp 16 shared-memory loads of
 // 512 bytes, more than the SM can deliver in the time of the products (measured: 1.8 x the time of the
 // dX kernel at H = 64).  So tensor memory is read in fragments in which a thread has two neighbouring
 // columns of every 8, in rows l / 4, + 8, + 16, + 24 of its warp's 32 (l = lane): a quarter of the
 // loads.  v[16 h + 4 g + 2 a + b]: row 16 h + 8 a + l / 4, column 8 g + 2 (l % 4) + b.
 template <int FORM, int N, int PATH>
-__device__ __forceinline__ void probs_col(uint32_t* v, float descale, float up, const float* stat,
-                                          int mine) {
-  const uint64_t l2e = pack2(kLog2e, kLog2e), ds = pack2(descale, descale), up2 = pack2(up, up);
+__device__ __forceinline__ void probs_col(uint32_t* v, float up, const float* stat, int mine) {
+  const uint64_t l2e = pack2(kLog2e, kLog2e), up2 = pack2(up, up);
   const int lane = threadIdx.x & 31, c = 2 * (lane & 3);
   const bool hits = PATH == kEither && hit_row(stat, lane & (N - 1), mine - lane / 4);
 #pragma unroll
   for (int g = 0; g < N / 8; ++g) {
     const uint64_t nl = *reinterpret_cast<const uint64_t*>(stat + kNlse + 8 * g + c);
     const uint64_t g2 = *reinterpret_cast<const uint64_t*>(stat + kG + 8 * g + c);
+    const uint64_t ds = FORM == kBf16 ? 0 : *reinterpret_cast<const uint64_t*>(stat + kDs + 8 * g + c);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       uint32_t* p = v + (k >> 1) * (N / 2) + 4 * g + 2 * (k & 1);
@@ -1132,7 +1160,7 @@ __device__ __forceinline__ void z_to_p(uint32_t at, float descale, float up, con
         tmem_ld_frag16(at + pc + (16u << 16), v + 8);
       }
       tmem_wait_ld();
-      probs_col<FORM, N, PATH>(v, descale, up, stat + pc, mine);
+      probs_col<FORM, N, PATH>(v, up, stat + pc, mine);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -1191,17 +1219,15 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
   constexpr int GQ = HC * 16;
   const int c0 = wg * C::CW;
   const uint32_t quarter = (uint32_t)(q * 32) << 16;
-  const int sx = FORM == kBf16 ? 0 : a.head[1], sw = FORM == kBf16 ? 0 : a.head[2];
-  const float descale = FORM == kBf16 ? 1.f : pow2(max(-126, min(127, -(sx + sw))));
-  // P is scaled by 2^up: probabilities to 2^15 for dX, times g to 2^15 for dW
-  const int up = FORM == kBf16 ? 0 : DW ? a.head[3] : 15;
+  // P is scaled by 2^up: probabilities to 2^15 for dX, times the weights to 2^15 for dW
+  const int up = FORM == kBf16 ? 0 : DW ? a.head[2] : 15;
   float acc[C::KEEP ? GQ : 1];
   uint32_t groups = 0;
   int in_group = 0;
   Turn<C::ST> s;
   Turn<C::ZB> b;
   bool fresh = true, pending = false, spilled = false, ok = true;
-  float nlse = 0.f;
+  float nlse = 0.f, descale = 1.f;
   int tgt = -1, first = 0;
   auto wait = [&](uint64_t* bar, uint32_t parity, int site, uint32_t backoff_ns) {
     return C::UNIFORM ? mbar_wait_warp(bar, parity, a.status, site, abort, backoff_ns)
@@ -1236,6 +1262,7 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       const float* st = a.stat + stat_at(w.t * 128 + r);
       nlse = st[kNlse];
       tgt = __float_as_int(st[kTgt]);
+      if (FORM != kBf16) descale = st[kDs];
     }
     ok = wait(&bars->z_full[b.i], b.parity, 718, 20);
     if (!ok) break;
@@ -1276,11 +1303,11 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
     float s1 = 1.f, s2 = 1.f, s3 = 1.f;
     if (DW) {
       if (orow >= a.V) orow = -1;
-      if (FORM != kBf16) s1 = pow2(-up), s2 = pow2(-sx);
+      if (FORM != kBf16) s1 = pow2(-up), s2 = pow2(-14);  // (X's elements are times 2^14, once 2^e is undone)
     } else {
-      s3 = a.stat[stat_at(orow) + kG];
       orow = a.row[orow];
-      if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-sw);
+      s3 = orow < 0 ? 0.f : a.dloss[orow];
+      if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-a.head[1]);
     }
     float* pt = a.part + ((int64_t)blockIdx.x * 2 + un.slot(cta, w.t)) * 128 * a.H;
 #pragma unroll(C::KEEP ? 4 : 1)
@@ -1577,17 +1604,17 @@ __global__ void __launch_bounds__(256)
   }
   float s1 = 1.f, s2 = 1.f;
   if (form != kBf16) {
-    s1 = pow2(dw ? -a.head[3] : -15);
-    s2 = pow2(dw ? -a.head[1] : -a.head[2]);
+    s1 = pow2(dw ? -a.head[2] : -15);
+    s2 = pow2(dw ? -14 : -a.head[1]);
   }
   int64_t orow = (int64_t)un.tile((int)t) * 128 + r;
   float s3 = 1.f;
   if (dw) {
     if (orow >= a.V) return;
   } else {
-    s3 = a.stat[stat_at(orow) + kG];
     orow = a.row[orow];
     if (orow < 0) return;
+    s3 = a.dloss[orow];
   }
   x = make_float4(x.x * s1 * s2 * s3, x.y * s1 * s2 * s3, x.z * s1 * s2 * s3, x.w * s1 * s2 * s3);
   if (a.out_bf16) {
@@ -1632,6 +1659,7 @@ cudaError_t prepare(const XentArgs& a, Call& c, RowArgs r) {
   r.head = c.at<int>(c.w.head);
   r.counts = c.at<int>(c.w.counts);
   r.amax = c.at<uint32_t>(c.w.amax);
+  r.xexp = c.at<int8_t>(c.w.xexp);
   r.row = c.at<int32_t>(c.w.row);
   r.stat = c.at<float>(c.w.stat);
   r.x = c.at<uint16_t>(c.w.x);
@@ -1835,6 +1863,7 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
   b.head = c.at<int>(c.w.head);
   b.row = c.at<int32_t>(c.w.row);
   b.stat = c.at<float>(c.w.stat);
+  b.dloss = dloss;
   b.part = c.at<float>(c.w.part);
   b.status = a.status;
   b.out_bf16 = grad_bf16;

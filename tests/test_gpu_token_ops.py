@@ -462,6 +462,45 @@ def test_xent_of_small_and_large_values(scale):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("large", [1e6, 1e10, 1e15])
+def test_xent_a_large_row_costs_the_others_nothing(dtype, large):
+    """Rows are independent of one another: beside a few that are many times as large, and some as much
+    smaller, the loss and dX of the others have the accuracy that they have among their likes."""
+    n, H, V = 300, 64, 500
+    X, W, target, g = xent_inputs(n, H, V, dtype)
+    X[[7, 130, 299]] *= large
+    X[[8, 131, 290]] /= large
+    got = run_xent(dtype, X, W, target, g, "f32")
+    rows = np.setdiff1d(np.arange(n), [7, 130, 299])
+    only = np.full(n, -1, np.int32)
+    only[rows] = target[rows]
+    r = ref.xent(host(X), host(W), only, g)
+    loss, bX, _ = xent_bounds(r, n, H, V, "f32")
+    within(host(got[0])[rows], r["loss"][rows], loss[rows], "loss")
+    within(host(got[1])[rows], r["lse"][rows], loss[rows], "lse")
+    within(host(got[2])[rows], r["dX"][rows], bX[rows], "dX")
+
+
+def test_xent_of_a_table_with_one_large_row():
+    """An element of W is off by 2^-39 of W's largest at most, a logit by that times the sum of its state:
+    rows that the large token does not dominate keep a loss of that accuracy."""
+    n, H, V = 300, 64, 500
+    X, W, target, g = xent_inputs(n, H, V, "f32")
+    W[3] *= 1e8
+    target[target == 3] = 4
+    z = host(X) @ host(W).T
+    rows = np.flatnonzero(z[:, 3] < -1e3)
+    assert rows.size > n // 4
+    got = run_xent("f32", X, W, target, g, "f32")
+    r = ref.xent(host(X), host(W), target, g)
+    zabs = (np.abs(host(X[rows])) @ np.delete(np.abs(host(W)), 3, 0).T).max()
+    dz = (2 * H * U + 2.0 ** -21) * zabs + 2.0 ** -39 * np.abs(host(W)).max() * np.abs(host(X[rows])).sum(1)
+    tol = 2 * dz + 2.0 ** -20 * (1 + np.abs(r["lse"][rows]))
+    within(host(got[0])[rows], r["loss"][rows], tol, "loss")
+    within(host(got[1])[rows], r["lse"][rows], tol, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_xent_gradient_against_differences(dtype):
     """Directional differences of the forward itself, over states and table.  With step e along a
     direction whose logits move by at most m, the central difference is off by e^2 m^3 / 6 of the
