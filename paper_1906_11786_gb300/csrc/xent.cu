@@ -652,7 +652,10 @@ __device__ __forceinline__ void fwd_finish(const FwdArgs& a, int64_t s, int tgt,
     // (top + log2 l) / c with c = kLog2e as it was rounded, 1 / c in two parts, so that the only error
     // that counts is the result's own rounding
     constexpr float inv = (float)(1.0 / (double)kLog2e), rest = (float)(1.0 / (double)kLog2e - (double)inv);
-    const float hi = top * inv, lo = fmaf(top, inv, -hi) + fmaf(top, rest, log2f(l) * inv);
+    // (a sum of 0: the reference, rounded up, lies 2^7 or more above the largest logit, which it then
+    // stands for to the last bit of fp32)
+    const float log_l = l == 0.f ? 0.f : log2f(l);
+    const float hi = top * inv, lo = fmaf(top, inv, -hi) + fmaf(top, rest, log_l * inv);
     v = hi + lo;
     loss = (hi - a.hit[s]) + lo;
   }
@@ -878,7 +881,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             m = -3.0e38f;
             l = 0.f;
           }
-          const float top = start || !(sum <= 0x1p40f) ? fmaxf(m, max32(v) * c) : m;
+          // (rounded up: of logits beyond 2^31, whose products with c are rounded by more than 2^7, the terms
+          // may vanish but not overflow)
+          const float top = start || !(sum <= 0x1p40f) ? fmaxf(m, __fmul_ru(max32(v), c)) : m;
           l *= ex2(m - top);
           m = top;
           sum = sum32(v, c, m);

@@ -481,6 +481,28 @@ def test_xent_a_large_row_costs_the_others_nothing(dtype, large):
     within(host(got[2])[rows], r["dX"][rows], bX[rows], "dX")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("large", [1e8, 1e10, 1e15, 1e30])
+@pytest.mark.parametrize("V", [3, 500])
+def test_xent_of_enormous_logits(dtype, large, V):
+    """Logits far beyond what exp can tell apart: loss and lse are those of the largest one, to the
+    precision of the logits, whatever their sign."""
+    n, H = 260, 64
+    X, W, target, g = xent_inputs(n, H, V, dtype)
+    if V == 3:
+        W, X[::2] = W.abs(), -X[::2].abs()  # every logit of these rows is negative
+    X *= large
+    t = torch.from_numpy(target).cuda()
+    loss, lse = (torch.full((n,), float("nan"), device="cuda") for _ in range(2))
+    ws = torch.empty(L.xent_workspace_bytes(dtype, n, H, V, L.BG_OP_XENT_FWD), device="cuda",
+                     dtype=torch.uint8)
+    L.xent_fwd(dtype, X, W, t, loss, lse, ws)
+    r = ref.xent(host(X), host(W), target, g)
+    tol = xent_bounds(r, n, H, V, "f32")[0]
+    within(host(loss), r["loss"], tol, "loss")
+    within(host(lse), r["lse"], tol, "lse")
+
+
 def test_xent_of_a_table_with_one_large_row():
     """An element of W is off by 2^-39 of W's largest at most, a logit by that times the sum of its state:
     rows that the large token does not dominate keep a loss of that accuracy."""
