@@ -372,6 +372,8 @@ int bg_xent_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, 
 /* Gradient of sum_i dloss[i] loss[i]; lse is bg_xent_fwd's of the same X, W and target:
  *   dX[i] = dloss[i] (softmax(z[i]) - onehot(target[i])) W,
  *   dW    = sum_i dloss[i] (softmax(z[i]) - onehot(target[i]))^T X[i].
+ * Probabilities are exp(z - lse): z and lse are fp32, so that they are good to some |lse| 2^-20 of
+ * themselves.  Rows with |lse| beyond 2^20 have them lowered so that none passes 1, to 0 far out.
  * dloss [n] fp32 (not used in rows left out, whose dX is 0).  dX [n, H] and dW [V, H] in
  * grad_dtype, either of them may be NULL (not computed).  grad_dtype BG_F32: probabilities enter the
  * products with 21 bits, down to an absolute 2^-38 (for dW: times dloss[i], down to 2^-38 of the largest

@@ -503,6 +503,39 @@ def test_xent_of_enormous_logits(dtype, large, V):
     within(host(lse), r["lse"], tol, "lse")
 
 
+@pytest.mark.parametrize("dtype,grad", TYPES)
+@pytest.mark.parametrize("large", [1e6, 1e10, 1e20])
+@pytest.mark.parametrize("H", [64, 128, 256])
+def test_xent_gradients_beside_rows_of_enormous_logits(dtype, grad, large, H):
+    """exp(z - lse) cannot be told from fp32 values of some 1e6 and more: such a row's probabilities are only
+    kept within [0, 1].  So no element of dX or dW is more than each probability at its worst makes it, and the
+    rest of dW, where those rows are left out, stands beside it."""
+    n, V = 300, 500
+    X, W, target, g = xent_inputs(n, H, V, dtype)
+    far = [7, 130, 299]
+    X[far] *= large
+    g[130] = 0  # (a weight of 0 leaves nothing of an infinite one)
+    got = run_xent(dtype, X, W, target, g, grad)
+    only = target.copy()
+    only[far] = -1
+    r = ref.xent(host(X), host(W), only, g)
+    loss, bX, bW = xent_bounds(r, n, H, V, grad)
+    near = np.setdiff1d(np.arange(n), far)
+    within(host(got[2])[near], r["dX"][near], bX[near], "dX")
+    # a far row: every probability from 0 to 1, its target's less 1; results rounded
+    x, w = np.abs(host(X)), np.abs(host(W))
+    more = 1 + 2.0 ** -7
+    assert (np.abs(host(got[2])[far]) <= more * g[far][:, None] * w.sum(0) + bX[far]).all()
+    within(host(got[3]), r["dW"], bW + more * ((g[far][:, None] * x[far]).sum(0)) + 2.0 ** -7 * np.abs(r["dW"]), "dW")
+    # a token's row of dW takes nothing from a far row whose logit is far below its largest
+    z = host(X)[far] @ host(W).T
+    low = (z < z.max(1, keepdims=True) - 0.01 * np.abs(z).max(1, keepdims=True)).all(0)
+    low[target[far]] = False
+    assert low.sum() > V // 2
+    floor = 2.0 ** -37 * (g[:, None] * x).max() if grad == "f32" else 0
+    within(host(got[3])[low], r["dW"][low], bW[low] + n * floor, "dW of tokens that far rows do not reach")
+
+
 def test_xent_of_a_table_with_one_large_row():
     """An element of W is off by 2^-39 of W's largest at most, a logit by that times the sum of its state:
     rows that the large token does not dominate keep a loss of that accuracy."""
