@@ -117,7 +117,7 @@ extern "C" int bg_embed_bwd(int64_t n, int32_t H, int32_t V, const int32_t* ids,
       return bg_fail(BG_ECAPACITY, "workspace too small");
   }
   int* status = nullptr;
-  TOK_TRY(bg_status_word(&status));
+  if (n > 0) TOK_TRY(bg_status_word(&status));
   return cuda_rc(bg::embed_bwd(n, H, V, ids, dout, scale, bg::make_drop(p, seed, call), dtable,
                                (flags & BG_ACCUM) != 0, ws, status, (cudaStream_t)stream),
                  "bg_embed_bwd");
@@ -170,12 +170,13 @@ extern "C" int bg_xent_bwd(bg_dtype dt, int64_t n, int32_t H, int32_t V, const v
     return bg_fail(BG_EINVAL, "fp32 states and table have fp32 gradients");
   if ((flags & BG_ACCUM) && grad_dt != BG_F32)
     return bg_fail(BG_EINVAL, "BG_ACCUM needs fp32 gradients");
-  if (!dX && !dW) return bg_fail(BG_EINVAL, "dX and dW are NULL");
+  // (without rows dX is empty and may be NULL all the same)
+  if (n > 0 && !dX && !dW) return bg_fail(BG_EINVAL, "dX and dW are NULL");
   TOK_OPT_PTR(dX); TOK_OPT_PTR(dW);
   if (n > 0) {
     TOK_PTR(lse); TOK_PTR(dloss);
+    TOK_TRY(bg_status_word(&a.status));
   }
-  TOK_TRY(bg_status_word(&a.status));
   return cuda_rc(bg::xent_bwd(a, lse, dloss, grad_dt == BG_BF16, dX, dW, (flags & BG_ACCUM) != 0,
                               (cudaStream_t)stream), "bg_xent_bwd");
 }

@@ -169,3 +169,14 @@ def test_the_workspace_holds_what_a_call_takes_on_any_device(lib):
                     for grad_bf16 in (0, 1) if dt == L.BG_BF16 else (0,):
                         assert used(dt, n, H, V, backward, grad_bf16, sms) <= \
                             lib.bg_xent_workspace_bytes(dt, n, H, V, op)
+
+
+def test_gradients_without_rows_are_not_refused(lib):
+    """A tensor of no rows has no address: the gradient of the states alone is then nothing to do, and one
+    that is added to is left as it is."""
+    for grad in (L.BG_F32, L.BG_BF16):
+        assert lib.bg_xent_bwd(L.BG_BF16, 0, 64, 9, None, P16, None, None, None, grad, None, None, 0, None,
+                               0, None) == 0
+    assert lib.bg_xent_bwd(L.BG_F32, 0, 64, 9, None, P16, None, None, None, L.BG_F32, None, P16, L.BG_ACCUM,
+                           None, 0, None) == 0
+    assert lib.bg_embed_bwd(0, 64, 9, None, None, 1.0, 0.0, 0, 0, P16, L.BG_ACCUM, None, 0, None) == 0
