@@ -317,7 +317,9 @@ int bg_adam_step(int64_t n, float* master, void* working, bg_dtype working_dtype
  * states are scored against a vocabulary; both can share one [V, H] table.  None needs a plan: rows
  * are rows, in band order or in any other.  n up to 2^29 rows, V in [1, 2^24].  An id or target of V
  * or more counts as negative (no row) and is reported by bg_check_device as BG_EDEVICE (site 130:
- * an id; 131: a target).  n = 0 is valid everywhere.
+ * an id; 131: a target).  n = 0 is valid everywhere.  The
+ * first call on a device allocates the status word (256 bytes), also within a stream capture; nothing
+ * else is allocated.
  *
  * Dropout keeps no mask.  The elements of the (flat) array are numbered from 0; element i is dropped
  * where its 16 random bits are below round(p 2^16), and kept elements are multiplied by

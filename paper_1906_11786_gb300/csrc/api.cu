@@ -139,14 +139,39 @@ namespace {
 std::mutex g_status_mu;
 int* g_status[64] = {nullptr};
 
+// A cleared word, or nothing.
+cudaError_t new_status_word(int** out) {
+  int* p = nullptr;
+  cudaStream_t st = nullptr;
+  cudaError_t e = cudaMalloc(&p, 256);
+  if (e != cudaSuccess) return e;
+  e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+  if (e == cudaSuccess) {
+    e = cudaMemsetAsync(p, 0, 256, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    cudaStreamDestroy(st);
+  }
+  if (e != cudaSuccess) {
+    cudaFree(p);
+    return e;
+  }
+  *out = p;
+  return cudaSuccess;
+}
+
 int status_word_ptr(int** out) {
   int dev = 0;
   BG_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return bg_fail(BG_EINVAL, "device index out of range");
   std::lock_guard<std::mutex> g(g_status_mu);
   if (!g_status[dev]) {
-    BG_CUDA(cudaMalloc(&g_status[dev], 256));
-    BG_CUDA(cudaMemset(g_status[dev], 0, 256));
+    // The first call may stand in a stream capture: this thread's calls are let through, and the word is
+    // cleared on a stream of its own (the legacy stream would wait for the captured one).
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    BG_CUDA(cudaThreadExchangeStreamCaptureMode(&mode));
+    const cudaError_t e = new_status_word(&g_status[dev]);
+    BG_CUDA(cudaThreadExchangeStreamCaptureMode(&mode));
+    BG_CUDA(e);
   }
   *out = g_status[dev];
   return BG_OK;

@@ -6,6 +6,10 @@ fp32, and a result rounded to bf16 adds 2^-8 of itself.
 """
 from __future__ import annotations
 
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -699,3 +703,49 @@ def test_token_operators_run_on_the_stream_they_are_given():
     for u, v in zip(outs, want):
         assert torch.equal(u, v)
     assert torch.equal(dE, first)
+
+
+FIRST_CALLS = """
+import torch
+from paper_1906_11786_gb300 import lib as L
+n, H, V = 500, 64, 300
+gen = torch.Generator(device="cuda").manual_seed(1)
+X, W, dout = (torch.randn(m, H, device="cuda", generator=gen) for m in (n, V, n))
+t = torch.randint(0, V, (n,), device="cuda", generator=gen, dtype=torch.int32)
+g = torch.ones(n, device="cuda")
+ws = torch.empty(max([L.embed_workspace_bytes(n, H, V)] +
+                     [L.xent_workspace_bytes("f32", n, H, V, op)
+                      for op in (L.BG_OP_XENT_FWD, L.BG_OP_XENT_BWD)]), device="cuda",
+                 dtype=torch.uint8)
+outs = [torch.zeros(*s, device="cuda") for s in ((n, H), (V, H), (n,), (n,), (n, H), (V, H))]
+out, dtable, loss, lse, dX, dW = outs
+
+def calls():
+    L.embed_fwd("f32", t, W, out, p=0.1, seed=3, call=4)
+    L.embed_bwd(t, dout, dtable, ws)
+    L.xent_fwd("f32", X, W, t, loss, lse, ws)
+    L.xent_bwd("f32", X, W, t, lse, g, "f32", dX, dW, ws)
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls()
+graph.replay()
+torch.cuda.synchronize()
+L.check_device()
+replayed = [o.clone() for o in outs]
+for o in outs:
+    o.zero_()
+calls()
+torch.cuda.synchronize()
+L.check_device()
+assert all(torch.equal(a, b) and torch.count_nonzero(a) for a, b in zip(replayed, outs))
+print("captured")
+"""
+
+
+def test_the_first_token_calls_of_a_process_can_be_captured():
+    """No plan comes before them, so that a process may capture its very first call to the library."""
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
