@@ -380,35 +380,59 @@ def adam_step(master, working, m, v, grad, lr, beta1, beta2, eps, step, stream=N
 # --------------------------------------------------------------------------------- token operators
 
 
-def _shaped(t, name, dtype, *shape):
-    """Device pointer of a contiguous CUDA tensor of this element type and shape (None passes)."""
+def _current_device():
+    """The device that the library launches on (None without one).  From the first call on torch's function
+    stands in its place: an import statement a call shows in the time of the smallest operators."""
+    global _current_device
+    import torch
+    if not torch.cuda.is_available():
+        return None
+    _current_device = torch._C._cuda_getDevice
+    return _current_device()
+
+
+def _raw_stream(device):
+    """Handle of torch's current stream on the device (a Stream object of it takes as long to make as a
+    kernel launch); replaced in the same way."""
+    global _raw_stream
+    import torch
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+    return _raw_stream(device)
+
+
+def _on(t, name, device):
+    """Device pointer of a contiguous CUDA tensor on the current device."""
+    if t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _dev_ptr(t, name)  # raises for what is no contiguous CUDA tensor
+    raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
+
+
+def _shaped(t, name, device, dtype, *shape):
+    """The same of a tensor of this element type and shape (None passes)."""
     if t is None:
         return None
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
-    if t.is_cuda and t.is_contiguous():
+    if t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
-    return _dev_ptr(t, name)  # raises
+    return _on(t, name, device)  # raises
 
 
-def _elements(t, name, dtype, n):
+def _elements(t, name, device, dtype, n):
     """The same for n elements of any shape."""
     if t is None:
         return None
     if t.dtype is not dtype or t.numel() != n:
         raise ValueError(f"{name} must have {n} elements of {dtype}, not {t.numel()} of {t.dtype}")
-    if t.is_cuda and t.is_contiguous():
+    if t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
-    return _dev_ptr(t, name)  # raises
+    return _on(t, name, device)  # raises
 
 
-def _stream_of(stream, t):
-    """The stream given, else torch's current one on t's device (by its handle: making a Stream object
-    of it takes as long as a kernel launch)."""
-    if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(t.device.index)
-    return _stream(stream)
+def _stream_of(stream, device):
+    """The stream given, else torch's current one on the device."""
+    return _raw_stream(device) if stream is None else _stream(stream)
 
 
 _types = {}  # what dtype_code takes -> (code, torch dtype)
@@ -429,25 +453,26 @@ def _type(dtype):
 
 def dropout_fwd(dtype, x, y, p, seed, call, residual=None, stream=None):
     """y = residual + drop(x) elementwise (tensors of `dtype` with equal element counts)."""
-    (dt, td), n = _type(dtype), x.numel()
-    _check(load().bg_dropout_fwd(dt, n, p, seed, call, _elements(x, "x", td, n),
-                                 _elements(residual, "residual", td, n),
-                                 _elements(y, "y", td, n), _stream_of(stream, x)))
+    (dt, td), n, d = _type(dtype), x.numel(), _current_device()
+    _check(load().bg_dropout_fwd(dt, n, p, seed, call, _elements(x, "x", d, td, n),
+                                 _elements(residual, "residual", d, td, n),
+                                 _elements(y, "y", d, td, n), _stream_of(stream, d)))
 
 
 def dropout_bwd(dy, dx, p, seed, call, flags=0, stream=None):
     """dx (+)= drop(dy) with the mask of the forward call of the same (p, seed, call); fp32."""
-    (_, td), n = _type(BG_F32), dy.numel()
-    _check(load().bg_dropout_bwd(n, p, seed, call, _elements(dy, "dy", td, n),
-                                 _elements(dx, "dx", td, n), flags, _stream_of(stream, dy)))
+    (_, td), n, d = _type(BG_F32), dy.numel(), _current_device()
+    _check(load().bg_dropout_bwd(n, p, seed, call, _elements(dy, "dy", d, td, n),
+                                 _elements(dx, "dx", d, td, n), flags, _stream_of(stream, d)))
 
 
 def embed_fwd(dtype, ids, table, out, scale=1.0, p=0.0, seed=0, call=0, stream=None):
     """out[i] = drop(scale * table[ids[i]]), zero rows where ids[i] < 0; ids [n] int32."""
     (dt, td), (_, ti), n, (V, H) = _type(dtype), _type("ids"), ids.numel(), table.shape
-    _check(load().bg_embed_fwd(dt, n, H, V, _shaped(ids, "ids", ti, n),
-                               _shaped(table, "table", td, V, H), scale, p, seed, call,
-                               _shaped(out, "out", td, n, H), _stream_of(stream, out)))
+    d = _current_device()
+    _check(load().bg_embed_fwd(dt, n, H, V, _shaped(ids, "ids", d, ti, n),
+                               _shaped(table, "table", d, td, V, H), scale, p, seed, call,
+                               _shaped(out, "out", d, td, n, H), _stream_of(stream, d)))
 
 
 def embed_workspace_bytes(n, H, V) -> int:
@@ -457,11 +482,12 @@ def embed_workspace_bytes(n, H, V) -> int:
 def embed_bwd(ids, dout, dtable, ws, scale=1.0, p=0.0, seed=0, call=0, flags=0, stream=None):
     """dtable[v] (+)= scale * sum over ids[i] = v of drop(dout[i]); fp32."""
     (_, td), (_, ti), n, (V, H) = _type(BG_F32), _type("ids"), ids.numel(), dtable.shape
-    _check(load().bg_embed_bwd(n, H, V, _shaped(ids, "ids", ti, n),
-                               _shaped(dout, "dout", td, n, H), scale, p, seed, call,
-                               _shaped(dtable, "dtable", td, V, H), flags,
-                               _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
-                               _stream_of(stream, dtable)))
+    d = _current_device()
+    _check(load().bg_embed_bwd(n, H, V, _shaped(ids, "ids", d, ti, n),
+                               _shaped(dout, "dout", d, td, n, H), scale, p, seed, call,
+                               _shaped(dtable, "dtable", d, td, V, H), flags,
+                               _on(ws, "ws", d), ws.numel() * ws.element_size(),
+                               _stream_of(stream, d)))
 
 
 def xent_workspace_bytes(dtype, n, H, V, op) -> int:
@@ -472,26 +498,26 @@ def xent_fwd(dtype, X, W, target, loss, lse, ws, stream=None):
     """loss[i] = lse[i] - X[i] . W[target[i]], lse[i] = log sum_v exp(X[i] . W[v]); 0 for rows with
     target[i] < 0."""
     (dt, td), (_, tf), (_, ti) = _type(dtype), _type(BG_F32), _type("ids")
-    n, (V, H) = target.numel(), W.shape
-    _check(load().bg_xent_fwd(dt, n, H, V, _shaped(X, "X", td, n, H), _shaped(W, "W", td, V, H),
-                              _shaped(target, "target", ti, n),
-                              _shaped(loss, "loss", tf, n),
-                              _shaped(lse, "lse", tf, n), _dev_ptr(ws, "ws"),
-                              ws.numel() * ws.element_size(), _stream_of(stream, W)))
+    n, (V, H), d = target.numel(), W.shape, _current_device()
+    _check(load().bg_xent_fwd(dt, n, H, V, _shaped(X, "X", d, td, n, H), _shaped(W, "W", d, td, V, H),
+                              _shaped(target, "target", d, ti, n),
+                              _shaped(loss, "loss", d, tf, n),
+                              _shaped(lse, "lse", d, tf, n), _on(ws, "ws", d),
+                              ws.numel() * ws.element_size(), _stream_of(stream, d)))
 
 
 def xent_bwd(dtype, X, W, target, lse, dloss, grad_dtype, dX, dW, ws, flags=0, stream=None):
     """Gradients of sum_i dloss[i] loss[i] in grad_dtype; dX or dW may be None."""
     (dt, td), (gt, gd), (_, tf), (_, ti) = (_type(dtype), _type(grad_dtype), _type(BG_F32),
                                             _type("ids"))
-    n, (V, H) = target.numel(), W.shape
-    _check(load().bg_xent_bwd(dt, n, H, V, _shaped(X, "X", td, n, H), _shaped(W, "W", td, V, H),
-                              _shaped(target, "target", ti, n),
-                              _shaped(lse, "lse", tf, n),
-                              _shaped(dloss, "dloss", tf, n), gt,
-                              _shaped(dX, "dX", gd, n, H), _shaped(dW, "dW", gd, V, H), flags,
-                              _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
-                              _stream_of(stream, W)))
+    n, (V, H), d = target.numel(), W.shape, _current_device()
+    _check(load().bg_xent_bwd(dt, n, H, V, _shaped(X, "X", d, td, n, H), _shaped(W, "W", d, td, V, H),
+                              _shaped(target, "target", d, ti, n),
+                              _shaped(lse, "lse", d, tf, n),
+                              _shaped(dloss, "dloss", d, tf, n), gt,
+                              _shaped(dX, "dX", d, gd, n, H), _shaped(dW, "dW", d, gd, V, H), flags,
+                              _on(ws, "ws", d), ws.numel() * ws.element_size(),
+                              _stream_of(stream, d)))
 
 
 def check_device(stream=None):

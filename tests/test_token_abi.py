@@ -180,3 +180,46 @@ def test_gradients_without_rows_are_not_refused(lib):
     assert lib.bg_xent_bwd(L.BG_F32, 0, 64, 9, None, P16, None, None, None, L.BG_F32, None, P16, L.BG_ACCUM,
                            None, 0, None) == 0
     assert lib.bg_embed_bwd(0, 64, 9, None, None, 1.0, 0.0, 0, 0, P16, L.BG_ACCUM, None, 0, None) == 0
+
+
+class _Elsewhere:
+    """What the binding reads of a CUDA tensor, on a device of choice."""
+
+    def __init__(self, device, dtype, *shape):
+        self.device_index, self.dtype, self.shape, self.is_cuda = device, dtype, shape, True
+
+    def numel(self):
+        n = 1
+        for m in self.shape:
+            n *= m
+        return n
+
+    element_size = data_ptr = lambda self: P16
+    is_contiguous = lambda self: True
+    get_device = lambda self: self.device_index
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The library launches on the current device: a tensor elsewhere is refused by name, before anything
+    is launched, whichever of a call's tensors it is."""
+    import torch
+    monkeypatch.setattr(L, "_current_device", lambda: 0)
+    f, i = torch.float32, torch.int32
+    n, V, H = 6, 9, 64
+
+    args = {"x": (f, n), "y": (f, n), "residual": (f, n), "dy": (f, n), "dx": (f, n), "ids": (i, n),
+            "table": (f, V, H), "out": (f, n, H), "dout": (f, n, H), "dtable": (f, V, H),
+            "ws": (f, 1 << 20), "X": (f, n, H), "W": (f, V, H), "target": (i, n), "loss": (f, n),
+            "lse": (f, n), "dloss": (f, n), "dX": (f, n, H), "dW": (f, V, H)}
+    calls = [
+        ("x y residual", lambda x, y, residual: L.dropout_fwd("f32", x, y, 0.1, 1, 2, residual)),
+        ("dy dx", lambda dy, dx: L.dropout_bwd(dy, dx, 0.1, 1, 2)),
+        ("ids table out", lambda *t: L.embed_fwd("f32", *t)),
+        ("ids dout dtable ws", lambda *t: L.embed_bwd(*t)),
+        ("X W target loss lse ws", lambda *t: L.xent_fwd("f32", *t)),
+        ("X W target lse dloss dX dW ws", lambda *t: L.xent_bwd("f32", *t[:5], "f32", *t[5:])),
+    ]
+    for names, call in calls:
+        for away in names.split():
+            with pytest.raises(ValueError, match=f"^{away} is on cuda:1, the current device is cuda:0"):
+                call(*(_Elsewhere(int(name == away), *args[name]) for name in names.split()))
