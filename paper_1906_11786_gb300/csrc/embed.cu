@@ -11,6 +11,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "tc_util.cuh"
@@ -75,15 +76,16 @@ __global__ void __launch_bounds__(256)
   // 32 bytes of each array in flight a thread: at 64, or with more or fewer than 8 blocks an SM, both
   // types took up to 15% longer
   constexpr int kDropUnroll = 4 / (int)sizeof(T);
-  for (; b + (kDropUnroll - 1) * step < full; b += kDropUnroll * step) {
-    float v[kDropUnroll][8], r[kDropUnroll][8];
+  auto blocks8 = [&](auto unroll) {
+    constexpr int U = decltype(unroll)::value;
+    float v[U][8], r[U][8];
 #pragma unroll
-    for (int u = 0; u < kDropUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       load8(x + (b + u * step) * 8, v[u]);
       if (res) load8(res + (b + u * step) * 8, r[u]);
     }
 #pragma unroll
-    for (int u = 0; u < kDropUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       if (d.thr) drop8(d, (uint64_t)(b + u * step), d.scale, v[u]);
       if (res) {
 #pragma unroll
@@ -94,17 +96,20 @@ __global__ void __launch_bounds__(256)
       else
         store8(y + (b + u * step) * 8, v[u]);
     }
-  }
-  for (; b * 8 < n; b += step) {
-    const int64_t i = b * 8;
-    const int m = (int)min((int64_t)8, n - i);
+  };
+  for (; b + (kDropUnroll - 1) * step < full; b += kDropUnroll * step)
+    blocks8(std::integral_constant<int, kDropUnroll>());
+  for (; b < full; b += step) blocks8(std::integral_constant<int, 1>());
+  if (b == full && full * 8 < n) {  // the last elements, fewer than 8: one thread's
+    const int64_t i = full * 8;
+    const int m = (int)(n - i);
     float v[8], r[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       v[j] = j < m ? load1(x + i + j) : 0.f;
       r[j] = j < m && res ? load1(res + i + j) : 0.f;
     }
-    if (d.thr) drop8(d, (uint64_t)b, d.scale, v);
+    if (d.thr) drop8(d, (uint64_t)full, d.scale, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (j < m) store1(y + i + j, res ? v[j] + r[j] : v[j]);
