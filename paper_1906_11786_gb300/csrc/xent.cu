@@ -687,7 +687,7 @@ struct FCfg {
 };
 
 struct FwdBars {
-  uint64_t a_full, a_empty, full[6], empty[6], s_full[2], s_empty[2], q_full, drain;
+  uint64_t a_full, a_empty, full[6], empty[6], s_full[2], s_empty[2], q_full[2], drain;
   uint32_t tmem;
   int abort;
 };
@@ -741,8 +741,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->s_full[b], 1);
       mbar_init(&bars->s_empty[b], 16);
+      mbar_init(&bars->q_full[b], 16);
     }
-    mbar_init(&bars->q_full, 16);
     mbar_init(&bars->drain, 1);
     bars->abort = 0;
     fence_mbar_init();
@@ -904,11 +904,20 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         // the sum's reference is m itself, so that fwd_finish undoes exactly what was done here
         const int64_t slot = (int64_t)w.t * 128 + r;
         if (un.whole(blockIdx.x, w.t)) {
+          // The first warpgroup waits for all four quarters.  Tiles take turns at two barriers, and a warp
+          // arrives for a tile only once all warps have for the one before: nothing else keeps the other
+          // warpgroups, which do not wait here, from arriving for the next tile in a slow warp's place (a
+          // tile may be a single unit, and the accumulator is free before its sum is done).
+          auto quarters = [&](uint32_t tile) {
+            return __all_sync(0xffffffffu, mbar_wait(&bars->q_full[tile & 1], (tile >> 1) & 1, a.status, 707, abort,
+                                                     32));
+          };
+          if (finished > 0 && !quarters(finished - 1)) break;
           a.full[wg * a.cap + slot] = make_float2(m, l);
           __syncwarp();
-          if (lane == 0) mbar_arrive(&bars->q_full);
+          if (lane == 0) mbar_arrive(&bars->q_full[finished & 1]);
           if (wg == 0) {
-            if (!__all_sync(0xffffffffu, mbar_wait(&bars->q_full, finished & 1, a.status, 707, abort, 32))) break;
+            if (!quarters(finished)) break;
             float2 p[4];
             for (int k = 0; k < 4; ++k) p[k] = a.full[k * a.cap + slot];
             const float top = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x));

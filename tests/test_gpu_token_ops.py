@@ -377,6 +377,32 @@ def test_xent_of_larger_shapes(dtype, grad):
     check_xent(dtype, grad, *xent_inputs(3001, 256, 9001, dtype, 0.9))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 70, 130, 256, 257, 700, 1024])
+def test_xent_of_many_rows_against_few_tokens(dtype, V):
+    """Several tiles of rows a block, each of one to four pieces of the vocabulary: the four quarters of a
+    tile's columns are joined within the block, whose warps do not wait for one another otherwise.  Every
+    row, twenty times over."""
+    n, H = 150001, 32
+    X, W, target, g = xent_inputs(n, H, V, dtype, 0.9)
+    t = torch.from_numpy(target).cuda()
+    ws = torch.empty(L.xent_workspace_bytes(dtype, n, H, V, L.BG_OP_XENT_FWD), device="cuda",
+                     dtype=torch.uint8)
+    z = X.double() @ W.double().T
+    ok = t >= 0
+    want_lse = torch.where(ok, torch.logsumexp(z, 1), 0.0)
+    want = torch.where(ok, want_lse - z.gather(1, t.clamp(min=0).long()[:, None])[:, 0], 0.0)
+    zabs = float((X.double().abs() @ W.double().abs().T).max())
+    tol = 2 * (2 * H * U + 2.0 ** -21) * zabs + 2.0 ** -20 * (1 + want_lse.abs())
+    for _ in range(20):
+        loss, lse = (torch.full((n,), float("nan"), device="cuda") for _ in range(2))
+        L.xent_fwd(dtype, X, W, t, loss, lse, ws)
+        for got, right in ((lse, want_lse), (loss, want)):
+            over = (got.double() - right).abs() - tol
+            assert float(over.max()) <= 0, (int(over.argmax()), float(over.max()))
+    L.check_device()
+
+
 @pytest.mark.parametrize("dtype,grad", TYPES)
 def test_xent_of_confident_and_of_wrong_rows(dtype, grad):
     """Logits in the hundreds: softmax is all but one-hot, right or wrong, and nothing overflows."""
