@@ -228,6 +228,50 @@ def test_embed_bwd(n, H, V, kind):
         assert torch.equal(acc, base + got), "BG_ACCUM adds the finished sum"
 
 
+# (rows, H, V): the largest sort of one cluster; then counting passes of many blocks: two and three
+# passes, one tile of keys a block and several, all keys of one digit
+SORTS = [(32768, 32, 600, "uniform"), (32769, 32, 600, "uniform"), (40001, 64, 5000, "one"),
+         (100003, 64, 49999, "zipf"), (50001, 32, 300000, "zipf"), (330000, 32, 1 << 18, "uniform"),
+         (700001, 32, 5000, "zipf")]
+
+
+@pytest.mark.parametrize("n,H,V,kind", SORTS)
+def test_embed_bwd_of_many_ids(n, H, V, kind):
+    """Integers as gradients: every sum is exact in fp32, so that a row in the wrong place, lost or taken
+    twice shows, whatever the order of additions."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    ids = torch.from_numpy(make_ids(np.random.default_rng(n + V), n, V, kind)).cuda()
+    dout = torch.randint(-9, 10, (n, H), generator=gen, device="cuda").float()
+    dout[ids < 0] = float("nan")  # padding rows are not read
+    want = torch.zeros(V, H, device="cuda", dtype=torch.float64)
+    want.index_add_(0, ids[ids >= 0].long(), dout[ids >= 0].double())
+    ws = torch.empty(L.embed_workspace_bytes(n, H, V), device="cuda", dtype=torch.uint8)
+    for fill in (0xA5, 0x5A):
+        got = torch.full((V, H), float("nan"), device="cuda")
+        ws.fill_(fill)
+        L.embed_bwd(ids, dout, got, ws, scale=2.0)
+        assert torch.equal(got.double(), 2.0 * want)
+    base = torch.randint(-9, 10, (V, H), generator=gen, device="cuda").float()
+    acc = base.clone()
+    L.embed_bwd(ids, dout, acc, ws, scale=2.0, flags=L.BG_ACCUM)
+    assert torch.equal(acc.double(), base + 2.0 * want)
+    # real values with dropout: the same bits again, and the sums of the formula
+    real = torch.randn(n, H, generator=gen, device="cuda")
+    outs = []
+    for fill in (0xA5, 0x5A):
+        outs.append(torch.full((V, H), float("nan"), device="cuda"))
+        ws.fill_(fill)
+        L.embed_bwd(ids, real, outs[-1], ws, scale=0.6, p=0.3, seed=SEED, call=CALL)
+    assert torch.equal(*outs)
+    kept = torch.from_numpy(ref.drop(np.ones((n, H)), 0.3, SEED, CALL)).cuda() * real.double()
+    ok = ids >= 0
+    want, mag = (torch.zeros(V, H, device="cuda", dtype=torch.float64).index_add_(
+        0, ids[ok].long(), v[ok] * float(np.float32(0.6))) for v in (kept, kept.abs()))
+    count = torch.bincount(ids[ok].long(), minlength=V).double()[:, None]
+    within(host(outs[0]), host(want), host((count + 3) * U * mag))
+    L.check_device()
+
+
 def test_embed_gradient_is_the_adjoint():
     """<embed(D), G> = <D, embed_bwd(G)>: the lookup is linear in its table, so differences of it are
     the lookup itself.  Both sides are sums of n H products of fp32 values with a few roundings each."""
@@ -401,6 +445,14 @@ def test_xent_of_many_rows_against_few_tokens(dtype, V):
             over = (got.double() - right).abs() - tol
             assert float(over.max()) <= 0, (int(over.argmax()), float(over.max()))
     L.check_device()
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+@pytest.mark.parametrize("n,H,V,share", [(40001, 96, 300, 0.9), (70001, 32, 130, 0.9),
+                                         (600001, 32, 40, 0.5)])
+def test_xent_of_many_rows(dtype, grad, n, H, V, share):
+    """Rows that are counted before they are gathered, in blocks of 64, of 256 and of two times 256."""
+    check_xent(dtype, grad, *xent_inputs(n, H, V, dtype, share))
 
 
 @pytest.mark.parametrize("dtype,grad", TYPES)
