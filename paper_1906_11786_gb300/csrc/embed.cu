@@ -3,11 +3,13 @@
 //
 // Every kernel here moves bytes and does little arithmetic; a thread works on 8 consecutive
 // elements, the elements of one generator block (philox.h), as one 16-byte (bf16) or two 16-byte
-// (fp32) accesses.  Measured (GB300; a 67 MB fill takes 20.6 us there, a copy 27.5 us): dropout of 33.5 M
-// bf16 elements with residual 34 us (201 MB, 5.9 TB/s), of 25.6 M fp32 gradients 36 us (205 MB); lookup of
-// 131072 x 256 bf16 states 23 us, with dropout 28 (67 MB written; the generator's integer work shows);
-// table gradient of 131071 x 256 over 49999 tokens 75 us, of which the sums take 43 (134 MB read,
-// 51 written), sorting 20, joining 6.
+// (fp32) accesses.  Measured (GB300; a fill of 67 MB takes 12.4 us there, of 134 MB 20.7): dropout of 33.5 M
+// bf16 elements with residual 34 us (201 MB, 5.9 TB/s), of 25.6 M fp32 gradients 37 us (205 MB); lookup of
+// 131072 x 256 bf16 states 23 us, with dropout 29 (67 MB written), of fp32 states 33-35 (134 MB written);
+// table gradient of 131071 x 256 over 49999 tokens 75 us a pass (134 MB read, 51 written).  Its kernels one by
+// one, caches cold (ncu): sorting 31 us, sums 34-37 (3.9 TB/s), joining 12.  No unit is full in the lookup
+// (with dropout: issue slots 70%, ALU 57%): the way from an id to its row to the store is hidden by other
+// warps alone.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -8,14 +8,17 @@
 //                               nothing after this and may hold anything), and the operands' 16-bit forms;
 //                               a few microseconds, bytes and latency
 //   k_xent_fwd (+ join)         128 x 256 tiles of z in tensor memory, sum of exponentials.  65537 rows x
-//                               49999: 0.87 ms at H = 256, bound by the product (tensor pipe 92% active,
-//                               0.87 ms at the measured peak); 0.62 ms at H = 64, bound by the epilogue
-//                               (exponentials: 59% of the special-function rate, issue slots 52%)
+//                               49999: 0.88 ms at H = 256, bound by the product (tensor pipe 92% active,
+//                               0.87 ms at the measured peak); 0.63 ms at H = 64, in the epilogue, no unit
+//                               of it full (special functions 59% of their rate, issue slots 52%): its 16
+//                               warps work on one accumulator in step and wait for the special functions'
+//                               queue together
 //   k_xent_bwd (+ join)         128 x 128 tiles of z recomputed, P written back over z in tensor
 //                               memory as the A operand of the second product; some CTAs with the rows
 //                               of X staying (dX), the others with the rows of W (dW).  The same shape:
-//                               3.7 ms at H = 256 for four products (3.5 at the measured peak; tensor
-//                               pipe 80%), 1.55 ms at H = 64 (epilogue: issue slots 68%)
+//                               4.0 ms at H = 256 for four products (3.5 at the measured peak; tensor
+//                               pipe 78%), 1.56 ms at H = 64 (epilogue: issue slots 67%); with fp32
+//                               gradients 6.6 ms and 2.66 (six products)
 // A staying tile of 128 rows against one passing tile is a unit; the units of a launch, staying tile
 // by staying tile, are cut into as many equal runs as there are SMs, so one row or a hundred thousand
 // fill the card alike.  A staying tile whose units fall to several CTAs leaves partial results, which
@@ -28,7 +31,7 @@
 //                  fp16 (down to 2^-29 of the largest), and P, as the sum of two fp16 terms, keeps 21 bits;
 //                  fp16 and bf16 operands cannot be mixed in one product
 //   fp16, 2 terms  fp32 X and W, each the sum of two fp16 terms (22 bits, down to 2^-17 of the largest,
-//                  below that an absolute 2^-40 of it); products of the two low terms (2^-22) are left out
+//                  below that off by 2^-39 of it at most); products of the two low terms (2^-22) are left out
 // The largest is that of a row of X, and that of all of W.  X's exponents go with the rows' statistics (as
 // W's could not: a row of X is a thread's in the forward, a row of W a column, whose factor would have to
 // be read for each of its logits); one exponent for all of X lost other rows' bits to one large row.
@@ -1027,7 +1030,8 @@ struct BCfg {
   // H = 128 1204 -> 1140; bf16 gradients, H = 256 3950 -> 3910.  With bf16 gradients the path apart takes
   // back at H = 64 what the branch gains (1690 -> 1550 with the branch alone, 1686 with both).  At H = 128,
   // where the two products take the tensor cores as long as each other and the epilogue is not what is
-  // waited for, either costs (1970 -> 2120).
+  // waited for, either costs (1970 -> 2120).  At H = 192 the branch gains (3120 -> 3000) and the path apart
+  // makes no difference (fp32 forms: neither does).
   static constexpr bool APART = KEEP || HC > 2;
   static constexpr bool UNIFORM = KEEP || HC != 2;
   static constexpr int S_BYTES = T * HC * 16384;
