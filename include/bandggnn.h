@@ -386,6 +386,55 @@ int bg_xent_bwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, 
                 const int32_t* target, const float* lse, const float* dloss, bg_dtype grad_dtype,
                 void* dX, void* dW, uint32_t flags, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- answers (device) -----------------------------------------------------------------------
+ * What a model over token-labelled nodes answers with, and what another learns from such answers: the
+ * logits of states against the vocabulary, their adjustment, the largest of each row (rows n, V and the
+ * status word as for the token operators).  Logits lie in rows of V elements, ldz (ldo) elements
+ * apart, V or more and at most 2^31; the elements between rows are neither read nor written.
+ *
+ * bg_logits_fwd: Z[i][v] = X[i] . W[v].  X [n, H] and W [V, H] dtype, Z [n] rows of out_dtype.  bf16 X and W
+ * enter as they are; fp32 ones with 22 bits, down to 2^-17 of the largest magnitude in their row, smaller
+ * elements are off by up to 2^-39 of that magnitude.  A row of X or W that is not finite makes its own logits
+ * NaN and no others.  ws may be NULL where bg_logits_workspace_bytes is 0 (bf16). */
+size_t bg_logits_workspace_bytes(bg_dtype dtype, int64_t n, int32_t H, int32_t V);
+int bg_logits_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
+                  bg_dtype out_dtype, int64_t ldz, void* Z, void* ws, size_t ws_bytes, void* stream);
+
+/* An adjustment of logits: any of a bias, penalties for repeated tokens and masks (all zero: none).  The
+ * adjusted logit of token v in row i is, in fp32 and with every operation rounded by itself,
+ *   z1 = z + bias[v];
+ *   c = how often v occurs in the row's history, and where c > 0
+ *   z1 = (z1 > 0 ? z1 / rep : z1 * rep) - (presence + frequency * c);
+ *   z1 where bit v % 32 of word v / 32 of the row's mask is set, -inf (whatever z1 is) where it is not.
+ * Device pointers.  Tokens of a history below 0 are skipped; those of V or more too, and they are reported by
+ * bg_check_device as BG_EDEVICE (site 132).  A row whose mask number is n_masks or more has no mask (reported,
+ * site 133), one whose offsets fall or leave the history has none (site 134). */
+struct bg_adjust {
+  const float* bias;          /* [V] or NULL */
+  const uint32_t* mask;       /* [n_masks][ceil(V / 32)] or NULL */
+  int32_t n_masks;
+  const int32_t* mask_row;    /* [n] mask of each row, negative: none; NULL: mask 0 for all rows where n_masks
+                                 is 1, else mask i for row i */
+  const int32_t* history;     /* [history_len] tokens of all rows' histories */
+  int64_t history_len;
+  const int64_t* history_off; /* [n + 1] row i's are history_off[i] .. history_off[i + 1] - 1; or NULL */
+  const float* penalty;       /* [n][3] repetition (above 0; 1: none), presence and frequency of each row; with
+                                 history_off only */
+};
+typedef struct bg_adjust bg_adjust;
+
+/* out = the adjusted logits, rounded once to dtype.  out may be Z (with ldo = ldz). */
+int bg_logits_adjust(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const void* Z,
+                     const bg_adjust* adjust, int64_t ldo, void* out, void* stream);
+
+/* The K in [1, 128] largest adjusted logits of each row in falling order, equal ones in the order of their
+ * tokens (0 and -0 are equal), and the log-sum-exp of all of them: top_logit [n, K] fp32, top_id [n, K], lse
+ * [n] or NULL.  adjust may be NULL.  Logits that are -inf or NaN are not answers: places past the last
+ * answer have top_id -1 and top_logit -inf (a row whose mask leaves nothing: all of them, and lse -inf).
+ * lse is NaN where a logit is NaN, +inf or 2^127 or more; logits below -2^127 count as -inf in it. */
+int bg_logits_top(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const void* Z, const bg_adjust* adjust,
+                  int32_t K, float* top_logit, int32_t* top_id, float* lse, void* stream);
+
 /* ---- diagnostics --------------------------------------------------------------------------- */
 const char* bg_last_error(void);
 /* Synchronise `stream` and read the device status word that bounded waits and in-kernel checks

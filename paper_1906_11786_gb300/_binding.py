@@ -67,6 +67,13 @@ class bg_grads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("dW", "db", "dW_ih", "dW_hh", "db_ih", "db_hh")]
 
 
+class bg_adjust(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("n_masks", ctypes.c_int32),
+                ("mask_row", ctypes.c_void_p), ("history", ctypes.c_void_p),
+                ("history_len", ctypes.c_int64), ("history_off", ctypes.c_void_p),
+                ("penalty", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -123,6 +130,10 @@ def load(path: str = LIB_PATH):
         "bg_xent_fwd": (c.c_int, [c.c_int, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
         "bg_xent_bwd": (c.c_int, [c.c_int, i64, i32, i32, vp, vp, vp, vp, vp, c.c_int, vp, vp,
                                   c.c_uint32, vp, sz, vp]),
+        "bg_logits_workspace_bytes": (sz, [c.c_int, i64, i32, i32]),
+        "bg_logits_fwd": (c.c_int, [c.c_int, i64, i32, i32, vp, vp, c.c_int, i64, vp, vp, sz, vp]),
+        "bg_logits_adjust": (c.c_int, [c.c_int, i64, i32, i64, vp, vp, i64, vp, vp]),
+        "bg_logits_top": (c.c_int, [c.c_int, i64, i32, i64, vp, vp, i32, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -518,6 +529,119 @@ def xent_bwd(dtype, X, W, target, lse, dloss, grad_dtype, dX, dW, ws, flags=0, s
                               _shaped(dX, "dX", d, gd, n, H), _shaped(dW, "dW", d, gd, V, H), flags,
                               _on(ws, "ws", d), ws.numel() * ws.element_size(),
                               _stream_of(stream, d)))
+
+
+# --------------------------------------------------------------------------------- answers
+
+
+def _logit_rows(t, name, device, dtype, n, V):
+    """(device pointer, elements between rows) of n rows of V logits, each row's side by side."""
+    if t.dtype is not dtype or t.shape != (n, V):
+        raise ValueError(f"{name} must be {dtype} {(n, V)}, not {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != device:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
+    ld = t.stride(0) if n > 1 else V
+    if (V > 1 and t.stride(1) != 1) or ld < V:
+        raise ValueError(f"{name} must have rows of neighbouring elements, one after the other")
+    return t.data_ptr(), ld
+
+
+class LogitAdjust:
+    """An adjustment of logits (bg_adjust), made once and passed to any number of calls.  The tensors are
+    kept, not copied: what is written into them later counts for later calls.
+
+    bias [V] fp32; mask [masks, ceil(V / 32)] int32, bit v % 32 of word v / 32: token v is allowed; mask_row
+    [n] int32 (negative: no mask; None: the one mask there is, or mask i for row i); history int32,
+    history_off [n + 1] int64 and penalty [n, 3] fp32 (repetition, presence, frequency) belong together."""
+
+    def __init__(self, bias=None, mask=None, mask_row=None, history=None, history_off=None, penalty=None):
+        import torch
+        if (history is None) != (history_off is None) or (history is None) != (penalty is None):
+            raise ValueError("history, history_off and penalty belong together")
+        if mask is None and mask_row is not None:
+            raise ValueError("mask_row without a mask")
+        self._kept = {"bias": bias, "mask": mask, "mask_row": mask_row, "history": history,
+                      "history_off": history_off, "penalty": penalty}
+        types = {"bias": torch.float32, "history_off": torch.int64, "penalty": torch.float32}
+        devices = set()
+        for name, t in self._kept.items():
+            if t is None:
+                continue
+            if t.dtype is not types.get(name, torch.int32):
+                raise ValueError(f"{name} must be {types.get(name, torch.int32)}, not {t.dtype}")
+            _dev_ptr(t, name)
+            devices.add(t.get_device())
+        if len(devices) > 1:
+            raise ValueError("the tensors of an adjustment must be on one device")
+        self._device = devices.pop() if devices else None
+        # what a call's shape must agree with
+        self._V = None if bias is None else tuple(bias.shape)
+        self._words = None if mask is None else tuple(mask.shape)
+        if mask is not None and mask.dim() != 2:
+            raise ValueError(f"mask must be [masks, ceil(V / 32)], not {tuple(mask.shape)}")
+        self._n = [(name, tuple(t.shape), more) for name, t, more in
+                   (("mask_row", mask_row, ()), ("penalty", penalty, (3,))) if t is not None]
+        self._off = None if history_off is None else tuple(history_off.shape)
+        if history is not None and history.dim() != 1:
+            raise ValueError(f"history must have one dimension, not {tuple(history.shape)}")
+        self._c = bg_adjust(_dev_ptr(bias, "bias"), _dev_ptr(mask, "mask"), 0 if mask is None else mask.shape[0],
+                            _dev_ptr(mask_row, "mask_row"), _dev_ptr(history, "history") or None,
+                            0 if history is None else history.numel(), _dev_ptr(history_off, "history_off"),
+                            _dev_ptr(penalty, "penalty"))
+        self._ref = ctypes.addressof(self._c)
+
+    def _for(self, n, V, device):
+        """Address of the C structure for n rows of V logits on the device."""
+        if self._device is not None and self._device != device:
+            raise ValueError(f"adjust is on cuda:{self._device}, the current device is cuda:{device}")
+        if self._V is not None and self._V != (V,):
+            raise ValueError(f"bias must be {(V,)}, not {self._V}")
+        if self._words is not None and self._words[1] != (V + 31) // 32:
+            raise ValueError(f"mask must be [masks, {(V + 31) // 32}], not {self._words}")
+        for name, shape, more in self._n:
+            if shape != (n,) + more:
+                raise ValueError(f"{name} must be {(n,) + more}, not {shape}")
+        if self._off is not None and self._off != (n + 1,):
+            raise ValueError(f"history_off must be {(n + 1,)}, not {self._off}")
+        return self._ref
+
+
+def logits_workspace_bytes(dtype, n, H, V) -> int:
+    return int(load().bg_logits_workspace_bytes(dtype_code(dtype), n, H, V))
+
+
+def logits_fwd(dtype, X, W, out_dtype, Z, ws=None, stream=None):
+    """Z[i][v] = X[i] . W[v]; Z [n, V] of out_dtype may have rows further apart than V.  ws may be None where
+    logits_workspace_bytes is 0."""
+    (dt, td), (ot, od) = _type(dtype), _type(out_dtype)
+    n, (V, H), d = X.shape[0], W.shape, _current_device()
+    z, ld = _logit_rows(Z, "Z", d, od, n, V)
+    _check(load().bg_logits_fwd(dt, n, H, V, _shaped(X, "X", d, td, n, H), _shaped(W, "W", d, td, V, H), ot, ld,
+                                z, None if ws is None else _on(ws, "ws", d),
+                                0 if ws is None else ws.numel() * ws.element_size(), _stream_of(stream, d)))
+
+
+def logits_adjust(dtype, Z, out, adjust, stream=None):
+    """out = Z adjusted (a LogitAdjust); out may be Z."""
+    (dt, td), (n, V), d = _type(dtype), Z.shape, _current_device()
+    z, ldz = _logit_rows(Z, "Z", d, td, n, V)
+    o, ldo = _logit_rows(out, "out", d, td, n, V)
+    _check(load().bg_logits_adjust(dt, n, V, ldz, z, None if adjust is None else adjust._for(n, V, d), ldo, o,
+                                   _stream_of(stream, d)))
+
+
+def logits_top(dtype, Z, top_logit, top_id, lse=None, adjust=None, stream=None):
+    """The K largest adjusted logits of each row of Z and their tokens (top_logit fp32, top_id int32 [n, K]) and
+    the log-sum-exp of all of them (lse [n])."""
+    (dt, td), (_, tf), (_, ti), (n, V), d = _type(dtype), _type(BG_F32), _type("ids"), Z.shape, _current_device()
+    K = top_id.shape[1]
+    z, ldz = _logit_rows(Z, "Z", d, td, n, V)
+    _check(load().bg_logits_top(dt, n, V, ldz, z, None if adjust is None else adjust._for(n, V, d), K,
+                                _shaped(top_logit, "top_logit", d, tf, n, K),
+                                _shaped(top_id, "top_id", d, ti, n, K), _shaped(lse, "lse", d, tf, n),
+                                _stream_of(stream, d)))
 
 
 def check_device(stream=None):

@@ -1,0 +1,145 @@
+// C ABI of the operators that answer with a vocabulary: argument checks and hand-over to their launchers.
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <string>
+
+#include "answer.h"
+#include "internal.h"
+
+namespace {
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+
+#define ANS_PTR(p)                                                                \
+  do {                                                                            \
+    if (!(p)) return bg_fail(BG_EINVAL, #p " is NULL");                           \
+    if (misaligned(p)) return bg_fail(BG_EINVAL, #p " not 16-byte aligned");      \
+  } while (0)
+#define ANS_OPT_PTR(p)                                                            \
+  do {                                                                            \
+    if ((p) && misaligned(p)) return bg_fail(BG_EINVAL, #p " not 16-byte aligned"); \
+  } while (0)
+#define ANS_TRY(call)             \
+  do {                            \
+    const int rc_ = (call);       \
+    if (rc_ != BG_OK) return rc_; \
+  } while (0)
+
+int cuda_rc(cudaError_t e, const char* what) {
+  if (e == cudaSuccess) return BG_OK;
+  return bg_fail(BG_ECUDA, std::string(what) + ": " + cudaGetErrorString(e));
+}
+
+bool is_dtype(bg_dtype dt) { return dt == BG_F32 || dt == BG_BF16; }
+int check_dtype(bg_dtype dt) { return is_dtype(dt) ? BG_OK : bg_fail(BG_EINVAL, "unknown dtype"); }
+
+constexpr int64_t kMaxRows = (int64_t)1 << 29;
+constexpr int32_t kMaxVocab = 1 << 24;
+constexpr int64_t kMaxStride = (int64_t)1 << 31;
+
+bool valid_rows(int64_t n, int32_t V) { return n >= 0 && n <= kMaxRows && V >= 1 && V <= kMaxVocab; }
+bool valid_h(int32_t H) { return H >= 32 && H <= 256 && H % 32 == 0; }
+
+int check_rows(int64_t n, int32_t V) {
+  if (n < 0 || n > kMaxRows) return bg_fail(BG_EINVAL, "n must be in [0, 2^29]");
+  if (V < 1 || V > kMaxVocab) return bg_fail(BG_EINVAL, "V must be in [1, 2^24]");
+  return BG_OK;
+}
+int check_h(int32_t H) {
+  return valid_h(H) ? BG_OK : bg_fail(BG_EINVAL, "H must be a multiple of 32 in [32, 256]");
+}
+int check_stride(const char* name, int64_t ld, int32_t V) {
+  return ld >= V && ld <= kMaxStride ? BG_OK
+                                     : bg_fail(BG_EINVAL, std::string(name) + " must be in [V, 2^31]");
+}
+
+// The adjustment as the launchers take it (an empty one for NULL).
+int check_adjust(const bg_adjust* in, int64_t n, bg_adjust* out) {
+  *out = bg_adjust{};
+  if (!in) return BG_OK;
+  const bg_adjust& adjust = *in;
+  ANS_OPT_PTR(adjust.bias);
+  ANS_OPT_PTR(adjust.mask);
+  ANS_OPT_PTR(adjust.mask_row);
+  ANS_OPT_PTR(adjust.history);
+  ANS_OPT_PTR(adjust.history_off);
+  ANS_OPT_PTR(adjust.penalty);
+  if (adjust.mask) {
+    if (adjust.n_masks < 1) return bg_fail(BG_EINVAL, "adjust.n_masks must be 1 or more with a mask");
+    if (!adjust.mask_row && adjust.n_masks != 1 && adjust.n_masks < n)
+      return bg_fail(BG_EINVAL, "adjust.n_masks must be 1 or at least n without adjust.mask_row");
+  } else if (adjust.mask_row || adjust.n_masks) {
+    return bg_fail(BG_EINVAL, "adjust.mask_row or n_masks without adjust.mask");
+  }
+  if (adjust.history_len < 0) return bg_fail(BG_EINVAL, "adjust.history_len < 0");
+  if (!adjust.history_off != !adjust.penalty)
+    return bg_fail(BG_EINVAL, "adjust.history_off and adjust.penalty belong together");
+  if (adjust.history_len > 0 && (!adjust.history || !adjust.history_off))
+    return bg_fail(BG_EINVAL, "adjust.history_len without adjust.history and adjust.history_off");
+  *out = adjust;
+  return BG_OK;
+}
+
+}  // namespace
+
+extern "C" size_t bg_logits_workspace_bytes(bg_dtype dt, int64_t n, int32_t H, int32_t V) {
+  return is_dtype(dt) && valid_rows(n, V) && valid_h(H) ? bg::logits_ws_bytes(dt == BG_BF16, n, H, V) : 0;
+}
+
+extern "C" int bg_logits_fwd(bg_dtype dt, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
+                             bg_dtype out_dt, int64_t ldz, void* Z, void* ws, size_t ws_bytes, void* stream) {
+  bg_clear_error();
+  ANS_TRY(check_dtype(dt));
+  ANS_TRY(check_dtype(out_dt));
+  ANS_TRY(check_rows(n, V));
+  ANS_TRY(check_h(H));
+  ANS_TRY(check_stride("ldz", ldz, V));
+  if (n == 0) return BG_OK;
+  ANS_PTR(X); ANS_PTR(W); ANS_PTR(Z);
+  const size_t need = bg::logits_ws_bytes(dt == BG_BF16, n, H, V);
+  if (need > 0) {
+    ANS_PTR(ws);
+    if (ws_bytes < need) return bg_fail(BG_ECAPACITY, "workspace too small");
+  }
+  bg::LogitsArgs a{dt == BG_BF16, out_dt == BG_BF16, n, H, V, X, W, ldz, Z, ws, nullptr};
+  ANS_TRY(bg_status_word(&a.status));
+  return cuda_rc(bg::logits_fwd(a, (cudaStream_t)stream), "bg_logits_fwd");
+}
+
+extern "C" int bg_logits_adjust(bg_dtype dt, int64_t n, int32_t V, int64_t ldz, const void* Z,
+                                const bg_adjust* adjust, int64_t ldo, void* out, void* stream) {
+  bg_clear_error();
+  bg_adjust adj;
+  ANS_TRY(check_dtype(dt));
+  ANS_TRY(check_rows(n, V));
+  ANS_TRY(check_stride("ldz", ldz, V));
+  ANS_TRY(check_stride("ldo", ldo, V));
+  ANS_TRY(check_adjust(adjust, n, &adj));
+  if (n == 0) return BG_OK;
+  ANS_PTR(Z); ANS_PTR(out);
+  if (out == Z && ldo != ldz) return bg_fail(BG_EINVAL, "in place, ldo must be ldz");
+  int* status = nullptr;
+  ANS_TRY(bg_status_word(&status));
+  return cuda_rc(bg::logits_adjust(dt == BG_BF16, n, V, ldz, Z, adj, ldo, out, status, (cudaStream_t)stream),
+                 "bg_logits_adjust");
+}
+
+extern "C" int bg_logits_top(bg_dtype dt, int64_t n, int32_t V, int64_t ldz, const void* Z,
+                             const bg_adjust* adjust, int32_t K, float* top_logit, int32_t* top_id, float* lse,
+                             void* stream) {
+  bg_clear_error();
+  bg_adjust adj;
+  ANS_TRY(check_dtype(dt));
+  ANS_TRY(check_rows(n, V));
+  ANS_TRY(check_stride("ldz", ldz, V));
+  if (K < 1 || K > bg::kMaxTop) return bg_fail(BG_EINVAL, "K must be in [1, 128]");
+  ANS_TRY(check_adjust(adjust, n, &adj));
+  if (n == 0) return BG_OK;
+  ANS_PTR(Z); ANS_PTR(top_logit); ANS_PTR(top_id); ANS_OPT_PTR(lse);
+  int* status = nullptr;
+  ANS_TRY(bg_status_word(&status));
+  return cuda_rc(bg::logits_top(dt == BG_BF16, n, V, ldz, Z, adj, K, top_logit, top_id, lse, status,
+                                (cudaStream_t)stream),
+                 "bg_logits_top");
+}

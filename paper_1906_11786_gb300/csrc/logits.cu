@@ -1,0 +1,420 @@
+// Logits of states against a vocabulary: Z = X W^T, every one of them written.
+//
+// A tile is 128 tokens x up to 256 rows of X (128 with two terms), computed transposed: the tokens are
+// the rows of tensor memory, so that a warp, a lane a token, writes 32 neighbouring logits of a row of Z
+// at once, whatever the row's length and alignment, without a turn through shared memory.  The tile of X
+// stays in shared memory while W passes through a ring in pieces of 128 rows x 64 elements.
+//
+// bf16 X and W enter the product as they are.  fp32 ones enter as two fp16 terms each (22 bits, down to
+// 2^-17 of the largest magnitude in the row; each row of X and of W has a power of two of its own, undone in
+// the epilogue), three products, the two small ones first, while the accumulator is small and loses little.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "answer.h"
+#include "gemm_tc.h"
+#include "kernels.h"
+#include "tc_util.cuh"
+#include "token.h"
+
+namespace bg {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kThreads = 320;  // 8 epilogue warps, a TMA warp, an MMA warp
+constexpr int kMaxStages = 8;
+
+inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Workspace of the fp32 form: the terms' planes (rows rounded up to whole tiles) and the rows' exponents.
+struct Ws {
+  int64_t cap, vcap;
+  size_t x, w, xe, we, total;
+};
+Ws layout(int bf16, int64_t n, int H, int V) {
+  Ws w{};
+  if (bf16) return w;
+  w.cap = (n + 127) / 128 * 128;
+  w.vcap = ((int64_t)V + 127) / 128 * 128;
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o += al(bytes);
+    return at;
+  };
+  w.x = take((size_t)2 * w.cap * H * 2);
+  w.w = take((size_t)2 * w.vcap * H * 2);
+  w.xe = take((size_t)w.cap * 4);
+  w.we = take((size_t)w.vcap * 4);
+  w.total = o;
+  return w;
+}
+
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+
+// Two fp16 terms of each row of X and W, times 2^(14 - e), e the exponent of the row's largest finite
+// element.  A row is `lanes` = H / 8 threads out of a power of two of them.
+struct SplitArgs {
+  const float* src[2];
+  uint16_t* dst[2];
+  int32_t* exps[2];
+  int64_t rows[2], plane[2];
+  int H, width;
+};
+__global__ void __launch_bounds__(256) k_logits_split(SplitArgs a) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int lanes = a.H / 8, q = threadIdx.x & (a.width - 1), per = 256 / a.width;
+  int64_t row = (int64_t)blockIdx.x * per + threadIdx.x / a.width;
+  const int which = row >= a.rows[0];
+  if (which) row -= a.rows[0];
+  const bool in = row < a.rows[which] && q < lanes;
+  float v[8];
+  uint32_t top = 0;
+  if (in) {
+    const float4* p = reinterpret_cast<const float4*>(a.src[which] + row * a.H) + 2 * q;
+    const float4 x = p[0], y = p[1];
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t b = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+      if (b < 0x7F800000u) top = max(top, b);
+    }
+  }
+  for (int o = a.width / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (!in) return;
+  const int e = max((int)(top >> 23) - 127, -100);
+  const float up = pow2(14 - e);
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float x = v[2 * j] * up, y = v[2 * j + 1] * up;
+    const __half2 h = __floats2half2_rn(x, y);
+    hi[j] = *reinterpret_cast<const uint32_t*>(&h);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+    lo[j] = *reinterpret_cast<const uint32_t*>(&l);
+  }
+  uint16_t* d = a.dst[which] + row * a.H + q * 8;
+  *reinterpret_cast<uint4*>(d) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  *reinterpret_cast<uint4*>(d + a.plane[which] * a.H) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  if (q == 0) a.exps[which][row] = e - 14;
+}
+
+template <int HC, int T>
+struct Cfg {
+  static constexpr int RN = T == 1 ? 256 : 128;  // rows of X of a tile
+  static constexpr int XPIECE = RN * 128;        // 64 elements of each
+  static constexpr int X_BYTES = T * HC * XPIECE;
+  static constexpr int PIECE = 16384;
+  static constexpr int ROOM = (232448 - 2048 - X_BYTES) / PIECE;
+  static constexpr int ST = ROOM < kMaxStages ? ROOM : kMaxStages;
+  static constexpr int SMEM = X_BYTES + ST * PIECE + 2048;
+  // (the pieces of the high terms of a tile of W are used twice and stay in the ring until then)
+  static_assert(ST > HC && SMEM <= 232448, "shared memory");
+};
+
+struct Bars {
+  uint64_t x_full, x_empty, full[kMaxStages], empty[kMaxStages], d_full[2], d_empty[2], drain;
+  uint32_t tmem;
+  int abort;
+};
+
+struct Args {
+  int V, vt, stream;  // vt: tiles of W; stream: results do not stay in the cache
+  int64_t n, units, cap, vcap, ldz;
+  const int32_t* xe;
+  const int32_t* we;
+  int* status;
+};
+
+// Unit u is tile u / vt of X against tile u % vt of W; CTA c takes a run of them.
+struct Walk {
+  int64_t u, end;
+  int64_t rt;
+  int v, vt;
+  bool fresh;  // first unit of its tile of X
+  __device__ Walk(const Args& a) : vt(a.vt) {
+    u = a.units * blockIdx.x / gridDim.x;
+    end = a.units * (blockIdx.x + 1) / gridDim.x;
+    rt = u / vt;
+    v = (int)(u - rt * vt);
+    fresh = true;
+  }
+  __device__ bool more() const { return u < end; }
+  __device__ bool last_of_tile() const { return u + 1 == end || v + 1 == vt; }
+  __device__ void next() {
+    ++u;
+    fresh = false;
+    if (++v == vt) v = 0, ++rt, fresh = true;
+  }
+};
+
+template <bool STREAM>
+__device__ __forceinline__ void put(float* p, float x) {
+  if (STREAM) __stcs(p, x); else *p = x;
+}
+template <bool STREAM>
+__device__ __forceinline__ void put(__nv_bfloat16* p, float x) {
+  const __nv_bfloat16 h = __float2bfloat16(x);
+  if (STREAM)
+    __stcs(reinterpret_cast<unsigned short*>(p), *reinterpret_cast<const unsigned short*>(&h));
+  else
+    *p = h;
+}
+
+// 32 rows of Z (of which `rows` exist) from a warp's lanes' tokens.
+template <int T, bool STREAM, typename O>
+__device__ __forceinline__ void write32(const uint32_t* d, O* p, int64_t ldz, int rows, bool mine, int we,
+                                        int xe) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    float z = __uint_as_float(d[j]);
+    if (T == 2) {  // in two steps: the power of two may be outside fp32's range where the logit is not
+      const int e = we + __shfl_sync(0xffffffffu, xe, j), h = e >> 1;
+      z = z * pow2(h) * pow2(e - h);
+    }
+    if (mine && j < rows) put<STREAM>(p + j * ldz, z);
+  }
+}
+
+template <int HC, int T, typename O>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_logits(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
+             const __grid_constant__ Args a, O* Z) {
+  using C = Cfg<HC, T>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem =
+      reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = smem + C::X_BYTES;
+  Bars* bars = reinterpret_cast<Bars*>(ring + C::ST * C::PIECE);
+  volatile int* abort = &bars->abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(&bars->x_full, 1);
+    mbar_init(&bars->x_empty, 1);
+    for (int s = 0; s < C::ST; ++s) {
+      mbar_init(&bars->full[s], 1);
+      mbar_init(&bars->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&bars->d_full[b], 1);
+      mbar_init(&bars->d_empty[b], 8);
+    }
+    mbar_init(&bars->drain, 1);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc(&bars->tmem, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  grid_dep_launch();
+  grid_dep_wait();
+  const uint32_t tmem = bars->tmem;
+  Walk w(a);
+
+  if (warp == 8) {
+    if (lane == 0) {
+      tma_prefetch_desc(&tmX);
+      tma_prefetch_desc(&tmW);
+      uint32_t it = 0, seg = 0;
+      bool ok = true;
+      for (; w.more() && ok; w.next()) {
+        if (w.fresh) {
+          ok = seg == 0 || mbar_wait(&bars->x_empty, (seg - 1) & 1, a.status, 721, abort, 32);
+          if (!ok) break;
+          mbar_expect_tx(&bars->x_full, C::X_BYTES);
+          for (int p = 0; p < T * HC; ++p)
+            tma_load_2d(smem + p * C::XPIECE, &tmX, &bars->x_full, p % HC * 64,
+                        (int)(p / HC * a.cap + w.rt * C::RN));
+          ++seg;
+        }
+        // two terms: the low one's pieces, then the high one's
+        for (int p = 0; p < T * HC && ok; ++p, ++it) {
+          const int s = it % C::ST;
+          ok = mbar_wait(&bars->empty[s], ((it / C::ST) & 1) ^ 1, a.status, 722, abort, 32);
+          if (!ok) break;
+          mbar_expect_tx(&bars->full[s], C::PIECE);
+          tma_load_2d(ring + s * C::PIECE, &tmW, &bars->full[s], p % HC * 64,
+                      (int)(T == 2 && p < HC ? a.vcap : 0) + w.v * 128);
+        }
+      }
+      if (*abort) {  // copies in flight land before the block leaves
+        for (uint32_t k = 0; seg && k < (1u << 22) && !mbar_try(&bars->x_full, (seg - 1) & 1); ++k) {
+        }
+        for (uint32_t q = it > C::ST ? it - C::ST : 0; q < it; ++q)
+          for (uint32_t k = 0; k < (1u << 22) && !mbar_try(&bars->full[q % C::ST], (q / C::ST) & 1); ++k) {
+          }
+      }
+    }
+  } else if (warp == 9) {
+    const bool leader = elect_one_sync();
+    const uint64_t X = desc_sw128_kmajor(smem_u32(smem)), R = desc_sw128_kmajor(smem_u32(ring));
+    uint32_t it = 0, seg = 0, k = 0;
+    bool ok = true;
+    for (; w.more() && ok; w.next(), ++k) {
+      if (w.fresh) {
+        ok = mbar_wait(&bars->x_full, seg & 1, a.status, 723, abort);
+        ++seg;
+      }
+      const int b = k & 1;
+      ok = ok && mbar_wait(&bars->d_empty[b], ((k >> 1) & 1) ^ 1, a.status, 724, abort);
+      const int rows = (int)min((int64_t)C::RN, a.n - w.rt * C::RN), N = (rows + 15) & ~15;
+      const uint32_t idesc = T == 1 ? idesc_bf16_f32(128, N) : idesc_f16_f32(128, N);
+      // piece p of W (in ring stage s) by the term of X that begins at piece xp
+      auto product = [&](int s, int xp, bool more) {
+        const uint64_t ad = R + s * (C::PIECE >> 4), bd = X + (uint64_t)xp * (C::XPIECE >> 4);
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_ss(tmem + b * 256, ad + kk * 2, bd + kk * 2, idesc, more || kk > 0);
+        }
+      };
+      // (past H the pieces hold zeros)
+      for (int p = 0; p < T * HC && ok; ++p) {
+        const uint32_t i = it + p;
+        ok = mbar_wait(&bars->full[i % C::ST], (i / C::ST) & 1, a.status, 725, abort);
+        if (!ok) break;
+        tc_fence_after();
+        // low x high, then high x low; the high terms' pieces stay for high x high
+        product(i % C::ST, p, p > 0);
+        if (leader && (T == 1 || p < HC)) tc_commit(&bars->empty[i % C::ST]);
+        __syncwarp();
+      }
+      if (T == 2 && ok)
+        for (int p = 0; p < HC; ++p) {
+          const uint32_t i = it + HC + p;
+          product(i % C::ST, p, true);
+          if (leader) tc_commit(&bars->empty[i % C::ST]);
+          __syncwarp();
+        }
+      it += T * HC;
+      if (ok && leader) {
+        tc_commit(&bars->d_full[b]);
+        if (w.last_of_tile()) tc_commit(&bars->x_empty);
+      }
+      __syncwarp();
+    }
+    if (leader) tc_commit(&bars->drain);
+    __syncwarp();
+    for (uint32_t q = 0; q < (1u << 24) && !mbar_try(&bars->drain, 0); ++q) {
+    }
+  } else {
+    const int q = warp & 3, half = warp >> 2;
+    const uint32_t base = tmem + ((uint32_t)(q * 32) << 16);
+    uint32_t k = 0;
+    for (; w.more(); w.next(), ++k) {
+      const int b = k & 1, v = w.v * 128 + q * 32 + lane;
+      const int64_t row0 = w.rt * C::RN;
+      const int rows = (int)min((int64_t)C::RN, a.n - row0);
+      const bool mine = v < a.V;
+      const int we = T == 2 && mine ? a.we[v] : 0;
+      const bool ok = mbar_wait(&bars->d_full[b], (k >> 1) & 1, a.status, 726, abort, 20);
+      if (__any_sync(0xffffffffu, !ok)) break;
+      tc_fence_after();
+      O* p = Z + (row0 + half * 32) * a.ldz + v;
+      for (int c = half * 32; c < rows; c += 64, p += 64 * a.ldz) {
+        const int xe = T == 2 && c + lane < rows ? a.xe[row0 + c + lane] : 0;
+        uint32_t d[32];
+        tmem_ld32(base + b * 256 + c, d);
+        tmem_wait_ld();
+        if (a.stream)
+          write32<T, true>(d, p, a.ldz, rows - c, mine, we, xe);
+        else
+          write32<T, false>(d, p, a.ldz, rows - c, mine, we, xe);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->d_empty[b]);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int HC, int T, typename O>
+cudaError_t run(const LogitsArgs& l, const Ws& ws, cudaStream_t st) {
+  using C = Cfg<HC, T>;
+  char* base = static_cast<char*>(l.ws);
+  CUtensorMap mx, mw;
+  const bool ok = T == 1 ? make_map_ld(&mx, l.X, l.n, l.H, l.H, C::RN) && make_map_ld(&mw, l.W, l.V, l.H, l.H, 128)
+                         : make_map_ld(&mx, base + ws.x, 2 * ws.cap, l.H, l.H, C::RN) &&
+                               make_map_ld(&mw, base + ws.w, 2 * ws.vcap, l.H, l.H, 128);
+  if (!ok) return cudaErrorInvalidValue;
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = allow_smem(k_logits<HC, T, O>, C::SMEM, done);
+  if (e != cudaSuccess) return e;
+  Args a{};
+  a.V = l.V;
+  a.vt = (l.V + 127) / 128;
+  a.n = l.n;
+  a.units = (l.n + C::RN - 1) / C::RN * a.vt;
+  a.cap = ws.cap;
+  a.vcap = ws.vcap;
+  a.ldz = l.ldz;
+  a.xe = reinterpret_cast<const int32_t*>(base + ws.xe);
+  a.we = reinterpret_cast<const int32_t*>(base + ws.we);
+  a.status = l.status;
+  a.stream = l.n * (int64_t)l.V * (int64_t)sizeof(O) > ((int64_t)64 << 20);
+  const int ctas = (int)std::min<int64_t>(gemm_tn_num_sms(), a.units);
+  e = launch_pdl(k_logits<HC, T, O>, dim3(ctas), dim3(kThreads), C::SMEM, st, mx, mw, a, static_cast<O*>(l.Z));
+  if (e == cudaSuccess) note_launch();
+  return e;
+}
+
+template <int T, typename O>
+cudaError_t run_h(const LogitsArgs& l, const Ws& ws, cudaStream_t st) {
+  switch ((l.H + 63) / 64) {
+    case 1: return run<1, T, O>(l, ws, st);
+    case 2: return run<2, T, O>(l, ws, st);
+    case 3: return run<3, T, O>(l, ws, st);
+    default: return run<4, T, O>(l, ws, st);
+  }
+}
+
+}  // namespace
+
+size_t logits_ws_bytes(int bf16, int64_t n, int H, int V) { return layout(bf16, n, H, V).total; }
+
+cudaError_t logits_fwd(const LogitsArgs& l, cudaStream_t st) {
+  if (l.n == 0) return cudaSuccess;
+  const Ws ws = layout(l.bf16, l.n, l.H, l.V);
+  if (l.bf16)
+    return l.out_bf16 ? run_h<1, __nv_bfloat16>(l, ws, st) : run_h<1, float>(l, ws, st);
+  SplitArgs s{};
+  char* base = static_cast<char*>(l.ws);
+  s.src[0] = static_cast<const float*>(l.X);
+  s.src[1] = static_cast<const float*>(l.W);
+  s.dst[0] = reinterpret_cast<uint16_t*>(base + ws.x);
+  s.dst[1] = reinterpret_cast<uint16_t*>(base + ws.w);
+  s.exps[0] = reinterpret_cast<int32_t*>(base + ws.xe);
+  s.exps[1] = reinterpret_cast<int32_t*>(base + ws.we);
+  s.rows[0] = l.n;
+  s.rows[1] = l.V;
+  s.plane[0] = ws.cap;
+  s.plane[1] = ws.vcap;
+  s.H = l.H;
+  s.width = l.H / 8 <= 4 ? 4 : l.H / 8 <= 8 ? 8 : l.H / 8 <= 16 ? 16 : 32;
+  const int per = 256 / s.width;
+  cudaError_t e = launch_pdl(k_logits_split, dim3((unsigned)((l.n + l.V + per - 1) / per)), dim3(256), 0, st, s);
+  if (e != cudaSuccess) return e;
+  note_launch();
+  return l.out_bf16 ? run_h<2, __nv_bfloat16>(l, ws, st) : run_h<2, float>(l, ws, st);
+}
+
+}  // namespace bg
