@@ -435,6 +435,31 @@ int bg_logits_adjust(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const vo
 int bg_logits_top(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const void* Z, const bg_adjust* adjust,
                   int32_t K, float* top_logit, int32_t* top_id, float* lse, void* stream);
 
+/* Distillation: the cross entropy of states against a teacher's largest logits instead of one token.  Row i has
+ * up to K in [1, 128] entries, token top_id[i][k] with logit top_logit[i][k] (n K at most 2^29); entries with a
+ * negative token or a logit of -inf are none, those with a token of V or more are none either and are reported
+ * (site 135).  With a temperature tau in [0.001, 1000],
+ *   q_i = softmax(top_logit[i] / tau) over its entries,   z = X W^T,   lse[i] = log sum_v exp(z[i][v] / tau),
+ *   loss[i] = tau^2 (sum_k q_ik (log q_ik - z[i][top_id[i][k]] / tau) + lse[i])
+ * (the Kullback-Leibler divergence from the student's whole distribution to the teacher's, times tau^2 so that
+ * gradients keep their size at any tau).  A row without entries is left out: loss, lse and its gradient are 0,
+ * its X is not used.  A token may be in several entries of a row.  The [n, V] logits are never stored; operands
+ * and their precision are as for bg_xent_fwd. */
+#define BG_OP_DISTILL_FWD 7
+#define BG_OP_DISTILL_BWD 8
+size_t bg_distill_workspace_bytes(bg_dtype dtype, int64_t n, int32_t H, int32_t V, int32_t K, int32_t op);
+int bg_distill_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, int32_t K, const void* X, const void* W,
+                   const int32_t* top_id, const float* top_logit, float tau, float* loss, float* lse, void* ws,
+                   size_t ws_bytes, void* stream);
+/* Gradient of sum_i dloss[i] loss[i]; lse is bg_distill_fwd's of the same inputs:
+ *   d[i] = dloss[i] tau (softmax(z[i] / tau) - q_i),   dX = d W,   dW = d^T X,
+ * in grad_dtype, either of them may be NULL (types, flags and precision as for bg_xent_bwd; with bf16 gradients
+ * the entries' own coefficients are fp32).  dloss is not used in rows left out. */
+int bg_distill_bwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, int32_t K, const void* X, const void* W,
+                   const int32_t* top_id, const float* top_logit, float tau, const float* lse,
+                   const float* dloss, bg_dtype grad_dtype, void* dX, void* dW, uint32_t flags, void* ws,
+                   size_t ws_bytes, void* stream);
+
 /* ---- diagnostics --------------------------------------------------------------------------- */
 const char* bg_last_error(void);
 /* Synchronise `stream` and read the device status word that bounded waits and in-kernel checks

@@ -25,6 +25,7 @@ BG_FLOPS_BAND, BG_FLOPS_XFORM, BG_FLOPS_GRU, BG_FLOPS_NNZ = 0, 1, 2, 3
  BG_EXPORT_GATHER, BG_EXPORT_SUPER_EDGES, BG_EXPORT_SUPER_COUNT) = range(8)
 BG_OP_PROPAGATE_FWD, BG_OP_PROPAGATE_BWD, BG_OP_GGNN_FWD, BG_OP_GGNN_BWD, BG_OP_READOUT = range(5)
 BG_OP_XENT_FWD, BG_OP_XENT_BWD = 5, 6
+BG_OP_DISTILL_FWD, BG_OP_DISTILL_BWD = 7, 8
 BG_KID_BAND_FWD, BG_KID_BAND_BWD, BG_KID_GRU_FWD, BG_KID_GRU_BWD, BG_KID_DW = range(5)
 STATUS = {0: "BG_OK", -1: "BG_EINVAL", -2: "BG_ECAPACITY", -3: "BG_ENOMEM", -4: "BG_ECUDA",
           -5: "BG_ETIMEOUT", -6: "BG_EDEVICE", -7: "BG_ESTATE"}
@@ -134,6 +135,10 @@ def load(path: str = LIB_PATH):
         "bg_logits_fwd": (c.c_int, [c.c_int, i64, i32, i32, vp, vp, c.c_int, i64, vp, vp, sz, vp]),
         "bg_logits_adjust": (c.c_int, [c.c_int, i64, i32, i64, vp, vp, i64, vp, vp]),
         "bg_logits_top": (c.c_int, [c.c_int, i64, i32, i64, vp, vp, i32, vp, vp, vp, vp]),
+        "bg_distill_workspace_bytes": (sz, [c.c_int, i64, i32, i32, i32, i32]),
+        "bg_distill_fwd": (c.c_int, [c.c_int, i64, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]),
+        "bg_distill_bwd": (c.c_int, [c.c_int, i64, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, c.c_int, vp, vp,
+                                     c.c_uint32, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -642,6 +647,35 @@ def logits_top(dtype, Z, top_logit, top_id, lse=None, adjust=None, stream=None):
                                 _shaped(top_logit, "top_logit", d, tf, n, K),
                                 _shaped(top_id, "top_id", d, ti, n, K), _shaped(lse, "lse", d, tf, n),
                                 _stream_of(stream, d)))
+
+
+def distill_workspace_bytes(dtype, n, H, V, K, op) -> int:
+    return int(load().bg_distill_workspace_bytes(dtype_code(dtype), n, H, V, K, op))
+
+
+def distill_fwd(dtype, X, W, top_id, top_logit, loss, lse, ws, tau=1.0, stream=None):
+    """loss[i] = tau^2 KL(softmax(top_logit[i] / tau) || softmax(X[i] W^T / tau)); top_id (int32, negative: no
+    entry) and top_logit (fp32) [n, K]; 0 for rows without entries."""
+    (dt, td), (_, tf), (_, ti) = _type(dtype), _type(BG_F32), _type("ids")
+    (n, K), (V, H), d = top_id.shape, W.shape, _current_device()
+    _check(load().bg_distill_fwd(dt, n, H, V, K, _shaped(X, "X", d, td, n, H), _shaped(W, "W", d, td, V, H),
+                                 _shaped(top_id, "top_id", d, ti, n, K),
+                                 _shaped(top_logit, "top_logit", d, tf, n, K), tau,
+                                 _shaped(loss, "loss", d, tf, n), _shaped(lse, "lse", d, tf, n),
+                                 _on(ws, "ws", d), ws.numel() * ws.element_size(), _stream_of(stream, d)))
+
+
+def distill_bwd(dtype, X, W, top_id, top_logit, lse, dloss, grad_dtype, dX, dW, ws, tau=1.0, flags=0,
+                stream=None):
+    """Gradients of sum_i dloss[i] loss[i] in grad_dtype; dX or dW may be None."""
+    (dt, td), (gt, gd), (_, tf), (_, ti) = (_type(dtype), _type(grad_dtype), _type(BG_F32), _type("ids"))
+    (n, K), (V, H), d = top_id.shape, W.shape, _current_device()
+    _check(load().bg_distill_bwd(dt, n, H, V, K, _shaped(X, "X", d, td, n, H), _shaped(W, "W", d, td, V, H),
+                                 _shaped(top_id, "top_id", d, ti, n, K),
+                                 _shaped(top_logit, "top_logit", d, tf, n, K), tau,
+                                 _shaped(lse, "lse", d, tf, n), _shaped(dloss, "dloss", d, tf, n), gt,
+                                 _shaped(dX, "dX", d, gd, n, H), _shaped(dW, "dW", d, gd, V, H), flags,
+                                 _on(ws, "ws", d), ws.numel() * ws.element_size(), _stream_of(stream, d)))
 
 
 def check_device(stream=None):

@@ -143,3 +143,66 @@ extern "C" int bg_logits_top(bg_dtype dt, int64_t n, int32_t V, int64_t ldz, con
                                 (cudaStream_t)stream),
                  "bg_logits_top");
 }
+
+extern "C" size_t bg_distill_workspace_bytes(bg_dtype dt, int64_t n, int32_t H, int32_t V, int32_t K,
+                                             int32_t op) {
+  if (!is_dtype(dt) || !valid_rows(n, V) || !valid_h(H) || K < 1 || K > bg::kMaxTop || n * K > kMaxRows ||
+      (op != BG_OP_DISTILL_FWD && op != BG_OP_DISTILL_BWD))
+    return 0;
+  return bg::distill_ws_bytes(dt == BG_BF16, n, H, V, K, op == BG_OP_DISTILL_BWD);
+}
+
+static int distill_args(bg_dtype dt, int64_t n, int32_t H, int32_t V, int32_t K, const void* X, const void* W,
+                        const int32_t* top_id, const float* top_logit, float tau, void* ws, size_t ws_bytes,
+                        int backward, bg::DistillArgs* a) {
+  ANS_TRY(check_dtype(dt));
+  ANS_TRY(check_rows(n, V));
+  ANS_TRY(check_h(H));
+  if (K < 1 || K > bg::kMaxTop) return bg_fail(BG_EINVAL, "K must be in [1, 128]");
+  if (n * K > kMaxRows) return bg_fail(BG_EINVAL, "n K must be at most 2^29");
+  if (!(tau >= 1e-3f && tau <= 1e3f)) return bg_fail(BG_EINVAL, "tau must be in [0.001, 1000]");  // NaN fails too
+  ANS_PTR(W);
+  if (n > 0) {
+    ANS_PTR(X); ANS_PTR(top_id); ANS_PTR(top_logit); ANS_PTR(ws);
+    if (ws_bytes < bg::distill_ws_bytes(dt == BG_BF16, n, H, V, K, backward))
+      return bg_fail(BG_ECAPACITY, "workspace too small");
+  }
+  *a = bg::DistillArgs{dt == BG_BF16, n, H, V, K, X, W, top_id, top_logit, tau, ws, nullptr};
+  return BG_OK;
+}
+
+extern "C" int bg_distill_fwd(bg_dtype dt, int64_t n, int32_t H, int32_t V, int32_t K, const void* X,
+                              const void* W, const int32_t* top_id, const float* top_logit, float tau,
+                              float* loss, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  bg_clear_error();
+  bg::DistillArgs a;
+  ANS_TRY(distill_args(dt, n, H, V, K, X, W, top_id, top_logit, tau, ws, ws_bytes, 0, &a));
+  if (n == 0) return BG_OK;
+  ANS_PTR(loss); ANS_PTR(lse);
+  ANS_TRY(bg_status_word(&a.status));
+  return cuda_rc(bg::distill_fwd(a, loss, lse, (cudaStream_t)stream), "bg_distill_fwd");
+}
+
+extern "C" int bg_distill_bwd(bg_dtype dt, int64_t n, int32_t H, int32_t V, int32_t K, const void* X,
+                              const void* W, const int32_t* top_id, const float* top_logit, float tau,
+                              const float* lse, const float* dloss, bg_dtype grad_dt, void* dX, void* dW,
+                              uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
+  bg_clear_error();
+  bg::DistillArgs a;
+  ANS_TRY(distill_args(dt, n, H, V, K, X, W, top_id, top_logit, tau, ws, ws_bytes, 1, &a));
+  ANS_TRY(check_dtype(grad_dt));
+  if (flags & ~BG_ACCUM) return bg_fail(BG_EINVAL, "unknown flags");
+  if (dt == BG_F32 && grad_dt != BG_F32)
+    return bg_fail(BG_EINVAL, "fp32 states and table have fp32 gradients");
+  if ((flags & BG_ACCUM) && grad_dt != BG_F32) return bg_fail(BG_EINVAL, "BG_ACCUM needs fp32 gradients");
+  // (without rows dX is empty and may be NULL all the same)
+  if (n > 0 && !dX && !dW) return bg_fail(BG_EINVAL, "dX and dW are NULL");
+  ANS_OPT_PTR(dX); ANS_OPT_PTR(dW);
+  if (n > 0) {
+    ANS_PTR(lse); ANS_PTR(dloss);
+    ANS_TRY(bg_status_word(&a.status));
+  }
+  return cuda_rc(bg::distill_bwd(a, lse, dloss, grad_dt == BG_BF16, dX, dW, (flags & BG_ACCUM) != 0,
+                                 (cudaStream_t)stream),
+                 "bg_distill_bwd");
+}

@@ -208,7 +208,7 @@ struct SumPlan {
   int64_t pieces, blocks;
   int smem;
 };
-SumPlan sum_plan(int64_t n, int H) {
+SumPlan sum_plan(int64_t n, int H, int weighted = 0) {
   SumPlan p;
   p.lanes = H / 8 <= 4 ? 4 : H / 8 <= 8 ? 8 : H / 8 <= 16 ? 16 : 32;
   p.groups = 256 / p.lanes;
@@ -220,11 +220,30 @@ SumPlan sum_plan(int64_t n, int H) {
   p.piece = (int)std::min<int64_t>(kMaxPiece, std::max<int64_t>(8, (piece + 1) / 2 * 2));
   p.pieces = (n + p.piece - 1) / p.piece;
   p.blocks = (p.pieces + p.groups - 1) / p.groups;
-  p.smem = kRing * 8192 + (2 * p.groups * p.piece + 4) * 4;
+  p.smem = kRing * 8192 + ((2 + weighted) * p.groups * p.piece + 4) * 4;
   return p;
 }
 
 inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Where the rows that are summed come from, and what each is multiplied by: the gradient's rows (an id each)
+// under a dropout, or rows that K ids share, with a weight for each id.
+struct GradRows {
+  static constexpr bool kWeighted = false;
+  using T = float;
+  const float* dout;
+  Drop d;
+  __device__ const T* row(int i, int H) const { return dout + (int64_t)i * H; }
+};
+template <typename E>
+struct SharedRows {
+  static constexpr bool kWeighted = true;
+  using T = E;
+  const T* X;
+  const float* weight;
+  uint32_t K;
+  __device__ const T* row(int i, int H) const { return X + (int64_t)i * H; }
+};
 
 struct BwdWs {
   size_t key[2], pos[2], hist, head, tail, total;
@@ -579,15 +598,17 @@ __device__ __forceinline__ void copy16_async(void* dst, const void* src) {
 // The rows of dout come through rings in shared memory, kRing - 1 rows a group ahead.  Held in registers
 // instead, the same number ahead, uniform tokens took 69 us for 131071 x 256 over 49999 (63 now); deeper or
 // shallower rings with fewer or more blocks an SM take up to 5% longer.
+template <typename Src>
 __global__ void __launch_bounds__(256)
     k_embed_sum(int64_t n, int H, int V, SumPlan sp, const int32_t* __restrict__ key,
-                const int32_t* __restrict__ pos, const float* __restrict__ dout, float scale,
-                Drop d, float* __restrict__ dtable, int accumulate, float* __restrict__ head,
-                float* __restrict__ tail) {
+                const int32_t* __restrict__ pos, Src src, float scale, float* __restrict__ dtable,
+                int accumulate, float* __restrict__ head, float* __restrict__ tail) {
+  using T = typename Src::T;
   extern __shared__ __align__(16) uint8_t sum_smem[];
   __shared__ uint8_t occurs[256];
   int* keys = reinterpret_cast<int*>(sum_smem + kRing * 8192);  // [groups * piece + 2]
   int* rows = keys + sp.groups * sp.piece + 2;                  // [groups * piece]
+  float* wts = reinterpret_cast<float*>(rows + sp.groups * sp.piece);  // the same, of weighted rows
   const int g = threadIdx.x / sp.lanes, c = threadIdx.x % sp.lanes, lanes = H / 8;
   grid_dep_launch();
   grid_dep_wait();
@@ -598,7 +619,15 @@ __global__ void __launch_bounds__(256)
     for (int i = threadIdx.x; i < run + 2; i += 256) {
       const int64_t e = first + i - 1;
       keys[i] = e >= 0 && e < n ? key[e] : -1;
-      if (i < run) rows[i] = pos[first + i];
+      if (i < run) {
+        const int p = pos[first + i];
+        if constexpr (Src::kWeighted) {
+          rows[i] = (int)((uint32_t)p / src.K);
+          wts[i] = src.weight[p];
+        } else {
+          rows[i] = p;
+        }
+      }
     }
   __syncthreads();
   const int e0 = g * sp.piece, m = max(0, min(sp.piece, run - e0));
@@ -610,10 +639,11 @@ __global__ void __launch_bounds__(256)
     uint8_t* ring = sum_smem + (threadIdx.x >> 5) * (kRing * 1024) + (threadIdx.x & 31 & ~(sp.lanes - 1)) * 32;
     auto fetch = [&](int i) {
       if (i < m && c < lanes && k0[i] < V) {
-        const float* src = dout + (int64_t)rows[e0 + i] * H;
+        const T* from = src.row(rows[e0 + i], H);
         uint8_t* dst = ring + i % kRing * 1024;
-        copy16_async(dst + c * 16, src + c * 4);
-        copy16_async(dst + (c + lanes) * 16, src + (c + lanes) * 4);
+        constexpr int each = 16 / (int)sizeof(T);  // elements of a copy; 8 a thread in all
+        copy16_async(dst + c * 16, from + c * each);
+        if (sizeof(T) == 4) copy16_async(dst + (c + lanes) * 16, from + (c + lanes) * each);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -622,7 +652,8 @@ __global__ void __launch_bounds__(256)
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     auto finish = [&](bool goes_on) {
       if (cur >= V || c >= lanes) return;
-      const float f = d.thr ? scale * d.scale : scale;
+      float f = scale;
+      if constexpr (!Src::kWeighted) f = src.d.thr ? scale * src.d.scale : scale;
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] *= f;
       if (begun || goes_on) {
@@ -646,10 +677,16 @@ __global__ void __launch_bounds__(256)
         }
         if (k < V && c < lanes) {
           float v[8];
-          load8(reinterpret_cast<const float*>(ring + i % kRing * 1024) + c * 8, v);
-          if (d.thr) drop8(d, (uint64_t)rows[e0 + i] * lanes + c, 1.f, v);
+          load8(reinterpret_cast<const T*>(ring + i % kRing * 1024) + c * 8, v);
+          if constexpr (Src::kWeighted) {
+            const float wt = wts[e0 + i];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] += v[j];
+            for (int j = 0; j < 8; ++j) acc[j] = fmaf(wt, v[j], acc[j]);
+          } else {
+            if (src.d.thr) drop8(src.d, (uint64_t)rows[e0 + i] * lanes + c, 1.f, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += v[j];
+          }
         }
       }
       // the place that the row before this one had: every lane has read it before the barrier above
@@ -758,40 +795,10 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-}  // namespace
-
-cudaError_t dropout_fwd(int bf16, int64_t n, const Drop& d, const void* x, const void* res, void* y,
-                        cudaStream_t st) {
-  return bf16 ? run_dropout<__nv_bfloat16>(n, d, x, res, y, st)
-              : run_dropout<float>(n, d, x, res, y, st);
-}
-
-cudaError_t dropout_bwd(int64_t n, const Drop& d, const float* dy, float* dx, int accumulate,
-                        cudaStream_t st) {
-  return run_dropout<float>(n, d, dy, accumulate ? dx : nullptr, dx, st);
-}
-
-cudaError_t embed_fwd(int bf16, int64_t n, int H, int V, const int32_t* ids, const void* table,
-                      float scale, const Drop& d, void* out, int* status, cudaStream_t st) {
-  if (n == 0) return cudaSuccess;
-  const int rows = 256 / (H / 8) * kEmbedUnroll;
-  const unsigned grid = (unsigned)((n + rows - 1) / rows);
-  if (bf16)
-    k_embed_fwd<__nv_bfloat16><<<grid, 256, 0, st>>>(n, H, V, ids,
-                                                     static_cast<const __nv_bfloat16*>(table), scale,
-                                                     d, static_cast<__nv_bfloat16*>(out), status);
-  else
-    k_embed_fwd<float><<<grid, 256, 0, st>>>(n, H, V, ids, static_cast<const float*>(table), scale,
-                                             d, static_cast<float*>(out), status);
-  note_launch();
-  return cudaGetLastError();
-}
-
-size_t embed_bwd_ws_bytes(int64_t n, int H, int V) { return bwd_ws(n, H, V).total; }
-
-cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* dout, float scale,
-                      const Drop& d, float* dtable, int accumulate, void* ws, int* status,
-                      cudaStream_t st) {
+// Sums the rows of `src` by token: sort, pieces, join.
+template <typename Src>
+cudaError_t sum_by_token(int64_t n, int H, int V, const int32_t* ids, const Src& src, float scale,
+                         float* dtable, int accumulate, void* ws, int* status, cudaStream_t st) {
   if (n == 0)
     return accumulate ? cudaSuccess : cudaMemsetAsync(dtable, 0, (size_t)V * H * sizeof(float), st);
   const SortPlan s = sort_plan(n, V);
@@ -828,15 +835,16 @@ cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* 
   }
   const int32_t* k = key[(s.passes - 1) & 1];
   const int32_t* at = pos[(s.passes - 1) & 1];
-  const SumPlan sp = sum_plan(n, H);
+  const SumPlan sp = sum_plan(n, H, Src::kWeighted);
   // with few rows, blocks for the table's zeros
   const int64_t blocks =
       accumulate ? sp.blocks : std::max<int64_t>(sp.blocks, std::min<int64_t>((V + 127) / 128, 152 * 2));
   static std::atomic<uint64_t> done{0};
-  e = allow_smem(k_embed_sum, kRing * 8192 + (2 * 64 * kMaxPiece + 4) * 4, done);  // the most it takes
+  // (the most it takes)
+  e = allow_smem(k_embed_sum<Src>, kRing * 8192 + ((2 + Src::kWeighted) * 64 * kMaxPiece + 4) * 4, done);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(k_embed_sum, dim3((unsigned)blocks), dim3(256), sp.smem, st, n, H, V, sp, k, at, dout,
-                 scale, d, dtable, accumulate, head, tail);
+  e = launch_pdl(k_embed_sum<Src>, dim3((unsigned)blocks), dim3(256), sp.smem, st, n, H, V, sp, k, at, src,
+                 scale, dtable, accumulate, head, tail);
   if (e != cudaSuccess) return e;
   note_launch();
   if (sp.pieces == 1) return cudaSuccess;
@@ -846,6 +854,56 @@ cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* 
   if (e != cudaSuccess) return e;
   note_launch();
   return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t dropout_fwd(int bf16, int64_t n, const Drop& d, const void* x, const void* res, void* y,
+                        cudaStream_t st) {
+  return bf16 ? run_dropout<__nv_bfloat16>(n, d, x, res, y, st)
+              : run_dropout<float>(n, d, x, res, y, st);
+}
+
+cudaError_t dropout_bwd(int64_t n, const Drop& d, const float* dy, float* dx, int accumulate,
+                        cudaStream_t st) {
+  return run_dropout<float>(n, d, dy, accumulate ? dx : nullptr, dx, st);
+}
+
+cudaError_t embed_fwd(int bf16, int64_t n, int H, int V, const int32_t* ids, const void* table,
+                      float scale, const Drop& d, void* out, int* status, cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  const int rows = 256 / (H / 8) * kEmbedUnroll;
+  const unsigned grid = (unsigned)((n + rows - 1) / rows);
+  if (bf16)
+    k_embed_fwd<__nv_bfloat16><<<grid, 256, 0, st>>>(n, H, V, ids,
+                                                     static_cast<const __nv_bfloat16*>(table), scale,
+                                                     d, static_cast<__nv_bfloat16*>(out), status);
+  else
+    k_embed_fwd<float><<<grid, 256, 0, st>>>(n, H, V, ids, static_cast<const float*>(table), scale,
+                                             d, static_cast<float*>(out), status);
+  note_launch();
+  return cudaGetLastError();
+}
+
+size_t embed_bwd_ws_bytes(int64_t n, int H, int V) { return bwd_ws(n, H, V).total; }
+
+cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* dout, float scale,
+                      const Drop& d, float* dtable, int accumulate, void* ws, int* status,
+                      cudaStream_t st) {
+  return sum_by_token(n, H, V, ids, GradRows{dout, d}, scale, dtable, accumulate, ws, status, st);
+}
+
+size_t token_sum_ws_bytes(int64_t n, int H, int V) { return bwd_ws(n, H, V).total; }
+
+cudaError_t token_sum(int64_t n, int H, int V, const int32_t* ids, int bf16, const void* X, int K,
+                      const float* weight, float* dtable, int accumulate, void* ws, int* status,
+                      cudaStream_t st) {
+  if (bf16)
+    return sum_by_token(n, H, V, ids,
+                        SharedRows<__nv_bfloat16>{static_cast<const __nv_bfloat16*>(X), weight, (uint32_t)K},
+                        1.f, dtable, accumulate, ws, status, st);
+  return sum_by_token(n, H, V, ids, SharedRows<float>{static_cast<const float*>(X), weight, (uint32_t)K}, 1.f,
+                      dtable, accumulate, ws, status, st);
 }
 
 }  // namespace bg

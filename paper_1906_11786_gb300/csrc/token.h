@@ -29,6 +29,21 @@ cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* 
                       const Drop& d, float* dtable, int accumulate, void* ws, int* status,
                       cudaStream_t st);
 
+// dtable[v] (+)= sum over ids[e] == v of weight[e] X[e / K] (X: rows of fp32 or bf16): embed_bwd's sum with
+// weighted rows that K ids share.  ids outside [0, V) name no row.
+size_t token_sum_ws_bytes(int64_t n, int H, int V);
+cudaError_t token_sum(int64_t n, int H, int V, const int32_t* ids, int bf16, const void* X, int K,
+                      const float* weight, float* dtable, int accumulate, void* ws, int* status,
+                      cudaStream_t st);
+
+// Soft targets instead of one token a row (distill.cu): probabilities softmax(z / tau) without a target's
+// one, a row counts where `target` is 0 or more; loss = tau^2 (inner + lse), gradients times tau.
+struct XentSoft {
+  float tau;
+  const float* inner;  // [n] forward
+  const float* add_x;  // bf16 gradients: what is added to dX and dW before they are rounded (or NULL)
+  const float* add_w;
+};
 struct XentArgs {
   int bf16;  // type of X and W
   int64_t n;
@@ -38,6 +53,7 @@ struct XentArgs {
   const int32_t* target;  // [n], < 0: the row is left out
   void* ws;
   int* status;
+  const XentSoft* soft = nullptr;
 };
 size_t xent_ws_bytes(int bf16, int64_t n, int H, int V, int backward);
 // CTAs of a tile kernel on a device of so many SMs, and the workspace that a call takes there: never more
@@ -48,6 +64,15 @@ cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st
 // Gradients in the type grad_bf16 says; dX or dW may be NULL.
 cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, int grad_bf16,
                      void* dX, void* dW, int accumulate, cudaStream_t st);
+
+// The lse that probabilities exp(z - lse) are taken with.  Both z and lse are fp32: from |lse| of 2^20 on their
+// own roundings (2^-19 of them at most) may make the largest probability more than 2, beyond fp16 with its
+// scale, and from 2^26 on infinite, from where one row would spread to all of dW.  Such rows have it raised by
+// as much as that, so that no probability passes 1 (and, far out, all of them are 0).  Cutting them to 1 in
+// the epilogues instead took up to 17% longer.
+__device__ __forceinline__ float safe_lse(float lse) {
+  return lse + fmaxf(fabsf(lse) - 0x1p20f, 0.f) * 0x1p-18f;
+}
 
 // Lets a kernel use `bytes` of dynamic shared memory, once a device.
 template <typename K>

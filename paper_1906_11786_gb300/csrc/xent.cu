@@ -118,11 +118,14 @@ Ws layout(int form, int64_t n, int H, int V, int backward, int ctas) {
 // form: times log2 e), dloss (fp16 forms: times 2^e, e the exponent of the row's largest element, which X's
 // terms lack), the target, and what the row's logits are multiplied by to undo the operands' scales.
 enum { kNlse = 0, kG = 64, kTgt = 128, kDs = 192 };
+constexpr int kNoTarget = -2;  // target of a row that counts and has none (-1: no row)
 __host__ __device__ __forceinline__ int64_t stat_at(int64_t slot) { return slot / 64 * 256 + slot % 64; }
 
 // ------------------------------------------------------------------------------ rows
 struct RowArgs {
   int form, x_bf16, backward, grad_bf16, clear_dx;
+  int soft;            // rows have no target of their own
+  float inv_tau, tau;  // the logits' and the weights' factor (1: plain cross entropy)
   int direct;  // k_xent_rows counts by itself: k_xent_count did not run
   int tb;      // blocks that work on the table
   int64_t n, rb, nb, cap, vcap;
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(256) k_xent_count(RowArgs a) {
     const int e = exp_of(top[tid]);
     a.xexp[i] = (int8_t)e;
     if (a.backward) {
-      const uint32_t b = __float_as_uint(a.dloss[i] * pow2(e)) & 0x7FFFFFFFu;
+      const uint32_t b = __float_as_uint(a.dloss[i] * a.tau * pow2(e)) & 0x7FFFFFFFu;
       if (b < 0x7F800000u) mg = max(mg, b);
     }
   }
@@ -260,15 +263,6 @@ __global__ void __launch_bounds__(256) k_xent_count(RowArgs a) {
     a.counts[blockIdx.x] = s;
     a.amax[blockIdx.x] = mg;
   }
-}
-
-// The lse that probabilities exp(z - lse) are taken with.  Both z and lse are fp32: from |lse| of 2^20 on their
-// own roundings (2^-19 of them at most) may make the largest probability more than 2, beyond fp16 with its
-// scale, and from 2^26 on infinite, from where one row would spread to all of dW.  Such rows have it raised by
-// as much as that, so that no probability passes 1 (and, far out, all of them are 0).  Cutting them to 1 in
-// the epilogues instead took up to 17% longer.
-__device__ __forceinline__ float safe_lse(float lse) {
-  return lse + fmaxf(fabsf(lse) - 0x1p20f, 0.f) * 0x1p-18f;
 }
 
 // 8 elements to the form's terms: plane t of `dst` starts at t * plane.
@@ -364,17 +358,17 @@ __global__ void __launch_bounds__(256) k_xent_rows(RowArgs a) {
       from[k] = i;
       a.row[slot] = (int32_t)i;
       float* st = a.stat + stat_at(slot);
-      st[kTgt] = __int_as_float(t);
+      st[kTgt] = __int_as_float(a.soft ? kNoTarget : t);
       int e = 0;
       if (a.form != kBf16) {
         e = a.xexp[i];
         up[k] = pow2(14 - e);
-        st[kDs] = pow2(max(-126, min(127, e - 14 - shift_of(mw))));
+        st[kDs] = pow2(max(-126, min(127, e - 14 - shift_of(mw)))) * a.inv_tau;
       }
       if (a.backward) {
         const float lse = safe_lse(a.lse_in[i]);
         st[kNlse] = a.form == kBf16 ? -lse * kLog2e : -lse;
-        st[kG] = a.dloss[i] * pow2(e);
+        st[kG] = a.dloss[i] * a.tau * pow2(e);
       }
     } else if (i < r1 && !a.backward) {
       a.loss[i] = 0.f;
@@ -630,6 +624,9 @@ struct FwdArgs {
   int H, V;
   int direct;  // X is the caller's, all n rows of it
   int tiles;   // runs of whole tiles
+  float c;     // bf16 form: log2 e / tau, what logits are multiplied by
+  float tau2;  // soft targets: tau^2
+  const float* inner;  // [n] soft targets: what loss / tau^2 - lse is; else NULL
   int64_t n, cap, vcap;
   const int* head;
   const int32_t* target;  // direct: the caller's
@@ -649,6 +646,7 @@ __device__ __forceinline__ int64_t fwd_rows(const FwdArgs& a) { return a.direct 
 __device__ __forceinline__ int fwd_target(const FwdArgs& a, int64_t s) {
   if (!a.direct) return __float_as_int(a.stat[stat_at(s) + kTgt]);
   int t = s < a.n ? a.target[s] : -1;
+  if (a.inner) return t < 0 ? -1 : kNoTarget;
   if (t >= a.V) {
     if (atomicCAS(a.status, 0, 2) == 0) atomicExch(a.status + 1, kSiteXentTarget);
     t = -1;
@@ -661,7 +659,7 @@ __device__ __forceinline__ void fwd_finish(const FwdArgs& a, int64_t s, int tgt,
   const int64_t i = a.direct ? s : a.row[s];
   if (i < 0 || i >= a.n) return;
   float v = 0.f, loss = 0.f;
-  if (tgt >= 0) {
+  if (tgt != -1) {
     // (top + log2 l) / c with c = kLog2e as it was rounded, 1 / c in two parts, so that the only error
     // that counts is the result's own rounding
     constexpr float inv = (float)(1.0 / (double)kLog2e), rest = (float)(1.0 / (double)kLog2e - (double)inv);
@@ -670,7 +668,7 @@ __device__ __forceinline__ void fwd_finish(const FwdArgs& a, int64_t s, int tgt,
     const float log_l = l == 0.f ? 0.f : log2f(l);
     const float hi = top * inv, lo = fmaf(top, inv, -hi) + fmaf(top, rest, log_l * inv);
     v = hi + lo;
-    loss = (hi - a.hit[s]) + lo;
+    loss = a.inner ? ((hi + a.inner[i]) + lo) * a.tau2 : (hi - a.hit[s]) + lo;
   }
   a.lse[i] = v;
   a.loss[i] = loss;
@@ -840,7 +838,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
   } else {
     // a thread is a row; each warpgroup has 64 columns of a tile
     const int q = warp & 3, wg = warp >> 2, r = q * 32 + lane;
-    float ds = 1.f, c = kLog2e;  // z ds is the logit, z c the same in base 2
+    float ds = 1.f, c = a.c;  // z ds is the logit, z c the same in base 2 (over tau)
     const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + wg * 64;
     float m = -3.0e38f, l = 0.f;
     int tgt = -1;
@@ -993,6 +991,10 @@ struct BwdArgs {
   int split;  // CTAs that compute dX; the others compute dW
   int tiles;  // runs of whole tiles
   int step;   // of the order of dW's tiles
+  float l2e;  // bf16 form: log2 e / tau
+  float tau;
+  const float* add_x;  // bf16 gradients: added before they are rounded (or NULL)
+  const float* add_w;
   int64_t cap, vcap;
   const int* head;
   const int32_t* row;
@@ -1082,9 +1084,9 @@ __device__ __forceinline__ bool hit_row(const float* stat, int i, int first) {
 // P of N columns of a row (a thread's) from their logits, for dX: descale and nlse = -lse of the row, hit =
 // its target's place among the columns, of which the first `valid` exist.
 template <int FORM, int N, int PATH>
-__device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, float nlse, int hit,
+__device__ __forceinline__ void probs_row(uint32_t* v, float log2e, float descale, float up, float nlse, int hit,
                                           int valid) {
-  const uint64_t l2e = pack2(kLog2e, kLog2e), ds = pack2(descale, descale), up2 = pack2(up, up);
+  const uint64_t l2e = pack2(log2e, log2e), ds = pack2(descale, descale), up2 = pack2(up, up);
   const uint64_t nl = pack2(nlse, nlse);
 #pragma unroll
   for (int i = 0; i < N; i += 2) {
@@ -1112,8 +1114,8 @@ __device__ __forceinline__ void probs_row(uint32_t* v, float descale, float up, 
 // columns of every 8, in rows l / 4, + 8, + 16, + 24 of its warp's 32 (l = lane): a quarter of the
 // loads.  v[16 h + 4 g + 2 a + b]: row 16 h + 8 a + l / 4, column 8 g + 2 (l % 4) + b.
 template <int FORM, int N, int PATH>
-__device__ __forceinline__ void probs_col(uint32_t* v, float up, const float* stat, int mine) {
-  const uint64_t l2e = pack2(kLog2e, kLog2e), up2 = pack2(up, up);
+__device__ __forceinline__ void probs_col(uint32_t* v, float log2e, float up, const float* stat, int mine) {
+  const uint64_t l2e = pack2(log2e, log2e), up2 = pack2(up, up);
   const int lane = threadIdx.x & 31, c = 2 * (lane & 3);
   const bool hits = PATH == kEither && hit_row(stat, lane & (N - 1), mine - lane / 4);
 #pragma unroll
@@ -1171,7 +1173,7 @@ __device__ __forceinline__ void terms(uint32_t a, uint32_t b, uint32_t& hi, uint
 
 // A warp's part of a unit: P over z in tensor memory (columns from `at`).
 template <int HC, int FORM, bool DW, int PATH>
-__device__ __forceinline__ void z_to_p(uint32_t at, float descale, float up, const float* stat, int mine,
+__device__ __forceinline__ void z_to_p(uint32_t at, float log2e, float descale, float up, const float* stat, int mine,
                                        float nlse, int hit, int valid) {
   using C = BCfg<HC, FORM>;
   constexpr int N = PATH == kRare ? 16 : C::PW;  // (short: its time matters little)
@@ -1188,7 +1190,7 @@ __device__ __forceinline__ void z_to_p(uint32_t at, float descale, float up, con
         tmem_ld_frag16(at + pc + (16u << 16), v + 8);
       }
       tmem_wait_ld();
-      probs_col<FORM, N, PATH>(v, up, stat + pc, mine);
+      probs_col<FORM, N, PATH>(v, log2e, up, stat + pc, mine);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -1208,7 +1210,7 @@ __device__ __forceinline__ void z_to_p(uint32_t at, float descale, float up, con
       else
         tmem_ld16(at + pc, v);
       tmem_wait_ld();
-      probs_row<FORM, N, PATH>(v, descale, up, nlse, hit - pc, valid - pc);
+      probs_row<FORM, N, PATH>(v, log2e, descale, up, nlse, hit - pc, valid - pc);
 #pragma unroll
       for (int c = 0; c < N; c += 16) {
         uint32_t hi[8], lo[8];
@@ -1303,9 +1305,9 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       rare = DW ? hit_row(st, lane & (C::CW - 1), first + q * 32)
                 : __any_sync(0xffffffffu, (hit >= 0 && hit < C::CW) || w0 + C::CW > a.V);
     if (rare)
-      z_to_p<HC, FORM, DW, C::APART ? kRare : kEither>(at, descale, (float)up, st, mine, nlse, hit, a.V - w0);
+      z_to_p<HC, FORM, DW, C::APART ? kRare : kEither>(at, FORM == kBf16 ? a.l2e : kLog2e, descale, (float)up, st, mine, nlse, hit, a.V - w0);
     else
-      z_to_p<HC, FORM, DW, kUsual>(at, descale, (float)up, st, mine, nlse, hit, a.V - w0);
+      z_to_p<HC, FORM, DW, kUsual>(at, FORM == kBf16 ? a.l2e : kLog2e, descale, (float)up, st, mine, nlse, hit, a.V - w0);
     tmem_wait_st();
     tc_fence_before();
     __syncwarp();
@@ -1334,7 +1336,7 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       if (FORM != kBf16) s1 = pow2(-up), s2 = pow2(-14);  // (X's elements are times 2^14, once 2^e is undone)
     } else {
       orow = a.row[orow];
-      s3 = orow < 0 ? 0.f : a.dloss[orow];
+      s3 = orow < 0 ? 0.f : a.dloss[orow] * a.tau;
       if (FORM != kBf16) s1 = pow2(-15), s2 = pow2(-a.head[1]);
     }
     float* pt = a.part + ((int64_t)blockIdx.x * 2 + un.slot(cta, w.t)) * 128 * a.H;
@@ -1363,6 +1365,18 @@ __device__ __forceinline__ void bwd_epilogue(const BwdArgs& a, const Units& un, 
       for (int i = 0; i < 16; ++i) x[i] = x[i] * s1 * s2 * s3;
       if (a.out_bf16) {
         __nv_bfloat16* o = static_cast<__nv_bfloat16*>(DW ? a.dW : a.dX) + orow * a.H + col;
+        const float* add = DW ? a.add_w : a.add_x;
+        if (add) {
+          add += orow * a.H + col;
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const float4 p = *reinterpret_cast<const float4*>(add + i);
+            x[i] += p.x;
+            x[i + 1] += p.y;
+            x[i + 2] += p.z;
+            x[i + 3] += p.w;
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 16; i += 8) {
           __nv_bfloat162 h[4];
@@ -1642,10 +1656,14 @@ __global__ void __launch_bounds__(256)
   } else {
     orow = a.row[orow];
     if (orow < 0) return;
-    s3 = a.dloss[orow];
+    s3 = a.dloss[orow] * a.tau;
   }
   x = make_float4(x.x * s1 * s2 * s3, x.y * s1 * s2 * s3, x.z * s1 * s2 * s3, x.w * s1 * s2 * s3);
   if (a.out_bf16) {
+    if (const float* add = dw ? a.add_w : a.add_x) {
+      const float4 p = *reinterpret_cast<const float4*>(add + orow * a.H + col);
+      x = make_float4(x.x + p.x, x.y + p.y, x.z + p.z, x.w + p.w);
+    }
     __nv_bfloat162 w[2] = {__floats2bfloat162_rn(x.x, x.y), __floats2bfloat162_rn(x.z, x.w)};
     *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + orow * a.H + col) =
         *reinterpret_cast<const uint2*>(w);
@@ -1693,6 +1711,9 @@ cudaError_t prepare(const XentArgs& a, Call& c, RowArgs r) {
   r.x = c.at<uint16_t>(c.w.x);
   r.w = c.at<uint16_t>(c.w.w);
   r.status = a.status;
+  r.soft = a.soft != nullptr;
+  r.tau = a.soft ? a.soft->tau : 1.f;
+  r.inv_tau = 1.f / r.tau;
   // Up to kDirectRows rows, each block of k_xent_rows counts the rows before its own (at most 128 KB of
   // targets, from L2) in less time than a launch takes; the fp16 forms need the magnitudes first anyway.
   r.direct = c.form == kBf16 && a.n <= kDirectRows;
@@ -1834,6 +1855,9 @@ cudaError_t xent_fwd(const XentArgs& a, float* loss, float* lse, cudaStream_t st
   f.loss = loss;
   f.lse = lse;
   f.status = a.status;
+  f.c = a.soft ? kLog2e * (1.f / a.soft->tau) : kLog2e;
+  f.tau2 = a.soft ? a.soft->tau * a.soft->tau : 1.f;
+  f.inner = a.soft ? a.soft->inner : nullptr;
   // A row's logits depend on no other row, so bf16 rows need no gathering to be right; up to two units
   // a CTA it would only take longer (one row against 32000 x 128: 17 us with it, 13 without).
   const int64_t ct = ((int64_t)a.V + 255) / 256, units = c.w.cap / 128 * ct;
@@ -1894,6 +1918,10 @@ cudaError_t xent_bwd(const XentArgs& a, const float* lse, const float* dloss, in
   b.dloss = dloss;
   b.part = c.at<float>(c.w.part);
   b.status = a.status;
+  b.l2e = a.soft ? kLog2e * (1.f / a.soft->tau) : kLog2e;
+  b.tau = a.soft ? a.soft->tau : 1.f;
+  b.add_x = a.soft ? a.soft->add_x : nullptr;
+  b.add_w = a.soft ? a.soft->add_w : nullptr;
   b.out_bf16 = grad_bf16;
   // a unit of dW takes 2-20% longer (column statistics, frequent tokens): 72 of 152 CTAs for dX
   b.split = !dW ? c.ctas : !dX ? 0 : std::max(1, c.ctas * 9 / 19);

@@ -54,3 +54,39 @@ def top(z, K):
             m = float(z[i, ok].max())
             lse[i] = m + np.log(np.exp(z[i, ok].astype(np.float64) - m).sum())
     return vals, ids, lse
+
+
+def distill(X, W, ids, logits, tau, g):
+    """dict of loss, lse, dX, dW and the magnitudes the error bounds need."""
+    n, V = X.shape[0], W.shape[0]
+    X, W = np.asarray(X, np.float64), np.asarray(W, np.float64)
+    ok = (ids >= 0) & (ids < V) & (logits > -np.inf)
+    rows = ok.any(1)
+    r = {"loss": np.zeros(n), "lse": np.zeros(n), "dX": np.zeros(X.shape), "dW": np.zeros(W.shape),
+         "absX": np.zeros(X.shape), "absW": np.zeros(W.shape), "allX": np.zeros(X.shape),
+         "allW": np.zeros(W.shape), "zabs": 0.0, "rows": rows}
+    if not rows.any():
+        return r
+    x, t, m, gg = X[rows], np.where(ok, ids, 0)[rows], ok[rows], np.asarray(g, np.float64)[rows] * tau
+    u = np.where(m, np.asarray(logits, np.float64)[rows] / tau, -np.inf)
+    e = np.exp(u - u.max(1, keepdims=True))
+    q = e / e.sum(1, keepdims=True)
+    log_q = np.where(m, u - u.max(1, keepdims=True) - np.log(e.sum(1, keepdims=True)), 0.0)
+    z = x @ W.T / tau
+    top = z.max(1, keepdims=True)
+    p = np.exp(z - top)
+    r["lse"][rows] = lse = top[:, 0] + np.log(p.sum(1))
+    p /= p.sum(1, keepdims=True)
+    zk = np.take_along_axis(z, t, 1)
+    r["loss"][rows] = tau * tau * (np.where(m, q * (log_q - zk), 0.0).sum(1) + lse)
+    Q = np.zeros_like(p)
+    np.add.at(Q, (np.arange(len(t))[:, None], t), np.where(m, q, 0.0))
+    r["dX"][rows] = (gg[:, None] * (p - Q)) @ W
+    r["dW"] = (gg[:, None] * (p - Q)).T @ x
+    r["absX"][rows] = (np.abs(gg)[:, None] * (p + Q)) @ np.abs(W)
+    r["absW"] = (np.abs(gg)[:, None] * (p + Q)).T @ np.abs(x)
+    r["allX"][rows] = np.abs(gg)[:, None] * np.abs(W).sum(0)
+    r["allW"][:] = np.abs(gg).max() * np.abs(x).sum(0)
+    r["zabs"] = float((np.abs(x) @ np.abs(W).T).max()) / tau
+    r["uabs"] = float(np.abs(np.where(m, u, 0.0)).max())
+    return r

@@ -109,7 +109,56 @@ def test_adjustments_are_checked(lib, kw, word):
     _refused(lib.bg_logits_top(L.BG_BF16, 8, 9, 9, A, adjust, 2, A, A, A, None), word)
 
 
+def test_distillation_checks_its_arguments(lib):
+    f, b = L.BG_F32, L.BG_BF16
+
+    def fwd(dt=f, n=8, H=64, V=9, K=4, X=A, W=A, ids=A, u=A, tau=1.0, loss=A, lse=A, ws=A, size=BIG):
+        return lib.bg_distill_fwd(dt, n, H, V, K, X, W, ids, u, tau, loss, lse, ws, size, None)
+
+    def bwd(dt=f, n=8, H=64, V=9, K=4, X=A, W=A, ids=A, u=A, tau=1.0, lse=A, g=A, gd=f, dX=A, dW=A, flags=0, ws=A,
+            size=BIG):
+        return lib.bg_distill_bwd(dt, n, H, V, K, X, W, ids, u, tau, lse, g, gd, dX, dW, flags, ws, size, None)
+
+    for call in (fwd, bwd):
+        for kw, word in ((dict(dt=9), "dtype"), (dict(n=-1), "n must"), (dict(H=48), "H must"), (dict(V=0), "V must"),
+                         (dict(K=0), "K must"), (dict(K=129), "K must"), (dict(n=1 << 29, K=2), "n K must"),
+                         (dict(tau=0.0), "tau must"), (dict(tau=-1.0), "tau must"), (dict(tau=1e4), "tau must"),
+                         (dict(tau=float("nan")), "tau must"), (dict(W=None), "W is NULL"), (dict(X=A + 8), "X not"),
+                         (dict(ids=None), "top_id is NULL"), (dict(u=A + 4), "top_logit not"),
+                         (dict(ws=None), "ws is NULL"), (dict(lse=None), "lse is NULL")):
+            _refused(call(**kw), word)
+    for dt in (f, b):
+        for op, call in ((L.BG_OP_DISTILL_FWD, fwd), (L.BG_OP_DISTILL_BWD, bwd)):
+            need = lib.bg_distill_workspace_bytes(dt, 8, 64, 9, 4, op)
+            assert need > 0
+            _refused(call(dt=dt, size=need - 1), "workspace", code=-2)
+    _refused(fwd(loss=None), "loss is NULL")
+    _refused(bwd(g=None), "dloss is NULL")
+    _refused(bwd(gd=b), "fp32 gradients")
+    _refused(bwd(dt=b, gd=b, flags=1), "BG_ACCUM")
+    _refused(bwd(flags=2), "flags")
+    _refused(bwd(dX=None, dW=None), "dX and dW")
+    _refused(bwd(gd=4), "dtype")
+    for bad in ((f, -1, 64, 9, 4, 7), (f, 8, 40, 9, 4, 7), (f, 8, 64, 9, 0, 7), (f, 8, 64, 9, 4, L.BG_OP_XENT_FWD),
+                (5, 8, 64, 9, 4, 7), (f, 1 << 29, 64, 9, 2, 7)):
+        assert lib.bg_distill_workspace_bytes(*bad) == 0
+
+
+def test_distillation_workspaces_do_not_hold_the_logits(lib):
+    n, H, V, K = 1 << 20, 256, 1 << 20, 64
+    for dt in (L.BG_F32, L.BG_BF16):
+        for op in (L.BG_OP_DISTILL_FWD, L.BG_OP_DISTILL_BWD):
+            assert 0 < lib.bg_distill_workspace_bytes(dt, n, H, V, K, op) < 64 * H * (n + V) + 24 * n * K * (1 + H // 32)
+
+
 def test_nothing_to_do_is_done_without_a_device(lib):
+    f, b = L.BG_F32, L.BG_BF16
+    assert lib.bg_distill_fwd(f, 0, 64, 9, 4, None, A, None, None, 1.0, None, None, None, 0, None) == 0
+    for grad in (f, b):
+        assert lib.bg_distill_bwd(b, 0, 64, 9, 4, None, A, None, None, 1.0, None, None, grad, None, None, 0, None, 0,
+                                  None) == 0
+    assert lib.bg_distill_bwd(f, 0, 64, 9, 4, None, A, None, None, 1.0, None, None, f, None, A, L.BG_ACCUM, None, 0,
+                              None) == 0
     assert lib.bg_logits_fwd(L.BG_F32, 0, 64, 9, None, A, L.BG_F32, 9, None, None, 0, None) == 0
     assert lib.bg_logits_adjust(L.BG_BF16, 0, 9, 9, None, None, 9, None, None) == 0
     assert lib.bg_logits_top(L.BG_BF16, 0, 9, 9, None, None, 3, None, None, None, None) == 0
@@ -151,10 +200,13 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     f, i = torch.float32, torch.int32
     n, V, H, K = 6, 9, 64, 3
     args = {"X": (f, n, H), "W": (f, V, H), "Z": (f, n, V), "out": (f, n, V), "ws": (f, 1 << 20),
-            "top_logit": (f, n, K), "top_id": (i, n, K), "lse": (f, n)}
+            "top_logit": (f, n, K), "top_id": (i, n, K), "lse": (f, n), "loss": (f, n), "dloss": (f, n),
+            "dX": (f, n, H), "dW": (f, V, H)}
     calls = [("X W Z ws", lambda X, W, Z, ws: L.logits_fwd("f32", X, W, "f32", Z, ws)),
              ("Z out", lambda Z, out: L.logits_adjust("f32", Z, out, None)),
-             ("Z top_logit top_id lse", lambda *t: L.logits_top("f32", *t))]
+             ("Z top_logit top_id lse", lambda *t: L.logits_top("f32", *t)),
+             ("X W top_id top_logit loss lse ws", lambda *t: L.distill_fwd("f32", *t)),
+             ("X W top_id top_logit lse dloss dX dW ws", lambda *t: L.distill_bwd("f32", *t[:6], "f32", *t[6:]))]
     for names, call in calls:
         for away in names.split():
             with pytest.raises(ValueError, match=f"^{away} is on cuda:1, the current device is cuda:0"):

@@ -349,3 +349,396 @@ def test_top_from_rows_beyond_32_bit_offsets():
 
 def z_bf16(z):
     return torch.from_numpy(np.asarray(z, np.float32)).to(torch.bfloat16).double().numpy()
+
+
+# ------------------------------------------------------------------------------ distillation
+
+
+def teacher(n, V, K, rng, share=1.0):
+    """(ids, logits) of teachers' answers: K different tokens a row, some rows fewer, some none, some ids past
+    the end replaced by -1, some logits -inf."""
+    ids = rng.integers(0, V, (n, K)) if K > V else \
+        np.argsort(rng.random((n, V)), 1)[:, :K] if n * V <= 1 << 22 else \
+        (rng.integers(0, V, (n, 1)) + np.arange(K) * max(1, V // (K + 1))) % V
+    logits = np.sort(rng.standard_normal((n, K)) * 3, 1)[:, ::-1].astype(np.float32)
+    ids = ids.astype(np.int32)
+    short = rng.random(n) < 0.2
+    ids[short, K // 2 + 1:] = -1
+    logits[rng.random(n) < 0.1, K - 1] = -np.inf
+    out = rng.random(n) >= share
+    ids[out] = -1
+    return ids, logits
+
+
+def distill_inputs(n, H, V, K, dtype, share=1.0, seed=0):
+    rng = np.random.default_rng(seed + n + H + V + K)
+    W = rng.standard_normal((V, H)) * 2.0 / np.sqrt(H)
+    ids, logits = teacher(n, V, K, rng, share)
+    X = rng.standard_normal((n, H)) + rng.random((n, 1)) * W[np.maximum(ids[:, 0], 0)]
+    g = (0.5 + rng.random(n)).astype(np.float32) / max(n, 1)
+    return dev(X, dtype), dev(W, dtype), ids, logits, g
+
+
+def distill_ws(dtype, n, H, V, K):
+    return torch.full((max(L.distill_workspace_bytes(dtype, n, H, V, K, op)
+                           for op in (L.BG_OP_DISTILL_FWD, L.BG_OP_DISTILL_BWD)),), 0xFF, device="cuda",
+                      dtype=torch.uint8)
+
+
+def run_distill(dtype, X, W, ids, logits, g, tau, grad, flags=0, into=None):
+    (n, K), (V, H) = ids.shape, W.shape
+    t, u, gd = ints(ids), dev(logits), dev(g)
+    loss, lse = (torch.full((n,), float("nan"), device="cuda") for _ in range(2))
+    ws = distill_ws(dtype, n, H, V, K)
+    L.distill_fwd(dtype, X, W, t, u, loss, lse, ws, tau=tau)
+    dX, dW = into or (torch.full((m, H), float("nan"), device="cuda", dtype=TD[grad]) for m in (n, V))
+    ws.fill_(0xFF)
+    L.distill_bwd(dtype, X, W, t, u, lse, gd, grad, dX, dW, ws, tau=tau, flags=flags)
+    return loss, lse, dX, dW
+
+
+def distill_bounds(r, n, H, V, K, tau, grad):
+    """A logit over tau: H products to 21 bits or better added in fp32 (2 u each), its division (u).  lse is as
+    exact as the largest of them, to 2^-20 of itself; the loss has K terms q (log q - z) more (each to a few u,
+    of at most 2 uabs + log K + zabs).  A gradient element: terms off by their probabilities' error (of P: two
+    logits' errors; of Q: 4 u uabs), 2^-19 of the products' representation, and with bf16 gradients 2^-7 of P
+    (its rounding in the products) and 2^-8 of the result; the sums add V u or (n + K) u of the terms'
+    magnitude.  Below 2^-38 (for dW: of the largest weight) a probability may be lost."""
+    dz = (2 * H * U + 2.0 ** -21) * r["zabs"]
+    lse = 2 * dz + 2.0 ** -20 * (1 + np.abs(r["lse"]))
+    loss = tau * tau * (lse + (K + 16) * U * (2 * r["uabs"] + 8 + r["zabs"]) + dz) + 4 * U * np.abs(r["loss"])
+    term = 2 * dz + 8 * U * r["uabs"] + 2.0 ** -19 + (2.0 ** -7 if grad == "bf16" else 0)
+    bX = (term + 2 * (V + K) * U) * r["absX"] + 2.0 ** -38 * r["allX"] + 2.0 ** -126
+    bW = (term + 2 * (n + K) * U) * r["absW"] + 2.0 ** -38 * r["allW"] + 2.0 ** -126
+    if grad == "bf16":
+        bX, bW = bX + HALF * 1.01 * np.abs(r["dX"]), bW + HALF * 1.01 * np.abs(r["dW"])
+    return loss, lse, bX, bW
+
+
+def check_distill(dtype, grad, X, W, ids, logits, g, tau, norm=True):
+    (n, K), (V, H) = ids.shape, W.shape
+    got = run_distill(dtype, X, W, ids, logits, g, tau, grad)
+    L.check_device()
+    r = ref.distill(host(X), host(W), ids, logits, tau, g)
+    if not r["rows"].any():
+        assert all(not bool(t.any()) for t in got)
+        return got
+    loss, lse, bX, bW = distill_bounds(r, n, H, V, K, tau, grad)
+    within(host(got[1]), r["lse"], lse * r["rows"], "lse")
+    within(host(got[0]), r["loss"], loss * r["rows"], "loss")
+    within(host(got[2]), r["dX"], bX, "dX")
+    within(host(got[3]), r["dW"], bW, "dW")
+    if norm and V > 1:  # roundings average out: 2^-15 of the norm in fp32, 2^-8 in bf16
+        for k in ("dX", "dW"):
+            off = np.linalg.norm(host(got[2 if k == "dX" else 3]) - r[k]) / np.linalg.norm(r[k])
+            assert off < (2.0 ** -8 if grad == "bf16" else 2.0 ** -15), (k, off)
+    return got
+
+
+TYPES = [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")]
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+@pytest.mark.parametrize("n,H,V,K,tau,share", [
+    (1, 32, 2, 1, 1.0, 1.0), (1, 128, 4001, 5, 2.0, 1.0), (2, 64, 1000, 128, 0.5, 1.0),
+    (7, 96, 65, 33, 1.0, 1.0), (127, 160, 127, 2, 3.5, 0.5), (128, 256, 128, 31, 1.0, 1.0),
+    (129, 192, 257, 32, 2.0, 0.7), (300, 224, 513, 64, 1.0, 0.15), (513, 256, 1023, 16, 4.0, 1.0),
+    (1000, 32, 3001, 8, 1.0, 1.0), (2500, 64, 400, 100, 2.0, 0.3), (4097, 128, 130, 4, 1.0, 1.0),
+    (700, 256, 2049, 12, 1.0, 0.02), (20, 64, 30, 128, 1.0, 1.0)])
+def test_distill(dtype, grad, n, H, V, K, tau, share):
+    X, W, ids, logits, g = distill_inputs(n, H, V, K, dtype, share)
+    check_distill(dtype, grad, X, W, ids, logits, g, tau)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_distill_of_larger_shapes(dtype, grad):
+    """Several units a CTA, tiles that fall to several, entries that are sorted in several passes."""
+    for n, H, V, K in ((9001, 64, 7000, 32), (3000, 256, 20001, 20), (33000, 32, 300, 8)):
+        X, W, ids, logits, g = distill_inputs(n, H, V, K, dtype, 0.8)
+        check_distill(dtype, grad, X, W, ids, logits, g, 2.0)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_distill_with_one_entry_is_the_cross_entropy(dtype, grad):
+    """One entry a row and tau = 1: q is one, the loss that of the token."""
+    n, H, V = 700, 96, 900
+    X, W, ids, logits, g = distill_inputs(n, H, V, 1, dtype, 0.8)
+    got = check_distill(dtype, grad, X, W, ids, logits, g, 1.0)
+    t, gd = ints(np.where(np.isinf(logits[:, 0]), -1, ids[:, 0])), dev(g)
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    dX, dW = (torch.empty(m, H, device="cuda", dtype=TD[grad]) for m in (n, V))
+    ws = torch.empty(L.xent_workspace_bytes(dtype, n, H, V, L.BG_OP_XENT_BWD) +
+                     L.xent_workspace_bytes(dtype, n, H, V, L.BG_OP_XENT_FWD), device="cuda", dtype=torch.uint8)
+    L.xent_fwd(dtype, X, W, t, loss, lse, ws)
+    L.xent_bwd(dtype, X, W, t, lse, gd, grad, dX, dW, ws)
+    r = ref.distill(host(X), host(W), ids, logits, 1.0, g)
+    b = distill_bounds(r, n, H, V, 1, 1.0, grad)
+    assert torch.equal(got[1], lse)
+    for a, c, tol in ((got[0], loss, b[0]), (got[2], dX, b[2]), (got[3], dW, b[3])):
+        within(host(a), host(c), 2 * tol)
+
+
+def test_distill_bf16_gradients_of_a_student_that_nearly_agrees():
+    """Every token has an entry and the student is 2^-8 from its teacher: P rounded to bf16 alone would be as far
+    off as the gradient is large; the entries' coefficients P - Q are fp32.  What is left is the result's
+    rounding (2^-9 on average, 2^-8 at most), a few entries whose P rounds to the other side in the product
+    (their z differs by 2^-20; 2^-11 of them, each off by 2^-7 of P: 2^-12 of the norm of P, 2^-4 of d) and the
+    entries' own error, 2 dz / 2^-8."""
+    n, H, V = 600, 64, 96
+    rng = np.random.default_rng(2)
+    W, X = dev(rng.standard_normal((V, H)) / 4, "bf16"), dev(rng.standard_normal((n, H)) / 2, "bf16")
+    z = host(X) @ host(W).T
+    ids = np.tile(np.arange(V, dtype=np.int32), (n, 1))
+    for i in range(n):
+        rng.shuffle(ids[i])
+    logits = (np.take_along_axis(z, ids.astype(np.int64), 1) + 2.0 ** -8 * rng.standard_normal((n, V))).astype(np.float32)
+    g = (0.5 + rng.random(n)).astype(np.float32)
+    got = run_distill("bf16", X, W, ids, logits, g, 1.0, "bf16")
+    r = ref.distill(host(X), host(W), ids, logits, 1.0, g)
+    for k, t in (("dX", got[2]), ("dW", got[3])):
+        off = np.linalg.norm(host(t) - r[k]) / np.linalg.norm(r[k])
+        assert off < 2.0 ** -4, (k, off)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_distill_of_a_token_in_several_entries(dtype, grad):
+    n, H, V, K = 200, 64, 300, 40
+    X, W, ids, logits, g = distill_inputs(n, H, V, K, dtype)
+    rng = np.random.default_rng(1)
+    ids[:100] = np.where(ids[:100] >= 0, rng.integers(0, 3, (100, K)), -1)
+    ids[100:110] = np.where(ids[100:110] >= 0, 7, -1)
+    check_distill(dtype, grad, X, W, ids, logits, g, 1.5)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_distill_rows_left_out_may_hold_anything(dtype, grad):
+    """Rows without an entry, or with entries of -inf alone: their X, g and lse are not used."""
+    n, H, V, K = 300, 64, 200, 6
+    X, W, ids, logits, g = distill_inputs(n, H, V, K, dtype, 0.5)
+    logits[5:9] = -np.inf
+    r = ref.distill(host(X), host(W), ids, logits, 2.0, g)
+    out = torch.from_numpy(~r["rows"]).cuda()
+    want = run_distill(dtype, X, W, ids, logits, g, 2.0, grad)
+    X[out] = float("nan")
+    g = np.where(r["rows"], g, np.nan).astype(np.float32)
+    logits = np.where(ids < 0, np.nan, logits).astype(np.float32)
+    got = run_distill(dtype, X, W, ids, logits, g, 2.0, grad)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for a in (got[0], got[1], got[2]):
+        assert not bool(a[out].any())
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_distill_with_no_row_left(dtype, grad):
+    X, W, ids, logits, g = distill_inputs(150, 64, 300, 5, dtype, 0.0)
+    ids[:] = -1
+    check_distill(dtype, grad, X, W, ids, logits, g, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_distill_accumulates_and_skips_what_is_not_asked(dtype):
+    n, H, V, K = 400, 96, 500, 9
+    X, W, ids, logits, g = distill_inputs(n, H, V, K, dtype, 0.7)
+    rng = np.random.default_rng(0)
+    old = [rng.standard_normal((m, H)).astype(np.float32) for m in (n, V)]
+    r = ref.distill(host(X), host(W), ids, logits, 2.0, g)
+    _, _, bX, bW = distill_bounds(r, n, H, V, K, 2.0, "f32")
+    _, lse, dX, dW = run_distill(dtype, X, W, ids, logits, g, 2.0, "f32", flags=L.BG_ACCUM,
+                                 into=[dev(o) for o in old])
+    # two additions to what was there
+    within(host(dX), old[0] + r["dX"], bX + 3 * U * (np.abs(old[0]) + r["absX"]))
+    within(host(dW), old[1] + r["dW"], bW + 3 * U * (np.abs(old[1]) + r["absW"]))
+    for grad in ("f32", "bf16") if dtype == "bf16" else ("f32",):
+        _, _, wX, wW = run_distill(dtype, X, W, ids, logits, g, 2.0, grad)
+        t, u, gd, ws = ints(ids), dev(logits), dev(g), distill_ws(dtype, n, H, V, K)
+        for which in (0, 1):
+            into = [torch.full((m, H), float("nan"), device="cuda", dtype=TD[grad]) if k == which else None
+                    for k, m in enumerate((n, V))]
+            ws.fill_(0xFF)
+            L.distill_bwd(dtype, X, W, t, u, lse, gd, grad, into[0], into[1], ws, tau=2.0)
+            want = (wX, wW)[which]
+            # (alone it has all CTAs: sums in another order)
+            within(host(into[which]), host(want), (bX, bW)[which] + 2 * HALF * np.abs(host(want)) * (grad == "bf16"))
+
+
+def test_distill_reports_tokens_past_the_vocabulary():
+    n, H, V, K = 90, 64, 100, 4
+    X, W, ids, logits, g = distill_inputs(n, H, V, K, "bf16")
+    bad = ids.copy()
+    bad[3, 1], bad[40] = V, V + 7
+    r = ref.distill(host(X), host(W), bad, logits, 1.0, g)
+    got = run_distill("bf16", X, W, bad, logits, g, 1.0, "f32")
+    with pytest.raises(L.BandGGNNError, match="site 135"):
+        L.check_device()
+    loss, _, bX, _ = distill_bounds(r, n, H, V, K, 1.0, "f32")
+    within(host(got[0]), r["loss"], loss * r["rows"])
+    within(host(got[2]), r["dX"], bX)
+    L.check_device()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tau", [1.0, 3.0])
+def test_distill_gradient_against_differences(dtype, tau):
+    """Directional differences of the forward itself.  With step e along a direction whose logits (over tau) move
+    by at most m, the central difference is off by e^2 m^3 / 6 of the weights' sum times tau^2, and by the loss's
+    rounding over e."""
+    n, H, V, K = 96, 64, 200, 12
+    X, W, ids, logits, g = distill_inputs(n, H, V, K, dtype)
+    rng = np.random.default_rng(3)
+    r = ref.distill(host(X), host(W), ids, logits, tau, g)
+    _, _, dX, dW = run_distill(dtype, X, W, ids, logits, g, tau, "f32")
+    Xf, Wf = X.float(), W.float()
+    for which, d in (("X", dX), ("W", dW)):
+        Dd = dev(rng.standard_normal(tuple(d.shape)))
+        move = host(Dd) @ host(Wf).T if which == "X" else host(Xf) @ host(Dd).T
+        m = 2 * np.abs(move).max() / tau
+        e = 0.02 / m
+        f = []
+        for s in (e, -e):
+            args = (Xf + s * Dd, Wf) if which == "X" else (Xf, Wf + s * Dd)
+            f.append(float((host(run_distill("f32", *args, ids, logits, g, tau, "f32")[0]) * g).sum()))
+        got, want = float((host(d) * host(Dd)).sum()), (f[0] - f[1]) / (2 * e)
+        loss, _, _, _ = distill_bounds(r, n, H, V, K, tau, "f32")
+        # X + e D itself is rounded to fp32: a logit moves by u of its magnitude
+        tol = g.sum() * (tau * tau * (e * m) ** 2 * m / 6 + (loss.max() + 2 * tau * tau * U * r["zabs"]) / e)
+        assert abs(got - want) <= tol, (which, got, want, tol)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
+def test_distill_gives_the_same_bits_again(dtype, grad):
+    X, W, ids, logits, g = distill_inputs(3000, 64, 900, 24, dtype, 0.8)
+    first = run_distill(dtype, X, W, ids, logits, g, 2.0, grad)
+    for _ in range(3):
+        for a, b in zip(run_distill(dtype, X, W, ids, logits, g, 2.0, grad), first):
+            assert torch.equal(a, b)
+
+
+def test_distill_of_enormous_logits_stays_within_its_rows():
+    """Rows with |lse| beyond 2^20 have gradients of no meaning, but finite ones; the other rows keep theirs."""
+    n, H, V, K = 200, 64, 150, 8
+    for grad in ("f32", "bf16"):
+        X, W, ids, logits, g = distill_inputs(n, H, V, K, "bf16")
+        want = run_distill("bf16", X, W, ids, logits, g, 1.0, grad)
+        X[::20] *= 1e9
+        got = run_distill("bf16", X, W, ids, logits, g, 1.0, grad)
+        keep = torch.ones(n, dtype=torch.bool)
+        keep[::20] = False
+        r = ref.distill(host(X)[keep], host(W), ids[keep.numpy()], logits[keep.numpy()], 1.0, g[keep.numpy()])
+        _, _, bX, _ = distill_bounds(r, n, H, V, K, 1.0, grad)
+        within(host(got[2])[keep.numpy()], host(want[2])[keep.numpy()], 2 * bX)
+        assert all(bool(torch.isfinite(t).all()) for t in got)
+
+
+# ------------------------------------------------------------------------------ all of them together
+
+
+def answer_and_learn(teacher_x, teacher_w, x, w, adjust, bufs, stream=None):
+    """A teacher's answers under a grammar, and the student's loss and gradients on them."""
+    Z, u, t, tlse, loss, lse, g, dX, dW, ws = bufs
+    L.logits_fwd("bf16", teacher_x, teacher_w, "bf16", Z, stream=stream)
+    L.logits_top("bf16", Z, u, t, tlse, adjust, stream=stream)
+    L.logits_adjust("bf16", Z, Z, adjust, stream=stream)
+    L.distill_fwd("bf16", x, w, t, u, loss, lse, ws, tau=2.0, stream=stream)
+    L.distill_bwd("bf16", x, w, t, u, lse, g, "f32", dX, dW, ws, tau=2.0, stream=stream)
+
+
+def test_a_student_learns_from_a_teachers_answers_on_its_stream_and_in_a_graph():
+    """The operators one after the other, as they are used: on a side stream, and captured and replayed on new
+    values (with an adjustment that changes between replays)."""
+    n, H, V, K = 600, 64, 777, 16
+    rng = np.random.default_rng(9)
+    tx, tw = dev(rng.standard_normal((n, H)), "bf16"), dev(rng.standard_normal((V, H)) / 4, "bf16")
+    x, w = dev(rng.standard_normal((n, H)), "bf16"), dev(rng.standard_normal((V, H)) / 4, "bf16")
+    kw, adjust = constraints(n, V, 5)
+    g = rng.random(n).astype(np.float32)
+
+    def make():
+        Z, _ = rows(n, V, 3, "bf16", 0.0)
+        return [Z, torch.zeros(n, K, device="cuda"), torch.zeros(n, K, device="cuda", dtype=torch.int32),
+                torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), dev(g),
+                torch.zeros(n, H, device="cuda"), torch.zeros(V, H, device="cuda"), distill_ws("bf16", n, H, V, K)]
+
+    bufs = make()
+    st = torch.cuda.Stream()
+    x2 = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        x2.copy_(x)
+    answer_and_learn(tx, tw, x2, w, adjust, bufs, stream=st)
+    st.synchronize()
+    L.check_device()
+    z = torch.empty(n, V, device="cuda", dtype=torch.bfloat16)
+    L.logits_fwd("bf16", tx, tw, "bf16", z)
+    adj = ref.adjusted(host(z), **kw)
+    vals, ids, _ = ref.top(adj, K)
+    assert np.array_equal(bits(bufs[0]), bits(torch.from_numpy(adj).to(torch.bfloat16).cuda()))
+    assert np.array_equal(bufs[2].cpu().numpy(), ids) and np.array_equal(bufs[1].cpu().numpy(), vals)
+    r = ref.distill(host(x), host(w), ids, vals, 2.0, g)
+    loss, lse, bX, bW = distill_bounds(r, n, H, V, K, 2.0, "f32")
+    within(host(bufs[4]), r["loss"], loss * r["rows"])
+    within(host(bufs[7]), r["dX"], bX)
+    within(host(bufs[8]), r["dW"], bW)
+    again = make()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        answer_and_learn(tx, tw, x2, w, adjust, again)
+    adjust._kept["bias"].zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert not torch.equal(again[2], bufs[2])
+    adjust._kept["bias"].copy_(dev(kw["bias"]))
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(again[:9], bufs[:9]):
+        assert np.array_equal(bits(a), bits(b)) if a.dtype != torch.int32 else torch.equal(a, b)
+
+
+FIRST_CALLS = """
+import torch
+from paper_1906_11786_gb300 import lib as L
+n, H, V, K = 500, 64, 300, 8
+gen = torch.Generator(device="cuda").manual_seed(1)
+X, W = (torch.randn(m, H, device="cuda", generator=gen) for m in (n, V))
+g, bias = torch.ones(n, device="cuda"), torch.randn(V, device="cuda", generator=gen)
+ws = torch.empty(max([L.logits_workspace_bytes("f32", n, H, V)] +
+                     [L.distill_workspace_bytes("f32", n, H, V, K, op)
+                      for op in (L.BG_OP_DISTILL_FWD, L.BG_OP_DISTILL_BWD)]), device="cuda", dtype=torch.uint8)
+outs = [torch.zeros(*s, device="cuda") for s in ((n, V), (n, V), (n, K), (n,), (n,), (n, H), (V, H))]
+Z, Y, u, loss, lse, dX, dW = outs
+t = torch.zeros(n, K, device="cuda", dtype=torch.int32)
+adjust = L.LogitAdjust(bias=bias)
+
+def calls():
+    L.logits_fwd("f32", X, W, "f32", Z, ws)
+    L.logits_adjust("f32", Z, Y, adjust)
+    L.logits_top("f32", Z, u, t, None, adjust)
+    L.distill_fwd("f32", X, W, t, u, loss, lse, ws)
+    L.distill_bwd("f32", X, W, t, u, lse, g, "f32", dX, dW, ws)
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls()
+graph.replay()
+torch.cuda.synchronize()
+L.check_device()
+replayed = [o.clone() for o in outs]
+for o in outs:
+    o.zero_()
+calls()
+torch.cuda.synchronize()
+L.check_device()
+assert all(torch.equal(a, b) and torch.count_nonzero(a) for a, b in zip(replayed, outs))
+print("captured")
+"""
+
+
+def test_the_first_calls_of_a_process_can_be_captured():
+    import os
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
