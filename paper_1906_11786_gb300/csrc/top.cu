@@ -30,7 +30,9 @@ using tc::smem_u32;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSegment = 8192;  // elements whose occurrences are counted at a time
+constexpr int kSlots = 2048;         // of a hash table of a history's tokens
+constexpr int kHashed = kSlots / 2;  // tokens of a history that go there; longer ones are counted
+constexpr int kSegment = 2 * kSlots; // elements whose occurrences are counted at a time (in the same place)
 constexpr int kEach = 16;       // elements of a thread at a time
 constexpr int kChunk = kThreads * kEach;
 
@@ -62,9 +64,9 @@ __device__ __forceinline__ void report(int* status, int site) {
 }
 
 // A row of logits and its part of the adjustment.
-template <typename T>
+template <typename T, int W = 16>
 struct Row {
-  static constexpr int G = 16 / (int)sizeof(T);  // elements of a group
+  static constexpr int G = W / (int)sizeof(T);   // elements of a group
   const T* base;                                 // the group that holds column 0
   int a;                                         // column 0's place in it
   int V;
@@ -77,12 +79,12 @@ struct Row {
   __device__ int groups() const { return (V + a + G - 1) / G; }
 };
 
-template <typename T, int F>
-__device__ __forceinline__ Row<T> make_row(const T* Z, int64_t ldz, int64_t i, int V, const Adjust& adj,
-                                           int* status) {
-  Row<T> r;
+template <typename T, int F, int W = 16>
+__device__ __forceinline__ Row<T, W> make_row(const T* Z, int64_t ldz, int64_t i, int V, const Adjust& adj,
+                                              int* status) {
+  Row<T, W> r;
   const T* p = Z + i * ldz;
-  r.a = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+  r.a = (int)((reinterpret_cast<uintptr_t>(p) & (W - 1)) / sizeof(T));
   r.base = p - r.a;
   r.V = V;
   r.bias = adj.bias;
@@ -113,8 +115,8 @@ __device__ __forceinline__ Row<T> make_row(const T* Z, int64_t ldz, int64_t i, i
 }
 
 // Occurrences of the tokens of elements [first, first + kSegment) of a row (element = column + a).
-template <typename T>
-__device__ __forceinline__ void count_history(const Row<T>& r, int64_t first, uint32_t* counts, int* status) {
+template <typename T, int W>
+__device__ __forceinline__ void count_history(const Row<T, W>& r, int64_t first, uint32_t* counts, int* status) {
   __syncthreads();
   for (int i = threadIdx.x; i < kSegment / 4; i += kThreads)
     reinterpret_cast<uint4*>(counts)[i] = make_uint4(0, 0, 0, 0);
@@ -151,12 +153,18 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 // The logits of group g (G of them) as they are; -inf past the row's ends.
-template <typename T>
-__device__ __forceinline__ void load_group(const Row<T>& r, int64_t g, float* v) {
-  constexpr int G = Row<T>::G;
+template <typename T, int W>
+__device__ __forceinline__ void load_group(const Row<T, W>& r, int64_t g, float* v) {
+  constexpr int G = Row<T, W>::G;
   const int64_t c0 = g * G - r.a;
   if (c0 >= 0 && c0 + G <= r.V) {
-    unpack(__ldcs(reinterpret_cast<const uint4*>(r.base + g * G)), v, T());
+    if constexpr (W == 16) {
+      unpack(__ldcs(reinterpret_cast<const uint4*>(r.base + g * G)), v, T());
+    } else {
+      const uint32_t x = __ldcs(reinterpret_cast<const uint32_t*>(r.base + g * G));
+      v[0] = __uint_as_float(G == 1 ? x : x << 16);
+      if (G == 2) v[G - 1] = __uint_as_float(x & 0xFFFF0000u);
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < G; ++j) v[j] = c0 + j >= 0 && c0 + j < r.V ? to_f32(r.base[g * G + j]) : -INFINITY;
@@ -164,12 +172,21 @@ __device__ __forceinline__ void load_group(const Row<T>& r, int64_t g, float* v)
 }
 
 // Adjusts group g in place; counts: the occurrences of its elements.
-template <typename T, int F>
-__device__ __forceinline__ void adjust_group(const Row<T>& r, int64_t g, const uint32_t* counts, float* v) {
-  constexpr int G = Row<T>::G;
+template <typename T, int F, int W>
+__device__ __forceinline__ void adjust_group(const Row<T, W>& r, int64_t g, const uint32_t* counts, float* v) {
+  constexpr int G = Row<T, W>::G;
   const int c0 = (int)(g * G - r.a);
   if (F & kBias) {
-    if (c0 >= 0 && c0 + G <= r.V) {
+    if (G >= 4 && r.a == 0 && c0 + G <= r.V) {
+#pragma unroll
+      for (int j = 0; j + 4 <= G; j += 4) {
+        const float4 b = __ldg(reinterpret_cast<const float4*>(r.bias + c0 + j));
+        v[j] = __fadd_rn(v[j], b.x);
+        v[j + 1] = __fadd_rn(v[j + 1], b.y);
+        v[j + 2] = __fadd_rn(v[j + 2], b.z);
+        v[j + 3] = __fadd_rn(v[j + 3], b.w);
+      }
+    } else if (c0 >= 0 && c0 + G <= r.V) {
 #pragma unroll
       for (int j = 0; j < G; ++j) v[j] = __fadd_rn(v[j], __ldg(r.bias + c0 + j));
     } else {
@@ -180,7 +197,10 @@ __device__ __forceinline__ void adjust_group(const Row<T>& r, int64_t g, const u
   }
   if ((F & kHistory) && r.hist_n > 0) {
 #pragma unroll
-    for (int k = 0; k < G; k += 4) {
+    for (int k = 0; k < G; ++k)
+      if (G < 4 && counts[k]) v[k] = penalised(v[k], counts[k], r.rep, r.presence, r.frequency);
+#pragma unroll
+    for (int k = 0; k + 4 <= G; k += 4) {
       const uint4 c = *reinterpret_cast<const uint4*>(counts + k);
       if (c.x | c.y | c.z | c.w) {
         const uint32_t u[4] = {c.x, c.y, c.z, c.w};
@@ -202,64 +222,169 @@ __device__ __forceinline__ void adjust_group(const Row<T>& r, int64_t g, const u
   }
 }
 
-// ------------------------------------------------------------------------------ adjustment
-__device__ __forceinline__ void store_group(float* p, const float* v) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+// A hash table of a history's tokens and their counts in shared memory (2 kSlots words).  Only the part that
+// the history needs is used: a small one is cleared and looked through quickly.
+struct Hash {
+  uint32_t* token;  // plus one; 0: none
+  uint32_t* count;
+  int size;  // a power of two
+};
+
+__device__ __forceinline__ void hash_add(const Hash& h, uint32_t id) {
+  uint32_t at = (id * 2654435761u) >> 7 & (h.size - 1);
+  for (int k = 0; k < h.size; ++k, at = (at + 1) & (h.size - 1)) {  // (half of the slots stay empty)
+    const uint32_t was = atomicCAS(&h.token[at], 0u, id + 1);
+    if (was == 0 || was == id + 1) {
+      atomicAdd(&h.count[at], 1u);
+      return;
+    }
+  }
 }
+
+// The table of the tokens of r's history whose elements (column + a) are in [first, last); the whole block calls
+// it, and a barrier has to follow before the table is read.
+template <typename T, int W>
+__device__ __forceinline__ Hash hash_history(const Row<T, W>& r, int64_t first, int64_t last, uint32_t* table,
+                                             int* status) {
+  Hash h{table, nullptr, 64};
+  while (h.size < 2 * r.hist_n) h.size *= 2;
+  h.count = table + h.size;
+  for (int i = threadIdx.x; i < 2 * h.size; i += kThreads) table[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < (int)r.hist_n; i += kThreads) {
+    const int id = r.hist[i];
+    if (id >= r.V) report(status, kSiteHistoryId);
+    const int64_t e = (int64_t)id + r.a;
+    if (id >= 0 && id < r.V && e >= first && e < last) hash_add(h, (uint32_t)id);
+  }
+  return h;
+}
+
+// ------------------------------------------------------------------------------ adjustment
+template <int G>
+__device__ __forceinline__ void store_group(float* p, const float* v) {
+  if constexpr (G == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  else *p = v[0];
+}
+template <int G>
 __device__ __forceinline__ void store_group(__nv_bfloat16* p, const float* v) {
-  __nv_bfloat162 h[4];
+  __nv_bfloat162 h[G / 2];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-  *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
+  for (int j = 0; j < G / 2; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+  if constexpr (G == 8) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
+  else *reinterpret_cast<__nv_bfloat162*>(p) = h[0];
 }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 
-// Block (segment, row).
-template <typename T, int F>
+template <typename T, int W>
+__device__ __forceinline__ void store_row_group(const Row<T, W>& r, T* o, bool vec, int64_t g, const float* v) {
+  constexpr int G = Row<T, W>::G;
+  const int64_t c0 = g * G - r.a;
+  if (vec && c0 >= 0 && c0 + G <= r.V) {
+    store_group<G>(o + c0, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < G; ++j)
+      if (c0 + j >= 0 && c0 + j < r.V) store1(o + c0 + j, v[j]);
+  }
+}
+
+// Block (row, run of `per` groups).  Biases and masks are one pass over the elements; the tokens of the history
+// come after it, from a hash table, their logits read before it (out may be Z).
+template <typename T, int F, int W>
 __global__ void __launch_bounds__(kThreads)
-    k_adjust(int64_t n, int V, int64_t ldz, const T* Z, Adjust adj, int64_t ldo, T* out, int* status) {
-  constexpr int G = Row<T>::G, SG = kSegment / G;
-  __shared__ __align__(16) uint32_t counts[F & kHistory ? kSegment : 4];
+    k_adjust(int V, int64_t ldz, const T* Z, Adjust adj, int64_t ldo, T* out, int per, int* status) {
+  constexpr int G = Row<T, W>::G, U = 64 / W;  // U groups of a thread on their way
+  __shared__ __align__(16) uint32_t table[F & kHistory ? 2 * kSlots : 4];
+  __shared__ float raw[F & kHistory ? kSlots : 1];
   tc::grid_dep_launch();
   tc::grid_dep_wait();
   const int64_t i = blockIdx.x;
-  const Row<T> r = make_row<T, F>(Z, ldz, i, V, adj, status);
+  const Row<T, W> r = make_row<T, F, W>(Z, ldz, i, V, adj, status);
   T* o = out + i * ldo;
-  const bool vec = (reinterpret_cast<uintptr_t>(o - r.a) & 15) == 0;
-  for (int64_t g0 = (int64_t)blockIdx.y * SG; g0 < r.groups(); g0 += (int64_t)gridDim.y * SG) {
-    if ((F & kHistory) && r.hist_n > 0) count_history(r, g0 * G, counts, status);
-    const int64_t g1 = min((int64_t)r.groups(), g0 + SG);
-    for (int64_t g = g0 + threadIdx.x; g < g1; g += kThreads) {
-      float v[G];
-      load_group(r, g, v);
-      adjust_group<T, F>(r, g, counts + (F & kHistory ? (g - g0) * G : 0), v);
-      const int64_t c0 = g * G - r.a;
-      if (vec && c0 >= 0 && c0 + G <= V) {
-        store_group(o + c0, v);
-      } else {
-#pragma unroll
-        for (int j = 0; j < G; ++j)
-          if (c0 + j >= 0 && c0 + j < V) store1(o + c0 + j, v[j]);
+  const bool vec = (reinterpret_cast<uintptr_t>(o - r.a) & (W - 1)) == 0;
+  const int64_t g0 = (int64_t)blockIdx.y * per, g1 = min((int64_t)r.groups(), g0 + per);
+  if (g0 >= g1) return;
+  if ((F & kHistory) && r.hist_n > kHashed) {
+    constexpr int SG = kSegment / G;
+    for (int64_t s0 = g0; s0 < g1; s0 += SG) {
+      count_history(r, s0 * G, table, status);
+      for (int64_t g = s0 + threadIdx.x; g < min(g1, s0 + SG); g += kThreads) {
+        float v[G];
+        load_group(r, g, v);
+        adjust_group<T, F>(r, g, table + (g - s0) * G, v);
+        store_row_group(r, o, vec, g, v);
       }
+    }
+    return;
+  }
+  Hash h{nullptr, nullptr, 0};
+  if ((F & kHistory) && r.hist_n > 0) {
+    h = hash_history(r, g0 * G, g1 * G, table, status);
+    __syncthreads();
+    for (int k = threadIdx.x; k < h.size; k += kThreads)
+      if (h.token[k]) raw[k] = to_f32(r.base[(int64_t)h.token[k] - 1 + r.a]);
+    __syncthreads();
+  }
+  if ((F & (kBias | kMask)) || out != Z) {
+    for (int64_t g = g0 + threadIdx.x; g < g1; g += U * kThreads) {
+      float v[U][G];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (g + u * kThreads < g1) load_group(r, g + u * kThreads, v[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (g + u * kThreads >= g1) break;
+        adjust_group<T, F & ~kHistory>(r, g + u * kThreads, nullptr, v[u]);
+        store_row_group(r, o, vec, g + u * kThreads, v[u]);
+      }
+    }
+  }
+  if ((F & kHistory) && r.hist_n > 0) {
+    __syncthreads();
+    for (int k = threadIdx.x; k < h.size; k += kThreads) {
+      if (!h.token[k]) continue;
+      const int id = (int)(h.token[k] - 1);
+      float v = raw[k];
+      if (F & kBias) v = __fadd_rn(v, __ldg(r.bias + id));
+      v = penalised(v, h.count[k], r.rep, r.presence, r.frequency);
+      if ((F & kMask) && r.mask && !(__ldg(r.mask + (id >> 5)) >> (id & 31) & 1u)) v = -INFINITY;
+      store1(o + id, v);
     }
   }
 }
 
 // ------------------------------------------------------------------------------ largest logits
-constexpr int kRoom = kChunk + 1024;  // candidates a block keeps
+// A row's candidates are the logits above a bound that at least K of its logits are known to reach: each
+// warp's ceil(K / 8)-th largest of its lanes' maxima so far, the least over the warps.  The bound rises
+// after 1, 2, 4, ... chunks; warps read each other's parts of it as they find them (an old part is a lower
+// bound too), so that there is one barrier, after the first chunk, and none after that.  For 49999 logits
+// and K = 32 some 200 become candidates; where they outgrow their room (ties without end, rows that rise), the
+// block goes over the row again with exact bounds (rising_row, some times slower).
+//
+// Masks and histories come as bits in shared memory, kBits elements at a time: a cleared bit leaves an element
+// out.  The tokens of a history are cleared too, counted in a hash table, and added one by one after the
+// others: c > 0 for a few hundred of 50000 tokens costs no element a test of its own.
+constexpr int kBits = 65536;  // elements whose bits are in shared memory at a time
+constexpr int kRoom = 2304;   // candidates: those of a pass of rising_row (2048) and the K before it
+constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoLogit = -3.0e38f;  // reference of a sum without terms
+constexpr float kLeast = -3.402823466e38f;
 
 struct TopShared {
   uint64_t cand[kRoom];
+  uint64_t few[kThreads];
   uint64_t best[kMaxTop];
-  float m[kThreads / 32], l[kThreads / 32];
+  float m[kWarps], l[kWarps];
   float block_m, block_l;
-  uint32_t warp_t[kThreads / 32];
-  int count, sum[64];
+  uint32_t part[kWarps];  // of the bound, as orders
+  int count, found, sum[64];
 };
+// After it in dynamic shared memory, as far as the adjustment needs them: the bits, then the hash table, whose
+// place rising_row takes for occurrences.
 
 // Order of logits as unsigned numbers (-0 counts as 0), and keys: the larger logit, then the lower token.
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -278,6 +403,30 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// two fp32 at a time
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 
 // log of the sum l to the reference m (in base 2).  A sum of 0 with a reference: every term vanished beside
 // the rounding of the reference, which then is the result to the last bit.
@@ -285,23 +434,44 @@ __device__ __forceinline__ float lse_of(float m, float l) {
   return (l == 0.f && m > kNoLogit ? m : m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Keeps the candidates with keys of t or more; the whole block calls it.
-__device__ __noinline__ void keep_from(TopShared& s, uint64_t t) {
-  uint64_t mine[kRoom / kThreads];
-  __syncthreads();
-  const int n = s.count;
-#pragma unroll
-  for (int k = 0; k < kRoom / kThreads; ++k) {
-    const int i = threadIdx.x + k * kThreads;
-    mine[k] = i < n ? s.cand[i] : 0;
+// A thread's sum of exp2(c z) to the reference m, near the largest so far.
+struct Sum {
+  float m = kNoLogit, l = 0.f;
+  // (rounded up: of logits beyond 2^31 the terms may vanish but not overflow)
+  __device__ __forceinline__ void refer(float most) {
+    const float mc = __fmul_ru(most, kLog2e);
+    if (mc > m) {
+      l *= ex2(m - mc);
+      m = mc;
+    }
   }
-  __syncthreads();
-  if (threadIdx.x == 0) s.count = 0;
-  __syncthreads();
+  template <int N>
+  __device__ __forceinline__ void add(const float* v, float most) {
+    refer(most);
+    const uint64_t c2 = pack2(kLog2e, kLog2e), m2 = pack2(-m, -m);
+    uint64_t s[2] = {0, 0};
 #pragma unroll
-  for (int k = 0; k < kRoom / kThreads; ++k)
-    if (mine[k] >= t && mine[k] != 0) s.cand[atomicAdd(&s.count, 1)] = mine[k];
-  __syncthreads();
+    for (int j = 0; j < N; j += 2) {
+      float a, b;
+      unpack2(fma2(pack2(v[j], v[j + 1]), c2, m2), a, b);
+      s[(j >> 1) & 1] = add2(s[(j >> 1) & 1], pack2(ex2(a), ex2(b)));
+    }
+    float a, b;
+    unpack2(add2(s[0], s[1]), a, b);
+    l += a + b;
+  }
+};
+
+template <int N>
+__device__ __forceinline__ float max_of(const float* v) {
+  static_assert(N % 4 == 0, "");
+  float a = v[0], b = v[1];
+#pragma unroll
+  for (int j = 2; j < N - 2; j += 4) {
+    a = max3(a, v[j], v[j + 1]);
+    b = max3(b, v[j + 2], v[j + 3]);
+  }
+  return max3(fmaxf(a, b), v[N - 2], v[N - 1]);
 }
 
 // The K-th largest candidate's key (0 where there are fewer), a bit at a time; the whole block calls it.
@@ -324,21 +494,41 @@ __device__ __noinline__ uint64_t kth_key(TopShared& s, int K) {
   return t;
 }
 
-// A value that K of the row's logits reach at least, from a logit of each thread: each warp's
-// ceil(K / 8)-th largest, the least of them.
-__device__ __forceinline__ float reached(TopShared& s, float top, int K) {
-  const int rounds = (K + kThreads / 32 - 1) / (kThreads / 32), lane = threadIdx.x & 31;
+// The candidates with keys of t or more (kThreads at most) to `few`; the whole block calls it.  Their number.
+__device__ __forceinline__ int pick(TopShared& s, uint64_t t) {
+  __syncthreads();
+  if (threadIdx.x == 0) s.found = 0;
+  __syncthreads();
+  const int n = s.count;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t key = s.cand[i];
+    if (key >= t) {
+      const int at = atomicAdd(&s.found, 1);
+      if (at < kThreads) s.few[at] = key;
+    }
+  }
+  __syncthreads();
+  return s.found;
+}
+
+// This warp's part of the bound: the ceil(K / 8)-th largest of its lanes' maxima.
+__device__ __forceinline__ void raise(TopShared& s, float top, int K) {
+  const int rounds = (K + kWarps - 1) / kWarps, lane = threadIdx.x & 31;
   uint32_t mine = order_of(top), t = 0;
   for (int k = 0; k < rounds; ++k) {
     t = __reduce_max_sync(0xffffffffu, mine);
     const unsigned holds = __ballot_sync(0xffffffffu, mine == t);
     if (lane == __ffs(holds) - 1) mine = 0;
   }
-  if (lane == 0) s.warp_t[threadIdx.x >> 5] = t;
-  __syncthreads();
+  if (lane == 0) *const_cast<volatile uint32_t*>(&s.part[threadIdx.x >> 5]) = t;
+}
+// The bound: the least of the parts, as they are found.
+__device__ __forceinline__ float bound(const TopShared& s) {
+  const volatile uint32_t* p = s.part;
+  uint32_t t = p[0];
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) t = min(t, s.warp_t[w]);
-  return t == 0 ? -INFINITY : value_of(t);
+  for (int w = 1; w < kWarps; ++w) t = min(t, p[w]);
+  return t == 0 ? kLeast : fmaxf(kLeast, value_of(t));
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -365,118 +555,223 @@ __device__ __forceinline__ float cluster_ldf(const void* p, int rank) {
   return v;
 }
 
+// Groups [begin, end) of a row whatever they hold: a barrier and, where there is no more room, an exact
+// bound before each pass of 256 groups.  The sum goes on only where `summing`.
+template <typename T, int F>
+__device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t begin, int64_t end, int K,
+                                        uint32_t* counts, bool summing, Sum& sum, int* status) {
+  constexpr int G = Row<T>::G, SG = kSegment / G;
+  __syncthreads();
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  float least = kLeast;
+  uint64_t least_key = 0;
+  int upper = 0;
+  for (int64_t s0 = begin; s0 < end; s0 += SG) {
+    if ((F & kHistory) && r.hist_n > 0) count_history(r, s0 * G, counts, status);
+    const int64_t s1 = min(end, s0 + SG);
+    for (int64_t g0 = s0; g0 < s1; g0 += kThreads) {
+      const int64_t g = g0 + threadIdx.x;
+      float v[G];
+      if (g < s1) {
+        load_group(r, g, v);
+        adjust_group<T, F>(r, g, counts + (F & kHistory ? (g - s0) * G : 0), v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < G; ++j) v[j] = -INFINITY;
+      }
+      const float most = max_of<G>(v);
+      if (summing) sum.add<G>(v, most);
+      const int threads = __syncthreads_count(most >= least);
+      upper += threads * G;
+      if (upper > kRoom) {  // (nobody adds candidates between the barrier above and those below)
+        if (s.count + threads * G > kRoom) {
+          least_key = max(least_key, kth_key(s, K));
+          least = fmaxf(least, value_of((uint32_t)(least_key >> 32)));
+          const int kept = pick(s, least_key);
+          if (threadIdx.x < kept) s.cand[threadIdx.x] = s.few[threadIdx.x];
+          if (threadIdx.x == 0) s.count = kept;
+          __syncthreads();
+        }
+        upper = s.count + threads * G;
+        __syncthreads();
+      }
+#pragma unroll
+      for (int j = 0; j < G; ++j)
+        if (v[j] >= least) {
+          const uint64_t key = key_of(v[j], (int)(g * G - r.a) + j);
+          if (key >= least_key) s.cand[atomicAdd(&s.count, 1)] = key;
+        }
+    }
+  }
+  __syncthreads();
+}
+
+// Group g of a row as it lies in memory, -inf past the row's ends and from group `end` on.
+template <typename T>
+__device__ __forceinline__ uint4 load_raw(const Row<T>& r, int64_t g, int64_t end) {
+  constexpr int G = Row<T>::G;
+  constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+  if (g >= end) return make_uint4(none, none, none, none);
+  const int64_t c0 = g * G - r.a;
+  if (c0 >= 0 && c0 + G <= r.V) return __ldcs(reinterpret_cast<const uint4*>(r.base + g * G));
+  uint32_t u[4] = {none, none, none, none};
+#pragma unroll
+  for (int j = 0; j < G; ++j)
+    if (c0 + j >= 0 && c0 + j < r.V) {
+      if (sizeof(T) == 4) {
+        u[j & 3] = reinterpret_cast<const uint32_t*>(r.base)[g * G + j];
+      } else {
+        const uint32_t h = reinterpret_cast<const unsigned short*>(r.base)[g * G + j];
+        u[j >> 1] = j & 1 ? (u[j >> 1] & 0xFFFFu) | h << 16 : (u[j >> 1] & 0xFFFF0000u) | h;
+      }
+    }
+  return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
 // A cluster of CL blocks a row, each with a run of its groups.
 template <typename T, int F>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
     k_top(int V, int64_t ldz, const T* Z, Adjust adj, int K, int CL, float* top_logit, int32_t* top_id,
           float* lse, int* status) {
-  constexpr int G = Row<T>::G, NV = kEach / G, SG = kSegment / G, CG = kThreads * NV;
+  constexpr int G = Row<T>::G, NV = kEach / G, CG = kThreads * NV, BG = kBits / G;
   extern __shared__ __align__(16) uint8_t top_smem[];
   TopShared& s = *reinterpret_cast<TopShared*>(top_smem);
-  uint32_t* counts = reinterpret_cast<uint32_t*>(top_smem + sizeof(TopShared));
+  uint32_t* bits = reinterpret_cast<uint32_t*>(top_smem + sizeof(TopShared));
+  uint32_t* table = bits + kBits / 32;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = CL > 1 ? (int)cluster_rank() : 0;
   const int64_t row = blockIdx.x / CL;
   if (tid == 0) s.count = 0;
+  if (tid < kWarps) s.part[tid] = 0;
+  __syncthreads();
   tc::grid_dep_launch();
   tc::grid_dep_wait();
   const Row<T> r = make_row<T, F>(Z, ldz, row, V, adj, status);
   const int64_t NG = r.groups(), begin = NG * rank / CL, end = NG * (rank + 1) / CL;
-  float m = kNoLogit, l = 0.f, top = -INFINITY;  // of this thread
-  float least = -3.402823466e38f;                // candidates are at least this large
-  uint64_t least_key = 0;
-  int upper = 0, chunk = 0;  // candidates at most; chunks so far
-  __syncthreads();
-  for (int64_t s0 = begin; s0 < end; s0 += SG) {
-    if ((F & kHistory) && r.hist_n > 0) count_history(r, s0 * G, counts, status);
-    const int64_t s1 = min(end, s0 + SG);
-    for (int64_t g0 = s0; g0 < s1; g0 += CG, ++chunk) {
-      float v[kEach];
-#pragma unroll
-      for (int u = 0; u < NV; ++u) {
-        const int64_t g = g0 + u * kThreads + tid;
-        if (g < s1) {
-          load_group(r, g, v + u * G);
-        } else {
-#pragma unroll
-          for (int j = 0; j < G; ++j) v[u * G + j] = -INFINITY;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < NV; ++u) {
-        const int64_t g = g0 + u * kThreads + tid;
-        if (F && g < s1) adjust_group<T, F>(r, g, counts + (F & kHistory ? (g - s0) * G : 0), v + u * G);
-      }
-      float most = v[0];
-#pragma unroll
-      for (int j = 1; j < kEach; ++j) most = fmaxf(most, v[j]);
-      if (lse) {
-        // (rounded up: of logits beyond 2^31 the terms may vanish but not overflow)
-        const float mc = __fmul_ru(most, kLog2e);
-        if (mc > m) {
-          l *= ex2(m - mc);
-          m = mc;
-        }
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) sum[j & 1] += ex2(fmaf(v[j], kLog2e, -m));
-        l += sum[0] + sum[1];
-      }
-      top = fmaxf(top, most);
-      // after 1, 2, 4, ... chunks the bound rises
-      if ((chunk & (chunk + 1)) == 0) {
-        const float t = reached(s, top, K);
-        if (t > least) {
-          least = t;
-          least_key = (uint64_t)order_of(t) << 32;
-        }
-      }
-      const bool some = most >= least;
-      const int threads = __syncthreads_count(some);
-      if (threads == 0) continue;
-      upper += threads * kEach;
-      if (upper > kRoom) {  // (rare; nobody adds candidates between the barrier above and those below)
-        if (s.count + threads * kEach > kRoom) {
-          least_key = max(least_key, kth_key(s, K));
-          least = fmaxf(least, value_of((uint32_t)(least_key >> 32)));
-          keep_from(s, least_key);
-        }
-        upper = s.count + threads * kEach;
+  Sum sum;
+  const bool hashed = !(F & kHistory) || r.hist_n <= kHashed;
+  if (!hashed) {
+    rising_row<T, F>(s, r, begin, end, K, table, lse != nullptr, sum, status);
+  } else {
+    float top = -INFINITY, least = kLeast;
+    Hash h{table, table, 0};
+    if ((F & kHistory) && r.hist_n > 0) h = hash_history(r, begin * G, end * G, table, status);
+    // a candidate from here on; the barrier after the first chunk comes before any is read
+    auto offer = [&](float v, int id) {
+      const int at = atomicAdd(&s.count, 1);
+      if (at < kRoom) s.cand[at] = key_of(v, id);
+    };
+    int chunk = 0;
+    for (int64_t s0 = begin; s0 < end; s0 += BG) {
+      const int64_t s1 = min(end, s0 + BG), first = s0 * G;  // (first: a multiple of 8)
+      if (F & (kMask | kHistory)) {
         __syncthreads();
-      }
-      if (some) {
-#pragma unroll
-        for (int j = 0; j < kEach; ++j)
-          if (v[j] >= least) {
-            const int64_t g = g0 + j / G * kThreads + tid;
-            const uint64_t key = key_of(v[j], (int)(g * G - r.a) + j % G);
-            if (key >= least_key) s.cand[atomicAdd(&s.count, 1)] = key;
+        // bit e is element first + e, column first + e - a
+        const int words = (int)(((s1 - s0) * G + 31) / 32);
+        for (int w = tid; w < words; w += kThreads) {
+          uint32_t b = 0xFFFFFFFFu;
+          if ((F & kMask) && r.mask) {
+            const int64_t c = first + w * 32 - r.a;  // the word's first column
+            const int64_t q = c >> 5;
+            const int sh = (int)(c & 31);
+            const uint32_t lo = q >= 0 && q < r.words ? __ldg(r.mask + q) : 0u;
+            const uint32_t hi = sh && q + 1 < r.words ? __ldg(r.mask + q + 1) : 0u;
+            b = __funnelshift_r(lo, hi, sh);
           }
+          bits[w] = b;
+        }
+        __syncthreads();
+        if ((F & kHistory) && r.hist_n > 0) {
+          for (int i = tid; i < h.size; i += kThreads) {
+            const uint32_t id = h.token[i] - 1;
+            const int64_t e = (int64_t)id + r.a - first;
+            if (id != 0xFFFFFFFFu && e >= 0 && e < (s1 - s0) * G)
+              atomicAnd(&bits[e >> 5], ~(1u << (e & 31)));
+          }
+          __syncthreads();
+        }
+      }
+      uint4 raw[NV];
+#pragma unroll
+      for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, s0 + u * kThreads + tid, s1);
+      for (int64_t g0 = s0; g0 < s1; g0 += CG, ++chunk) {
+        float v[kEach];
+#pragma unroll
+        for (int u = 0; u < NV; ++u) unpack(raw[u], v + u * G, T());
+        if (g0 + CG < s1) {
+#pragma unroll
+          for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, g0 + CG + u * kThreads + tid, s1);
+        }
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+          const int64_t g = g0 + u * kThreads + tid;
+          if ((F & kBias) && g < s1) adjust_group<T, F & kBias>(r, g, nullptr, v + u * G);
+          if (F & (kMask | kHistory)) {
+            const int e = (int)(g - s0) * G;  // (past the last group its bits do not matter: -inf stands there)
+            const uint32_t b = reinterpret_cast<const uint8_t*>(bits)[min(e, kBits - 8) >> 3] >> (e & 7);
+#pragma unroll
+            for (int j = 0; j < G; ++j)
+              if (!(b >> j & 1u)) v[u * G + j] = -INFINITY;
+          }
+        }
+        const float most = max_of<kEach>(v);
+        if (lse) sum.add<kEach>(v, most);
+        top = fmaxf(top, most);
+        if ((chunk & (chunk + 1)) == 0) {
+          raise(s, top, K);
+          if (chunk == 0) __syncthreads();
+        }
+        least = fmaxf(least, bound(s));
+        if (most >= least) {
+#pragma unroll
+          for (int j = 0; j < kEach; ++j)
+            if (v[j] >= least) offer(v[j], (int)((g0 + j / G * kThreads + tid) * G - r.a) + j % G);
+        }
       }
     }
-  }
-  // the block's largest in order: few candidates, each one's place counted
-  {
-    const float t = reached(s, top, K);  // (and a barrier)
-    if (t > least) least_key = (uint64_t)order_of(t) << 32;
-    if (s.count > 64) keep_from(s, least_key);
-    if (s.count > kThreads) keep_from(s, kth_key(s, K));
+    if ((F & kHistory) && r.hist_n > 0) {
+      // the tokens of the history
+      for (int i = tid; i < h.size; i += kThreads) {
+        const int id = (int)(h.token[i] - 1);
+        if (id < 0) continue;
+        const int64_t e = (int64_t)id + r.a;
+        if ((F & kMask) && r.mask && !(__ldg(r.mask + (id >> 5)) >> (id & 31) & 1u)) continue;
+        float v = to_f32(r.base[e]);
+        if (F & kBias) v = __fadd_rn(v, __ldg(r.bias + id));
+        v = penalised(v, h.count[i], r.rep, r.presence, r.frequency);
+        if (lse) {
+          sum.refer(v);
+          sum.l += ex2(fmaf(v, kLog2e, -sum.m));
+        }
+        if (v >= least) offer(v, id);
+      }
+    }
+    raise(s, top, K);
     __syncthreads();
-    const int n = s.count;
+    if (s.count > kRoom) rising_row<T, F>(s, r, begin, end, K, table, false, sum, status);
+  }
+  // the block's largest in order: few candidates, each one's place counted, four threads a candidate
+  {
+    int n = pick(s, hashed ? (uint64_t)order_of(bound(s)) << 32 : 0);
+    if (n > kThreads) n = pick(s, kth_key(s, K));
     if (tid < kMaxTop) s.best[tid] = 0;
     __syncthreads();
-    if (tid < n) {
-      const uint64_t key = s.cand[tid];
+    for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+      const int i = i0 + tid / 4;
+      const uint64_t key = i < n ? s.few[i] : 0;
       int place = 0;
-      for (int i = 0; i < n; ++i) place += s.cand[i] > key;
-      if (place < K) s.best[place] = key;
+      for (int o = tid & 3; o < n; o += 4) place += s.few[o] > key;
+      place += __shfl_xor_sync(0xffffffffu, place, 1);
+      place += __shfl_xor_sync(0xffffffffu, place, 2);
+      if ((tid & 3) == 0 && i < n && place < K) s.best[place] = key;
     }
   }
   if (lse) {
-    float top_m = m;
+    float top_m = sum.m, l = sum.l;
 #pragma unroll
     for (int o = 16; o; o >>= 1) top_m = fmaxf(top_m, __shfl_xor_sync(0xffffffffu, top_m, o));
-    l *= ex2(m - top_m);
+    l *= ex2(sum.m - top_m);
 #pragma unroll
     for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     if (lane == 0) s.m[warp] = top_m, s.l[warp] = l;
@@ -484,9 +779,9 @@ __global__ void __launch_bounds__(kThreads)
   __syncthreads();
   if (lse && tid == 0) {
     float bm = s.m[0];
-    for (int w = 1; w < kThreads / 32; ++w) bm = fmaxf(bm, s.m[w]);
+    for (int w = 1; w < kWarps; ++w) bm = fmaxf(bm, s.m[w]);
     float bl = 0.f;
-    for (int w = 0; w < kThreads / 32; ++w) bl += s.l[w] * ex2(s.m[w] - bm);
+    for (int w = 0; w < kWarps; ++w) bl += s.l[w] * ex2(s.m[w] - bm);
     s.block_m = bm;
     s.block_l = bl;
   }
@@ -548,13 +843,17 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 // ------------------------------------------------------------------------------ host
-template <typename T, int F>
+template <typename T, int F, int W>
 cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int64_t ldo, void* out,
                        int* status, cudaStream_t st) {
-  const int segments = (int)(((int64_t)V + 7 + kSegment - 1) / kSegment);
+  constexpr int G = Row<T, W>::G;
+  // runs of 8192 elements, longer ones where there are blocks enough (a history is read for each run)
+  const int64_t groups = ((int64_t)V + 2 * G - 2) / G;
+  int64_t per = 8192 / G;
+  while (per * G < kBits && n * ((groups + 2 * per - 1) / (2 * per)) >= 152 * 16) per *= 2;
   const cudaError_t e =
-      launch_pdl(k_adjust<T, F>, dim3((unsigned)n, (unsigned)segments), dim3(kThreads), 0, st, n, V, ldz,
-                 static_cast<const T*>(Z), adj, ldo, static_cast<T*>(out), status);
+      launch_pdl(k_adjust<T, F, W>, dim3((unsigned)n, (unsigned)((groups + per - 1) / per)), dim3(kThreads), 0, st,
+                 V, ldz, static_cast<const T*>(Z), adj, ldo, static_cast<T*>(out), (int)per, status);
   if (e == cudaSuccess) note_launch();
   return e;
 }
@@ -570,7 +869,7 @@ template <typename T, int F>
 cudaError_t run_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int K, float* top_logit,
                     int32_t* top_id, float* lse, int* status, cudaStream_t st) {
   const int CL = cluster_of(n, V);
-  constexpr int smem = (int)sizeof(TopShared) + (F & kHistory ? kSegment * 4 : 0);
+  constexpr int smem = (int)sizeof(TopShared) + (F & (kMask | kHistory) ? kBits / 8 : 0) + (F & kHistory ? kSlots * 8 : 0);
   static std::atomic<uint64_t> done{0};
   cudaError_t e = allow_smem(k_top<T, F>, smem, done);
   if (e != cudaSuccess) return e;
@@ -617,8 +916,14 @@ cudaError_t logits_adjust(int bf16, int64_t n, int V, int64_t ldz, const void* Z
   const Adjust adj = make_adjust(b, V);
   return with_flags(flags_of(b), [&](auto f) {
     constexpr int F = decltype(f)::value;
-    return bf16 ? run_adjust<__nv_bfloat16, F>(n, V, ldz, Z, adj, ldo, out, status, st)
-                : run_adjust<float, F>(n, V, ldz, Z, adj, ldo, out, status, st);
+    // Rows that begin anywhere in 16 bytes meet the biases unaligned, a 16-byte group's G of them one by one and
+    // G apart in a warp; in groups of 4 bytes a warp's are side by side.
+    if constexpr (F & kBias)
+      if (ldz * (bf16 ? 2 : 4) % 16)
+        return bf16 ? run_adjust<__nv_bfloat16, F, 4>(n, V, ldz, Z, adj, ldo, out, status, st)
+                    : run_adjust<float, F, 4>(n, V, ldz, Z, adj, ldo, out, status, st);
+    return bf16 ? run_adjust<__nv_bfloat16, F, 16>(n, V, ldz, Z, adj, ldo, out, status, st)
+                : run_adjust<float, F, 16>(n, V, ldz, Z, adj, ldo, out, status, st);
   });
 }
 

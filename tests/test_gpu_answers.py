@@ -347,6 +347,44 @@ def test_top_from_rows_beyond_32_bit_offsets():
     assert np.array_equal(bits(Z), bits(torch.from_numpy(ref.adjusted(z_bf16(z), **kw)).to(torch.bfloat16).cuda()))
 
 
+@pytest.mark.parametrize("dtype,pad", [("f32", 0), ("bf16", 1), ("bf16", 7)])
+@pytest.mark.parametrize("n", [1, 3, 160])
+def test_rows_longer_than_their_bits_in_shared_memory(dtype, pad, n):
+    """Masks and histories over several runs of 65536 elements, with tokens at the runs' ends."""
+    V = 140001
+    rng = np.random.default_rng(n)
+    Z, _ = rows(n, V, pad, dtype)
+    Z.copy_(dev(rng.standard_normal((n, V)), dtype))
+    allowed = rng.random((2, V)) < 0.9
+    history = [np.concatenate([rng.integers(0, V, rng.integers(0, 300)), np.arange(65526, 65546)]) for _ in range(n)]
+    penalty = np.tile(np.array([[0.01, -3.0, -1.0]], np.float32), (n, 1))  # the history's tokens come first
+    off = np.concatenate([[0], np.cumsum([len(h) for h in history])])
+    kw = dict(allowed=allowed, mask_row=rng.integers(-1, 2, n), history=history, penalty=penalty)
+    adjust = L.LogitAdjust(mask=torch.from_numpy(ref.pack_mask(allowed)).cuda(), mask_row=ints(kw["mask_row"]),
+                           history=ints(np.concatenate(history)), history_off=ints(off, np.int64), penalty=dev(penalty))
+    want = ref.adjusted(host(Z), **kw)
+    check_top(Z, 33, dtype, adjust, want)
+    out, _ = rows(n, V, 0, dtype)
+    L.logits_adjust(dtype, Z, out, adjust)
+    assert np.array_equal(bits(out), bits(torch.from_numpy(want).to(TD[dtype]).cuda()))
+
+
+@pytest.mark.parametrize("n", [4, 400])
+@pytest.mark.parametrize("size", [1, 32, 33, 512, 1023, 1024, 1025, 3000])
+def test_histories_of_every_size_of_table(size, n):
+    V = 9001
+    rng = np.random.default_rng(size)
+    z = dev(rng.standard_normal((n, V)) * 2)
+    history = [rng.integers(0, V if i % 2 else 40, size) for i in range(n)]
+    penalty = np.stack([1 + rng.random(n), rng.random(n), rng.random(n) / 50], 1).astype(np.float32)
+    off = np.concatenate([[0], np.cumsum([len(h) for h in history])])
+    adjust = L.LogitAdjust(history=ints(np.concatenate(history)), history_off=ints(off, np.int64), penalty=dev(penalty))
+    want = ref.adjusted(host(z), history=history, penalty=penalty)
+    check_top(z, 20, "f32", adjust, want)
+    L.logits_adjust("f32", z, z, adjust)
+    assert np.array_equal(bits(z), bits(torch.from_numpy(want).cuda()))
+
+
 def z_bf16(z):
     return torch.from_numpy(np.asarray(z, np.float32)).to(torch.bfloat16).double().numpy()
 
