@@ -375,12 +375,12 @@ constexpr float kNoLogit = -3.0e38f;  // reference of a sum without terms
 constexpr float kLeast = -3.402823466e38f;
 
 struct TopShared {
-  uint64_t cand[kRoom];
-  uint64_t few[kThreads];
+  uint2 cand[kRoom];
+  uint64_t few[kThreads > kMaxCluster * kMaxTop ? kThreads : kMaxCluster * kMaxTop];
   uint64_t best[kMaxTop];
   float m[kWarps], l[kWarps];
   float block_m, block_l;
-  uint32_t part[kWarps];  // of the bound, as orders
+  alignas(16) uint32_t part[kWarps];  // of the bound, as orders
   int count, found, sum[64];
 };
 // After it in dynamic shared memory, as far as the adjustment needs them: the bits, then the hash table, whose
@@ -397,6 +397,9 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 __device__ __forceinline__ uint64_t key_of(float v, int id) {
   return (uint64_t)order_of(v) << 32 | (uint32_t)~id;
 }
+// A candidate: a logit and its token (its key is made where it is wanted, of few of them).
+__device__ __forceinline__ uint2 candidate(float v, int id) { return make_uint2(__float_as_uint(v), (uint32_t)id); }
+__device__ __forceinline__ uint64_t key_of(uint2 c) { return key_of(__uint_as_float(c.x), (int)c.y); }
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -485,7 +488,7 @@ __device__ __noinline__ uint64_t kth_key(TopShared& s, int K) {
   for (int bit = 63; bit >= 0; --bit) {
     const uint64_t trial = t | (uint64_t)1 << bit;
     int c = 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) c += s.cand[i] >= trial;
+    for (int i = threadIdx.x; i < n; i += kThreads) c += key_of(s.cand[i]) >= trial;
     c = __reduce_add_sync(0xffffffffu, c);
     if ((threadIdx.x & 31) == 0 && c) atomicAdd(&s.sum[bit], c);
     __syncthreads();
@@ -501,7 +504,7 @@ __device__ __forceinline__ int pick(TopShared& s, uint64_t t) {
   __syncthreads();
   const int n = s.count;
   for (int i = threadIdx.x; i < n; i += kThreads) {
-    const uint64_t key = s.cand[i];
+    const uint64_t key = key_of(s.cand[i]);
     if (key >= t) {
       const int at = atomicAdd(&s.found, 1);
       if (at < kThreads) s.few[at] = key;
@@ -524,10 +527,14 @@ __device__ __forceinline__ void raise(TopShared& s, float top, int K) {
 }
 // The bound: the least of the parts, as they are found.
 __device__ __forceinline__ float bound(const TopShared& s) {
-  const volatile uint32_t* p = s.part;
-  uint32_t t = p[0];
+  static_assert(kWarps == 8, "two reads");
+  uint32_t p[8];
 #pragma unroll
-  for (int w = 1; w < kWarps; ++w) t = min(t, p[w]);
+  for (int k = 0; k < 8; k += 4)
+    asm volatile("ld.volatile.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(p[k]), "=r"(p[k + 1]), "=r"(p[k + 2]), "=r"(p[k + 3])
+                 : "r"(smem_u32(s.part + k)));
+  const uint32_t t = min(min(min(p[0], p[1]), min(p[2], p[3])), min(min(p[4], p[5]), min(p[6], p[7])));
   return t == 0 ? kLeast : fmaxf(kLeast, value_of(t));
 }
 
@@ -589,7 +596,10 @@ __device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t b
           least_key = max(least_key, kth_key(s, K));
           least = fmaxf(least, value_of((uint32_t)(least_key >> 32)));
           const int kept = pick(s, least_key);
-          if (threadIdx.x < kept) s.cand[threadIdx.x] = s.few[threadIdx.x];
+          if (threadIdx.x < kept) {
+            const uint64_t key = s.few[threadIdx.x];
+            s.cand[threadIdx.x] = candidate(value_of((uint32_t)(key >> 32)), (int)~(uint32_t)key);
+          }
           if (threadIdx.x == 0) s.count = kept;
           __syncthreads();
         }
@@ -599,8 +609,8 @@ __device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t b
 #pragma unroll
       for (int j = 0; j < G; ++j)
         if (v[j] >= least) {
-          const uint64_t key = key_of(v[j], (int)(g * G - r.a) + j);
-          if (key >= least_key) s.cand[atomicAdd(&s.count, 1)] = key;
+          const uint2 c = candidate(v[j], (int)(g * G - r.a) + j);
+          if (key_of(c) >= least_key) s.cand[atomicAdd(&s.count, 1)] = c;
         }
     }
   }
@@ -657,24 +667,24 @@ __global__ void __launch_bounds__(kThreads, 4)
     float top = -INFINITY, least = kLeast;
     Hash h{table, table, 0};
     if ((F & kHistory) && r.hist_n > 0) h = hash_history(r, begin * G, end * G, table, status);
-    // a candidate from here on; the barrier after the first chunk comes before any is read
+    // (the barrier after the first chunk comes before any is read)
     auto offer = [&](float v, int id) {
       const int at = atomicAdd(&s.count, 1);
-      if (at < kRoom) s.cand[at] = key_of(v, id);
+      if (at < kRoom) s.cand[at] = candidate(v, id);
     };
+    const uint4* lane_base = reinterpret_cast<const uint4*>(r.base) + tid;
+    const uint8_t* lane_bits = reinterpret_cast<const uint8_t*>(bits) + tid * G / 8;
     int chunk = 0;
-    for (int64_t s0 = begin; s0 < end; s0 += BG) {
-      const int64_t s1 = min(end, s0 + BG), first = s0 * G;  // (first: a multiple of 8)
+    for (int s0 = (int)begin; s0 < (int)end; s0 += BG) {
+      const int s1 = min((int)end, s0 + BG), first = s0 * G;  // (first: a multiple of 8)
       if (F & (kMask | kHistory)) {
         __syncthreads();
         // bit e is element first + e, column first + e - a
-        const int words = (int)(((s1 - s0) * G + 31) / 32);
+        const int words = ((s1 - s0) * G + 31) / 32;
         for (int w = tid; w < words; w += kThreads) {
           uint32_t b = 0xFFFFFFFFu;
           if ((F & kMask) && r.mask) {
-            const int64_t c = first + w * 32 - r.a;  // the word's first column
-            const int64_t q = c >> 5;
-            const int sh = (int)(c & 31);
+            const int c = first + w * 32 - r.a, q = c >> 5, sh = c & 31;  // c: the word's first column
             const uint32_t lo = q >= 0 && q < r.words ? __ldg(r.mask + q) : 0u;
             const uint32_t hi = sh && q + 1 < r.words ? __ldg(r.mask + q + 1) : 0u;
             b = __funnelshift_r(lo, hi, sh);
@@ -685,34 +695,57 @@ __global__ void __launch_bounds__(kThreads, 4)
         if ((F & kHistory) && r.hist_n > 0) {
           for (int i = tid; i < h.size; i += kThreads) {
             const uint32_t id = h.token[i] - 1;
-            const int64_t e = (int64_t)id + r.a - first;
-            if (id != 0xFFFFFFFFu && e >= 0 && e < (s1 - s0) * G)
-              atomicAnd(&bits[e >> 5], ~(1u << (e & 31)));
+            const int e = (int)id + r.a - first;
+            if (id != 0xFFFFFFFFu && e >= 0 && e < (s1 - s0) * G) atomicAnd(&bits[e >> 5], ~(1u << (e & 31)));
           }
           __syncthreads();
         }
       }
+      // chunks with nothing past the row's or the run's ends are read without a look at each group
+      auto inside = [&](int g0) { return g0 * G >= r.a && g0 + CG <= s1 && (g0 + CG) * G - r.a <= V; };
       uint4 raw[NV];
+      auto fetch = [&](int g0) {
+        if (inside(g0)) {
 #pragma unroll
-      for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, s0 + u * kThreads + tid, s1);
-      for (int64_t g0 = s0; g0 < s1; g0 += CG, ++chunk) {
+          for (int u = 0; u < NV; ++u) raw[u] = __ldcs(lane_base + g0 + u * kThreads);
+        } else {
+#pragma unroll
+          for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, g0 + u * kThreads + tid, s1);
+        }
+      };
+      fetch(s0);
+      for (int g0 = s0; g0 < s1; g0 += CG, ++chunk) {
         float v[kEach];
 #pragma unroll
         for (int u = 0; u < NV; ++u) unpack(raw[u], v + u * G, T());
-        if (g0 + CG < s1) {
+        if (g0 + CG < s1) fetch(g0 + CG);
+        const int c0 = (g0 + tid) * G - r.a;  // column of v[0]
+        if (F & kBias) {
+          if (r.a == 0 && inside(g0)) {
+            const float4* b = reinterpret_cast<const float4*>(r.bias + c0);
 #pragma unroll
-          for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, g0 + CG + u * kThreads + tid, s1);
+            for (int j = 0; j < kEach; j += 4) {
+              const float4 x = __ldg(b + (j / G * kThreads * G + j % G) / 4);
+              v[j] = __fadd_rn(v[j], x.x);
+              v[j + 1] = __fadd_rn(v[j + 1], x.y);
+              v[j + 2] = __fadd_rn(v[j + 2], x.z);
+              v[j + 3] = __fadd_rn(v[j + 3], x.w);
+            }
+          } else {
+#pragma unroll
+            for (int u = 0; u < NV; ++u)
+              if (g0 + u * kThreads + tid < s1)
+                adjust_group<T, F & kBias>(r, g0 + u * kThreads + tid, nullptr, v + u * G);
+          }
         }
+        if (F & (kMask | kHistory)) {
+          const uint8_t* q = lane_bits + (g0 - s0) * G / 8;
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
-          const int64_t g = g0 + u * kThreads + tid;
-          if ((F & kBias) && g < s1) adjust_group<T, F & kBias>(r, g, nullptr, v + u * G);
-          if (F & (kMask | kHistory)) {
-            const int e = (int)(g - s0) * G;  // (past the last group its bits do not matter: -inf stands there)
-            const uint32_t b = reinterpret_cast<const uint8_t*>(bits)[min(e, kBits - 8) >> 3] >> (e & 7);
+          for (int u = 0; u < NV; ++u) {
+            const uint32_t b = G == 8 ? q[u * kThreads] : q[u * kThreads / 2] >> (tid & 1) * 4;
 #pragma unroll
             for (int j = 0; j < G; ++j)
-              if (!(b >> j & 1u)) v[u * G + j] = -INFINITY;
+              if (!(b & 1u << j)) v[u * G + j] = -INFINITY;
           }
         }
         const float most = max_of<kEach>(v);
@@ -726,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, 4)
         if (most >= least) {
 #pragma unroll
           for (int j = 0; j < kEach; ++j)
-            if (v[j] >= least) offer(v[j], (int)((g0 + j / G * kThreads + tid) * G - r.a) + j % G);
+            if (v[j] >= least) offer(v[j], c0 + j / G * kThreads * G + j % G);
         }
       }
     }
@@ -789,17 +822,17 @@ __global__ void __launch_bounds__(kThreads, 4)
     cluster_sync();
     if (rank == 0) {
       // the blocks' lists, each in order: a key's place is the number of larger ones in all lists
-      for (int i = tid; i < CL * K; i += kThreads) s.cand[i] = cluster_ld64(&s.best[i % K], i / K);
+      for (int i = tid; i < CL * K; i += kThreads) s.few[i] = cluster_ld64(&s.best[i % K], i / K);
       __syncthreads();
       for (int i = tid; i < CL * K; i += kThreads) {
-        const uint64_t key = s.cand[i];
+        const uint64_t key = s.few[i];
         if (key == 0) continue;
         int place = 0;
         for (int b = 0; b < CL; ++b) {
           int lo = 0, hi = K;  // entries of list b larger than key
           while (lo < hi) {
             const int mid = (lo + hi) / 2;
-            if (s.cand[b * K + mid] > key) lo = mid + 1; else hi = mid;
+            if (s.few[b * K + mid] > key) lo = mid + 1; else hi = mid;
           }
           place += lo;
         }
@@ -813,7 +846,7 @@ __global__ void __launch_bounds__(kThreads, 4)
         int lo = 0, hi = K;
         while (lo < hi) {
           const int mid = (lo + hi) / 2;
-          if (s.cand[b * K + mid] != 0) lo = mid + 1; else hi = mid;
+          if (s.few[b * K + mid] != 0) lo = mid + 1; else hi = mid;
         }
         have += lo;
       }
