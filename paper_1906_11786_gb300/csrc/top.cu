@@ -241,23 +241,32 @@ __device__ __forceinline__ void hash_add(const Hash& h, uint32_t id) {
   }
 }
 
-// The table of the tokens of r's history whose elements (column + a) are in [first, last); the whole block calls
-// it, and a barrier has to follow before the table is read.
+// An empty table for the tokens of r's history (a barrier has to follow before it is filled).
 template <typename T, int W>
-__device__ __forceinline__ Hash hash_history(const Row<T, W>& r, int64_t first, int64_t last, uint32_t* table,
-                                             int* status) {
+__device__ __forceinline__ Hash clear_hash(const Row<T, W>& r, uint32_t* table) {
   Hash h{table, nullptr, 64};
   while (h.size < 2 * r.hist_n) h.size *= 2;
   h.count = table + h.size;
-  for (int i = threadIdx.x; i < 2 * h.size; i += kThreads) table[i] = 0;
-  __syncthreads();
+  for (int i = threadIdx.x; i < h.size / 2; i += kThreads)
+    reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
+  return h;
+}
+// Adds the tokens whose elements (column + a) are in [first, last), calling seen(element) for each (a barrier has
+// to follow before the table is read).
+template <typename T, int W, typename Fn>
+__device__ __forceinline__ void fill_hash(const Hash& h, const Row<T, W>& r, int64_t first, int64_t last, int* status,
+                                          Fn seen) {
+  int next = threadIdx.x < r.hist_n ? r.hist[threadIdx.x] : -1;
   for (int i = threadIdx.x; i < (int)r.hist_n; i += kThreads) {
-    const int id = r.hist[i];
+    const int id = next;
+    if (i + kThreads < (int)r.hist_n) next = r.hist[i + kThreads];
     if (id >= r.V) report(status, kSiteHistoryId);
     const int64_t e = (int64_t)id + r.a;
-    if (id >= 0 && id < r.V && e >= first && e < last) hash_add(h, (uint32_t)id);
+    if (id >= 0 && id < r.V && e >= first && e < last) {
+      hash_add(h, (uint32_t)id);
+      seen(e);
+    }
   }
-  return h;
 }
 
 // ------------------------------------------------------------------------------ adjustment
@@ -321,7 +330,9 @@ __global__ void __launch_bounds__(kThreads)
   }
   Hash h{nullptr, nullptr, 0};
   if ((F & kHistory) && r.hist_n > 0) {
-    h = hash_history(r, g0 * G, g1 * G, table, status);
+    h = clear_hash(r, table);
+    __syncthreads();
+    fill_hash(h, r, g0 * G, g1 * G, status, [](int64_t) {});
     __syncthreads();
     for (int k = threadIdx.x; k < h.size; k += kThreads)
       if (h.token[k]) raw[k] = to_f32(r.base[(int64_t)h.token[k] - 1 + r.a]);
@@ -370,13 +381,14 @@ constexpr int kBits = 65536;  // elements whose bits are in shared memory at a t
 constexpr int kRoom = 2304;   // candidates: those of a pass of rising_row (2048) and the K before it
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kFew = kMaxCluster * kMaxTop;  // candidates that are put in order
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoLogit = -3.0e38f;  // reference of a sum without terms
 constexpr float kLeast = -3.402823466e38f;
 
 struct TopShared {
   uint2 cand[kRoom];
-  uint64_t few[kThreads > kMaxCluster * kMaxTop ? kThreads : kMaxCluster * kMaxTop];
+  uint64_t few[kFew];
   uint64_t best[kMaxTop];
   float m[kWarps], l[kWarps];
   float block_m, block_l;
@@ -497,17 +509,15 @@ __device__ __noinline__ uint64_t kth_key(TopShared& s, int K) {
   return t;
 }
 
-// The candidates with keys of t or more (kThreads at most) to `few`; the whole block calls it.  Their number.
+// The candidates with keys of t or more to `few` (kFew of them at most); the whole block calls it, with the
+// candidates complete and `found` 0 behind a barrier.  Their number.
 __device__ __forceinline__ int pick(TopShared& s, uint64_t t) {
-  __syncthreads();
-  if (threadIdx.x == 0) s.found = 0;
-  __syncthreads();
   const int n = s.count;
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t key = key_of(s.cand[i]);
     if (key >= t) {
       const int at = atomicAdd(&s.found, 1);
-      if (at < kThreads) s.few[at] = key;
+      if (at < kFew) s.few[at] = key;
     }
   }
   __syncthreads();
@@ -595,6 +605,8 @@ __device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t b
         if (s.count + threads * G > kRoom) {
           least_key = max(least_key, kth_key(s, K));
           least = fmaxf(least, value_of((uint32_t)(least_key >> 32)));
+          if (threadIdx.x == 0) s.found = 0;
+          __syncthreads();
           const int kept = pick(s, least_key);
           if (threadIdx.x < kept) {
             const uint64_t key = s.few[threadIdx.x];
@@ -614,6 +626,7 @@ __device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t b
         }
     }
   }
+  if (threadIdx.x == 0) s.found = 0;
   __syncthreads();
 }
 
@@ -642,7 +655,7 @@ __device__ __forceinline__ uint4 load_raw(const Row<T>& r, int64_t g, int64_t en
 // A cluster of CL blocks a row, each with a run of its groups.
 template <typename T, int F>
 __global__ void __launch_bounds__(kThreads, 4)
-    k_top(int V, int64_t ldz, const T* Z, Adjust adj, int K, int CL, float* top_logit, int32_t* top_id,
+    k_top(int V, int64_t ldz, const T* Z, Adjust adj, int K, int log_cl, float* top_logit, int32_t* top_id,
           float* lse, int* status) {
   constexpr int G = Row<T>::G, NV = kEach / G, CG = kThreads * NV, BG = kBits / G;
   extern __shared__ __align__(16) uint8_t top_smem[];
@@ -650,15 +663,16 @@ __global__ void __launch_bounds__(kThreads, 4)
   uint32_t* bits = reinterpret_cast<uint32_t*>(top_smem + sizeof(TopShared));
   uint32_t* table = bits + kBits / 32;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = CL > 1 ? (int)cluster_rank() : 0;
-  const int64_t row = blockIdx.x / CL;
-  if (tid == 0) s.count = 0;
+  const int CL = 1 << log_cl, rank = CL > 1 ? (int)cluster_rank() : 0;
+  const int64_t row = blockIdx.x >> log_cl;
+  if (tid == 0) s.count = 0, s.found = 0;
   if (tid < kWarps) s.part[tid] = 0;
   __syncthreads();
   tc::grid_dep_launch();
   tc::grid_dep_wait();
   const Row<T> r = make_row<T, F>(Z, ldz, row, V, adj, status);
-  const int64_t NG = r.groups(), begin = NG * rank / CL, end = NG * (rank + 1) / CL;
+  const int NG = r.groups(), begin = (int)((int64_t)NG * rank >> log_cl),
+            end = (int)((int64_t)NG * (rank + 1) >> log_cl);
   Sum sum;
   const bool hashed = !(F & kHistory) || r.hist_n <= kHashed;
   if (!hashed) {
@@ -666,7 +680,6 @@ __global__ void __launch_bounds__(kThreads, 4)
   } else {
     float top = -INFINITY, least = kLeast;
     Hash h{table, table, 0};
-    if ((F & kHistory) && r.hist_n > 0) h = hash_history(r, begin * G, end * G, table, status);
     // (the barrier after the first chunk comes before any is read)
     auto offer = [&](float v, int id) {
       const int at = atomicAdd(&s.count, 1);
@@ -675,32 +688,8 @@ __global__ void __launch_bounds__(kThreads, 4)
     const uint4* lane_base = reinterpret_cast<const uint4*>(r.base) + tid;
     const uint8_t* lane_bits = reinterpret_cast<const uint8_t*>(bits) + tid * G / 8;
     int chunk = 0;
-    for (int s0 = (int)begin; s0 < (int)end; s0 += BG) {
-      const int s1 = min((int)end, s0 + BG), first = s0 * G;  // (first: a multiple of 8)
-      if (F & (kMask | kHistory)) {
-        __syncthreads();
-        // bit e is element first + e, column first + e - a
-        const int words = ((s1 - s0) * G + 31) / 32;
-        for (int w = tid; w < words; w += kThreads) {
-          uint32_t b = 0xFFFFFFFFu;
-          if ((F & kMask) && r.mask) {
-            const int c = first + w * 32 - r.a, q = c >> 5, sh = c & 31;  // c: the word's first column
-            const uint32_t lo = q >= 0 && q < r.words ? __ldg(r.mask + q) : 0u;
-            const uint32_t hi = sh && q + 1 < r.words ? __ldg(r.mask + q + 1) : 0u;
-            b = __funnelshift_r(lo, hi, sh);
-          }
-          bits[w] = b;
-        }
-        __syncthreads();
-        if ((F & kHistory) && r.hist_n > 0) {
-          for (int i = tid; i < h.size; i += kThreads) {
-            const uint32_t id = h.token[i] - 1;
-            const int e = (int)id + r.a - first;
-            if (id != 0xFFFFFFFFu && e >= 0 && e < (s1 - s0) * G) atomicAnd(&bits[e >> 5], ~(1u << (e & 31)));
-          }
-          __syncthreads();
-        }
-      }
+    for (int s0 = begin; s0 < end; s0 += BG) {
+      const int s1 = min(end, s0 + BG), first = s0 * G;  // (first: a multiple of 8)
       // chunks with nothing past the row's or the run's ends are read without a look at each group
       auto inside = [&](int g0) { return g0 * G >= r.a && g0 + CG <= s1 && (g0 + CG) * G - r.a <= V; };
       uint4 raw[NV];
@@ -714,6 +703,37 @@ __global__ void __launch_bounds__(kThreads, 4)
         }
       };
       fetch(s0);
+      if (F & (kMask | kHistory)) {
+        const bool past = (F & kHistory) && r.hist_n > 0;
+        if (s0 != begin) __syncthreads();
+        // bit e is element first + e, column first + e - a
+        const int words = ((s1 - s0) * G + 31) / 32;
+        for (int w = tid; w < words; w += kThreads) {
+          uint32_t b = 0xFFFFFFFFu;
+          if ((F & kMask) && r.mask) {
+            const int c = first + w * 32 - r.a, q = c >> 5, sh = c & 31;  // c: the word's first column
+            const uint32_t lo = q >= 0 && q < r.words ? __ldg(r.mask + q) : 0u;
+            const uint32_t hi = sh && q + 1 < r.words ? __ldg(r.mask + q + 1) : 0u;
+            b = __funnelshift_r(lo, hi, sh);
+          }
+          bits[w] = b;
+        }
+        auto leave_out = [&](int64_t element) {
+          const int64_t e = element - first;
+          if (e >= 0 && e < (s1 - s0) * G) atomicAnd(&bits[e >> 5], ~(1u << (e & 31)));
+        };
+        if (past && s0 == begin) h = clear_hash(r, table);
+        __syncthreads();
+        if (past) {
+          if (s0 == begin) {
+            fill_hash(h, r, begin * G, end * G, status, leave_out);
+          } else {
+            for (int i = tid; i < h.size; i += kThreads)
+              if (h.token[i]) leave_out((int64_t)h.token[i] - 1 + r.a);
+          }
+          __syncthreads();
+        }
+      }
       for (int g0 = s0; g0 < s1; g0 += CG, ++chunk) {
         float v[kEach];
 #pragma unroll
@@ -781,24 +801,6 @@ __global__ void __launch_bounds__(kThreads, 4)
       }
     }
     raise(s, top, K);
-    __syncthreads();
-    if (s.count > kRoom) rising_row<T, F>(s, r, begin, end, K, table, false, sum, status);
-  }
-  // the block's largest in order: few candidates, each one's place counted, four threads a candidate
-  {
-    int n = pick(s, hashed ? (uint64_t)order_of(bound(s)) << 32 : 0);
-    if (n > kThreads) n = pick(s, kth_key(s, K));
-    if (tid < kMaxTop) s.best[tid] = 0;
-    __syncthreads();
-    for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
-      const int i = i0 + tid / 4;
-      const uint64_t key = i < n ? s.few[i] : 0;
-      int place = 0;
-      for (int o = tid & 3; o < n; o += 4) place += s.few[o] > key;
-      place += __shfl_xor_sync(0xffffffffu, place, 1);
-      place += __shfl_xor_sync(0xffffffffu, place, 2);
-      if ((tid & 3) == 0 && i < n && place < K) s.best[place] = key;
-    }
   }
   if (lse) {
     float top_m = sum.m, l = sum.l;
@@ -810,13 +812,49 @@ __global__ void __launch_bounds__(kThreads, 4)
     if (lane == 0) s.m[warp] = top_m, s.l[warp] = l;
   }
   __syncthreads();
-  if (lse && tid == 0) {
-    float bm = s.m[0];
+  if (hashed && s.count > kRoom) rising_row<T, F>(s, r, begin, end, K, table, false, sum, status);
+  if (lse && tid == kThreads - 1) {
+    float bm = s.m[0], bl = 0.f;
+#pragma unroll
     for (int w = 1; w < kWarps; ++w) bm = fmaxf(bm, s.m[w]);
-    float bl = 0.f;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) bl += s.l[w] * ex2(s.m[w] - bm);
-    s.block_m = bm;
-    s.block_l = bl;
+    if (CL > 1)
+      s.block_m = bm, s.block_l = bl;
+    else
+      lse[row] = lse_of(bm, bl);
+  }
+  // the block's largest in order: few candidates, each one's place counted, four threads a candidate
+  int n = pick(s, hashed ? (uint64_t)order_of(bound(s)) << 32 : 0);
+  if (n > kFew) {
+    const uint64_t t = kth_key(s, K);
+    if (tid == 0) s.found = 0;
+    __syncthreads();
+    n = pick(s, t);
+  }
+  auto answer = [&](int place, uint64_t key) {
+    top_logit[row * K + place] = key ? value_of((uint32_t)(key >> 32)) : -INFINITY;
+    top_id[row * K + place] = key ? (int32_t) ~(uint32_t)key : -1;
+  };
+  for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+    const int i = i0 + tid / 4;
+    const uint64_t key = i < n ? s.few[i] : 0;
+    int place = 0;
+    for (int o = tid & 3; o < n; o += 4) place += s.few[o] > key;
+    place += __shfl_xor_sync(0xffffffffu, place, 1);
+    place += __shfl_xor_sync(0xffffffffu, place, 2);
+    if ((tid & 3) == 0 && i < n && place < K) {
+      if (CL > 1)
+        s.best[place] = key;
+      else
+        answer(place, key);
+    }
+  }
+  for (int k = n + tid; k < K; k += kThreads) {
+    if (CL > 1)
+      s.best[k] = 0;
+    else
+      answer(k, 0);
   }
   if (CL > 1) {
     cluster_sync();
@@ -864,14 +902,6 @@ __global__ void __launch_bounds__(kThreads, 4)
     }
     __syncthreads();
     cluster_sync();  // (no block leaves while the first may still read its list)
-  } else {
-    __syncthreads();
-    if (tid < K) {
-      const uint64_t key = s.best[tid];
-      top_logit[row * K + tid] = key ? value_of((uint32_t)(key >> 32)) : -INFINITY;
-      top_id[row * K + tid] = key ? (int32_t) ~(uint32_t)key : -1;
-    }
-    if (lse && tid == 0) lse[row] = lse_of(s.block_m, s.block_l);
   }
 }
 
@@ -891,17 +921,17 @@ cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjus
   return e;
 }
 
-// Blocks a row: one where rows fill the card, else as many as still leave a block a chunk.
+// Blocks a row, as a power of two: one where rows fill the card, else as many as still leave a block a chunk.
 int cluster_of(int64_t n, int V) {
-  int c = 1;
-  while (c < kMaxCluster && n * c * 2 <= 152 * 2 && V >= c * 2 * kChunk / 4) c *= 2;
+  int c = 0;
+  while (1 << c < kMaxCluster && (n << (c + 1)) <= 152 * 2 && V >> (c + 1) >= kChunk / 4) ++c;
   return c;
 }
 
 template <typename T, int F>
 cudaError_t run_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int K, float* top_logit,
                     int32_t* top_id, float* lse, int* status, cudaStream_t st) {
-  const int CL = cluster_of(n, V);
+  const int log_cl = cluster_of(n, V), CL = 1 << log_cl;
   constexpr int smem = (int)sizeof(TopShared) + (F & (kMask | kHistory) ? kBits / 8 : 0) + (F & kHistory ? kSlots * 8 : 0);
   static std::atomic<uint64_t> done{0};
   cudaError_t e = allow_smem(k_top<T, F>, smem, done);
@@ -920,7 +950,7 @@ cudaError_t run_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& 
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL > 1 ? 2 : 1;
-  e = cudaLaunchKernelEx(&cfg, k_top<T, F>, V, ldz, static_cast<const T*>(Z), adj, K, CL, top_logit, top_id, lse,
+  e = cudaLaunchKernelEx(&cfg, k_top<T, F>, V, ldz, static_cast<const T*>(Z), adj, K, log_cl, top_logit, top_id, lse,
                          status);
   if (e == cudaSuccess) note_launch();
   return e;
