@@ -26,7 +26,8 @@ using namespace tc;
 
 namespace {
 
-constexpr int kThreads = 320;  // 8 epilogue warps, a TMA warp, an MMA warp
+constexpr int kEpilogue = 16;  // warps of the epilogue, four warpgroups; then a TMA warp and an MMA warp
+constexpr int kThreads = (kEpilogue + 2) * 32;
 constexpr int kMaxStages = 8;
 
 inline size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -107,17 +108,24 @@ __global__ void __launch_bounds__(256) k_logits_split(SplitArgs a) {
   if (q == 0) a.exps[which][row] = e - 14;
 }
 
-template <int HC, int T>
+template <int HC, int T, typename O>
 struct Cfg {
-  static constexpr int RN = T == 1 ? 256 : 128;  // rows of X of a tile
-  static constexpr int XPIECE = RN * 128;        // 64 elements of each
+  static constexpr int RN = T == 1 || HC <= 2 ? 256 : 128;  // rows of X of a tile
+  static constexpr int XPIECE = RN * 128;                   // 64 elements of each
   static constexpr int X_BYTES = T * HC * XPIECE;
+  // Staging of results on their way from a lane a token to a lane 16 bytes of a row, SR rows of a warpgroup.
+  static constexpr int S = 32 / (int)sizeof(O), E = 16 / (int)sizeof(O);  // elements of a sector, of 16 bytes
+  static constexpr int STEP = 128 - S;  // tokens from tile to tile
+  static constexpr int SR = T == 2 && HC == 4 ? 8 : 16;
+  static constexpr int STRIDE = 128 + S;  // elements of a staged row
+  static constexpr int BUF = SR * STRIDE * (int)sizeof(O);
+  static constexpr int STAGING = kEpilogue / 4 * BUF;
   static constexpr int PIECE = 16384;
-  static constexpr int ROOM = (232448 - 2048 - X_BYTES) / PIECE;
+  static constexpr int ROOM = (232448 - 2048 - X_BYTES - STAGING) / PIECE;
   static constexpr int ST = ROOM < kMaxStages ? ROOM : kMaxStages;
-  static constexpr int SMEM = X_BYTES + ST * PIECE + 2048;
+  static constexpr int SMEM = X_BYTES + ST * PIECE + STAGING + 2048;
   // (the pieces of the high terms of a tile of W are used twice and stay in the ring until then)
-  static_assert(ST > HC && SMEM <= 232448, "shared memory");
+  static_assert(ST >= 3 && (T == 1 || ST > HC) && SMEM <= 232448, "shared memory");
 };
 
 struct Bars {
@@ -127,7 +135,7 @@ struct Bars {
 };
 
 struct Args {
-  int V, vt, stream;  // vt: tiles of W; stream: results do not stay in the cache
+  int V, vt;  // vt: tiles of W
   int64_t n, units, cap, vcap, ldz;
   const int32_t* xe;
   const int32_t* we;
@@ -156,44 +164,110 @@ struct Walk {
   }
 };
 
-template <bool STREAM>
-__device__ __forceinline__ void put(float* p, float x) {
-  if (STREAM) __stcs(p, x); else *p = x;
+__device__ __forceinline__ float as_out(float x, float) { return x; }
+__device__ __forceinline__ __nv_bfloat16 as_out(float x, __nv_bfloat16) { return __float2bfloat16(x); }
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
-template <bool STREAM>
-__device__ __forceinline__ void put(__nv_bfloat16* p, float x) {
-  const __nv_bfloat16 h = __float2bfloat16(x);
-  if (STREAM)
-    __stcs(reinterpret_cast<unsigned short*>(p), *reinterpret_cast<const unsigned short*>(&h));
-  else
-    *p = h;
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+                 "=r"(r[7])
+               : "r"(taddr));
 }
 
-// 32 rows of Z (of which `rows` exist) from a warp's lanes' tokens.
-template <int T, bool STREAM, typename O>
-__device__ __forceinline__ void write32(const uint32_t* d, O* p, int64_t ldz, int rows, bool mine, int we,
-                                        int xe) {
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    float z = __uint_as_float(d[j]);
-    if (T == 2) {  // in two steps: the power of two may be outside fp32's range where the logit is not
-      const int e = we + __shfl_sync(0xffffffffu, xe, j), h = e >> 1;
-      z = z * pow2(h) * pow2(e - h);
-    }
-    if (mine && j < rows) put<STREAM>(p + j * ldz, z);
+// A warpgroup's way of SR rows of a tile to memory.
+//
+// A row of Z begins anywhere in a 32-byte sector, and a sector that is written in parts costs HBM twice (16383
+// rows x 49999 fp32: 1240 us when each warp wrote its 32 tokens of a row at once, 611 where rows were aligned).
+// So tiles overlap by a sector: of a tile's 128 tokens each row writes the STEP of them that fill whole sectors,
+// wherever those begin in this row.  A staged row has its tokens at columns o .. o + 127, o the first one's
+// place in its sector, so that sectors begin at multiples of S and 16 aligned bytes are a lane's.
+template <typename C, int T, typename O>
+struct Writer {
+  const Args& a;
+  O* Z;
+  O* buf;  // of this warpgroup
+  int wg, q, lane;
+
+  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
+  __device__ __forceinline__ int offset(const O* p) const {
+    return (int)((reinterpret_cast<uintptr_t>(p) & 31) / sizeof(O));
   }
-}
+  // d: rows c .. c + SR - 1 of the tile that begins at row0 and token t0, from this lane's token
+  __device__ __forceinline__ void write(const uint32_t* d, int64_t row0, int rows, int c, int t0, int we, bool dead) {
+    sync();  // the rows before these have been read
+    O* first = Z + (row0 + c) * a.ldz + t0;
+    {
+      int o = offset(first);
+      const int step = (int)(a.ldz & (C::S - 1));
+      const int xe = T == 2 && c + lane < rows && lane < C::SR ? a.xe[row0 + c + lane] : 0;
+      O* p = buf + q * 32 + lane;
+#pragma unroll
+      for (int j = 0; j < C::SR; ++j, o = (o + step) & (C::S - 1)) {
+        float z = __uint_as_float(d[j]);
+        if (T == 2) {  // in two steps: the power of two may be outside fp32's range where the logit is not
+          const int e = we + __shfl_sync(0xffffffffu, xe, j), h = e >> 1;
+          z = z * pow2(h) * pow2(e - h);
+        }
+        p[j * C::STRIDE + o] = as_out(z, O());
+      }
+    }
+    sync();
+    if (dead) return;
+    constexpr int LPR = 128 / C::E, RPI = 32 / LPR, N = C::SR / (4 * RPI);  // lanes of a row, rows of a warp at a time
+    const int l = lane % LPR, j0 = q * RPI + lane / LPR;
+    uint4 x[N];
+    O* to[N];
+    int col[N];  // of the row's first whole sector, then of this lane's part
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int j = j0 + 4 * RPI * k;
+      to[k] = first + (int64_t)j * a.ldz;
+      const int o = offset(to[k]);
+      to[k] -= o;  // column 0
+      col[k] = (o ? C::S : 0) + l * C::E;
+      x[k] = *reinterpret_cast<const uint4*>(buf + j * C::STRIDE + min(col[k], 128 + C::S - C::E));
+    }
+    if (t0 > 0 && t0 + 128 < a.V) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (l < C::STEP / C::E && c + j0 + 4 * RPI * k < rows) __stcs(reinterpret_cast<uint4*>(to[k] + col[k]), x[k]);
+      return;
+    }
+    // the row's first and last tiles: the tokens before the first whole sector and all that are left
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int j = j0 + 4 * RPI * k, o = offset(first + (int64_t)j * a.ldz), cs = o ? C::S : 0;
+      if (c + j >= rows) continue;
+      const int lo = t0 > 0 ? cs : o, hi = t0 + 128 >= a.V ? o + a.V - t0 : cs + C::STEP;
+      for (int b = l * C::E; b < 128 + C::S; b += 128) {
+#pragma unroll
+        for (int e = 0; e < C::E; ++e)
+          if (b + e >= lo && b + e < hi) to[k][b + e] = buf[j * C::STRIDE + b + e];
+      }
+    }
+  }
+};
 
 template <int HC, int T, typename O>
 __global__ void __launch_bounds__(kThreads, 1)
     k_logits(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
              const __grid_constant__ Args a, O* Z) {
-  using C = Cfg<HC, T>;
+  using C = Cfg<HC, T, O>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem =
       reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = smem + C::X_BYTES;
-  Bars* bars = reinterpret_cast<Bars*>(ring + C::ST * C::PIECE);
+  uint8_t* staging = ring + C::ST * C::PIECE;
+  Bars* bars = reinterpret_cast<Bars*>(staging + C::STAGING);
   volatile int* abort = &bars->abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -205,13 +279,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->d_full[b], 1);
-      mbar_init(&bars->d_empty[b], 8);
+      mbar_init(&bars->d_empty[b], kEpilogue);
     }
     mbar_init(&bars->drain, 1);
     bars->abort = 0;
     fence_mbar_init();
   }
-  if (warp == 9) {
+  if (warp == kEpilogue + 1) {
     tmem_alloc(&bars->tmem, 512);
     tmem_relinquish();
   }
@@ -223,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = bars->tmem;
   Walk w(a);
 
-  if (warp == 8) {
+  if (warp == kEpilogue) {
     if (lane == 0) {
       tma_prefetch_desc(&tmX);
       tma_prefetch_desc(&tmW);
@@ -246,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) break;
           mbar_expect_tx(&bars->full[s], C::PIECE);
           tma_load_2d(ring + s * C::PIECE, &tmW, &bars->full[s], p % HC * 64,
-                      (int)(T == 2 && p < HC ? a.vcap : 0) + w.v * 128);
+                      (int)(T == 2 && p < HC ? a.vcap : 0) + w.v * C::STEP);
         }
       }
       if (*abort) {  // copies in flight land before the block leaves
@@ -257,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == kEpilogue + 1) {
     const bool leader = elect_one_sync();
     const uint64_t X = desc_sw128_kmajor(smem_u32(smem)), R = desc_sw128_kmajor(smem_u32(ring));
     uint32_t it = 0, seg = 0, k = 0;
@@ -310,37 +384,43 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (uint32_t q = 0; q < (1u << 24) && !mbar_try(&bars->drain, 0); ++q) {
     }
   } else {
-    const int q = warp & 3, half = warp >> 2;
+    const int q = warp & 3, wg = warp >> 2;
     const uint32_t base = tmem + ((uint32_t)(q * 32) << 16);
+    Writer<C, T, O> out{a, Z, reinterpret_cast<O*>(staging + wg * C::BUF), wg, q, lane};
+    constexpr int ROUND = kEpilogue / 4 * C::SR;  // rows of all warpgroups
     uint32_t k = 0;
+    bool dead = false;  // a wait gave up: the warpgroup's barriers are met all the same, nothing is written
     for (; w.more(); w.next(), ++k) {
-      const int b = k & 1, v = w.v * 128 + q * 32 + lane;
+      const int b = k & 1, t0 = w.v * C::STEP, v = t0 + q * 32 + lane;
       const int64_t row0 = w.rt * C::RN;
       const int rows = (int)min((int64_t)C::RN, a.n - row0);
-      const bool mine = v < a.V;
-      const int we = T == 2 && mine ? a.we[v] : 0;
-      const bool ok = mbar_wait(&bars->d_full[b], (k >> 1) & 1, a.status, 726, abort, 20);
-      if (__any_sync(0xffffffffu, !ok)) break;
+      const int we = T == 2 && v < a.V ? a.we[v] : 0;
+      dead = dead || !mbar_wait(&bars->d_full[b], (k >> 1) & 1, a.status, 726, abort, 20);
+      dead = __any_sync(0xffffffffu, dead);
       tc_fence_after();
-      O* p = Z + (row0 + half * 32) * a.ldz + v;
-      for (int c = half * 32; c < rows; c += 64, p += 64 * a.ldz) {
-        const int xe = T == 2 && c + lane < rows ? a.xe[row0 + c + lane] : 0;
-        uint32_t d[32];
-        tmem_ld32(base + b * 256 + c, d);
-        tmem_wait_ld();
-        if (a.stream)
-          write32<T, true>(d, p, a.ldz, rows - c, mine, we, xe);
+      for (int c = wg * C::SR; c < rows; c += ROUND) {
+        uint32_t d[C::SR];
+        if (C::SR == 16)
+          tmem_ld16(base + b * 256 + c, d);
         else
-          write32<T, false>(d, p, a.ldz, rows - c, mine, we, xe);
+          tmem_ld8(base + b * 256 + c, d);
+        tmem_wait_ld();
+        if (c + ROUND >= rows) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->d_empty[b]);
+        }
+        out.write(d, row0, rows, c, t0, we, dead);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->d_empty[b]);
+      if (wg * C::SR >= rows) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->d_empty[b]);
+      }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kEpilogue + 1) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 512);
@@ -349,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 template <int HC, int T, typename O>
 cudaError_t run(const LogitsArgs& l, const Ws& ws, cudaStream_t st) {
-  using C = Cfg<HC, T>;
+  using C = Cfg<HC, T, O>;
   char* base = static_cast<char*>(l.ws);
   CUtensorMap mx, mw;
   const bool ok = T == 1 ? make_map_ld(&mx, l.X, l.n, l.H, l.H, C::RN) && make_map_ld(&mw, l.W, l.V, l.H, l.H, 128)
@@ -361,7 +441,7 @@ cudaError_t run(const LogitsArgs& l, const Ws& ws, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   Args a{};
   a.V = l.V;
-  a.vt = (l.V + 127) / 128;
+  a.vt = l.V <= 128 ? 1 : (l.V - 128 + C::STEP - 1) / C::STEP + 1;
   a.n = l.n;
   a.units = (l.n + C::RN - 1) / C::RN * a.vt;
   a.cap = ws.cap;
@@ -370,7 +450,6 @@ cudaError_t run(const LogitsArgs& l, const Ws& ws, cudaStream_t st) {
   a.xe = reinterpret_cast<const int32_t*>(base + ws.xe);
   a.we = reinterpret_cast<const int32_t*>(base + ws.we);
   a.status = l.status;
-  a.stream = l.n * (int64_t)l.V * (int64_t)sizeof(O) > ((int64_t)64 << 20);
   const int ctas = (int)std::min<int64_t>(gemm_tn_num_sms(), a.units);
   e = launch_pdl(k_logits<HC, T, O>, dim3(ctas), dim3(kThreads), C::SMEM, st, mx, mw, a, static_cast<O*>(l.Z));
   if (e == cudaSuccess) note_launch();
