@@ -213,15 +213,15 @@ __global__ void __launch_bounds__(kWarps * 32) k_distill_rows(const __grid_const
       for (int j = 0; j < 8; ++j) acc[j] = fmaf(cx, w[s][j], acc[j]);
     }
   }
-  if constexpr (MODE == kForward) {
+  if (MODE == kForward) {
     inner = warp_sum(inner);
     if (lane == 0) a.inner[i] = inner;
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    for (int o = a.width; o < 32; o <<= 1) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
-  if (MODE != kForward && keep_dx && group == 0 && in) {
+    for (int j = 0; j < 8; ++j)
+      for (int o = a.width; o < 32; o <<= 1) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
+  }
+  if (keep_dx && group == 0 && in) {
     float4* d = reinterpret_cast<float4*>(a.dX + i * a.H + at);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {

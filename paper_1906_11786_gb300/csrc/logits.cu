@@ -50,7 +50,7 @@ Ws layout(int bf16, int64_t n, int H, int V) {
   };
   w.x = take((size_t)2 * w.cap * H * 2);
   w.w = take((size_t)2 * w.vcap * H * 2);
-  w.xe = take((size_t)w.cap * 4);
+  w.xe = take((size_t)(w.cap + 128) * 4);  // (whole tiles of 256 rows)
   w.we = take((size_t)w.vcap * 4);
   w.total = o;
   return w;
@@ -63,7 +63,8 @@ __device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)
 struct SplitArgs {
   const float* src[2];
   uint16_t* dst[2];
-  int32_t* exps[2];
+  float* xs;    // scales of the rows of X
+  int32_t* we;  // exponents of those of W
   int64_t rows[2], plane[2];
   int H, width;
 };
@@ -105,7 +106,54 @@ __global__ void __launch_bounds__(256) k_logits_split(SplitArgs a) {
   uint16_t* d = a.dst[which] + row * a.H + q * 8;
   *reinterpret_cast<uint4*>(d) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
   *reinterpret_cast<uint4*>(d + a.plane[which] * a.H) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-  if (q == 0) a.exps[which][row] = e - 14;
+  if (q == 0) {
+    if (which == 0)
+      a.xs[row] = pow2(e - 14);
+    else
+      a.we[row] = e - 14;
+  }
+}
+
+// A few rows of X in fp32, without terms: a row of W is `width` threads of 8 elements (H / 8 rounded up to a power
+// of two), read once for all of them, and what bounds it.  One row x 32000 x 128: 15 us with the terms' pass over
+// W, 7 without (16 rows: 15 with it, 37 without).
+constexpr int kFew = 4;
+template <typename O>
+__global__ void __launch_bounds__(256)
+    k_logits_few(int n, int H, int V, int width, const float* __restrict__ X, const float* __restrict__ W, int64_t ldz,
+                 O* __restrict__ Z) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int lane = threadIdx.x & (width - 1), at = lane * 8;
+  const bool in = at < H;
+  float x[kFew][8];
+#pragma unroll
+  for (int r = 0; r < kFew; ++r)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[r][j] = in && r < n ? X[r * H + at + j] : 0.f;
+  const int step = gridDim.x * (256 / width);
+  // (whole warps: the sums go over lanes)
+  for (int v0 = blockIdx.x * (256 / width) + (threadIdx.x & ~31) / width; v0 < V; v0 += step) {
+    const int v = v0 + (threadIdx.x & 31) / width;
+    float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (in && v < V) {
+      const float4* p = reinterpret_cast<const float4*>(W + (int64_t)v * H + at);
+      const float4 a = __ldg(p), b = __ldg(p + 1);
+      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+      w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+    float mine = 0.f;
+#pragma unroll
+    for (int r = 0; r < kFew; ++r) {
+      if (r >= n) break;
+      float z = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z = fmaf(x[r][j], w[j], z);
+      for (int o = width / 2; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+      if (lane == r) mine = z;  // (four threads at least)
+    }
+    if (lane < n && v < V) Z[lane * ldz + v] = (O)mine;
+  }
 }
 
 template <int HC, int T, typename O>
@@ -117,6 +165,7 @@ struct Cfg {
   static constexpr int S = 32 / (int)sizeof(O), E = 16 / (int)sizeof(O);  // elements of a sector, of 16 bytes
   static constexpr int STEP = 128 - S;  // tokens from tile to tile
   static constexpr int SR = T == 2 && HC == 4 ? 8 : 16;
+  static constexpr int ROUND = kEpilogue / 4 * SR;  // rows of all warpgroups
   static constexpr int STRIDE = 128 + S;  // elements of a staged row
   static constexpr int BUF = SR * STRIDE * (int)sizeof(O);
   static constexpr int STAGING = kEpilogue / 4 * BUF;
@@ -124,8 +173,11 @@ struct Cfg {
   static constexpr int ROOM = (232448 - 2048 - X_BYTES - STAGING) / PIECE;
   static constexpr int ST = ROOM < kMaxStages ? ROOM : kMaxStages;
   static constexpr int SMEM = X_BYTES + ST * PIECE + STAGING + 2048;
-  // (the pieces of the high terms of a tile of W are used twice and stay in the ring until then)
-  static_assert(ST >= 3 && (T == 1 || ST > HC) && SMEM <= 232448, "shared memory");
+  // The pieces of the high terms of a tile of W are used twice: they stay in the ring where they fit beside one
+  // more (16383 rows x 49999 x 256 with fewer stages, loaded twice: 1270 instead of 1170 us).
+  static constexpr bool KEPT = T == 2 && ST > HC;
+  static constexpr int PIECES = T == 1 || KEPT ? T * HC : 3 * HC;  // of a tile of W that are loaded
+  static_assert(ST >= 3 && SMEM <= 232448, "shared memory");
 };
 
 struct Bars {
@@ -137,7 +189,7 @@ struct Bars {
 struct Args {
   int V, vt;  // vt: tiles of W
   int64_t n, units, cap, vcap, ldz;
-  const int32_t* xe;
+  const float* xs;
   const int32_t* we;
   int* status;
 };
@@ -164,9 +216,6 @@ struct Walk {
   }
 };
 
-__device__ __forceinline__ float as_out(float x, float) { return x; }
-__device__ __forceinline__ __nv_bfloat16 as_out(float x, __nv_bfloat16) { return __float2bfloat16(x); }
-
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
@@ -189,69 +238,85 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
 // rows x 49999 fp32: 1240 us when each warp wrote its 32 tokens of a row at once, 611 where rows were aligned).
 // So tiles overlap by a sector: of a tile's 128 tokens each row writes the STEP of them that fill whole sectors,
 // wherever those begin in this row.  A staged row has its tokens at columns o .. o + 127, o the first one's
-// place in its sector, so that sectors begin at multiples of S and 16 aligned bytes are a lane's.
+// place in its sector, so that sectors begin at multiples of S and 16 aligned bytes are a lane's.  STEP and the
+// rows from one turn to the next are multiples of S: a place in the staging has the same o all along, and all
+// addresses but one are made once.  (As bulk copies of a row each the same writes took 750-990 us.)
 template <typename C, int T, typename O>
 struct Writer {
+  static constexpr int LPR = 128 / C::E, RPI = 32 / LPR, N = C::SR / (4 * RPI);  // lanes of a row; rows of a warp
   const Args& a;
   O* Z;
   O* buf;  // of this warpgroup
   int wg, q, lane;
+  uint32_t put[C::SR];  // where this lane's token goes in the staged rows
+  int64_t to[N];        // bytes from the first row's token t0 to this lane's parts of rows
+  uint32_t get[N];
 
-  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
   __device__ __forceinline__ int offset(const O* p) const {
     return (int)((reinterpret_cast<uintptr_t>(p) & 31) / sizeof(O));
   }
-  // d: rows c .. c + SR - 1 of the tile that begins at row0 and token t0, from this lane's token
-  __device__ __forceinline__ void write(const uint32_t* d, int64_t row0, int rows, int c, int t0, int we, bool dead) {
-    sync();  // the rows before these have been read
-    O* first = Z + (row0 + c) * a.ldz + t0;
-    {
-      int o = offset(first);
-      const int step = (int)(a.ldz & (C::S - 1));
-      const int xe = T == 2 && c + lane < rows && lane < C::SR ? a.xe[row0 + c + lane] : 0;
-      O* p = buf + q * 32 + lane;
+  __device__ __forceinline__ Writer(const Args& a_, O* Z_, O* buf_, int wg_, int q_, int lane_)
+      : a(a_), Z(Z_), buf(buf_), wg(wg_), q(q_), lane(lane_) {
+    const O* first = Z + (int64_t)wg * C::SR * a.ldz;
+    const int step = (int)(a.ldz & (C::S - 1)), o0 = offset(first), l = lane % LPR;
 #pragma unroll
-      for (int j = 0; j < C::SR; ++j, o = (o + step) & (C::S - 1)) {
-        float z = __uint_as_float(d[j]);
-        if (T == 2) {  // in two steps: the power of two may be outside fp32's range where the logit is not
-          const int e = we + __shfl_sync(0xffffffffu, xe, j), h = e >> 1;
-          z = z * pow2(h) * pow2(e - h);
-        }
-        p[j * C::STRIDE + o] = as_out(z, O());
+    for (int j = 0; j < C::SR; ++j)
+      put[j] = smem_u32(buf + j * C::STRIDE + q * 32 + lane + ((o0 + j * step) & (C::S - 1)));
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int j = q * RPI + lane / LPR + 4 * RPI * k, o = (o0 + j * step) & (C::S - 1);
+      const int col = (o ? C::S : 0) + l * C::E;  // of the row's whole sectors
+      to[k] = ((int64_t)j * a.ldz + col - o) * (int)sizeof(O);
+      get[k] = smem_u32(buf + j * C::STRIDE + min(col, 128 + C::S - C::E));
+    }
+  }
+  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
+  __device__ __forceinline__ void stage(uint32_t at, float z, float) const {
+    asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(z) : "memory");
+  }
+  __device__ __forceinline__ void stage(uint32_t at, float z, __nv_bfloat16) const {
+    const __nv_bfloat16 h = __float2bfloat16(z);
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(*reinterpret_cast<const unsigned short*>(&h)) : "memory");
+  }
+  // d: rows c .. c + SR - 1 of the tile that begins at row0 and token t0, from this lane's token
+  // (fp32 form: xs their rows' scales, up and up2 the token's)
+  __device__ __forceinline__ void write(const uint32_t* d, const float* xs, int64_t row0, int rows, int c, int t0,
+                                        float up, float up2, bool dead) {
+    float z[C::SR];
+#pragma unroll
+    for (int j = 0; j < C::SR; ++j) z[j] = __uint_as_float(d[j]);
+    if constexpr (T == 2) {
+#pragma unroll
+      for (int j = 0; j < C::SR; ++j) z[j] = z[j] * up * xs[j];
+      if (__any_sync(0xffffffffu, up2 != 1.f)) {
+#pragma unroll
+        for (int j = 0; j < C::SR; ++j) z[j] *= up2;
       }
     }
+    sync();  // the rows before these have been read
+#pragma unroll
+    for (int j = 0; j < C::SR; ++j) stage(put[j], z[j], O());
     sync();
     if (dead) return;
-    constexpr int LPR = 128 / C::E, RPI = 32 / LPR, N = C::SR / (4 * RPI);  // lanes of a row, rows of a warp at a time
-    const int l = lane % LPR, j0 = q * RPI + lane / LPR;
-    uint4 x[N];
-    O* to[N];
-    int col[N];  // of the row's first whole sector, then of this lane's part
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int j = j0 + 4 * RPI * k;
-      to[k] = first + (int64_t)j * a.ldz;
-      const int o = offset(to[k]);
-      to[k] -= o;  // column 0
-      col[k] = (o ? C::S : 0) + l * C::E;
-      x[k] = *reinterpret_cast<const uint4*>(buf + j * C::STRIDE + min(col[k], 128 + C::S - C::E));
-    }
+    char* first = reinterpret_cast<char*>(Z + (row0 + c) * a.ldz + t0);
     if (t0 > 0 && t0 + 128 < a.V) {
+      uint4 x[N];
 #pragma unroll
       for (int k = 0; k < N; ++k)
-        if (l < C::STEP / C::E && c + j0 + 4 * RPI * k < rows) __stcs(reinterpret_cast<uint4*>(to[k] + col[k]), x[k]);
-      return;
-    }
-    // the row's first and last tiles: the tokens before the first whole sector and all that are left
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(x[k].x), "=r"(x[k].y), "=r"(x[k].z), "=r"(x[k].w)
+                     : "r"(get[k]));
+      const int left = lane % LPR < C::STEP / C::E ? rows - c - q * RPI - lane / LPR : 0;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int j = j0 + 4 * RPI * k, o = offset(first + (int64_t)j * a.ldz), cs = o ? C::S : 0;
-      if (c + j >= rows) continue;
-      const int lo = t0 > 0 ? cs : o, hi = t0 + 128 >= a.V ? o + a.V - t0 : cs + C::STEP;
-      for (int b = l * C::E; b < 128 + C::S; b += 128) {
-#pragma unroll
-        for (int e = 0; e < C::E; ++e)
-          if (b + e >= lo && b + e < hi) to[k][b + e] = buf[j * C::STRIDE + b + e];
+      for (int k = 0; k < N; ++k)
+        if (left > 4 * RPI * k) __stcs(reinterpret_cast<uint4*>(first + to[k]), x[k]);
+    } else {
+      // the row's first and last tiles: also the tokens before the first whole sector, and all that are left
+      for (int j = q; j < C::SR && c + j < rows; j += 4) {
+        O* row = reinterpret_cast<O*>(first) + (int64_t)j * a.ldz;
+        const int o = offset(row), cs = o ? C::S : 0;
+        const int lo = t0 > 0 ? cs : o, hi = t0 + 128 >= a.V ? o + a.V - t0 : cs + C::STEP;
+        for (int k = lo + lane; k < hi; k += 32) row[k - o] = buf[j * C::STRIDE + k];
       }
     }
   }
@@ -313,8 +378,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         (int)(p / HC * a.cap + w.rt * C::RN));
           ++seg;
         }
-        // two terms: the low one's pieces, then the high one's
-        for (int p = 0; p < T * HC && ok; ++p, ++it) {
+        // two terms: the low one's pieces, then the high one's (twice where the ring does not keep them)
+        for (int p = 0; p < C::PIECES && ok; ++p, ++it) {
           const int s = it % C::ST;
           ok = mbar_wait(&bars->empty[s], ((it / C::ST) & 1) ^ 1, a.status, 722, abort, 32);
           if (!ok) break;
@@ -355,24 +420,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       };
       // (past H the pieces hold zeros)
-      for (int p = 0; p < T * HC && ok; ++p) {
+      for (int p = 0; p < C::PIECES && ok; ++p) {
         const uint32_t i = it + p;
         ok = mbar_wait(&bars->full[i % C::ST], (i / C::ST) & 1, a.status, 725, abort);
         if (!ok) break;
         tc_fence_after();
         // low x high, then high x low; the high terms' pieces stay for high x high
-        product(i % C::ST, p, p > 0);
-        if (leader && (T == 1 || p < HC)) tc_commit(&bars->empty[i % C::ST]);
+        product(i % C::ST, p < T * HC ? p : p - T * HC, p > 0);
+        if (leader && (!C::KEPT || p < HC)) tc_commit(&bars->empty[i % C::ST]);
         __syncwarp();
       }
-      if (T == 2 && ok)
+      if (C::KEPT && ok)
         for (int p = 0; p < HC; ++p) {
           const uint32_t i = it + HC + p;
           product(i % C::ST, p, true);
           if (leader) tc_commit(&bars->empty[i % C::ST]);
           __syncwarp();
         }
-      it += T * HC;
+      it += C::PIECES;
       if (ok && leader) {
         tc_commit(&bars->d_full[b]);
         if (w.last_of_tile()) tc_commit(&bars->x_empty);
@@ -386,31 +451,41 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     const int q = warp & 3, wg = warp >> 2;
     const uint32_t base = tmem + ((uint32_t)(q * 32) << 16);
-    Writer<C, T, O> out{a, Z, reinterpret_cast<O*>(staging + wg * C::BUF), wg, q, lane};
-    constexpr int ROUND = kEpilogue / 4 * C::SR;  // rows of all warpgroups
+    Writer<C, T, O> out(a, Z, reinterpret_cast<O*>(staging + wg * C::BUF), wg, q, lane);
     uint32_t k = 0;
     bool dead = false;  // a wait gave up: the warpgroup's barriers are met all the same, nothing is written
     for (; w.more(); w.next(), ++k) {
       const int b = k & 1, t0 = w.v * C::STEP, v = t0 + q * 32 + lane;
       const int64_t row0 = w.rt * C::RN;
       const int rows = (int)min((int64_t)C::RN, a.n - row0);
-      const int we = T == 2 && v < a.V ? a.we[v] : 0;
+      // a token's scale in two parts: with the row's between them nothing overflows that the logit does not
+      const int we = T == 2 && v < a.V ? a.we[v] : 0, we1 = min(we, 60);
+      const float up = pow2(we1), up2 = pow2(we - we1);
       dead = dead || !mbar_wait(&bars->d_full[b], (k >> 1) & 1, a.status, 726, abort, 20);
       dead = __any_sync(0xffffffffu, dead);
       tc_fence_after();
-      for (int c = wg * C::SR; c < rows; c += ROUND) {
-        uint32_t d[C::SR];
+      auto fetch = [&](int c, uint32_t* d) {
         if (C::SR == 16)
           tmem_ld16(base + b * 256 + c, d);
         else
           tmem_ld8(base + b * 256 + c, d);
         tmem_wait_ld();
-        if (c + ROUND >= rows) {
+      };
+      for (int c = wg * C::SR; c < rows; c += C::ROUND) {
+        uint32_t d[C::SR];
+        float xs[T == 2 ? C::SR : 4];
+        if constexpr (T == 2) {  // (the scales' array is as long as whole tiles are)
+#pragma unroll
+          for (int j = 0; j < C::SR; j += 4)
+            *reinterpret_cast<float4*>(xs + j) = __ldg(reinterpret_cast<const float4*>(a.xs + row0 + c + j));
+        }
+        fetch(c, d);
+        if (c + C::ROUND >= rows) {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars->d_empty[b]);
         }
-        out.write(d, row0, rows, c, t0, we, dead);
+        out.write(d, xs, row0, rows, c, t0, up, up2, dead);
       }
       if (wg * C::SR >= rows) {
         __syncwarp();
@@ -447,7 +522,7 @@ cudaError_t run(const LogitsArgs& l, const Ws& ws, cudaStream_t st) {
   a.cap = ws.cap;
   a.vcap = ws.vcap;
   a.ldz = l.ldz;
-  a.xe = reinterpret_cast<const int32_t*>(base + ws.xe);
+  a.xs = reinterpret_cast<const float*>(base + ws.xe);
   a.we = reinterpret_cast<const int32_t*>(base + ws.we);
   a.status = l.status;
   const int ctas = (int)std::min<int64_t>(gemm_tn_num_sms(), a.units);
@@ -468,27 +543,41 @@ cudaError_t run_h(const LogitsArgs& l, const Ws& ws, cudaStream_t st) {
 
 }  // namespace
 
-size_t logits_ws_bytes(int bf16, int64_t n, int H, int V) { return layout(bf16, n, H, V).total; }
+size_t logits_ws_bytes(int bf16, int64_t n, int H, int V) { return n <= kFew ? 0 : layout(bf16, n, H, V).total; }
 
 cudaError_t logits_fwd(const LogitsArgs& l, cudaStream_t st) {
   if (l.n == 0) return cudaSuccess;
   const Ws ws = layout(l.bf16, l.n, l.H, l.V);
   if (l.bf16)
     return l.out_bf16 ? run_h<1, __nv_bfloat16>(l, ws, st) : run_h<1, float>(l, ws, st);
+  const int width = l.H / 8 <= 4 ? 4 : l.H / 8 <= 8 ? 8 : l.H / 8 <= 16 ? 16 : 32;
+  if (l.n <= kFew) {
+    // rows of W that are a block's at a time, eight blocks an SM
+    const int per = 256 / width;
+    const dim3 grid((unsigned)std::min<int64_t>((l.V + per - 1) / per, 152 * 8));
+    const float *X = static_cast<const float*>(l.X), *W = static_cast<const float*>(l.W);
+    const cudaError_t e =
+        l.out_bf16 ? launch_pdl(k_logits_few<__nv_bfloat16>, grid, dim3(256), 0, st, (int)l.n, l.H, l.V, width, X, W,
+                                l.ldz, static_cast<__nv_bfloat16*>(l.Z))
+                   : launch_pdl(k_logits_few<float>, grid, dim3(256), 0, st, (int)l.n, l.H, l.V, width, X, W, l.ldz,
+                                static_cast<float*>(l.Z));
+    if (e == cudaSuccess) note_launch();
+    return e;
+  }
   SplitArgs s{};
   char* base = static_cast<char*>(l.ws);
   s.src[0] = static_cast<const float*>(l.X);
   s.src[1] = static_cast<const float*>(l.W);
   s.dst[0] = reinterpret_cast<uint16_t*>(base + ws.x);
   s.dst[1] = reinterpret_cast<uint16_t*>(base + ws.w);
-  s.exps[0] = reinterpret_cast<int32_t*>(base + ws.xe);
-  s.exps[1] = reinterpret_cast<int32_t*>(base + ws.we);
+  s.xs = reinterpret_cast<float*>(base + ws.xe);
+  s.we = reinterpret_cast<int32_t*>(base + ws.we);
   s.rows[0] = l.n;
   s.rows[1] = l.V;
   s.plane[0] = ws.cap;
   s.plane[1] = ws.vcap;
   s.H = l.H;
-  s.width = l.H / 8 <= 4 ? 4 : l.H / 8 <= 8 ? 8 : l.H / 8 <= 16 ? 16 : 32;
+  s.width = width;
   const int per = 256 / s.width;
   cudaError_t e = launch_pdl(k_logits_split, dim3((unsigned)((l.n + l.V + per - 1) / per)), dim3(256), 0, st, s);
   if (e != cudaSuccess) return e;

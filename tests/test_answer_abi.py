@@ -80,10 +80,11 @@ def test_pointers_types_and_strides_are_checked(lib):
     _refused(lib.bg_logits_fwd(f, 8, 64, 9, None, A, f, 9, A, A, BIG, None), "X is NULL")
     _refused(lib.bg_logits_fwd(f, 8, 64, 9, A, odd, f, 9, A, A, BIG, None), "W not 16-byte")
     _refused(lib.bg_logits_fwd(f, 8, 64, 9, A, A, f, 9, odd, A, BIG, None), "Z not 16-byte")
-    need = lib.bg_logits_workspace_bytes(f, 8, 64, 9)
-    assert need > 0 and lib.bg_logits_workspace_bytes(L.BG_BF16, 8, 64, 9) == 0
-    _refused(lib.bg_logits_fwd(f, 8, 64, 9, A, A, f, 9, A, A, need - 1, None), "workspace", code=-2)
-    _refused(lib.bg_logits_fwd(f, 8, 64, 9, A, A, f, 9, A, None, BIG, None), "ws is NULL")
+    need = lib.bg_logits_workspace_bytes(f, 5, 64, 9)
+    assert need > 0 == lib.bg_logits_workspace_bytes(f, 4, 64, 9)
+    assert lib.bg_logits_workspace_bytes(L.BG_BF16, 800, 64, 9) == 0
+    _refused(lib.bg_logits_fwd(f, 5, 64, 9, A, A, f, 9, A, A, need - 1, None), "workspace", code=-2)
+    _refused(lib.bg_logits_fwd(f, 5, 64, 9, A, A, f, 9, A, None, BIG, None), "ws is NULL")
     _refused(lib.bg_logits_adjust(5, 8, 9, 9, A, None, 9, A, None), "dtype")
     _refused(lib.bg_logits_adjust(f, 8, 9, 9, A, None, 8, A, None), "ldo must")
     _refused(lib.bg_logits_adjust(f, 8, 9, 9, A, None, 10, A, None), "in place")
@@ -165,7 +166,7 @@ def test_nothing_to_do_is_done_without_a_device(lib):
 
 
 def test_workspaces_grow_with_the_operands_alone(lib):
-    for n, H, V in ((1, 32, 1), (1 << 20, 256, 1 << 20)):
+    for n, H, V in ((5, 32, 1), (1 << 20, 256, 1 << 20)):
         need = lib.bg_logits_workspace_bytes(L.BG_F32, n, H, V)
         assert 0 < need < 6 * H * (n + V + 512) + 4096
 

@@ -91,7 +91,8 @@ def check_logits(n, H, V, dtype, out, pad=0, seed=0, X=None, W=None):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,H,V", [(1, 32, 1), (1, 128, 32000), (2, 96, 129), (15, 64, 127), (16, 160, 128),
                                    (17, 256, 1000), (33, 224, 50), (128, 128, 513), (129, 32, 700),
-                                   (255, 64, 255), (256, 256, 300), (257, 192, 4001), (1000, 256, 3001)])
+                                   (255, 64, 255), (256, 256, 300), (257, 192, 4001), (1000, 256, 3001), (3, 96, 1001), (4, 32, 999),
+                                   (5, 224, 130), (4, 256, 5000), (3, 160, 33)])
 def test_logits(n, H, V, dtype):
     check_logits(n, H, V, dtype, "f32", seed=n)
 
