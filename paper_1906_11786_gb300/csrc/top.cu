@@ -29,12 +29,11 @@ using tc::smem_u32;
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;     // of a block of the adjustment
 constexpr int kSlots = 2048;         // of a hash table of a history's tokens
 constexpr int kHashed = kSlots / 2;  // tokens of a history that go there; longer ones are counted
-constexpr int kSegment = 2 * kSlots; // elements whose occurrences are counted at a time (in the same place)
+constexpr int kSegment = kSlots;      // elements whose occurrences are counted at a time (in the same place)
 constexpr int kEach = 16;       // elements of a thread at a time
-constexpr int kChunk = kThreads * kEach;
 
 // What an adjustment has (template flags): one without any costs nothing.
 enum { kBias = 1, kMask = 2, kHistory = 4 };
@@ -115,13 +114,13 @@ __device__ __forceinline__ Row<T, W> make_row(const T* Z, int64_t ldz, int64_t i
 }
 
 // Occurrences of the tokens of elements [first, first + kSegment) of a row (element = column + a).
-template <typename T, int W>
+template <int NT, typename T, int W>
 __device__ __forceinline__ void count_history(const Row<T, W>& r, int64_t first, uint32_t* counts, int* status) {
   __syncthreads();
-  for (int i = threadIdx.x; i < kSegment / 4; i += kThreads)
+  for (int i = threadIdx.x; i < kSegment / 4; i += NT)
     reinterpret_cast<uint4*>(counts)[i] = make_uint4(0, 0, 0, 0);
   __syncthreads();
-  for (int64_t i = threadIdx.x; i < r.hist_n; i += kThreads) {
+  for (int64_t i = threadIdx.x; i < r.hist_n; i += NT) {
     const int id = r.hist[i];
     if (id >= r.V) report(status, kSiteHistoryId);
     const int64_t at = (int64_t)id + r.a - first;
@@ -222,44 +221,52 @@ __device__ __forceinline__ void adjust_group(const Row<T, W>& r, int64_t g, cons
   }
 }
 
-// A hash table of a history's tokens and their counts in shared memory (2 kSlots words).  Only the part that
-// the history needs is used: a small one is cleared and looked through quickly.
+// A hash table of a history's tokens and their counts in shared memory (kSlots words): a slot holds a token plus
+// one in its low `low` bits and its count above.  Only the part that the history needs is used: a small one is
+// cleared and looked through quickly.
 struct Hash {
-  uint32_t* token;  // plus one; 0: none
-  uint32_t* count;
+  uint32_t* slot;
   int size;  // a power of two
+  int low;
+  __device__ int token(uint32_t x) const { return (int)(x & ((1u << low) - 1)) - 1; }
+  __device__ uint32_t count(uint32_t x) const { return x >> low; }
 };
+// Whether a history goes there: it is short, and its length fits beside a token.
+template <typename R>
+__device__ __forceinline__ bool hashed(const R& r) {
+  return r.hist_n <= kHashed && r.V < 1 << 21;
+}
 
 __device__ __forceinline__ void hash_add(const Hash& h, uint32_t id) {
+  const uint32_t mask = (1u << h.low) - 1;
   uint32_t at = (id * 2654435761u) >> 7 & (h.size - 1);
   for (int k = 0; k < h.size; ++k, at = (at + 1) & (h.size - 1)) {  // (half of the slots stay empty)
-    const uint32_t was = atomicCAS(&h.token[at], 0u, id + 1);
-    if (was == 0 || was == id + 1) {
-      atomicAdd(&h.count[at], 1u);
+    const uint32_t was = atomicCAS(&h.slot[at], 0u, 1u << h.low | (id + 1));
+    if (was == 0) return;
+    if ((was & mask) == id + 1) {
+      atomicAdd(&h.slot[at], 1u << h.low);
       return;
     }
   }
 }
 
 // An empty table for the tokens of r's history (a barrier has to follow before it is filled).
-template <typename T, int W>
+template <int NT, typename T, int W>
 __device__ __forceinline__ Hash clear_hash(const Row<T, W>& r, uint32_t* table) {
-  Hash h{table, nullptr, 64};
+  Hash h{table, 64, 32 - __clz(r.V)};  // (tokens plus one: 1 .. V)
   while (h.size < 2 * r.hist_n) h.size *= 2;
-  h.count = table + h.size;
-  for (int i = threadIdx.x; i < h.size / 2; i += kThreads)
-    reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
+  for (int i = threadIdx.x; i < h.size / 4; i += NT) reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
   return h;
 }
 // Adds the tokens whose elements (column + a) are in [first, last), calling seen(element) for each (a barrier has
 // to follow before the table is read).
-template <typename T, int W, typename Fn>
+template <int NT, typename T, int W, typename Fn>
 __device__ __forceinline__ void fill_hash(const Hash& h, const Row<T, W>& r, int64_t first, int64_t last, int* status,
                                           Fn seen) {
   int next = threadIdx.x < r.hist_n ? r.hist[threadIdx.x] : -1;
-  for (int i = threadIdx.x; i < (int)r.hist_n; i += kThreads) {
+  for (int i = threadIdx.x; i < (int)r.hist_n; i += NT) {
     const int id = next;
-    if (i + kThreads < (int)r.hist_n) next = r.hist[i + kThreads];
+    if (i + NT < (int)r.hist_n) next = r.hist[i + NT];
     if (id >= r.V) report(status, kSiteHistoryId);
     const int64_t e = (int64_t)id + r.a;
     if (id >= 0 && id < r.V && e >= first && e < last) {
@@ -305,7 +312,7 @@ template <typename T, int F, int W>
 __global__ void __launch_bounds__(kThreads)
     k_adjust(int V, int64_t ldz, const T* Z, Adjust adj, int64_t ldo, T* out, int per, int* status) {
   constexpr int G = Row<T, W>::G, U = 64 / W;  // U groups of a thread on their way
-  __shared__ __align__(16) uint32_t table[F & kHistory ? 2 * kSlots : 4];
+  __shared__ __align__(16) uint32_t table[F & kHistory ? kSlots : 4];
   __shared__ float raw[F & kHistory ? kSlots : 1];
   tc::grid_dep_launch();
   tc::grid_dep_wait();
@@ -315,10 +322,10 @@ __global__ void __launch_bounds__(kThreads)
   const bool vec = (reinterpret_cast<uintptr_t>(o - r.a) & (W - 1)) == 0;
   const int64_t g0 = (int64_t)blockIdx.y * per, g1 = min((int64_t)r.groups(), g0 + per);
   if (g0 >= g1) return;
-  if ((F & kHistory) && r.hist_n > kHashed) {
+  if ((F & kHistory) && !hashed(r)) {
     constexpr int SG = kSegment / G;
     for (int64_t s0 = g0; s0 < g1; s0 += SG) {
-      count_history(r, s0 * G, table, status);
+      count_history<kThreads>(r, s0 * G, table, status);
       for (int64_t g = s0 + threadIdx.x; g < min(g1, s0 + SG); g += kThreads) {
         float v[G];
         load_group(r, g, v);
@@ -328,14 +335,14 @@ __global__ void __launch_bounds__(kThreads)
     }
     return;
   }
-  Hash h{nullptr, nullptr, 0};
+  Hash h{table, 0, 0};
   if ((F & kHistory) && r.hist_n > 0) {
-    h = clear_hash(r, table);
+    h = clear_hash<kThreads>(r, table);
     __syncthreads();
-    fill_hash(h, r, g0 * G, g1 * G, status, [](int64_t) {});
+    fill_hash<kThreads>(h, r, g0 * G, g1 * G, status, [](int64_t) {});
     __syncthreads();
     for (int k = threadIdx.x; k < h.size; k += kThreads)
-      if (h.token[k]) raw[k] = to_f32(r.base[(int64_t)h.token[k] - 1 + r.a]);
+      if (const uint32_t x = h.slot[k]) raw[k] = to_f32(r.base[h.token(x) + r.a]);
     __syncthreads();
   }
   if ((F & (kBias | kMask)) || out != Z) {
@@ -355,11 +362,12 @@ __global__ void __launch_bounds__(kThreads)
   if ((F & kHistory) && r.hist_n > 0) {
     __syncthreads();
     for (int k = threadIdx.x; k < h.size; k += kThreads) {
-      if (!h.token[k]) continue;
-      const int id = (int)(h.token[k] - 1);
+      const uint32_t x = h.slot[k];
+      if (!x) continue;
+      const int id = h.token(x);
       float v = raw[k];
       if (F & kBias) v = __fadd_rn(v, __ldg(r.bias + id));
-      v = penalised(v, h.count[k], r.rep, r.presence, r.frequency);
+      v = penalised(v, h.count(x), r.rep, r.presence, r.frequency);
       if ((F & kMask) && r.mask && !(__ldg(r.mask + (id >> 5)) >> (id & 31) & 1u)) v = -INFINITY;
       store1(o + id, v);
     }
@@ -367,36 +375,53 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 // ------------------------------------------------------------------------------ largest logits
-// A row's candidates are the logits above a bound that at least K of its logits are known to reach: each
-// warp's ceil(K / 8)-th largest of its lanes' maxima so far, the least over the warps.  The bound rises
-// after 1, 2, 4, ... chunks; warps read each other's parts of it as they find them (an old part is a lower
-// bound too), so that there is one barrier, after the first chunk, and none after that.  For 49999 logits
-// and K = 32 some 200 become candidates; where they outgrow their room (ties without end, rows that rise), the
-// block goes over the row again with exact bounds (rising_row, some times slower).
+// One pass over a row notes which lanes' pieces of it (16 logits) may hold answers: those whose largest reaches a
+// bound that at least K of the row's logits are known to reach, each warp's ceil(K / 4)-th largest of its
+// lanes' maxima so far, the least over the warps.  The bound rises after 1, 2, 4, ... chunks; warps read each
+// other's parts of it as they find them (an old part is a lower bound too), so that there is one barrier, after
+// the first chunk.  Then the pieces noted, some 150 of 3100 for 49999 logits and K = 32, are read again, and their
+// logits that reach the last bound, some 60, become candidates.  (Candidates taken as they were met, by the bound
+// of the time, were a third of the kernel's instructions.)  Where pieces or candidates outgrow their room (ties
+// without end, rows that rise), the block goes over the row again with exact bounds (rising_row, some times
+// slower).
 //
 // Masks and histories come as bits in shared memory, kBits elements at a time: a cleared bit leaves an element
 // out.  The tokens of a history are cleared too, counted in a hash table, and added one by one after the
 // others: c > 0 for a few hundred of 50000 tokens costs no element a test of its own.
 constexpr int kBits = 65536;  // elements whose bits are in shared memory at a time
-constexpr int kRoom = 2304;   // candidates: those of a pass of rising_row (2048) and the K before it
-constexpr int kWarps = kThreads / 32;
+constexpr int kPass = 128;    // groups of a pass of rising_row
+constexpr int kRoom = 1152;   // candidates: those of a pass (1024) and the K before it
 constexpr int kMaxCluster = 8;
-constexpr int kFew = kMaxCluster * kMaxTop;  // candidates that are put in order
+constexpr int kFew = 512;       // candidates that are put in order
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoLogit = -3.0e38f;  // reference of a sum without terms
 constexpr float kLeast = -3.402823466e38f;
 
+constexpr int kNotes = 256;  // pieces a warp notes
+// What a block of NT threads has in shared memory; `space` is followed by the bits and the hash table, as far as the
+// adjustment needs them.
+template <int NT>
 struct TopShared {
-  uint2 cand[kRoom];
+  static constexpr int W = NT / 32;
   uint64_t few[kFew];
   uint64_t best[kMaxTop];
-  float m[kWarps], l[kWarps];
+  float m[W], l[W];
   float block_m, block_l;
-  alignas(16) uint32_t part[kWarps];  // of the bound, as orders
-  int count, found, sum[64];
+  alignas(16) uint32_t part[W];  // of the bound, as orders
+  int count, found, over, sum[64];  // over: pieces or candidates outgrew their room
+  alignas(16) uint32_t note[W][kNotes];
 };
-// After it in dynamic shared memory, as far as the adjustment needs them: the bits, then the hash table, whose
-// place rising_row takes for occurrences.
+// In the place of the notes and, where they are, the bits, once those are done with: rising_row's candidates, and
+// the lists of a cluster's blocks.
+constexpr int kLate = kRoom * 8 > kMaxCluster * kMaxTop * 8 ? kRoom * 8 : kMaxCluster * kMaxTop * 8;
+template <int NT, int F>
+__host__ __device__ constexpr int top_smem_bytes() {
+  const int before = (int)sizeof(TopShared<NT>) - (NT / 32) * kNotes * 4;
+  const int notes = (NT / 32) * kNotes * 4 + (F & (kMask | kHistory) ? kBits / 8 : 0);
+  return before + (notes > kLate ? notes : kLate) + (F & kHistory ? kSlots * 4 : 0);
+}
+template <int NT>
+__device__ __forceinline__ uint2* cands(TopShared<NT>& s) { return reinterpret_cast<uint2*>(s.note); }
 
 // Order of logits as unsigned numbers (-0 counts as 0), and keys: the larger logit, then the lower token.
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -490,7 +515,8 @@ __device__ __forceinline__ float max_of(const float* v) {
 }
 
 // The K-th largest candidate's key (0 where there are fewer), a bit at a time; the whole block calls it.
-__device__ __noinline__ uint64_t kth_key(TopShared& s, int K) {
+template <int NT>
+__device__ __noinline__ uint64_t kth_key(TopShared<NT>& s, int K) {
   __syncthreads();
   const int n = s.count;
   if (n < K) return 0;
@@ -500,7 +526,7 @@ __device__ __noinline__ uint64_t kth_key(TopShared& s, int K) {
   for (int bit = 63; bit >= 0; --bit) {
     const uint64_t trial = t | (uint64_t)1 << bit;
     int c = 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) c += key_of(s.cand[i]) >= trial;
+    for (int i = threadIdx.x; i < n; i += NT) c += key_of(cands(s)[i]) >= trial;
     c = __reduce_add_sync(0xffffffffu, c);
     if ((threadIdx.x & 31) == 0 && c) atomicAdd(&s.sum[bit], c);
     __syncthreads();
@@ -511,10 +537,11 @@ __device__ __noinline__ uint64_t kth_key(TopShared& s, int K) {
 
 // The candidates with keys of t or more to `few` (kFew of them at most); the whole block calls it, with the
 // candidates complete and `found` 0 behind a barrier.  Their number.
-__device__ __forceinline__ int pick(TopShared& s, uint64_t t) {
+template <int NT>
+__device__ __forceinline__ int pick(TopShared<NT>& s, uint64_t t) {
   const int n = s.count;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const uint64_t key = key_of(s.cand[i]);
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const uint64_t key = key_of(cands(s)[i]);
     if (key >= t) {
       const int at = atomicAdd(&s.found, 1);
       if (at < kFew) s.few[at] = key;
@@ -524,27 +551,35 @@ __device__ __forceinline__ int pick(TopShared& s, uint64_t t) {
   return s.found;
 }
 
-// This warp's part of the bound: the ceil(K / 8)-th largest of its lanes' maxima.
-__device__ __forceinline__ void raise(TopShared& s, float top, int K) {
-  const int rounds = (K + kWarps - 1) / kWarps, lane = threadIdx.x & 31;
-  uint32_t mine = order_of(top), t = 0;
+// This warp's part of the bound: of its lanes' two largest pieces' maxima the one that is K-th over all warps at
+// worst, ceil(K / W)-th here.
+template <int NT>
+__device__ __forceinline__ void raise(TopShared<NT>& s, float top, float second, int K) {
+  constexpr int W = NT / 32;
+  const int rounds = (K + W - 1) / W, lane = threadIdx.x & 31;
+  uint32_t mine = order_of(top), then = order_of(second), t = 0;
   for (int k = 0; k < rounds; ++k) {
     t = __reduce_max_sync(0xffffffffu, mine);
     const unsigned holds = __ballot_sync(0xffffffffu, mine == t);
-    if (lane == __ffs(holds) - 1) mine = 0;
+    if (lane == __ffs(holds) - 1) {
+      mine = then;
+      then = 0;
+    }
   }
   if (lane == 0) *const_cast<volatile uint32_t*>(&s.part[threadIdx.x >> 5]) = t;
 }
 // The bound: the least of the parts, as they are found.
-__device__ __forceinline__ float bound(const TopShared& s) {
-  static_assert(kWarps == 8, "two reads");
-  uint32_t p[8];
+template <int NT>
+__device__ __forceinline__ float bound(const TopShared<NT>& s) {
+  uint32_t t = 0xFFFFFFFFu;
 #pragma unroll
-  for (int k = 0; k < 8; k += 4)
+  for (int w = 0; w < NT / 32; w += 4) {
+    uint32_t p[4];
     asm volatile("ld.volatile.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(p[k]), "=r"(p[k + 1]), "=r"(p[k + 2]), "=r"(p[k + 3])
-                 : "r"(smem_u32(s.part + k)));
-  const uint32_t t = min(min(min(p[0], p[1]), min(p[2], p[3])), min(min(p[4], p[5]), min(p[6], p[7])));
+                 : "=r"(p[0]), "=r"(p[1]), "=r"(p[2]), "=r"(p[3])
+                 : "r"(smem_u32(s.part + w)));
+    t = min(min(t, min(p[0], p[1])), min(p[2], p[3]));
+  }
   return t == 0 ? kLeast : fmaxf(kLeast, value_of(t));
 }
 
@@ -573,9 +608,9 @@ __device__ __forceinline__ float cluster_ldf(const void* p, int rank) {
 }
 
 // Groups [begin, end) of a row whatever they hold: a barrier and, where there is no more room, an exact
-// bound before each pass of 256 groups.  The sum goes on only where `summing`.
-template <typename T, int F>
-__device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t begin, int64_t end, int K,
+// bound before each pass.  The sum goes on only where `summing`.
+template <int NT, typename T, int F>
+__device__ __noinline__ void rising_row(TopShared<NT>& s, const Row<T>& r, int64_t begin, int64_t end, int K,
                                         uint32_t* counts, bool summing, Sum& sum, int* status) {
   constexpr int G = Row<T>::G, SG = kSegment / G;
   __syncthreads();
@@ -585,12 +620,12 @@ __device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t b
   uint64_t least_key = 0;
   int upper = 0;
   for (int64_t s0 = begin; s0 < end; s0 += SG) {
-    if ((F & kHistory) && r.hist_n > 0) count_history(r, s0 * G, counts, status);
+    if ((F & kHistory) && r.hist_n > 0) count_history<NT>(r, s0 * G, counts, status);
     const int64_t s1 = min(end, s0 + SG);
-    for (int64_t g0 = s0; g0 < s1; g0 += kThreads) {
+    for (int64_t g0 = s0; g0 < s1; g0 += kPass) {
       const int64_t g = g0 + threadIdx.x;
       float v[G];
-      if (g < s1) {
+      if (threadIdx.x < kPass && g < s1) {
         load_group(r, g, v);
         adjust_group<T, F>(r, g, counts + (F & kHistory ? (g - s0) * G : 0), v);
       } else {
@@ -610,7 +645,7 @@ __device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t b
           const int kept = pick(s, least_key);
           if (threadIdx.x < kept) {
             const uint64_t key = s.few[threadIdx.x];
-            s.cand[threadIdx.x] = candidate(value_of((uint32_t)(key >> 32)), (int)~(uint32_t)key);
+            cands(s)[threadIdx.x] = candidate(value_of((uint32_t)(key >> 32)), (int)~(uint32_t)key);
           }
           if (threadIdx.x == 0) s.count = kept;
           __syncthreads();
@@ -622,7 +657,7 @@ __device__ __noinline__ void rising_row(TopShared& s, const Row<T>& r, int64_t b
       for (int j = 0; j < G; ++j)
         if (v[j] >= least) {
           const uint2 c = candidate(v[j], (int)(g * G - r.a) + j);
-          if (key_of(c) >= least_key) s.cand[atomicAdd(&s.count, 1)] = c;
+          if (key_of(c) >= least_key) cands(s)[atomicAdd(&s.count, 1)] = c;
         }
     }
   }
@@ -653,20 +688,20 @@ __device__ __forceinline__ uint4 load_raw(const Row<T>& r, int64_t g, int64_t en
 }
 
 // A cluster of CL blocks a row, each with a run of its groups.
-template <typename T, int F>
-__global__ void __launch_bounds__(kThreads, 4)
+template <int NT, typename T, int F>
+__global__ void __launch_bounds__(NT, 1024 / NT)
     k_top(int V, int64_t ldz, const T* Z, Adjust adj, int K, int log_cl, float* top_logit, int32_t* top_id,
           float* lse, int* status) {
-  constexpr int G = Row<T>::G, NV = kEach / G, CG = kThreads * NV, BG = kBits / G;
+  constexpr int G = Row<T>::G, NV = kEach / G, CG = NT * NV, BG = kBits / G;
   extern __shared__ __align__(16) uint8_t top_smem[];
-  TopShared& s = *reinterpret_cast<TopShared*>(top_smem);
-  uint32_t* bits = reinterpret_cast<uint32_t*>(top_smem + sizeof(TopShared));
-  uint32_t* table = bits + kBits / 32;
+  TopShared<NT>& s = *reinterpret_cast<TopShared<NT>*>(top_smem);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(top_smem + sizeof(TopShared<NT>));
+  uint32_t* table = reinterpret_cast<uint32_t*>(top_smem + top_smem_bytes<NT, F>() - kSlots * 4);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int CL = 1 << log_cl, rank = CL > 1 ? (int)cluster_rank() : 0;
   const int64_t row = blockIdx.x >> log_cl;
-  if (tid == 0) s.count = 0, s.found = 0;
-  if (tid < kWarps) s.part[tid] = 0;
+  if (tid == 0) s.found = 0, s.over = 0;
+  if (tid < (NT / 32)) s.part[tid] = 0;
   __syncthreads();
   tc::grid_dep_launch();
   tc::grid_dep_wait();
@@ -674,17 +709,17 @@ __global__ void __launch_bounds__(kThreads, 4)
   const int NG = r.groups(), begin = (int)((int64_t)NG * rank >> log_cl),
             end = (int)((int64_t)NG * (rank + 1) >> log_cl);
   Sum sum;
-  const bool hashed = !(F & kHistory) || r.hist_n <= kHashed;
-  if (!hashed) {
-    rising_row<T, F>(s, r, begin, end, K, table, lse != nullptr, sum, status);
+  bool quick = !(F & kHistory) || hashed(r);
+  if (!quick) {
+    rising_row<NT, T, F>(s, r, begin, end, K, table, lse != nullptr, sum, status);
   } else {
-    float top = -INFINITY, least = kLeast;
-    Hash h{table, table, 0};
-    // (the barrier after the first chunk comes before any is read)
+    float top = -INFINITY, second = -INFINITY, least = kLeast;
+    Hash h{table, 0, 0};
     auto offer = [&](float v, int id) {
-      const int at = atomicAdd(&s.count, 1);
-      if (at < kRoom) s.cand[at] = candidate(v, id);
+      const int at = atomicAdd(&s.found, 1);
+      if (at < kFew) s.few[at] = key_of(v, id);
     };
+    int notes = 0;  // of this warp
     const uint4* lane_base = reinterpret_cast<const uint4*>(r.base) + tid;
     const uint8_t* lane_bits = reinterpret_cast<const uint8_t*>(bits) + tid * G / 8;
     int chunk = 0;
@@ -696,10 +731,10 @@ __global__ void __launch_bounds__(kThreads, 4)
       auto fetch = [&](int g0) {
         if (inside(g0)) {
 #pragma unroll
-          for (int u = 0; u < NV; ++u) raw[u] = __ldcs(lane_base + g0 + u * kThreads);
+          for (int u = 0; u < NV; ++u) raw[u] = __ldcs(lane_base + g0 + u * NT);
         } else {
 #pragma unroll
-          for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, g0 + u * kThreads + tid, s1);
+          for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, g0 + u * NT + tid, s1);
         }
       };
       fetch(s0);
@@ -708,9 +743,12 @@ __global__ void __launch_bounds__(kThreads, 4)
         if (s0 != begin) __syncthreads();
         // bit e is element first + e, column first + e - a
         const int words = ((s1 - s0) * G + 31) / 32;
-        for (int w = tid; w < words; w += kThreads) {
+        for (int w = tid; w < words; w += NT) {
           uint32_t b = 0xFFFFFFFFu;
-          if ((F & kMask) && r.mask) {
+          if ((F & kMask) && r.mask && (first - r.a) % 32 == 0) {
+            const int q = (first - r.a) / 32 + w;
+            b = q < r.words ? __ldg(r.mask + q) : 0u;
+          } else if ((F & kMask) && r.mask) {
             const int c = first + w * 32 - r.a, q = c >> 5, sh = c & 31;  // c: the word's first column
             const uint32_t lo = q >= 0 && q < r.words ? __ldg(r.mask + q) : 0u;
             const uint32_t hi = sh && q + 1 < r.words ? __ldg(r.mask + q + 1) : 0u;
@@ -722,14 +760,14 @@ __global__ void __launch_bounds__(kThreads, 4)
           const int64_t e = element - first;
           if (e >= 0 && e < (s1 - s0) * G) atomicAnd(&bits[e >> 5], ~(1u << (e & 31)));
         };
-        if (past && s0 == begin) h = clear_hash(r, table);
+        if (past && s0 == begin) h = clear_hash<NT>(r, table);
         __syncthreads();
         if (past) {
           if (s0 == begin) {
-            fill_hash(h, r, begin * G, end * G, status, leave_out);
+            fill_hash<NT>(h, r, begin * G, end * G, status, leave_out);
           } else {
-            for (int i = tid; i < h.size; i += kThreads)
-              if (h.token[i]) leave_out((int64_t)h.token[i] - 1 + r.a);
+            for (int i = tid; i < h.size; i += NT)
+              if (const uint32_t x = h.slot[i]) leave_out(h.token(x) + r.a);
           }
           __syncthreads();
         }
@@ -745,7 +783,7 @@ __global__ void __launch_bounds__(kThreads, 4)
             const float4* b = reinterpret_cast<const float4*>(r.bias + c0);
 #pragma unroll
             for (int j = 0; j < kEach; j += 4) {
-              const float4 x = __ldg(b + (j / G * kThreads * G + j % G) / 4);
+              const float4 x = __ldg(b + (j / G * NT * G + j % G) / 4);
               v[j] = __fadd_rn(v[j], x.x);
               v[j + 1] = __fadd_rn(v[j + 1], x.y);
               v[j + 2] = __fadd_rn(v[j + 2], x.z);
@@ -754,15 +792,15 @@ __global__ void __launch_bounds__(kThreads, 4)
           } else {
 #pragma unroll
             for (int u = 0; u < NV; ++u)
-              if (g0 + u * kThreads + tid < s1)
-                adjust_group<T, F & kBias>(r, g0 + u * kThreads + tid, nullptr, v + u * G);
+              if (g0 + u * NT + tid < s1)
+                adjust_group<T, F & kBias>(r, g0 + u * NT + tid, nullptr, v + u * G);
           }
         }
         if (F & (kMask | kHistory)) {
           const uint8_t* q = lane_bits + (g0 - s0) * G / 8;
 #pragma unroll
           for (int u = 0; u < NV; ++u) {
-            const uint32_t b = G == 8 ? q[u * kThreads] : q[u * kThreads / 2] >> (tid & 1) * 4;
+            const uint32_t b = G == 8 ? q[u * NT] : q[u * NT / 2] >> (tid & 1) * 4;
 #pragma unroll
             for (int j = 0; j < G; ++j)
               if (!(b & 1u << j)) v[u * G + j] = -INFINITY;
@@ -770,37 +808,79 @@ __global__ void __launch_bounds__(kThreads, 4)
         }
         const float most = max_of<kEach>(v);
         if (lse) sum.add<kEach>(v, most);
+        second = fmaxf(second, fminf(top, most));
         top = fmaxf(top, most);
         if ((chunk & (chunk + 1)) == 0) {
-          raise(s, top, K);
+          raise(s, top, second, K);
           if (chunk == 0) __syncthreads();
         }
         least = fmaxf(least, bound(s));
-        if (most >= least) {
-#pragma unroll
-          for (int j = 0; j < kEach; ++j)
-            if (v[j] >= least) offer(v[j], c0 + j / G * kThreads * G + j % G);
+        const unsigned pass = __ballot_sync(0xffffffffu, most >= least);
+        if (pass) {
+          const int at = notes + __popc(pass & ((1u << lane) - 1));
+          if (most >= least && at < kNotes) s.note[warp][at] = (uint32_t)(g0 + tid);
+          notes += __popc(pass);
         }
       }
+      // the pieces noted, by the last bound where this is the last run
+      if (s1 == end) {
+        raise(s, top, second, K);
+        __syncthreads();
+      } else {
+        __syncwarp();
+      }
+      least = fmaxf(least, bound(s));
+      if (notes > kNotes && lane == 0) s.over = 1;
+      for (int i = lane; i < min(notes, kNotes); i += 32) {
+        const int p = (int)s.note[warp][i];  // the piece's first group
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+          const int g = p + u * NT;
+          if (g >= s1) break;
+          float v[G];
+          load_group(r, g, v);
+          if (F & kBias) adjust_group<T, F & kBias>(r, g, nullptr, v);
+          uint32_t b = 0xFFu;
+          if (F & (kMask | kHistory))
+            b = reinterpret_cast<const uint8_t*>(bits)[(g - s0) * G / 8] >> ((g - s0) * G & 7);
+#pragma unroll
+          for (int j = 0; j < G; ++j)
+            if (v[j] >= least && (b >> j & 1u)) offer(v[j], g * G - r.a + j);
+        }
+      }
+      notes = 0;
     }
     if ((F & kHistory) && r.hist_n > 0) {
-      // the tokens of the history
-      for (int i = tid; i < h.size; i += kThreads) {
-        const int id = (int)(h.token[i] - 1);
-        if (id < 0) continue;
-        const int64_t e = (int64_t)id + r.a;
-        if ((F & kMask) && r.mask && !(__ldg(r.mask + (id >> 5)) >> (id & 31) & 1u)) continue;
-        float v = to_f32(r.base[e]);
-        if (F & kBias) v = __fadd_rn(v, __ldg(r.bias + id));
-        v = penalised(v, h.count[i], r.rep, r.presence, r.frequency);
-        if (lse) {
-          sum.refer(v);
-          sum.l += ex2(fmaf(v, kLog2e, -sum.m));
+      // the tokens of the history, the logits of several on their way
+      constexpr int U = 4;
+      for (int i0 = tid; i0 < h.size; i0 += U * NT) {
+        uint32_t slot[U];
+        int id[U];
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + u * NT;
+          slot[u] = i < h.size ? h.slot[i] : 0u;
+          id[u] = h.token(slot[u]);
+          if ((F & kMask) && r.mask && id[u] >= 0 && !(__ldg(r.mask + (id[u] >> 5)) >> (id[u] & 31) & 1u)) id[u] = -1;
         }
-        if (v >= least) offer(v, id);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          v[u] = id[u] >= 0 ? to_f32(r.base[id[u] + r.a]) : -INFINITY;
+          if ((F & kBias) && id[u] >= 0) v[u] = __fadd_rn(v[u], __ldg(r.bias + id[u]));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (id[u] < 0) continue;
+          v[u] = penalised(v[u], h.count(slot[u]), r.rep, r.presence, r.frequency);
+          if (lse) {
+            sum.refer(v[u]);
+            sum.l += ex2(fmaf(v[u], kLog2e, -sum.m));
+          }
+          if (v[u] >= least) offer(v[u], id[u]);
+        }
       }
     }
-    raise(s, top, K);
   }
   if (lse) {
     float top_m = sum.m, l = sum.l;
@@ -812,20 +892,23 @@ __global__ void __launch_bounds__(kThreads, 4)
     if (lane == 0) s.m[warp] = top_m, s.l[warp] = l;
   }
   __syncthreads();
-  if (hashed && s.count > kRoom) rising_row<T, F>(s, r, begin, end, K, table, false, sum, status);
-  if (lse && tid == kThreads - 1) {
+  if (quick && (s.over || s.found > kFew)) {
+    rising_row<NT, T, F>(s, r, begin, end, K, table, false, sum, status);
+    quick = false;
+  }
+  if (lse && tid == NT - 1) {
     float bm = s.m[0], bl = 0.f;
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) bm = fmaxf(bm, s.m[w]);
+    for (int w = 1; w < (NT / 32); ++w) bm = fmaxf(bm, s.m[w]);
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) bl += s.l[w] * ex2(s.m[w] - bm);
+    for (int w = 0; w < (NT / 32); ++w) bl += s.l[w] * ex2(s.m[w] - bm);
     if (CL > 1)
       s.block_m = bm, s.block_l = bl;
     else
       lse[row] = lse_of(bm, bl);
   }
   // the block's largest in order: few candidates, each one's place counted, four threads a candidate
-  int n = pick(s, hashed ? (uint64_t)order_of(bound(s)) << 32 : 0);
+  int n = quick ? s.found : pick(s, 0);
   if (n > kFew) {
     const uint64_t t = kth_key(s, K);
     if (tid == 0) s.found = 0;
@@ -836,7 +919,7 @@ __global__ void __launch_bounds__(kThreads, 4)
     top_logit[row * K + place] = key ? value_of((uint32_t)(key >> 32)) : -INFINITY;
     top_id[row * K + place] = key ? (int32_t) ~(uint32_t)key : -1;
   };
-  for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+  for (int i0 = 0; i0 < n; i0 += NT / 4) {
     const int i = i0 + tid / 4;
     const uint64_t key = i < n ? s.few[i] : 0;
     int place = 0;
@@ -850,7 +933,7 @@ __global__ void __launch_bounds__(kThreads, 4)
         answer(place, key);
     }
   }
-  for (int k = n + tid; k < K; k += kThreads) {
+  for (int k = n + tid; k < K; k += NT) {
     if (CL > 1)
       s.best[k] = 0;
     else
@@ -859,18 +942,19 @@ __global__ void __launch_bounds__(kThreads, 4)
   if (CL > 1) {
     cluster_sync();
     if (rank == 0) {
+      uint64_t* lists = reinterpret_cast<uint64_t*>(s.note);
       // the blocks' lists, each in order: a key's place is the number of larger ones in all lists
-      for (int i = tid; i < CL * K; i += kThreads) s.few[i] = cluster_ld64(&s.best[i % K], i / K);
+      for (int i = tid; i < CL * K; i += NT) lists[i] = cluster_ld64(&s.best[i % K], i / K);
       __syncthreads();
-      for (int i = tid; i < CL * K; i += kThreads) {
-        const uint64_t key = s.few[i];
+      for (int i = tid; i < CL * K; i += NT) {
+        const uint64_t key = lists[i];
         if (key == 0) continue;
         int place = 0;
         for (int b = 0; b < CL; ++b) {
           int lo = 0, hi = K;  // entries of list b larger than key
           while (lo < hi) {
             const int mid = (lo + hi) / 2;
-            if (s.few[b * K + mid] > key) lo = mid + 1; else hi = mid;
+            if (lists[b * K + mid] > key) lo = mid + 1; else hi = mid;
           }
           place += lo;
         }
@@ -884,11 +968,11 @@ __global__ void __launch_bounds__(kThreads, 4)
         int lo = 0, hi = K;
         while (lo < hi) {
           const int mid = (lo + hi) / 2;
-          if (s.few[b * K + mid] != 0) lo = mid + 1; else hi = mid;
+          if (lists[b * K + mid] != 0) lo = mid + 1; else hi = mid;
         }
         have += lo;
       }
-      for (int k = have + tid; k < K; k += kThreads) {
+      for (int k = have + tid; k < K; k += NT) {
         top_logit[row * K + k] = -INFINITY;
         top_id[row * K + k] = -1;
       }
@@ -921,39 +1005,48 @@ cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjus
   return e;
 }
 
-// Blocks a row, as a power of two: one where rows fill the card, else as many as still leave a block a chunk.
+// Blocks a row, as a power of two: one where rows fill the card, else as many as leave a block 1024 logits.
 int cluster_of(int64_t n, int V) {
   int c = 0;
-  while (1 << c < kMaxCluster && (n << (c + 1)) <= 152 * 2 && V >> (c + 1) >= kChunk / 4) ++c;
+  while (1 << c < kMaxCluster && (n << (c + 1)) <= 152 * 2 && V >> (c + 1) >= 1024) ++c;
   return c;
 }
 
-template <typename T, int F>
-cudaError_t run_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int K, float* top_logit,
-                    int32_t* top_id, float* lse, int* status, cudaStream_t st) {
-  const int log_cl = cluster_of(n, V), CL = 1 << log_cl;
-  constexpr int smem = (int)sizeof(TopShared) + (F & (kMask | kHistory) ? kBits / 8 : 0) + (F & kHistory ? kSlots * 8 : 0);
+template <int NT, typename T, int F>
+cudaError_t launch_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int K, int log_cl,
+                       float* top_logit, int32_t* top_id, float* lse, int* status, cudaStream_t st) {
+  constexpr int smem = top_smem_bytes<NT, F>();
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = allow_smem(k_top<T, F>, smem, done);
+  cudaError_t e = allow_smem(k_top<NT, T, F>, smem, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(n * CL));
-  cfg.blockDim = dim3(kThreads);
+  cfg.gridDim = dim3((unsigned)(n << log_cl));
+  cfg.blockDim = dim3(NT);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)CL;
+  attr[1].val.clusterDim.x = 1u << log_cl;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = CL > 1 ? 2 : 1;
-  e = cudaLaunchKernelEx(&cfg, k_top<T, F>, V, ldz, static_cast<const T*>(Z), adj, K, log_cl, top_logit, top_id, lse,
-                         status);
+  cfg.numAttrs = log_cl > 0 ? 2 : 1;
+  e = cudaLaunchKernelEx(&cfg, k_top<NT, T, F>, V, ldz, static_cast<const T*>(Z), adj, K, log_cl, top_logit, top_id,
+                         lse, status);
   if (e == cudaSuccess) note_launch();
   return e;
+}
+
+template <typename T, int F>
+cudaError_t run_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int K, float* top_logit,
+                    int32_t* top_id, float* lse, int* status, cudaStream_t st) {
+  const int log_cl = cluster_of(n, V);
+  // Many rows: small blocks, so that one's latencies are another's work.  Few: a row's own work in one go.
+  if ((n << log_cl) <= 152 * 4)
+    return launch_top<512, T, F>(n, V, ldz, Z, adj, K, log_cl, top_logit, top_id, lse, status, st);
+  return launch_top<128, T, F>(n, V, ldz, Z, adj, K, log_cl, top_logit, top_id, lse, status, st);
 }
 
 // f with the adjustment's flags as a constant.
