@@ -10,7 +10,7 @@
 //
 // Rows are read once, as the aligned 16-byte groups that cover them: a row may begin anywhere in a group
 // (odd row lengths), so column c of a row is element c + a of its groups, a its first element's place in the
-// first one.  Occurrences are counted in shared memory, kSegment columns at a time, by reading the
+// first one.  Occurrences are counted in shared memory, a few thousand columns at a time, by reading the
 // row's history once for each segment: no sorting and no workspace.
 #include <cuda_bf16.h>
 
@@ -30,9 +30,7 @@ using tc::smem_u32;
 namespace {
 
 constexpr int kThreads = 256;     // of a block of the adjustment
-constexpr int kSlots = 2048;         // of a hash table of a history's tokens
-constexpr int kHashed = kSlots / 2;  // tokens of a history that go there; longer ones are counted
-constexpr int kSegment = kSlots;      // elements whose occurrences are counted at a time (in the same place)
+constexpr int kSlots = 2048;      // of a hash table of a history's tokens, at most
 constexpr int kEach = 16;       // elements of a thread at a time
 
 // What an adjustment has (template flags): one without any costs nothing.
@@ -63,9 +61,9 @@ __device__ __forceinline__ void report(int* status, int site) {
 }
 
 // A row of logits and its part of the adjustment.
-template <typename T, int W = 16>
+template <typename T>
 struct Row {
-  static constexpr int G = W / (int)sizeof(T);   // elements of a group
+  static constexpr int G = 16 / (int)sizeof(T);  // elements of a group
   const T* base;                                 // the group that holds column 0
   int a;                                         // column 0's place in it
   int V;
@@ -78,12 +76,12 @@ struct Row {
   __device__ int groups() const { return (V + a + G - 1) / G; }
 };
 
-template <typename T, int F, int W = 16>
-__device__ __forceinline__ Row<T, W> make_row(const T* Z, int64_t ldz, int64_t i, int V, const Adjust& adj,
-                                              int* status) {
-  Row<T, W> r;
+template <typename T, int F>
+__device__ __forceinline__ Row<T> make_row(const T* Z, int64_t ldz, int64_t i, int V, const Adjust& adj,
+                                           int* status) {
+  Row<T> r;
   const T* p = Z + i * ldz;
-  r.a = (int)((reinterpret_cast<uintptr_t>(p) & (W - 1)) / sizeof(T));
+  r.a = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
   r.base = p - r.a;
   r.V = V;
   r.bias = adj.bias;
@@ -113,18 +111,19 @@ __device__ __forceinline__ Row<T, W> make_row(const T* Z, int64_t ldz, int64_t i
   return r;
 }
 
-// Occurrences of the tokens of elements [first, first + kSegment) of a row (element = column + a).
-template <int NT, typename T, int W>
-__device__ __forceinline__ void count_history(const Row<T, W>& r, int64_t first, uint32_t* counts, int* status) {
+// Occurrences of the tokens of elements [first, first + segment) of a row (element = column + a).
+template <int NT, typename T>
+__device__ __forceinline__ void count_history(const Row<T>& r, int64_t first, int segment, uint32_t* counts,
+                                              int* status) {
   __syncthreads();
-  for (int i = threadIdx.x; i < kSegment / 4; i += NT)
+  for (int i = threadIdx.x; i < segment / 4; i += NT)
     reinterpret_cast<uint4*>(counts)[i] = make_uint4(0, 0, 0, 0);
   __syncthreads();
   for (int64_t i = threadIdx.x; i < r.hist_n; i += NT) {
     const int id = r.hist[i];
     if (id >= r.V) report(status, kSiteHistoryId);
     const int64_t at = (int64_t)id + r.a - first;
-    if (id >= 0 && id < r.V && at >= 0 && at < kSegment) atomicAdd(&counts[at], 1u);
+    if (id >= 0 && id < r.V && at >= 0 && at < segment) atomicAdd(&counts[at], 1u);
   }
   __syncthreads();
 }
@@ -152,18 +151,12 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 // The logits of group g (G of them) as they are; -inf past the row's ends.
-template <typename T, int W>
-__device__ __forceinline__ void load_group(const Row<T, W>& r, int64_t g, float* v) {
-  constexpr int G = Row<T, W>::G;
+template <typename T>
+__device__ __forceinline__ void load_group(const Row<T>& r, int64_t g, float* v) {
+  constexpr int G = Row<T>::G;
   const int64_t c0 = g * G - r.a;
   if (c0 >= 0 && c0 + G <= r.V) {
-    if constexpr (W == 16) {
-      unpack(__ldcs(reinterpret_cast<const uint4*>(r.base + g * G)), v, T());
-    } else {
-      const uint32_t x = __ldcs(reinterpret_cast<const uint32_t*>(r.base + g * G));
-      v[0] = __uint_as_float(G == 1 ? x : x << 16);
-      if (G == 2) v[G - 1] = __uint_as_float(x & 0xFFFF0000u);
-    }
+    unpack(__ldcs(reinterpret_cast<const uint4*>(r.base + g * G)), v, T());
   } else {
 #pragma unroll
     for (int j = 0; j < G; ++j) v[j] = c0 + j >= 0 && c0 + j < r.V ? to_f32(r.base[g * G + j]) : -INFINITY;
@@ -171,14 +164,14 @@ __device__ __forceinline__ void load_group(const Row<T, W>& r, int64_t g, float*
 }
 
 // Adjusts group g in place; counts: the occurrences of its elements.
-template <typename T, int F, int W>
-__device__ __forceinline__ void adjust_group(const Row<T, W>& r, int64_t g, const uint32_t* counts, float* v) {
-  constexpr int G = Row<T, W>::G;
+template <typename T, int F>
+__device__ __forceinline__ void adjust_group(const Row<T>& r, int64_t g, const uint32_t* counts, float* v) {
+  constexpr int G = Row<T>::G;
   const int c0 = (int)(g * G - r.a);
   if (F & kBias) {
-    if (G >= 4 && r.a == 0 && c0 + G <= r.V) {
+    if (r.a == 0 && c0 + G <= r.V) {
 #pragma unroll
-      for (int j = 0; j + 4 <= G; j += 4) {
+      for (int j = 0; j < G; j += 4) {
         const float4 b = __ldg(reinterpret_cast<const float4*>(r.bias + c0 + j));
         v[j] = __fadd_rn(v[j], b.x);
         v[j + 1] = __fadd_rn(v[j + 1], b.y);
@@ -196,10 +189,7 @@ __device__ __forceinline__ void adjust_group(const Row<T, W>& r, int64_t g, cons
   }
   if ((F & kHistory) && r.hist_n > 0) {
 #pragma unroll
-    for (int k = 0; k < G; ++k)
-      if (G < 4 && counts[k]) v[k] = penalised(v[k], counts[k], r.rep, r.presence, r.frequency);
-#pragma unroll
-    for (int k = 0; k + 4 <= G; k += 4) {
+    for (int k = 0; k < G; k += 4) {
       const uint4 c = *reinterpret_cast<const uint4*>(counts + k);
       if (c.x | c.y | c.z | c.w) {
         const uint32_t u[4] = {c.x, c.y, c.z, c.w};
@@ -221,7 +211,7 @@ __device__ __forceinline__ void adjust_group(const Row<T, W>& r, int64_t g, cons
   }
 }
 
-// A hash table of a history's tokens and their counts in shared memory (kSlots words): a slot holds a token plus
+// A hash table of a history's tokens and their counts in shared memory: a slot holds a token plus
 // one in its low `low` bits and its count above.  Only the part that the history needs is used: a small one is
 // cleared and looked through quickly.
 struct Hash {
@@ -231,16 +221,17 @@ struct Hash {
   __device__ int token(uint32_t x) const { return (int)(x & ((1u << low) - 1)) - 1; }
   __device__ uint32_t count(uint32_t x) const { return x >> low; }
 };
-// Whether a history goes there: it is short, and its length fits beside a token.
+// Whether a history goes there: it leaves a quarter of the slots free, and its length fits beside a token.  Longer
+// ones are counted, as many elements at a time as there are slots.
 template <typename R>
-__device__ __forceinline__ bool hashed(const R& r) {
-  return r.hist_n <= kHashed && r.V < 1 << 21;
+__device__ __forceinline__ bool hashed(const R& r, int slots) {
+  return r.hist_n <= slots / 4 * 3 && r.V < 1 << 21;
 }
 
 __device__ __forceinline__ void hash_add(const Hash& h, uint32_t id) {
   const uint32_t mask = (1u << h.low) - 1;
   uint32_t at = (id * 2654435761u) >> 7 & (h.size - 1);
-  for (int k = 0; k < h.size; ++k, at = (at + 1) & (h.size - 1)) {  // (half of the slots stay empty)
+  for (int k = 0; k < h.size; ++k, at = (at + 1) & (h.size - 1)) {  // (a quarter of the slots stays empty)
     const uint32_t was = atomicCAS(&h.slot[at], 0u, 1u << h.low | (id + 1));
     if (was == 0) return;
     if ((was & mask) == id + 1) {
@@ -251,54 +242,54 @@ __device__ __forceinline__ void hash_add(const Hash& h, uint32_t id) {
 }
 
 // An empty table for the tokens of r's history (a barrier has to follow before it is filled).
-template <int NT, typename T, int W>
-__device__ __forceinline__ Hash clear_hash(const Row<T, W>& r, uint32_t* table) {
+template <int NT, typename T>
+__device__ __forceinline__ Hash clear_hash(const Row<T>& r, uint32_t* table, int slots) {
   Hash h{table, 64, 32 - __clz(r.V)};  // (tokens plus one: 1 .. V)
-  while (h.size < 2 * r.hist_n) h.size *= 2;
+  while (h.size < 2 * r.hist_n && h.size < slots) h.size *= 2;
   for (int i = threadIdx.x; i < h.size / 4; i += NT) reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
   return h;
 }
 // Adds the tokens whose elements (column + a) are in [first, last), calling seen(element) for each (a barrier has
 // to follow before the table is read).
-template <int NT, typename T, int W, typename Fn>
-__device__ __forceinline__ void fill_hash(const Hash& h, const Row<T, W>& r, int64_t first, int64_t last, int* status,
+template <int NT, typename T, typename Fn>
+__device__ __forceinline__ void fill_hash(const Hash& h, const Row<T>& r, int64_t first, int64_t last, int* status,
                                           Fn seen) {
-  int next = threadIdx.x < r.hist_n ? r.hist[threadIdx.x] : -1;
-  for (int i = threadIdx.x; i < (int)r.hist_n; i += NT) {
-    const int id = next;
-    if (i + NT < (int)r.hist_n) next = r.hist[i + NT];
-    if (id >= r.V) report(status, kSiteHistoryId);
-    const int64_t e = (int64_t)id + r.a;
-    if (id >= 0 && id < r.V && e >= first && e < last) {
-      hash_add(h, (uint32_t)id);
-      seen(e);
+  constexpr int U = 4;  // tokens on their way
+  for (int i0 = threadIdx.x; i0 < (int)r.hist_n; i0 += U * NT) {
+    int id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = i0 + u * NT < (int)r.hist_n ? r.hist[i0 + u * NT] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (id[u] >= r.V) report(status, kSiteHistoryId);
+      const int64_t e = (int64_t)id[u] + r.a;
+      if (id[u] >= 0 && id[u] < r.V && e >= first && e < last) {
+        hash_add(h, (uint32_t)id[u]);
+        seen(e);
+      }
     }
   }
 }
 
 // ------------------------------------------------------------------------------ adjustment
-template <int G>
 __device__ __forceinline__ void store_group(float* p, const float* v) {
-  if constexpr (G == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  else *p = v[0];
+  __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
 }
-template <int G>
 __device__ __forceinline__ void store_group(__nv_bfloat16* p, const float* v) {
-  __nv_bfloat162 h[G / 2];
+  __nv_bfloat162 h[4];
 #pragma unroll
-  for (int j = 0; j < G / 2; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-  if constexpr (G == 8) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
-  else *reinterpret_cast<__nv_bfloat162*>(p) = h[0];
+  for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+  __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(h));
 }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 
-template <typename T, int W>
-__device__ __forceinline__ void store_row_group(const Row<T, W>& r, T* o, bool vec, int64_t g, const float* v) {
-  constexpr int G = Row<T, W>::G;
+template <typename T>
+__device__ __forceinline__ void store_row_group(const Row<T>& r, T* o, bool vec, int64_t g, const float* v) {
+  constexpr int G = Row<T>::G;
   const int64_t c0 = g * G - r.a;
   if (vec && c0 >= 0 && c0 + G <= r.V) {
-    store_group<G>(o + c0, v);
+    store_group(o + c0, v);
   } else {
 #pragma unroll
     for (int j = 0; j < G; ++j)
@@ -306,26 +297,18 @@ __device__ __forceinline__ void store_row_group(const Row<T, W>& r, T* o, bool v
   }
 }
 
-// Block (row, run of `per` groups).  Biases and masks are one pass over the elements; the tokens of the history
-// come after it, from a hash table, their logits read before it (out may be Z).
-template <typename T, int F, int W>
-__global__ void __launch_bounds__(kThreads)
-    k_adjust(int V, int64_t ldz, const T* Z, Adjust adj, int64_t ldo, T* out, int per, int* status) {
-  constexpr int G = Row<T, W>::G, U = 64 / W;  // U groups of a thread on their way
-  __shared__ __align__(16) uint32_t table[F & kHistory ? kSlots : 4];
-  __shared__ float raw[F & kHistory ? kSlots : 1];
-  tc::grid_dep_launch();
-  tc::grid_dep_wait();
-  const int64_t i = blockIdx.x;
-  const Row<T, W> r = make_row<T, F, W>(Z, ldz, i, V, adj, status);
-  T* o = out + i * ldo;
-  const bool vec = (reinterpret_cast<uintptr_t>(o - r.a) & (W - 1)) == 0;
-  const int64_t g0 = (int64_t)blockIdx.y * per, g1 = min((int64_t)r.groups(), g0 + per);
-  if (g0 >= g1) return;
-  if ((F & kHistory) && !hashed(r)) {
-    constexpr int SG = kSegment / G;
+// A row's groups [g0, g1).  Biases and masks are one pass over the elements (not where `tokens`: another launch has
+// done that); the tokens of the history come after it, from a hash table, their logits read before it (out may be
+// Z).  staged: the biases of the groups' elements, NULL: they are read where they lie.
+template <typename T, int F>
+__device__ __forceinline__ void adjust_run(const Row<T>& r, T* o, bool in_place, bool tokens, int64_t g0, int64_t g1,
+                                           const float* staged, uint32_t* table, float* raw, int* status) {
+  constexpr int G = Row<T>::G;
+  const bool vec = (reinterpret_cast<uintptr_t>(o - r.a) & 15) == 0;
+  if ((F & kHistory) && !hashed(r, kSlots)) {
+    constexpr int SG = kSlots / G;
     for (int64_t s0 = g0; s0 < g1; s0 += SG) {
-      count_history<kThreads>(r, s0 * G, table, status);
+      count_history<kThreads>(r, s0 * G, kSlots, table, status);
       for (int64_t g = s0 + threadIdx.x; g < min(g1, s0 + SG); g += kThreads) {
         float v[G];
         load_group(r, g, v);
@@ -337,26 +320,32 @@ __global__ void __launch_bounds__(kThreads)
   }
   Hash h{table, 0, 0};
   if ((F & kHistory) && r.hist_n > 0) {
-    h = clear_hash<kThreads>(r, table);
+    h = clear_hash<kThreads>(r, table, kSlots);
     __syncthreads();
     fill_hash<kThreads>(h, r, g0 * G, g1 * G, status, [](int64_t) {});
     __syncthreads();
     for (int k = threadIdx.x; k < h.size; k += kThreads)
       if (const uint32_t x = h.slot[k]) raw[k] = to_f32(r.base[h.token(x) + r.a]);
-    __syncthreads();
+    if (in_place) __syncthreads();
   }
-  if ((F & (kBias | kMask)) || out != Z) {
-    for (int64_t g = g0 + threadIdx.x; g < g1; g += U * kThreads) {
-      float v[U][G];
+  if (!tokens && ((F & (kBias | kMask)) || !in_place)) {
+    for (int64_t g = g0 + threadIdx.x; g < g1; g += kThreads) {
+      float v[G];
+      load_group(r, g, v);
+      if ((F & kBias) && staged) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (g + u * kThreads < g1) load_group(r, g + u * kThreads, v[u]);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (g + u * kThreads >= g1) break;
-        adjust_group<T, F & ~kHistory>(r, g + u * kThreads, nullptr, v[u]);
-        store_row_group(r, o, vec, g + u * kThreads, v[u]);
+        for (int j = 0; j < G; j += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(staged + (g - g0) * G + j);
+          v[j] = __fadd_rn(v[j], b.x);
+          v[j + 1] = __fadd_rn(v[j + 1], b.y);
+          v[j + 2] = __fadd_rn(v[j + 2], b.z);
+          v[j + 3] = __fadd_rn(v[j + 3], b.w);
+        }
+        adjust_group<T, F & kMask>(r, g, nullptr, v);
+      } else {
+        adjust_group<T, F & ~kHistory>(r, g, nullptr, v);
       }
+      store_row_group(r, o, vec, g, v);
     }
   }
   if ((F & kHistory) && r.hist_n > 0) {
@@ -371,6 +360,52 @@ __global__ void __launch_bounds__(kThreads)
       if ((F & kMask) && r.mask && !(__ldg(r.mask + (id >> 5)) >> (id & 31) & 1u)) v = -INFINITY;
       store1(o + id, v);
     }
+  }
+}
+
+// Block (row, run of `per` groups).
+template <typename T, int F>
+__global__ void __launch_bounds__(kThreads)
+    k_adjust(int V, int64_t ldz, const T* Z, Adjust adj, int64_t ldo, T* out, int per, int tokens, int* status) {
+  __shared__ __align__(16) uint32_t table[F & kHistory ? kSlots : 4];
+  __shared__ float raw[F & kHistory ? kSlots : 1];
+  tc::grid_dep_launch();
+  tc::grid_dep_wait();
+  const int64_t i = blockIdx.x;
+  const Row<T> r = make_row<T, F>(Z, ldz, i, V, adj, status);
+  const int64_t g0 = (int64_t)blockIdx.y * per, g1 = min((int64_t)r.groups(), g0 + per);
+  if (g0 >= g1) return;
+  adjust_run<T, F>(r, out + i * ldo, out == Z, tokens, g0, g1, nullptr, table, raw, status);
+}
+
+// The same with biases where rows begin anywhere in 16 bytes: rows `step` apart begin at the same place, and kShare of
+// them share a run of kRun biases, laid out in shared memory as their groups lie.  (Read one by one, a warp's biases
+// are 16 or 32 bytes apart.  8192 x 49999 bf16 with biases: 1142 us in groups of 4 bytes, 343 shared.)
+constexpr int kRun = 8192, kShare = 8;
+template <typename T, int F>
+__global__ void __launch_bounds__(kThreads)
+    k_adjust_shared(int64_t n, int V, int64_t ldz, const T* Z, Adjust adj, int64_t ldo, T* out, int step, int* status) {
+  constexpr int G = Row<T>::G, per = kRun / G;
+  extern __shared__ __align__(16) uint8_t adjust_smem[];
+  float* staged = reinterpret_cast<float*>(adjust_smem);
+  tc::grid_dep_launch();
+  tc::grid_dep_wait();
+  const int64_t first = (int64_t)(blockIdx.x / step) * step * kShare + blockIdx.x % step;
+  const int64_t g0 = (int64_t)blockIdx.y * per;
+  for (int k = 0; k < kShare; ++k) {
+    const int64_t i = first + (int64_t)k * step;
+    if (i >= n) break;
+    const Row<T> r = make_row<T, F>(Z, ldz, i, V, adj, status);
+    const int64_t g1 = min((int64_t)r.groups(), g0 + per);
+    if (g0 >= g1) break;
+    if (k == 0) {
+      for (int e = threadIdx.x; e < (g1 - g0) * G; e += kThreads) {
+        const int64_t c = g0 * G + e - r.a;
+        staged[e] = c >= 0 && c < V ? __ldg(adj.bias + c) : 0.f;
+      }
+    }
+    if (k == 0) __syncthreads();
+    adjust_run<T, F>(r, out + i * ldo, out == Z, false, g0, g1, staged, nullptr, nullptr, status);
   }
 }
 
@@ -389,40 +424,58 @@ __global__ void __launch_bounds__(kThreads)
 // out.  The tokens of a history are cleared too, counted in a hash table, and added one by one after the
 // others: c > 0 for a few hundred of 50000 tokens costs no element a test of its own.
 constexpr int kBits = 65536;  // elements whose bits are in shared memory at a time
-constexpr int kPass = 128;    // groups of a pass of rising_row
-constexpr int kRoom = 1152;   // candidates: those of a pass (1024) and the K before it
+constexpr int kPass = 64;     // groups of a pass of rising_row
+constexpr int kRoom = kPass * 8 + kMaxTop;  // candidates: those of a pass and the K before it
 constexpr int kMaxCluster = 8;
-constexpr int kFew = 512;       // candidates that are put in order
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoLogit = -3.0e38f;  // reference of a sum without terms
 constexpr float kLeast = -3.402823466e38f;
 
-constexpr int kNotes = 256;  // pieces a warp notes
-// What a block of NT threads has in shared memory; `space` is followed by the bits and the hash table, as far as the
-// adjustment needs them.
+// What a block of NT threads has in shared memory, and after it, at the places of Room: the best candidates, a
+// block's answers (in a cluster), the notes, the bits and the hash table.  The less there is of it, the more is left
+// to the L1 cache, through which the logits and the biases come (with 26 KB a block, eight blocks an SM, fp32 rows
+// take a quarter longer than with 15).
 template <int NT>
 struct TopShared {
   static constexpr int W = NT / 32;
-  uint64_t few[kFew];
-  uint64_t best[kMaxTop];
   float m[W], l[W];
   float block_m, block_l;
   alignas(16) uint32_t part[W];  // of the bound, as orders
   int count, found, over, sum[64];  // over: pieces or candidates outgrew their room
-  alignas(16) uint32_t note[W][kNotes];
+  uint64_t* few;
+  uint2* cand;  // rising_row's candidates: in the place of the notes and the bits, once those are done with
+  int most;     // of few
 };
-// In the place of the notes and, where they are, the bits, once those are done with: rising_row's candidates, and
-// the lists of a cluster's blocks.
-constexpr int kLate = kRoom * 8 > kMaxCluster * kMaxTop * 8 ? kRoom * 8 : kMaxCluster * kMaxTop * 8;
-template <int NT, int F>
-__host__ __device__ constexpr int top_smem_bytes() {
-  const int before = (int)sizeof(TopShared<NT>) - (NT / 32) * kNotes * 4;
-  const int notes = (NT / 32) * kNotes * 4 + (F & (kMask | kHistory) ? kBits / 8 : 0);
-  return before + (notes > kLate ? notes : kLate) + (F & kHistory ? kSlots * 4 : 0);
-}
+struct Room {
+  int few, notes, slots;                         // candidates, pieces a warp notes, slots
+  int at_few, at_best, at_note, at_bits, at_table;  // in bytes
+  int bytes;
+};
 template <int NT>
-__device__ __forceinline__ uint2* cands(TopShared<NT>& s) { return reinterpret_cast<uint2*>(s.note); }
-
+Room room_of(int flags, int V, int K, int64_t n, int64_t history_len, bool cluster) {
+  Room r{};
+  r.few = K <= 32 ? 256 : 512;
+  r.notes = K <= 64 ? 128 : 256;
+  // room for three histories of the average length
+  r.slots = flags & kHistory ? 1024 : 0;
+  while (r.slots && r.slots < kSlots && r.slots < 4 * history_len / std::max<int64_t>(n, 1)) r.slots *= 2;
+  int at = ((int)sizeof(TopShared<NT>) + 15) / 16 * 16;
+  auto take = [&](int bytes) {
+    const int here = at;
+    at += (bytes + 15) / 16 * 16;
+    return here;
+  };
+  r.at_few = take(r.few * 8);
+  r.at_best = take(cluster ? kMaxTop * 8 : 0);
+  r.at_note = take(NT / 32 * r.notes * 4);
+  // (whole chunks of the row)
+  r.at_bits = take(flags & (kMask | kHistory) ? std::min(kBits, (V + 8 + NT * kEach - 1) / (NT * kEach) * NT * kEach) / 8 : 0);
+  // (a cluster's lists come where the notes were)
+  at = std::max(at, r.at_note + std::max(kRoom * 8, cluster ? kMaxCluster * kMaxTop * 8 : 0));
+  r.at_table = take(r.slots * 4);
+  r.bytes = at;
+  return r;
+}
 // Order of logits as unsigned numbers (-0 counts as 0), and keys: the larger logit, then the lower token.
 __device__ __forceinline__ uint32_t order_of(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);
@@ -526,7 +579,7 @@ __device__ __noinline__ uint64_t kth_key(TopShared<NT>& s, int K) {
   for (int bit = 63; bit >= 0; --bit) {
     const uint64_t trial = t | (uint64_t)1 << bit;
     int c = 0;
-    for (int i = threadIdx.x; i < n; i += NT) c += key_of(cands(s)[i]) >= trial;
+    for (int i = threadIdx.x; i < n; i += NT) c += key_of(s.cand[i]) >= trial;
     c = __reduce_add_sync(0xffffffffu, c);
     if ((threadIdx.x & 31) == 0 && c) atomicAdd(&s.sum[bit], c);
     __syncthreads();
@@ -535,16 +588,16 @@ __device__ __noinline__ uint64_t kth_key(TopShared<NT>& s, int K) {
   return t;
 }
 
-// The candidates with keys of t or more to `few` (kFew of them at most); the whole block calls it, with the
+// The candidates with keys of t or more to `few` (as many of them as it holds); the whole block calls it, with the
 // candidates complete and `found` 0 behind a barrier.  Their number.
 template <int NT>
 __device__ __forceinline__ int pick(TopShared<NT>& s, uint64_t t) {
   const int n = s.count;
   for (int i = threadIdx.x; i < n; i += NT) {
-    const uint64_t key = key_of(cands(s)[i]);
+    const uint64_t key = key_of(s.cand[i]);
     if (key >= t) {
       const int at = atomicAdd(&s.found, 1);
-      if (at < kFew) s.few[at] = key;
+      if (at < s.most) s.few[at] = key;
     }
   }
   __syncthreads();
@@ -611,8 +664,9 @@ __device__ __forceinline__ float cluster_ldf(const void* p, int rank) {
 // bound before each pass.  The sum goes on only where `summing`.
 template <int NT, typename T, int F>
 __device__ __noinline__ void rising_row(TopShared<NT>& s, const Row<T>& r, int64_t begin, int64_t end, int K,
-                                        uint32_t* counts, bool summing, Sum& sum, int* status) {
-  constexpr int G = Row<T>::G, SG = kSegment / G;
+                                        uint32_t* counts, int segment, bool summing, Sum& sum, int* status) {
+  constexpr int G = Row<T>::G;
+  const int64_t SG = F & kHistory && r.hist_n > 0 ? segment / G : end - begin;
   __syncthreads();
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
@@ -620,7 +674,7 @@ __device__ __noinline__ void rising_row(TopShared<NT>& s, const Row<T>& r, int64
   uint64_t least_key = 0;
   int upper = 0;
   for (int64_t s0 = begin; s0 < end; s0 += SG) {
-    if ((F & kHistory) && r.hist_n > 0) count_history<NT>(r, s0 * G, counts, status);
+    if ((F & kHistory) && r.hist_n > 0) count_history<NT>(r, s0 * G, segment, counts, status);
     const int64_t s1 = min(end, s0 + SG);
     for (int64_t g0 = s0; g0 < s1; g0 += kPass) {
       const int64_t g = g0 + threadIdx.x;
@@ -645,7 +699,7 @@ __device__ __noinline__ void rising_row(TopShared<NT>& s, const Row<T>& r, int64
           const int kept = pick(s, least_key);
           if (threadIdx.x < kept) {
             const uint64_t key = s.few[threadIdx.x];
-            cands(s)[threadIdx.x] = candidate(value_of((uint32_t)(key >> 32)), (int)~(uint32_t)key);
+            s.cand[threadIdx.x] = candidate(value_of((uint32_t)(key >> 32)), (int)~(uint32_t)key);
           }
           if (threadIdx.x == 0) s.count = kept;
           __syncthreads();
@@ -657,7 +711,7 @@ __device__ __noinline__ void rising_row(TopShared<NT>& s, const Row<T>& r, int64
       for (int j = 0; j < G; ++j)
         if (v[j] >= least) {
           const uint2 c = candidate(v[j], (int)(g * G - r.a) + j);
-          if (key_of(c) >= least_key) cands(s)[atomicAdd(&s.count, 1)] = c;
+          if (key_of(c) >= least_key) s.cand[atomicAdd(&s.count, 1)] = c;
         }
     }
   }
@@ -689,18 +743,26 @@ __device__ __forceinline__ uint4 load_raw(const Row<T>& r, int64_t g, int64_t en
 
 // A cluster of CL blocks a row, each with a run of its groups.
 template <int NT, typename T, int F>
-__global__ void __launch_bounds__(NT, 1024 / NT)
+__global__ void __launch_bounds__(NT, (NT > 128 ? 2 : !(F & kBias) ? 8 : sizeof(T) == 4 ? 6 : 7))
     k_top(int V, int64_t ldz, const T* Z, Adjust adj, int K, int log_cl, float* top_logit, int32_t* top_id,
-          float* lse, int* status) {
+          float* lse, Room room, int* status) {
   constexpr int G = Row<T>::G, NV = kEach / G, CG = NT * NV, BG = kBits / G;
   extern __shared__ __align__(16) uint8_t top_smem[];
   TopShared<NT>& s = *reinterpret_cast<TopShared<NT>*>(top_smem);
-  uint32_t* bits = reinterpret_cast<uint32_t*>(top_smem + sizeof(TopShared<NT>));
-  uint32_t* table = reinterpret_cast<uint32_t*>(top_smem + top_smem_bytes<NT, F>() - kSlots * 4);
+  uint64_t* few = reinterpret_cast<uint64_t*>(top_smem + room.at_few);
+  uint64_t* best = reinterpret_cast<uint64_t*>(top_smem + room.at_best);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(top_smem + room.at_bits);
+  uint32_t* table = reinterpret_cast<uint32_t*>(top_smem + room.at_table);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int CL = 1 << log_cl, rank = CL > 1 ? (int)cluster_rank() : 0;
   const int64_t row = blockIdx.x >> log_cl;
-  if (tid == 0) s.found = 0, s.over = 0;
+  uint32_t* note = reinterpret_cast<uint32_t*>(top_smem + room.at_note) + (tid >> 5) * room.notes;
+  if (tid == 0) {
+    s.found = s.over = 0;
+    s.few = few;
+    s.cand = reinterpret_cast<uint2*>(top_smem + room.at_note);
+    s.most = room.few;
+  }
   if (tid < (NT / 32)) s.part[tid] = 0;
   __syncthreads();
   tc::grid_dep_launch();
@@ -709,15 +771,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
   const int NG = r.groups(), begin = (int)((int64_t)NG * rank >> log_cl),
             end = (int)((int64_t)NG * (rank + 1) >> log_cl);
   Sum sum;
-  bool quick = !(F & kHistory) || hashed(r);
+  bool quick = !(F & kHistory) || hashed(r, room.slots);
   if (!quick) {
-    rising_row<NT, T, F>(s, r, begin, end, K, table, lse != nullptr, sum, status);
+    rising_row<NT, T, F>(s, r, begin, end, K, table, room.slots, lse != nullptr, sum, status);
   } else {
     float top = -INFINITY, second = -INFINITY, least = kLeast;
     Hash h{table, 0, 0};
     auto offer = [&](float v, int id) {
       const int at = atomicAdd(&s.found, 1);
-      if (at < kFew) s.few[at] = key_of(v, id);
+      if (at < room.few) few[at] = key_of(v, id);
     };
     int notes = 0;  // of this warp
     const uint4* lane_base = reinterpret_cast<const uint4*>(r.base) + tid;
@@ -737,7 +799,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
           for (int u = 0; u < NV; ++u) raw[u] = load_raw(r, g0 + u * NT + tid, s1);
         }
       };
+      // biases ahead too, where rows begin with a group and they lie as the logits do
+      constexpr bool ahead = (F & kBias) != 0;
+      float4 soon[ahead ? kEach / 4 : 1];
+      auto fetch_bias = [&](int g0) {
+        const float4* b = reinterpret_cast<const float4*>(r.bias + (g0 + tid) * G);
+#pragma unroll
+        for (int j = 0; j < kEach; j += 4) soon[ahead ? j / 4 : 0] = __ldg(b + (j / G * NT * G + j % G) / 4);
+      };
       fetch(s0);
+      if (ahead && r.a == 0 && inside(s0)) fetch_bias(s0);
       if (F & (kMask | kHistory)) {
         const bool past = (F & kHistory) && r.hist_n > 0;
         if (s0 != begin) __syncthreads();
@@ -760,7 +831,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
           const int64_t e = element - first;
           if (e >= 0 && e < (s1 - s0) * G) atomicAnd(&bits[e >> 5], ~(1u << (e & 31)));
         };
-        if (past && s0 == begin) h = clear_hash<NT>(r, table);
+        if (past && s0 == begin) h = clear_hash<NT>(r, table, room.slots);
         __syncthreads();
         if (past) {
           if (s0 == begin) {
@@ -783,7 +854,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
             const float4* b = reinterpret_cast<const float4*>(r.bias + c0);
 #pragma unroll
             for (int j = 0; j < kEach; j += 4) {
-              const float4 x = __ldg(b + (j / G * NT * G + j % G) / 4);
+              const float4 x = ahead ? soon[ahead ? j / 4 : 0] : __ldg(b + (j / G * NT * G + j % G) / 4);
               v[j] = __fadd_rn(v[j], x.x);
               v[j + 1] = __fadd_rn(v[j + 1], x.y);
               v[j + 2] = __fadd_rn(v[j + 2], x.z);
@@ -796,6 +867,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
                 adjust_group<T, F & kBias>(r, g0 + u * NT + tid, nullptr, v + u * G);
           }
         }
+        if (ahead && r.a == 0 && g0 + CG < s1 && inside(g0 + CG)) fetch_bias(g0 + CG);
         if (F & (kMask | kHistory)) {
           const uint8_t* q = lane_bits + (g0 - s0) * G / 8;
 #pragma unroll
@@ -818,7 +890,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
         const unsigned pass = __ballot_sync(0xffffffffu, most >= least);
         if (pass) {
           const int at = notes + __popc(pass & ((1u << lane) - 1));
-          if (most >= least && at < kNotes) s.note[warp][at] = (uint32_t)(g0 + tid);
+          uint32_t groups = 0;  // of the piece that reach it
+#pragma unroll
+          for (int u = 0; u < NV; ++u) groups |= max_of<G>(v + u * G) >= least ? 1u << (28 + u) : 0u;
+          if (groups && at < room.notes) note[at] = groups | (uint32_t)(g0 + tid);
           notes += __popc(pass);
         }
       }
@@ -830,13 +905,13 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
         __syncwarp();
       }
       least = fmaxf(least, bound(s));
-      if (notes > kNotes && lane == 0) s.over = 1;
-      for (int i = lane; i < min(notes, kNotes); i += 32) {
-        const int p = (int)s.note[warp][i];  // the piece's first group
+      if (notes > room.notes && lane == 0) s.over = 1;
+      for (int i = lane; i < min(notes, room.notes); i += 32) {
+        const uint32_t piece = note[i], p = piece & 0xFFFFFFFu;  // the piece's first group
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-          const int g = p + u * NT;
-          if (g >= s1) break;
+          const int g = (int)p + u * NT;
+          if (!(piece >> (28 + u) & 1u)) continue;
           float v[G];
           load_group(r, g, v);
           if (F & kBias) adjust_group<T, F & kBias>(r, g, nullptr, v);
@@ -852,7 +927,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
     }
     if ((F & kHistory) && r.hist_n > 0) {
       // the tokens of the history, the logits of several on their way
-      constexpr int U = 4;
+      constexpr int U = 8;
       for (int i0 = tid; i0 < h.size; i0 += U * NT) {
         uint32_t slot[U];
         int id[U];
@@ -892,8 +967,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
     if (lane == 0) s.m[warp] = top_m, s.l[warp] = l;
   }
   __syncthreads();
-  if (quick && (s.over || s.found > kFew)) {
-    rising_row<NT, T, F>(s, r, begin, end, K, table, false, sum, status);
+  if (quick && (s.over || s.found > room.few)) {
+    rising_row<NT, T, F>(s, r, begin, end, K, table, room.slots, false, sum, status);
     quick = false;
   }
   if (lse && tid == NT - 1) {
@@ -909,7 +984,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
   }
   // the block's largest in order: few candidates, each one's place counted, four threads a candidate
   int n = quick ? s.found : pick(s, 0);
-  if (n > kFew) {
+  if (n > room.few) {
     const uint64_t t = kth_key(s, K);
     if (tid == 0) s.found = 0;
     __syncthreads();
@@ -921,30 +996,30 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
   };
   for (int i0 = 0; i0 < n; i0 += NT / 4) {
     const int i = i0 + tid / 4;
-    const uint64_t key = i < n ? s.few[i] : 0;
+    const uint64_t key = i < n ? few[i] : 0;
     int place = 0;
-    for (int o = tid & 3; o < n; o += 4) place += s.few[o] > key;
+    for (int o = tid & 3; o < n; o += 4) place += few[o] > key;
     place += __shfl_xor_sync(0xffffffffu, place, 1);
     place += __shfl_xor_sync(0xffffffffu, place, 2);
     if ((tid & 3) == 0 && i < n && place < K) {
       if (CL > 1)
-        s.best[place] = key;
+        best[place] = key;
       else
         answer(place, key);
     }
   }
   for (int k = n + tid; k < K; k += NT) {
     if (CL > 1)
-      s.best[k] = 0;
+      best[k] = 0;
     else
       answer(k, 0);
   }
   if (CL > 1) {
     cluster_sync();
     if (rank == 0) {
-      uint64_t* lists = reinterpret_cast<uint64_t*>(s.note);
+      uint64_t* lists = reinterpret_cast<uint64_t*>(top_smem + room.at_note);
       // the blocks' lists, each in order: a key's place is the number of larger ones in all lists
-      for (int i = tid; i < CL * K; i += NT) lists[i] = cluster_ld64(&s.best[i % K], i / K);
+      for (int i = tid; i < CL * K; i += NT) lists[i] = cluster_ld64(best + i % K, i / K);
       __syncthreads();
       for (int i = tid; i < CL * K; i += NT) {
         const uint64_t key = lists[i];
@@ -990,17 +1065,34 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
 }
 
 // ------------------------------------------------------------------------------ host
-template <typename T, int F, int W>
+template <typename T, int F>
 cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int64_t ldo, void* out,
                        int* status, cudaStream_t st) {
-  constexpr int G = Row<T, W>::G;
-  // runs of 8192 elements, longer ones where there are blocks enough (a history is read for each run)
+  constexpr int G = Row<T>::G;
+  const T* z = static_cast<const T*>(Z);
+  T* o = static_cast<T*>(out);
   const int64_t groups = ((int64_t)V + 2 * G - 2) / G;
+  const int lead = (int)(ldz % G);  // rows begin so much further on than the one before
+  int tokens = 0;
+  // (in place, the tokens' logits would be gone after the first launch)
+  if ((F & kBias) && lead && n >= 4 * kShare && !((F & kHistory) && out == Z)) {
+    constexpr int D = F & ~kHistory;
+    int step = 1;
+    while (lead * step % G) step *= 2;
+    const int64_t sets = (n + step * kShare - 1) / (step * kShare) * step;
+    const cudaError_t e =
+        launch_pdl(k_adjust_shared<T, D>, dim3((unsigned)sets, (unsigned)((groups * G + kRun - 1) / kRun)),
+                   dim3(kThreads), kRun * 4, st, n, V, ldz, z, adj, ldo, o, step, status);
+    if (e != cudaSuccess) return e;
+    note_launch();
+    if (!(F & kHistory)) return e;
+    tokens = 1;
+  }
+  // runs of 8192 elements; with histories, which are read for each run, longer ones where there are blocks enough
   int64_t per = 8192 / G;
-  while (per * G < kBits && n * ((groups + 2 * per - 1) / (2 * per)) >= 152 * 16) per *= 2;
-  const cudaError_t e =
-      launch_pdl(k_adjust<T, F, W>, dim3((unsigned)n, (unsigned)((groups + per - 1) / per)), dim3(kThreads), 0, st,
-                 V, ldz, static_cast<const T*>(Z), adj, ldo, static_cast<T*>(out), (int)per, status);
+  while ((F & kHistory) && per * G < 65536 && n * ((groups + 2 * per - 1) / (2 * per)) >= 152 * 16) per *= 2;
+  const cudaError_t e = launch_pdl(k_adjust<T, F>, dim3((unsigned)n, (unsigned)((groups + per - 1) / per)),
+                                   dim3(kThreads), 0, st, V, ldz, z, adj, ldo, o, (int)per, tokens, status);
   if (e == cudaSuccess) note_launch();
   return e;
 }
@@ -1015,14 +1107,14 @@ int cluster_of(int64_t n, int V) {
 template <int NT, typename T, int F>
 cudaError_t launch_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int K, int log_cl,
                        float* top_logit, int32_t* top_id, float* lse, int* status, cudaStream_t st) {
-  constexpr int smem = top_smem_bytes<NT, F>();
+  const Room room = room_of<NT>(F, V, K, n, adj.history_len, log_cl > 0);
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = allow_smem(k_top<NT, T, F>, smem, done);
+  cudaError_t e = allow_smem(k_top<NT, T, F>, 65536, done);  // (more than it takes)
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(n << log_cl));
   cfg.blockDim = dim3(NT);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = room.bytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1034,7 +1126,7 @@ cudaError_t launch_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjus
   cfg.attrs = attr;
   cfg.numAttrs = log_cl > 0 ? 2 : 1;
   e = cudaLaunchKernelEx(&cfg, k_top<NT, T, F>, V, ldz, static_cast<const T*>(Z), adj, K, log_cl, top_logit, top_id,
-                         lse, status);
+                         lse, room, status);
   if (e == cudaSuccess) note_launch();
   return e;
 }
@@ -1072,14 +1164,8 @@ cudaError_t logits_adjust(int bf16, int64_t n, int V, int64_t ldz, const void* Z
   const Adjust adj = make_adjust(b, V);
   return with_flags(flags_of(b), [&](auto f) {
     constexpr int F = decltype(f)::value;
-    // Rows that begin anywhere in 16 bytes meet the biases unaligned, a 16-byte group's G of them one by one and
-    // G apart in a warp; in groups of 4 bytes a warp's are side by side.
-    if constexpr (F & kBias)
-      if (ldz * (bf16 ? 2 : 4) % 16)
-        return bf16 ? run_adjust<__nv_bfloat16, F, 4>(n, V, ldz, Z, adj, ldo, out, status, st)
-                    : run_adjust<float, F, 4>(n, V, ldz, Z, adj, ldo, out, status, st);
-    return bf16 ? run_adjust<__nv_bfloat16, F, 16>(n, V, ldz, Z, adj, ldo, out, status, st)
-                : run_adjust<float, F, 16>(n, V, ldz, Z, adj, ldo, out, status, st);
+    return bf16 ? run_adjust<__nv_bfloat16, F>(n, V, ldz, Z, adj, ldo, out, status, st)
+                : run_adjust<float, F>(n, V, ldz, Z, adj, ldo, out, status, st);
   });
 }
 
