@@ -169,48 +169,60 @@ __global__ void __launch_bounds__(kWarps * 32) k_distill_rows(const __grid_const
   const float nlse = MODE == kCorrected ? -safe_lse(a.lse[i]) * kLog2e : 0.f, l2e = kLog2e * a.inv_tau;
   const bool rows = MODE != kBackward || a.dX;  // rows of W are needed
   float inner = 0.f;
-  constexpr int U = 4;  // rows of W on their way
+  // Four rows of W at a time: their products with x are added up over the row's threads so that thread t ends with
+  // the product of entry t mod 4, makes that entry's coefficient, and hands it to the others.
+  constexpr int U = 4;
   for (int k0 = 0; k0 < a.K; k0 += U * groups) {
     float w[U][8];
-    Entry en[U];
+    bool there[U];
 #pragma unroll
     for (int s = 0; s < U; ++s) {
-      const int k = k0 + s * groups + group;
-      en[s] = k < a.K ? e[k] : Entry{-1, 0.f, 0.f};
+      const int k = k0 + s * groups + group, t = k < a.K ? e[k].id : -1;
+      there[s] = t >= 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[s][j] = 0.f;
-      if (rows && en[s].id >= 0 && in) load8(static_cast<const T*>(a.W) + (int64_t)en[s].id * a.H + at, w[s]);
+      if (rows && t >= 0 && in) load8(static_cast<const T*>(a.W) + (int64_t)t * a.H + at, w[s]);
     }
+    const int mine = k0 + (lane & 3) * groups + group;
+    const Entry en = mine < a.K ? e[mine] : Entry{-1, 0.f, 0.f};
+    float z = 0.f;
+    if (MODE != kBackward) {
+      float p[U];
+#pragma unroll
+      for (int s = 0; s < U; ++s) {
+        p[s] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[s] = fmaf(x[j], w[s][j], p[s]);
+      }
+      const bool odd = lane & 1, high = lane & 2;
+      const float x01 = (odd ? p[1] : p[0]) + __shfl_xor_sync(0xffffffffu, odd ? p[0] : p[1], 1);
+      const float x23 = (odd ? p[3] : p[2]) + __shfl_xor_sync(0xffffffffu, odd ? p[2] : p[3], 1);
+      z = (high ? x23 : x01) + __shfl_xor_sync(0xffffffffu, high ? x01 : x23, 2);
+      for (int o = 4; o < a.width; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+    }
+    if (MODE == kForward) {
+      if (q0 < U && en.id >= 0) inner += en.q * (en.other - z * a.inv_tau);
+      continue;
+    }
+    float cx = -en.q, cw = -g * en.q;
+    if (MODE == kCorrected && en.other != 0.f) {
+      // the dense kernels' P: bf16(p) for dX, bf16(g p) for dW
+      const float p = ex2(fmaf(z, l2e, nlse)), gp = p * g;
+      cx += p - __bfloat162float(__float2bfloat16(p));
+      cw += gp - __bfloat162float(__float2bfloat16(gp));
+    }
+    if (q0 < U && mine < a.K && a.id) {
+      a.id[i * a.K + mine] = en.id;
+      a.c[i * a.K + mine] = cw;
+    }
+    if (!rows) continue;
 #pragma unroll
     for (int s = 0; s < U; ++s) {
-      const int k = k0 + s * groups + group;
-      float z = 0.f;
-      if (MODE != kBackward) {
+      const float c = __shfl_sync(0xffffffffu, cx, (lane & ~3) | s);
+      if (there[s]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z = fmaf(x[j], w[s][j], z);
-        for (int o = a.width / 2; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(c, w[s][j], acc[j]);
       }
-      if (MODE == kForward) {
-        if (q0 == 0 && en[s].id >= 0) inner += en[s].q * (en[s].other - z * a.inv_tau);
-        continue;
-      }
-      if (en[s].id < 0) {
-        if (q0 == 0 && k < a.K && a.id) a.id[i * a.K + k] = -1;
-        continue;
-      }
-      float cx = -en[s].q, cw = -g * en[s].q;
-      if (MODE == kCorrected && en[s].other != 0.f) {
-        // the dense kernels' P: bf16(p) for dX, bf16(g p) for dW
-        const float p = ex2(fmaf(z, l2e, nlse)), gp = p * g;
-        cx += p - __bfloat162float(__float2bfloat16(p));
-        cw += gp - __bfloat162float(__float2bfloat16(gp));
-      }
-      if (q0 == 0 && a.id) {
-        a.id[i * a.K + k] = en[s].id;
-        a.c[i * a.K + k] = cw;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = fmaf(cx, w[s][j], acc[j]);
     }
   }
   if (MODE == kForward) {

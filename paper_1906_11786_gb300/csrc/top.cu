@@ -305,8 +305,9 @@ __device__ __forceinline__ void adjust_run(const Row<T>& r, T* o, bool in_place,
                                            const float* staged, uint32_t* table, float* raw, int* status) {
   constexpr int G = Row<T>::G;
   const bool vec = (reinterpret_cast<uintptr_t>(o - r.a) & 15) == 0;
-  if ((F & kHistory) && !hashed(r, kSlots)) {
-    constexpr int SG = kSlots / G;
+  // (short runs, of a few rows: occurrences by element are the shorter way)
+  constexpr int SG = kSlots / G;
+  if ((F & kHistory) && r.hist_n > 0 && (!hashed(r, kSlots) || (!tokens && g1 - g0 <= SG))) {
     for (int64_t s0 = g0; s0 < g1; s0 += SG) {
       count_history<kThreads>(r, s0 * G, kSlots, table, status);
       for (int64_t g = s0 + threadIdx.x; g < min(g1, s0 + SG); g += kThreads) {
@@ -1088,8 +1089,10 @@ cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjus
     if (!(F & kHistory)) return e;
     tokens = 1;
   }
-  // runs of 8192 elements; with histories, which are read for each run, longer ones where there are blocks enough
+  // runs of 8192 elements; with histories, which are read for each run, longer ones where there are blocks enough, and
+  // shorter ones where there are few
   int64_t per = 8192 / G;
+  if ((F & kHistory) && n * V <= 152 * 8 * kSlots) per = kSlots / G;
   while ((F & kHistory) && per * G < 65536 && n * ((groups + 2 * per - 1) / (2 * per)) >= 152 * 16) per *= 2;
   const cudaError_t e = launch_pdl(k_adjust<T, F>, dim3((unsigned)n, (unsigned)((groups + per - 1) / per)),
                                    dim3(kThreads), 0, st, V, ldz, z, adj, ldo, o, (int)per, tokens, status);
