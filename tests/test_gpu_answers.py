@@ -136,6 +136,49 @@ def test_logits_of_rows_that_are_not_finite_stay_theirs(dtype):
     assert np.array_equal(np.isfinite(host(Z)), ~bad)
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("pad", [0, 1, 8])
+def test_logits_and_their_readers_from_the_middle_of_a_sector(out, pad):
+    """Pointers are aligned to 16 bytes, not to the 32 of a sector."""
+    n, H, V = 70, 64, 900
+    rng = np.random.default_rng(0)
+    X, W = dev(rng.standard_normal((n, H)), "bf16"), dev(rng.standard_normal((V, H)) * 0.3, "bf16")
+    lead = 16 // TD[out].itemsize
+    buf = torch.full((lead + n * (V + pad),), 7.0, device="cuda", dtype=TD[out])
+    Z = buf[lead:].view(n, V + pad)[:, :V]
+    assert Z.data_ptr() % 32 == 16
+    L.logits_fwd("bf16", X, W, out, Z)
+    want = host(X) @ host(W).T
+    tol = logits_tolerance(host(X), host(W), "bf16", out)
+    within(host(Z), want, tol * 1.01 + HALF * 1.01 * np.abs(want) if out == "bf16" else tol)
+    assert bool((buf[:lead] == 7.0).all())
+    kw, adjust = constraints(n, V, 3)
+    adj = ref.adjusted(host(Z), **kw)
+    check_top(Z, 17, out, adjust, adj)
+    L.logits_adjust(out, Z, Z, adjust)
+    assert np.array_equal(bits(Z), bits(torch.from_numpy(adj).to(TD[out]).cuda()))
+    assert bool((buf[:lead] == 7.0).all())
+
+
+def test_logits_past_32_bits_of_elements():
+    """86001 x 50001 logits (4.3 10^9); rows all along, and the tokens at both ends, against 64 bits."""
+    n, H, V = 86001, 32, 50001
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    X, W = (torch.randn(m, H, device="cuda", generator=gen).to(torch.bfloat16) for m in (n, V))
+    Z = torch.empty(n, V, device="cuda", dtype=torch.bfloat16)
+    L.logits_fwd("bf16", X, W, "bf16", Z)
+    L.check_device()
+    for i in list(range(0, n, 9001)) + [n - 2, n - 1, 42949, 42950]:
+        want = host(X[i:i + 1]) @ host(W).T
+        tol = logits_tolerance(host(X[i:i + 1]), host(W), "bf16", "bf16")
+        within(host(Z[i:i + 1]), want, tol * 1.01 + HALF * 1.01 * np.abs(want))
+    top = torch.empty(n, 3, device="cuda")
+    ids = torch.empty(n, 3, device="cuda", dtype=torch.int32)
+    L.logits_top("bf16", Z, top, ids)
+    assert torch.equal(top.max(1).values, Z.max(1).values.float())
+    assert torch.equal(Z.gather(1, ids.long()).float(), top)
+
+
 # ------------------------------------------------------------------------------ adjustment
 
 
@@ -479,7 +522,7 @@ TYPES = [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")]
 
 @pytest.mark.parametrize("dtype,grad", TYPES)
 @pytest.mark.parametrize("n,H,V,K,tau,share", [
-    (1, 32, 2, 1, 1.0, 1.0), (1, 128, 4001, 5, 2.0, 1.0), (2, 64, 1000, 128, 0.5, 1.0),
+    (1, 32, 2, 1, 1.0, 1.0), (3, 32, 1, 2, 1.0, 1.0), (1, 128, 4001, 5, 2.0, 1.0), (2, 64, 1000, 128, 0.5, 1.0),
     (7, 96, 65, 33, 1.0, 1.0), (127, 160, 127, 2, 3.5, 0.5), (128, 256, 128, 31, 1.0, 1.0),
     (129, 192, 257, 32, 2.0, 0.7), (300, 224, 513, 64, 1.0, 0.15), (513, 256, 1023, 16, 4.0, 1.0),
     (1000, 32, 3001, 8, 1.0, 1.0), (2500, 64, 400, 100, 2.0, 0.3), (4097, 128, 130, 4, 1.0, 1.0),
@@ -732,6 +775,58 @@ def test_a_student_learns_from_a_teachers_answers_on_its_stream_and_in_a_graph()
     torch.cuda.synchronize()
     for a, b in zip(again[:9], bufs[:9]):
         assert np.array_equal(bits(a), bits(b)) if a.dtype != torch.int32 else torch.equal(a, b)
+
+
+def test_graphs_that_share_a_workspace_replay_one_after_the_other():
+    """Two captured training steps over one workspace, replayed in turn: nothing in it outlives a call."""
+    n, H, V, K = 500, 64, 700, 10
+    steps = []
+    ws = distill_ws("bf16", n, H, V, K)
+    for seed in (1, 2):
+        X, W, ids, logits, g = distill_inputs(n, H, V, K, "bf16", 0.8, seed)
+        want = run_distill("bf16", X, W, ids, logits, g, 2.0, "f32")
+        outs = [torch.zeros_like(t) for t in want]
+        args = (ints(ids), dev(logits))
+        gd = dev(g)
+
+        def step(X=X, W=W, args=args, gd=gd, outs=outs):
+            L.distill_fwd("bf16", X, W, *args, outs[0], outs[1], ws, tau=2.0)
+            L.distill_bwd("bf16", X, W, *args, outs[1], gd, "f32", outs[2], outs[3], ws, tau=2.0)
+
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        steps.append((graph, outs, want, step))  # (step: what the graph reads stays where it is)
+    for k in (0, 1, 1, 0, 1, 0):
+        for t in steps[k][1]:
+            t.zero_()
+        steps[k][0].replay()
+        torch.cuda.synchronize()
+        for a, b in zip(steps[k][1], steps[k][2]):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_top_and_adjust_give_the_same_bits_again(dtype):
+    """Blocks raise their bounds as they find each other's: what is done differs from run to run, its result does
+    not (lse included: each thread's sum, and the order in which they are joined, are fixed)."""
+    n, V, K = 700, 20001, 40
+    rng = np.random.default_rng(11)
+    z = dev(np.round(rng.standard_normal((n, V)) * 8) / 4, dtype)  # ties
+    kw, adjust = constraints(n, V, 3)
+    first = None
+    for _ in range(6):
+        got = [torch.empty(n, K, device="cuda"), torch.empty(n, K, device="cuda", dtype=torch.int32)]
+        L.logits_top(dtype, z, got[0], got[1], None, adjust)
+        out = torch.empty_like(z)
+        L.logits_adjust(dtype, z, out, adjust)
+        got.append(torch.nan_to_num(out, nan=1.0))
+        if first is None:
+            first = got
+        for a, b in zip(got, first):
+            assert torch.equal(a, b)
+    assert np.array_equal(first[1].cpu().numpy(), ref.top(ref.adjusted(host(z), **kw), K)[1])
 
 
 FIRST_CALLS = """
