@@ -13,6 +13,11 @@
 // gradient's own rounding; so c_k also holds what that rounding took from the entry's own P (whose z is a
 // product of H terms, computed again): the entries' coefficients P - Q are exact to fp32, and only tokens
 // without an entry, whose whole coefficient is P, have it rounded.
+//
+// 65537 rows x 49999 x 256 bf16 with 32 entries: 5.8 ms forward and backward, of which the dense products take 4.6-4.9
+// (xent.cu), the rows 0.12 and 0.19 (1.07 GB each from L2: 8.8 TB/s forward; backward also two more passes over the
+// registers), the sort of 2.1 M entries 0.14 and their sums 0.31.  15% of 71969 rows x 10000 x 64, 16 entries, fp32
+// gradients: 328 us, a chain of fifteen kernels.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -10,8 +10,17 @@
 //
 // Rows are read once, as the aligned 16-byte groups that cover them: a row may begin anywhere in a group
 // (odd row lengths), so column c of a row is element c + a of its groups, a its first element's place in the
-// first one.  Occurrences are counted in shared memory, a few thousand columns at a time, by reading the
-// row's history once for each segment: no sorting and no workspace.
+// first one.  The tokens of a history are counted in a hash table in shared memory (long ones by element, a few
+// thousand elements at a time, the history read once for each such segment): no sorting and no workspace.
+//
+// Measured (GB300; reading at the copy rate of 6.77 TB/s is the floor, beside the writing of the adjustment):
+//   adjustment of 8192 x 50000 bf16: 260 us (floor 243, 6.3 TB/s); biases 271, masks 285, histories of 0 to 512 tokens
+//     345, all three 444; with rows of 49999, which begin anywhere, 264, 340, 288, 347 and 470.  fp32: 506 (6.5 TB/s),
+//     508, 516, 603, 676.  What histories add is scattered: a sector read and one written in part for each token.
+//   top 32 of 16383 x 50000 bf16: 370 us (floor 243), biases 458, masks 455, histories 527, all three 729; fp32 536
+//     (6.1 TB/s; floor 485), 604, 572, 704, 879; top 1 305, top 128 675.  bf16 rows are bound by instructions and by
+//     the latency of what comes one after the other in a row (issue slots 64%, fp32's unpacked rows hide it): 80
+//     instructions a warp for 512 logits, 44 for the sum of exponentials, 37 for the biases, 55 for the bits.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -31,7 +40,7 @@ namespace {
 
 constexpr int kThreads = 256;     // of a block of the adjustment
 constexpr int kSlots = 2048;      // of a hash table of a history's tokens, at most
-constexpr int kEach = 16;       // elements of a thread at a time
+constexpr int kEach = 16;         // elements of a thread at a time
 
 // What an adjustment has (template flags): one without any costs nothing.
 enum { kBias = 1, kMask = 2, kHistory = 4 };
@@ -330,9 +339,7 @@ __device__ __forceinline__ void adjust_run(const Row<T>& r, T* o, bool in_place,
     if (in_place) __syncthreads();
   }
   if (!tokens && ((F & (kBias | kMask)) || !in_place)) {
-    for (int64_t g = g0 + threadIdx.x; g < g1; g += kThreads) {
-      float v[G];
-      load_group(r, g, v);
+    auto finish = [&](int64_t g, float* v) {
       if ((F & kBias) && staged) {
 #pragma unroll
         for (int j = 0; j < G; j += 4) {
@@ -347,6 +354,11 @@ __device__ __forceinline__ void adjust_run(const Row<T>& r, T* o, bool in_place,
         adjust_group<T, F & ~kHistory>(r, g, nullptr, v);
       }
       store_row_group(r, o, vec, g, v);
+    };
+    for (int64_t g = g0 + threadIdx.x; g < g1; g += kThreads) {
+      float v[G];
+      load_group(r, g, v);
+      finish(g, v);
     }
   }
   if ((F & kHistory) && r.hist_n > 0) {
@@ -393,15 +405,20 @@ __global__ void __launch_bounds__(kThreads)
   tc::grid_dep_wait();
   const int64_t first = (int64_t)(blockIdx.x / step) * step * kShare + blockIdx.x % step;
   const int64_t g0 = (int64_t)blockIdx.y * per;
+  // (what a row's own part of the adjustment is comes while the row before it is worked on)
+  Row<T> next = make_row<T, F>(Z, ldz, min(first, n - 1), V, adj, status);
   for (int k = 0; k < kShare; ++k) {
     const int64_t i = first + (int64_t)k * step;
     if (i >= n) break;
-    const Row<T> r = make_row<T, F>(Z, ldz, i, V, adj, status);
+    const Row<T> r = next;
+    if (k + 1 < kShare && i + step < n) next = make_row<T, F>(Z, ldz, i + step, V, adj, status);
     const int64_t g1 = min((int64_t)r.groups(), g0 + per);
     if (g0 >= g1) break;
     if (k == 0) {
-      for (int e = threadIdx.x; e < (g1 - g0) * G; e += kThreads) {
-        const int64_t c = g0 * G + e - r.a;
+      const int c0 = (int)(g0 * G) - r.a;
+#pragma unroll 8
+      for (int e = threadIdx.x; e < kRun; e += kThreads) {
+        const int c = c0 + e;
         staged[e] = c >= 0 && c < V ? __ldg(adj.bias + c) : 0.f;
       }
     }
@@ -420,6 +437,11 @@ __global__ void __launch_bounds__(kThreads)
 // of the time, were a third of the kernel's instructions.)  Where pieces or candidates outgrow their room (ties
 // without end, rows that rise), the block goes over the row again with exact bounds (rising_row, some times
 // slower).
+//
+// A block is a row's, of 128 threads where there are rows enough, eight blocks an SM: what one waits for (the
+// history's offsets, its tokens, their logits; barriers) is hidden by the others (top 32 of 16383 x 50000 bf16 425 us
+// with four blocks of 256 threads, 370 with eight of 128).  With few rows it has 512, and up to eight blocks of a
+// cluster share a row, whose lists the first one joins.
 //
 // Masks and histories come as bits in shared memory, kBits elements at a time: a cleared bit leaves an element
 // out.  The tokens of a history are cleared too, counted in a hash table, and added one by one after the
