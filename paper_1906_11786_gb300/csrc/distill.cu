@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_distill_rows(const __grid_const
     if (t >= a.V && atomicCAS(a.status, 0, 2) == 0) atomicExch(a.status + 1, kSiteTeacherId);
     if (t < 0 || t >= a.V || x == -INFINITY) continue;
     id[j] = t;
-    u[j] = x * a.inv_tau;
+    u[j] = x;
     some = true;
     high = fmaxf(high, u[j]);
   }
@@ -143,14 +143,18 @@ __global__ void __launch_bounds__(kWarps * 32) k_distill_rows(const __grid_const
   }
   high = warp_max(high);
   float sum = 0.f;
+  // (the largest is taken off before tau divides: the type's lowest value stays an entry, with q = 0 beside larger ones)
 #pragma unroll
-  for (int j = 0; j < E; ++j) sum += id[j] < 0 ? 0.f : expf(u[j] - high);
+  for (int j = 0; j < E; ++j) {
+    u[j] = (u[j] - high) * a.inv_tau;
+    sum += id[j] < 0 ? 0.f : expf(u[j]);
+  }
   sum = warp_sum(sum);
   const float log_sum = logf(sum), inv = 1.f / sum;
 #pragma unroll
   for (int j = 0; j < E; ++j) {
     const int k = j * 32 + lane;
-    if (k < a.K) e[k] = Entry{id[j], id[j] < 0 ? 0.f : expf(u[j] - high) * inv, u[j] - high - log_sum};
+    if (k < a.K) e[k] = Entry{id[j], id[j] < 0 ? 0.f : expf(u[j]) * inv, u[j] - log_sum};
   }
   __syncwarp();
   if (MODE == kCorrected) {
@@ -206,7 +210,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_distill_rows(const __grid_const
       for (int o = 4; o < a.width; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
     }
     if (MODE == kForward) {
-      if (q0 < U && en.id >= 0) inner += en.q * (en.other - z * a.inv_tau);
+      if (q0 < U && en.id >= 0 && en.q != 0.f) inner += en.q * (en.other - z * a.inv_tau);
       continue;
     }
     float cx = -en.q, cw = -g * en.q;

@@ -612,6 +612,28 @@ def test_distill_rows_left_out_may_hold_anything(dtype, grad):
 
 
 @pytest.mark.parametrize("dtype,grad", TYPES)
+def test_distill_of_entries_of_the_lowest_value(dtype, grad):
+    """Beside larger entries the lowest value has q = 0, as an entry that is none; a row of nothing else is one of
+    equal logits.  At tau < 1 their quotients by tau pass the type's range."""
+    n, H, V, K, tau = 300, 64, 200, 6, 0.5
+    X, W, ids, logits, g = distill_inputs(n, H, V, K, dtype)
+    rng = np.random.default_rng(4)
+    low = rng.random((n, K)) < 0.4
+    low[:, 0] &= ids[:, 1] < 0
+    low[50:60] = True
+    logits[50:60] = np.where(np.isinf(logits[50:60]), -np.inf, 0.0)
+    mixed = ((ids >= 0) & ~np.isinf(logits) & ~low).any(1)
+    same = np.where(low & mixed[:, None], -1, ids).astype(np.int32)
+    equal = np.where(low & ~mixed[:, None] & ~np.isinf(logits), 0.0, logits).astype(np.float32)
+    lowest = np.where(low & ~np.isinf(logits), np.finfo(np.float32).min, logits).astype(np.float32)
+    r = ref.distill(host(X), host(W), same, equal, tau, g)
+    assert r["rows"][50:60].any() and (low & mixed[:, None] & (ids >= 0)).any()
+    for a, k, tol in zip(run_distill(dtype, X, W, ids, lowest, g, tau, grad), ("loss", "lse", "dX", "dW"),
+                         distill_bounds(r, n, H, V, K, tau, grad)):
+        within(host(a), r[k], tol)
+
+
+@pytest.mark.parametrize("dtype,grad", TYPES)
 def test_distill_with_no_row_left(dtype, grad):
     X, W, ids, logits, g = distill_inputs(150, 64, 300, 5, dtype, 0.0)
     ids[:] = -1
