@@ -23,7 +23,7 @@
  *     [32, 256]; P (edge types) in [1, 64].
  *   - dtype BG_BF16: states E, weights W, W_ih, W_hh are bf16 and accumulation is fp32.
  *     dtype BG_F32: all fp32.  Biases, messages Y and every gradient are fp32 for both dtypes
- *     (bg_xent_bwd can also write bf16 gradients).
+ *     (bg_xent_bwd and bg_distill_bwd can also write bf16 gradients).
  */
 #ifndef BANDGGNN_H_
 #define BANDGGNN_H_
