@@ -901,7 +901,8 @@ __global__ void __launch_bounds__(NT, (NT > 128 ? 2 : !(F & kBias) ? 8 : sizeof(
               if (!(b & 1u << j)) v[u * G + j] = -INFINITY;
           }
         }
-        const float most = max_of<kEach>(v);
+        // (a piece of nothing but NaN has no largest: as NaN it would make `second` the lane's own `top` again)
+        const float most = fmaxf(max_of<kEach>(v), -INFINITY);
         if (lse) sum.add<kEach>(v, most);
         second = fmaxf(second, fminf(top, most));
         top = fmaxf(top, most);

@@ -378,6 +378,25 @@ def test_top_of_rows_made_to_be_hard(kind, n):
         check_top(dev(z), K, "f32", None, z)
 
 
+@pytest.mark.parametrize("dtype,pad", [("f32", 0), ("bf16", 1)])
+@pytest.mark.parametrize("n,V", [(640, 4096), (310, 16384), (2, 32001)])
+@pytest.mark.parametrize("where", ["second half", "first half", "an eighth", "all but a few", "every other run"])
+def test_top_of_rows_with_runs_of_nan(where, n, V, dtype, pad):
+    """Whole pieces, chunks and a cluster block's share of NaN are no answers and leave the others theirs: blocks of
+    128 threads, of 512, and clusters of them."""
+    v = np.arange(V)
+    rng = np.random.default_rng(V)
+    nan = {"second half": v >= V // 2, "first half": v < V // 2, "an eighth": v * 8 // V == 2,
+           "all but a few": rng.random(V) < 1 - 200 / V, "every other run": v // 512 % 2 == 0}[where]
+    z = np.where(nan[None], np.nan, rng.standard_normal((n, V)) * 3)
+    Z, _ = rows(n, V, pad, dtype)
+    Z.copy_(dev(z, dtype))
+    for K in (5, 32, 128):
+        check_top(Z, K, dtype, None, host(Z).astype(np.float32))
+    kw, adjust = constraints(n, V, 7)
+    check_top(Z, 32, dtype, adjust, ref.adjusted(host(Z), **kw))
+
+
 def test_top_from_rows_beyond_32_bit_offsets():
     """Rows at element offsets past 2^32, in a buffer of which only they are used."""
     n, V, ld = 3, 700, (1 << 31) - 8
