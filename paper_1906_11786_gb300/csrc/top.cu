@@ -237,17 +237,29 @@ __device__ __forceinline__ bool hashed(const R& r, int slots) {
   return r.hist_n <= slots / 4 * 3 && r.V < 1 << 21;
 }
 
-__device__ __forceinline__ void hash_add(const Hash& h, uint32_t id) {
-  const uint32_t mask = (1u << h.low) - 1;
-  uint32_t at = (id * 2654435761u) >> 7 & (h.size - 1);
+// A token's place: a slot keeps the largest of the tokens that come to it and sends the smaller one on to the next.
+// So where each ends up depends on which tokens there are and not on which came first, and with it the order in which
+// their exponentials are added.  (By the order of arrival, lse differed in its last bits from run to run.)
+__device__ __forceinline__ uint32_t hash_home(const Hash& h, uint32_t id) {
+  return (id * 2654435761u) >> 7 & (h.size - 1);
+}
+__device__ __forceinline__ void hash_insert(const Hash& h, uint32_t id) {
+  uint32_t at = hash_home(h, id), key = id + 1;
   for (int k = 0; k < h.size; ++k, at = (at + 1) & (h.size - 1)) {  // (a quarter of the slots stays empty)
-    const uint32_t was = atomicCAS(&h.slot[at], 0u, 1u << h.low | (id + 1));
-    if (was == 0) return;
-    if ((was & mask) == id + 1) {
+    const uint32_t was = atomicMax(&h.slot[at], key);
+    if (was == 0 || was == key) return;
+    key = min(key, was);
+  }
+}
+// One more of a token that is there; all are, behind a barrier.
+__device__ __forceinline__ void hash_count(const Hash& h, uint32_t id) {
+  const uint32_t mask = (1u << h.low) - 1;
+  uint32_t at = hash_home(h, id);
+  for (int k = 0; k < h.size; ++k, at = (at + 1) & (h.size - 1))
+    if ((h.slot[at] & mask) == id + 1) {
       atomicAdd(&h.slot[at], 1u << h.low);
       return;
     }
-  }
 }
 
 // An empty table for the tokens of r's history (a barrier has to follow before it is filled).
@@ -258,25 +270,37 @@ __device__ __forceinline__ Hash clear_hash(const Row<T>& r, uint32_t* table, int
   for (int i = threadIdx.x; i < h.size / 4; i += NT) reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
   return h;
 }
-// Adds the tokens whose elements (column + a) are in [first, last), calling seen(element) for each (a barrier has
-// to follow before the table is read).
-template <int NT, typename T, typename Fn>
+// Adds the tokens whose elements (column + a) are in [first, last), calling seen(element) for each; the whole block
+// calls it (a barrier has to follow before the table is read).  Two passes over the history, the second from the L1
+// cache: counts can be added once no token moves any more.  U tokens of a thread are on their way in the first: one
+// for the largest logits, whose kernel is bound by its code's length (top 32 of 16383 x 49999 bf16, all constraints
+// and up to 512 tokens: 754 us, 773 with four), four for the adjustment (8192 x 49999 bf16, all constraints and up to
+// 1024 tokens: 477 us, 493 with one).
+template <int NT, int U, typename T, typename Fn>
 __device__ __forceinline__ void fill_hash(const Hash& h, const Row<T>& r, int64_t first, int64_t last, int* status,
                                           Fn seen) {
-  constexpr int U = 4;  // tokens on their way
-  for (int i0 = threadIdx.x; i0 < (int)r.hist_n; i0 += U * NT) {
+  const int n = (int)r.hist_n;
+  const uint32_t lo = (uint32_t)max((int64_t)0, first - r.a);
+  const uint32_t span = (uint32_t)min((int64_t)r.V, last - r.a) - lo;
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < n; i0 += U * NT) {
     int id[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) id[u] = i0 + u * NT < (int)r.hist_n ? r.hist[i0 + u * NT] : -1;
+    for (int u = 0; u < U; ++u) id[u] = u == 0 || i0 + u * NT < n ? r.hist[i0 + u * NT] : -1;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (id[u] >= r.V) report(status, kSiteHistoryId);
-      const int64_t e = (int64_t)id[u] + r.a;
-      if (id[u] >= 0 && id[u] < r.V && e >= first && e < last) {
-        hash_add(h, (uint32_t)id[u]);
-        seen(e);
+      if ((uint32_t)id[u] - lo < span) {
+        hash_insert(h, (uint32_t)id[u]);
+        seen(id[u] + r.a);
       }
     }
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const int id = r.hist[i];
+    if ((uint32_t)id - lo < span) hash_count(h, (uint32_t)id);
   }
 }
 
@@ -332,7 +356,7 @@ __device__ __forceinline__ void adjust_run(const Row<T>& r, T* o, bool in_place,
   if ((F & kHistory) && r.hist_n > 0) {
     h = clear_hash<kThreads>(r, table, kSlots);
     __syncthreads();
-    fill_hash<kThreads>(h, r, g0 * G, g1 * G, status, [](int64_t) {});
+    fill_hash<kThreads, 4>(h, r, g0 * G, g1 * G, status, [](int64_t) {});
     __syncthreads();
     for (int k = threadIdx.x; k < h.size; k += kThreads)
       if (const uint32_t x = h.slot[k]) raw[k] = to_f32(r.base[h.token(x) + r.a]);
@@ -858,7 +882,7 @@ __global__ void __launch_bounds__(NT, (NT > 128 ? 2 : !(F & kBias) ? 8 : sizeof(
         __syncthreads();
         if (past) {
           if (s0 == begin) {
-            fill_hash<NT>(h, r, begin * G, end * G, status, leave_out);
+            fill_hash<NT, 1>(h, r, begin * G, end * G, status, leave_out);
           } else {
             for (int i = tid; i < h.size; i += NT)
               if (const uint32_t x = h.slot[i]) leave_out(h.token(x) + r.a);

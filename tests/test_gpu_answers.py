@@ -870,6 +870,28 @@ def test_top_and_adjust_give_the_same_bits_again(dtype):
     assert np.array_equal(first[1].cpu().numpy(), ref.top(ref.adjusted(host(z), **kw), K)[1])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 300, 700])
+def test_lse_of_rows_with_dense_histories_has_the_same_bits_again(n, dtype):
+    """Tables half full and more, whose tokens make most of the sum: the order in which their exponentials are added
+    is that of the tokens' places, which must not depend on which thread came first."""
+    V, K = 20001, 5
+    rng = np.random.default_rng(n)
+    z = dev(rng.standard_normal((n, V)), dtype)
+    history = [rng.integers(0, V, m) for m in rng.integers(900, 1500, n)]
+    penalty = np.tile(np.array([[0.5, -6.0, -0.5]], np.float32), (n, 1))
+    off = np.concatenate([[0], np.cumsum([len(h) for h in history])])
+    adjust = L.LogitAdjust(history=ints(np.concatenate(history)), history_off=ints(off, np.int64), penalty=dev(penalty))
+    check_top(z, K, dtype, adjust, ref.adjusted(host(z), history=history, penalty=penalty))
+    vals, ids = torch.empty(n, K, device="cuda"), torch.empty(n, K, device="cuda", dtype=torch.int32)
+    first = None
+    for _ in range(20):
+        lse = torch.full((n,), float("nan"), device="cuda")
+        L.logits_top(dtype, z, vals, ids, lse, adjust)
+        first = lse if first is None else first
+        assert torch.equal(lse, first)
+
+
 FIRST_CALLS = """
 import torch
 from paper_1906_11786_gb300 import lib as L
