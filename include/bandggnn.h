@@ -394,8 +394,9 @@ int bg_xent_bwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, 
  *
  * bg_logits_fwd: Z[i][v] = X[i] . W[v].  X [n, H] and W [V, H] dtype, Z [n] rows of out_dtype.  bf16 X and W
  * enter as they are; fp32 ones of more than 4 rows with 22 bits, down to 2^-17 of the largest magnitude in their
- * row, smaller elements are off by up to 2^-39 of that magnitude.  A row of X or W that is not finite makes its own logits
- * NaN and no others.  ws may be NULL where bg_logits_workspace_bytes is 0 (bf16, and up to 4 rows). */
+ * row, smaller elements are off by up to 2^-39 of that magnitude.  A row of X or W with an element that is infinite or
+ * NaN makes its own logits not finite and no others: NaN with fp32 X and W, what their products and sum are with bf16
+ * ones (an infinite element may make them infinite).  ws may be NULL where bg_logits_workspace_bytes is 0 (bf16, and up to 4 rows). */
 size_t bg_logits_workspace_bytes(bg_dtype dtype, int64_t n, int32_t H, int32_t V);
 int bg_logits_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
                   bg_dtype out_dtype, int64_t ldz, void* Z, void* ws, size_t ws_bytes, void* stream);

@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(256) k_logits_split(SplitArgs a) {
 }
 
 // A few rows of X in fp32, without terms: a row of W is `width` threads of 8 elements (H / 8 rounded up to a power
-// of two), read once for all of them, and what bounds it.  One row x 32000 x 128: 15 us with the terms' pass over
-// W, 7 without (16 rows: 15 with it, 37 without).
+// of two), read once for all of them, and what bounds it.  32000 x 128: 4 rows 9 us without terms, 5 rows 15 with
+// their pass over W (49999 x 256: 22 and 36, 4001 x 64: 6 and 8; one row 6, 10 and 6).
 constexpr int kFew = 4;
 template <typename O>
 __global__ void __launch_bounds__(256)
@@ -156,6 +156,20 @@ __global__ void __launch_bounds__(256)
       for (int j = 0; j < 8; ++j) z = fmaf(x[r][j], w[j], z);
       for (int o = width / 2; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
       if (lane == r) mine = z;  // (four threads at least)
+    }
+    // An infinite element makes a logit NaN, as the terms do (of an infinite one the second is NaN): which kernel a
+    // number of rows takes is not seen in its logits.  (Finite elements whose sum overflows stay infinite there too.)
+    if (__any_sync(0xffffffffu, !(fabsf(mine) < INFINITY))) {
+      unsigned bad = 0;  // bit r: row r of X with this row of W
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (!(fabsf(w[j]) < INFINITY)) bad = ~0u;
+#pragma unroll
+        for (int r = 0; r < kFew; ++r)
+          if (!(fabsf(x[r][j]) < INFINITY)) bad |= 1u << r;
+      }
+      for (int o = width / 2; o; o >>= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+      if (lane < kFew && (bad >> lane & 1u)) mine = NAN;
     }
     if (lane < n && v < V) Z[lane * ldz + v] = (O)mine;
   }

@@ -136,6 +136,34 @@ def test_logits_of_rows_that_are_not_finite_stay_theirs(dtype):
     assert np.array_equal(np.isfinite(host(Z)), ~bad)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 3, 4, 5, 40])
+@pytest.mark.parametrize("H", [32, 96, 160, 256])
+def test_logits_of_infinite_elements_do_not_depend_on_the_number_of_rows(H, n, dtype):
+    """fp32: NaN; bf16: what products and sum are; and infinite where finite elements' sum overflows."""
+    V = 300
+    rng = np.random.default_rng(H + n)
+    X, W = rng.standard_normal((n, H)), rng.standard_normal((V, H))
+    X[n - 1, H - 1] = np.inf
+    W[17, 9], W[33, 1], W[40, :], W[299, 0] = -np.inf, np.nan, 0.0, np.inf
+    if n > 1:
+        X[0, :], W[5, :], W[6, :] = 2.0 ** 100, 2.0 ** 100, -2.0 ** 100
+    Z, _ = rows(n, V, 1, "f32")
+    need = L.logits_workspace_bytes(dtype, n, H, V)
+    L.logits_fwd(dtype, dev(X, dtype), dev(W, dtype), "f32", Z,
+                 torch.empty(need, device="cuda", dtype=torch.uint8) if need else None)
+    x, w = host(dev(X, dtype)), host(dev(W, dtype))
+    with np.errstate(all="ignore"):
+        want = (x[:, None] * w[None]).sum(2)
+        if dtype == "f32":
+            want[~np.isfinite(x).all(1)] = np.nan
+            want[:, ~np.isfinite(w).all(1)] = np.nan
+        want = want.astype(np.float32)
+    got = Z.cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(np.where(np.isinf(got), got, 0), np.where(np.isinf(want), want, 0))
+
+
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("pad", [0, 1, 8])
 def test_logits_and_their_readers_from_the_middle_of_a_sector(out, pad):
