@@ -424,7 +424,8 @@ struct bg_adjust {
 };
 typedef struct bg_adjust bg_adjust;
 
-/* out = the adjusted logits, rounded once to dtype.  out may be Z (with ldo = ldz). */
+/* out = the adjusted logits, rounded once to dtype.  out may be Z (with ldo = ldz); else no row of it may
+ * overlap one of Z (refused), though they may lie between each other's. */
 int bg_logits_adjust(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const void* Z,
                      const bg_adjust* adjust, int64_t ldo, void* out, void* stream);
 

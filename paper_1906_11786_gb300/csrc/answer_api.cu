@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 
 #include <cmath>
+#include <cstdlib>
 #include <string>
 
 #include "answer.h"
@@ -52,6 +53,24 @@ int check_h(int32_t H) {
 int check_stride(const char* name, int64_t ld, int32_t V) {
   return ld >= V && ld <= kMaxStride ? BG_OK
                                      : bg_fail(BG_EINVAL, std::string(name) + " must be in [V, 2^31]");
+}
+
+// Whether any of n rows of `width` bytes from a, lda bytes apart, shares a byte with one of those from b.
+bool rows_meet(const void* pa, int64_t lda, const void* pb, int64_t ldb, int64_t n, int64_t width) {
+  const int64_t a = (int64_t)(uintptr_t)pa, b = (int64_t)(uintptr_t)pb;
+  if (a + (n - 1) * lda + width <= b || b + (n - 1) * ldb + width <= a) return false;
+  if (lda == ldb) {  // rows i and j are b - a + (j - i) lda apart
+    const int64_t d = b - a, k = d / lda;
+    for (int64_t s = k - 1; s <= k + 1; ++s)
+      if (s > -n && s < n && std::abs(d - s * lda) < width) return true;
+    return false;
+  }
+  for (int64_t i = 0, j = 0; i < n && j < n;) {
+    const int64_t x = a + i * lda, y = b + j * ldb;
+    if (x < y + width && y < x + width) return true;
+    ++(x < y ? i : j);
+  }
+  return false;
 }
 
 // The adjustment as the launchers take it (an empty one for NULL).
@@ -119,6 +138,9 @@ extern "C" int bg_logits_adjust(bg_dtype dt, int64_t n, int32_t V, int64_t ldz, 
   if (n == 0) return BG_OK;
   ANS_PTR(Z); ANS_PTR(out);
   if (out == Z && ldo != ldz) return bg_fail(BG_EINVAL, "in place, ldo must be ldz");
+  const int64_t e = dt == BG_BF16 ? 2 : 4;
+  if (out != Z && rows_meet(Z, ldz * e, out, ldo * e, n, V * e))
+    return bg_fail(BG_EINVAL, "out overlaps Z and is not Z");
   int* status = nullptr;
   ANS_TRY(bg_status_word(&status));
   return cuda_rc(bg::logits_adjust(dt == BG_BF16, n, V, ldz, Z, adj, ldo, out, status, (cudaStream_t)stream),

@@ -95,6 +95,21 @@ def test_pointers_types_and_strides_are_checked(lib):
     _refused(lib.bg_logits_top(f, 8, 9, 9, A, None, 2, A, A, odd, None), "lse not 16-byte")
 
 
+def test_results_over_other_rows_of_the_logits_are_refused(lib):
+    """out is Z or has no element in common with it, whatever the distances between rows."""
+    def adjust(dt, n, V, ldz, out, ldo):
+        return lib.bg_logits_adjust(dt, n, V, ldz, A, None, ldo, out, None)
+
+    f, b = L.BG_F32, L.BG_BF16
+    for dt, e in ((f, 4), (b, 2)):
+        step = 16 // e  # elements of 16 bytes
+        for n, V, ldz, at, ldo in [(1, 100, 100, step, 100), (1, 100, 100, -step, 100), (8, 100, 104, 104, 104),
+                                   (8, 100, 104, -104, 104), (8, 100, 240, 96, 240), (8, 100, 240, 240 * 7 - 96, 240),
+                                   (8, 100, 240, 240 + 96, 240), (8, 100, 240, -96, 240), (8, 100, 200, 104, 208),
+                                   (8, 100, 104, -8 * 200 + 104, 200), (1 << 20, 8, 16, 8, 24), (3, 100, 100, 296, 1000)]:
+            _refused(adjust(dt, n, V, ldz, A + at * e, ldo), "out overlaps Z")
+
+
 @pytest.mark.parametrize("kw,word", [
     (dict(bias=A + 4), "bias not 16-byte"), (dict(mask=A), "n_masks must be 1"),
     (dict(mask=A, n_masks=-2), "n_masks must be 1"), (dict(mask=A, n_masks=7), "at least n"),

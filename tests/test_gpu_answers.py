@@ -266,6 +266,21 @@ def test_adjust_is_bit_exact(dtype, pad, parts):
         assert bool((buf[:, V:] == 7.0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_adjust_into_rows_that_lie_between_those_of_the_logits(dtype):
+    n, V = 40, 100
+    for ldz, at, ldo in ((240, 112, 240), (240, 240 * 3 + 112, 240), (240, -120, 240), (720, 112, 720), (240, 240 * n - 136, 304)):
+        low = -min(at, 0)
+        buf = torch.full((low + max(n * ldz, max(at, 0) + n * ldo),), 7.0, device="cuda", dtype=TD[dtype])
+        Z, out = buf.as_strided((n, V), (ldz, 1), low), buf.as_strided((n, V), (ldo, 1), low + at)
+        Z.copy_(dev(np.random.default_rng(1).standard_normal((n, V)), dtype))
+        z = host(Z)
+        kw, adjust = constraints(n, V, 2)
+        L.logits_adjust(dtype, Z, out, adjust)
+        assert np.array_equal(host(Z), z)
+        assert np.array_equal(bits(out), bits(torch.from_numpy(ref.adjusted(z, **kw)).to(TD[dtype]).cuda()))
+
+
 def test_adjust_of_values_that_are_not_finite():
     """A masked place is -inf whatever stood there; elsewhere infinities and NaN go the way of the formula."""
     n, V = 4, 1001
