@@ -205,19 +205,26 @@ SortPlan sort_plan(int64_t n, int V) {
 constexpr int kMaxPiece = 64, kRing = 8;
 struct SumPlan {
   int lanes, groups, piece;
+  int resident;  // blocks of an SM that the pieces are made for
   int64_t pieces, blocks;
   int smem;
 };
-SumPlan sum_plan(int64_t n, int H, int weighted = 0) {
+SumPlan sum_plan(int64_t n, int H, int weighted) {
   SumPlan p;
   p.lanes = H / 8 <= 4 ? 4 : H / 8 <= 8 ? 8 : H / 8 <= 16 ? 16 : 32;
   p.groups = 256 / p.lanes;
-  // pieces of at most kMaxPiece that fill the SMs (two or three blocks each) a whole number of times
-  const int most = p.groups * kMaxPiece * 8 + kRing * 8192 + 1024;
-  const int64_t slots = 152LL * std::min(3, 232448 / most) * p.groups;
-  const int64_t waves = std::max<int64_t>(1, (n + slots * kMaxPiece - 1) / (slots * kMaxPiece));
+  // pieces that fill the SMs a whole number of times: of at most kMaxPiece, or as long as leaves room for a third
+  // block of an SM where that takes little off (weighted sums of 64 < H <= 128: 56 of 64; planned for three blocks
+  // with pieces of 57 to 64, of which two fit, distillation's dW of 1.28 M entries over 2000 x 128 took 336 us, so 302)
+  const int entry = (2 + weighted) * 4 * p.groups, room = 232448 / 3 - kRing * 8192 - 1024;
+  const int third = std::min(kMaxPiece, room / entry & ~1);
+  const bool three = third >= kMaxPiece / 4 * 3;
+  const int longest = three ? third : kMaxPiece;
+  p.resident = three ? 3 : 2;
+  const int64_t slots = 152LL * p.resident * p.groups;
+  const int64_t waves = std::max<int64_t>(1, (n + slots * longest - 1) / (slots * longest));
   const int64_t piece = (n + slots * waves - 1) / (slots * waves);
-  p.piece = (int)std::min<int64_t>(kMaxPiece, std::max<int64_t>(8, (piece + 1) / 2 * 2));
+  p.piece = (int)std::min<int64_t>(longest, std::max<int64_t>(8, (piece + 1) / 2 * 2));
   p.pieces = (n + p.piece - 1) / p.piece;
   p.blocks = (p.pieces + p.groups - 1) / p.groups;
   p.smem = kRing * 8192 + ((2 + weighted) * p.groups * p.piece + 4) * 4;
@@ -248,7 +255,7 @@ struct SharedRows {
 struct BwdWs {
   size_t key[2], pos[2], hist, head, tail, total;
 };
-BwdWs bwd_ws(int64_t n, int H, int V) {
+BwdWs bwd_ws(int64_t n, int H, int V, int weighted) {
   const SortPlan s = sort_plan(n, V);
   BwdWs w;
   size_t o = 0;
@@ -257,7 +264,7 @@ BwdWs bwd_ws(int64_t n, int H, int V) {
     o += al(bytes);
     return at;
   };
-  const size_t pieces = (size_t)sum_plan(n, H).pieces;
+  const size_t pieces = (size_t)sum_plan(n, H, weighted).pieces;
   for (int i = 0; i < 2; ++i) {
     w.key[i] = take((size_t)n * 4);
     w.pos[i] = take((size_t)n * 4);
@@ -802,7 +809,7 @@ cudaError_t sum_by_token(int64_t n, int H, int V, const int32_t* ids, const Src&
   if (n == 0)
     return accumulate ? cudaSuccess : cudaMemsetAsync(dtable, 0, (size_t)V * H * sizeof(float), st);
   const SortPlan s = sort_plan(n, V);
-  const BwdWs w = bwd_ws(n, H, V);
+  const BwdWs w = bwd_ws(n, H, V, Src::kWeighted);
   char* base = static_cast<char*>(ws);
   int32_t* key[2] = {reinterpret_cast<int32_t*>(base + w.key[0]),
                      reinterpret_cast<int32_t*>(base + w.key[1])};
@@ -885,7 +892,7 @@ cudaError_t embed_fwd(int bf16, int64_t n, int H, int V, const int32_t* ids, con
   return cudaGetLastError();
 }
 
-size_t embed_bwd_ws_bytes(int64_t n, int H, int V) { return bwd_ws(n, H, V).total; }
+size_t embed_bwd_ws_bytes(int64_t n, int H, int V) { return bwd_ws(n, H, V, 0).total; }
 
 cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* dout, float scale,
                       const Drop& d, float* dtable, int accumulate, void* ws, int* status,
@@ -893,7 +900,13 @@ cudaError_t embed_bwd(int64_t n, int H, int V, const int32_t* ids, const float* 
   return sum_by_token(n, H, V, ids, GradRows{dout, d}, scale, dtable, accumulate, ws, status, st);
 }
 
-size_t token_sum_ws_bytes(int64_t n, int H, int V) { return bwd_ws(n, H, V).total; }
+size_t token_sum_ws_bytes(int64_t n, int H, int V) { return bwd_ws(n, H, V, 1).total; }
+
+int token_sum_resident(int64_t n, int H, int weighted, int* smem) {
+  const SumPlan p = sum_plan(n, H, weighted);
+  *smem = p.smem;
+  return p.resident;
+}
 
 cudaError_t token_sum(int64_t n, int H, int V, const int32_t* ids, int bf16, const void* X, int K,
                       const float* weight, float* dtable, int accumulate, void* ws, int* status,

@@ -36,6 +36,9 @@ cudaError_t token_sum(int64_t n, int H, int V, const int32_t* ids, int bf16, con
                       const float* weight, float* dtable, int accumulate, void* ws, int* status,
                       cudaStream_t st);
 
+// Blocks of an SM that the sum (embed_bwd's or the weighted one) cuts its rows for, and each one's shared memory.
+int token_sum_resident(int64_t n, int H, int weighted, int* smem);
+
 // Soft targets instead of one token a row (distill.cu): probabilities softmax(z / tau) without a target's
 // one, a row counts where `target` is 0 or more; loss = tau^2 (inner + lse), gradients times tau.
 struct XentSoft {

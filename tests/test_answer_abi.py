@@ -186,6 +186,18 @@ def test_workspaces_grow_with_the_operands_alone(lib):
         assert 0 < need < 6 * H * (n + V + 512) + 4096
 
 
+def test_sums_by_token_are_cut_for_as_many_blocks_as_an_sm_holds(lib):
+    """228 KB of shared memory an SM, of which each block takes 1 KB beside its own (256 bytes of them fixed)."""
+    resident = lib["_ZN2bg18token_sum_residentEliiPi"]
+    resident.argtypes = [ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_int)]
+    smem = ctypes.c_int()
+    for weighted in (0, 1):
+        for H in range(32, 257, 32):
+            for n in [1, 100, 10 ** 4, 311296, 311297, 450000, 466944, 466945, 933888, 1300000, 1 << 21, 1 << 29]:
+                blocks = resident(n, H, weighted, ctypes.byref(smem))
+                assert blocks >= 2 and blocks * (smem.value + 256 + 1024) <= 228 * 1024, (n, H, weighted)
+
+
 class _Elsewhere:
     """What the binding reads of a CUDA tensor, on a device of choice."""
 
