@@ -266,6 +266,37 @@ def test_adjust_is_bit_exact(dtype, pad, parts):
         assert bool((buf[:, V:] == 7.0).all())
 
 
+@pytest.mark.parametrize("n,V", [(37, 8191), (37, 8193), (37, 16385), (130, 20001), (700, 20001), (2500, 9001),
+                                 (33, 70001)])
+@pytest.mark.parametrize("dtype,pad", [("f32", 0), ("f32", 2), ("bf16", 0), ("bf16", 1), ("bf16", 2), ("bf16", 4)])
+@pytest.mark.parametrize("parts", ["all", "bias", "bias and mask", "bias and histories", "long histories"])
+def test_adjust_of_rows_over_several_runs_of_biases(parts, dtype, pad, n, V):
+    """Rows that begin anywhere in 16 bytes share runs of 8192 biases; histories follow in a launch of their own,
+    except in place, and long ones do the row again."""
+    rng = np.random.default_rng(n + V)
+    kw = {"bias": rng.standard_normal(V).astype(np.float32)}
+    if parts in ("all", "bias and mask"):
+        kw["allowed"], kw["mask_row"] = rng.random((3, V)) < 0.7, rng.integers(-1, 3, n)
+    if parts not in ("bias", "bias and mask"):
+        most = 40 if parts == "all" else 300
+        kw["history"] = [rng.integers(0, V, 1537 + i if parts == "long histories" and i % 31 == 5 else
+                                      rng.integers(0, most)) for i in range(n)]
+        for h in kw["history"][:3]:
+            h[:2] = (0, V - 1)[:len(h)]
+        kw["penalty"] = np.stack([1 + rng.random(n), rng.standard_normal(n), rng.random(n)], 1).astype(np.float32)
+    Z, buf = rows(n, V, pad, dtype, 7.0)
+    Z.copy_(3 * torch.randn(n, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(V)))
+    adjust = repeated(kw, 1)
+    want = torch.from_numpy(ref.adjusted(Z.float().cpu().numpy(), **kw)).to(TD[dtype]).cuda()
+    for other in (0, 1):  # of the same distance between rows, and of another
+        out, obuf = rows(n, V, pad + other, dtype, 9.0)
+        L.logits_adjust(dtype, Z, out, adjust)
+        L.check_device()
+        assert torch.equal(out, want) and bool((obuf[:, V:] == 9.0).all())
+    L.logits_adjust(dtype, Z, Z, adjust)
+    assert torch.equal(Z, want) and bool((buf[:, V:] == 7.0).all())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_adjust_into_rows_that_lie_between_those_of_the_logits(dtype):
     n, V = 40, 100
@@ -438,6 +469,135 @@ def test_top_of_rows_with_runs_of_nan(where, n, V, dtype, pad):
         check_top(Z, K, dtype, None, host(Z).astype(np.float32))
     kw, adjust = constraints(n, V, 7)
     check_top(Z, 32, dtype, adjust, ref.adjusted(host(Z), **kw))
+
+
+MANY = 609  # rows from which a block of 128 threads takes one (below, 512 threads, and clusters of blocks)
+
+
+def check_top_of_repeated_rows(Z, K, dtype, adjust, adjusted, times):
+    """check_top of rows that are those of `adjusted` over and over: the answer of each place is looked up."""
+    n, V = Z.shape
+    vals = torch.full((n, K), 5.0, device="cuda")
+    ids = torch.full((n, K), 77, device="cuda", dtype=torch.int32)
+    lse = torch.full((n,), 5.0, device="cuda")
+    L.logits_top(dtype, Z, vals, ids, lse, adjust)
+    L.check_device()
+    wv, wi, wl = ref.top(adjusted, K)
+    assert np.array_equal(ids.cpu().numpy(), np.tile(wi, (times, 1)))
+    assert np.array_equal(vals.cpu().numpy(), np.tile(wv, (times, 1)))
+    got, wl, some = host(lse), np.tile(wl, times), np.tile(np.isfinite(wl), times)
+    assert np.array_equal(got[~some], wl[~some], equal_nan=True)
+    if some.any():
+        within(got[some], wl[some], np.tile(lse_tolerance(adjusted, V), times)[some], "lse")
+    only = torch.full_like(ids, 77)
+    L.logits_top(dtype, Z, vals, only, None, adjust)
+    assert torch.equal(only, ids)
+
+
+def repeated(kw, times):
+    """`times` of the rows of an adjustment (answer_ref's names), as a LogitAdjust."""
+    own = {}
+    if "bias" in kw:
+        own["bias"] = dev(kw["bias"])
+    if "allowed" in kw:
+        own["mask"] = torch.from_numpy(ref.pack_mask(kw["allowed"])).cuda()
+        own["mask_row"] = ints(np.tile(kw["mask_row"], times))
+    if "history" in kw:
+        history = kw["history"] * times
+        off = np.concatenate([[0], np.cumsum([len(h) for h in history])])
+        own["history"] = ints(np.concatenate(history) if off[-1] else np.zeros(0))
+        own["history_off"], own["penalty"] = ints(off, np.int64), dev(np.tile(kw["penalty"], (times, 1)))
+    return L.LogitAdjust(**own)
+
+
+def test_many_rows_are_as_many_as_the_library_means():
+    import os
+    src = open(os.path.join(os.path.dirname(L.LIB_PATH), "csrc", "top.cu")).read()
+    assert f"if ((n << log_cl) <= {152} * {(MANY - 1) // 152})" in src and (MANY - 1) % 152 == 0
+
+
+@pytest.mark.parametrize("dtype,pad", [("f32", 0), ("f32", 1), ("bf16", 0), ("bf16", 3)])
+@pytest.mark.parametrize("K", [1, 5, 64, 128])
+def test_top_of_many_rows(K, dtype, pad):
+    for distinct, V in [(7, 1), (29, 31), (203, 129), (87, 2047), (29, 2048), (87, 2049), (29, 20001), (7, 49999)]:
+        times = -(-MANY // distinct)
+        rng = np.random.default_rng(V)
+        Z, _ = rows(distinct * times, V, pad, dtype)
+        one = dev(rng.standard_normal((distinct, V)) * 3, dtype)
+        Z.copy_(one.repeat(times, 1))
+        check_top_of_repeated_rows(Z, K, dtype, None, host(one).astype(np.float32), times)
+
+
+@pytest.mark.parametrize("parts", [dict(), dict(bias=False, masks=0), dict(bias=False, history=0),
+                                   dict(masks=0, history=0), dict(history=0), dict(bias=False, masks=1),
+                                   dict(masks=0)])
+@pytest.mark.parametrize("dtype,pad", [("f32", 0), ("f32", 2), ("bf16", 0), ("bf16", 1)])
+def test_top_of_many_adjusted_rows(dtype, pad, parts):
+    for distinct, V, K in [(7, 1, 2), (29, 33, 40), (203, 129, 16), (87, 8193, 128), (29, 20001, 16)]:
+        times = -(-MANY // distinct)
+        rng = np.random.default_rng(V)
+        Z, _ = rows(distinct * times, V, pad, dtype)
+        one = dev(rng.standard_normal((distinct, V)) * 3, dtype)
+        Z.copy_(one.repeat(times, 1))
+        kw, _ = constraints(distinct, V, V, **parts)
+        check_top_of_repeated_rows(Z, K, dtype, repeated(kw, times), ref.adjusted(host(one), **kw), times)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["constant", "rising", "falling", "two values", "steps", "zeros of both signs",
+                                  "one answer", "none", "not finite"])
+def test_top_of_many_rows_made_to_be_hard(kind, dtype):
+    """As for few rows; a block of 128 threads copies up to 128 candidates when its room is full."""
+    V, v = 20003, np.arange(20003)
+    z = {"constant": np.full(V, 1.5), "rising": v / 64.0, "falling": -v / 64.0,
+         "two values": np.where(v % 3 == 0, 2.0, 1.0), "steps": (v // 500) * 0.5,
+         "zeros of both signs": np.where(v % 2 == 0, -0.0, 0.0), "one answer": np.where(v == 12345, -3e30, -np.inf),
+         "none": np.full(V, -np.inf),
+         "not finite": np.where(v % 1000 == 7, np.inf, np.where(v % 1000 == 8, np.nan, -v))}[kind]
+    one = dev(z[None], dtype)
+    Z = one.repeat(MANY, 1)
+    for K in (1, 100, 127, 128):
+        check_top_of_repeated_rows(Z, K, dtype, None, host(one).astype(np.float32), MANY)
+
+
+@pytest.mark.parametrize("size", [1, 128, 129, 768, 769, 1024, 1536, 1537, 3000])
+def test_histories_of_every_size_of_many_rows(size):
+    distinct, times, V = 29, 21, 9001
+    rng = np.random.default_rng(size)
+    one = dev(rng.standard_normal((distinct, V)) * 2)
+    kw = dict(history=[rng.integers(0, V if i % 2 else 40, size if i % 7 else size // 2) for i in range(distinct)],
+              penalty=np.stack([1 + rng.random(distinct), rng.random(distinct), rng.random(distinct) / 50],
+                               1).astype(np.float32))
+    want, adjust, Z = ref.adjusted(host(one), **kw), repeated(kw, times), one.repeat(times, 1)
+    for K in (20, 128):
+        check_top_of_repeated_rows(Z, K, "f32", adjust, want, times)
+    L.logits_adjust("f32", Z, Z, adjust)
+    assert np.array_equal(bits(Z), np.tile(bits(torch.from_numpy(want).cuda()), (times, 1)))
+
+
+def test_one_long_history_among_short_ones():
+    """The table is sized by the average: the row whose history outgrows it goes its own way."""
+    distinct, times, V = 29, 21, 9001
+    rng = np.random.default_rng(8)
+    one = dev(rng.standard_normal((distinct, V)) * 2, "bf16")
+    kw = dict(history=[rng.integers(0, V, 4000 if i == 11 else 900 if i == 20 else 30) for i in range(distinct)],
+              penalty=np.tile(np.array([[1.5, -2.0, 0.1]], np.float32), (distinct, 1)))
+    want = ref.adjusted(host(one), **kw)
+    check_top_of_repeated_rows(one.repeat(times, 1), 33, "bf16", repeated(kw, times), want, times)
+
+
+@pytest.mark.parametrize("dtype,pad", [("f32", 0), ("bf16", 1), ("bf16", 7)])
+def test_many_rows_longer_than_their_bits_in_shared_memory(dtype, pad):
+    distinct, times, V = 7, 88, 140001
+    rng = np.random.default_rng(2)
+    one = dev(rng.standard_normal((distinct, V)), dtype)
+    Z, _ = rows(distinct * times, V, pad, dtype)
+    Z.copy_(one.repeat(times, 1))
+    kw = dict(allowed=rng.random((2, V)) < 0.9, mask_row=rng.integers(-1, 2, distinct),
+              history=[np.concatenate([rng.integers(0, V, rng.integers(0, 300)), np.arange(65526, 65546)])
+                       for _ in range(distinct)],
+              penalty=np.tile(np.array([[0.01, -3.0, -1.0]], np.float32), (distinct, 1)))
+    check_top_of_repeated_rows(Z, 33, dtype, repeated(kw, times), ref.adjusted(host(one), **kw), times)
 
 
 def test_top_from_rows_beyond_32_bit_offsets():
