@@ -417,7 +417,8 @@ __global__ void __launch_bounds__(kThreads)
 
 // The same with biases where rows begin anywhere in 16 bytes: rows `step` apart begin at the same place, and kShare of
 // them share a run of kRun biases, laid out in shared memory as their groups lie.  (Read one by one, a warp's biases
-// are 16 or 32 bytes apart.  8192 x 49999 bf16 with biases: 1142 us in groups of 4 bytes, 343 shared.)
+// are 16 bytes apart, 32 in bf16.)  Laying them out is worth it for many long bf16 rows at odd places alone: see
+// shares_biases.
 constexpr int kRun = 8192, kShare = 8;
 template <typename T, int F>
 __global__ void __launch_bounds__(kThreads)
@@ -1113,6 +1114,14 @@ __global__ void __launch_bounds__(NT, (NT > 128 ? 2 : !(F & kBias) ? 8 : sizeof(
 }
 
 // ------------------------------------------------------------------------------ host
+// Whether n bf16 rows with biases, each of which begins `lead` elements further on in a group than the one before,
+// share them.  8192 x 49999 takes 355 us shared and 390 with the biases read one by one (masks too 370 and 414,
+// histories too 498 and 523), 8192 x 32769 242 and 263; but 1024 x 20001 38 and 27, 32 x 49999 21 and 11, rows 4
+// elements further on each (8192 x 50004) 355 and 324, and fp32 (8192 x 49999) 699 and 533.
+bool shares_biases(int64_t n, int V, int lead) {
+  return lead % 2 && V >= 4 * kRun && n * V >= (int64_t)1 << 27;
+}
+
 template <typename T, int F>
 cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int64_t ldo, void* out,
                        int* status, cudaStream_t st) {
@@ -1122,19 +1131,20 @@ cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjus
   const int64_t groups = ((int64_t)V + 2 * G - 2) / G;
   const int lead = (int)(ldz % G);  // rows begin so much further on than the one before
   int tokens = 0;
-  // (in place, the tokens' logits would be gone after the first launch)
-  if ((F & kBias) && lead && n >= 4 * kShare && !((F & kHistory) && out == Z)) {
-    constexpr int D = F & ~kHistory;
-    int step = 1;
-    while (lead * step % G) step *= 2;
-    const int64_t sets = (n + step * kShare - 1) / (step * kShare) * step;
-    const cudaError_t e =
-        launch_pdl(k_adjust_shared<T, D>, dim3((unsigned)sets, (unsigned)((groups * G + kRun - 1) / kRun)),
-                   dim3(kThreads), kRun * 4, st, n, V, ldz, z, adj, ldo, o, step, status);
-    if (e != cudaSuccess) return e;
-    note_launch();
-    if (!(F & kHistory)) return e;
-    tokens = 1;
+  if constexpr (sizeof(T) == 2 && (F & kBias) != 0) {
+    // (in place, the tokens' logits would be gone after the first launch)
+    if (shares_biases(n, V, lead) && !((F & kHistory) && out == Z)) {
+      constexpr int D = F & ~kHistory;
+      constexpr int step = G;  // (an odd lead)
+      const int64_t sets = (n + step * kShare - 1) / (step * kShare) * step;
+      const cudaError_t e =
+          launch_pdl(k_adjust_shared<T, D>, dim3((unsigned)sets, (unsigned)((groups * G + kRun - 1) / kRun)),
+                     dim3(kThreads), kRun * 4, st, n, V, ldz, z, adj, ldo, o, step, status);
+      if (e != cudaSuccess) return e;
+      note_launch();
+      if (!(F & kHistory)) return e;
+      tokens = 1;
+    }
   }
   // runs of 8192 elements; with histories, which are read for each run, longer ones where there are blocks enough, and
   // shorter ones where there are few

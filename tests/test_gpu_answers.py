@@ -297,6 +297,36 @@ def test_adjust_of_rows_over_several_runs_of_biases(parts, dtype, pad, n, V):
     assert torch.equal(Z, want) and bool((buf[:, V:] == 7.0).all())
 
 
+@pytest.mark.parametrize("V,pad", [(32769, 0), (40001, 2), (49999, 0)])
+@pytest.mark.parametrize("parts", ["bias", "bias and mask", "all", "long histories"])
+def test_adjust_of_many_long_rows_at_odd_places(parts, V, pad):
+    """bf16 rows from 2^27 elements on share their biases; the same rows again and again begin at every place."""
+    distinct, times = 41, 103
+    assert V >= 32768 and distinct * times * V >= 1 << 27 and (V + pad) % 2
+    rng = np.random.default_rng(V)
+    kw = {"bias": rng.standard_normal(V).astype(np.float32)}
+    if parts in ("all", "bias and mask"):
+        kw["allowed"], kw["mask_row"] = rng.random((3, V)) < 0.7, rng.integers(-1, 3, distinct)
+    if parts in ("all", "long histories"):
+        kw["history"] = [np.concatenate([[0, V - 1, 8191, 8192], rng.integers(0, V, 1533 + i if parts != "all" and i % 9 == 5
+                                                                              else rng.integers(0, 300))])
+                         for i in range(distinct)]
+        kw["penalty"] = np.stack([1 + rng.random(distinct), rng.standard_normal(distinct), rng.random(distinct)],
+                                 1).astype(np.float32)
+    one = dev(rng.standard_normal((distinct, V)) * 3, "bf16")
+    Z, buf = rows(distinct * times, V, pad, "bf16", 7.0)
+    Z.copy_(one.repeat(times, 1))
+    adjust = repeated(kw, times)
+    want = torch.from_numpy(ref.adjusted(host(one), **kw)).to(torch.bfloat16).cuda().repeat(times, 1)
+    for other in (0, 1):
+        out, obuf = rows(distinct * times, V, pad + other, "bf16", 9.0)
+        L.logits_adjust("bf16", Z, out, adjust)
+        L.check_device()
+        assert torch.equal(out, want) and bool((obuf[:, V:] == 9.0).all())
+    L.logits_adjust("bf16", Z, Z, adjust)
+    assert torch.equal(Z, want) and bool((buf[:, V:] == 7.0).all())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_adjust_into_rows_that_lie_between_those_of_the_logits(dtype):
     n, V = 40, 100
