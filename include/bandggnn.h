@@ -396,7 +396,8 @@ int bg_xent_bwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, 
  * enter as they are; fp32 ones of more than 4 rows with 22 bits, down to 2^-17 of the largest magnitude in their
  * row, smaller elements are off by up to 2^-39 of that magnitude.  A row of X or W with an element that is infinite or
  * NaN makes its own logits not finite and no others: NaN with fp32 X and W, what their products and sum are with bf16
- * ones (an infinite element may make them infinite).  ws may be NULL where bg_logits_workspace_bytes is 0 (bf16, and up to 4 rows). */
+ * ones (an infinite element may make them infinite).  ws may be NULL where bg_logits_workspace_bytes is 0 (bf16, and
+ * up to 4 rows). */
 size_t bg_logits_workspace_bytes(bg_dtype dtype, int64_t n, int32_t H, int32_t V);
 int bg_logits_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X, const void* W,
                   bg_dtype out_dtype, int64_t ldz, void* Z, void* ws, size_t ws_bytes, void* stream);
@@ -409,7 +410,9 @@ int bg_logits_fwd(bg_dtype dtype, int64_t n, int32_t H, int32_t V, const void* X
  *   z1 where bit v % 32 of word v / 32 of the row's mask is set, -inf (whatever z1 is) where it is not.
  * Device pointers.  Tokens of a history below 0 are skipped; those of V or more too, and they are reported by
  * bg_check_device as BG_EDEVICE (site 132).  A row whose mask number is n_masks or more has no mask (reported,
- * site 133), one whose offsets fall or leave the history has none (site 134). */
+ * site 133), one whose offsets fall or leave the history has none (site 134).  Histories may have any length;
+ * from 1537 tokens on (769 where the average is 256 or less) and with V of 2^21 or more they take a slower way,
+ * a row of bg_logits_top four to ten times as long. */
 struct bg_adjust {
   const float* bias;          /* [V] or NULL */
   const uint32_t* mask;       /* [n_masks][ceil(V / 32)] or NULL */
@@ -425,7 +428,8 @@ struct bg_adjust {
 typedef struct bg_adjust bg_adjust;
 
 /* out = the adjusted logits, rounded once to dtype.  out may be Z (with ldo = ldz); else no row of it may
- * overlap one of Z (refused), though they may lie between each other's. */
+ * overlap one of Z (refused), though they may lie between each other's.  bf16 rows of out that begin at
+ * another place in 16 bytes than Z's take up to four times as long. */
 int bg_logits_adjust(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const void* Z,
                      const bg_adjust* adjust, int64_t ldo, void* out, void* stream);
 
@@ -433,7 +437,8 @@ int bg_logits_adjust(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const vo
  * tokens (0 and -0 are equal), and the log-sum-exp of all of them: top_logit [n, K] fp32, top_id [n, K], lse
  * [n] or NULL.  adjust may be NULL.  Logits that are -inf or NaN are not answers: places past the last
  * answer have top_id -1 and top_logit -inf (a row whose mask leaves nothing: all of them, and lse -inf).
- * lse is NaN where a logit is NaN, +inf or 2^127 or more; logits below -2^127 count as -inf in it. */
+ * lse is NaN where a logit is NaN, +inf or 2^127 or more; logits below -2^127 count as -inf in it.  All three
+ * are the same bits in every run. */
 int bg_logits_top(bg_dtype dtype, int64_t n, int32_t V, int64_t ldz, const void* Z, const bg_adjust* adjust,
                   int32_t K, float* top_logit, int32_t* top_id, float* lse, void* stream);
 

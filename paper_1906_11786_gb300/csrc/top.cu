@@ -11,14 +11,17 @@
 // Rows are read once, as the aligned 16-byte groups that cover them: a row may begin anywhere in a group
 // (odd row lengths), so column c of a row is element c + a of its groups, a its first element's place in the
 // first one.  The tokens of a history are counted in a hash table in shared memory (long ones by element, a few
-// thousand elements at a time, the history read once for each such segment): no sorting and no workspace.
+// thousand elements at a time, the history read once for each such segment, and slow: see hashed): no sorting and no
+// workspace.
 //
 // Measured (GB300; reading at the copy rate of 6.77 TB/s is the floor, beside the writing of the adjustment):
-//   adjustment of 8192 x 50000 bf16: 260 us (floor 243, 6.3 TB/s); biases 271, masks 285, histories of 0 to 512 tokens
-//     345, all three 444; with rows of 49999, which begin anywhere, 264, 340, 288, 347 and 470.  fp32: 506 (6.5 TB/s),
-//     508, 516, 603, 676.  What histories add is scattered: a sector read and one written in part for each token.
-//   top 32 of 16383 x 50000 bf16: 370 us (floor 243), biases 458, masks 455, histories 527, all three 729; fp32 536
-//     (6.1 TB/s; floor 485), 604, 572, 704, 879; top 1 305, top 128 675.  bf16 rows are bound by instructions and by
+//   adjustment of 8192 x 50000 bf16: 259 us (floor 243, 6.3 TB/s); biases 271, masks 285, histories of 0 to 512 tokens
+//     347, all three (of 0 to 1024) 448; with rows of 49999, which begin anywhere, 263, 335, 288, 348 and 472.  fp32: 505
+//     (6.5 TB/s), 507, 515, 599, 675; rows of 49999 513, 516, 524, 610, 696.  In place within 9% of that, and less
+//     where histories alone are asked for (bf16 130).  What histories add is scattered: a sector read and one written
+//     in part for each token.
+//   top 32 of 16383 x 50000 bf16: 371 us (floor 243), biases 459, masks 456, histories 526, all three 711; fp32 541
+//     (6.1 TB/s; floor 485), 603, 573, 675, 875; top 1 306, top 128 678.  bf16 rows are bound by instructions and by
 //     the latency of what comes one after the other in a row (issue slots 64%, fp32's unpacked rows hide it): 80
 //     instructions a warp for 512 logits, 44 for the sum of exponentials, 37 for the biases, 55 for the bits.
 #include <cuda_bf16.h>
@@ -231,7 +234,9 @@ struct Hash {
   __device__ uint32_t count(uint32_t x) const { return x >> low; }
 };
 // Whether a history goes there: it leaves a quarter of the slots free, and its length fits beside a token.  Longer
-// ones are counted, as many elements at a time as there are slots.
+// ones are counted, as many elements at a time as there are slots.  That is the slow way: top 32 of 16383 x 49999 bf16
+// with 1536 tokens a row 1110 us, with 1537 4920, with 4096 7060 (adjustment in place 580, 1250, 2070); one row of 2000
+// among rows of 256 740 (572 without it); 300 rows of 1536 45 us, of 1537 270; one row of 256 19 us, of 4096 83.
 template <typename R>
 __device__ __forceinline__ bool hashed(const R& r, int slots) {
   return r.hist_n <= slots / 4 * 3 && r.V < 1 << 21;
@@ -337,6 +342,8 @@ template <typename T, int F>
 __device__ __forceinline__ void adjust_run(const Row<T>& r, T* o, bool in_place, bool tokens, int64_t g0, int64_t g1,
                                            const float* staged, uint32_t* table, float* raw, int* status) {
   constexpr int G = Row<T>::G;
+  // (rows of out at another place in 16 bytes than Z's are stored one by one: 8192 x 49999 into rows of 50000, bf16 970 us
+  // instead of 268, fp32 534 instead of 518)
   const bool vec = (reinterpret_cast<uintptr_t>(o - r.a) & 15) == 0;
   // (short runs, of a few rows: occurrences by element are the shorter way)
   constexpr int SG = kSlots / G;
@@ -460,7 +467,7 @@ __global__ void __launch_bounds__(kThreads)
 // the first chunk.  Then the pieces noted, some 150 of 3100 for 49999 logits and K = 32, are read again, and their
 // logits that reach the last bound, some 60, become candidates.  (Candidates taken as they were met, by the bound
 // of the time, were a third of the kernel's instructions.)  Where pieces or candidates outgrow their room (ties
-// without end, rows that rise), the block goes over the row again with exact bounds (rising_row, some times
+// without end, rows that rise), the block goes over the row again with exact bounds (rising_row, four to ten times
 // slower).
 //
 // A block is a row's, of 128 threads where there are rows enough, eight blocks an SM: what one waits for (the
@@ -1147,7 +1154,8 @@ cudaError_t run_adjust(int64_t n, int V, int64_t ldz, const void* Z, const Adjus
     }
   }
   // runs of 8192 elements; with histories, which are read for each run, longer ones where there are blocks enough, and
-  // shorter ones where there are few
+  // shorter ones where there are few (49999 elements and 256 tokens a row, short and 8192: fp32 50 rows 5.6 and 8.4 us,
+  // 100 8.7 and 11.5, 200 17 and 14; bf16 50 5.7 and 5.7, 100 8.3 and 7.3)
   int64_t per = 8192 / G;
   if ((F & kHistory) && n * V <= 152 * 8 * kSlots) per = kSlots / G;
   while ((F & kHistory) && per * G < 65536 && n * ((groups + 2 * per - 1) / (2 * per)) >= 152 * 16) per *= 2;
@@ -1195,7 +1203,9 @@ template <typename T, int F>
 cudaError_t run_top(int64_t n, int V, int64_t ldz, const void* Z, const Adjust& adj, int K, float* top_logit,
                     int32_t* top_id, float* lse, int* status, cudaStream_t st) {
   const int log_cl = cluster_of(n, V);
-  // Many rows: small blocks, so that one's latencies are another's work.  Few: a row's own work in one go.
+  // Many rows: small blocks, so that one's latencies are another's work.  Few: a row's own work in one go.  (Top 32 of
+  // 49999, 512 and 128 threads: bf16 456 rows 25 and 29 us, 608 28 and 26, 912 39 and 36; fp32 305 22 and 29, 608 32 and
+  // 33, 912 47 and 41.  With biases and histories 128 would be ahead sooner: 305 rows 39 and 38, fp32 48 and 38.)
   if ((n << log_cl) <= 152 * 4)
     return launch_top<512, T, F>(n, V, ldz, Z, adj, K, log_cl, top_logit, top_id, lse, status, st);
   return launch_top<128, T, F>(n, V, ldz, Z, adj, K, log_cl, top_logit, top_id, lse, status, st);
